@@ -390,6 +390,43 @@ int sol_attn3d_sparse_selection(sol_attn3d_plan_t plan, const void* sparse_ws, i
                                 int* kv_blocks, int capacity, int* count);
 
 /*
+ * Differential attention: the dense attention of Section 3.2 ("SDPA") in the form of a block whose heads come in pairs
+ * (the paper's DiT uses plain softmax attention; this is the same step for a model trained with the difference of two
+ * softmax maps).  The plan has head_dim 64 and an even number of heads; heads 2i and 2i+1 are pair i, and the pair's two
+ * V rows side by side are one value of 128 dims:
+ *     x   = softmax(q~_2i k~_2i^T / 8) [v_2i | v_2i+1]  -  lambda * softmax(q~_2i+1 k~_2i+1^T / 8) [v_2i | v_2i+1]
+ *     lambda = exp(lambda_q1 . lambda_k1) - exp(lambda_q2 . lambda_k2) + lambda_init
+ *     out = (1 - lambda_init) * x / sqrt(mean over 128 of x^2 + eps) * gain         (gain == NULL: out = x)
+ * with q~, k~ rotated per head as in sol_attn3d_forward; the 128 values of out go to heads 2i and 2i+1.
+ *   lambda_*            DEVICE pointers, fp32, 4-byte aligned: 64 values each, pair i's at i * lambda_pair_stride elements
+ *                       (0: one set for all pairs; otherwise at least 64).
+ *   gain                DEVICE pointer, 128 fp32, 16-byte aligned, shared by the pairs, or NULL.
+ *   lambda_init, eps    finite; eps >= 0.
+ * The struct is read during the call, the arrays when the kernel runs.
+ */
+typedef struct {
+  uint32_t size;                /* sizeof(sol_attn3d_diff_weights) */
+  float lambda_init;
+  const float* lambda_q1;
+  const float* lambda_k1;
+  const float* lambda_q2;
+  const float* lambda_k2;
+  int64_t lambda_pair_stride;
+  const float* gain;
+  float eps;
+} sol_attn3d_diff_weights;
+
+/*
+ * Arguments as for sol_attn3d_forward (strides of the plan included); query_mask may be NULL (every row) or as for
+ * sol_attn3d_forward_rect.  Rows of a sequence without a valid key are zeros.  K and V values at masked positions must be
+ * finite.  Deterministic; may be captured.  Always runs on CTA pairs (SOL_ATTN3D_PAIR does not apply).
+ * Errors: as for sol_attn3d_forward, UNSUPPORTED_SHAPE for head_dim 128 or an odd number of heads, INVALID_ARG for weights.
+ */
+int sol_attn3d_forward_diff(sol_attn3d_plan_t plan, const void* q, const void* k, const void* v, void* out,
+                            const uint8_t* key_mask, const uint8_t* query_mask, const sol_attn3d_diff_weights* weights,
+                            sol_attn3d_stream_t stream);
+
+/*
  * sol_attn3d_forward for callers that must not allocate device memory.  (The paper has no counterpart:
  * this is a deployment variant of the call above, not a step of the method.)
  *
@@ -401,9 +438,9 @@ int sol_attn3d_sparse_selection(sol_attn3d_plan_t plan, const void* sparse_ws, i
  * array built into the library image, so the caller passes only inputs and outputs.  Every GPU context
  * that loads the library holds those 32 MiB until the process ends, whether this function is used or not.
  *
- *   plan           any plan with sol_attn3d_workspace_bytes(plan) <= 32 MiB (33,554,432 bytes); larger
- *                  plans are refused with SOL_ATTN3D_ERR_SCRATCH_LIMIT before anything is enqueued.
- *                  No workspace needs to be bound.
+ *   plan           any plan with sol_attn3d_workspace_bytes(plan) <= 32 MiB (33,554,432 bytes; the few bytes that
+ *                  only sol_attn3d_forward_diff uses do not count); larger plans are refused with
+ *                  SOL_ATTN3D_ERR_SCRATCH_LIMIT before anything is enqueued.  No workspace needs to be bound.
  *   q, k, v, out, key_mask, stream   exactly as for sol_attn3d_forward.
  *   device_status  optional DEVICE pointer to one 4-byte word (4-byte aligned) that receives the status
  *                  word of this call: zeroed on `stream` first, nonzero after the stream has drained if

@@ -42,6 +42,20 @@ class sol_attn3d_desc(ctypes.Structure):
     ]
 
 
+class _DiffWeights(ctypes.Structure):
+    _fields_ = [
+        ("size", ctypes.c_uint32),
+        ("lambda_init", ctypes.c_float),
+        ("lambda_q1", ctypes.c_void_p),
+        ("lambda_k1", ctypes.c_void_p),
+        ("lambda_q2", ctypes.c_void_p),
+        ("lambda_k2", ctypes.c_void_p),
+        ("lambda_pair_stride", ctypes.c_int64),
+        ("gain", ctypes.c_void_p),
+        ("eps", ctypes.c_float),
+    ]
+
+
 # error codes (mirror include/sol_attn3d.h)
 OK = 0
 ERR_INVALID_ARG = -1
@@ -124,6 +138,8 @@ def _lib():
     lib.sol_attn3d_sparse_stats.restype = i32
     lib.sol_attn3d_sparse_selection.argtypes = [vp, vp, i32, i32, i32, ctypes.POINTER(i32), i32, ctypes.POINTER(i32)]
     lib.sol_attn3d_sparse_selection.restype = i32
+    lib.sol_attn3d_forward_diff.argtypes = [vp, vp, vp, vp, vp, vp, vp, ctypes.POINTER(_DiffWeights), vp]
+    lib.sol_attn3d_forward_diff.restype = i32
     lib.sol_attn3d_rope_qk.argtypes = [vp, vp, vp, vp, vp, vp]
     lib.sol_attn3d_rope_qk.restype = i32
     lib.sol_attn3d_status.argtypes = [vp]
@@ -475,6 +491,45 @@ def sol_attn3d_forward_qknorm(plan, q, k, v, out, key_mask, q_gain: torch.Tensor
 def sol_attn3d_qknorm_rope(plan, q, k, q_gain, k_gain, eps: float, q_out, k_out, stream=None) -> None:
     _check(_lib().sol_attn3d_qknorm_rope(plan, _ptr(q), _ptr(k), _ptr(q_gain), _ptr(k_gain), ctypes.c_float(eps),
                                          _ptr(q_out), _ptr(k_out), _stream(stream)), "sol_attn3d_qknorm_rope")
+
+
+class sol_attn3d_diff_weights:
+    """Learned weights of the differential attention: keeps the tensors alive and marshals them.
+
+    lambda_*: contiguous CUDA fp32, [64] (shared by the head pairs) or [pairs, 64]; gain: [128] or None (no norm)."""
+
+    def __init__(self, lambda_q1, lambda_k1, lambda_q2, lambda_k2, lambda_init: float, gain: Optional[torch.Tensor] = None,
+                 eps: float = 1e-5):
+        vecs = (lambda_q1, lambda_k1, lambda_q2, lambda_k2)
+        for t in vecs:
+            if not t.is_cuda or t.dtype != torch.float32 or not t.is_contiguous() or t.shape != lambda_q1.shape or \
+                    t.dim() not in (1, 2) or t.shape[-1] != 64:
+                raise ValueError("lambda vectors must be contiguous CUDA float32 tensors of one shape, [64] or [pairs, 64]")
+        if gain is not None and (not gain.is_cuda or gain.dtype != torch.float32 or not gain.is_contiguous() or gain.numel() != 128):
+            raise ValueError("gain must be a contiguous CUDA float32 tensor of 128 elements")
+        self.tensors = vecs + (gain,)
+        self.pairs = lambda_q1.shape[0] if lambda_q1.dim() == 2 else None
+        self.struct = _DiffWeights(ctypes.sizeof(_DiffWeights), lambda_init, *(t.data_ptr() for t in vecs),
+                                   64 if self.pairs is not None else 0, None if gain is None else gain.data_ptr(), eps)
+
+
+def _check_pairs(weights: sol_attn3d_diff_weights, heads: int) -> None:
+    if weights.pairs is not None and weights.pairs != heads // 2:
+        raise ValueError("one set of lambda vectors, or one per head pair")
+
+
+def sol_attn3d_forward_diff(plan, q, k, v, out, key_mask, weights: sol_attn3d_diff_weights,
+                            query_mask: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Differential attention over a plan with head_dim 64: heads 2i, 2i+1 are two softmax maps over one 128-dim value."""
+    for t in (q, k, v, out):
+        if not t.is_cuda or t.dtype != torch.bfloat16:
+            raise ValueError("q, k, v, out must be CUDA bf16 tensors")
+    for m, name in ((key_mask, "key_mask"), (query_mask, "query_mask")):
+        if m is not None and (not m.is_cuda or m.dtype != torch.uint8 or not m.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous CUDA uint8 tensor")
+    _check_pairs(weights, q.shape[-2])
+    _check(_lib().sol_attn3d_forward_diff(plan, _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(key_mask), _ptr(query_mask),
+                                          ctypes.byref(weights.struct), _stream(stream)), "sol_attn3d_forward_diff")
 
 
 def sol_attn3d_rope_qk(plan, q, k, q_rot, k_rot, stream=None) -> None:

@@ -81,6 +81,27 @@ __device__ __forceinline__ uint8_t* out_row_ptr(const AttnParams& p, long long t
          ((tok - p.sink.tok_begin[g]) * p.o_tok_stride + (long long)head * p.o_head_stride) * elem_bytes;
 }
 
+// Writes a warp's 32 staged rows (16-byte chunks XOR-swizzled by row) to global memory, one chunk per lane.
+template <int kRowBytes>
+__device__ __forceinline__ void write_staged_rows(const AttnParams& p, const SeqDev& sq, int head, int first_row, int lane,
+                                                  int elem_bytes, const uint8_t* stage) {
+  constexpr int kLanesPerRow = kRowBytes / 16;
+  __syncwarp();
+  const uint64_t pol_once = l2_policy_evict_first();            // output rows are written once, never read here
+  const int ch = lane % kLanesPerRow;
+#pragma unroll 4
+  for (int r0 = 0; r0 < 32; r0 += 32 / kLanesPerRow) {
+    const int rr = r0 + lane / kLanesPerRow;
+    const int qrow = first_row + rr;
+    bool store = qrow < sq.n_tokens;
+    if (store && p.query_mask != nullptr) store = p.query_mask[sq.tok_start + qrow] != 0;
+    SOL_DEVICE_CHECK(p.status, !store || (sq.tok_start + qrow >= 0 && sq.tok_start + qrow < p.sink.tok_begin[p.sink.n_dst]),
+                     kCheckOutputRow);
+    const uint4 w = *reinterpret_cast<const uint4*>(stage + rr * kRowBytes + ((ch ^ (rr & (kLanesPerRow - 1))) << 4));
+    if (store) st_global_evict_first(out_row_ptr(p, sq.tok_start + qrow, head, elem_bytes) + ch * 16, w, pol_once);
+  }
+}
+
 // Epilogue of one warp: its 32 accumulator rows O * inv -> bf16 (or raw E4M3 bytes) -> staged in the part of
 // the query tile's shared memory that belongs to those rows (every MMA that read it has completed; 16-byte
 // chunks XOR-swizzled by row) -> written out with one 16-byte chunk per lane, so every store instruction
@@ -123,20 +144,7 @@ __device__ __forceinline__ void store_rows(const AttnParams& p, const SeqDev& sq
       }
     }
   }
-  __syncwarp();
-  const uint64_t pol_once = l2_policy_evict_first();            // output rows are written once, never read here
-  const int ch = lane % kLanesPerRow;
-#pragma unroll 4
-  for (int r0 = 0; r0 < 32; r0 += 32 / kLanesPerRow) {
-    const int rr = r0 + lane / kLanesPerRow;
-    const int qrow = first_row + rr;
-    bool store = qrow < sq.n_tokens;
-    if (store && p.query_mask != nullptr) store = p.query_mask[sq.tok_start + qrow] != 0;
-    SOL_DEVICE_CHECK(p.status, !store || (sq.tok_start + qrow >= 0 && sq.tok_start + qrow < p.sink.tok_begin[p.sink.n_dst]),
-                     kCheckOutputRow);
-    const uint4 w = *reinterpret_cast<const uint4*>(stage + rr * kRowBytes + ((ch ^ (rr & (kLanesPerRow - 1))) << 4));
-    if (store) st_global_evict_first(out_row_ptr(p, sq.tok_start + qrow, head, kFp8 ? 1 : 2) + ch * 16, w, pol_once);
-  }
+  write_staged_rows<kRowBytes>(p, sq, head, first_row, lane, kFp8 ? 1 : 2, stage);
 }
 
 // Epilogue in the block-INT8 wire format of the exchange (Section 3.2, "Quantized communication"): the thread that owns
@@ -200,30 +208,116 @@ __device__ __forceinline__ void softmax_half(const uint32_t (&r)[64], float c, f
   }
 }
 
-template <int D, int kCtas = 1>
+template <int D, int kCtas = 1, bool kDiff = false>
 struct AttnSmem {
   static constexpr int kTile = 128 * D * 2;               // bytes of one 128 x D bf16 tile
   static constexpr int kHalves = D / 64;                  // 64-column (128-byte) swizzle boxes per row
   static constexpr int kHalfBytes = 128 * 128;            // one box: 128 rows x 128 bytes
   static constexpr int kStageBytes = kTile / kCtas;       // what one CTA holds of a K or V tile
   static constexpr int kKBoxBytes = kHalfBytes / kCtas;   // one K box: (128 / kCtas) keys x 128 bytes
-  static constexpr int kStages = ((D == 128) ? 5 : 10) * (kCtas == 2 ? 8 : 5) / 5;   // K/V ring (K and V tiles alternate)
+  // K/V ring (K and V tiles alternate); differential attention has one Q tile instead of two: its bytes go to the ring
+  static constexpr int kStages = kDiff ? 10 : ((D == 128) ? 5 : 10) * (kCtas == 2 ? 8 : 5) / 5;
   static constexpr int kOffQ = 0;
-  static constexpr int kOffKV = 2 * kTile;
+  static constexpr int kOffKV = (kDiff ? 1 : 2) * kTile;
   static constexpr int kOffBars = kOffKV + kStages * kStageBytes;
   static constexpr int kNumBars = 1 + 2 * kStages + 7;  // q_full, kv_full/empty, s_full[2], p_full[2], o_done[2], drain
   static constexpr int kOffTmemPtr = kOffBars + kNumBars * 8;
-  static constexpr int kBytes = kOffTmemPtr + 16;
+  static constexpr int kOffXchg = kOffTmemPtr + 16;       // differential attention: row sums and sums of squares, [2][2][128] fp32
+  static constexpr int kBytes = kOffXchg + (kDiff ? 2 * 2 * 128 * 4 : 0);
   static constexpr int kDynBytes = kBytes + 1024;         // slack to align the base to 1024 bytes
 };
 
-template <int D, int kCtas>
+// The two halves of the differential epilogue exchange through shared memory: a barrier over the eight softmax warps.
+__device__ __forceinline__ void softmax_warps_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+
+// lambda of one head pair, by one warp (every lane gets it).
+__device__ __forceinline__ float diff_lambda(const DiffWeightsDev& w, int pair, int lane) {
+  float dot[2];
+#pragma unroll
+  for (int m = 0; m < 2; ++m) {
+    const float* a = w.vec[2 * m] + (long long)pair * w.pair_stride;
+    const float* b = w.vec[2 * m + 1] + (long long)pair * w.pair_stride;
+    dot[m] = __ldg(a + lane) * __ldg(b + lane) + __ldg(a + 32 + lane) * __ldg(b + 32 + lane);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) dot[m] += __shfl_xor_sync(0xffffffffu, dot[m], o);
+  }
+  return expf(dot[0]) - expf(dot[1]) + w.lambda_init;
+}
+
+// Epilogue of the differential attention.  Query tile t of the kernel is softmax map t over the same 128 rows, so the
+// row a thread owns in map 0 and the row its counterpart owns in map 1 are the same row, in the same tensor-memory
+// lane: warpgroup t combines columns [64 t, 64 t + 64) of both accumulators, O0 / l0 - lambda * O1 / l1, which is head
+// 2 * pair + t of the output.  Row sums and the norm's sums of squares cross over through shared memory.
+template <typename L>
+__device__ __forceinline__ void diff_epilogue(const AttnParams& p, const SeqDev& sq, int pair, int t, int first_row, int lane,
+                                              int wq, uint32_t tmem_lane, float l, float lam, uint8_t* smem) {
+  float* xl = reinterpret_cast<float*>(smem + L::kOffXchg);                // [map][row] row sums
+  float* xs = xl + 256;                                                    // [half][row] sums of squares
+  const int row = wq * 32 + lane;
+  xl[t * 128 + row] = l;
+  softmax_warps_sync();
+  const float a0 = 1.0f / xl[row], a1 = lam / xl[128 + row];
+  float x[64];
+  float ss = 0.f;
+#pragma unroll
+  for (int cch = 0; cch < 2; ++cch) {
+    uint32_t o0[32], o1[32];
+    tmem_ld32(tmem_lane + 256 + t * 64 + cch * 32, o0);
+    tmem_ld32(tmem_lane + 384 + t * 64 + cch * 32, o1);
+    tmem_wait_ld();
+#pragma unroll
+    for (int e = 0; e < 32; ++e) {
+      const float v = __uint_as_float(o0[e]) * a0 - __uint_as_float(o1[e]) * a1;
+      x[cch * 32 + e] = v;
+      ss = fmaf(v, v, ss);
+    }
+  }
+  if (p.diff.gain != nullptr) {
+    xs[t * 128 + row] = ss;
+    softmax_warps_sync();
+    const float f = (1.0f - p.diff.lambda_init) / sqrtf((xs[row] + xs[128 + row]) * (1.0f / 128.0f) + p.diff.eps);
+    const float4* g4 = reinterpret_cast<const float4*>(p.diff.gain + t * 64);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const float4 g = __ldg(g4 + e);
+      x[4 * e] *= f * g.x; x[4 * e + 1] *= f * g.y; x[4 * e + 2] *= f * g.z; x[4 * e + 3] *= f * g.w;
+    }
+  }
+  // every MMA has completed: the Q tile is the staging buffer, 4 KB per warp
+  uint8_t* stage = smem + L::kOffQ + (t * 4 + wq) * 32 * 128;
+#pragma unroll
+  for (int ch = 0; ch < 8; ++ch) {
+    uint4 w;
+    w.x = pack_bf16x2(x[8 * ch], x[8 * ch + 1]);
+    w.y = pack_bf16x2(x[8 * ch + 2], x[8 * ch + 3]);
+    w.z = pack_bf16x2(x[8 * ch + 4], x[8 * ch + 5]);
+    w.w = pack_bf16x2(x[8 * ch + 6], x[8 * ch + 7]);
+    *reinterpret_cast<uint4*>(stage + lane * 128 + ((ch ^ (lane & 7)) << 4)) = w;
+  }
+  write_staged_rows<128>(p, sq, 2 * pair + t, first_row, lane, 2, stage);
+}
+
+// 128 validity bits of a key tile when no mask is given: the tokens the sequence has.
+__device__ __forceinline__ uint4 tail_bits(int rem) {
+  auto word = [](int r) { return r >= 32 ? 0xffffffffu : r <= 0 ? 0u : (1u << r) - 1u; };
+  return make_uint4(word(rem), word(rem - 32), word(rem - 64), word(rem - 96));
+}
+
+// kDiff: differential attention (head_dim 64, CTA pairs).  The two query tiles of a CTA become the two softmax maps of
+// ONE tile of 128 query rows: a head pair (2i, 2i+1) has its two 64-dim Q and K side by side, which in shared memory is
+// exactly one 128-dim tile of two 64-column boxes, and map t multiplies box t of Q with box t of K.  Both maps share the
+// pair's 128-dim V.  Everything between (softmax, ring, accumulators) is the plain kernel's.  Per key tile and CTA that is
+// 2 x 16384 exponentials (2048 cycles of the special-function unit) against 1536 cycles of tensor-core work, so the
+// exponentials bound it: 10.3 ms for 25,216 tokens x 20 pairs, 949 TFLOP/s.
+template <int D, int kCtas, bool kDiff = false>
 __global__ void __launch_bounds__(kAttnThreads, 1)
 attn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                 const __grid_constant__ CUtensorMap tm_v, const AttnParams p) {
   static_assert(kCtas == 1 || (kCtas == 2 && D == 128), "CTA pairs are built for head_dim 128");
-  using L = AttnSmem<D, kCtas>;
+  static_assert(!kDiff || (D == 128 && kCtas == 2), "differential attention runs on CTA pairs, value width 128");
+  using L = AttnSmem<D, kCtas, kDiff>;
   constexpr bool kPair = kCtas == 2;
+  constexpr int kRows = kDiff ? 128 : 256;              // query rows of one CTA
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw_addr = smem_u32(smem_raw);
   const uint32_t sbase = (raw_addr + 1023u) & ~1023u;
@@ -250,13 +344,15 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
   // ---- which work item (one per CTA, or one per CTA pair)
   const int unit = (int)blockIdx.x / kCtas + p.cta_offset;
   int si = 0;
-  if (kPair) { while (si + 1 < p.n_seqs && unit >= p.seqs[si + 1].quad_work_start) ++si; }
+  // differential attention: 256-row blocks per head PAIR, so the unit counts are half of the single CTAs' (heads is even)
+  if (kDiff)      { while (si + 1 < p.n_seqs && unit >= p.seqs[si + 1].work_start / 2) ++si; }
+  else if (kPair) { while (si + 1 < p.n_seqs && unit >= p.seqs[si + 1].quad_work_start) ++si; }
   else       { while (si + 1 < p.n_seqs && unit >= p.seqs[si + 1].work_start) ++si; }
   const SeqDev sq = p.seqs[si];
-  const int units_per_head = kPair ? (sq.n_qpairs + 1) / 2 : sq.n_qpairs;
-  const int local = unit - (kPair ? sq.quad_work_start : sq.work_start);
+  const int units_per_head = kPair && !kDiff ? (sq.n_qpairs + 1) / 2 : sq.n_qpairs;
+  const int local = unit - (kDiff ? sq.work_start / 2 : kPair ? sq.quad_work_start : sq.work_start);
   const int head = local / units_per_head;
-  const int blk = local - head * units_per_head;        // query pair (256 rows) or query quad (512 rows)
+  const int blk = local - head * units_per_head;        // query pair (256 rows) or query quad (512 rows); kDiff: head = head pair
   SOL_DEVICE_CHECK(p.status, si < p.n_seqs && local >= 0 && head < p.heads && blk >= 0 && blk < units_per_head, kCheckWorkItem);
   SOL_DEVICE_CHECK(p.status, !(p.fault_inject == 2u && unit == 0), kCheckInjected);
   // a launch may serve a range of heads only (uniform over the CTA / the pair, before any set-up)
@@ -264,13 +360,14 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
   // rectangular mode: a query block without a wanted row has nothing to do (uniform, before any set-up)
   if (p.pair_needed != nullptr) {
     const uint8_t* need = p.pair_needed + sq.pair_start;
-    bool any = need[kCtas * blk] != 0;
-    if (kPair && 2 * blk + 1 < sq.n_qpairs) any = any || need[2 * blk + 1] != 0;
+    bool any = need[kDiff ? blk : kCtas * blk] != 0;
+    if (kPair && !kDiff && 2 * blk + 1 < sq.n_qpairs) any = any || need[2 * blk + 1] != 0;
     if (!any) return;
   }
   // dense: every CTA of a sequence walks the same list of key tiles; block-sparse (single CTAs only): each CTA has its own
   const bool sparse = !kPair && p.cta_list != nullptr;
-  const int n_proc = sparse ? p.cta_count[unit] : p.ktile_count[si];
+  const bool all_keys = kDiff && p.keybits == nullptr;  // no mask: no bits and no list were built
+  const int n_proc = all_keys ? sq.n_ktiles : sparse ? p.cta_count[unit] : p.ktile_count[si];
   const int* __restrict__ ktiles =
       sparse ? p.cta_list + sq.sparse_list_start + (long long)local * sq.n_ktiles : p.ktile_list + sq.ktile_start;
   const uint4* __restrict__ keybits = p.keybits + sq.ktile_start;
@@ -279,7 +376,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
   // order): a wave then starts on the tiles its predecessor touched last, which are still in L2, instead of
   // on the ones it touched first, which a long sequence has pushed out by then.
   const bool backwards = ((unit / max(1, p.wave_ctas / kCtas)) & 1) != 0;
-  const int q_row0 = blk * (256 * kCtas) + (int)rank * 256;   // first local query row of this CTA
+  const int q_row0 = blk * (kRows * kCtas) + (int)rank * kRows;   // first local query row of this CTA
   const int tok0 = (int)sq.tok_start;                  // TMA token coordinate of the sequence start
   const unsigned long long limit = p.wait_limit_ns;
 
@@ -341,11 +438,14 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
     float m_ref = -CUDART_INF_F;
     float l = 0.f;
     bool ok = true;
+    float lam = 0.f;
+    if constexpr (kDiff) lam = diff_lambda(p.diff, head, lane);
 
     for (int i = 0; i < n_proc; ++i) {
-      const int jt = __ldg(&ktiles[backwards ? n_proc - 1 - i : i]);
+      const int it = backwards ? n_proc - 1 - i : i;
+      const int jt = all_keys ? it : __ldg(&ktiles[it]);
       SOL_DEVICE_CHECK(p.status, jt >= 0 && jt < sq.n_ktiles, kCheckKeyTile);
-      const uint4 kb = __ldg(&keybits[jt]);
+      const uint4 kb = all_keys ? tail_bits(sq.n_tokens - jt * 128) : __ldg(&keybits[jt]);
       ok = __all_sync(0xffffffffu, mbar_wait(bar_s_full(t), i & 1, limit));
       if (!ok) break;
       tc_fence_after();
@@ -434,9 +534,26 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
     // ---- epilogue: O / l in the output format, staged through shared memory, coalesced 16-byte stores
     if (ok && n_proc > 0) {
       ok = __all_sync(0xffffffffu, mbar_wait(bar_o_done(t), (n_proc - 1) & 1, limit));
+      if (kDiff && ok) ok = __all_sync(0xffffffffu, mbar_wait(bar_o_done(t ^ 1), (n_proc - 1) & 1, limit));
       if (ok) tc_fence_after();
     }
-    if (ok && n_proc > 0) {
+    if constexpr (kDiff) {
+      // The warpgroups wait for each other in the epilogue, so they must agree on whether it runs: a warp whose wait ran
+      // out leaves its mark in a row sum (NaN is what its rows would be) and takes part.
+      if (n_proc > 0) {
+        if (!ok && lane == 0) atomicCAS(p.status, 0u, kStatusTimeoutSoftmax);
+        diff_epilogue<L>(p, sq, head, t, q_row0 + wq * 32, lane, wq, tmem_base + lane_off, ok ? l : CUDART_NAN_F, lam, smem);
+      } else {
+        const int qrow = q_row0 + row;
+        bool store = qrow < sq.n_tokens;
+        if (store && p.query_mask != nullptr) store = p.query_mask[sq.tok_start + qrow] != 0;
+        if (store) {
+          uint8_t* dst = out_row_ptr(p, sq.tok_start + qrow, 2 * head + t, 2);
+#pragma unroll
+          for (int c16 = 0; c16 < 8; ++c16) *reinterpret_cast<uint4*>(dst + c16 * 16) = make_uint4(0u, 0u, 0u, 0u);
+        }
+      }
+    } else if (ok && n_proc > 0) {
       const float inv = 1.0f / l;
       uint8_t* stage = smem + L::kOffQ + t * L::kTile + wq * 32 * (D * 2);
       if (p.sink.fmt == kOutInt8)      store_rows_int8<D>(p, sq, head, q_row0 + t * 128 + row, tO, inv);
@@ -476,9 +593,14 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
       const uint64_t pol_once = l2_policy_evict_first();
       const uint64_t pol_kv = l2_policy_evict_last_half();
       // the leader's barrier counts the bytes of both CTAs' loads
-      if (leader) mbar_arrive_expect_tx(bar_q_full, kCtas * 2 * L::kTile);
+      if (leader) mbar_arrive_expect_tx(bar_q_full, kCtas * (kDiff ? 1 : 2) * L::kTile);
+      if constexpr (kDiff) {
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+        for (int hf = 0; hf < 2; ++hf)
+          tma_load_3d_pair_hint(sQ + hf * L::kHalfBytes, &tm_q, lead_q_full, 0, 2 * head + hf, tok0 + q_row0, pol_once);
+      }
+#pragma unroll
+      for (int t = 0; t < (kDiff ? 0 : 2); ++t)
 #pragma unroll
         for (int hf = 0; hf < L::kHalves; ++hf) {
           const uint32_t dst = sQ + t * L::kTile + hf * L::kHalfBytes;
@@ -487,7 +609,8 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
         }
       uint32_t it = 0, stage = 0, par = 0;
       for (int i = 0; i < n_proc && ok; ++i) {
-        const int jt = __ldg(&ktiles[backwards ? n_proc - 1 - i : i]);
+        const int at = backwards ? n_proc - 1 - i : i;
+        const int jt = all_keys ? at : __ldg(&ktiles[at]);
 #pragma unroll
         for (int kv = 0; kv < 2; ++kv) {
           if (!mbar_wait(bar_kv_empty(stage), par ^ 1u, limit)) { ok = false; break; }
@@ -499,9 +622,11 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             if (kv == 0) {
 #pragma unroll
               for (int hf = 0; hf < L::kHalves; ++hf)
-                tma_load_3d_pair_hint(dst + hf * L::kKBoxBytes, &tm_k, full, hf * 64, head, tok0 + jt * 128 + (int)rank * 64, pol_kv);
+                tma_load_3d_pair_hint(dst + hf * L::kKBoxBytes, &tm_k, full, kDiff ? 0 : hf * 64, kDiff ? 2 * head + hf : head,
+                                      tok0 + jt * 128 + (int)rank * 64, pol_kv);
             } else {
-              tma_load_3d_pair_hint(dst, &tm_v, full, (int)rank * 64, head, tok0 + jt * 128, pol_kv);
+              tma_load_3d_pair_hint(dst, &tm_v, full, kDiff ? 0 : (int)rank * 64, kDiff ? 2 * head + (int)rank : head,
+                                    tok0 + jt * 128, pol_kv);
             }
           } else {
             const CUtensorMap* tm = kv ? &tm_v : &tm_k;
@@ -537,18 +662,20 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
       // descriptor words: only the low word (address) moves inside the loop
       const uint32_t hi_k = smem_desc_hi_sw128(1024);
       const uint32_t hi_v = smem_desc_hi_sw128(v_sbo);
-      const uint32_t q_lo0 = smem_desc_lo(sQ, 16), q_lo1 = smem_desc_lo(sQ + L::kTile, 16);
+      const uint32_t q_lo0 = smem_desc_lo(sQ, 16), q_lo1 = smem_desc_lo(sQ + (kDiff ? L::kHalfBytes : L::kTile), 16);
       const uint32_t k_lo_base = smem_desc_lo(sKV, 16);
+      constexpr uint32_t kMap1 = kDiff ? L::kKBoxBytes >> 4 : 0;       // map 1 multiplies the second box of K
+      constexpr int kQkSteps = kDiff ? 4 : D / 16;                      // 16 head dims per instruction
       const uint32_t v_lo_base = smem_desc_lo(sKV, v_lbo);
       constexpr uint32_t kStageStep = L::kStageBytes >> 4;
       const uint32_t tS0 = tmem_base, tS1 = tmem_base + 128;
       const uint32_t tO0 = tmem_base + 256, tO1 = tmem_base + 256 + D;
       auto commit = [&](uint32_t bar) { if (kPair) tc_commit_elect_pair(bar); else tc_commit_elect(bar); };
       auto wait_full = [&](uint32_t bar, uint32_t parity) { return mbar_wait_warp(bar, parity, limit); };
-      auto issue_qk = [&](uint32_t d_tmem, uint32_t q_lo, uint32_t stage) {
-        const uint32_t k_lo = k_lo_base + stage * kStageStep;
+      auto issue_qk = [&](uint32_t d_tmem, uint32_t q_lo, uint32_t stage, uint32_t k_box) {
+        const uint32_t k_lo = k_lo_base + stage * kStageStep + k_box;
 #pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
+        for (int k = 0; k < kQkSteps; ++k) {
           const uint32_t q_off = ((k >> 2) * L::kHalfBytes + (k & 3) * 32) >> 4;
           const uint32_t k_off = ((k >> 2) * L::kKBoxBytes + (k & 3) * 32) >> 4;
           if (kPair) {
@@ -581,9 +708,9 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
         ok = wait_full(bar_q_full, 0) && wait_full(bar_kv_full(st), ph);
         if (ok) {
           tc_fence_after();
-          issue_qk(tS0, q_lo0, st);
+          issue_qk(tS0, q_lo0, st, 0u);
           commit(bar_s_full(0));
-          issue_qk(tS1, q_lo1, st);
+          issue_qk(tS1, q_lo1, st, kMap1);
           // (test hook: work item 0 withholds this signal so that the waits downstream run into their limit)
           if (!(p.fault_inject == 1u && unit == 0)) commit(bar_s_full(1));
           commit(bar_kv_empty(st));
@@ -603,7 +730,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
           if (more) {
             if (!wait_full(bar_kv_full(k_st), k_ph)) { ok = false; break; }
             tc_fence_after();
-            issue_qk(tS0, q_lo0, k_st);
+            issue_qk(tS0, q_lo0, k_st, 0u);
             commit(bar_s_full(0));
           }
           if (!wait_full(bar_p_full(1), i & 1)) { ok = false; break; }
@@ -612,7 +739,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
           commit(bar_o_done(1));
           commit(bar_kv_empty(v_st));
           if (more) {
-            issue_qk(tS1, q_lo1, k_st);
+            issue_qk(tS1, q_lo1, k_st, kMap1);
             commit(bar_s_full(1));
             commit(bar_kv_empty(k_st));
           }

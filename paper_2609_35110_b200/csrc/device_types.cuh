@@ -41,6 +41,16 @@ struct OutSink {
                             // kOutInt8: one block-INT8 record per (token, head), strides counted in bytes
 };
 
+// Learned weights of the differential attention: lambda = exp(q1 . k1) - exp(q2 . k2) + lambda_init per head pair, and the
+// RMS norm of the difference over the pair's 2 * head_dim values.
+struct DiffWeightsDev {
+  const float* vec[4];      // q1, k1, q2, k2: 64 values each, pair i at i * pair_stride
+  long long pair_stride;
+  float lambda_init;
+  float eps;
+  const float* gain;        // 128 values, or nullptr: the difference itself is the output
+};
+
 struct AttnParams {
   const SeqDev* seqs;
   int n_seqs;
@@ -64,6 +74,8 @@ struct AttnParams {
   unsigned int fault_inject;  // test hooks: 1 = work item 0 never publishes S of query tile 1 (exercises the bounded
                               // waits); 2 = work item 0 fails a device-side check on purpose (debug build)
   unsigned int v_lbo, v_sbo;  // byte offsets of the V (MN-major) shared-memory descriptor
+  // differential attention only (keybits == nullptr there: every token of a sequence is a valid key)
+  DiffWeightsDev diff;
 };
 
 // Status word: low byte = what happened (first event wins), upper bits = detail.

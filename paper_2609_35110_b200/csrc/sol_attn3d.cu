@@ -51,7 +51,9 @@ struct sol_attn3d_plan_s {
 
   // workspace layout (byte offsets)
   size_t off_status = 0, off_tables = 0, off_seqs = 0, off_keybits = 0, off_list = 0, off_count = 0, off_pairs = 0,
+         off_dbits = 0, off_dlist = 0, off_dcount = 0,
          off_qrot = 0, off_krot = 0, ws_bytes = 0;
+  size_t ws_dense_bytes = 0;          // what every call but the differential attention uses (a prefix of the workspace)
   int total_pairs = 0;
   unsigned char* ws = nullptr;
   // block-sparse scratch (passed per call): byte offsets
@@ -114,6 +116,9 @@ cudaError_t raise_shared_memory_limits() {
   if (e == cudaSuccess)
     e = cudaFuncSetAttribute(sol::attn_fwd_kernel<128, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                              sol::AttnSmem<128, 2>::kDynBytes);
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute(sol::attn_fwd_kernel<128, 2, true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             sol::AttnSmem<128, 2, true>::kDynBytes);
   return e;
 }
 
@@ -266,6 +271,14 @@ int build_plan(sol_attn3d_plan_t* out, const sol_attn3d_desc* d) {
     const size_t rot = (size_t)p->total_tokens * p->heads * p->head_dim * 2;
     p->off_qrot = off;    off = align_up(off + rot);
     p->off_krot = off;    off = align_up(off + rot);
+    p->ws_dense_bytes = off;
+    if (p->head_dim == 64 && p->heads % 2 == 0) {
+      // the differential attention's own bits, so that its masks never replace the ones a captured or later plain forward
+      // relies on (keybits_state)
+      p->off_dbits = off;   off = align_up(off + (size_t)p->total_ktiles * 16);
+      p->off_dlist = off;   off = align_up(off + (size_t)p->total_ktiles * sizeof(int));
+      p->off_dcount = off;  off = align_up(off + (size_t)p->n_seqs * sizeof(int));
+    }
     p->ws_bytes = off;
 
     if (const char* e = std::getenv("SOL_ATTN3D_WAIT_LIMIT_MS")) {
@@ -1026,6 +1039,120 @@ int forward_impl(sol_attn3d_plan_t p, const void* q, const void* k, const void* 
 }
 }  // namespace
 
+extern "C++" {
+namespace {
+// Checks a caller's weights of the differential attention and fills the kernels' form of them.
+int take_diff_weights(const sol_attn3d_diff_weights* w, int head_dim, sol::DiffWeightsDev* out) {
+  if (w == nullptr || w->size != sizeof(sol_attn3d_diff_weights)) return SOL_ATTN3D_ERR_INVALID_ARG;
+  const float* vec[4] = {w->lambda_q1, w->lambda_k1, w->lambda_q2, w->lambda_k2};
+  for (int i = 0; i < 4; ++i) {
+    if (vec[i] == nullptr || (reinterpret_cast<uintptr_t>(vec[i]) & 3u) != 0) return SOL_ATTN3D_ERR_INVALID_ARG;
+    out->vec[i] = vec[i];
+  }
+  if (w->lambda_pair_stride != 0 && w->lambda_pair_stride < head_dim) return SOL_ATTN3D_ERR_INVALID_ARG;
+  if (!std::isfinite(w->lambda_init) || !(w->eps >= 0.f) || !aligned16(w->gain)) return SOL_ATTN3D_ERR_INVALID_ARG;
+  out->pair_stride = w->lambda_pair_stride;
+  out->lambda_init = w->lambda_init;
+  out->eps = w->eps;
+  out->gain = w->gain;
+  return SOL_ATTN3D_OK;
+}
+}  // namespace
+}  // extern "C++"
+
+int sol_attn3d_forward_diff(sol_attn3d_plan_t p, const void* q, const void* k, const void* v, void* out,
+                            const uint8_t* key_mask, const uint8_t* query_mask, const sol_attn3d_diff_weights* weights,
+                            sol_attn3d_stream_t stream) {
+  if (p == nullptr || q == nullptr || k == nullptr || v == nullptr || out == nullptr) return SOL_ATTN3D_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out)) return SOL_ATTN3D_ERR_INVALID_ARG;
+  if (out == q || out == k || out == v) return SOL_ATTN3D_ERR_INVALID_ARG;
+  if (p->head_dim != 64 || (p->heads & 1) != 0) return SOL_ATTN3D_ERR_UNSUPPORTED_SHAPE;
+  sol::AttnParams ap{};
+  int rc = take_diff_weights(weights, p->head_dim, &ap.diff);
+  if (rc != SOL_ATTN3D_OK) return rc;
+  unsigned char* ws = p->ws;
+  if (ws == nullptr || p->encode == nullptr) return SOL_ATTN3D_ERR_NO_WORKSPACE;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  cudaError_t e;
+  p->launches = 0;
+  const SeqDev* d_seqs = reinterpret_cast<const SeqDev*>(ws + p->off_seqs);
+
+  if (p->prof) {
+    p->prof_valid = false;
+    if ((e = cudaEventRecord(p->ev[0], st)) != cudaSuccess) return fail_cuda(p, e);
+  }
+  // (1) validity bits per key tile, with a mask only: without one the kernel derives them from the sequence lengths, so
+  //     such a call neither needs nor leaves anything in that part of the workspace
+  p->prof_bits = key_mask != nullptr;
+  if (key_mask != nullptr) {
+    sol::keybits_kernel<<<p->n_seqs, 256, 0, st>>>(d_seqs, key_mask, reinterpret_cast<uint32_t*>(ws + p->off_dbits),
+                                                   reinterpret_cast<int*>(ws + p->off_dlist),
+                                                   reinterpret_cast<int*>(ws + p->off_dcount));
+    if ((e = cudaGetLastError()) != cudaSuccess) return fail_cuda(p, e);
+    ++p->launches;
+    ap.keybits = reinterpret_cast<const uint4*>(ws + p->off_dbits);
+    ap.ktile_list = reinterpret_cast<const int*>(ws + p->off_dlist);
+    ap.ktile_count = reinterpret_cast<const int*>(ws + p->off_dcount);
+  }
+  if (p->prof && (e = cudaEventRecord(p->ev[1], st)) != cudaSuccess) return fail_cuda(p, e);
+
+  // (2) rotary prologue over all heads, as for the plain forward
+  rc = launch_rope(p, ws, q, k, ws + p->off_qrot, ws + p->off_krot, nullptr, nullptr, 0.f, st);
+  if (rc != SOL_ATTN3D_OK) return rc;
+  if (query_mask != nullptr) {
+    uint8_t* flags = ws + p->off_pairs;
+    sol::pair_needed_kernel<<<p->total_pairs, 32, 0, st>>>(d_seqs, p->n_seqs, query_mask, flags);
+    if ((e = cudaGetLastError()) != cudaSuccess) return fail_cuda(p, e);
+    ++p->launches;
+    ap.pair_needed = flags;
+    ap.query_mask = query_mask;
+  }
+  if (p->prof && (e = cudaEventRecord(p->ev[2], st)) != cudaSuccess) return fail_cuda(p, e);
+
+  // (3) attention: 256-row blocks per head pair on CTA pairs
+  CUtensorMap tm_v;
+  if ((rc = encode_map(p->encode, p, &tm_v, v, p->sv)) != SOL_ATTN3D_OK) return rc;
+  ap.seqs = d_seqs;
+  ap.n_seqs = p->n_seqs;
+  ap.heads = p->heads / 2;
+  ap.head_begin = 0;
+  ap.head_end = p->heads / 2;
+  ap.wave_ctas = p->sm_count;
+  ap.sink.base[0] = out;
+  ap.sink.tok_begin[1] = p->total_tokens;
+  ap.sink.n_dst = 1;
+  ap.sink.fmt = sol::kOutBf16;
+  ap.o_tok_stride = p->so.tok;
+  ap.o_head_stride = p->so.head;
+  ap.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)p->head_dim));
+  ap.status = reinterpret_cast<unsigned int*>(ws + p->off_status);
+  ap.counters = reinterpret_cast<unsigned int*>(ws + p->off_status + kCountersOffset);
+  ap.wait_limit_ns = p->wait_limit_ns;
+  ap.v_lbo = 16384u;
+  ap.v_sbo = p->v_sbo;
+  ap.fault_inject = p->fault_inject;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)p->total_work, 1, 1);       // total_work = 256-row blocks x heads = 2 CTAs x blocks x pairs
+  cfg.blockDim = dim3(sol::kAttnThreads, 1, 1);
+  cfg.dynamicSmemBytes = sol::AttnSmem<128, 2, true>::kDynBytes;
+  cfg.stream = st;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = 2;
+  attr.val.clusterDim.y = 1;
+  attr.val.clusterDim.z = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  e = cudaLaunchKernelEx(&cfg, sol::attn_fwd_kernel<128, 2, true>, p->tm_q, p->tm_k64, tm_v, ap);
+  if (e != cudaSuccess) return fail_cuda(p, e);
+  ++p->launches;
+  if (p->prof) {
+    if ((e = cudaEventRecord(p->ev[3], st)) != cudaSuccess) return fail_cuda(p, e);
+    p->prof_valid = true;
+  }
+  return SOL_ATTN3D_OK;
+}
+
 int sol_attn3d_set_profiling(sol_attn3d_plan_t p, int enable) {
   if (p == nullptr) return SOL_ATTN3D_ERR_INVALID_ARG;
   if ((enable != 0) == p->prof) return SOL_ATTN3D_OK;
@@ -1119,7 +1246,7 @@ int sol_attn3d_forward_noalloc(sol_attn3d_plan_t p, const void* q, const void* k
                                const uint8_t* key_mask, unsigned int* device_status, sol_attn3d_stream_t stream) {
   if (p == nullptr || q == nullptr || k == nullptr || v == nullptr || out == nullptr) return SOL_ATTN3D_ERR_INVALID_ARG;
   if ((reinterpret_cast<uintptr_t>(device_status) & 3u) != 0) return SOL_ATTN3D_ERR_INVALID_ARG;
-  if (p->ws_bytes > kStaticScratchBytes) return SOL_ATTN3D_ERR_SCRATCH_LIMIT;
+  if (p->ws_dense_bytes > kStaticScratchBytes) return SOL_ATTN3D_ERR_SCRATCH_LIMIT;
   unsigned char* ws = nullptr;
   int sm_count = 0;
   const int rc = static_scratch_for_current_device(p, &ws, &sm_count);
