@@ -427,6 +427,65 @@ int sol_attn3d_forward_diff(sol_attn3d_plan_t plan, const void* q, const void* k
                             sol_attn3d_stream_t stream);
 
 /*
+ * A cache of K and V rows (bf16, DEVICE): row (slot, token, head) at slot * strides[0] + token * strides[1] + head *
+ * strides[2] elements; 0 stands for the dense value ([n_slots][capacity][heads][head_dim]).  Byte strides are multiples
+ * of 16, the pointers 16-byte aligned; offsets are 64-bit.  K rows hold rotated keys (sol_attn3d_rope_qk).
+ *   key_mask   uint8 [n_slots][capacity] (slot stride mask_slot_stride bytes, 0 = capacity), nonzero = attend; or NULL.
+ */
+typedef struct {
+  uint32_t size;                /* sizeof(sol_attn3d_kv_cache) */
+  const void* k;
+  const void* v;
+  int64_t k_strides[3];
+  int64_t v_strides[3];
+  int64_t n_slots;
+  int64_t capacity;             /* tokens per slot */
+  const uint8_t* key_mask;
+  int64_t mask_slot_stride;
+} sol_attn3d_kv_cache;
+
+/*
+ * The differential attention of one new query token per stream over a cache (the single-query case of Section 3.2's
+ * "SDPA" with cached K/V, cf. "Reference KV caching mechanism"): row b of q attends to the first lens[b] tokens of slot
+ * slots[b].  The formula is that of sol_attn3d_forward_diff on q and K as they are (both rotated by the caller).
+ *   q, out     DEVICE, bf16 [batch, heads, 64] with element strides {row, head} ({0,0} = dense); 16-byte aligned.
+ *   lens       DEVICE, int32 [batch].  Values are clamped to [0, capacity]; 0 tokens, or none with a nonzero mask, give
+ *              a row of zeros.  Cache rows beyond the length and masked ones may hold anything (infinities, NaN).
+ *   slots      DEVICE, int32 [batch], or NULL: row b uses slot b.  A row whose slot is outside [0, n_slots) is idle: its
+ *              output is left as it was.  Several rows may name one slot.
+ *   workspace  DEVICE, 256-byte aligned, at least sol_attn3d_diff_step_workspace_bytes(...) bytes, which may be 0 (then
+ *              NULL is fine): partial results of the key ranges that different CTAs handle, written and read by every
+ *              call.  Calls that may overlap on the GPU need one each.
+ * No plan, no device-side wait, deterministic, may be captured.  batch = 0 is a no-op.
+ * Errors: INVALID_ARG, UNSUPPORTED_SHAPE (head_dim other than 64, odd heads, strides), NO_WORKSPACE, CUDA.
+ */
+size_t sol_attn3d_diff_step_workspace_bytes(int batch, int heads, int head_dim, int64_t capacity);
+int sol_attn3d_diff_step(const void* q, const int64_t q_strides[2], const sol_attn3d_kv_cache* cache, const int32_t* lens,
+                         const int32_t* slots, void* out, const int64_t out_strides[2], int batch, int heads, int head_dim,
+                         const sol_attn3d_diff_weights* weights, void* workspace, size_t workspace_bytes,
+                         sol_attn3d_stream_t stream);
+
+/*
+ * Linear attention with a decay per head, one token per row: the recurrent form of sol_attn3d_forward_linear.  Every
+ * (slot, head) has a state S of head_dim x head_dim fp32, S[i][j] for K dim i and V dim j:
+ *     S' = exp(log_decay[head]) * S + k^T v,      out = scale * q S'
+ *   q, k, v, out  DEVICE, bf16 [batch, heads, head_dim] (64 or 128), element strides {row, head} ({0,0} = dense), 16-byte
+ *                 aligned; out must not alias an input.  q and k are taken as they are (sol_attn3d_rope_qk rotates).
+ *   log_decay     DEVICE, fp32 [heads], natural logarithm of the decay; values above 0 count as 0, -infinity forgets all.
+ *   state_in, state_out   DEVICE, fp32 [n_slots][heads][head_dim][head_dim], 16-byte aligned; the same pointer (in place)
+ *                 or disjoint memory.  States of slots that no row names are not touched.
+ *   slots         DEVICE, int32 [batch], or NULL: row b uses slot b (n_slots >= batch).  A row whose slot is outside
+ *                 [0, n_slots) is idle: its output is left as it was.  Rows that name the same slot are successive tokens
+ *                 of that stream, in row order.
+ * One kernel, no workspace, fp32 state arithmetic, deterministic, may be captured.  batch = 0 is a no-op.
+ * Errors: INVALID_ARG, UNSUPPORTED_SHAPE, CUDA.
+ */
+int sol_attn3d_linear_step(const void* q, const void* k, const void* v, void* out, const int64_t q_strides[2],
+                           const int64_t k_strides[2], const int64_t v_strides[2], const int64_t out_strides[2], int batch,
+                           int heads, int head_dim, const float* log_decay, float scale, const float* state_in,
+                           float* state_out, int64_t n_slots, const int32_t* slots, sol_attn3d_stream_t stream);
+
+/*
  * sol_attn3d_forward for callers that must not allocate device memory.  (The paper has no counterpart:
  * this is a deployment variant of the call above, not a step of the method.)
  *

@@ -56,6 +56,20 @@ class _DiffWeights(ctypes.Structure):
     ]
 
 
+class _KvCache(ctypes.Structure):
+    _fields_ = [
+        ("size", ctypes.c_uint32),
+        ("k", ctypes.c_void_p),
+        ("v", ctypes.c_void_p),
+        ("k_strides", ctypes.c_int64 * 3),
+        ("v_strides", ctypes.c_int64 * 3),
+        ("n_slots", ctypes.c_int64),
+        ("capacity", ctypes.c_int64),
+        ("key_mask", ctypes.c_void_p),
+        ("mask_slot_stride", ctypes.c_int64),
+    ]
+
+
 # error codes (mirror include/sol_attn3d.h)
 OK = 0
 ERR_INVALID_ARG = -1
@@ -140,6 +154,15 @@ def _lib():
     lib.sol_attn3d_sparse_selection.restype = i32
     lib.sol_attn3d_forward_diff.argtypes = [vp, vp, vp, vp, vp, vp, vp, ctypes.POINTER(_DiffWeights), vp]
     lib.sol_attn3d_forward_diff.restype = i32
+    p64 = ctypes.POINTER(i64)
+    lib.sol_attn3d_diff_step_workspace_bytes.argtypes = [i32, i32, i32, i64]
+    lib.sol_attn3d_diff_step_workspace_bytes.restype = ctypes.c_size_t
+    lib.sol_attn3d_diff_step.argtypes = [vp, p64, ctypes.POINTER(_KvCache), vp, vp, vp, p64, i32, i32, i32,
+                                         ctypes.POINTER(_DiffWeights), vp, ctypes.c_size_t, vp]
+    lib.sol_attn3d_diff_step.restype = i32
+    lib.sol_attn3d_linear_step.argtypes = [vp, vp, vp, vp, p64, p64, p64, p64, i32, i32, i32, vp, ctypes.c_float, vp, vp, i64,
+                                           vp, vp]
+    lib.sol_attn3d_linear_step.restype = i32
     lib.sol_attn3d_rope_qk.argtypes = [vp, vp, vp, vp, vp, vp]
     lib.sol_attn3d_rope_qk.restype = i32
     lib.sol_attn3d_status.argtypes = [vp]
@@ -528,8 +551,85 @@ def sol_attn3d_forward_diff(plan, q, k, v, out, key_mask, weights: sol_attn3d_di
         if m is not None and (not m.is_cuda or m.dtype != torch.uint8 or not m.is_contiguous()):
             raise ValueError(f"{name} must be a contiguous CUDA uint8 tensor")
     _check_pairs(weights, q.shape[-2])
+    _check_on_device(q, k, v, out, key_mask, query_mask, *weights.tensors)
     _check(_lib().sol_attn3d_forward_diff(plan, _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(key_mask), _ptr(query_mask),
                                           ctypes.byref(weights.struct), _stream(stream)), "sol_attn3d_forward_diff")
+
+
+def _check_on_device(*tensors) -> None:
+    """The library launches on the current device: refuse tensors that live on another one."""
+    for t in tensors:
+        if t is not None and t.device.index != torch.cuda.current_device():
+            raise ValueError(f"tensor on {t.device}, current device is cuda:{torch.cuda.current_device()}")
+
+
+def _check_index(t: Optional[torch.Tensor], n: int, name: str) -> None:
+    if t is not None and (not t.is_cuda or t.dtype != torch.int32 or not t.is_contiguous() or t.numel() != n):
+        raise ValueError(f"{name} must be a contiguous CUDA int32 tensor with one element per row")
+
+
+def sol_attn3d_diff_step_workspace_bytes(batch: int, heads: int, head_dim: int, capacity: int) -> int:
+    return int(_lib().sol_attn3d_diff_step_workspace_bytes(batch, heads, head_dim, capacity))
+
+
+def _cache_strides(t: torch.Tensor, batch_like):
+    slots, cap, heads, head_dim = batch_like
+    if t.dim() != 4 or tuple(t.shape) != tuple(batch_like) or t.stride(3) != 1:
+        raise ValueError("caches: [slots, capacity, heads, head_dim] of one shape with contiguous head_dim")
+    # the stride torch reports for an axis of extent 0 or 1 is arbitrary: 0 asks for the dense value there
+    return (ctypes.c_int64 * 3)(*(t.stride(i) if t.shape[i] > 1 else 0 for i in range(3)))
+
+
+def sol_attn3d_diff_step(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, lens: torch.Tensor, out: torch.Tensor,
+                         weights: sol_attn3d_diff_weights, workspace: Optional[torch.Tensor],
+                         key_mask: Optional[torch.Tensor] = None, slots: Optional[torch.Tensor] = None, stream=None) -> None:
+    """One query token per row, q, out [batch, heads, 64], over caches [slots, capacity, heads, 64] (all rotated)."""
+    batch, heads, head_dim = q.shape
+    for t in (q, k_cache, v_cache, out):
+        if not t.is_cuda or t.dtype != torch.bfloat16:
+            raise ValueError("q, caches and out must be CUDA bf16 tensors")
+    if out.shape != q.shape or k_cache.dim() != 4 or k_cache.shape[2:] != q.shape[1:]:
+        raise ValueError("q, out: [batch, heads, 64]; caches: [slots, capacity, heads, 64]")
+    _check_index(lens, batch, "lens")
+    _check_index(slots, batch, "slots")
+    n_slots, capacity = k_cache.shape[:2]
+    if key_mask is not None and (not key_mask.is_cuda or key_mask.dtype != torch.uint8 or not key_mask.is_contiguous() or
+                                 tuple(key_mask.shape) != (n_slots, capacity)):
+        raise ValueError("key_mask must be a contiguous CUDA uint8 tensor [slots, capacity]")
+    _check_pairs(weights, heads)
+    _check_on_device(q, k_cache, v_cache, lens, out, workspace, key_mask, slots, *weights.tensors)
+    cache = _KvCache(ctypes.sizeof(_KvCache), k_cache.data_ptr(), v_cache.data_ptr(), _cache_strides(k_cache, k_cache.shape),
+                     _cache_strides(v_cache, k_cache.shape), n_slots, capacity, None if key_mask is None else key_mask.data_ptr(), 0)
+    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(_lib().sol_attn3d_diff_step(_ptr(q), _strides_of(q, head_dim), ctypes.byref(cache), _ptr(lens), _ptr(slots), _ptr(out),
+                                       _strides_of(out, head_dim), batch, heads, head_dim, ctypes.byref(weights.struct),
+                                       _ptr(workspace), nbytes, _stream(stream)), "sol_attn3d_diff_step")
+
+
+def sol_attn3d_linear_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, log_decay: torch.Tensor,
+                           scale: float, state_in: torch.Tensor, state_out: torch.Tensor, slots: Optional[torch.Tensor] = None,
+                           stream=None) -> None:
+    """One token per row, q, k, v, out [batch, heads, D]; states fp32 [slots, heads, D, D], in place or not."""
+    batch, heads, head_dim = q.shape
+    for t in (q, k, v, out):
+        if not t.is_cuda or t.dtype != torch.bfloat16 or t.shape != q.shape:
+            raise ValueError("q, k, v, out must be CUDA bf16 tensors of one shape")
+    for t in (state_in, state_out):
+        if not t.is_cuda or t.dtype != torch.float32 or not t.is_contiguous() or t.dim() != 4 or \
+                tuple(t.shape[1:]) != (heads, head_dim, head_dim) or t.shape != state_in.shape:
+            raise ValueError("states must be contiguous CUDA float32 tensors [slots, heads, D, D]")
+    _check_decay(log_decay, heads)
+    _check_index(slots, batch, "slots")
+    _check_on_device(q, k, v, out, log_decay, state_in, state_out, slots)
+    _check(_lib().sol_attn3d_linear_step(_ptr(q), _ptr(k), _ptr(v), _ptr(out), _strides_of(q, head_dim), _strides_of(k, head_dim),
+                                         _strides_of(v, head_dim), _strides_of(out, head_dim), batch, heads, head_dim,
+                                         _ptr(log_decay), ctypes.c_float(scale), _ptr(state_in), _ptr(state_out),
+                                         state_in.shape[0], _ptr(slots), _stream(stream)), "sol_attn3d_linear_step")
+
+
+def _check_decay(log_decay: torch.Tensor, heads: int) -> None:
+    if not log_decay.is_cuda or log_decay.dtype != torch.float32 or not log_decay.is_contiguous() or log_decay.numel() != heads:
+        raise ValueError("log_decay must be a contiguous CUDA float32 tensor with one element per head")
 
 
 def sol_attn3d_rope_qk(plan, q, k, q_rot, k_rot, stream=None) -> None:

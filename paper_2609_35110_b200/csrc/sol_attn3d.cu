@@ -15,6 +15,7 @@
 #include "device_types.cuh"
 #include "prologue_kernels.cuh"
 #include "sparse_kernels.cuh"
+#include "step_kernels.cuh"
 
 namespace {
 
@@ -1151,6 +1152,139 @@ int sol_attn3d_forward_diff(sol_attn3d_plan_t p, const void* q, const void* k, c
     p->prof_valid = true;
   }
   return SOL_ATTN3D_OK;
+}
+
+extern "C++" {
+namespace {
+// How many CTAs share the keys of one (stream, head pair): enough for about kStepCtas CTAs in all, but no split shorter
+// than kStepMinKeys keys of a full cache.  Depends on the sizes of the call only (the lengths live on the device).
+constexpr long long kStepCtas = 148 * 8, kStepMinKeys = 256;
+int diff_step_splits(int batch, int pairs, long long capacity) {
+  const long long items = (long long)batch * pairs;
+  const long long want = (kStepCtas + items - 1) / items;
+  return (int)std::max<long long>(1, std::min<long long>(want, capacity / kStepMinKeys));
+}
+bool diff_step_sizes_ok(int batch, int heads, int head_dim, long long capacity) {
+  return batch >= 0 && heads >= 2 && heads % 2 == 0 && heads <= 65534 && head_dim == 64 && capacity >= 0 &&
+         (long long)batch * (heads / 2) * diff_step_splits(std::max(batch, 1), heads / 2, capacity) < (1ll << 31);
+}
+}  // namespace
+}  // extern "C++"
+
+size_t sol_attn3d_diff_step_workspace_bytes(int batch, int heads, int head_dim, int64_t capacity) {
+  if (!diff_step_sizes_ok(batch, heads, head_dim, capacity) || batch == 0) return 0;
+  const int n_split = diff_step_splits(batch, heads / 2, capacity);
+  return n_split == 1 ? 0 : align_up((size_t)batch * (heads / 2) * n_split * sol::kStepPartial * sizeof(float));
+}
+
+int sol_attn3d_diff_step(const void* q, const int64_t q_strides[2], const sol_attn3d_kv_cache* cache, const int32_t* lens,
+                         const int32_t* slots, void* out, const int64_t out_strides[2], int batch, int heads, int head_dim,
+                         const sol_attn3d_diff_weights* weights, void* workspace, size_t workspace_bytes,
+                         sol_attn3d_stream_t stream) {
+  if (cache == nullptr || cache->size != sizeof(sol_attn3d_kv_cache) || batch < 0 || heads < 1 || head_dim < 1 ||
+      cache->n_slots < 0 || cache->capacity < 0)
+    return SOL_ATTN3D_ERR_INVALID_ARG;
+  if (!diff_step_sizes_ok(batch, heads, head_dim, cache->capacity)) return SOL_ATTN3D_ERR_UNSUPPORTED_SHAPE;
+  if (batch == 0) return SOL_ATTN3D_OK;
+  if (q == nullptr || out == nullptr || out == q || lens == nullptr || q_strides == nullptr || out_strides == nullptr ||
+      !aligned16(q) || !aligned16(out) || !aligned16(cache->k) || !aligned16(cache->v) ||
+      (reinterpret_cast<uintptr_t>(lens) & 3u) != 0 || (reinterpret_cast<uintptr_t>(slots) & 3u) != 0)
+    return SOL_ATTN3D_ERR_INVALID_ARG;
+  const bool empty = cache->n_slots == 0 || cache->capacity == 0;
+  if (!empty && (cache->k == nullptr || cache->v == nullptr)) return SOL_ATTN3D_ERR_INVALID_ARG;
+  sol::DiffStepArgs a{};
+  const int rc = take_diff_weights(weights, head_dim, &a.w);
+  if (rc != SOL_ATTN3D_OK) return rc;
+  const long long row = (long long)heads * head_dim;
+  a.q_row = q_strides[0] == 0 ? row : q_strides[0];
+  a.q_head = q_strides[1] == 0 ? head_dim : q_strides[1];
+  a.o_row = out_strides[0] == 0 ? row : out_strides[0];
+  a.o_head = out_strides[1] == 0 ? head_dim : out_strides[1];
+  auto take = [&](const int64_t st[3], long long* slot, long long* tok, long long* head) {
+    *head = st[2] == 0 ? head_dim : st[2];
+    *tok = st[1] == 0 ? row : st[1];
+    *slot = st[0] == 0 ? cache->capacity * *tok : st[0];
+    return stride_ok(*head) && stride_ok(*tok) && (empty || (*slot > 0 && *slot % 8 == 0));
+  };
+  if (!stride_ok(a.q_row) || !stride_ok(a.q_head) || !stride_ok(a.o_row) || !stride_ok(a.o_head) ||
+      !take(cache->k_strides, &a.k_slot, &a.k_tok, &a.k_head) || !take(cache->v_strides, &a.v_slot, &a.v_tok, &a.v_head) ||
+      cache->mask_slot_stride < 0)
+    return SOL_ATTN3D_ERR_UNSUPPORTED_SHAPE;
+  a.q = static_cast<const __nv_bfloat16*>(q);
+  a.k = static_cast<const __nv_bfloat16*>(cache->k);
+  a.v = static_cast<const __nv_bfloat16*>(cache->v);
+  a.key_mask = cache->key_mask;
+  a.mask_slot = cache->mask_slot_stride == 0 ? cache->capacity : cache->mask_slot_stride;
+  a.lens = lens;
+  a.slots = slots;
+  a.out = static_cast<__nv_bfloat16*>(out);
+  a.batch = batch;
+  a.pairs = heads / 2;
+  a.n_split = diff_step_splits(batch, a.pairs, cache->capacity);
+  a.n_slots = cache->n_slots;
+  a.capacity = cache->capacity;
+  a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)head_dim));
+  if (a.n_split > 1) {
+    if (workspace == nullptr || workspace_bytes < sol_attn3d_diff_step_workspace_bytes(batch, heads, head_dim, cache->capacity) ||
+        (reinterpret_cast<uintptr_t>(workspace) % kAlign) != 0)
+      return SOL_ATTN3D_ERR_NO_WORKSPACE;
+    a.partial = static_cast<float*>(workspace);
+  }
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const unsigned items = (unsigned)batch * (unsigned)a.pairs;
+  sol::diff_step_kernel<<<items * (unsigned)a.n_split, sol::kStepThreads, 0, st>>>(a);
+  if (cudaGetLastError() != cudaSuccess) return SOL_ATTN3D_ERR_CUDA;
+  if (a.n_split > 1) {
+    sol::diff_step_join_kernel<<<items, 128, 0, st>>>(a);
+    if (cudaGetLastError() != cudaSuccess) return SOL_ATTN3D_ERR_CUDA;
+  }
+  return SOL_ATTN3D_OK;
+}
+
+int sol_attn3d_linear_step(const void* q, const void* k, const void* v, void* out, const int64_t q_strides[2],
+                           const int64_t k_strides[2], const int64_t v_strides[2], const int64_t out_strides[2], int batch,
+                           int heads, int head_dim, const float* log_decay, float scale, const float* state_in,
+                           float* state_out, int64_t n_slots, const int32_t* slots, sol_attn3d_stream_t stream) {
+  if (batch < 0 || heads < 1 || head_dim < 1 || n_slots < 0 || !std::isfinite(scale)) return SOL_ATTN3D_ERR_INVALID_ARG;
+  if ((head_dim != 64 && head_dim != 128) || heads > 65535) return SOL_ATTN3D_ERR_UNSUPPORTED_SHAPE;
+  const long long ctas = (long long)batch * heads * (head_dim / 32);
+  if (ctas >= (1ll << 31)) return SOL_ATTN3D_ERR_UNSUPPORTED_SHAPE;
+  if (batch == 0) return SOL_ATTN3D_OK;
+  if (slots == nullptr && n_slots < batch) return SOL_ATTN3D_ERR_INVALID_ARG;
+  const void* x[3] = {q, k, v};
+  const int64_t* st[4] = {q_strides, k_strides, v_strides, out_strides};
+  if (out == nullptr || !aligned16(out) || log_decay == nullptr || (reinterpret_cast<uintptr_t>(log_decay) & 3u) != 0 ||
+      (reinterpret_cast<uintptr_t>(slots) & 3u) != 0 || !aligned16(state_in) || !aligned16(state_out))
+    return SOL_ATTN3D_ERR_INVALID_ARG;
+  if (n_slots > 0 && (state_in == nullptr || state_out == nullptr)) return SOL_ATTN3D_ERR_INVALID_ARG;
+  sol::LinearStepArgs a{};
+  const long long dense = (long long)heads * head_dim;
+  for (int i = 0; i < 4; ++i) {
+    if (st[i] == nullptr) return SOL_ATTN3D_ERR_INVALID_ARG;
+    const long long r = st[i][0] == 0 ? dense : st[i][0], h = st[i][1] == 0 ? head_dim : st[i][1];
+    if (!stride_ok(r) || !stride_ok(h)) return SOL_ATTN3D_ERR_UNSUPPORTED_SHAPE;
+    if (i < 3) {
+      if (x[i] == nullptr || !aligned16(x[i]) || x[i] == out) return SOL_ATTN3D_ERR_INVALID_ARG;
+      a.x[i] = static_cast<const __nv_bfloat16*>(x[i]);
+      a.row[i] = r;
+      a.head[i] = h;
+    } else {
+      a.o_row = r;
+      a.o_head = h;
+    }
+  }
+  a.out = static_cast<__nv_bfloat16*>(out);
+  a.log_decay = log_decay;
+  a.scale = scale;
+  a.state_in = state_in;
+  a.state_out = state_out;
+  a.slots = slots;
+  a.batch = batch;
+  a.heads = heads;
+  a.n_slots = n_slots;
+  if (head_dim == 128) sol::linear_step_kernel<128><<<(unsigned)ctas, 128, 0, static_cast<cudaStream_t>(stream)>>>(a);
+  else                 sol::linear_step_kernel<64><<<(unsigned)ctas, 128, 0, static_cast<cudaStream_t>(stream)>>>(a);
+  return cudaGetLastError() == cudaSuccess ? SOL_ATTN3D_OK : SOL_ATTN3D_ERR_CUDA;
 }
 
 int sol_attn3d_set_profiling(sol_attn3d_plan_t p, int enable) {

@@ -2,6 +2,7 @@
 import ctypes
 
 import pytest
+import torch
 
 from paper_2609_35110_b200 import binding as B
 from paper_2609_35110_b200 import build as build_mod
@@ -46,6 +47,7 @@ def test_forward_diff_refusals():
         B.sol_attn3d_destroy(x)
 
 
+@pytest.mark.skipif(torch.cuda.is_available(), reason="with a device the call would go on to use the made-up pointers")
 def test_differential_workspace_leaves_the_builtin_scratch_limit_alone():
     """The scratch of sol_attn3d_forward_noalloc counts what the plain forward uses: a plan just under 32 MiB without the
     differential attention's few bytes stays accepted (it is refused for the missing device, not for its size)."""
@@ -61,3 +63,49 @@ def test_differential_workspace_leaves_the_builtin_scratch_limit_alone():
             break
         n -= 1
     assert total > 32 * 2 ** 20
+
+
+def _s2(a=0, b=0):
+    return (ctypes.c_int64 * 2)(a, b)
+
+
+def test_diff_step_refusals():
+    lib = B._lib()
+    w = _weights()
+
+    def call(q=16, lens=4, slots=None, out=64, batch=3, heads=4, head_dim=64, ws=None, nbytes=0, w=w, q_st=(0, 0), **kw):
+        c = B._KvCache(ctypes.sizeof(B._KvCache), 32, 48, (0, 0, 0), (0, 0, 0), 3, 4096, None, 0)
+        for k, v in kw.items():
+            setattr(c, k, (ctypes.c_int64 * 3)(*v) if k.endswith("k_strides") else v)
+        return lib.sol_attn3d_diff_step(q, _s2(*q_st), ctypes.byref(c), lens, slots, out, _s2(), batch, heads, head_dim,
+                                        ctypes.byref(w), ws, nbytes, None)
+
+    need = B.sol_attn3d_diff_step_workspace_bytes(3, 4, 64, 4096)
+    assert need > 0 and need % 256 == 0
+    assert call() == B.ERR_NO_WORKSPACE                                # everything else is in order
+    assert call(ws=256, nbytes=need - 1) == B.ERR_NO_WORKSPACE
+    assert call(ws=128, nbytes=need) == B.ERR_NO_WORKSPACE
+    assert call(batch=0, q=None, out=None, lens=None) == 0             # nothing to do
+    for bad in (dict(q=None), dict(q=8), dict(out=16), dict(out=None), dict(lens=None), dict(lens=6), dict(slots=2), dict(k=None),
+                dict(v=40), dict(batch=-1), dict(n_slots=-1), dict(capacity=-1), dict(size=8), dict(w=_weights(gain=4))):
+        assert call(**bad) == B.ERR_INVALID_ARG, bad
+    for bad in (dict(head_dim=128), dict(heads=3), dict(q_st=(257, 64)), dict(k_strides=(0, 260, 64)), dict(k_strides=(-8, 0, 0)),
+                dict(mask_slot_stride=-1), dict(batch=2 ** 30, heads=8)):
+        assert call(**bad) == B.ERR_UNSUPPORTED_SHAPE, bad
+    assert B.sol_attn3d_diff_step_workspace_bytes(3, 3, 64, 4096) == 0
+    assert B.sol_attn3d_diff_step_workspace_bytes(2000, 40, 64, 4096) == 0         # enough streams: no split
+
+
+def test_linear_step_refusals():
+    lib = B._lib()
+
+    def call(q=16, k=32, v=48, out=64, st=(0, 0), batch=2, heads=4, head_dim=64, decay=4, scale=1.0, a=16, b=16, n_slots=2, slots=4):
+        return lib.sol_attn3d_linear_step(q, k, v, out, _s2(), _s2(*st), _s2(), _s2(), batch, heads, head_dim, decay,
+                                          scale, a, b, n_slots, slots, None)
+
+    assert call(batch=0, q=None) == 0
+    for bad in (dict(q=None), dict(v=8), dict(out=32), dict(out=None), dict(decay=None), dict(decay=2), dict(scale=float("nan")),
+                dict(a=None), dict(b=8), dict(slots=6), dict(slots=None, n_slots=1), dict(batch=-1), dict(heads=0)):
+        assert call(**bad) == B.ERR_INVALID_ARG, bad
+    for bad in (dict(head_dim=96), dict(st=(257, 64)), dict(st=(-256, 64)), dict(batch=2 ** 30), dict(heads=70000)):
+        assert call(**bad) == B.ERR_UNSUPPORTED_SHAPE, bad
