@@ -466,6 +466,32 @@ int sol_attn3d_diff_step(const void* q, const int64_t q_strides[2], const sol_at
                          sol_attn3d_stream_t stream);
 
 /*
+ * Linear attention with a decay per head over the tokens of a plan: what stands in the place of Section 3.2's "SDPA" in a
+ * block with a recurrent state instead of a K/V cache (the paper has none).  Causal over the flat token order of every
+ * sequence (prefix tokens first), all heads independent, S a head_dim x head_dim state:
+ *     S_t = exp(log_decay[head]) * S_(t-1) + k_t^T v_t,      out_t = scale * q_t S_t
+ * A token whose key_mask byte is 0 adds nothing to the state (the decay still applies and its output row is computed).
+ *   q, k, v, out, key_mask   as for sol_attn3d_forward (head_dim 64 or 128, the plan's strides); q and k are taken as they
+ *                 are: run sol_attn3d_rope_qk or sol_attn3d_qknorm_rope first where the model rotates them.  K and V
+ *                 values at masked positions may be anything; values of the others must be finite.
+ *   log_decay     DEVICE, fp32 [heads], natural logarithm of the decay; values above 0 count as 0, -infinity forgets all.
+ *   state_in      DEVICE, fp32 [n_seqs][heads][head_dim][head_dim] (sequences in the caller's order), 16-byte aligned:
+ *                 the state before each sequence's first token; NULL = zeros.
+ *   state_out     the same shape: the state after each sequence's last token; NULL = not wanted.  May equal state_in.
+ *                 Both have the layout of sol_attn3d_linear_step.
+ *   linear_ws     DEVICE scratch, 256-byte aligned, at least sol_attn3d_linear_workspace_bytes(plan) bytes, which may be 0
+ *                 (then NULL is fine): states of the pieces that long sequences are cut into, written and read by every
+ *                 call.  Calls that may overlap on the GPU need one each.
+ * The plan's workspace must be bound (its rotated Q / K part is not used).  Deterministic; may be captured; one or two
+ * kernels.  Time-outs are reported by sol_attn3d_status.
+ * Errors: INVALID_ARG, NO_WORKSPACE, UNSUPPORTED_SHAPE, CUDA.
+ */
+size_t sol_attn3d_linear_workspace_bytes(sol_attn3d_plan_t plan);
+int sol_attn3d_forward_linear(sol_attn3d_plan_t plan, const void* q, const void* k, const void* v, void* out,
+                              const uint8_t* key_mask, const float* log_decay, float scale, const float* state_in,
+                              float* state_out, void* linear_ws, size_t linear_ws_bytes, sol_attn3d_stream_t stream);
+
+/*
  * Linear attention with a decay per head, one token per row: the recurrent form of sol_attn3d_forward_linear.  Every
  * (slot, head) has a state S of head_dim x head_dim fp32, S[i][j] for K dim i and V dim j:
  *     S' = exp(log_decay[head]) * S + k^T v,      out = scale * q S'

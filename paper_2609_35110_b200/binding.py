@@ -160,6 +160,10 @@ def _lib():
     lib.sol_attn3d_diff_step.argtypes = [vp, p64, ctypes.POINTER(_KvCache), vp, vp, vp, p64, i32, i32, i32,
                                          ctypes.POINTER(_DiffWeights), vp, ctypes.c_size_t, vp]
     lib.sol_attn3d_diff_step.restype = i32
+    lib.sol_attn3d_linear_workspace_bytes.argtypes = [vp]
+    lib.sol_attn3d_linear_workspace_bytes.restype = ctypes.c_size_t
+    lib.sol_attn3d_forward_linear.argtypes = [vp, vp, vp, vp, vp, vp, vp, ctypes.c_float, vp, vp, vp, ctypes.c_size_t, vp]
+    lib.sol_attn3d_forward_linear.restype = i32
     lib.sol_attn3d_linear_step.argtypes = [vp, vp, vp, vp, p64, p64, p64, p64, i32, i32, i32, vp, ctypes.c_float, vp, vp, i64,
                                            vp, vp]
     lib.sol_attn3d_linear_step.restype = i32
@@ -604,6 +608,32 @@ def sol_attn3d_diff_step(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.
     _check(_lib().sol_attn3d_diff_step(_ptr(q), _strides_of(q, head_dim), ctypes.byref(cache), _ptr(lens), _ptr(slots), _ptr(out),
                                        _strides_of(out, head_dim), batch, heads, head_dim, ctypes.byref(weights.struct),
                                        _ptr(workspace), nbytes, _stream(stream)), "sol_attn3d_diff_step")
+
+
+def sol_attn3d_linear_workspace_bytes(plan) -> int:
+    return int(_lib().sol_attn3d_linear_workspace_bytes(plan))
+
+
+def sol_attn3d_forward_linear(plan, q, k, v, out, key_mask, log_decay: torch.Tensor, scale: float,
+                              state_in: Optional[torch.Tensor] = None, state_out: Optional[torch.Tensor] = None,
+                              workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Causal linear attention with a decay per head over a plan; states fp32 [sequences, heads, D, D]."""
+    for t in (q, k, v, out):
+        if not t.is_cuda or t.dtype != torch.bfloat16:
+            raise ValueError("q, k, v, out must be CUDA bf16 tensors")
+    if key_mask is not None and (not key_mask.is_cuda or key_mask.dtype != torch.uint8 or not key_mask.is_contiguous()):
+        raise ValueError("key_mask must be a contiguous CUDA uint8 tensor")
+    heads, head_dim = q.shape[-2:]
+    for t in (state_in, state_out):
+        if t is not None and (not t.is_cuda or t.dtype != torch.float32 or not t.is_contiguous() or t.dim() != 4 or
+                              tuple(t.shape[1:]) != (heads, head_dim, head_dim)):
+            raise ValueError("states must be contiguous CUDA float32 tensors [sequences, heads, D, D]")
+    _check_decay(log_decay, heads)
+    _check_on_device(q, k, v, out, key_mask, log_decay, state_in, state_out, workspace)
+    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(_lib().sol_attn3d_forward_linear(plan, _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(key_mask), _ptr(log_decay),
+                                            ctypes.c_float(scale), _ptr(state_in), _ptr(state_out), _ptr(workspace), nbytes,
+                                            _stream(stream)), "sol_attn3d_forward_linear")
 
 
 def sol_attn3d_linear_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, log_decay: torch.Tensor,

@@ -13,6 +13,7 @@
 
 #include "attn_fwd_sm100.cuh"
 #include "device_types.cuh"
+#include "linear_attn_sm100.cuh"
 #include "prologue_kernels.cuh"
 #include "sparse_kernels.cuh"
 #include "step_kernels.cuh"
@@ -47,6 +48,8 @@ struct sol_attn3d_plan_s {
   int total_quad_work = 0;            // work items when CTA pairs serve 512-row query blocks
   int pair_mode = 1;                  // CTA pairs (cta_group::2) where they apply: head_dim 128, not block-sparse
   int total_ktiles = 0;
+  int lin_seg_tiles = 1;              // linear attention: tiles per piece of a sequence, pieces, pieces with a successor
+  long long lin_pieces = 0, lin_local = 0;
   std::vector<float2> tables;
   int tab_off[3] = {0, 0, 0};
 
@@ -120,7 +123,48 @@ cudaError_t raise_shared_memory_limits() {
   if (e == cudaSuccess)
     e = cudaFuncSetAttribute(sol::attn_fwd_kernel<128, 2, true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                              sol::AttnSmem<128, 2, true>::kDynBytes);
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute(sol::linear_attn_kernel<128, false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             sol::LinearSmem<128, false>::kDynBytes);
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute(sol::linear_attn_kernel<128, true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             sol::LinearSmem<128, true>::kDynBytes);
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute(sol::linear_attn_kernel<64, false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             sol::LinearSmem<64, false>::kDynBytes);
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute(sol::linear_attn_kernel<64, true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             sol::LinearSmem<64, true>::kDynBytes);
   return e;
+}
+
+// Linear attention: into how many pieces the sequences are cut.  Whole sequences need one launch and read K and V once;
+// pieces keep more SMs busy, but every piece with a successor has its K and V read twice (a launch for the state it adds,
+// then the main one) and a piece starts by summing its predecessors' states.  The cost counts tiles that an SM walks one
+// after another: a tile of the main launch is 1, of the state launch 0.6 (half the bytes and about half the work), starting a
+// piece 2, a predecessor's state 0.3, the extra launch 4.
+void choose_linear_segments(sol_attn3d_plan_t p) {
+  constexpr long long kSms = 148;
+  int longest = 1;
+  for (const SeqDev& q : p->sched) longest = std::max(longest, q.n_ktiles);
+  double best = 0.0;
+  for (int n = 1; n <= std::min(longest, 64); ++n) {
+    const int len = (longest + n - 1) / n;
+    long long pieces = 0, local = 0;
+    for (const SeqDev& q : p->sched) {
+      const long long segs = (q.n_ktiles + len - 1) / len;
+      pieces += segs * p->heads;
+      local += (segs - 1) * p->heads;
+    }
+    double cost = (double)((pieces + kSms - 1) / kSms) * (len + 2.0);
+    if (local > 0) cost += (double)((local + kSms - 1) / kSms) * (0.6 * len + 2.0) + 0.3 * (n - 1) + 4.0;
+    if (n == 1 || cost < best) {
+      best = cost;
+      p->lin_seg_tiles = len;
+      p->lin_pieces = pieces;
+      p->lin_local = local;
+    }
+  }
 }
 
 bool stride_ok(long long s) { return s > 0 && (s * 2) % 16 == 0 && (s * 2) < (1ll << 40); }
@@ -242,6 +286,7 @@ int build_plan(sol_attn3d_plan_t* out, const sol_attn3d_desc* d) {
     p->total_quad_work = (int)quad_work;
     p->total_ktiles = (int)ktiles;
     p->total_pairs = (int)pairs;
+    choose_linear_segments(p);
 
     // cos/sin tables, built in fp64 and rounded once to fp32
     size_t n_entries = 0;
@@ -1285,6 +1330,75 @@ int sol_attn3d_linear_step(const void* q, const void* k, const void* v, void* ou
   if (head_dim == 128) sol::linear_step_kernel<128><<<(unsigned)ctas, 128, 0, static_cast<cudaStream_t>(stream)>>>(a);
   else                 sol::linear_step_kernel<64><<<(unsigned)ctas, 128, 0, static_cast<cudaStream_t>(stream)>>>(a);
   return cudaGetLastError() == cudaSuccess ? SOL_ATTN3D_OK : SOL_ATTN3D_ERR_CUDA;
+}
+
+extern "C++" {
+namespace {
+template <int D>
+cudaError_t launch_linear(sol_attn3d_plan_t p, const CUtensorMap& tm_q, const CUtensorMap& tm_k, const CUtensorMap& tm_v,
+                          const sol::LinearParams& lp, cudaStream_t st) {
+  if (p->lin_local > 0) {
+    sol::linear_attn_kernel<D, true><<<(unsigned)p->lin_local, sol::kLinThreads, sol::LinearSmem<D, true>::kDynBytes, st>>>(
+        tm_q, tm_k, tm_v, lp);
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+    ++p->launches;
+  }
+  sol::linear_attn_kernel<D, false><<<(unsigned)p->lin_pieces, sol::kLinThreads, sol::LinearSmem<D, false>::kDynBytes, st>>>(
+      tm_q, tm_k, tm_v, lp);
+  const cudaError_t e = cudaGetLastError();
+  if (e == cudaSuccess) ++p->launches;
+  return e;
+}
+}  // namespace
+}  // extern "C++"
+
+size_t sol_attn3d_linear_workspace_bytes(sol_attn3d_plan_t p) {
+  // one state per piece with a successor, and a copy of every initial state
+  if (p == nullptr || p->lin_local == 0) return 0;
+  return align_up(((size_t)p->lin_local + (size_t)p->n_seqs * p->heads) * p->head_dim * p->head_dim * sizeof(float));
+}
+
+int sol_attn3d_forward_linear(sol_attn3d_plan_t p, const void* q, const void* k, const void* v, void* out,
+                              const uint8_t* key_mask, const float* log_decay, float scale, const float* state_in,
+                              float* state_out, void* linear_ws, size_t linear_ws_bytes, sol_attn3d_stream_t stream) {
+  if (p == nullptr || q == nullptr || k == nullptr || v == nullptr || out == nullptr || log_decay == nullptr)
+    return SOL_ATTN3D_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || !aligned16(state_in) || !aligned16(state_out) ||
+      (reinterpret_cast<uintptr_t>(log_decay) & 3u) != 0 || !std::isfinite(scale))
+    return SOL_ATTN3D_ERR_INVALID_ARG;
+  if (out == q || out == k || out == v) return SOL_ATTN3D_ERR_INVALID_ARG;
+  if (p->lin_pieces >= (1ll << 31)) return SOL_ATTN3D_ERR_UNSUPPORTED_SHAPE;
+  if (p->ws == nullptr || p->encode == nullptr) return SOL_ATTN3D_ERR_NO_WORKSPACE;
+  if (p->lin_local > 0 && (linear_ws == nullptr || linear_ws_bytes < sol_attn3d_linear_workspace_bytes(p) ||
+                           (reinterpret_cast<uintptr_t>(linear_ws) % kAlign) != 0))
+    return SOL_ATTN3D_ERR_NO_WORKSPACE;
+  CUtensorMap tm_q, tm_k, tm_v;
+  int rc = encode_map(p->encode, p, &tm_q, q, p->sq);
+  if (rc == SOL_ATTN3D_OK) rc = encode_map(p->encode, p, &tm_k, k, p->sk);
+  if (rc == SOL_ATTN3D_OK) rc = encode_map(p->encode, p, &tm_v, v, p->sv);
+  if (rc != SOL_ATTN3D_OK) return rc;
+  sol::LinearParams lp{};
+  lp.seqs = reinterpret_cast<const SeqDev*>(p->ws + p->off_seqs);
+  lp.n_seqs = p->n_seqs;
+  lp.heads = p->heads;
+  lp.seg_tiles = p->lin_seg_tiles;
+  lp.key_mask = key_mask;
+  lp.log_decay = log_decay;
+  lp.scale = scale;
+  lp.state_in = state_in;
+  lp.state_out = state_out;
+  lp.local = static_cast<float*>(linear_ws);
+  lp.initial = lp.local + (size_t)p->lin_local * p->head_dim * p->head_dim;
+  lp.out = static_cast<__nv_bfloat16*>(out);
+  lp.o_tok_stride = p->so.tok;
+  lp.o_head_stride = p->so.head;
+  lp.status = reinterpret_cast<unsigned int*>(p->ws + p->off_status);
+  lp.wait_limit_ns = p->wait_limit_ns;
+  p->launches = 0;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const cudaError_t e = p->head_dim == 128 ? launch_linear<128>(p, tm_q, tm_k, tm_v, lp, st) : launch_linear<64>(p, tm_q, tm_k, tm_v, lp, st);
+  return e == cudaSuccess ? SOL_ATTN3D_OK : fail_cuda(p, e);
 }
 
 int sol_attn3d_set_profiling(sol_attn3d_plan_t p, int enable) {

@@ -109,3 +109,23 @@ def test_linear_step_refusals():
         assert call(**bad) == B.ERR_INVALID_ARG, bad
     for bad in (dict(head_dim=96), dict(st=(257, 64)), dict(st=(-256, 64)), dict(batch=2 ** 30), dict(heads=70000)):
         assert call(**bad) == B.ERR_UNSUPPORTED_SHAPE, bad
+
+
+def test_forward_linear_refusals_and_scratch_size():
+    lib = B._lib()
+    p = B.sol_attn3d_plan(1, 4, 64, 4, 8, 8, 0, (16, 24, 24))
+
+    def call(plan=p, q=16, k=32, v=48, out=64, decay=4, scale=1.0, a=None, b=None):
+        return lib.sol_attn3d_forward_linear(plan, q, k, v, out, None, decay, scale, a, b, None, 0, None)
+
+    assert call() == B.ERR_NO_WORKSPACE                                # no workspace bound; everything else is in order
+    for bad in (dict(plan=None), dict(q=None), dict(k=8), dict(out=16), dict(out=None), dict(decay=None), dict(decay=6),
+                dict(scale=float("inf")), dict(a=8), dict(b=24)):
+        assert call(**bad) == B.ERR_INVALID_ARG, bad
+    assert B.sol_attn3d_linear_workspace_bytes(p) == 0                 # two tiles: one piece per head
+    B.sol_attn3d_destroy(p)
+    # a long sequence with few heads is cut; its scratch holds a state per piece with a successor and per (sequence, head)
+    p = B.sol_attn3d_plan_ex([(256, 5, 30, 20)], 2, 128, (32, 48, 48))
+    n = B.sol_attn3d_linear_workspace_bytes(p)
+    assert n % (128 * 128 * 4) == 0 and n // (128 * 128 * 4) > 4
+    B.sol_attn3d_destroy(p)
