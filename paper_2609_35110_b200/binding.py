@@ -70,6 +70,9 @@ class _KvCache(ctypes.Structure):
     ]
 
 
+_KV_CACHE_SIZE = ctypes.sizeof(_KvCache)
+
+
 # error codes (mirror include/sol_attn3d.h)
 OK = 0
 ERR_INVALID_ARG = -1
@@ -252,13 +255,13 @@ def sol_attn3d_set_workspace(plan, workspace: torch.Tensor) -> None:
 
 
 def _ptr(t: Optional[torch.Tensor]):
-    return None if t is None else ctypes.c_void_p(t.data_ptr())
+    return None if t is None else t.data_ptr()
 
 
-def _stream(stream) -> ctypes.c_void_p:
-    if stream is None:
-        stream = torch.cuda.current_stream()
-    return ctypes.c_void_p(stream.cuda_stream)
+def _stream(stream):
+    if stream is None:                   # the raw handle: torch.cuda.current_stream() builds a Stream object every time
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    return stream.cuda_stream
 
 
 def sol_attn3d_forward(plan, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor,
@@ -380,14 +383,16 @@ def sol_attn3d_forward_scatter(plan, q, k, v, key_mask, dst: Sequence[int], tok_
            "sol_attn3d_forward_scatter")
 
 
+_I64x2, _I64x3 = ctypes.c_int64 * 2, ctypes.c_int64 * 3
+
+
 def _strides_of(t: torch.Tensor, head_dim: int):
     """(token, head) element strides of a [tokens, heads, head_dim] tensor whose head_dim axis is contiguous."""
-    if t.dim() != 3 or t.shape[2] != head_dim or t.stride(2) != 1:
+    shape, st = t.shape, t.stride()
+    if len(shape) != 3 or shape[2] != head_dim or st[2] != 1:
         raise ValueError("expected [tokens, heads, head_dim] with contiguous head_dim")
     # the stride torch reports for an axis of extent 0 or 1 is arbitrary: use the dense value there
-    tok = t.stride(0) if t.shape[0] > 1 else t.shape[1] * head_dim
-    head = t.stride(1) if t.shape[1] > 1 else head_dim
-    return (ctypes.c_int64 * 2)(tok, head)
+    return _I64x2(st[0] if shape[0] > 1 else shape[1] * head_dim, st[1] if shape[1] > 1 else head_dim)
 
 
 def sol_attn3d_exchange_pack_qkv(q, k, v, n_ranks: int, dst: Sequence[int], dst_row0: int = 0, stream=None,
@@ -562,9 +567,10 @@ def sol_attn3d_forward_diff(plan, q, k, v, out, key_mask, weights: sol_attn3d_di
 
 def _check_on_device(*tensors) -> None:
     """The library launches on the current device: refuse tensors that live on another one."""
+    here = torch._C._cuda_getDevice()
     for t in tensors:
-        if t is not None and t.device.index != torch.cuda.current_device():
-            raise ValueError(f"tensor on {t.device}, current device is cuda:{torch.cuda.current_device()}")
+        if t is not None and t.get_device() != here:
+            raise ValueError(f"tensor on {t.device}, current device is cuda:{here}")
 
 
 def _check_index(t: Optional[torch.Tensor], n: int, name: str) -> None:
@@ -576,12 +582,12 @@ def sol_attn3d_diff_step_workspace_bytes(batch: int, heads: int, head_dim: int, 
     return int(_lib().sol_attn3d_diff_step_workspace_bytes(batch, heads, head_dim, capacity))
 
 
-def _cache_strides(t: torch.Tensor, batch_like):
-    slots, cap, heads, head_dim = batch_like
-    if t.dim() != 4 or tuple(t.shape) != tuple(batch_like) or t.stride(3) != 1:
+def _cache_strides(t: torch.Tensor, shape):
+    st = t.stride()
+    if t.shape != shape or st[3] != 1:
         raise ValueError("caches: [slots, capacity, heads, head_dim] of one shape with contiguous head_dim")
     # the stride torch reports for an axis of extent 0 or 1 is arbitrary: 0 asks for the dense value there
-    return (ctypes.c_int64 * 3)(*(t.stride(i) if t.shape[i] > 1 else 0 for i in range(3)))
+    return _I64x3(st[0] if shape[0] > 1 else 0, st[1] if shape[1] > 1 else 0, st[2] if shape[2] > 1 else 0)
 
 
 def sol_attn3d_diff_step(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, lens: torch.Tensor, out: torch.Tensor,
@@ -596,15 +602,15 @@ def sol_attn3d_diff_step(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.
         raise ValueError("q, out: [batch, heads, 64]; caches: [slots, capacity, heads, 64]")
     _check_index(lens, batch, "lens")
     _check_index(slots, batch, "slots")
-    n_slots, capacity = k_cache.shape[:2]
+    shape = k_cache.shape
     if key_mask is not None and (not key_mask.is_cuda or key_mask.dtype != torch.uint8 or not key_mask.is_contiguous() or
-                                 tuple(key_mask.shape) != (n_slots, capacity)):
+                                 key_mask.shape != shape[:2]):
         raise ValueError("key_mask must be a contiguous CUDA uint8 tensor [slots, capacity]")
     _check_pairs(weights, heads)
     _check_on_device(q, k_cache, v_cache, lens, out, workspace, key_mask, slots, *weights.tensors)
-    cache = _KvCache(ctypes.sizeof(_KvCache), k_cache.data_ptr(), v_cache.data_ptr(), _cache_strides(k_cache, k_cache.shape),
-                     _cache_strides(v_cache, k_cache.shape), n_slots, capacity, None if key_mask is None else key_mask.data_ptr(), 0)
-    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    cache = _KvCache(_KV_CACHE_SIZE, k_cache.data_ptr(), v_cache.data_ptr(), _cache_strides(k_cache, shape),
+                     _cache_strides(v_cache, shape), shape[0], shape[1], _ptr(key_mask), 0)
+    nbytes = 0 if workspace is None else workspace.nbytes
     _check(_lib().sol_attn3d_diff_step(_ptr(q), _strides_of(q, head_dim), ctypes.byref(cache), _ptr(lens), _ptr(slots), _ptr(out),
                                        _strides_of(out, head_dim), batch, heads, head_dim, ctypes.byref(weights.struct),
                                        _ptr(workspace), nbytes, _stream(stream)), "sol_attn3d_diff_step")
@@ -644,16 +650,16 @@ def sol_attn3d_linear_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, ou
     for t in (q, k, v, out):
         if not t.is_cuda or t.dtype != torch.bfloat16 or t.shape != q.shape:
             raise ValueError("q, k, v, out must be CUDA bf16 tensors of one shape")
+    want = (state_in.shape[0], heads, head_dim, head_dim)
     for t in (state_in, state_out):
-        if not t.is_cuda or t.dtype != torch.float32 or not t.is_contiguous() or t.dim() != 4 or \
-                tuple(t.shape[1:]) != (heads, head_dim, head_dim) or t.shape != state_in.shape:
+        if not t.is_cuda or t.dtype != torch.float32 or not t.is_contiguous() or t.shape != want:
             raise ValueError("states must be contiguous CUDA float32 tensors [slots, heads, D, D]")
     _check_decay(log_decay, heads)
     _check_index(slots, batch, "slots")
     _check_on_device(q, k, v, out, log_decay, state_in, state_out, slots)
     _check(_lib().sol_attn3d_linear_step(_ptr(q), _ptr(k), _ptr(v), _ptr(out), _strides_of(q, head_dim), _strides_of(k, head_dim),
                                          _strides_of(v, head_dim), _strides_of(out, head_dim), batch, heads, head_dim,
-                                         _ptr(log_decay), ctypes.c_float(scale), _ptr(state_in), _ptr(state_out),
+                                         _ptr(log_decay), scale, _ptr(state_in), _ptr(state_out),
                                          state_in.shape[0], _ptr(slots), _stream(stream)), "sol_attn3d_linear_step")
 
 

@@ -655,7 +655,8 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
     // =========================================================== MMA issuer
     {
       // The whole warp runs this loop (convergent); one elected lane issues each tcgen05 instruction.
-      constexpr uint32_t idesc_qk = idesc_bf16_f32(128 * kCtas, 128, false);
+      // differential attention: Q~ and K~ are fp16 (see rope_qk_kernel), P and V bf16 as everywhere
+      constexpr uint32_t idesc_qk = kDiff ? idesc_f16_f32(128 * kCtas, 128) : idesc_bf16_f32(128 * kCtas, 128, false);
       constexpr uint32_t idesc_pv = idesc_bf16_f32(128 * kCtas, D, true);
       bool ok = true;
       const uint32_t v_lbo = p.v_lbo, v_sbo = p.v_sbo;

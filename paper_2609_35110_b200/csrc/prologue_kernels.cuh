@@ -5,6 +5,7 @@
 
 #include "device_types.cuh"
 #include "exchange_kernels.cuh"
+#include "ptx_sm100.cuh"
 
 namespace sol {
 
@@ -97,7 +98,10 @@ struct RopeArgs {
   unsigned int* status;       // status word (written by the index checks of the debug build only)
 };
 
-template <bool kNorm>
+// kF16: the rotated values are rounded to fp16 instead of bf16 (differential attention: the difference of two softmax maps
+// amplifies the error that rounding Q~ and K~ puts into the scores, and three more bits cost nothing on the tensor cores).
+// Magnitudes above 65504 saturate.
+template <bool kNorm, bool kF16 = false>
 __global__ void __launch_bounds__(256, 3) rope_qk_kernel(const RopeArgs a) {
   const int chunks = a.g.head_dim >> 3;          // 16-byte chunks per head row (8 or 16: divides the warp)
   const int heads_per_pass = blockDim.x / chunks;
@@ -216,8 +220,12 @@ __global__ void __launch_bounds__(256, 3) rope_qk_kernel(const RopeArgs a) {
               re = f[2 * u] * cs[u].x - f[2 * u + 1] * cs[u].y;
               ro = f[2 * u] * cs[u].y + f[2 * u + 1] * cs[u].x;
             }
-            const __nv_bfloat162 r2 = __floats2bfloat162_rn(re, ro);
-            o[u] = *reinterpret_cast<const uint32_t*>(&r2);
+            if (kF16) {
+              o[u] = pack_f16x2_sat(re, ro);
+            } else {
+              const __nv_bfloat162 r2 = __floats2bfloat162_rn(re, ro);
+              o[u] = *reinterpret_cast<const uint32_t*>(&r2);
+            }
           }
           if (h < a.head_end) *reinterpret_cast<uint4*>(dst + (long long)h * a.g.head_dim) = make_uint4(o[0], o[1], o[2], o[3]);
         }

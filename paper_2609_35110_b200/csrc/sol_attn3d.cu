@@ -367,7 +367,7 @@ bool aligned16(const void* x) { return (reinterpret_cast<uintptr_t>(x) & 15u) ==
 
 int launch_rope(sol_attn3d_plan_t p, const unsigned char* ws, const void* q, const void* k, void* qr, void* kr,
                 const float* q_gain, const float* k_gain, float eps, cudaStream_t st, int head_begin = 0,
-                int head_end = 0) {
+                int head_end = 0, bool f16 = false) {
   sol::RopeArgs a{};
   a.gain[0] = q_gain;
   a.gain[1] = k_gain;
@@ -398,7 +398,8 @@ int launch_rope(sol_attn3d_plan_t p, const unsigned char* ws, const void* q, con
     if (n_heads % d == 0) { hpp = d; break; }
   const int threads = chunks * hpp;
   const long long blocks = std::min<long long>(p->total_tokens, 148ll * 16);
-  if (norm) sol::rope_qk_kernel<true><<<(unsigned)blocks, threads, 0, st>>>(a);
+  if (f16)  sol::rope_qk_kernel<false, true><<<(unsigned)blocks, threads, 0, st>>>(a);
+  else if (norm) sol::rope_qk_kernel<true><<<(unsigned)blocks, threads, 0, st>>>(a);
   else                                        sol::rope_qk_kernel<false><<<(unsigned)blocks, threads, 0, st>>>(a);
   const cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return fail_cuda(p, e);
@@ -1142,8 +1143,8 @@ int sol_attn3d_forward_diff(sol_attn3d_plan_t p, const void* q, const void* k, c
   }
   if (p->prof && (e = cudaEventRecord(p->ev[1], st)) != cudaSuccess) return fail_cuda(p, e);
 
-  // (2) rotary prologue over all heads, as for the plain forward
-  rc = launch_rope(p, ws, q, k, ws + p->off_qrot, ws + p->off_krot, nullptr, nullptr, 0.f, st);
+  // (2) rotary prologue over all heads, rounding to fp16
+  rc = launch_rope(p, ws, q, k, ws + p->off_qrot, ws + p->off_krot, nullptr, nullptr, 0.f, st, 0, 0, true);
   if (rc != SOL_ATTN3D_OK) return rc;
   if (query_mask != nullptr) {
     uint8_t* flags = ws + p->off_pairs;

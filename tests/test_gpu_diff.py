@@ -77,6 +77,20 @@ def test_forward_diff_matches_the_oracle(seqs, heads, kw):
     attn.close()
 
 
+@pytest.mark.parametrize("n", [2, 3, 7])
+def test_maps_that_nearly_cancel(n):
+    """Few keys and lambda close to 1: the norm blows up what is left of two nearly equal maps.  The output's own rounding
+    aside, the error is that of the two maps (P rounded to bf16, scores from fp16 operands) times the condition number."""
+    from paper_2609_35110_b200 import binding as B
+    attn, (q, k, v), w, o = make([(0, 1, 1, n)], 40, 30 + n, lambda_init=0.8)
+    out = torch.empty_like(q)
+    B.sol_attn3d_forward_diff(attn.plan, q, k, v, out, None, w)
+    torch.cuda.synchronize()
+    ref, cond = dlo.diff_oracle(q, k, v, [(0, 1, 1, n)], ROPE, 10000.0, **o)
+    check(out, ref, cond)
+    attn.close()
+
+
 def test_masks_empty_rows_and_query_mask():
     from paper_2609_35110_b200 import binding as B
     seqs = [(200, 3, 8, 16), (40, 2, 5, 5), (0, 1, 9, 30)]
