@@ -18,12 +18,16 @@
 // is fp32 and carried from tile to tile, keeps about 17 bits of every factor instead of 8; the running state itself is
 // never rounded below fp32 and never accumulated in tensor memory for longer than one tile.
 //
-// Warp roles:
-//   warps 0-3   thread = query row: S-scores -> P, and the output epilogue
-//   warps 4-7   thread = token row: K -> K' (hi in place of K, lo beside it); thread = K dim: row of the state
-//   warp  8     TMA producer;   warp 9: MMA issuer, owns the tensor memory
-// Tensor memory (512 columns): scores / P [0,128), P V [128,256), Q S [256,384), K'^T V [384,512).
-// Bound by HBM: 4 x 128 x D x 2 bytes per tile and head against 5 (4 and the lo half) small products.
+// Warp roles (the state launch has only the second group, the producer and the issuer):
+//   8 warps   two threads per query row: scores -> P (column blocks of 32 alternate between them), output epilogue
+//   8 warps   K -> K', transposed on the way (ldmatrix) into tensor memory; two threads per K dim: a row of the state
+//   1 warp    TMA producer;   1 warp: MMA issuer, owns the tensor memory;   1 warp: TMA stores of the outputs
+// Tensor memory (512 columns): scores / P [0,128); K' hi | lo [128,256), replaced by P V; Q S [256,384); K'^T V [384,512).
+//
+// Bound by HBM: 4 x 128 x D x 2 bytes per tile and head (2.9 us at D = 128 with every SM streaming) against 5 small
+// products (4 and the lo half).  Next comes shared-memory bandwidth, which operands of 128-wide products use up as fast as
+// the tensor core: so K' is a tensor-memory operand, outputs leave through the V tile's own space with a TMA store, and
+// nothing is staged twice.
 #pragma once
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -52,51 +56,41 @@ struct LinearParams {
   unsigned long long wait_limit_ns;
 };
 
-constexpr int kLinThreads = 320;
+// Compute warps, then the producer, the MMA issuer and (main launch) the store warp and an idle one, which completes a
+// warpgroup.  Registers of the main launch: 640 threads x 96 = 256 x 88 + 256 x 128 + 128 x 48.
+constexpr int linear_threads(bool state_only) { return state_only ? 320 : 640; }
 
 template <int D, bool kStateOnly>
 struct LinearSmem {
   static constexpr int kTile = 128 * D * 2;
   static constexpr int kHalves = D / 64;
-  static constexpr int kQStages = kStateOnly ? 0 : D == 128 ? 1 : 2;
-  static constexpr int kStages = D == 128 ? 2 : 3;
+  static constexpr int kQStages = kStateOnly ? 0 : 2;
+  static constexpr int kStages = D == 128 ? (kStateOnly ? 3 : 2) : 4;
   static constexpr int kOffQ = 0;
-  static constexpr int kOffLo = kOffQ + kQStages * kTile;
-  static constexpr int kOffK = kOffLo + kTile;
+  static constexpr int kOffK = kOffQ + kQStages * kTile;
   static constexpr int kOffV = kOffK + kStages * kTile;
   static constexpr int kOffSt = kOffV + kStages * kTile;                 // bf16 copy of the state, laid out like V
   static constexpr int kOffDec = kOffSt + (kStateOnly ? 0 : D * D * 2);  // powers of the decay: [128 + d], zero for d < 0
   static constexpr int kOffBars = kOffDec + 264 * 4;
-  static constexpr int kNumBars = 2 * kQStages + 4 * kStages + 8;
+  static constexpr int kNumBars = 2 * kQStages + 4 * kStages + 9;
   static constexpr int kOffTmemPtr = kOffBars + kNumBars * 8;
   static constexpr int kBytes = kOffTmemPtr + 16;
   static constexpr int kDynBytes = kBytes + 1024;
 };
 
-// kind::f16 descriptor with both operands MN-major (bits 15 and 16)
-__host__ __device__ constexpr uint32_t idesc_bf16_f32_tt(int M, int N) { return idesc_bf16_f32(M, N, true) | (1u << 15); }
-
-__device__ __forceinline__ uint4 ld_shared_v4(uint32_t addr) {
-  uint4 v;
-  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr));
-  return v;
-}
-__device__ __forceinline__ void st_shared_v4(uint32_t addr, const uint4& v) {
-  asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
-}
-
 template <int D, bool kStateOnly>
-__global__ void __launch_bounds__(kLinThreads, 1)
+__global__ void __launch_bounds__(linear_threads(kStateOnly), 1)
 linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
-                   const __grid_constant__ CUtensorMap tm_v, const LinearParams p) {
+                   const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_o, const LinearParams p) {
   using L = LinearSmem<D, kStateOnly>;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw_addr = smem_u32(smem_raw);
   const uint32_t sbase = (raw_addr + 1023u) & ~1023u;
   uint8_t* smem = smem_raw + (sbase - raw_addr);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  constexpr int kFirstB = kStateOnly ? 0 : 8, kTma = kFirstB + 8, kMma = kTma + 1, kStore = kTma + 2;
 
-  const uint32_t sQ = sbase + L::kOffQ, sLo = sbase + L::kOffLo, sK = sbase + L::kOffK, sV = sbase + L::kOffV, sSt = sbase + L::kOffSt;
+  const uint32_t sQ = sbase + L::kOffQ, sK = sbase + L::kOffK, sV = sbase + L::kOffV, sSt = sbase + L::kOffSt;
   float* dec = reinterpret_cast<float*>(smem + L::kOffDec) + 128;       // dec[d] = g^d, d in [-128, 128]
   const uint32_t bars = sbase + L::kOffBars;
   constexpr int kQB = 2 * L::kQStages, kSB = kQB + 4 * L::kStages;
@@ -108,7 +102,7 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
   auto bar_v_empty = [&](int s) { return bars + 8u * (kQB + 3 * L::kStages + s); };
   const uint32_t bar_s_full = bars + 8u * (kSB + 0), bar_p_full = bars + 8u * (kSB + 1), bar_kp_full = bars + 8u * (kSB + 2),
                  bar_t_full = bars + 8u * (kSB + 3), bar_st_full = bars + 8u * (kSB + 4), bar_o_full = bars + 8u * (kSB + 5),
-                 bar_o_empty = bars + 8u * (kSB + 6), bar_drain = bars + 8u * (kSB + 7);
+                 bar_o_empty = bars + 8u * (kSB + 6), bar_o_staged = bars + 8u * (kSB + 7), bar_drain = bars + 8u * (kSB + 8);
   volatile uint32_t* tmem_ptr_smem = reinterpret_cast<volatile uint32_t*>(smem + L::kOffTmemPtr);
 
   // ---- which piece: sequences in schedule order, then segments, heads fastest (CTAs that run together read neighbouring
@@ -130,27 +124,28 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
   const unsigned long long limit = p.wait_limit_ns;
   const int tok0 = (int)sq.tok_start;
 
-  if (warp == 8 && lane == 0) {
+  if (warp == kTma && lane == 0) {
     for (int s = 0; s < L::kQStages; ++s) { mbar_init(bar_q_full(s), 1); mbar_init(bar_q_empty(s), 1); }
     for (int s = 0; s < L::kStages; ++s) {
       mbar_init(bar_k_full(s), 1); mbar_init(bar_k_empty(s), 1);
       mbar_init(bar_v_full(s), 1); mbar_init(bar_v_empty(s), 1);
     }
     mbar_init(bar_s_full, 1);
-    mbar_init(bar_p_full, 4);
-    mbar_init(bar_kp_full, 4);
+    mbar_init(bar_p_full, 8);
+    mbar_init(bar_kp_full, 8);
     mbar_init(bar_t_full, 1);
-    mbar_init(bar_st_full, 4);
+    mbar_init(bar_st_full, 8);
     mbar_init(bar_o_full, 1);
-    mbar_init(bar_o_empty, 4);
+    mbar_init(bar_o_empty, 8);
+    mbar_init(bar_o_staged, 8);
     mbar_init(bar_drain, 1);
     fence_mbar_init();
-    if (!kStateOnly) prefetch_tensormap(&tm_q);
+    if (!kStateOnly) { prefetch_tensormap(&tm_q); prefetch_tensormap(&tm_o); }
     prefetch_tensormap(&tm_k);
     prefetch_tensormap(&tm_v);
   }
   if (threadIdx.x == 0) tmem_ptr_smem[1] = *reinterpret_cast<volatile unsigned int*>(p.status);
-  if (warp == 9) { tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_ptr_smem)), 512); tmem_relinquish(); }
+  if (warp == kMma) { tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_ptr_smem)), 512); tmem_relinquish(); }
   const double ld = fmin((double)__ldg(p.log_decay + head), 0.0);
   if (threadIdx.x < 257) {
     const int d = (int)threadIdx.x - 128;
@@ -162,57 +157,66 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
   const uint32_t tmem_base = tmem_ptr_smem[0];
   if (tmem_ptr_smem[1] != 0) {                             // a fault recorded earlier stops later CTAs at the door
     __syncthreads();
-    if (warp == 9) tmem_dealloc(tmem_base, 512);
+    if (warp == kMma) tmem_dealloc(tmem_base, 512);
     return;
   }
   constexpr uint32_t kColS = 0, kColO = 128, kColQS = 256, kColT = 384;
 
-  if (warp < 4) {
+  if (warp < kFirstB) {
     if constexpr (!kStateOnly) {
-      // =========================================================== scores -> P, outputs; thread = query row
-      const int row = warp * 32 + lane;
-      const uint32_t tm = tmem_base + (static_cast<uint32_t>(warp * 32) << 16);
-      const float g1 = dec[row + 1];
+      // =========================================================== scores -> P, outputs; two threads per query row
+      setmaxnreg_dec<88>();
+      const int wq = warp & 3, half = warp >> 2;
+      const int row = wq * 32 + lane;
+      const uint32_t tm = tmem_base + (static_cast<uint32_t>(wq * 32) << 16);
+      const float g1 = p.scale * dec[row + 1];
+      const float* dec_row = dec + row;
       bool ok = true;
       for (int c = 0; c < n_tiles; ++c) {
         const int t0 = (tile0 + c) * 128;
         const int m = min(128, sq.n_tokens - t0);
-        uint32_t bits[4] = {~0u, ~0u, ~0u, ~0u};
-        if (p.key_mask != nullptr || m < 128) {
+        const bool mixed = p.key_mask != nullptr || m < 128;
+        uint32_t bits[2] = {~0u, ~0u};                        // of this thread's two column blocks
+        if (mixed) {
 #pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            bool valid = 32 * w + lane < m;
-            if (valid && p.key_mask != nullptr) valid = p.key_mask[sq.tok_start + t0 + 32 * w + lane] != 0;
-            bits[w] = __ballot_sync(0xffffffffu, valid);
+          for (int b = 0; b < 2; ++b) {
+            const int j = 32 * (2 * b + half) + lane;
+            bool valid = j < m;
+            if (valid && p.key_mask != nullptr) valid = p.key_mask[sq.tok_start + t0 + j] != 0;
+            bits[b] = __ballot_sync(0xffffffffu, valid);
           }
         }
         ok = __all_sync(0xffffffffu, mbar_wait(bar_s_full, c & 1, limit));
         if (!ok) break;
         tc_fence_after();
+        // P of column block cb replaces the scores of that block, in its first 16 columns: a block is read and written by
+        // one warp alone.  Blocks right of the diagonal are zero, left of it every decay exponent is positive.
 #pragma unroll
-        for (int cb = 0; cb < 4; ++cb) {
+        for (int b = 0; b < 2; ++b) {
+          const int cb = 2 * b + half;
           uint32_t pk[16];
-          if (cb <= warp) {
+          if (cb <= wq) {
             uint32_t s[32];
             tmem_ld32(tm + kColS + cb * 32, s);
             tmem_wait_ld();
+            const float* d = dec_row - cb * 32;
+            if (cb < wq && !mixed) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              float f[2];
+              for (int e = 0; e < 16; ++e)
+                pk[e] = pack_bf16x2(__uint_as_float(s[2 * e]) * d[-2 * e], __uint_as_float(s[2 * e + 1]) * d[-2 * e - 1]);
+            } else {
+              const int last = row - cb * 32;                  // columns beyond it lie above the diagonal
+              const uint32_t on = bits[b] & (last >= 31 ? ~0u : (2u << last) - 1u);
 #pragma unroll
-              for (int u = 0; u < 2; ++u) {
-                const int j = cb * 32 + 2 * e + u;
-                const bool on = j <= row && ((bits[cb] >> (2 * e + u)) & 1u) != 0;
-                f[u] = on ? __uint_as_float(s[2 * e + u]) * dec[row - j] : 0.f;
-              }
-              pk[e] = pack_bf16x2(f[0], f[1]);
+              for (int e = 0; e < 16; ++e)
+                pk[e] = pack_bf16x2((on >> (2 * e)) & 1u ? __uint_as_float(s[2 * e]) * d[-2 * e] : 0.f,
+                                    (on >> (2 * e + 1)) & 1u ? __uint_as_float(s[2 * e + 1]) * d[-2 * e - 1] : 0.f);
             }
           } else {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) pk[e] = 0u;                       // above the diagonal
+            for (int e = 0; e < 16; ++e) pk[e] = 0u;
           }
-          // columns [16 cb, 16 cb + 16) hold scores of blocks <= cb / 2, which are in registers or done with
-          tmem_st16(tm + kColS + cb * 16, pk);
+          tmem_st16(tm + kColS + cb * 32, pk);
         }
         tmem_wait_st();
         tc_fence_before();
@@ -222,89 +226,90 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         ok = __all_sync(0xffffffffu, mbar_wait(bar_o_full, c & 1, limit));
         if (!ok) break;
         tc_fence_after();
-        const bool store = row < m;
-        // even lanes store 32 bytes of their own row, then of their neighbour's, and so do odd ones: whole sectors
-        const int peer_row = t0 + (row ^ 1);
-        __nv_bfloat16* mine = p.out + (sq.tok_start + t0 + row) * p.o_tok_stride + (long long)head * p.o_head_stride;
-        __nv_bfloat16* theirs = p.out + (sq.tok_start + peer_row) * p.o_tok_stride + (long long)head * p.o_head_stride;
-        const bool store_peer = (row ^ 1) < m;
-        const bool odd = lane & 1;
+        // The rows are staged where the tile's V was (nothing reads it any more), in the layout the TMA store expects.  A
+        // tile that reaches beyond its sequence is written row by row instead: the rows behind it are not ours.
+        const bool whole = m == 128;
+        __nv_bfloat16* dst = p.out + (sq.tok_start + t0 + row) * p.o_tok_stride + (long long)head * p.o_head_stride + half * (D / 2);
+        uint8_t* stage = smem + L::kOffV + (c % L::kStages) * L::kTile;
 #pragma unroll
-        for (int cb = 0; cb < D / 32; ++cb) {
+        for (int i = 0; i < D / 64; ++i) {
+          const int cb = half * (D / 64) + i;
           uint32_t a[32], b[32];
           tmem_ld32(tm + kColO + cb * 32, a);
           tmem_ld32(tm + kColQS + cb * 32, b);
           tmem_wait_ld();
-          uint32_t w[16];
+          if (i == D / 64 - 1) {                               // everything is in registers: the accumulators are free
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar_o_empty);
+          }
 #pragma unroll
-          for (int e = 0; e < 16; ++e)
-            w[e] = pack_bf16x2(p.scale * fmaf(g1, __uint_as_float(b[2 * e]), __uint_as_float(a[2 * e])),
-                               p.scale * fmaf(g1, __uint_as_float(b[2 * e + 1]), __uint_as_float(a[2 * e + 1])));
+          for (int ch = 0; ch < 4; ++ch) {
+            float f[8];
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {                                    // 16 values = two 16-byte chunks
-            uint32_t own[4], give[4], got[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              own[e] = odd ? w[8 * h + 4 + e] : w[8 * h + e];              // even lanes keep chunk 0, odd ones chunk 1
-              give[e] = odd ? w[8 * h + e] : w[8 * h + 4 + e];
-              got[e] = __shfl_xor_sync(0xffffffffu, give[e], 1);
-            }
-            const int col = cb * 32 + h * 16 + (odd ? 8 : 0);
-            // first the even row's two chunks, then the odd row's
-            const uint4 first_w = odd ? make_uint4(got[0], got[1], got[2], got[3]) : make_uint4(own[0], own[1], own[2], own[3]);
-            const uint4 second_w = odd ? make_uint4(own[0], own[1], own[2], own[3]) : make_uint4(got[0], got[1], got[2], got[3]);
-            if (odd ? store_peer : store) *reinterpret_cast<uint4*>((odd ? theirs : mine) + col) = first_w;
-            if (odd ? store : store_peer) *reinterpret_cast<uint4*>((odd ? mine : theirs) + col) = second_w;
+            for (int e = 0; e < 8; ++e)
+              f[e] = fmaf(g1, __uint_as_float(b[8 * ch + e]), p.scale * __uint_as_float(a[8 * ch + e]));
+            const int at = cb * 4 + ch;                        // 16-byte chunk of the row
+            if (whole)         *reinterpret_cast<uint4*>(stage + (at >> 3) * 16384 + row * 128 + (((at & 7) ^ (row & 7)) << 4)) = pack8(f);
+            else if (row < m)  *reinterpret_cast<uint4*>(dst + i * 32 + ch * 8) = pack8(f);
           }
         }
-        tc_fence_before();
+        fence_proxy_async_smem();
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar_o_empty);
+        if (lane == 0) mbar_arrive(bar_o_staged);
       }
       if (!ok && lane == 0) atomicCAS(p.status, 0u, kStatusTimeoutSoftmax);
     }
-  } else if (warp < 8) {
-    // =========================================================== K -> K', state; thread = token row, then K dim
-    const int row = (warp - 4) * 32 + lane;
-    const uint32_t tm = tmem_base + (static_cast<uint32_t>((warp - 4) * 32) << 16);
-    float S[D];
+  } else if (warp < kTma) {
+    // =========================================================== K -> K', state; two threads per token row / K dim
+    if (!kStateOnly) setmaxnreg_inc<128>();
+    const int wq = (warp - kFirstB) & 3, half = (warp - kFirstB) >> 2;
+    const int row = wq * 32 + lane;
+    constexpr int kCols = D / 2;                                           // columns of this thread's part of a row
+    const uint32_t tm = tmem_base + (static_cast<uint32_t>(wq * 32) << 16) + kColT + half * kCols;
+    float S[kCols];
 #pragma unroll
-    for (int e = 0; e < D; ++e) S[e] = 0.f;
+    for (int e = 0; e < kCols; ++e) S[e] = 0.f;
     const bool has_state = row < D;                                        // warp-uniform
+    // where this thread's 16-byte chunks of a row are in a tile (128-byte swizzle); D = 128: half = 64-column box
+    auto chunk = [&](int ch, int box_bytes) {
+      const int at = half * (kCols / 8) + ch;
+      return (at >> 3) * box_bytes + row * 128 + (((at & 7) ^ (row & 7)) << 4);
+    };
     auto publish = [&]() {
-      // row of the state, rounded to bf16, in the layout of a V tile (row = contraction index)
+      // this part of the state's row, rounded to bf16, in the layout of a V tile (row = contraction index)
 #pragma unroll
-      for (int ch = 0; ch < D / 8; ++ch) {
+      for (int ch = 0; ch < kCols / 8; ++ch) {
         float f[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) f[e] = S[ch * 8 + e];
-        st_shared_v4(sSt + (ch >> 3) * (D * 128) + row * 128 + (((ch & 7) ^ (row & 7)) << 4), pack8(f));
+        *reinterpret_cast<uint4*>(smem + L::kOffSt + chunk(ch, D * 128)) = pack8(f);
       }
       fence_proxy_async_smem();
     };
     // the state before this piece
     auto add_piece = [&](const float* piece, float g) {                    // S = g S + what a piece left in the workspace
-      const float4* src = reinterpret_cast<const float4*>(piece) + row;
+      const float4* src = reinterpret_cast<const float4*>(piece) + half * (kCols / 4) * D + row;
 #pragma unroll
-      for (int e = 0; e < D / 4; ++e) {
+      for (int e = 0; e < kCols / 4; ++e) {
         const float4 x = src[e * D];
         S[4 * e] = fmaf(g, S[4 * e], x.x); S[4 * e + 1] = fmaf(g, S[4 * e + 1], x.y);
         S[4 * e + 2] = fmaf(g, S[4 * e + 2], x.z); S[4 * e + 3] = fmaf(g, S[4 * e + 3], x.w);
       }
     };
     auto leave_piece = [&](float* piece) {
-      float4* dst = reinterpret_cast<float4*>(piece) + row;
+      float4* dst = reinterpret_cast<float4*>(piece) + half * (kCols / 4) * D + row;
 #pragma unroll
-      for (int e = 0; e < D / 4; ++e) dst[e * D] = make_float4(S[4 * e], S[4 * e + 1], S[4 * e + 2], S[4 * e + 3]);
+      for (int e = 0; e < kCols / 4; ++e) dst[e * D] = make_float4(S[4 * e], S[4 * e + 1], S[4 * e + 2], S[4 * e + 3]);
     };
     if (has_state && seg == 0 && p.state_in != nullptr) {
       // A cut sequence: the state launch is the only one that reads state_in (its first piece starts from it and leaves a
       // copy), so that the main launch may write state_out to the same memory at any time.
       float* copy = p.initial + (long long)(si * p.heads + head) * (D * D);
       if (kStateOnly || n_seg == 1) {
-        const float4* src = reinterpret_cast<const float4*>(p.state_in + (((long long)sq.seq_id * p.heads + head) * D + row) * D);
+        const float4* src = reinterpret_cast<const float4*>(p.state_in + (((long long)sq.seq_id * p.heads + head) * D + row) * D + half * kCols);
 #pragma unroll
-        for (int e = 0; e < D / 4; ++e) {
+        for (int e = 0; e < kCols / 4; ++e) {
           const float4 x = src[e];
           S[4 * e] = x.x; S[4 * e + 1] = x.y; S[4 * e + 2] = x.z; S[4 * e + 3] = x.w;
         }
@@ -322,47 +327,93 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       __syncwarp();
       if (lane == 0) mbar_arrive(bar_st_full);
     }
+    // K' of this warp: K dims 32 wq .. + 31 (tensor-memory lanes), tokens 64 half .. + 63.  ldmatrix hands thread i the token
+    // pairs 64 half + 8 t + 2 (i % 4), + 1 for t = 0..7: the weights of those 16 tokens stay in registers.
+    float w[16];
+    auto weights = [&](int m, const uint32_t (&bits)[2]) {
+#pragma unroll
+      for (int t = 0; t < 8; ++t)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const int in = 8 * t + 2 * (lane & 3) + u, tok = 64 * half + in;
+          w[2 * t + u] = (bits[in >> 5] >> (in & 31)) & 1u ? dec[m - 1 - tok] : 0.f;
+        }
+    };
+    {
+      const uint32_t all[2] = {~0u, ~0u};
+      weights(128, all);
+    }
+    // address of this lane's row in block (dim chunk dc, token block tb) of a K tile: lanes 0-7 and 16-23 the first 8 of 16
+    // dims, the others the second 8; lanes 0-15 the first token block, the others the next
+    const int tok_in = 64 * half + ((lane >> 4) << 3) + (lane & 7);
+    const uint32_t k_row = tok_in * 128;
+    const int dc_in = (lane >> 3) & 1;
     bool ok = true;
     int st = 0;
     uint32_t ph = 0;
     for (int c = 0; c < n_tiles; ++c) {
       const int t0 = (tile0 + c) * 128;
       const int m = min(128, sq.n_tokens - t0);
-      bool valid = row < m;
-      if (valid && p.key_mask != nullptr) valid = p.key_mask[sq.tok_start + t0 + row] != 0;
-      const float w = valid ? dec[m - 1 - row] : 0.f;
-      ok = __all_sync(0xffffffffu, mbar_wait(bar_k_full(st), ph, limit));
-      if (!kStateOnly) ok = ok && __all_sync(0xffffffffu, mbar_wait(bar_s_full, c & 1, limit));   // K has been multiplied with Q
-      if (!ok) break;
+      const bool mixed = p.key_mask != nullptr || m < 128;
+      uint32_t vbits = ~0u;                                                // of the 32 token rows 32 wq ..
+      if (mixed) {
+        uint32_t bits[2];
 #pragma unroll
-      for (int ch = 0; ch < D / 8; ++ch) {
-        const uint32_t off = (ch >> 3) * 16384 + row * 128 + (((ch & 7) ^ (row & 7)) << 4);
-        uint4 hi = make_uint4(0, 0, 0, 0), lo = make_uint4(0, 0, 0, 0);
-        if (valid) {
-          float f[8], r[8];
-          unpack8(ld_shared_v4(sK + st * L::kTile + off), f);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) f[e] *= w;
-          hi = pack8(f);
-          unpack8(hi, r);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) r[e] = f[e] - r[e];
-          lo = pack8(r);
+        for (int b = 0; b < 3; ++b) {
+          const int j = (b < 2 ? 64 * half + 32 * b : 32 * wq) + lane;
+          bool valid = j < m;
+          if (valid && p.key_mask != nullptr) valid = p.key_mask[sq.tok_start + t0 + j] != 0;
+          const uint32_t word = __ballot_sync(0xffffffffu, valid);
+          if (b < 2) bits[b] = word; else vbits = word;
         }
-        st_shared_v4(sK + st * L::kTile + off, hi);
-        st_shared_v4(sLo + off, lo);
+        weights(m, bits);
       }
-      if (m < 128 || p.key_mask != nullptr) {
+      ok = __all_sync(0xffffffffu, mbar_wait(bar_k_full(st), ph, limit));
+      // the accumulators of the previous tile's outputs, whose columns K' takes, have been read
+      if (!kStateOnly && c > 0) ok = ok && __all_sync(0xffffffffu, mbar_wait(bar_o_empty, (c - 1) & 1, limit));
+      if (!ok) break;
+      tc_fence_after();
+      if (has_state) {
+#pragma unroll
+        for (int lh = 0; lh < 2; ++lh) {                                   // 16 of the 32 K dims
+          const int dc = 4 * wq + 2 * lh + dc_in;                          // 16-byte chunk of the row
+          const uint32_t src = sK + st * L::kTile + (dc >> 3) * 16384 + k_row + (((dc & 7) ^ (lane & 7)) << 4);
+#pragma unroll
+          for (int tg = 0; tg < 2; ++tg) {                                 // 32 tokens
+            uint32_t x[2][4];
+            ldmatrix_x4_trans(src + tg * 32 * 128, x[0]);
+            ldmatrix_x4_trans(src + tg * 32 * 128 + 16 * 128, x[1]);
+            uint32_t hi[8], lo[8];
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+              const int t = tg * 4 + (r >> 1);                             // token block
+              float f0 = bf16_lo(x[r >> 2][r & 3]) * w[2 * t], f1 = bf16_hi(x[r >> 2][r & 3]) * w[2 * t + 1];
+              if (mixed) {                                                 // (a select: what stands under a mask may be NaN)
+                f0 = w[2 * t] != 0.f ? f0 : 0.f;
+                f1 = w[2 * t + 1] != 0.f ? f1 : 0.f;
+              }
+              hi[r] = pack_bf16x2(f0, f1);
+              lo[r] = pack_bf16x2(f0 - bf16_lo(hi[r]), f1 - bf16_hi(hi[r]));
+            }
+            const uint32_t dst = tmem_base + (static_cast<uint32_t>(wq * 32 + lh * 16) << 16) + kColO + half * 32 + tg * 16;
+            tmem_st_16x128b_x4(dst, hi);
+            tmem_st_16x128b_x4(dst + 64, lo);
+          }
+        }
+        tmem_wait_st();
+      }
+      if (mixed) {
         // V rows that do not count become zeros: 0 * (whatever stands there) would not be 0 for infinities and NaN
         ok = __all_sync(0xffffffffu, mbar_wait(bar_v_full(st), ph, limit));
         if (!ok) break;
-        if (!valid) {
+        if (((vbits >> lane) & 1u) == 0) {
 #pragma unroll
-          for (int ch = 0; ch < D / 8; ++ch)
-            st_shared_v4(sV + st * L::kTile + (ch >> 3) * 16384 + row * 128 + ((ch & 7) << 4), make_uint4(0, 0, 0, 0));
+          for (int ch = 0; ch < kCols / 8; ++ch)
+            *reinterpret_cast<uint4*>(smem + L::kOffV + st * L::kTile + chunk(ch, 16384)) = make_uint4(0, 0, 0, 0);
         }
+        fence_proxy_async_smem();
       }
-      fence_proxy_async_smem();
+      tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(bar_kp_full);
 
@@ -372,9 +423,9 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       if (has_state) {
         const float gm = dec[m];
 #pragma unroll
-        for (int cb = 0; cb < D / 32; ++cb) {
+        for (int cb = 0; cb < kCols / 32; ++cb) {
           uint32_t t[32];
-          tmem_ld32(tm + kColT + cb * 32, t);
+          tmem_ld32(tm + cb * 32, t);
           tmem_wait_ld();
 #pragma unroll
           for (int e = 0; e < 32; ++e) S[cb * 32 + e] = fmaf(gm, S[cb * 32 + e], __uint_as_float(t[e]));
@@ -392,12 +443,15 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       if constexpr (kStateOnly) {
         leave_piece(p.local + (long long)(local_first + rel) * (D * D));
       } else if (seg == n_seg - 1 && p.state_out != nullptr) {
-        float4* dst = reinterpret_cast<float4*>(p.state_out + (((long long)sq.seq_id * p.heads + head) * D + row) * D);
+        float4* dst = reinterpret_cast<float4*>(p.state_out + (((long long)sq.seq_id * p.heads + head) * D + row) * D + half * kCols);
 #pragma unroll
-        for (int e = 0; e < D / 4; ++e) dst[e] = make_float4(S[4 * e], S[4 * e + 1], S[4 * e + 2], S[4 * e + 3]);
+        for (int e = 0; e < kCols / 4; ++e) dst[e] = make_float4(S[4 * e], S[4 * e + 1], S[4 * e + 2], S[4 * e + 3]);
       }
     }
-  } else if (warp == 8) {
+  } else if (!kStateOnly) {
+    setmaxnreg_dec<48>();
+  }
+  if (warp == kTma) {
     // =========================================================== TMA producer
     if (lane == 0) {
       const uint64_t pol_once = l2_policy_evict_first();
@@ -437,18 +491,14 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       }
     }
     __syncwarp();
-  } else {
+  } else if (warp == kMma) {
     // =========================================================== MMA issuer
     constexpr uint32_t idesc_qk = idesc_bf16_f32(128, 128, false);
     constexpr uint32_t idesc_d = idesc_bf16_f32(128, D, true);             // B MN-major: P V and Q S
-    constexpr uint32_t idesc_t = idesc_bf16_f32_tt(128, D);                // A and B MN-major: K'^T V
     constexpr uint32_t kV_lbo = D == 128 ? 16384u : 16u, kSt_lbo = D == 128 ? 16384u : 16u;
     const uint32_t hi_desc = smem_desc_hi_sw128(1024);
     const uint32_t q_lo = smem_desc_lo(sQ, 16), k_lo = smem_desc_lo(sK, 16);
     const uint32_t v_lo = smem_desc_lo(sV, kV_lbo), st_lo = smem_desc_lo(sSt, kSt_lbo);
-    // K' as the A operand, M = 128 K dims.  With D = 64 the upper 64 rows come from whatever lies 16 KB further on (inside
-    // this CTA's shared memory) and end in tensor-memory lanes that nobody reads.
-    const uint32_t kt_lo = smem_desc_lo(sK, 16384), lo_lo = smem_desc_lo(sLo, 16384);
     constexpr uint32_t kStep = L::kTile >> 4;
     bool ok = true;
     int st = 0;
@@ -486,16 +536,12 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       if (!wait(bar_v_full(st), ph)) { ok = false; break; }
       if (!wait(bar_kp_full, c & 1)) { ok = false; break; }
       tc_fence_after();
+      // (D = 64: the upper 64 lanes hold no K dims; their rows of the product are never read)
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const uint32_t off = k * (2048 >> 4);
-        if (k == 0) mma_ss_elect<false>(tmem_base + kColT, kt_lo + st * kStep, v_lo + st * kStep, hi_desc, idesc_t, 0u);
-        else        mma_ss_elect<true>(tmem_base + kColT, kt_lo + st * kStep + off, v_lo + st * kStep + off, hi_desc, idesc_t, 1u);
-      }
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const uint32_t off = k * (2048 >> 4);
-        mma_ss_elect<true>(tmem_base + kColT, lo_lo + off, v_lo + st * kStep + off, hi_desc, idesc_t, 1u);
+      for (int k = 0; k < 16; ++k) {                                       // hi, then lo
+        const uint32_t off = (k & 7) * (2048 >> 4);
+        if (k == 0) mma_ts_elect<false>(tmem_base + kColT, tmem_base + kColO, v_lo + st * kStep, hi_desc, idesc_d, 0u);
+        else        mma_ts_elect<true>(tmem_base + kColT, tmem_base + kColO + k * 8, v_lo + st * kStep + off, hi_desc, idesc_d, 1u);
       }
       tc_commit_elect(bar_t_full);
       tc_commit_elect(bar_k_empty(st));
@@ -506,11 +552,12 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         for (int k = 0; k < 8; ++k) {
           const uint32_t off = k * (2048 >> 4);
           if (k == 0) mma_ts_elect<false>(tmem_base + kColO, tmem_base + kColS, v_lo + st * kStep, hi_desc, idesc_d, 0u);
-          else        mma_ts_elect<true>(tmem_base + kColO, tmem_base + kColS + k * 8, v_lo + st * kStep + off, hi_desc, idesc_d, 1u);
+          else        mma_ts_elect<true>(tmem_base + kColO, tmem_base + kColS + (k >> 1) * 32 + (k & 1) * 8, v_lo + st * kStep + off, hi_desc, idesc_d, 1u);
         }
         tc_commit_elect(bar_o_full);
+      } else {
+        tc_commit_elect(bar_v_empty(st));                                  // (main launch: once the outputs staged there are on their way)
       }
-      tc_commit_elect(bar_v_empty(st));
       if (++st == L::kStages) { st = 0; ph ^= 1u; }
     }
     if (!ok) {
@@ -519,11 +566,30 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       mbar_wait_warp(bar_drain, 0, limit);
     }
     __syncwarp();
+  } else if (warp == kStore) {
+    // =========================================================== output stores
+    if constexpr (!kStateOnly) {
+      if (lane == 0) {
+        for (int c = 0; c < n_tiles; ++c) {
+          const int st = c % L::kStages;
+          if (!mbar_wait(bar_o_staged, c & 1, limit)) { atomicCAS(p.status, 0u, kStatusTimeoutSoftmax); break; }
+          if (sq.n_tokens - (tile0 + c) * 128 >= 128) {
+#pragma unroll
+            for (int hf = 0; hf < L::kHalves; ++hf)
+              tma_store_3d(&tm_o, sV + st * L::kTile + hf * 16384, hf * 64, head, tok0 + (tile0 + c) * 128);
+            bulk_commit_group();
+            bulk_wait_read_all();
+          }
+          mbar_arrive(bar_v_empty(st));
+        }
+      }
+    }
+    __syncwarp();
   }
 
   tc_fence_before();
   __syncthreads();
-  if (warp == 9) {
+  if (warp == kMma) {
     tc_fence_after();
     tmem_dealloc(tmem_base, 512);
   }

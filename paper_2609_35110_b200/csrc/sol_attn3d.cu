@@ -1337,16 +1337,16 @@ extern "C++" {
 namespace {
 template <int D>
 cudaError_t launch_linear(sol_attn3d_plan_t p, const CUtensorMap& tm_q, const CUtensorMap& tm_k, const CUtensorMap& tm_v,
-                          const sol::LinearParams& lp, cudaStream_t st) {
+                          const CUtensorMap& tm_o, const sol::LinearParams& lp, cudaStream_t st) {
   if (p->lin_local > 0) {
-    sol::linear_attn_kernel<D, true><<<(unsigned)p->lin_local, sol::kLinThreads, sol::LinearSmem<D, true>::kDynBytes, st>>>(
-        tm_q, tm_k, tm_v, lp);
+    sol::linear_attn_kernel<D, true><<<(unsigned)p->lin_local, sol::linear_threads(true), sol::LinearSmem<D, true>::kDynBytes, st>>>(
+        tm_q, tm_k, tm_v, tm_o, lp);
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     ++p->launches;
   }
-  sol::linear_attn_kernel<D, false><<<(unsigned)p->lin_pieces, sol::kLinThreads, sol::LinearSmem<D, false>::kDynBytes, st>>>(
-      tm_q, tm_k, tm_v, lp);
+  sol::linear_attn_kernel<D, false><<<(unsigned)p->lin_pieces, sol::linear_threads(false), sol::LinearSmem<D, false>::kDynBytes, st>>>(
+      tm_q, tm_k, tm_v, tm_o, lp);
   const cudaError_t e = cudaGetLastError();
   if (e == cudaSuccess) ++p->launches;
   return e;
@@ -1374,10 +1374,11 @@ int sol_attn3d_forward_linear(sol_attn3d_plan_t p, const void* q, const void* k,
   if (p->lin_local > 0 && (linear_ws == nullptr || linear_ws_bytes < sol_attn3d_linear_workspace_bytes(p) ||
                            (reinterpret_cast<uintptr_t>(linear_ws) % kAlign) != 0))
     return SOL_ATTN3D_ERR_NO_WORKSPACE;
-  CUtensorMap tm_q, tm_k, tm_v;
+  CUtensorMap tm_q, tm_k, tm_v, tm_o;
   int rc = encode_map(p->encode, p, &tm_q, q, p->sq);
   if (rc == SOL_ATTN3D_OK) rc = encode_map(p->encode, p, &tm_k, k, p->sk);
   if (rc == SOL_ATTN3D_OK) rc = encode_map(p->encode, p, &tm_v, v, p->sv);
+  if (rc == SOL_ATTN3D_OK) rc = encode_map(p->encode, p, &tm_o, out, p->so);
   if (rc != SOL_ATTN3D_OK) return rc;
   sol::LinearParams lp{};
   lp.seqs = reinterpret_cast<const SeqDev*>(p->ws + p->off_seqs);
@@ -1398,7 +1399,8 @@ int sol_attn3d_forward_linear(sol_attn3d_plan_t p, const void* q, const void* k,
   lp.wait_limit_ns = p->wait_limit_ns;
   p->launches = 0;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const cudaError_t e = p->head_dim == 128 ? launch_linear<128>(p, tm_q, tm_k, tm_v, lp, st) : launch_linear<64>(p, tm_q, tm_k, tm_v, lp, st);
+  const cudaError_t e = p->head_dim == 128 ? launch_linear<128>(p, tm_q, tm_k, tm_v, tm_o, lp, st)
+                                            : launch_linear<64>(p, tm_q, tm_k, tm_v, tm_o, lp, st);
   return e == cudaSuccess ? SOL_ATTN3D_OK : fail_cuda(p, e);
 }
 
