@@ -15,8 +15,11 @@
 //
 // Precision: products of bf16 values are exact in the fp32 accumulators.  P and the copy of S that the tensor core reads
 // are rounded to bf16 (they only enter bf16 outputs).  K' is split into two bf16 parts, hi + lo, so that the state, which
-// is fp32 and carried from tile to tile, keeps about 17 bits of every factor instead of 8; the running state itself is
-// never rounded below fp32 and never accumulated in tensor memory for longer than one tile.
+// is fp32 and carried from tile to tile, keeps about 16 bits of every factor instead of 8; the running state itself is
+// never rounded below fp32 and never accumulated in tensor memory for longer than one tile.  The split needs three bf16x2
+// instructions for two values: with the weight as w = wb + wc (two bf16), hi = rn(k wb), lo = rn(k wc + rn(k wb - hi)),
+// where k wb - hi is exact before its rounding.  That is off by at most 2^-16 of |k w| (half a step, 2^-8, of two
+// quantities that are themselves at most 2^-8 of it, and of wc), against 5 instructions for one value in fp32.
 //
 // Warp roles (the state launch has only the second group, the producer and the issuer):
 //   8 warps   two threads per query row: scores -> P (column blocks of 32 alternate between them), output epilogue
@@ -71,7 +74,8 @@ struct LinearSmem {
   static constexpr int kOffV = kOffK + kStages * kTile;
   static constexpr int kOffSt = kOffV + kStages * kTile;                 // bf16 copy of the state, laid out like V
   static constexpr int kOffDec = kOffSt + (kStateOnly ? 0 : D * D * 2);  // powers of the decay: [128 + d], zero for d < 0
-  static constexpr int kOffBars = kOffDec + 264 * 4;
+  static constexpr int kOffFall = kOffDec + 260 * 4;                     // g^31 .. g^0
+  static constexpr int kOffBars = kOffFall + 32 * 4;
   static constexpr int kNumBars = 2 * kQStages + 4 * kStages + 9;
   static constexpr int kOffTmemPtr = kOffBars + kNumBars * 8;
   static constexpr int kBytes = kOffTmemPtr + 16;
@@ -151,6 +155,11 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     const int d = (int)threadIdx.x - 128;
     dec[d] = d < 0 ? 0.f : d == 0 ? 1.f : (float)exp((double)d * ld);     // (0 * -inf is NaN: g^0 is 1)
   }
+  float4* fall = reinterpret_cast<float4*>(smem + L::kOffFall);
+  if (threadIdx.x >= 288 && threadIdx.x < 320) {
+    const int d = 319 - (int)threadIdx.x;
+    reinterpret_cast<float*>(fall)[31 - d] = d == 0 ? 1.f : (float)exp((double)d * ld);
+  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -170,6 +179,7 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       const int row = wq * 32 + lane;
       const uint32_t tm = tmem_base + (static_cast<uint32_t>(wq * 32) << 16);
       const float g1 = p.scale * dec[row + 1];
+      const float2 g1_2 = make_float2(g1, g1);
       const float* dec_row = dec + row;
       bool ok = true;
       for (int c = 0; c < n_tiles; ++c) {
@@ -199,18 +209,28 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             uint32_t s[32];
             tmem_ld32(tm + kColS + cb * 32, s);
             tmem_wait_ld();
-            const float* d = dec_row - cb * 32;
             if (cb < wq && !mixed) {
+              // g^{row - j} = g^{row - 32 cb - 31} * g^{31 - jj}: the second factor is the same for every row and tile
+              const float lead = p.scale * dec_row[-cb * 32 - 31];
+              const float2 lead2 = make_float2(lead, lead);
 #pragma unroll
-              for (int e = 0; e < 16; ++e)
-                pk[e] = pack_bf16x2(__uint_as_float(s[2 * e]) * d[-2 * e], __uint_as_float(s[2 * e + 1]) * d[-2 * e - 1]);
+              for (int e = 0; e < 8; ++e) {
+                const float4 d = fall[e];                      // g^{31 - 4 e}, ... - 1, - 2, - 3
+                const float2 lo = mul_f32x2(make_float2(__uint_as_float(s[4 * e]), __uint_as_float(s[4 * e + 1])),
+                                            mul_f32x2(lead2, make_float2(d.x, d.y)));
+                const float2 hi = mul_f32x2(make_float2(__uint_as_float(s[4 * e + 2]), __uint_as_float(s[4 * e + 3])),
+                                            mul_f32x2(lead2, make_float2(d.z, d.w)));
+                pk[2 * e] = pack_bf16x2(lo.x, lo.y);
+                pk[2 * e + 1] = pack_bf16x2(hi.x, hi.y);
+              }
             } else {
+              const float* d = dec_row - cb * 32;
               const int last = row - cb * 32;                  // columns beyond it lie above the diagonal
               const uint32_t on = bits[b] & (last >= 31 ? ~0u : (2u << last) - 1u);
 #pragma unroll
               for (int e = 0; e < 16; ++e)
-                pk[e] = pack_bf16x2((on >> (2 * e)) & 1u ? __uint_as_float(s[2 * e]) * d[-2 * e] : 0.f,
-                                    (on >> (2 * e + 1)) & 1u ? __uint_as_float(s[2 * e + 1]) * d[-2 * e - 1] : 0.f);
+                pk[e] = pack_bf16x2((on >> (2 * e)) & 1u ? __uint_as_float(s[2 * e]) * (p.scale * d[-2 * e]) : 0.f,
+                                    (on >> (2 * e + 1)) & 1u ? __uint_as_float(s[2 * e + 1]) * (p.scale * d[-2 * e - 1]) : 0.f);
             }
           } else {
 #pragma unroll
@@ -247,8 +267,12 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
           for (int ch = 0; ch < 4; ++ch) {
             float f[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-              f[e] = fmaf(g1, __uint_as_float(b[8 * ch + e]), p.scale * __uint_as_float(a[8 * ch + e]));
+            for (int e = 0; e < 8; e += 2) {
+              const float2 x = fma_f32x2(g1_2, make_float2(__uint_as_float(b[8 * ch + e]), __uint_as_float(b[8 * ch + e + 1])),
+                                         make_float2(__uint_as_float(a[8 * ch + e]), __uint_as_float(a[8 * ch + e + 1])));
+              f[e] = x.x;
+              f[e + 1] = x.y;
+            }
             const int at = cb * 4 + ch;                        // 16-byte chunk of the row
             if (whole)         *reinterpret_cast<uint4*>(stage + (at >> 3) * 16384 + row * 128 + (((at & 7) ^ (row & 7)) << 4)) = pack8(f);
             else if (row < m)  *reinterpret_cast<uint4*>(dst + i * 32 + ch * 8) = pack8(f);
@@ -328,16 +352,23 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       if (lane == 0) mbar_arrive(bar_st_full);
     }
     // K' of this warp: K dims 32 wq .. + 31 (tensor-memory lanes), tokens 64 half .. + 63.  ldmatrix hands thread i the token
-    // pairs 64 half + 8 t + 2 (i % 4), + 1 for t = 0..7: the weights of those 16 tokens stay in registers.
-    float w[16];
+    // pairs 64 half + 8 t + 2 (i % 4), + 1 for t = 0..7: the weights of those 16 tokens, wb + wc, stay in registers.
+    uint32_t wb[8], wc[8], on[8];                                          // on: all ones for a token that counts
     auto weights = [&](int m, const uint32_t (&bits)[2]) {
 #pragma unroll
-      for (int t = 0; t < 8; ++t)
+      for (int t = 0; t < 8; ++t) {
+        float w[2];
+        on[t] = 0u;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
           const int in = 8 * t + 2 * (lane & 3) + u, tok = 64 * half + in;
-          w[2 * t + u] = (bits[in >> 5] >> (in & 31)) & 1u ? dec[m - 1 - tok] : 0.f;
+          const bool counts = ((bits[in >> 5] >> (in & 31)) & 1u) != 0;
+          w[u] = counts ? dec[m - 1 - tok] : 0.f;
+          if (counts) on[t] |= 0xffffu << (16 * u);
         }
+        wb[t] = pack_bf16x2(w[0], w[1]);
+        wc[t] = pack_bf16x2(w[0] - bf16_lo(wb[t]), w[1] - bf16_hi(wb[t]));
+      }
     };
     {
       const uint32_t all[2] = {~0u, ~0u};
@@ -387,13 +418,10 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
 #pragma unroll
             for (int r = 0; r < 8; ++r) {
               const int t = tg * 4 + (r >> 1);                             // token block
-              float f0 = bf16_lo(x[r >> 2][r & 3]) * w[2 * t], f1 = bf16_hi(x[r >> 2][r & 3]) * w[2 * t + 1];
-              if (mixed) {                                                 // (a select: what stands under a mask may be NaN)
-                f0 = w[2 * t] != 0.f ? f0 : 0.f;
-                f1 = w[2 * t + 1] != 0.f ? f1 : 0.f;
-              }
-              hi[r] = pack_bf16x2(f0, f1);
-              lo[r] = pack_bf16x2(f0 - bf16_lo(hi[r]), f1 - bf16_hi(hi[r]));
+              uint32_t k2 = x[r >> 2][r & 3];
+              if (mixed) k2 &= on[t];                                      // whatever stands under a mask, NaN included, is dropped
+              hi[r] = mul_bf16x2(k2, wb[t]);
+              lo[r] = fma_bf16x2(k2, wc[t], fma_bf16x2(k2, wb[t], hi[r] ^ 0x80008000u));
             }
             const uint32_t dst = tmem_base + (static_cast<uint32_t>(wq * 32 + lh * 16) << 16) + kColO + half * 32 + tg * 16;
             tmem_st_16x128b_x4(dst, hi);
@@ -428,7 +456,12 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
           tmem_ld32(tm + cb * 32, t);
           tmem_wait_ld();
 #pragma unroll
-          for (int e = 0; e < 32; ++e) S[cb * 32 + e] = fmaf(gm, S[cb * 32 + e], __uint_as_float(t[e]));
+          for (int e = 0; e < 32; e += 2) {
+            const float2 x = fma_f32x2(make_float2(gm, gm), make_float2(S[cb * 32 + e], S[cb * 32 + e + 1]),
+                                       make_float2(__uint_as_float(t[e]), __uint_as_float(t[e + 1])));
+            S[cb * 32 + e] = x.x;
+            S[cb * 32 + e + 1] = x.y;
+          }
         }
         tc_fence_before();
         if (!kStateOnly) publish();
