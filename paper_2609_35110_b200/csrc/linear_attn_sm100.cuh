@@ -11,7 +11,9 @@
 // One CTA = one piece: seg_tiles consecutive tiles of one (sequence, head), walked in order with the state in fp32
 // registers.  A sequence that is cut into several pieces takes two launches: the first (kStateOnly) computes, for every
 // piece but the last, the state that the piece adds on its own; the second starts each piece from the sum of its
-// predecessors' states (and the caller's), which it forms in a fixed order, and writes the outputs.
+// predecessors' states (and the caller's), which it forms in a fixed order, and writes the outputs.  (One launch whose
+// pieces hand their states on, so that the second walk finds K and V in L2, was built and measured: 1.6 to 2.0 ms where
+// two launches take LINTIME at 111,856 tokens x 40 heads x 128.  The chain of a tile bounds both, not HBM.)
 //
 // Precision: products of bf16 values are exact in the fp32 accumulators.  P and the copy of S that the tensor core reads
 // are rounded to bf16 (they only enter bf16 outputs).  K' is split into two bf16 parts, hi + lo, so that the state, which
@@ -21,16 +23,20 @@
 // where k wb - hi is exact before its rounding.  That is off by at most 2^-16 of |k w| (half a step, 2^-8, of two
 // quantities that are themselves at most 2^-8 of it, and of wc), against 5 instructions for one value in fp32.
 //
-// Warp roles (the state launch has only the second group, the producer and the issuer):
-//   8 warps   two threads per query row: scores -> P (column blocks of 32 alternate between them), output epilogue
-//   8 warps   K -> K', transposed on the way (ldmatrix) into tensor memory; two threads per K dim: a row of the state
-//   1 warp    TMA producer;   1 warp: MMA issuer, owns the tensor memory;   1 warp: TMA stores of the outputs
-// Tensor memory (512 columns): scores / P [0,128); K' hi | lo [128,256), replaced by P V; Q S [256,384); K'^T V [384,512).
+// Warp roles:
+//   0-7    (A) two threads per query row: scores -> P (column blocks of 32 alternate between them), output epilogue
+//   8-15   (B) K -> K', transposed on the way (ldmatrix) into tensor memory; two threads per K dim: a row of the state
+//   16     TMA producer;   17  MMA issuer, owns the tensor memory;   18  TMA stores of the outputs
+// (the state launch has no A and no stores: B is 0-7, 8 the producer, 9 the issuer).
+// Tensor memory (512 columns): scores / P (D = 64: two buffers, so that the scores of a tile are computed while P of its
+// predecessor is in use); K' hi | lo; the output, which is Q S first, scaled row by row by A, and then accumulates P V;
+// K'^T V.  The state launch has no scores and no outputs: there K' and K'^T V alternate between two places, so that a tile
+// is converted while its predecessor is multiplied.
 //
-// Bound by HBM: 4 x 128 x D x 2 bytes per tile and head (2.9 us at D = 128 with every SM streaming) against 5 small
-// products (4 and the lo half).  Next comes shared-memory bandwidth, which operands of 128-wide products use up as fast as
-// the tensor core: so K' is a tensor-memory operand, outputs leave through the V tile's own space with a TMA store, and
-// nothing is staged twice.
+// HBM needs 2.9 us per tile (4 x 128 x 128 x 2 bytes, every SM streaming).  What comes before it is shared-memory bandwidth,
+// which operands of 128-wide products use up as fast as the tensor core, and with it the latency of everything that goes
+// through that pipe, spilled registers included: so K' is a tensor-memory operand, outputs leave through the V tile's own
+// space with a TMA store, nothing is staged twice, and the decay of a score is computed, not looked up.
 #pragma once
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -59,8 +65,30 @@ struct LinearParams {
   unsigned long long wait_limit_ns;
 };
 
-// Compute warps, then the producer, the MMA issuer and (main launch) the store warp and an idle one, which completes a
-// warpgroup.  Registers of the main launch: 640 threads x 96 = 256 x 88 + 256 x 128 + 128 x 48.
+// Bits i and i + 1 of a word -> mask of a pair of 16-bit values (without a branch).
+__device__ __forceinline__ uint32_t pair_mask(uint32_t bits, int i) {
+  const uint32_t lo = static_cast<uint32_t>(static_cast<int>(bits << (31 - i)) >> 31);
+  const uint32_t hi = static_cast<uint32_t>(static_cast<int>(bits << (30 - i)) >> 31);
+  return (lo & 0xffffu) | (hi & 0xffff0000u);
+}
+
+// Powers of the decay: log2(g) as the sum of two floats, so that the exponent of a high power keeps its low bits.
+struct DecayPowers {
+  float hi, lo;
+  __device__ __forceinline__ explicit DecayPowers(float log_decay) {
+    const double l = fmin((double)log_decay, 0.0) * 1.4426950408889634;
+    hi = (float)l;
+    lo = hi < -1e4f ? 0.f : (float)(l - (double)hi);
+  }
+  __device__ __forceinline__ float operator()(int d) const {
+    if (d == 0) return 1.f;
+    if (hi < -1e4f) return 0.f;                            // 2^-10000, and the -infinity that forgets everything
+    const float x = (float)d * hi, e = fmaf((float)d, hi, -x) + (float)d * lo, r = exp2f(x);
+    return fmaf(r, e * 0.6931471806f, r);
+  }
+};
+
+// Main launch: 19 warps and an idle one, which completes a warpgroup; registers 640 threads x 96 = 256 x 88 + 256 x 128 + 128 x 48.
 constexpr int linear_threads(bool state_only) { return state_only ? 320 : 640; }
 
 template <int D, bool kStateOnly>
@@ -69,17 +97,19 @@ struct LinearSmem {
   static constexpr int kHalves = D / 64;
   static constexpr int kQStages = kStateOnly ? 0 : 2;
   static constexpr int kStages = D == 128 ? (kStateOnly ? 3 : 2) : 4;
+  static constexpr int kSBuf = D == 128 ? 1 : 2;
   static constexpr int kOffQ = 0;
   static constexpr int kOffK = kOffQ + kQStages * kTile;
   static constexpr int kOffV = kOffK + kStages * kTile;
   static constexpr int kOffSt = kOffV + kStages * kTile;                 // bf16 copy of the state, laid out like V
-  static constexpr int kOffDec = kOffSt + (kStateOnly ? 0 : D * D * 2);  // powers of the decay: [128 + d], zero for d < 0
-  static constexpr int kOffFall = kOffDec + 260 * 4;                     // g^31 .. g^0
-  static constexpr int kOffBars = kOffFall + 32 * 4;
-  static constexpr int kNumBars = 2 * kQStages + 4 * kStages + 9;
+  static constexpr int kOffTab = kOffSt + (kStateOnly ? 0 : D * D * 2);   // g^0 .. g^15, g^0, g^16 .. g^128, g^(128 seg_tiles)
+  static constexpr int kOffPairs = kOffTab + 32 * 4;                     // weights of the 64 token pairs of a whole tile, split
+  static constexpr int kOffBars = kOffPairs + 64 * 8;
+  static constexpr int kNumBars = 2 * kQStages + 5 * kStages + 2 * kSBuf + 9;
   static constexpr int kOffTmemPtr = kOffBars + kNumBars * 8;
   static constexpr int kBytes = kOffTmemPtr + 16;
   static constexpr int kDynBytes = kBytes + 1024;
+  static_assert(kDynBytes <= 232448, "shared memory of one CTA");
 };
 
 template <int D, bool kStateOnly>
@@ -95,19 +125,26 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
   constexpr int kFirstB = kStateOnly ? 0 : 8, kTma = kFirstB + 8, kMma = kTma + 1, kStore = kTma + 2;
 
   const uint32_t sQ = sbase + L::kOffQ, sK = sbase + L::kOffK, sV = sbase + L::kOffV, sSt = sbase + L::kOffSt;
-  float* dec = reinterpret_cast<float*>(smem + L::kOffDec) + 128;       // dec[d] = g^d, d in [-128, 128]
   const uint32_t bars = sbase + L::kOffBars;
-  constexpr int kQB = 2 * L::kQStages, kSB = kQB + 4 * L::kStages;
+  constexpr int kS = L::kStages, kQS = L::kQStages;
   auto bar_q_full = [&](int s) { return bars + 8u * s; };
-  auto bar_q_empty = [&](int s) { return bars + 8u * (L::kQStages + s); };
-  auto bar_k_full = [&](int s) { return bars + 8u * (kQB + s); };
-  auto bar_k_empty = [&](int s) { return bars + 8u * (kQB + L::kStages + s); };
-  auto bar_v_full = [&](int s) { return bars + 8u * (kQB + 2 * L::kStages + s); };
-  auto bar_v_empty = [&](int s) { return bars + 8u * (kQB + 3 * L::kStages + s); };
-  const uint32_t bar_s_full = bars + 8u * (kSB + 0), bar_p_full = bars + 8u * (kSB + 1), bar_kp_full = bars + 8u * (kSB + 2),
-                 bar_t_full = bars + 8u * (kSB + 3), bar_st_full = bars + 8u * (kSB + 4), bar_o_full = bars + 8u * (kSB + 5),
-                 bar_o_empty = bars + 8u * (kSB + 6), bar_o_staged = bars + 8u * (kSB + 7), bar_drain = bars + 8u * (kSB + 8);
+  auto bar_q_empty = [&](int s) { return bars + 8u * (kQS + s); };
+  auto bar_k_full = [&](int s) { return bars + 8u * (2 * kQS + s); };
+  auto bar_k_empty = [&](int s) { return bars + 8u * (2 * kQS + kS + s); };
+  auto bar_v_full = [&](int s) { return bars + 8u * (2 * kQS + 2 * kS + s); };
+  auto bar_v_empty = [&](int s) { return bars + 8u * (2 * kQS + 3 * kS + s); };
+  auto bar_o_staged = [&](int s) { return bars + 8u * (2 * kQS + 4 * kS + s); };
+  constexpr int kSB = 2 * kQS + 5 * kS;
+  auto bar_s_full = [&](int b) { return bars + 8u * (kSB + b); };
+  auto bar_p_full = [&](int b) { return bars + 8u * (kSB + L::kSBuf + b); };
+  constexpr int kIB = kSB + 2 * L::kSBuf;
+  auto bar_kp_full = [&](int t) { return bars + 8u * (kIB + (t & 1)); };
+  auto bar_t_full = [&](int t) { return bars + 8u * (kIB + 2 + (t & 1)); };
+  const uint32_t bar_st_full = bars + 8u * (kIB + 4), bar_qs_full = bars + 8u * (kIB + 5), bar_o_full = bars + 8u * (kIB + 6),
+                 bar_o_empty = bars + 8u * (kIB + 7), bar_drain = bars + 8u * (kIB + 8);
   volatile uint32_t* tmem_ptr_smem = reinterpret_cast<volatile uint32_t*>(smem + L::kOffTmemPtr);
+  float* tab = reinterpret_cast<float*>(smem + L::kOffTab);
+  uint2* pairs = reinterpret_cast<uint2*>(smem + L::kOffPairs);
 
   // ---- which piece: sequences in schedule order, then segments, heads fastest (CTAs that run together read neighbouring
   //      heads of the same tokens).  The state-only launch leaves out each sequence's last segment.
@@ -119,29 +156,27 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     first += here;
     local_first += (n_seg - 1) * p.heads;
   }
-  const SeqDev sq = p.seqs[si];
   const int rel = (int)blockIdx.x - first;
   const int seg = rel / p.heads, head = rel - seg * p.heads;
   SOL_DEVICE_CHECK(p.status, rel >= 0 && seg < n_seg, kCheckWorkItem);
-  const int tile0 = seg * p.seg_tiles;
-  const int n_tiles = min(p.seg_tiles, sq.n_ktiles - tile0);
+  const int n_tiles = min(p.seg_tiles, p.seqs[si].n_ktiles - seg * p.seg_tiles);
+  const int tok0 = (int)p.seqs[si].tok_start + seg * p.seg_tiles * 128;     // first token of the piece in the packed tensors
+  const int rem0 = p.seqs[si].n_tokens - seg * p.seg_tiles * 128;           // tokens from there to the sequence's end
   const unsigned long long limit = p.wait_limit_ns;
-  const int tok0 = (int)sq.tok_start;
 
   if (warp == kTma && lane == 0) {
-    for (int s = 0; s < L::kQStages; ++s) { mbar_init(bar_q_full(s), 1); mbar_init(bar_q_empty(s), 1); }
-    for (int s = 0; s < L::kStages; ++s) {
+    for (int s = 0; s < kQS; ++s) { mbar_init(bar_q_full(s), 1); mbar_init(bar_q_empty(s), 1); }
+    for (int s = 0; s < kS; ++s) {
       mbar_init(bar_k_full(s), 1); mbar_init(bar_k_empty(s), 1);
       mbar_init(bar_v_full(s), 1); mbar_init(bar_v_empty(s), 1);
+      mbar_init(bar_o_staged(s), 8);
     }
-    mbar_init(bar_s_full, 1);
-    mbar_init(bar_p_full, 8);
-    mbar_init(bar_kp_full, 8);
-    mbar_init(bar_t_full, 1);
+    for (int b = 0; b < L::kSBuf; ++b) { mbar_init(bar_s_full(b), 1); mbar_init(bar_p_full(b), 8); }
+    for (int t = 0; t < 2; ++t) { mbar_init(bar_kp_full(t), 8); mbar_init(bar_t_full(t), 1); }
+    mbar_init(bar_qs_full, 1);
     mbar_init(bar_st_full, 8);
     mbar_init(bar_o_full, 1);
     mbar_init(bar_o_empty, 8);
-    mbar_init(bar_o_staged, 8);
     mbar_init(bar_drain, 1);
     fence_mbar_init();
     if (!kStateOnly) { prefetch_tensormap(&tm_q); prefetch_tensormap(&tm_o); }
@@ -150,15 +185,16 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
   }
   if (threadIdx.x == 0) tmem_ptr_smem[1] = *reinterpret_cast<volatile unsigned int*>(p.status);
   if (warp == kMma) { tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_ptr_smem)), 512); tmem_relinquish(); }
-  const double ld = fmin((double)__ldg(p.log_decay + head), 0.0);
-  if (threadIdx.x < 257) {
-    const int d = (int)threadIdx.x - 128;
-    dec[d] = d < 0 ? 0.f : d == 0 ? 1.f : (float)exp((double)d * ld);     // (0 * -inf is NaN: g^0 is 1)
-  }
-  float4* fall = reinterpret_cast<float4*>(smem + L::kOffFall);
-  if (threadIdx.x >= 288 && threadIdx.x < 320) {
-    const int d = 319 - (int)threadIdx.x;
-    reinterpret_cast<float*>(fall)[31 - d] = d == 0 ? 1.f : (float)exp((double)d * ld);
+  const DecayPowers power(__ldg(p.log_decay + head));
+  auto split = [&](float w0, float w1) {                   // two weights as wb + wc, bf16x2 each
+    const uint32_t wb = pack_bf16x2(w0, w1);
+    return make_uint2(wb, pack_bf16x2(w0 - bf16_lo(wb), w1 - bf16_hi(wb)));
+  };
+  {
+    const int tid = threadIdx.x;
+    if (tid < 16) tab[tid] = power(tid);
+    else if (tid < 25) tab[tid] = power(16 * (tid - 16));
+    else if (tid >= 64 && tid < 128) pairs[tid - 64] = split(power(127 - 2 * (tid - 64)), power(126 - 2 * (tid - 64)));
   }
   tc_fence_before();
   __syncthreads();
@@ -169,148 +205,307 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     if (warp == kMma) tmem_dealloc(tmem_base, 512);
     return;
   }
-  constexpr uint32_t kColS = 0, kColO = 128, kColQS = 256, kColT = 384;
+  constexpr uint32_t kColK = 128 * L::kSBuf, kColO = kColK + 128, kColT = kColO + D;     // kColK: K' hi [0,64), lo [64,128)
+  auto col_s = [&](int b) { return (uint32_t)(128 * b); };
+  // where K' and K'^T V of tile c go
+  auto col_k = [&](int c) { return kStateOnly && (c & 1) ? 0u : kColK; };
+  auto col_t = [&](int c) { return kStateOnly && (c & 1) ? kColO : kColT; };
+  bool ok = true;
 
   if (warp < kFirstB) {
+    // =========================================================== A: scores -> P, outputs; two threads per query row
     if constexpr (!kStateOnly) {
-      // =========================================================== scores -> P, outputs; two threads per query row
-      setmaxnreg_dec<88>();
-      const int wq = warp & 3, half = warp >> 2;
-      const int row = wq * 32 + lane;
-      const uint32_t tm = tmem_base + (static_cast<uint32_t>(wq * 32) << 16);
-      const float g1 = p.scale * dec[row + 1];
-      const float2 g1_2 = make_float2(g1, g1);
-      const float* dec_row = dec + row;
-      bool ok = true;
-      for (int c = 0; c < n_tiles; ++c) {
-        const int t0 = (tile0 + c) * 128;
-        const int m = min(128, sq.n_tokens - t0);
+    setmaxnreg_dec<88>();
+    const int wq = warp & 3, half = warp >> 2;
+    const int row = wq * 32 + lane;
+    const uint32_t tm = tmem_base + (static_cast<uint32_t>(wq * 32) << 16);
+    {
+      // The decay of a score, scale * g^{row - j}, without a table (shared memory is what this kernel is short of).  Columns
+      // above the diagonal get whatever comes out and are masked.  All loops over columns are rolled: unrolled, the five
+      // roles' code did not fit the instruction cache, and waiting for instructions was the largest stall.
+      const float l2 = fmaxf(power.hi, -1e4f);
+      const float2 g1_2 = make_float2(p.scale * power(row + 1), p.scale * power(row + 1));
+      const float2 scale2 = make_float2(p.scale, p.scale);
+
+      auto make_p = [&](int c) {                                           // P of tile c
+        const int m = min(128, rem0 - c * 128);
         const bool mixed = p.key_mask != nullptr || m < 128;
-        uint32_t bits[2] = {~0u, ~0u};                        // of this thread's two column blocks
+        uint32_t bits[2] = {~0u, ~0u};                                     // of this thread's two column blocks
         if (mixed) {
 #pragma unroll
           for (int b = 0; b < 2; ++b) {
             const int j = 32 * (2 * b + half) + lane;
             bool valid = j < m;
-            if (valid && p.key_mask != nullptr) valid = p.key_mask[sq.tok_start + t0 + j] != 0;
+            if (valid && p.key_mask != nullptr) valid = p.key_mask[(long long)tok0 + c * 128 + j] != 0;
             bits[b] = __ballot_sync(0xffffffffu, valid);
           }
         }
-        ok = __all_sync(0xffffffffu, mbar_wait(bar_s_full, c & 1, limit));
-        if (!ok) break;
+        const int sb = c % L::kSBuf;
+        ok = __all_sync(0xffffffffu, mbar_wait(bar_s_full(sb), (c / L::kSBuf) & 1, limit));
+        if (!ok) return;
         tc_fence_after();
-        // P of column block cb replaces the scores of that block, in its first 16 columns: a block is read and written by
-        // one warp alone.  Blocks right of the diagonal are zero, left of it every decay exponent is positive.
-#pragma unroll
+        // P of 16 columns replaces the scores of a block of 32, in its first 16 columns (two chunks of 8): a block is read
+        // and written by one warp alone, its second half before the first is overwritten.  Blocks right of the diagonal are zero.
+#pragma unroll 1
         for (int b = 0; b < 2; ++b) {
           const int cb = 2 * b + half;
-          uint32_t pk[16];
+          const uint32_t at = tm + col_s(sb) + cb * 32;
+          const int last = row - cb * 32;                                  // columns up to here lie left of the diagonal or on it
+          const uint32_t on = (b ? bits[1] : bits[0]) & (last >= 31 ? ~0u : last < 0 ? 0u : (2u << last) - 1u);
+          uint32_t s[32];
           if (cb <= wq) {
-            uint32_t s[32];
-            tmem_ld32(tm + kColS + cb * 32, s);
+            tmem_ld32(at, s);
             tmem_wait_ld();
-            if (cb < wq && !mixed) {
-              // g^{row - j} = g^{row - 32 cb - 31} * g^{31 - jj}: the second factor is the same for every row and tile
-              const float lead = p.scale * dec_row[-cb * 32 - 31];
-              const float2 lead2 = make_float2(lead, lead);
+          }
+          uint32_t pk[16];
+          float x = l2 * (float)last;                                      // log2 of g^{row - j} at the block's first column
+          if (cb <= wq) {
 #pragma unroll
-              for (int e = 0; e < 8; ++e) {
-                const float4 d = fall[e];                      // g^{31 - 4 e}, ... - 1, - 2, - 3
-                const float2 lo = mul_f32x2(make_float2(__uint_as_float(s[4 * e]), __uint_as_float(s[4 * e + 1])),
-                                            mul_f32x2(lead2, make_float2(d.x, d.y)));
-                const float2 hi = mul_f32x2(make_float2(__uint_as_float(s[4 * e + 2]), __uint_as_float(s[4 * e + 3])),
-                                            mul_f32x2(lead2, make_float2(d.z, d.w)));
-                pk[2 * e] = pack_bf16x2(lo.x, lo.y);
-                pk[2 * e + 1] = pack_bf16x2(hi.x, hi.y);
-              }
-            } else {
-              const float* d = dec_row - cb * 32;
-              const int last = row - cb * 32;                  // columns beyond it lie above the diagonal
-              const uint32_t on = bits[b] & (last >= 31 ? ~0u : (2u << last) - 1u);
+            for (int e = 0; e < 16; ++e) {
+              const float2 w = mul_f32x2(scale2, make_float2(ex2_approx(x), ex2_approx(x - l2)));
+              const float2 y = mul_f32x2(make_float2(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1])), w);
+              pk[e] = pack_bf16x2(y.x, y.y);
+              x -= 2.f * l2;
+            }
+            if (cb == wq || mixed) {
 #pragma unroll
-              for (int e = 0; e < 16; ++e)
-                pk[e] = pack_bf16x2((on >> (2 * e)) & 1u ? __uint_as_float(s[2 * e]) * (p.scale * d[-2 * e]) : 0.f,
-                                    (on >> (2 * e + 1)) & 1u ? __uint_as_float(s[2 * e + 1]) * (p.scale * d[-2 * e - 1]) : 0.f);
+              for (int e = 0; e < 16; ++e) pk[e] &= pair_mask(on, 2 * e);
             }
           } else {
 #pragma unroll
             for (int e = 0; e < 16; ++e) pk[e] = 0u;
           }
-          tmem_st16(tm + kColS + cb * 32, pk);
+          tmem_st16(at, pk);
         }
-        tmem_wait_st();
+      };
+      // Q S of tile c times g^{i+1}, in place: P V is then accumulated on top.  After that P V may start.
+      auto scale_qs = [&](int c) {
+        ok = __all_sync(0xffffffffu, mbar_wait(bar_qs_full, c & 1, limit));
+        if (!ok) return;
+        tc_fence_after();
+#pragma unroll 1
+        for (int i = 0; i < D / 32; ++i) {
+          const uint32_t at = tm + kColO + half * (D / 2) + i * 16;
+          uint32_t a[16];
+          tmem_ld16(at, a);
+          tmem_wait_ld();
+#pragma unroll
+          for (int e = 0; e < 16; e += 2) {
+            const float2 x = mul_f32x2(g1_2, make_float2(__uint_as_float(a[e]), __uint_as_float(a[e + 1])));
+            a[e] = __float_as_uint(x.x);
+            a[e + 1] = __float_as_uint(x.y);
+          }
+          tmem_st16(at, a);
+        }
+        tmem_wait_st();                                                    // (P's stores too)
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar_p_full);
+        if (lane == 0) mbar_arrive(bar_p_full(c % L::kSBuf));
+      };
 
+      if (L::kSBuf == 2) {
+        make_p(0);
+        if (ok) scale_qs(0);
+      }
+#pragma unroll 1
+      for (int c = 0; c < n_tiles && ok; ++c) {
+        if (L::kSBuf == 1) {
+          make_p(c);
+          if (ok) scale_qs(c);
+        } else if (c + 1 < n_tiles) {
+          make_p(c + 1);
+        }
+        if (!ok) break;
+        const int m = min(128, rem0 - c * 128);
         ok = __all_sync(0xffffffffu, mbar_wait(bar_o_full, c & 1, limit));
         if (!ok) break;
         tc_fence_after();
         // The rows are staged where the tile's V was (nothing reads it any more), in the layout the TMA store expects.  A
         // tile that reaches beyond its sequence is written row by row instead: the rows behind it are not ours.
-        const bool whole = m == 128;
-        __nv_bfloat16* dst = p.out + (sq.tok_start + t0 + row) * p.o_tok_stride + (long long)head * p.o_head_stride + half * (D / 2);
-        uint8_t* stage = smem + L::kOffV + (c % L::kStages) * L::kTile;
-#pragma unroll
-        for (int i = 0; i < D / 64; ++i) {
-          const int cb = half * (D / 64) + i;
-          uint32_t a[32], b[32];
-          tmem_ld32(tm + kColO + cb * 32, a);
-          tmem_ld32(tm + kColQS + cb * 32, b);
+        const int stage_n = c % kS;
+        uint8_t* stage = smem + L::kOffV + stage_n * L::kTile;
+#pragma unroll 1
+        for (int i = 0; i < D / 64; ++i) {                     // 32 of this thread's columns
+          const int at0 = half * (D / 16) + i * 4;             // first of their four 16-byte chunks of the row
+          uint32_t a[32];
+          tmem_ld32(tm + kColO + at0 * 8, a);
           tmem_wait_ld();
           if (i == D / 64 - 1) {                               // everything is in registers: the accumulators are free
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar_o_empty);
           }
+          uint4 w[4];
 #pragma unroll
-          for (int ch = 0; ch < 4; ++ch) {
-            float f[8];
+          for (int ch = 0; ch < 4; ++ch)
+            w[ch] = make_uint4(pack_bf16x2(__uint_as_float(a[8 * ch]), __uint_as_float(a[8 * ch + 1])),
+                               pack_bf16x2(__uint_as_float(a[8 * ch + 2]), __uint_as_float(a[8 * ch + 3])),
+                               pack_bf16x2(__uint_as_float(a[8 * ch + 4]), __uint_as_float(a[8 * ch + 5])),
+                               pack_bf16x2(__uint_as_float(a[8 * ch + 6]), __uint_as_float(a[8 * ch + 7])));
+          if (m == 128) {
+            uint8_t* to = stage + (at0 >> 3) * 16384 + row * 128;
 #pragma unroll
-            for (int e = 0; e < 8; e += 2) {
-              const float2 x = fma_f32x2(g1_2, make_float2(__uint_as_float(b[8 * ch + e]), __uint_as_float(b[8 * ch + e + 1])),
-                                         make_float2(__uint_as_float(a[8 * ch + e]), __uint_as_float(a[8 * ch + e + 1])));
-              f[e] = x.x;
-              f[e + 1] = x.y;
-            }
-            const int at = cb * 4 + ch;                        // 16-byte chunk of the row
-            if (whole)         *reinterpret_cast<uint4*>(stage + (at >> 3) * 16384 + row * 128 + (((at & 7) ^ (row & 7)) << 4)) = pack8(f);
-            else if (row < m)  *reinterpret_cast<uint4*>(dst + i * 32 + ch * 8) = pack8(f);
+            for (int ch = 0; ch < 4; ++ch) *reinterpret_cast<uint4*>(to + ((((at0 & 7) + ch) ^ (row & 7)) << 4)) = w[ch];
+          } else if (row < m) {
+            __nv_bfloat16* to = p.out + ((long long)tok0 + c * 128 + row) * p.o_tok_stride + (long long)head * p.o_head_stride + at0 * 8;
+#pragma unroll
+            for (int ch = 0; ch < 4; ++ch) *reinterpret_cast<uint4*>(to + ch * 8) = w[ch];
           }
         }
         fence_proxy_async_smem();
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar_o_staged);
+        if (lane == 0) mbar_arrive(bar_o_staged(stage_n));
+        if (L::kSBuf == 2 && c + 1 < n_tiles) scale_qs(c + 1);
       }
-      if (!ok && lane == 0) atomicCAS(p.status, 0u, kStatusTimeoutSoftmax);
+    }
+    if (!ok && lane == 0) atomicCAS(p.status, 0u, kStatusTimeoutSoftmax);
     }
   } else if (warp < kTma) {
-    // =========================================================== K -> K', state; two threads per token row / K dim
+    // =========================================================== B: K -> K', state; two threads per token row / K dim
     if (!kStateOnly) setmaxnreg_inc<128>();
     const int wq = (warp - kFirstB) & 3, half = (warp - kFirstB) >> 2;
     const int row = wq * 32 + lane;
     constexpr int kCols = D / 2;                                           // columns of this thread's part of a row
-    const uint32_t tm = tmem_base + (static_cast<uint32_t>(wq * 32) << 16) + kColT + half * kCols;
+    const uint32_t tm = tmem_base + (static_cast<uint32_t>(wq * 32) << 16) + half * kCols;
     float S[kCols];
-#pragma unroll
-    for (int e = 0; e < kCols; ++e) S[e] = 0.f;
     const bool has_state = row < D;                                        // warp-uniform
     // where this thread's 16-byte chunks of a row are in a tile (128-byte swizzle); D = 128: half = 64-column box
-    auto chunk = [&](int ch, int box_bytes) {
+    auto chunk = [&](int r7, int ch, int box_bytes) {
       const int at = half * (kCols / 8) + ch;
-      return (at >> 3) * box_bytes + row * 128 + (((at & 7) ^ (row & 7)) << 4);
+      return (at >> 3) * box_bytes + row * 128 + (((at & 7) ^ r7) << 4);
+    };
+    // row & 7, anew for every use: the compiler would otherwise keep all chunk addresses in registers throughout
+    auto row7 = [&]() {
+      int r7 = row & 7;
+      asm volatile("" : "+r"(r7));
+      return r7;
     };
     auto publish = [&]() {
       // this part of the state's row, rounded to bf16, in the layout of a V tile (row = contraction index)
+      if (has_state) {
+        const int r7 = row7();
 #pragma unroll
-      for (int ch = 0; ch < kCols / 8; ++ch) {
-        float f[8];
+        for (int ch = 0; ch < kCols / 8; ++ch) {
+          float f[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = S[ch * 8 + e];
-        *reinterpret_cast<uint4*>(smem + L::kOffSt + chunk(ch, D * 128)) = pack8(f);
+          for (int e = 0; e < 8; ++e) f[e] = S[ch * 8 + e];
+          *reinterpret_cast<uint4*>(smem + L::kOffSt + chunk(r7, ch, D * 128)) = pack8(f);
+        }
+        fence_proxy_async_smem();
       }
-      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar_st_full);
     };
+    // K' of this warp: K dims 32 wq .. + 31 (tensor-memory lanes), tokens 64 half .. + 63.  ldmatrix hands thread i the token
+    // pairs 64 half + 8 t + 2 (i % 4), + 1 for t = 0..7.  The weights wb + wc of a pair of tokens of a whole tile are two
+    // words of a table; other tiles compute them.
+    auto weight = [&](int e) { return e < 0 ? 0.f : tab[e & 15] * tab[16 + (e >> 4)]; };       // g^e
+    // address of this lane's row for ldmatrix: lanes 0-7 and 16-23 the first 8 of 16 dims, the others the second 8; lanes
+    // 0-15 the first of two token blocks, the others the second
+    const uint32_t k_row = (64 * half + ((lane >> 4) << 3) + (lane & 7)) * 128;
+    const int dc_in = (lane >> 3) & 1;
+
+    // K' of tile n of the ring, into tensor memory at col; rem: tokens from the tile's first one to the sequence's end
+    auto convert = [&](int n, int rem, uint32_t col) {
+      const int m = min(128, rem);
+      const bool mixed = p.key_mask != nullptr || m < 128;
+      const int st = n % kS;
+      const uint32_t ph = (n / kS) & 1;
+      uint32_t bits_lo = ~0u, bits_hi = ~0u, vbits = ~0u;                  // tokens 64 half .., + 32 ..; token rows 32 wq ..
+      if (mixed) {
+#pragma unroll
+        for (int b = 0; b < 3; ++b) {
+          const int j = (b < 2 ? 64 * half + 32 * b : 32 * wq) + lane;
+          bool valid = j < m;
+          if (valid && p.key_mask != nullptr) valid = p.key_mask[(long long)tok0 + n * 128 + j] != 0;
+          const uint32_t word = __ballot_sync(0xffffffffu, valid);
+          if (b == 0) bits_lo = word; else if (b == 1) bits_hi = word; else vbits = word;
+        }
+      }
+      ok = __all_sync(0xffffffffu, mbar_wait(bar_k_full(st), ph, limit));
+      if (!ok) return;
+      tc_fence_after();
+      if (has_state) {
+#pragma unroll 1
+        for (int tg = 0; tg < 2; ++tg) {                                   // 32 tokens
+          uint2 w[4];                                                      // of this thread's pairs in the four token blocks
+          uint32_t on[4];
+#pragma unroll
+          for (int t = 0; t < 4; ++t) {
+            const int in = 32 * tg + 8 * t + 2 * (lane & 3);               // the pair's first token, from token 64 half on
+            if (!mixed) {
+              w[t] = pairs[32 * half + (in >> 1)];
+              on[t] = ~0u;
+            } else {
+              const int e = m - 1 - (64 * half + in);
+              w[t] = split(weight(e), weight(e - 1));
+              on[t] = pair_mask(tg ? bits_hi : bits_lo, in & 31);
+            }
+          }
+#pragma unroll
+          for (int lh = 0; lh < 2; ++lh) {                                 // 16 of the 32 K dims
+            const int dc = 4 * wq + 2 * lh + dc_in;                        // 16-byte chunk of the row
+            const uint32_t src = sK + st * L::kTile + (dc >> 3) * 16384 + k_row + (((dc & 7) ^ (lane & 7)) << 4);
+            uint32_t x[2][4];
+            ldmatrix_x4_trans(src + tg * 32 * 128, x[0]);
+            ldmatrix_x4_trans(src + tg * 32 * 128 + 16 * 128, x[1]);
+            uint32_t hi[8], lo[8];
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {                                  // token block r / 2
+              const uint32_t k2 = x[r >> 2][r & 3] & on[r >> 1];           // whatever stands under a mask, NaN included, is dropped
+              hi[r] = mul_bf16x2(k2, w[r >> 1].x);
+              lo[r] = fma_bf16x2(k2, w[r >> 1].y, fma_bf16x2(k2, w[r >> 1].x, hi[r] ^ 0x80008000u));
+            }
+            const uint32_t dst = tmem_base + (static_cast<uint32_t>(wq * 32 + lh * 16) << 16) + col + half * 32 + tg * 16;
+            tmem_st_16x128b_x4(dst, hi);
+            tmem_st_16x128b_x4(dst + 64, lo);
+          }
+        }
+        tmem_wait_st();
+      }
+      if (mixed) {
+        // V rows that do not count become zeros: 0 * (whatever stands there) would not be 0 for infinities and NaN
+        ok = __all_sync(0xffffffffu, mbar_wait(bar_v_full(st), ph, limit));
+        if (!ok) return;
+        if (((vbits >> lane) & 1u) == 0) {
+          const int r7 = row7();
+#pragma unroll
+          for (int ch = 0; ch < kCols / 8; ++ch)
+            *reinterpret_cast<uint4*>(smem + L::kOffV + st * L::kTile + chunk(r7, ch, 16384)) = make_uint4(0, 0, 0, 0);
+        }
+        fence_proxy_async_smem();
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar_kp_full(n));
+    };
+    // S = g^m S + K'^T V of tile n, read from col
+    auto update = [&](int n, int rem, uint32_t col) {
+      const int m = min(128, rem);
+      ok = __all_sync(0xffffffffu, mbar_wait(bar_t_full(n), (n >> 1) & 1, limit));
+      if (!ok) return;
+      tc_fence_after();
+      if (has_state) {
+        const float gm = tab[m & 15] * tab[16 + (m >> 4)];
+#pragma unroll
+        for (int cb = 0; cb < kCols / 16; ++cb) {
+          uint32_t t[16];
+          tmem_ld16(tm + col + cb * 16, t);
+          tmem_wait_ld();
+#pragma unroll
+          for (int e = 0; e < 16; e += 2) {
+            const float2 x = fma_f32x2(make_float2(gm, gm), make_float2(S[cb * 16 + e], S[cb * 16 + e + 1]),
+                                       make_float2(__uint_as_float(t[e]), __uint_as_float(t[e + 1])));
+            S[cb * 16 + e] = x.x;
+            S[cb * 16 + e + 1] = x.y;
+          }
+        }
+        tc_fence_before();
+      }
+    };
+
+#pragma unroll
+    for (int e = 0; e < kCols; ++e) S[e] = 0.f;
     // the state before this piece
     auto add_piece = [&](const float* piece, float g) {                    // S = g S + what a piece left in the workspace
       const float4* src = reinterpret_cast<const float4*>(piece) + half * (kCols / 4) * D + row;
@@ -326,12 +521,13 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
 #pragma unroll
       for (int e = 0; e < kCols / 4; ++e) dst[e * D] = make_float4(S[4 * e], S[4 * e + 1], S[4 * e + 2], S[4 * e + 3]);
     };
+    const long long state_row = (((long long)p.seqs[si].seq_id * p.heads + head) * D + row) * D + half * kCols;
     if (has_state && seg == 0 && p.state_in != nullptr) {
       // A cut sequence: the state launch is the only one that reads state_in (its first piece starts from it and leaves a
       // copy), so that the main launch may write state_out to the same memory at any time.
       float* copy = p.initial + (long long)(si * p.heads + head) * (D * D);
       if (kStateOnly || n_seg == 1) {
-        const float4* src = reinterpret_cast<const float4*>(p.state_in + (((long long)sq.seq_id * p.heads + head) * D + row) * D + half * kCols);
+        const float4* src = reinterpret_cast<const float4*>(p.state_in + state_row);
 #pragma unroll
         for (int e = 0; e < kCols / 4; ++e) {
           const float4 x = src[e];
@@ -344,254 +540,146 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     }
     if constexpr (!kStateOnly) {
       if (has_state) {
-        const float gs = (float)exp(128.0 * p.seg_tiles * ld);             // every earlier segment is whole
+        const float gs = power(128 * p.seg_tiles);                         // every earlier segment is whole
         for (int r = 0; r < seg; ++r) add_piece(p.local + (long long)(local_first + r * p.heads + head) * (D * D), gs);
-        publish();
       }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar_st_full);
+      publish();
     }
-    // K' of this warp: K dims 32 wq .. + 31 (tensor-memory lanes), tokens 64 half .. + 63.  ldmatrix hands thread i the token
-    // pairs 64 half + 8 t + 2 (i % 4), + 1 for t = 0..7: the weights of those 16 tokens, wb + wc, stay in registers.
-    uint32_t wb[8], wc[8], on[8];                                          // on: all ones for a token that counts
-    auto weights = [&](int m, const uint32_t (&bits)[2]) {
-#pragma unroll
-      for (int t = 0; t < 8; ++t) {
-        float w[2];
-        on[t] = 0u;
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const int in = 8 * t + 2 * (lane & 3) + u, tok = 64 * half + in;
-          const bool counts = ((bits[in >> 5] >> (in & 31)) & 1u) != 0;
-          w[u] = counts ? dec[m - 1 - tok] : 0.f;
-          if (counts) on[t] |= 0xffffu << (16 * u);
-        }
-        wb[t] = pack_bf16x2(w[0], w[1]);
-        wc[t] = pack_bf16x2(w[0] - bf16_lo(wb[t]), w[1] - bf16_hi(wb[t]));
-      }
-    };
-    {
-      const uint32_t all[2] = {~0u, ~0u};
-      weights(128, all);
-    }
-    // address of this lane's row in block (dim chunk dc, token block tb) of a K tile: lanes 0-7 and 16-23 the first 8 of 16
-    // dims, the others the second 8; lanes 0-15 the first token block, the others the next
-    const int tok_in = 64 * half + ((lane >> 4) << 3) + (lane & 7);
-    const uint32_t k_row = tok_in * 128;
-    const int dc_in = (lane >> 3) & 1;
-    bool ok = true;
-    int st = 0;
-    uint32_t ph = 0;
-    for (int c = 0; c < n_tiles; ++c) {
-      const int t0 = (tile0 + c) * 128;
-      const int m = min(128, sq.n_tokens - t0);
-      const bool mixed = p.key_mask != nullptr || m < 128;
-      uint32_t vbits = ~0u;                                                // of the 32 token rows 32 wq ..
-      if (mixed) {
-        uint32_t bits[2];
-#pragma unroll
-        for (int b = 0; b < 3; ++b) {
-          const int j = (b < 2 ? 64 * half + 32 * b : 32 * wq) + lane;
-          bool valid = j < m;
-          if (valid && p.key_mask != nullptr) valid = p.key_mask[sq.tok_start + t0 + j] != 0;
-          const uint32_t word = __ballot_sync(0xffffffffu, valid);
-          if (b < 2) bits[b] = word; else vbits = word;
-        }
-        weights(m, bits);
-      }
-      ok = __all_sync(0xffffffffu, mbar_wait(bar_k_full(st), ph, limit));
-      // the accumulators of the previous tile's outputs, whose columns K' takes, have been read
-      if (!kStateOnly && c > 0) ok = ok && __all_sync(0xffffffffu, mbar_wait(bar_o_empty, (c - 1) & 1, limit));
+    // the state launch converts one tile ahead
+    constexpr int kAhead = kStateOnly ? 1 : 0;
+#pragma unroll 1
+    for (int c = 0; c < n_tiles + kAhead; ++c) {
+      if (c < n_tiles) convert(c, rem0 - c * 128, col_k(c));
       if (!ok) break;
-      tc_fence_after();
-      if (has_state) {
-#pragma unroll
-        for (int lh = 0; lh < 2; ++lh) {                                   // 16 of the 32 K dims
-          const int dc = 4 * wq + 2 * lh + dc_in;                          // 16-byte chunk of the row
-          const uint32_t src = sK + st * L::kTile + (dc >> 3) * 16384 + k_row + (((dc & 7) ^ (lane & 7)) << 4);
-#pragma unroll
-          for (int tg = 0; tg < 2; ++tg) {                                 // 32 tokens
-            uint32_t x[2][4];
-            ldmatrix_x4_trans(src + tg * 32 * 128, x[0]);
-            ldmatrix_x4_trans(src + tg * 32 * 128 + 16 * 128, x[1]);
-            uint32_t hi[8], lo[8];
-#pragma unroll
-            for (int r = 0; r < 8; ++r) {
-              const int t = tg * 4 + (r >> 1);                             // token block
-              uint32_t k2 = x[r >> 2][r & 3];
-              if (mixed) k2 &= on[t];                                      // whatever stands under a mask, NaN included, is dropped
-              hi[r] = mul_bf16x2(k2, wb[t]);
-              lo[r] = fma_bf16x2(k2, wc[t], fma_bf16x2(k2, wb[t], hi[r] ^ 0x80008000u));
-            }
-            const uint32_t dst = tmem_base + (static_cast<uint32_t>(wq * 32 + lh * 16) << 16) + kColO + half * 32 + tg * 16;
-            tmem_st_16x128b_x4(dst, hi);
-            tmem_st_16x128b_x4(dst + 64, lo);
-          }
-        }
-        tmem_wait_st();
-      }
-      if (mixed) {
-        // V rows that do not count become zeros: 0 * (whatever stands there) would not be 0 for infinities and NaN
-        ok = __all_sync(0xffffffffu, mbar_wait(bar_v_full(st), ph, limit));
-        if (!ok) break;
-        if (((vbits >> lane) & 1u) == 0) {
-#pragma unroll
-          for (int ch = 0; ch < kCols / 8; ++ch)
-            *reinterpret_cast<uint4*>(smem + L::kOffV + st * L::kTile + chunk(ch, 16384)) = make_uint4(0, 0, 0, 0);
-        }
-        fence_proxy_async_smem();
-      }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar_kp_full);
-
-      ok = __all_sync(0xffffffffu, mbar_wait(bar_t_full, c & 1, limit));
+      if (c < kAhead) continue;
+      update(c - kAhead, rem0 - (c - kAhead) * 128, col_t(c - kAhead));
       if (!ok) break;
-      tc_fence_after();
-      if (has_state) {
-        const float gm = dec[m];
-#pragma unroll
-        for (int cb = 0; cb < kCols / 32; ++cb) {
-          uint32_t t[32];
-          tmem_ld32(tm + cb * 32, t);
-          tmem_wait_ld();
-#pragma unroll
-          for (int e = 0; e < 32; e += 2) {
-            const float2 x = fma_f32x2(make_float2(gm, gm), make_float2(S[cb * 32 + e], S[cb * 32 + e + 1]),
-                                       make_float2(__uint_as_float(t[e]), __uint_as_float(t[e + 1])));
-            S[cb * 32 + e] = x.x;
-            S[cb * 32 + e + 1] = x.y;
-          }
-        }
-        tc_fence_before();
-        if (!kStateOnly) publish();
-      }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar_st_full);
-      if (++st == L::kStages) { st = 0; ph ^= 1u; }
+      if (!kStateOnly && c + 1 < n_tiles) publish();
     }
-    if (!ok) {
-      if (lane == 0) atomicCAS(p.status, 0u, kStatusTimeoutSoftmax);
-    } else if (has_state) {
+    if (ok && has_state) {
       if constexpr (kStateOnly) {
         leave_piece(p.local + (long long)(local_first + rel) * (D * D));
       } else if (seg == n_seg - 1 && p.state_out != nullptr) {
-        float4* dst = reinterpret_cast<float4*>(p.state_out + (((long long)sq.seq_id * p.heads + head) * D + row) * D + half * kCols);
+        float4* dst = reinterpret_cast<float4*>(p.state_out + state_row);
 #pragma unroll
         for (int e = 0; e < kCols / 4; ++e) dst[e] = make_float4(S[4 * e], S[4 * e + 1], S[4 * e + 2], S[4 * e + 3]);
       }
     }
+    if (!ok && lane == 0) atomicCAS(p.status, 0u, kStatusTimeoutSoftmax);
   } else if (!kStateOnly) {
     setmaxnreg_dec<48>();
   }
+
   if (warp == kTma) {
     // =========================================================== TMA producer
     if (lane == 0) {
       const uint64_t pol_once = l2_policy_evict_first();
-      bool ok = true;
+      auto load = [&](const CUtensorMap* tm, uint32_t base, uint32_t full, int st, int tok, bool once) {
+        mbar_arrive_expect_tx(full, L::kTile);
+#pragma unroll
+        for (int hf = 0; hf < L::kHalves; ++hf) {
+          if (once) tma_load_3d_hint(base + st * L::kTile + hf * 16384, tm, full, hf * 64, head, tok, pol_once);
+          else      tma_load_3d(base + st * L::kTile + hf * 16384, tm, full, hf * 64, head, tok);
+        }
+      };
       int c = 0;
-      for (; c < n_tiles && ok; ++c) {
-        const int st = c % L::kStages, tok = tok0 + (tile0 + c) * 128;
-        const uint32_t par = ((c / L::kStages) & 1) ^ 1u;
+      for (; c < n_tiles; ++c) {
+        const int st = c % kS, tok = tok0 + c * 128;
+        const uint32_t par = ((c / kS) & 1) ^ 1u;
         if (!mbar_wait(bar_k_empty(st), par, limit)) { ok = false; break; }
-        mbar_arrive_expect_tx(bar_k_full(st), L::kTile);
-#pragma unroll
-        for (int hf = 0; hf < L::kHalves; ++hf)
-          tma_load_3d(sK + st * L::kTile + hf * 16384, &tm_k, bar_k_full(st), hf * 64, head, tok);
+        load(&tm_k, sK, bar_k_full(st), st, tok, false);
         if constexpr (!kStateOnly) {
-          const int qs = c % L::kQStages;
-          if (!mbar_wait(bar_q_empty(qs), ((c / L::kQStages) & 1) ^ 1u, limit)) { ok = false; break; }
-          mbar_arrive_expect_tx(bar_q_full(qs), L::kTile);
-#pragma unroll
-          for (int hf = 0; hf < L::kHalves; ++hf)
-            tma_load_3d_hint(sQ + qs * L::kTile + hf * 16384, &tm_q, bar_q_full(qs), hf * 64, head, tok, pol_once);
+          const int qs = c % kQS;
+          if (!mbar_wait(bar_q_empty(qs), ((c / kQS) & 1) ^ 1u, limit)) { ok = false; break; }
+          load(&tm_q, sQ, bar_q_full(qs), qs, tok, true);
         }
         if (!mbar_wait(bar_v_empty(st), par, limit)) { ok = false; break; }
-        mbar_arrive_expect_tx(bar_v_full(st), L::kTile);
-#pragma unroll
-        for (int hf = 0; hf < L::kHalves; ++hf)
-          tma_load_3d(sV + st * L::kTile + hf * 16384, &tm_v, bar_v_full(st), hf * 64, head, tok);
+        load(&tm_v, sV, bar_v_full(st), st, tok, false);
       }
       if (!ok) {
         atomicCAS(p.status, 0u, kStatusTimeoutProducer);
-        // copies still in flight land before the shared memory is given back: every stage's last phase that was begun
-        for (int b = max(0, c - L::kStages); b <= c; ++b) {
-          const int st = b % L::kStages;
-          const uint32_t par = (b / L::kStages) & 1;
-          if (b < c) { mbar_wait(bar_k_full(st), par, limit); mbar_wait(bar_v_full(st), par, limit); }
+        // copies still in flight land before the shared memory is given back; the latest ones (K and Q of the tile it gave
+        // up in) take far less than the limit that has just run out
+        for (int b = max(0, c - kS); b < c; ++b) {
+          mbar_wait(bar_k_full(b % kS), (b / kS) & 1, limit);
+          mbar_wait(bar_v_full(b % kS), (b / kS) & 1, limit);
         }
-        // the tile it gave up in: K (and Q) may have been asked for; a copy takes far less than the limit that has run out
       }
     }
     __syncwarp();
   } else if (warp == kMma) {
     // =========================================================== MMA issuer
     constexpr uint32_t idesc_qk = idesc_bf16_f32(128, 128, false);
-    constexpr uint32_t idesc_d = idesc_bf16_f32(128, D, true);             // B MN-major: P V and Q S
-    constexpr uint32_t kV_lbo = D == 128 ? 16384u : 16u, kSt_lbo = D == 128 ? 16384u : 16u;
+    constexpr uint32_t idesc_d = idesc_bf16_f32(128, D, true);             // B MN-major: P V, Q S and K'^T V
+    constexpr uint32_t kV_lbo = D == 128 ? 16384u : 16u;
     const uint32_t hi_desc = smem_desc_hi_sw128(1024);
     const uint32_t q_lo = smem_desc_lo(sQ, 16), k_lo = smem_desc_lo(sK, 16);
-    const uint32_t v_lo = smem_desc_lo(sV, kV_lbo), st_lo = smem_desc_lo(sSt, kSt_lbo);
+    const uint32_t v_lo = smem_desc_lo(sV, kV_lbo), st_lo = smem_desc_lo(sSt, kV_lbo);
     constexpr uint32_t kStep = L::kTile >> 4;
-    bool ok = true;
-    int st = 0;
-    uint32_t ph = 0;
-    auto wait = [&](uint32_t bar, uint32_t parity) { return mbar_wait_warp(bar, parity, limit); };
-    for (int c = 0; c < n_tiles; ++c) {
-      if (!wait(bar_k_full(st), ph)) { ok = false; break; }
-      if constexpr (!kStateOnly) {
-        const int qs = c % L::kQStages;
-        if (!wait(bar_q_full(qs), (c / L::kQStages) & 1)) { ok = false; break; }
-        tc_fence_after();
-        // scores (the previous tile's P V, which read P there, was issued before)
-#pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
-          const uint32_t off = ((k >> 2) * 16384 + (k & 3) * 32) >> 4;
-          if (k == 0) mma_ss_elect<false>(tmem_base + kColS, q_lo + qs * kStep, k_lo + st * kStep, hi_desc, idesc_qk, 0u);
-          else        mma_ss_elect<true>(tmem_base + kColS, q_lo + qs * kStep + off, k_lo + st * kStep + off, hi_desc, idesc_qk, 1u);
-        }
-        tc_commit_elect(bar_s_full);
-        // Q times the state before this tile
-        if (!wait(bar_st_full, c & 1)) { ok = false; break; }
-        if (c > 0 && !wait(bar_o_empty, (c - 1) & 1)) { ok = false; break; }
-        tc_fence_after();
-#pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
-          const uint32_t off = ((k >> 2) * 16384 + (k & 3) * 32) >> 4;
-          if (k == 0) mma_ss_elect<false>(tmem_base + kColQS, q_lo + qs * kStep, st_lo, hi_desc, idesc_d, 0u);
-          else        mma_ss_elect<true>(tmem_base + kColQS, q_lo + qs * kStep + off, st_lo + k * (2048 >> 4), hi_desc, idesc_d, 1u);
-        }
-        tc_commit_elect(bar_q_empty(qs));
-      } else {
-        if (c > 0 && !wait(bar_st_full, (c - 1) & 1)) { ok = false; break; }         // K'^T V of the previous tile has been read
+    auto wait = [&](uint32_t bar, uint32_t parity) { return ok = mbar_wait_warp(bar, parity, limit); };
+    // scores of tile n (the P V that read P in the same place was issued before)
+    auto issue_scores = [&](int n) {
+      const int qs = n % max(kQS, 1), st = n % kS;
+      if (!wait(bar_k_full(st), (n / kS) & 1) || !wait(bar_q_full(qs), (n / max(kQS, 1)) & 1)) return;
+      tc_fence_after();
+      const uint32_t d = tmem_base + col_s(n % L::kSBuf);
+#pragma unroll 1
+      for (int k = 0; k < D / 16; ++k) {
+        const uint32_t off = ((k >> 2) * 16384 + (k & 3) * 32) >> 4;
+        mma_ss_elect<false>(d, q_lo + qs * kStep + off, k_lo + st * kStep + off, hi_desc, idesc_qk, k);
       }
-      // what the tile adds to the state
-      if (!wait(bar_v_full(st), ph)) { ok = false; break; }
-      if (!wait(bar_kp_full, c & 1)) { ok = false; break; }
+      tc_commit_elect(bar_s_full(n % L::kSBuf));
+    };
+    // what tile kt adds to the state; the product that was there before has been read when K' is ready
+    auto issue_state = [&](int kt) {
+      const uint32_t from = col_k(kt), to = col_t(kt);
+      const int st = kt % kS;
+      if (!wait(bar_v_full(st), (kt / kS) & 1) || !wait(bar_kp_full(kt), (kt >> 1) & 1)) return;
       tc_fence_after();
       // (D = 64: the upper 64 lanes hold no K dims; their rows of the product are never read)
-#pragma unroll
-      for (int k = 0; k < 16; ++k) {                                       // hi, then lo
-        const uint32_t off = (k & 7) * (2048 >> 4);
-        if (k == 0) mma_ts_elect<false>(tmem_base + kColT, tmem_base + kColO, v_lo + st * kStep, hi_desc, idesc_d, 0u);
-        else        mma_ts_elect<true>(tmem_base + kColT, tmem_base + kColO + k * 8, v_lo + st * kStep + off, hi_desc, idesc_d, 1u);
-      }
-      tc_commit_elect(bar_t_full);
+#pragma unroll 1
+      for (int k = 0; k < 16; ++k)                                         // hi, then lo
+        mma_ts_elect<false>(tmem_base + to, tmem_base + from + k * 8, v_lo + st * kStep + (k & 7) * (2048 >> 4), hi_desc, idesc_d, k);
+      tc_commit_elect(bar_t_full(kt));
       tc_commit_elect(bar_k_empty(st));
-      if constexpr (!kStateOnly) {
-        if (!wait(bar_p_full, c & 1)) { ok = false; break; }
-        tc_fence_after();
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const uint32_t off = k * (2048 >> 4);
-          if (k == 0) mma_ts_elect<false>(tmem_base + kColO, tmem_base + kColS, v_lo + st * kStep, hi_desc, idesc_d, 0u);
-          else        mma_ts_elect<true>(tmem_base + kColO, tmem_base + kColS + (k >> 1) * 32 + (k & 1) * 8, v_lo + st * kStep + off, hi_desc, idesc_d, 1u);
-        }
-        tc_commit_elect(bar_o_full);
-      } else {
-        tc_commit_elect(bar_v_empty(st));                                  // (main launch: once the outputs staged there are on their way)
+    };
+    if constexpr (kStateOnly) {
+      for (int c = 0; c < n_tiles; ++c) {
+        issue_state(c);
+        if (!ok) break;
+        tc_commit_elect(bar_v_empty(c % kS));
       }
-      if (++st == L::kStages) { st = 0; ph ^= 1u; }
+    } else {
+      issue_scores(0);
+      for (int c = 0; c < n_tiles && ok; ++c) {
+        const int st = c % kS, qs = c % kQS;
+        // Q times the state before this tile
+        if (!wait(bar_st_full, c & 1)) break;
+        if (c > 0 && !wait(bar_o_empty, (c - 1) & 1)) break;
+        tc_fence_after();
+#pragma unroll 1
+        for (int k = 0; k < D / 16; ++k) {
+          const uint32_t off = ((k >> 2) * 16384 + (k & 3) * 32) >> 4;
+          mma_ss_elect<false>(tmem_base + kColO, q_lo + qs * kStep + off, st_lo + k * (2048 >> 4), hi_desc, idesc_d, k);
+        }
+        tc_commit_elect(bar_qs_full);
+        tc_commit_elect(bar_q_empty(qs));
+        issue_state(c);
+        if (!ok) break;
+        if (L::kSBuf == 2 && c + 1 < n_tiles) {
+          issue_scores(c + 1);
+          if (!ok) break;
+        }
+        const int sb = c % L::kSBuf;
+        if (!wait(bar_p_full(sb), (c / L::kSBuf) & 1)) break;
+        tc_fence_after();
+#pragma unroll 1
+        for (int k = 0; k < 8; ++k)                                        // on top of the scaled Q S
+          mma_ts_elect<true>(tmem_base + kColO, tmem_base + col_s(sb) + (k >> 1) * 32 + (k & 1) * 8,
+                             v_lo + st * kStep + k * (2048 >> 4), hi_desc, idesc_d, 1u);
+        tc_commit_elect(bar_o_full);                                       // (V's space is released once the outputs staged there are out)
+        if (L::kSBuf == 1 && c + 1 < n_tiles) issue_scores(c + 1);
+      }
     }
     if (!ok) {
       if (lane == 0) atomicCAS(p.status, 0u, kStatusTimeoutMma);
@@ -604,12 +692,11 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     if constexpr (!kStateOnly) {
       if (lane == 0) {
         for (int c = 0; c < n_tiles; ++c) {
-          const int st = c % L::kStages;
-          if (!mbar_wait(bar_o_staged, c & 1, limit)) { atomicCAS(p.status, 0u, kStatusTimeoutSoftmax); break; }
-          if (sq.n_tokens - (tile0 + c) * 128 >= 128) {
+          const int st = c % kS;
+          if (!mbar_wait(bar_o_staged(st), (c / kS) & 1, limit)) { atomicCAS(p.status, 0u, kStatusTimeoutSoftmax); break; }
+          if (rem0 - c * 128 >= 128) {
 #pragma unroll
-            for (int hf = 0; hf < L::kHalves; ++hf)
-              tma_store_3d(&tm_o, sV + st * L::kTile + hf * 16384, hf * 64, head, tok0 + (tile0 + c) * 128);
+            for (int hf = 0; hf < L::kHalves; ++hf) tma_store_3d(&tm_o, sV + st * L::kTile + hf * 16384, hf * 64, head, tok0 + c * 128);
             bulk_commit_group();
             bulk_wait_read_all();
           }
