@@ -28,10 +28,15 @@
 //   8-15   (B) K -> K', transposed on the way (ldmatrix) into tensor memory; two threads per K dim: a row of the state
 //   16     TMA producer;   17  MMA issuer, owns the tensor memory;   18  TMA stores of the outputs
 // (the state launch has no A and no stores: B is 0-7, 8 the producer, 9 the issuer).
-// Tensor memory (512 columns): scores / P (D = 64: two buffers, so that the scores of a tile are computed while P of its
-// predecessor is in use); K' hi | lo; the output, which is Q S first, scaled row by row by A, and then accumulates P V;
-// K'^T V.  The state launch has no scores and no outputs: there K' and K'^T V alternate between two places, so that a tile
-// is converted while its predecessor is multiplied.
+// Tensor memory (512 columns): scores / P; K' hi | lo; the output, which is Q S first, scaled row by row by A, and then
+// accumulates P V; K'^T V.  The state launch has no scores and no outputs: there K' and K'^T V alternate between two
+// places, so that a tile is converted while its predecessor is multiplied.
+//
+// head_dim 64 (kPairs): a CTA serves two neighbouring heads at once.  Their Q, K and V side by side are tiles of 128 columns;
+// K' and K'^T V are the products of a 128-dim head of which the two diagonal blocks count, and S is a block-diagonal matrix,
+// so that Q S is one product too.  Only the scores and P V run per head, one after the other.  (One head per CTA left half of
+// B and of the tensor-memory lanes idle: 0.58 ms for 38,871 tokens x 48 heads where pairs take PAIRTIME.)  With an odd number of
+// heads the last pair's second head lies outside the tensors: its loads are filled with zeros, its stores are dropped.
 //
 // HBM needs 2.9 us per tile (4 x 128 x 128 x 2 bytes, every SM streaming).  What comes before it is shared-memory bandwidth,
 // which operands of 128-wide products use up as fast as the tensor core, and with it the latency of everything that goes
@@ -89,34 +94,34 @@ struct DecayPowers {
 };
 
 // Main launch: 19 warps and an idle one, which completes a warpgroup; registers 640 threads x 96 = 256 x 88 + 256 x 128 + 128 x 48.
-constexpr int linear_threads(bool state_only) { return state_only ? 320 : 640; }
+__host__ __device__ constexpr int linear_threads(bool state_only) { return state_only ? 320 : 640; }
 
-template <int D, bool kStateOnly>
+template <bool kStateOnly>
 struct LinearSmem {
-  static constexpr int kTile = 128 * D * 2;
-  static constexpr int kHalves = D / 64;
+  static constexpr int kTile = 128 * 128 * 2;                            // 128 tokens x 128 columns, two boxes of 64 columns
   static constexpr int kQStages = kStateOnly ? 0 : 2;
-  static constexpr int kStages = D == 128 ? (kStateOnly ? 3 : 2) : 4;
-  static constexpr int kSBuf = D == 128 ? 1 : 2;
+  static constexpr int kStages = kStateOnly ? 3 : 2;
   static constexpr int kOffQ = 0;
   static constexpr int kOffK = kOffQ + kQStages * kTile;
   static constexpr int kOffV = kOffK + kStages * kTile;
   static constexpr int kOffSt = kOffV + kStages * kTile;                 // bf16 copy of the state, laid out like V
-  static constexpr int kOffTab = kOffSt + (kStateOnly ? 0 : D * D * 2);   // g^0 .. g^15, g^0, g^16 .. g^128, g^(128 seg_tiles)
-  static constexpr int kOffPairs = kOffTab + 32 * 4;                     // weights of the 64 token pairs of a whole tile, split
-  static constexpr int kOffBars = kOffPairs + 64 * 8;
-  static constexpr int kNumBars = 2 * kQStages + 5 * kStages + 2 * kSBuf + 9;
+  static constexpr int kOffTab = kOffSt + (kStateOnly ? 0 : kTile);       // per head: g^0 .. g^15, g^0, g^16 .. g^128
+  static constexpr int kOffPairs = kOffTab + 2 * 32 * 4;                  // per head: weights of the 64 token pairs of a whole tile, split
+  static constexpr int kOffBars = kOffPairs + 2 * 64 * 8;
+  static constexpr int kNumBars = 2 * kQStages + 5 * kStages + 11;
   static constexpr int kOffTmemPtr = kOffBars + kNumBars * 8;
   static constexpr int kBytes = kOffTmemPtr + 16;
   static constexpr int kDynBytes = kBytes + 1024;
   static_assert(kDynBytes <= 232448, "shared memory of one CTA");
 };
 
-template <int D, bool kStateOnly>
+// kPairs: head_dim 64, two heads per CTA; otherwise head_dim 128
+template <bool kPairs, bool kStateOnly>
 __global__ void __launch_bounds__(linear_threads(kStateOnly), 1)
 linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                    const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_o, const LinearParams p) {
-  using L = LinearSmem<D, kStateOnly>;
+  using L = LinearSmem<kStateOnly>;
+  constexpr int D = kPairs ? 64 : 128, kHeads = kPairs ? 2 : 1;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw_addr = smem_u32(smem_raw);
   const uint32_t sbase = (raw_addr + 1023u) & ~1023u;
@@ -135,29 +140,28 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
   auto bar_v_empty = [&](int s) { return bars + 8u * (2 * kQS + 3 * kS + s); };
   auto bar_o_staged = [&](int s) { return bars + 8u * (2 * kQS + 4 * kS + s); };
   constexpr int kSB = 2 * kQS + 5 * kS;
-  auto bar_s_full = [&](int b) { return bars + 8u * (kSB + b); };
-  auto bar_p_full = [&](int b) { return bars + 8u * (kSB + L::kSBuf + b); };
-  constexpr int kIB = kSB + 2 * L::kSBuf;
-  auto bar_kp_full = [&](int t) { return bars + 8u * (kIB + (t & 1)); };
-  auto bar_t_full = [&](int t) { return bars + 8u * (kIB + 2 + (t & 1)); };
-  const uint32_t bar_st_full = bars + 8u * (kIB + 4), bar_qs_full = bars + 8u * (kIB + 5), bar_o_full = bars + 8u * (kIB + 6),
-                 bar_o_empty = bars + 8u * (kIB + 7), bar_drain = bars + 8u * (kIB + 8);
+  auto bar_kp_full = [&](int t) { return bars + 8u * (kSB + (t & 1)); };
+  auto bar_t_full = [&](int t) { return bars + 8u * (kSB + 2 + (t & 1)); };
+  const uint32_t bar_st_full = bars + 8u * (kSB + 4), bar_qs_full = bars + 8u * (kSB + 5), bar_o_full = bars + 8u * (kSB + 6),
+                 bar_o_empty = bars + 8u * (kSB + 7), bar_drain = bars + 8u * (kSB + 8), bar_s_full = bars + 8u * (kSB + 9),
+                 bar_p_full = bars + 8u * (kSB + 10);
   volatile uint32_t* tmem_ptr_smem = reinterpret_cast<volatile uint32_t*>(smem + L::kOffTmemPtr);
   float* tab = reinterpret_cast<float*>(smem + L::kOffTab);
   uint2* pairs = reinterpret_cast<uint2*>(smem + L::kOffPairs);
 
-  // ---- which piece: sequences in schedule order, then segments, heads fastest (CTAs that run together read neighbouring
-  //      heads of the same tokens).  The state-only launch leaves out each sequence's last segment.
+  // ---- which piece: sequences in schedule order, then segments, heads (or pairs) fastest: CTAs that run together read
+  //      neighbouring heads of the same tokens.  The state-only launch leaves out each sequence's last segment.
+  const int units = (p.heads + kHeads - 1) / kHeads;
   int si = 0, first = 0, local_first = 0, n_seg = 0;
   for (;; ++si) {
     n_seg = (p.seqs[si].n_ktiles + p.seg_tiles - 1) / p.seg_tiles;
-    const int here = (kStateOnly ? n_seg - 1 : n_seg) * p.heads;
+    const int here = (kStateOnly ? n_seg - 1 : n_seg) * units;
     if ((int)blockIdx.x < first + here || si + 1 >= p.n_seqs) break;
     first += here;
-    local_first += (n_seg - 1) * p.heads;
+    local_first += (n_seg - 1) * units;
   }
   const int rel = (int)blockIdx.x - first;
-  const int seg = rel / p.heads, head = rel - seg * p.heads;
+  const int seg = rel / units, unit = rel - seg * units, head = unit * kHeads;              // head: the (first) one
   SOL_DEVICE_CHECK(p.status, rel >= 0 && seg < n_seg, kCheckWorkItem);
   const int n_tiles = min(p.seg_tiles, p.seqs[si].n_ktiles - seg * p.seg_tiles);
   const int tok0 = (int)p.seqs[si].tok_start + seg * p.seg_tiles * 128;     // first token of the piece in the packed tensors
@@ -171,7 +175,8 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       mbar_init(bar_v_full(s), 1); mbar_init(bar_v_empty(s), 1);
       mbar_init(bar_o_staged(s), 8);
     }
-    for (int b = 0; b < L::kSBuf; ++b) { mbar_init(bar_s_full(b), 1); mbar_init(bar_p_full(b), 8); }
+    mbar_init(bar_s_full, 1);
+    mbar_init(bar_p_full, 8);
     for (int t = 0; t < 2; ++t) { mbar_init(bar_kp_full(t), 8); mbar_init(bar_t_full(t), 1); }
     mbar_init(bar_qs_full, 1);
     mbar_init(bar_st_full, 8);
@@ -185,16 +190,23 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
   }
   if (threadIdx.x == 0) tmem_ptr_smem[1] = *reinterpret_cast<volatile unsigned int*>(p.status);
   if (warp == kMma) { tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_ptr_smem)), 512); tmem_relinquish(); }
-  const DecayPowers power(__ldg(p.log_decay + head));
+  auto powers_of = [&](int hd) { return DecayPowers(__ldg(p.log_decay + min(head + hd, p.heads - 1))); };
   auto split = [&](float w0, float w1) {                   // two weights as wb + wc, bf16x2 each
     const uint32_t wb = pack_bf16x2(w0, w1);
     return make_uint2(wb, pack_bf16x2(w0 - bf16_lo(wb), w1 - bf16_hi(wb)));
   };
   {
-    const int tid = threadIdx.x;
-    if (tid < 16) tab[tid] = power(tid);
-    else if (tid < 25) tab[tid] = power(16 * (tid - 16));
-    else if (tid >= 64 && tid < 128) pairs[tid - 64] = split(power(127 - 2 * (tid - 64)), power(126 - 2 * (tid - 64)));
+    const int hd = threadIdx.x >> 7, tid = threadIdx.x & 127;
+    if (hd < kHeads) {
+      const DecayPowers power = powers_of(hd);
+      if (tid < 16) tab[32 * hd + tid] = power(tid);
+      else if (tid < 25) tab[32 * hd + tid] = power(16 * (tid - 16));
+      else if (tid >= 64) pairs[tid - 64 + 64 * hd] = split(power(127 - 2 * (tid - 64)), power(126 - 2 * (tid - 64)));
+    }
+    if (kPairs && !kStateOnly)                              // the blocks of S beside the diagonal
+      for (int i = threadIdx.x; i < L::kTile / 16; i += linear_threads(kStateOnly))
+        *reinterpret_cast<uint4*>(smem + L::kOffSt + i * 16) = make_uint4(0, 0, 0, 0);
+    fence_proxy_async_smem();
   }
   tc_fence_before();
   __syncthreads();
@@ -205,10 +217,9 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     if (warp == kMma) tmem_dealloc(tmem_base, 512);
     return;
   }
-  constexpr uint32_t kColK = 128 * L::kSBuf, kColO = kColK + 128, kColT = kColO + D;     // kColK: K' hi [0,64), lo [64,128)
-  auto col_s = [&](int b) { return (uint32_t)(128 * b); };
+  constexpr uint32_t kColS = 0, kColK = 128, kColO = 256, kColT = 384;     // kColK: K' hi [0,64), lo [64,128)
   // where K' and K'^T V of tile c go
-  auto col_k = [&](int c) { return kStateOnly && (c & 1) ? 0u : kColK; };
+  auto col_k = [&](int c) { return kStateOnly && (c & 1) ? kColS : kColK; };
   auto col_t = [&](int c) { return kStateOnly && (c & 1) ? kColO : kColT; };
   bool ok = true;
 
@@ -223,11 +234,12 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       // The decay of a score, scale * g^{row - j}, without a table (shared memory is what this kernel is short of).  Columns
       // above the diagonal get whatever comes out and are masked.  All loops over columns are rolled: unrolled, the five
       // roles' code did not fit the instruction cache, and waiting for instructions was the largest stall.
-      const float l2 = fmaxf(power.hi, -1e4f);
-      const float2 g1_2 = make_float2(p.scale * power(row + 1), p.scale * power(row + 1));
+      const float l2s[2] = {fmaxf(powers_of(0).hi, -1e4f), kPairs ? fmaxf(powers_of(1).hi, -1e4f) : 0.f};
+      const float g1 = p.scale * powers_of(kPairs ? half : 0)(row + 1);    // this thread's 64 columns are one head's
+      const float2 g1_2 = make_float2(g1, g1);
       const float2 scale2 = make_float2(p.scale, p.scale);
 
-      auto make_p = [&](int c) {                                           // P of tile c
+      auto make_p = [&](int c, int hd) {                                   // P of tile c, head hd
         const int m = min(128, rem0 - c * 128);
         const bool mixed = p.key_mask != nullptr || m < 128;
         uint32_t bits[2] = {~0u, ~0u};                                     // of this thread's two column blocks
@@ -240,8 +252,8 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             bits[b] = __ballot_sync(0xffffffffu, valid);
           }
         }
-        const int sb = c % L::kSBuf;
-        ok = __all_sync(0xffffffffu, mbar_wait(bar_s_full(sb), (c / L::kSBuf) & 1, limit));
+        const float l2 = hd ? l2s[1] : l2s[0];
+        ok = __all_sync(0xffffffffu, mbar_wait(bar_s_full, (c * kHeads + hd) & 1, limit));
         if (!ok) return;
         tc_fence_after();
         // P of 16 columns replaces the scores of a block of 32, in its first 16 columns (two chunks of 8): a block is read
@@ -249,7 +261,7 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
 #pragma unroll 1
         for (int b = 0; b < 2; ++b) {
           const int cb = 2 * b + half;
-          const uint32_t at = tm + col_s(sb) + cb * 32;
+          const uint32_t at = tm + kColS + cb * 32;
           const int last = row - cb * 32;                                  // columns up to here lie left of the diagonal or on it
           const uint32_t on = (b ? bits[1] : bits[0]) & (last >= 31 ? ~0u : last < 0 ? 0u : (2u << last) - 1u);
           uint32_t s[32];
@@ -278,14 +290,20 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
           tmem_st16(at, pk);
         }
       };
-      // Q S of tile c times g^{i+1}, in place: P V is then accumulated on top.  After that P V may start.
+      auto p_done = [&]() {                                                // P (and the scaled Q S) are in place
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar_p_full);
+      };
+      // Q S of tile c times g^{i+1}, in place: P V is then accumulated on top
       auto scale_qs = [&](int c) {
         ok = __all_sync(0xffffffffu, mbar_wait(bar_qs_full, c & 1, limit));
         if (!ok) return;
         tc_fence_after();
 #pragma unroll 1
-        for (int i = 0; i < D / 32; ++i) {
-          const uint32_t at = tm + kColO + half * (D / 2) + i * 16;
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t at = tm + kColO + half * 64 + i * 16;
           uint32_t a[16];
           tmem_ld16(at, a);
           tmem_wait_ld();
@@ -297,23 +315,15 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
           }
           tmem_st16(at, a);
         }
-        tmem_wait_st();                                                    // (P's stores too)
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar_p_full(c % L::kSBuf));
       };
 
-      if (L::kSBuf == 2) {
-        make_p(0);
-        if (ok) scale_qs(0);
-      }
 #pragma unroll 1
       for (int c = 0; c < n_tiles && ok; ++c) {
-        if (L::kSBuf == 1) {
-          make_p(c);
-          if (ok) scale_qs(c);
-        } else if (c + 1 < n_tiles) {
-          make_p(c + 1);
+#pragma unroll 1
+        for (int hd = 0; hd < kHeads && ok; ++hd) {
+          make_p(c, hd);
+          if (ok && hd == 0) scale_qs(c);
+          if (ok) p_done();
         }
         if (!ok) break;
         const int m = min(128, rem0 - c * 128);
@@ -325,12 +335,12 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         const int stage_n = c % kS;
         uint8_t* stage = smem + L::kOffV + stage_n * L::kTile;
 #pragma unroll 1
-        for (int i = 0; i < D / 64; ++i) {                     // 32 of this thread's columns
-          const int at0 = half * (D / 16) + i * 4;             // first of their four 16-byte chunks of the row
+        for (int i = 0; i < 2; ++i) {                          // 32 of this thread's 64 columns
+          const int at0 = half * 8 + i * 4;             // first of their four 16-byte chunks of the row
           uint32_t a[32];
           tmem_ld32(tm + kColO + at0 * 8, a);
           tmem_wait_ld();
-          if (i == D / 64 - 1) {                               // everything is in registers: the accumulators are free
+          if (i == 1) {                               // everything is in registers: the accumulators are free
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar_o_empty);
@@ -346,8 +356,9 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             uint8_t* to = stage + (at0 >> 3) * 16384 + row * 128;
 #pragma unroll
             for (int ch = 0; ch < 4; ++ch) *reinterpret_cast<uint4*>(to + ((((at0 & 7) + ch) ^ (row & 7)) << 4)) = w[ch];
-          } else if (row < m) {
-            __nv_bfloat16* to = p.out + ((long long)tok0 + c * 128 + row) * p.o_tok_stride + (long long)head * p.o_head_stride + at0 * 8;
+          } else if (row < m && (!kPairs || head + half < p.heads)) {
+            __nv_bfloat16* to = p.out + ((long long)tok0 + c * 128 + row) * p.o_tok_stride +
+                                (long long)(kPairs ? head + half : head) * p.o_head_stride + (kPairs ? at0 & 7 : at0) * 8;
 #pragma unroll
             for (int ch = 0; ch < 4; ++ch) *reinterpret_cast<uint4*>(to + ch * 8) = w[ch];
           }
@@ -355,7 +366,6 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(bar_o_staged(stage_n));
-        if (L::kSBuf == 2 && c + 1 < n_tiles) scale_qs(c + 1);
       }
     }
     if (!ok && lane == 0) atomicCAS(p.status, 0u, kStatusTimeoutSoftmax);
@@ -366,13 +376,14 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     const int wq = (warp - kFirstB) & 3, half = (warp - kFirstB) >> 2;
     const int row = wq * 32 + lane;
     constexpr int kCols = D / 2;                                           // columns of this thread's part of a row
-    const uint32_t tm = tmem_base + (static_cast<uint32_t>(wq * 32) << 16) + half * kCols;
+    const int hd = kPairs ? wq >> 1 : 0, col0 = (kPairs ? 64 * hd : 0) + half * kCols;  // the row's head, its part's first column
+    const bool has_state = head + hd < p.heads;                            // warp-uniform
+    const uint32_t tm = tmem_base + (static_cast<uint32_t>(wq * 32) << 16) + col0;
     float S[kCols];
-    const bool has_state = row < D;                                        // warp-uniform
     // where this thread's 16-byte chunks of a row are in a tile (128-byte swizzle); D = 128: half = 64-column box
-    auto chunk = [&](int r7, int ch, int box_bytes) {
-      const int at = half * (kCols / 8) + ch;
-      return (at >> 3) * box_bytes + row * 128 + (((at & 7) ^ r7) << 4);
+    auto chunk = [&](int r7, int ch) {
+      const int at = col0 / 8 + ch;
+      return (at >> 3) * 16384 + row * 128 + (((at & 7) ^ r7) << 4);
     };
     // row & 7, anew for every use: the compiler would otherwise keep all chunk addresses in registers throughout
     auto row7 = [&]() {
@@ -382,24 +393,22 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     };
     auto publish = [&]() {
       // this part of the state's row, rounded to bf16, in the layout of a V tile (row = contraction index)
-      if (has_state) {
-        const int r7 = row7();
+      const int r7 = row7();
 #pragma unroll
-        for (int ch = 0; ch < kCols / 8; ++ch) {
-          float f[8];
+      for (int ch = 0; ch < kCols / 8; ++ch) {
+        float f[8];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) f[e] = S[ch * 8 + e];
-          *reinterpret_cast<uint4*>(smem + L::kOffSt + chunk(r7, ch, D * 128)) = pack8(f);
-        }
-        fence_proxy_async_smem();
+        for (int e = 0; e < 8; ++e) f[e] = S[ch * 8 + e];
+        *reinterpret_cast<uint4*>(smem + L::kOffSt + chunk(r7, ch)) = pack8(f);
       }
+      fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(bar_st_full);
     };
     // K' of this warp: K dims 32 wq .. + 31 (tensor-memory lanes), tokens 64 half .. + 63.  ldmatrix hands thread i the token
     // pairs 64 half + 8 t + 2 (i % 4), + 1 for t = 0..7.  The weights wb + wc of a pair of tokens of a whole tile are two
     // words of a table; other tiles compute them.
-    auto weight = [&](int e) { return e < 0 ? 0.f : tab[e & 15] * tab[16 + (e >> 4)]; };       // g^e
+    auto weight = [&](int e) { return e < 0 ? 0.f : tab[32 * hd + (e & 15)] * tab[32 * hd + 16 + (e >> 4)]; };       // g^e
     // address of this lane's row for ldmatrix: lanes 0-7 and 16-23 the first 8 of 16 dims, the others the second 8; lanes
     // 0-15 the first of two token blocks, the others the second
     const uint32_t k_row = (64 * half + ((lane >> 4) << 3) + (lane & 7)) * 128;
@@ -425,7 +434,6 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       ok = __all_sync(0xffffffffu, mbar_wait(bar_k_full(st), ph, limit));
       if (!ok) return;
       tc_fence_after();
-      if (has_state) {
 #pragma unroll 1
         for (int tg = 0; tg < 2; ++tg) {                                   // 32 tokens
           uint2 w[4];                                                      // of this thread's pairs in the four token blocks
@@ -434,7 +442,7 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
           for (int t = 0; t < 4; ++t) {
             const int in = 32 * tg + 8 * t + 2 * (lane & 3);               // the pair's first token, from token 64 half on
             if (!mixed) {
-              w[t] = pairs[32 * half + (in >> 1)];
+              w[t] = pairs[64 * hd + 32 * half + (in >> 1)];
               on[t] = ~0u;
             } else {
               const int e = m - 1 - (64 * half + in);
@@ -462,16 +470,14 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
           }
         }
         tmem_wait_st();
-      }
       if (mixed) {
         // V rows that do not count become zeros: 0 * (whatever stands there) would not be 0 for infinities and NaN
         ok = __all_sync(0xffffffffu, mbar_wait(bar_v_full(st), ph, limit));
         if (!ok) return;
-        if (((vbits >> lane) & 1u) == 0) {
-          const int r7 = row7();
+        if (((vbits >> lane) & 1u) == 0) {                                 // box `half` of token row `row`
 #pragma unroll
-          for (int ch = 0; ch < kCols / 8; ++ch)
-            *reinterpret_cast<uint4*>(smem + L::kOffV + st * L::kTile + chunk(r7, ch, 16384)) = make_uint4(0, 0, 0, 0);
+          for (int ch = 0; ch < 8; ++ch)
+            *reinterpret_cast<uint4*>(smem + L::kOffV + st * L::kTile + half * 16384 + row * 128 + ch * 16) = make_uint4(0, 0, 0, 0);
         }
         fence_proxy_async_smem();
       }
@@ -485,8 +491,7 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       ok = __all_sync(0xffffffffu, mbar_wait(bar_t_full(n), (n >> 1) & 1, limit));
       if (!ok) return;
       tc_fence_after();
-      if (has_state) {
-        const float gm = tab[m & 15] * tab[16 + (m >> 4)];
+        const float gm = weight(m);
 #pragma unroll
         for (int cb = 0; cb < kCols / 16; ++cb) {
           uint32_t t[16];
@@ -501,37 +506,38 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
           }
         }
         tc_fence_before();
-      }
     };
 
 #pragma unroll
     for (int e = 0; e < kCols; ++e) S[e] = 0.f;
     // the state before this piece
     auto add_piece = [&](const float* piece, float g) {                    // S = g S + what a piece left in the workspace
-      const float4* src = reinterpret_cast<const float4*>(piece) + half * (kCols / 4) * D + row;
+      const float4* src = reinterpret_cast<const float4*>(piece) + half * (kCols / 4) * 128 + row;
 #pragma unroll
       for (int e = 0; e < kCols / 4; ++e) {
-        const float4 x = src[e * D];
+        const float4 x = src[e * 128];
         S[4 * e] = fmaf(g, S[4 * e], x.x); S[4 * e + 1] = fmaf(g, S[4 * e + 1], x.y);
         S[4 * e + 2] = fmaf(g, S[4 * e + 2], x.z); S[4 * e + 3] = fmaf(g, S[4 * e + 3], x.w);
       }
     };
     auto leave_piece = [&](float* piece) {
-      float4* dst = reinterpret_cast<float4*>(piece) + half * (kCols / 4) * D + row;
+      float4* dst = reinterpret_cast<float4*>(piece) + half * (kCols / 4) * 128 + row;
 #pragma unroll
-      for (int e = 0; e < kCols / 4; ++e) dst[e * D] = make_float4(S[4 * e], S[4 * e + 1], S[4 * e + 2], S[4 * e + 3]);
+      for (int e = 0; e < kCols / 4; ++e) dst[e * 128] = make_float4(S[4 * e], S[4 * e + 1], S[4 * e + 2], S[4 * e + 3]);
     };
-    const long long state_row = (((long long)p.seqs[si].seq_id * p.heads + head) * D + row) * D + half * kCols;
-    if (has_state && seg == 0 && p.state_in != nullptr) {
+    const long long state_row = (((long long)p.seqs[si].seq_id * p.heads + head + hd) * D + row % D) * D + half * kCols;
+    if (seg == 0 && p.state_in != nullptr) {
       // A cut sequence: the state launch is the only one that reads state_in (its first piece starts from it and leaves a
       // copy), so that the main launch may write state_out to the same memory at any time.
-      float* copy = p.initial + (long long)(si * p.heads + head) * (D * D);
+      float* copy = p.initial + (long long)(si * units + unit) * (128 * D);
       if (kStateOnly || n_seg == 1) {
+        if (has_state) {
         const float4* src = reinterpret_cast<const float4*>(p.state_in + state_row);
 #pragma unroll
         for (int e = 0; e < kCols / 4; ++e) {
           const float4 x = src[e];
           S[4 * e] = x.x; S[4 * e + 1] = x.y; S[4 * e + 2] = x.z; S[4 * e + 3] = x.w;
+        }
         }
         if (kStateOnly) leave_piece(copy);
       } else {
@@ -539,9 +545,9 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       }
     }
     if constexpr (!kStateOnly) {
-      if (has_state) {
-        const float gs = power(128 * p.seg_tiles);                         // every earlier segment is whole
-        for (int r = 0; r < seg; ++r) add_piece(p.local + (long long)(local_first + r * p.heads + head) * (D * D), gs);
+      if (seg > 0) {
+        const float gs = powers_of(hd)(128 * p.seg_tiles);                 // every earlier segment is whole
+        for (int r = 0; r < seg; ++r) add_piece(p.local + (long long)(local_first + r * units + unit) * (128 * D), gs);
       }
       publish();
     }
@@ -556,10 +562,10 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       if (!ok) break;
       if (!kStateOnly && c + 1 < n_tiles) publish();
     }
-    if (ok && has_state) {
+    if (ok) {
       if constexpr (kStateOnly) {
-        leave_piece(p.local + (long long)(local_first + rel) * (D * D));
-      } else if (seg == n_seg - 1 && p.state_out != nullptr) {
+        leave_piece(p.local + (long long)(local_first + rel) * (128 * D));
+      } else if (has_state && seg == n_seg - 1 && p.state_out != nullptr) {
         float4* dst = reinterpret_cast<float4*>(p.state_out + state_row);
 #pragma unroll
         for (int e = 0; e < kCols / 4; ++e) dst[e] = make_float4(S[4 * e], S[4 * e + 1], S[4 * e + 2], S[4 * e + 3]);
@@ -577,9 +583,10 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       auto load = [&](const CUtensorMap* tm, uint32_t base, uint32_t full, int st, int tok, bool once) {
         mbar_arrive_expect_tx(full, L::kTile);
 #pragma unroll
-        for (int hf = 0; hf < L::kHalves; ++hf) {
-          if (once) tma_load_3d_hint(base + st * L::kTile + hf * 16384, tm, full, hf * 64, head, tok, pol_once);
-          else      tma_load_3d(base + st * L::kTile + hf * 16384, tm, full, hf * 64, head, tok);
+        for (int hf = 0; hf < 2; ++hf) {
+          const int x = kPairs ? 0 : hf * 64, h = kPairs ? head + hf : head;
+          if (once) tma_load_3d_hint(base + st * L::kTile + hf * 16384, tm, full, x, h, tok, pol_once);
+          else      tma_load_3d(base + st * L::kTile + hf * 16384, tm, full, x, h, tok);
         }
       };
       int c = 0;
@@ -610,25 +617,24 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
   } else if (warp == kMma) {
     // =========================================================== MMA issuer
     constexpr uint32_t idesc_qk = idesc_bf16_f32(128, 128, false);
-    constexpr uint32_t idesc_d = idesc_bf16_f32(128, D, true);             // B MN-major: P V, Q S and K'^T V
-    constexpr uint32_t kV_lbo = D == 128 ? 16384u : 16u;
+    constexpr uint32_t idesc_d = idesc_bf16_f32(128, 128, true);           // B MN-major: Q S and K'^T V
+    constexpr uint32_t idesc_pv = idesc_bf16_f32(128, D, true);            // P V of one head
     const uint32_t hi_desc = smem_desc_hi_sw128(1024);
     const uint32_t q_lo = smem_desc_lo(sQ, 16), k_lo = smem_desc_lo(sK, 16);
-    const uint32_t v_lo = smem_desc_lo(sV, kV_lbo), st_lo = smem_desc_lo(sSt, kV_lbo);
+    const uint32_t v_lo = smem_desc_lo(sV, 16384), st_lo = smem_desc_lo(sSt, 16384);
     constexpr uint32_t kStep = L::kTile >> 4;
     auto wait = [&](uint32_t bar, uint32_t parity) { return ok = mbar_wait_warp(bar, parity, limit); };
-    // scores of tile n (the P V that read P in the same place was issued before)
-    auto issue_scores = [&](int n) {
+    // scores of tile n, head hd (the P V that read P in the same place was issued before)
+    auto issue_scores = [&](int n, int hd) {
       const int qs = n % max(kQS, 1), st = n % kS;
-      if (!wait(bar_k_full(st), (n / kS) & 1) || !wait(bar_q_full(qs), (n / max(kQS, 1)) & 1)) return;
+      if (hd == 0 && (!wait(bar_k_full(st), (n / kS) & 1) || !wait(bar_q_full(qs), (n / max(kQS, 1)) & 1))) return;
       tc_fence_after();
-      const uint32_t d = tmem_base + col_s(n % L::kSBuf);
 #pragma unroll 1
       for (int k = 0; k < D / 16; ++k) {
-        const uint32_t off = ((k >> 2) * 16384 + (k & 3) * 32) >> 4;
-        mma_ss_elect<false>(d, q_lo + qs * kStep + off, k_lo + st * kStep + off, hi_desc, idesc_qk, k);
+        const uint32_t off = ((hd + (k >> 2)) * 16384 + (k & 3) * 32) >> 4;
+        mma_ss_elect<false>(tmem_base + kColS, q_lo + qs * kStep + off, k_lo + st * kStep + off, hi_desc, idesc_qk, k);
       }
-      tc_commit_elect(bar_s_full(n % L::kSBuf));
+      tc_commit_elect(bar_s_full);
     };
     // what tile kt adds to the state; the product that was there before has been read when K' is ready
     auto issue_state = [&](int kt) {
@@ -636,12 +642,11 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       const int st = kt % kS;
       if (!wait(bar_v_full(st), (kt / kS) & 1) || !wait(bar_kp_full(kt), (kt >> 1) & 1)) return;
       tc_fence_after();
-      // (D = 64: the upper 64 lanes hold no K dims; their rows of the product are never read)
 #pragma unroll 1
       for (int k = 0; k < 16; ++k)                                         // hi, then lo
         mma_ts_elect<false>(tmem_base + to, tmem_base + from + k * 8, v_lo + st * kStep + (k & 7) * (2048 >> 4), hi_desc, idesc_d, k);
       tc_commit_elect(bar_t_full(kt));
-      tc_commit_elect(bar_k_empty(st));
+      if (!kPairs || kStateOnly) tc_commit_elect(bar_k_empty(st));         // (pairs: the second head's scores need K still)
     };
     if constexpr (kStateOnly) {
       for (int c = 0; c < n_tiles; ++c) {
@@ -650,7 +655,7 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         tc_commit_elect(bar_v_empty(c % kS));
       }
     } else {
-      issue_scores(0);
+      issue_scores(0, 0);
       for (int c = 0; c < n_tiles && ok; ++c) {
         const int st = c % kS, qs = c % kQS;
         // Q times the state before this tile
@@ -658,27 +663,32 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         if (c > 0 && !wait(bar_o_empty, (c - 1) & 1)) break;
         tc_fence_after();
 #pragma unroll 1
-        for (int k = 0; k < D / 16; ++k) {
+        for (int k = 0; k < 8; ++k) {
           const uint32_t off = ((k >> 2) * 16384 + (k & 3) * 32) >> 4;
           mma_ss_elect<false>(tmem_base + kColO, q_lo + qs * kStep + off, st_lo + k * (2048 >> 4), hi_desc, idesc_d, k);
         }
         tc_commit_elect(bar_qs_full);
-        tc_commit_elect(bar_q_empty(qs));
+        if (!kPairs) tc_commit_elect(bar_q_empty(qs));
         issue_state(c);
         if (!ok) break;
-        if (L::kSBuf == 2 && c + 1 < n_tiles) {
-          issue_scores(c + 1);
-          if (!ok) break;
-        }
-        const int sb = c % L::kSBuf;
-        if (!wait(bar_p_full(sb), (c / L::kSBuf) & 1)) break;
-        tc_fence_after();
 #pragma unroll 1
-        for (int k = 0; k < 8; ++k)                                        // on top of the scaled Q S
-          mma_ts_elect<true>(tmem_base + kColO, tmem_base + col_s(sb) + (k >> 1) * 32 + (k & 1) * 8,
-                             v_lo + st * kStep + k * (2048 >> 4), hi_desc, idesc_d, 1u);
+        for (int hd = 0; hd < kHeads; ++hd) {
+          if (!wait(bar_p_full, (c * kHeads + hd) & 1)) break;
+          tc_fence_after();
+#pragma unroll 1
+          for (int k = 0; k < 8; ++k)                                      // on top of the scaled Q S
+            mma_ts_elect<true>(tmem_base + kColO + hd * 64, tmem_base + kColS + (k >> 1) * 32 + (k & 1) * 8,
+                               v_lo + st * kStep + ((hd * 16384 + k * 2048) >> 4), hi_desc, idesc_pv, 1u);
+          if (hd + 1 < kHeads) {
+            issue_scores(c, hd + 1);
+            if (!ok) break;
+            tc_commit_elect(bar_q_empty(qs));
+            tc_commit_elect(bar_k_empty(st));
+          }
+        }
+        if (!ok) break;
         tc_commit_elect(bar_o_full);                                       // (V's space is released once the outputs staged there are out)
-        if (L::kSBuf == 1 && c + 1 < n_tiles) issue_scores(c + 1);
+        if (c + 1 < n_tiles) issue_scores(c + 1, 0);
       }
     }
     if (!ok) {
@@ -696,7 +706,9 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
           if (!mbar_wait(bar_o_staged(st), (c / kS) & 1, limit)) { atomicCAS(p.status, 0u, kStatusTimeoutSoftmax); break; }
           if (rem0 - c * 128 >= 128) {
 #pragma unroll
-            for (int hf = 0; hf < L::kHalves; ++hf) tma_store_3d(&tm_o, sV + st * L::kTile + hf * 16384, hf * 64, head, tok0 + c * 128);
+            for (int hf = 0; hf < 2; ++hf)
+              if (!kPairs || head + hf < p.heads)
+                tma_store_3d(&tm_o, sV + st * L::kTile + hf * 16384, kPairs ? 0 : hf * 64, kPairs ? head + hf : head, tok0 + c * 128);
             bulk_commit_group();
             bulk_wait_read_all();
           }

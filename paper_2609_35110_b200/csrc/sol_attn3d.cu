@@ -124,19 +124,22 @@ cudaError_t raise_shared_memory_limits() {
     e = cudaFuncSetAttribute(sol::attn_fwd_kernel<128, 2, true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                              sol::AttnSmem<128, 2, true>::kDynBytes);
   if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(sol::linear_attn_kernel<128, false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             sol::LinearSmem<128, false>::kDynBytes);
+    e = cudaFuncSetAttribute(sol::linear_attn_kernel<false, false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             sol::LinearSmem<false>::kDynBytes);
   if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(sol::linear_attn_kernel<128, true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             sol::LinearSmem<128, true>::kDynBytes);
+    e = cudaFuncSetAttribute(sol::linear_attn_kernel<false, true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             sol::LinearSmem<true>::kDynBytes);
   if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(sol::linear_attn_kernel<64, false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             sol::LinearSmem<64, false>::kDynBytes);
+    e = cudaFuncSetAttribute(sol::linear_attn_kernel<true, false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             sol::LinearSmem<false>::kDynBytes);
   if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(sol::linear_attn_kernel<64, true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             sol::LinearSmem<64, true>::kDynBytes);
+    e = cudaFuncSetAttribute(sol::linear_attn_kernel<true, true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             sol::LinearSmem<true>::kDynBytes);
   return e;
 }
+
+// Linear attention: a CTA serves one head of 128 dims, or two of 64.
+int linear_units(sol_attn3d_plan_t p) { return p->head_dim == 64 ? (p->heads + 1) / 2 : p->heads; }
 
 // Linear attention: into how many pieces the sequences are cut.  Whole sequences need one launch and read K and V once;
 // pieces keep more SMs busy, but every piece with a successor has its K and V read twice (a launch for the state it adds,
@@ -145,6 +148,7 @@ cudaError_t raise_shared_memory_limits() {
 // piece 2, a predecessor's state 0.3, the extra launch 4.
 void choose_linear_segments(sol_attn3d_plan_t p) {
   constexpr long long kSms = 148;
+  const int units = linear_units(p);
   int longest = 1;
   for (const SeqDev& q : p->sched) longest = std::max(longest, q.n_ktiles);
   double best = 0.0;
@@ -153,8 +157,8 @@ void choose_linear_segments(sol_attn3d_plan_t p) {
     long long pieces = 0, local = 0;
     for (const SeqDev& q : p->sched) {
       const long long segs = (q.n_ktiles + len - 1) / len;
-      pieces += segs * p->heads;
-      local += (segs - 1) * p->heads;
+      pieces += segs * units;
+      local += (segs - 1) * units;
     }
     double cost = (double)((pieces + kSms - 1) / kSms) * (len + 2.0);
     if (local > 0) cost += (double)((local + kSms - 1) / kSms) * (0.6 * len + 2.0) + 0.3 * (n - 1) + 4.0;
@@ -1335,17 +1339,17 @@ int sol_attn3d_linear_step(const void* q, const void* k, const void* v, void* ou
 
 extern "C++" {
 namespace {
-template <int D>
+template <bool kPairs>
 cudaError_t launch_linear(sol_attn3d_plan_t p, const CUtensorMap& tm_q, const CUtensorMap& tm_k, const CUtensorMap& tm_v,
                           const CUtensorMap& tm_o, const sol::LinearParams& lp, cudaStream_t st) {
   if (p->lin_local > 0) {
-    sol::linear_attn_kernel<D, true><<<(unsigned)p->lin_local, sol::linear_threads(true), sol::LinearSmem<D, true>::kDynBytes, st>>>(
+    sol::linear_attn_kernel<kPairs, true><<<(unsigned)p->lin_local, sol::linear_threads(true), sol::LinearSmem<true>::kDynBytes, st>>>(
         tm_q, tm_k, tm_v, tm_o, lp);
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     ++p->launches;
   }
-  sol::linear_attn_kernel<D, false><<<(unsigned)p->lin_pieces, sol::linear_threads(false), sol::LinearSmem<D, false>::kDynBytes, st>>>(
+  sol::linear_attn_kernel<kPairs, false><<<(unsigned)p->lin_pieces, sol::linear_threads(false), sol::LinearSmem<false>::kDynBytes, st>>>(
       tm_q, tm_k, tm_v, tm_o, lp);
   const cudaError_t e = cudaGetLastError();
   if (e == cudaSuccess) ++p->launches;
@@ -1357,7 +1361,7 @@ cudaError_t launch_linear(sol_attn3d_plan_t p, const CUtensorMap& tm_q, const CU
 size_t sol_attn3d_linear_workspace_bytes(sol_attn3d_plan_t p) {
   // one state per piece with a successor, and a copy of every initial state
   if (p == nullptr || p->lin_local == 0) return 0;
-  return align_up(((size_t)p->lin_local + (size_t)p->n_seqs * p->heads) * p->head_dim * p->head_dim * sizeof(float));
+  return align_up(((size_t)p->lin_local + (size_t)p->n_seqs * linear_units(p)) * 128 * p->head_dim * sizeof(float));
 }
 
 int sol_attn3d_forward_linear(sol_attn3d_plan_t p, const void* q, const void* k, const void* v, void* out,
@@ -1391,7 +1395,7 @@ int sol_attn3d_forward_linear(sol_attn3d_plan_t p, const void* q, const void* k,
   lp.state_in = state_in;
   lp.state_out = state_out;
   lp.local = static_cast<float*>(linear_ws);
-  lp.initial = lp.local + (size_t)p->lin_local * p->head_dim * p->head_dim;
+  lp.initial = lp.local + (size_t)p->lin_local * 128 * p->head_dim;
   lp.out = static_cast<__nv_bfloat16*>(out);
   lp.o_tok_stride = p->so.tok;
   lp.o_head_stride = p->so.head;
@@ -1399,8 +1403,8 @@ int sol_attn3d_forward_linear(sol_attn3d_plan_t p, const void* q, const void* k,
   lp.wait_limit_ns = p->wait_limit_ns;
   p->launches = 0;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const cudaError_t e = p->head_dim == 128 ? launch_linear<128>(p, tm_q, tm_k, tm_v, tm_o, lp, st)
-                                            : launch_linear<64>(p, tm_q, tm_k, tm_v, tm_o, lp, st);
+  const cudaError_t e = p->head_dim == 128 ? launch_linear<false>(p, tm_q, tm_k, tm_v, tm_o, lp, st)
+                                            : launch_linear<true>(p, tm_q, tm_k, tm_v, tm_o, lp, st);
   return e == cudaSuccess ? SOL_ATTN3D_OK : fail_cuda(p, e);
 }
 

@@ -89,6 +89,7 @@ def check(case, got, got_state, scale=1.0, mask=None, tokens=None):
     ([(0, 4, 8, 8)], 4, {}),
     ([(3, 2, 9, 21), (0, 1, 1, 1), (200, 2, 5, 11), (64, 0, 1, 1)], 3, dict(strided=True)),
     ([(256, 4, 7, 13)], 40, dict(strided=True)),
+    ([(40, 3, 9, 11), (5, 1, 20, 20)], 5, dict(strided=True)),
 ])
 def test_forward_linear_matches_the_recurrence(seqs, heads, kw, D):
     case = make(seqs, heads, D, 70 + heads, **kw)
@@ -117,6 +118,10 @@ def test_long_sequence_in_pieces(D):
     no_state, _ = run(case, 1.0, mask, state_out=False)
     assert torch.equal(no_state, out)
     case[0].close()
+    odd = make([(17, 7, 20, 20)], 3, D, 81, strided=True)       # an odd number of heads, cut
+    out, dst = run(odd)
+    check(odd, out, dst)
+    odd[0].close()
 
 
 @pytest.mark.parametrize("D", [64, 128])
