@@ -105,7 +105,7 @@ struct LinearSmem {
   static constexpr int kOffK = kOffQ + kQStages * kTile;
   static constexpr int kOffV = kOffK + kStages * kTile;
   static constexpr int kOffSt = kOffV + kStages * kTile;                 // bf16 copy of the state, laid out like V
-  static constexpr int kOffTab = kOffSt + (kStateOnly ? 0 : kTile);       // per head: g^0 .. g^15, g^0, g^16 .. g^128
+  static constexpr int kOffTab = kOffSt + kTile;       // per head: g^0 .. g^15, g^0, g^16 .. g^128
   static constexpr int kOffPairs = kOffTab + 2 * 32 * 4;                  // per head: weights of the 64 token pairs of a whole tile, split
   static constexpr int kOffBars = kOffPairs + 2 * 64 * 8;
   static constexpr int kNumBars = 2 * kQStages + 5 * kStages + 11;
@@ -203,10 +203,6 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       else if (tid < 25) tab[32 * hd + tid] = power(16 * (tid - 16));
       else if (tid >= 64) pairs[tid - 64 + 64 * hd] = split(power(127 - 2 * (tid - 64)), power(126 - 2 * (tid - 64)));
     }
-    if (kPairs && !kStateOnly)                              // the blocks of S beside the diagonal
-      for (int i = threadIdx.x; i < L::kTile / 16; i += linear_threads(kStateOnly))
-        *reinterpret_cast<uint4*>(smem + L::kOffSt + i * 16) = make_uint4(0, 0, 0, 0);
-    fence_proxy_async_smem();
   }
   tc_fence_before();
   __syncthreads();
@@ -525,26 +521,60 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
 #pragma unroll
       for (int e = 0; e < kCols / 4; ++e) dst[e * 128] = make_float4(S[4 * e], S[4 * e + 1], S[4 * e + 2], S[4 * e + 3]);
     };
-    const long long state_row = (((long long)p.seqs[si].seq_id * p.heads + head + hd) * D + row % D) * D + half * kCols;
+    // The caller's states have rows of D values.  A thread reading its own row would touch 32 lines per instruction, so a warp
+    // moves 32 rows x 32 columns at a time, eight lanes per row, through 4 KB of its own in the place of the bf16 copy.
+    uint8_t* mine = smem + L::kOffSt + (warp - kFirstB) * 4096;
+    const long long state0 = (((long long)p.seqs[si].seq_id * p.heads + head + hd) * D + (row - lane) % D) * D + half * kCols;
+    const int l8 = lane & 7, r4 = lane >> 3;
+    auto read_state = [&](const float* state) {
+#pragma unroll
+      for (int b = 0; b < kCols / 32; ++b) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          *reinterpret_cast<float4*>(mine + (4 * i + r4) * 128 + ((l8 ^ ((4 * i + r4) & 7)) << 4)) =
+              *reinterpret_cast<const float4*>(state + state0 + (4 * i + r4) * D + b * 32 + l8 * 4);
+        __syncwarp();
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float4 x = *reinterpret_cast<const float4*>(mine + lane * 128 + ((e ^ l8) << 4));
+          S[b * 32 + 4 * e] = x.x; S[b * 32 + 4 * e + 1] = x.y; S[b * 32 + 4 * e + 2] = x.z; S[b * 32 + 4 * e + 3] = x.w;
+        }
+        __syncwarp();
+      }
+    };
+    auto write_state = [&](float* state) {
+#pragma unroll
+      for (int b = 0; b < kCols / 32; ++b) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          *reinterpret_cast<float4*>(mine + lane * 128 + ((e ^ l8) << 4)) =
+              make_float4(S[b * 32 + 4 * e], S[b * 32 + 4 * e + 1], S[b * 32 + 4 * e + 2], S[b * 32 + 4 * e + 3]);
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          *reinterpret_cast<float4*>(state + state0 + (4 * i + r4) * D + b * 32 + l8 * 4) =
+              *reinterpret_cast<const float4*>(mine + (4 * i + r4) * 128 + ((l8 ^ ((4 * i + r4) & 7)) << 4));
+        __syncwarp();
+      }
+    };
     if (seg == 0 && p.state_in != nullptr) {
       // A cut sequence: the state launch is the only one that reads state_in (its first piece starts from it and leaves a
       // copy), so that the main launch may write state_out to the same memory at any time.
       float* copy = p.initial + (long long)(si * units + unit) * (128 * D);
       if (kStateOnly || n_seg == 1) {
-        if (has_state) {
-        const float4* src = reinterpret_cast<const float4*>(p.state_in + state_row);
-#pragma unroll
-        for (int e = 0; e < kCols / 4; ++e) {
-          const float4 x = src[e];
-          S[4 * e] = x.x; S[4 * e + 1] = x.y; S[4 * e + 2] = x.z; S[4 * e + 3] = x.w;
-        }
-        }
+        if (has_state) read_state(p.state_in);
+        asm volatile("bar.sync 1, 256;" ::: "memory");                     // the others' staging space is theirs until here
         if (kStateOnly) leave_piece(copy);
       } else {
         add_piece(copy, 0.f);
       }
     }
     if constexpr (!kStateOnly) {
+      if (kPairs) {                                                        // S beside its diagonal blocks: this row's half of it
+#pragma unroll
+        for (int ch = 0; ch < 4; ++ch)
+          *reinterpret_cast<uint4*>(smem + L::kOffSt + (hd ^ 1) * 16384 + row * 128 + half * 64 + ch * 16) = make_uint4(0, 0, 0, 0);
+      }
       if (seg > 0) {
         const float gs = powers_of(hd)(128 * p.seg_tiles);                 // every earlier segment is whole
         for (int r = 0; r < seg; ++r) add_piece(p.local + (long long)(local_first + r * units + unit) * (128 * D), gs);
@@ -566,9 +596,7 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       if constexpr (kStateOnly) {
         leave_piece(p.local + (long long)(local_first + rel) * (128 * D));
       } else if (has_state && seg == n_seg - 1 && p.state_out != nullptr) {
-        float4* dst = reinterpret_cast<float4*>(p.state_out + state_row);
-#pragma unroll
-        for (int e = 0; e < kCols / 4; ++e) dst[e] = make_float4(S[4 * e], S[4 * e + 1], S[4 * e + 2], S[4 * e + 3]);
+        write_state(p.state_out);
       }
     }
     if (!ok && lane == 0) atomicCAS(p.status, 0u, kStatusTimeoutSoftmax);
