@@ -13,7 +13,7 @@
 // piece but the last, the state that the piece adds on its own; the second starts each piece from the sum of its
 // predecessors' states (and the caller's), which it forms in a fixed order, and writes the outputs.  (One launch whose
 // pieces hand their states on, so that the second walk finds K and V in L2, was built and measured: 1.6 to 2.0 ms where
-// two launches take LINTIME at 111,856 tokens x 40 heads x 128.  The chain of a tile bounds both, not HBM.)
+// two launches take 1.4 ms at 111,856 tokens x 40 heads x 128.  What bounds the second walk is not HBM.)
 //
 // Precision: products of bf16 values are exact in the fp32 accumulators.  P and the copy of S that the tensor core reads
 // are rounded to bf16 (they only enter bf16 outputs).  K' is split into two bf16 parts, hi + lo, so that the state, which
@@ -35,7 +35,7 @@
 // head_dim 64 (kPairs): a CTA serves two neighbouring heads at once.  Their Q, K and V side by side are tiles of 128 columns;
 // K' and K'^T V are the products of a 128-dim head of which the two diagonal blocks count, and S is a block-diagonal matrix,
 // so that Q S is one product too.  Only the scores and P V run per head, one after the other.  (One head per CTA left half of
-// B and of the tensor-memory lanes idle: 0.58 ms for 38,871 tokens x 48 heads where pairs take PAIRTIME.)  With an odd number of
+// B and of the tensor-memory lanes idle: 0.58 ms for 38,871 tokens x 48 heads where pairs take 0.41 ms.)  With an odd number of
 // heads the last pair's second head lies outside the tensors: its loads are filled with zeros, its stores are dropped.
 //
 // HBM needs 2.9 us per tile (4 x 128 x 128 x 2 bytes, every SM streaming).  What comes before it is shared-memory bandwidth,
