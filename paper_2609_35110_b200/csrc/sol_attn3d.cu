@@ -1230,13 +1230,15 @@ int sol_attn3d_forward_diff(sol_attn3d_plan_t p, const void* q, const void* k, c
 
 extern "C++" {
 namespace {
-// How many CTAs share the keys of one (stream, head pair): enough for about kStepCtas CTAs in all, but no split shorter
-// than kStepMinKeys keys of a full cache.  Depends on the sizes of the call only (the lengths live on the device).
-constexpr long long kStepCtas = 148 * 8, kStepMinKeys = 256;
+// How many CTAs share the keys of one (stream, head pair).  Few items: as many as make three whole waves of resident CTAs
+// (a last wave with a few CTAs costs as much as a full one).  Many items: six waves, so that streams of different length
+// even out.  No split shorter than kStepMinKeys keys of a full cache.  Depends on the sizes of the call only (the lengths live
+// on the device).
+constexpr long long kStepWave = 148 * sol::kStepResident, kStepMinKeys = 512;
 int diff_step_splits(int batch, int pairs, long long capacity) {
   const long long items = (long long)batch * pairs;
-  const long long want = (kStepCtas + items - 1) / items;
-  return (int)std::max<long long>(1, std::min<long long>(want, capacity / kStepMinKeys));
+  const long long want = 4 * items <= 3 * kStepWave ? 3 * kStepWave / items : (6 * kStepWave + items - 1) / items;
+  return (int)std::max<long long>(1, std::min<long long>(std::min<long long>(want, sol::kStepMaxSplit), capacity / kStepMinKeys));
 }
 bool diff_step_sizes_ok(int batch, int heads, int head_dim, long long capacity) {
   return batch >= 0 && heads >= 2 && heads % 2 == 0 && heads <= 65534 && head_dim == 64 && capacity >= 0 &&
@@ -1309,7 +1311,7 @@ int sol_attn3d_diff_step(const void* q, const int64_t q_strides[2], const sol_at
   sol::diff_step_kernel<<<items * (unsigned)a.n_split, sol::kStepThreads, 0, st>>>(a);
   if (cudaGetLastError() != cudaSuccess) return SOL_ATTN3D_ERR_CUDA;
   if (a.n_split > 1) {
-    sol::diff_step_join_kernel<<<items, 128, 0, st>>>(a);
+    sol::diff_step_join_kernel<<<items, 256, 0, st>>>(a);
     if (cudaGetLastError() != cudaSuccess) return SOL_ATTN3D_ERR_CUDA;
   }
   return SOL_ATTN3D_OK;

@@ -32,7 +32,14 @@ __device__ __forceinline__ uint4 pack8(const float (&f)[8]) {
 // softmax runs in the log2 domain with a running maximum per half-warp, moved once per batch of kStepKeys keys.  Every
 // lane accumulates its 8 value dims for both maps.  Half-warps, then splits, are joined with the usual
 // max / rescaled-sum rule in a fixed order, so results do not depend on timing.
+//
+// Bound by HBM once the instructions per key are few enough: 132 per two keys kept the schedulers 69 % busy and the kernel
+// at 222 us for 1.15 GB.  Hence paired fp32 arithmetic, running pointers, a loop without predicates for whole batches, and
+// no rescaling of the accumulators while the maximum stands.
 // ---------------------------------------------------------------------------------------------
+template <bool kValue>
+struct Flag { static constexpr bool value = kValue; };
+
 struct DiffStepArgs {
   const __nv_bfloat16* q;
   long long q_row, q_head;               // element strides
@@ -52,7 +59,7 @@ struct DiffStepArgs {
   float* partial;                        // [batch][pairs][n_split][kStepPartial] when n_split > 1
 };
 
-constexpr int kStepThreads = 256;
+constexpr int kStepThreads = 256, kStepResident = 3;          // CTAs on an SM (2 and 4 were 15 % slower)
 constexpr int kStepKeys = 4;             // keys a half-warp has in flight
 constexpr int kStepPartial = 4 + 256;    // m1, m2, l1, l2, then 128 values per map
 
@@ -73,7 +80,7 @@ __device__ __forceinline__ void diff_step_finish(const DiffStepArgs& a, int b, i
   a.out[(long long)b * a.o_row + (long long)(2 * pair + (e >> 6)) * a.o_head + (e & 63)] = __float2bfloat16_rn(x);
 }
 
-__global__ void __launch_bounds__(kStepThreads) diff_step_kernel(const DiffStepArgs a) {
+__global__ void __launch_bounds__(kStepThreads, kStepResident) diff_step_kernel(const DiffStepArgs a) {
   __shared__ float s_m[2][16], s_l[2][16];
   __shared__ float s_acc[2][16][128];
   __shared__ float s_red[4];
@@ -82,35 +89,44 @@ __global__ void __launch_bounds__(kStepThreads) diff_step_kernel(const DiffStepA
   if (slot < 0 || slot >= a.n_slots) return;                      // idle row: left as it is
   const long long len = max(0ll, min((long long)a.lens[b], a.capacity));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, half = lane >> 4, l16 = lane & 15, map = l16 >> 3;
-  // keys of this split: equal contiguous ranges
-  const long long per = (len + a.n_split - 1) / a.n_split;
+  // keys of this split: equal contiguous ranges, none for the last splits of a short stream
+  const long long per = max((len + a.n_split - 1) / a.n_split, 16ll * kStepKeys);
   const long long k0 = min(len, split * per), k1 = min(len, k0 + per);
 
   // lane l16 of a half-warp: head 2 * pair + map, dims 8 * (l16 & 7) .. + 7, for Q, K and V alike
   const int head = 2 * pair + map, d0 = (l16 & 7) * 8;
-  float q[8];
-  unpack8(*reinterpret_cast<const uint4*>(a.q + (long long)b * a.q_row + (long long)head * a.q_head + d0), q);
+  float2 q[4];
+  {
+    float f[8];
+    unpack8(*reinterpret_cast<const uint4*>(a.q + (long long)b * a.q_row + (long long)head * a.q_head + d0), f);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) q[i] *= a.scale_log2;
+    for (int i = 0; i < 4; ++i) q[i] = make_float2(f[2 * i] * a.scale_log2, f[2 * i + 1] * a.scale_log2);
+  }
   const __nv_bfloat16* kp = a.k + slot * a.k_slot + (long long)head * a.k_head + d0;
   const __nv_bfloat16* vp = a.v + slot * a.v_slot + (long long)head * a.v_head + d0;
   const uint8_t* mp = a.key_mask != nullptr ? a.key_mask + slot * a.mask_slot : nullptr;
 
   float m = -CUDART_INF_F, l = 0.f;      // of this lane's own map
-  float acc0[8] = {}, acc1[8] = {};      // this lane's value dims, map 1 and map 2
+  float2 acc0[4] = {}, acc1[4] = {};     // this lane's value dims, map 1 and map 2
   const int hw = warp * 2 + half;        // 16 half-warps
-  for (long long base = k0; base < k1; base += 16 * kStepKeys) {
+  const __nv_bfloat16* kc = kp + (k0 + hw) * a.k_tok;                      // this half-warp's next key
+  const __nv_bfloat16* vc = vp + (k0 + hw) * a.v_tok;
+  const long long k_step = 16 * a.k_tok, v_step = 16 * a.v_tok;
+  // a batch of keys first, first + 16, ...; kWhole: all of them exist
+  auto batch = [&](long long first, auto whole, auto masked) {
+    constexpr bool kWhole = decltype(whole)::value, kMasked = decltype(masked)::value;
     uint4 kw[kStepKeys], vw[kStepKeys];
     bool on[kStepKeys];
 #pragma unroll
     for (int u = 0; u < kStepKeys; ++u) {
-      const long long key = base + u * 16 + hw;
-      on[u] = key < k1;
-      kw[u] = on[u] ? __ldg(reinterpret_cast<const uint4*>(kp + key * a.k_tok)) : make_uint4(0, 0, 0, 0);
-      vw[u] = on[u] ? __ldg(reinterpret_cast<const uint4*>(vp + key * a.v_tok)) : make_uint4(0, 0, 0, 0);
-      if (mp != nullptr && on[u]) on[u] = mp[key] != 0;
+      on[u] = kWhole || first + u * 16 < k1;
+      kw[u] = on[u] ? __ldg(reinterpret_cast<const uint4*>(kc)) : make_uint4(0, 0, 0, 0);
+      vw[u] = on[u] ? __ldg(reinterpret_cast<const uint4*>(vc)) : make_uint4(0, 0, 0, 0);
+      kc += k_step;
+      vc += v_step;
+      if (kMasked && on[u]) on[u] = __ldg(mp + first + u * 16) != 0;
     }
-    if (mp != nullptr) {
+    if (kMasked) {
       // a masked key has score -inf and value 0: whatever the cache holds there, infinities and NaN included, has no effect
 #pragma unroll
       for (int u = 0; u < kStepKeys; ++u)
@@ -120,40 +136,61 @@ __global__ void __launch_bounds__(kStepThreads) diff_step_kernel(const DiffStepA
     float mx = m;
 #pragma unroll
     for (int u = 0; u < kStepKeys; ++u) {
-      float f[8];
-      unpack8(kw[u], f);
-      float d = 0.f;
+      const uint32_t w[4] = {kw[u].x, kw[u].y, kw[u].z, kw[u].w};
+      float2 d2 = make_float2(0.f, 0.f);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) d = fmaf(q[i], f[i], d);
+      for (int i = 0; i < 4; ++i) d2 = fma_f32x2(q[i], make_float2(bf16_lo(w[i]), bf16_hi(w[i])), d2);
+      float d = d2.x + d2.y;
       d += __shfl_xor_sync(0xffffffffu, d, 1);
       d += __shfl_xor_sync(0xffffffffu, d, 2);
       d += __shfl_xor_sync(0xffffffffu, d, 4);
-      s[u] = on[u] ? d : -CUDART_INF_F;
+      s[u] = (kWhole && !kMasked) || on[u] ? d : -CUDART_INF_F;
       mx = fmaxf(mx, s[u]);
     }
-    const float ref = mx == -CUDART_INF_F ? 0.f : mx;            // no key yet: every exponential below is 2^-inf = 0
-    const float f_old = ex2_approx(m - ref);
-    m = mx;
-    l *= f_old;
-    const float f_other = __shfl_xor_sync(0xffffffffu, f_old, 8);
-    const float g0 = map ? f_other : f_old, g1 = map ? f_old : f_other;
+    if (__any_sync(0xffffffffu, mx > m)) {
+      const float f_old = mx > m ? ex2_approx(m - mx) : 1.f;
+      m = mx;
+      l *= f_old;
+      const float f_other = __shfl_xor_sync(0xffffffffu, f_old, 8);
+      const float g0 = map ? f_other : f_old, g1 = map ? f_old : f_other;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) { acc0[i] *= g0; acc1[i] *= g1; }
+      for (int i = 0; i < 4; ++i) {
+        acc0[i] = mul_f32x2(acc0[i], make_float2(g0, g0));
+        acc1[i] = mul_f32x2(acc1[i], make_float2(g1, g1));
+      }
+    }
+    const float ref = m == -CUDART_INF_F ? 0.f : m;                        // no key yet: every exponential below is 2^-inf = 0
 #pragma unroll
     for (int u = 0; u < kStepKeys; ++u) {
       const float p = ex2_approx(s[u] - ref);
       l += p;
       const float p_other = __shfl_xor_sync(0xffffffffu, p, 8);
       const float p0 = map ? p_other : p, p1 = map ? p : p_other;
-      float f[8];
-      unpack8(vw[u], f);
+      const uint32_t w[4] = {vw[u].x, vw[u].y, vw[u].z, vw[u].w};
 #pragma unroll
-      for (int i = 0; i < 8; ++i) { acc0[i] = fmaf(p0, f[i], acc0[i]); acc1[i] = fmaf(p1, f[i], acc1[i]); }
+      for (int i = 0; i < 4; ++i) {
+        const float2 v2 = make_float2(bf16_lo(w[i]), bf16_hi(w[i]));
+        acc0[i] = fma_f32x2(make_float2(p0, p0), v2, acc0[i]);
+        acc1[i] = fma_f32x2(make_float2(p1, p1), v2, acc1[i]);
+      }
     }
+  };
+  long long base = k0;
+  if (mp == nullptr) {
+#pragma unroll 1
+    for (; base + 16 * kStepKeys <= k1; base += 16 * kStepKeys) batch(base + hw, Flag<true>{}, Flag<false>{});
+    if (base < k1) batch(base + hw, Flag<false>{}, Flag<false>{});
+  } else {
+#pragma unroll 1
+    for (; base + 16 * kStepKeys <= k1; base += 16 * kStepKeys) batch(base + hw, Flag<true>{}, Flag<true>{});
+    if (base < k1) batch(base + hw, Flag<false>{}, Flag<true>{});
   }
   if ((l16 & 7) == 0) { s_m[map][hw] = m; s_l[map][hw] = l; }
 #pragma unroll
-  for (int i = 0; i < 8; ++i) { s_acc[0][hw][l16 * 8 + i] = acc0[i]; s_acc[1][hw][l16 * 8 + i] = acc1[i]; }
+  for (int i = 0; i < 4; ++i) {
+    *reinterpret_cast<float2*>(&s_acc[0][hw][l16 * 8 + 2 * i]) = acc0[i];
+    *reinterpret_cast<float2*>(&s_acc[1][hw][l16 * 8 + 2 * i]) = acc1[i];
+  }
   __syncthreads();
   if (threadIdx.x >= 128) return;
   const int e = threadIdx.x;
@@ -182,30 +219,46 @@ __global__ void __launch_bounds__(kStepThreads) diff_step_kernel(const DiffStepA
   diff_step_finish(a, b, pair, e, x, s_red);
 }
 
-// Joins the splits of one (stream, pair).
-__global__ void __launch_bounds__(128) diff_step_join_kernel(const DiffStepArgs a) {
-  __shared__ float s_red[4];
-  const int pair = blockIdx.x % a.pairs, b = blockIdx.x / a.pairs, e = threadIdx.x;
+// Joins the splits of one (stream, pair): thread = one value of one map.  The weights of the splits are formed once, in
+// parallel, and the values are summed with eight loads in flight: a loop over dependent loads took longer than a tenth of
+// the whole call.
+constexpr int kStepMaxSplit = 512;
+__global__ void __launch_bounds__(256) diff_step_join_kernel(const DiffStepArgs a) {
+  __shared__ float s_w[2][kStepMaxSplit];
+  __shared__ float s_top[8], s_sum[8], s_x[128], s_red[4];
+  const int pair = blockIdx.x % a.pairs, b = blockIdx.x / a.pairs, t = threadIdx.x >> 7, e = threadIdx.x & 127;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const long long slot = a.slots != nullptr ? a.slots[b] : b;
   if (slot < 0 || slot >= a.n_slots) return;
   const float* src = a.partial + ((long long)b * a.pairs + pair) * a.n_split * kStepPartial;
-  float x[2];
-  bool any = true;
+  float top = -CUDART_INF_F;
+  for (int s = e; s < a.n_split; s += 128) top = fmaxf(top, src[(long long)s * kStepPartial + t]);
 #pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    float top = -CUDART_INF_F;
-    for (int s = 0; s < a.n_split; ++s) top = fmaxf(top, src[s * kStepPartial + t]);
-    float sl = 0.f, sx = 0.f;
-    for (int s = 0; s < a.n_split; ++s) {
-      const float w = part_weight(src[s * kStepPartial + t], top);
-      sl = fmaf(w, src[s * kStepPartial + 2 + t], sl);
-      sx = fmaf(w, src[s * kStepPartial + 4 + t * 128 + e], sx);
-    }
-    any = any && sl != 0.f;
-    x[t] = sx / sl;
+  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  if (lane == 0) s_top[warp] = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(s_top[4 * t], s_top[4 * t + 1]), fmaxf(s_top[4 * t + 2], s_top[4 * t + 3]));
+  float sl = 0.f;
+  for (int s = e; s < a.n_split; s += 128) {
+    const float w = part_weight(src[(long long)s * kStepPartial + t], top);
+    s_w[t][s] = w;
+    sl = fmaf(w, src[(long long)s * kStepPartial + 2 + t], sl);
   }
-  const float lam = diff_lambda(a.w, pair, e & 31);
-  diff_step_finish(a, b, pair, e, any ? x[0] - lam * x[1] : 0.f, s_red);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sl += __shfl_xor_sync(0xffffffffu, sl, o);
+  if (lane == 0) s_sum[warp] = sl;
+  __syncthreads();
+  sl = (s_sum[4 * t] + s_sum[4 * t + 1]) + (s_sum[4 * t + 2] + s_sum[4 * t + 3]);
+  float x = 0.f;
+  const float* val = src + 4 + t * 128 + e;
+#pragma unroll 8
+  for (int s = 0; s < a.n_split; ++s) x = fmaf(s_w[t][s], val[(long long)s * kStepPartial], x);
+  x = sl == 0.f ? 0.f : x / sl;                                            // no key: zeros (in both maps)
+  if (t == 1) s_x[e] = x;
+  __syncthreads();
+  if (t == 1) return;
+  const float lam = diff_lambda(a.w, pair, lane);
+  diff_step_finish(a, b, pair, e, x - lam * s_x[e], s_red);
 }
 
 // ---------------------------------------------------------------------------------------------
