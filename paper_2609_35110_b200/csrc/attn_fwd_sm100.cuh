@@ -59,6 +59,10 @@ __device__ __forceinline__ float row_max128(const uint32_t (&r)[128]) {
 // with a polynomial on the FMA pipes was measured more than once (scalar and packed fp32x2 arithmetic, 1/8 to 1/2
 // of the elements) and lost every time: the polynomial costs 12 to 16 issue cycles per element against 8
 // special-function cycles, and the thread-per-row layout has no registers left to interleave enough of them.
+template <bool kF16>
+__device__ __forceinline__ uint32_t pack_p(float lo, float hi) { return kF16 ? pack_f16x2_sat(lo, hi) : pack_bf16x2(lo, hi); }
+
+template <bool kF16 = false>
 __device__ __forceinline__ void softmax_pass(const uint32_t (&r)[128], float c, float mc, uint32_t (&pk)[64],
                                              float& sum) {
   float acc[4] = {0.f, 0.f, 0.f, 0.f};
@@ -68,7 +72,7 @@ __device__ __forceinline__ void softmax_pass(const uint32_t (&r)[128], float c, 
     const float p_hi = ex2_approx(fmaf(__uint_as_float(r[2 * cc + 1]), c, -mc));
     acc[(2 * cc) & 3] += p_lo;
     acc[(2 * cc + 1) & 3] += p_hi;
-    pk[cc] = pack_bf16x2(p_lo, p_hi);
+    pk[cc] = pack_p<kF16>(p_lo, p_hi);
   }
   sum = (acc[0] + acc[1]) + (acc[2] + acc[3]);
 }
@@ -197,6 +201,7 @@ __device__ __forceinline__ void store_rows_int8(const AttnParams& p, const SeqDe
 }
 
 // Half of softmax_pass: 64 columns -> 32 packed pairs, partial sums kept in acc.
+template <bool kF16 = false>
 __device__ __forceinline__ void softmax_half(const uint32_t (&r)[64], float c, float mc, uint32_t (&pk)[32], float (&acc)[4]) {
 #pragma unroll
   for (int cc = 0; cc < 32; ++cc) {
@@ -204,7 +209,7 @@ __device__ __forceinline__ void softmax_half(const uint32_t (&r)[64], float c, f
     const float p_hi = ex2_approx(fmaf(__uint_as_float(r[2 * cc + 1]), c, -mc));
     acc[(2 * cc) & 3] += p_lo;
     acc[(2 * cc + 1) & 3] += p_hi;
-    pk[cc] = pack_bf16x2(p_lo, p_hi);
+    pk[cc] = pack_p<kF16>(p_lo, p_hi);
   }
 }
 
@@ -220,7 +225,8 @@ struct AttnSmem {
   static constexpr int kOffQ = 0;
   static constexpr int kOffKV = (kDiff ? 1 : 2) * kTile;
   static constexpr int kOffBars = kOffKV + kStages * kStageBytes;
-  static constexpr int kNumBars = 1 + 2 * kStages + 7;  // q_full, kv_full/empty, s_full[2], p_full[2], o_done[2], drain
+  // q_full, kv_full/empty, s_full[2], p_full[2], o_done[2], drain; differential attention: v_ready per stage
+  static constexpr int kNumBars = 1 + 2 * kStages + 7 + (kDiff ? kStages : 0);
   static constexpr int kOffTmemPtr = kOffBars + kNumBars * 8;
   static constexpr int kOffXchg = kOffTmemPtr + 16;       // differential attention: row sums and sums of squares, [2][2][128] fp32
   static constexpr int kBytes = kOffXchg + (kDiff ? 2 * 2 * 128 * 4 : 0);
@@ -306,7 +312,12 @@ __device__ __forceinline__ uint4 tail_bits(int rem) {
 // kDiff: differential attention (head_dim 64, CTA pairs).  The two query tiles of a CTA become the two softmax maps of
 // ONE tile of 128 query rows: a head pair (2i, 2i+1) has its two 64-dim Q and K side by side, which in shared memory is
 // exactly one 128-dim tile of two 64-column boxes, and map t multiplies box t of Q with box t of K.  Both maps share the
-// pair's 128-dim V.  Everything between (softmax, ring, accumulators) is the plain kernel's.  Per key tile and CTA that is
+// pair's 128-dim V.  Everything between (softmax, ring, accumulators) is the plain kernel's, but for the types: a difference
+// of two maps amplifies their errors, so Q~, K~, P and V are fp16 operands (11 bits instead of 8).  P is held times 2^7, so
+// that its range, from 2^15 down to 2^-24, reaches 2^-31 of the reference; the two idle warps turn each V tile from bf16
+// into fp16 in shared memory, in place, tiles ahead of its use (values above 65504 saturate).  Error against fp64 at 25,216
+// tokens: 0.0017, the rounding of the output itself (0.0026 with bf16 P and V, 0.0040 with bf16 Q~ and K~ too).
+// Per key tile and CTA that is
 // 2 x 16384 exponentials (2048 cycles of the special-function unit) against 1536 cycles of tensor-core work, so the
 // exponentials bound it: 10.3 ms for 25,216 tokens x 20 pairs, 949 TFLOP/s.
 template <int D, int kCtas, bool kDiff = false>
@@ -339,6 +350,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
   auto bar_p_full = [&](int t) { return bars + 8u * (3 + 2 * L::kStages + t); };
   auto bar_o_done = [&](int t) { return bars + 8u * (5 + 2 * L::kStages + t); };
   const uint32_t bar_drain = bars + 8u * (7 + 2 * L::kStages);
+  auto bar_v_ready = [&](int s) { return bars + 8u * (8 + 2 * L::kStages + s); };   // kDiff: V of both CTAs is fp16
   volatile uint32_t* tmem_ptr_smem = reinterpret_cast<volatile uint32_t*>(smem + L::kOffTmemPtr);
 
   // ---- which work item (one per CTA, or one per CTA pair)
@@ -385,6 +397,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
     for (int s = 0; s < L::kStages; ++s) {
       mbar_init(bar_kv_full(s), 1);
       mbar_init(bar_kv_empty(s), 1);
+      if (kDiff) mbar_init(bar_v_ready(s), 4);           // two converting warps in either CTA
     }
     for (int t = 0; t < 2; ++t) {
       mbar_init(bar_s_full(t), 1);
@@ -435,6 +448,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
     const uint32_t tO = tmem_base + lane_off + 256 + t * D;
     const uint32_t lead_p_full = kPair ? mapa_shared(bar_p_full(t), 0) : bar_p_full(t);
     const float c = p.scale_log2;
+    constexpr float kBias = kDiff ? 7.0f : 0.0f;          // P is held times 2^kBias
     float m_ref = -CUDART_INF_F;
     float l = 0.f;
     bool ok = true;
@@ -466,12 +480,12 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
         tmem_ld32(tS + 64, *reinterpret_cast<uint32_t(*)[32]>(&r[64]));
         tmem_ld32(tS + 96, *reinterpret_cast<uint32_t(*)[32]>(&r[96]));
         float acc[4] = {0.f, 0.f, 0.f, 0.f};
-        const float mc = m_ref * c;
-        softmax_half(r_lo, c, mc, *reinterpret_cast<uint32_t(*)[32]>(&pk[0]), acc);
+        const float mc = m_ref * c - kBias;
+        softmax_half<kDiff>(r_lo, c, mc, *reinterpret_cast<uint32_t(*)[32]>(&pk[0]), acc);
         tmem_wait_ld_dep64(r_hi);
         tmem_st32(tS, *reinterpret_cast<uint32_t(*)[32]>(&pk[0]));       // columns [0,32): their scores are in registers
         first_half_stored = true;
-        softmax_half(r_hi, c, mc, *reinterpret_cast<uint32_t(*)[32]>(&pk[32]), acc);
+        softmax_half<kDiff>(r_hi, c, mc, *reinterpret_cast<uint32_t(*)[32]>(&pk[32]), acc);
         tile_sum = (acc[0] + acc[1]) + (acc[2] + acc[3]);
       } else {
 #pragma unroll
@@ -486,7 +500,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
           }
         }
         if (i == 0) m_ref = row_max128(r);
-        softmax_pass(r, c, m_ref * c, pk, tile_sum);
+        softmax_pass<kDiff>(r, c, m_ref * c - kBias, pk, tile_sum);
       }
       // The pass ran against the current reference maximum, no row maximum taken.
       // All terms are positive, so a row sum <= 2^8 proves that every term is <= 2^8: the reference
@@ -494,7 +508,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
       // does).  Only when the sum is larger (or not finite) is the row maximum computed; if it has grown
       // by more than 2^8 in the exp2 domain the reference moves, l and O are rescaled and the tile is
       // redone from the scores still held in registers, before any of its P is released.  Rare.
-      if (__any_sync(0xffffffffu, !(tile_sum <= 256.0f))) {
+      if (__any_sync(0xffffffffu, !(tile_sum <= (kDiff ? 32768.0f : 256.0f)))) {
         const float mx = row_max128(r);
         const bool grow = (mx - m_ref) * c > 8.0f;
         if (__any_sync(0xffffffffu, grow)) {
@@ -514,7 +528,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             for (int cc = 0; cc < 32; ++cc) o[cc] = __float_as_uint(__uint_as_float(o[cc]) * f);
             tmem_st32(tO + cch * 32, o);
           }
-          softmax_pass(r, c, m_ref * c, pk, tile_sum);
+          softmax_pass<kDiff>(r, c, m_ref * c - kBias, pk, tile_sum);
           if (first_half_stored) tmem_wait_st();                         // the stale first half lands before its replacement
           first_half_stored = false;
         }
@@ -614,7 +628,8 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
 #pragma unroll
         for (int kv = 0; kv < 2; ++kv) {
           if (!mbar_wait(bar_kv_empty(stage), par ^ 1u, limit)) { ok = false; break; }
-          if (leader) mbar_arrive_expect_tx(bar_kv_full(stage), L::kTile);
+          if (kDiff && kv == 1) mbar_arrive_expect_tx(bar_kv_full(stage), L::kStageBytes);   // V: this CTA's own half, see below
+          else if (leader) mbar_arrive_expect_tx(bar_kv_full(stage), L::kTile);
           const uint32_t dst = sKV + stage * L::kStageBytes;
           if (kPair) {
             // this CTA's half of the tile: K = its 64 keys (all head dims, two boxes), V = its 64 head dims (all keys)
@@ -624,9 +639,10 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
               for (int hf = 0; hf < L::kHalves; ++hf)
                 tma_load_3d_pair_hint(dst + hf * L::kKBoxBytes, &tm_k, full, kDiff ? 0 : hf * 64, kDiff ? 2 * head + hf : head,
                                       tok0 + jt * 128 + (int)rank * 64, pol_kv);
+            } else if (kDiff) {
+              tma_load_3d_hint(dst, &tm_v, bar_kv_full(stage), 0, 2 * head + (int)rank, tok0 + jt * 128, pol_kv);
             } else {
-              tma_load_3d_pair_hint(dst, &tm_v, full, kDiff ? 0 : (int)rank * 64, kDiff ? 2 * head + (int)rank : head,
-                                    tok0 + jt * 128, pol_kv);
+              tma_load_3d_pair_hint(dst, &tm_v, full, (int)rank * 64, head, tok0 + jt * 128, pol_kv);
             }
           } else {
             const CUtensorMap* tm = kv ? &tm_v : &tm_k;
@@ -647,6 +663,9 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
           mbar_wait(bar_q_full, 0, limit);
           const uint32_t first = it > (uint32_t)L::kStages ? it - L::kStages : 0u;
           for (uint32_t j = first; j < it; ++j) mbar_wait(bar_kv_full(j % L::kStages), (j / L::kStages) & 1u, limit);
+        } else if (kDiff) {
+          const uint32_t first = it > (uint32_t)L::kStages ? it - L::kStages : 0u;
+          for (uint32_t j = first | 1u; j < it; j += 2) mbar_wait(bar_kv_full(j % L::kStages), (j / L::kStages) & 1u, limit);
         }
       }
     }
@@ -655,9 +674,9 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
     // =========================================================== MMA issuer
     {
       // The whole warp runs this loop (convergent); one elected lane issues each tcgen05 instruction.
-      // differential attention: Q~ and K~ are fp16 (see rope_qk_kernel), P and V bf16 as everywhere
-      constexpr uint32_t idesc_qk = kDiff ? idesc_f16_f32(128 * kCtas, 128) : idesc_bf16_f32(128 * kCtas, 128, false);
-      constexpr uint32_t idesc_pv = idesc_bf16_f32(128 * kCtas, D, true);
+      // differential attention: all operands are fp16
+      constexpr uint32_t idesc_qk = kDiff ? idesc_f16_f32(128 * kCtas, 128, false) : idesc_bf16_f32(128 * kCtas, 128, false);
+      constexpr uint32_t idesc_pv = kDiff ? idesc_f16_f32(128 * kCtas, D, true) : idesc_bf16_f32(128 * kCtas, D, true);
       bool ok = true;
       const uint32_t v_lbo = p.v_lbo, v_sbo = p.v_sbo;
       // descriptor words: only the low word (address) moves inside the loop
@@ -723,7 +742,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
           const bool more = i + 1 < n_proc;
           const uint32_t k_st = st, k_ph = ph;
           if (more) advance();
-          if (!wait_full(bar_kv_full(v_st), v_ph)) { ok = false; break; }
+          if (kDiff ? !mbar_wait_warp_cluster(bar_v_ready(v_st), v_ph, limit) : !wait_full(bar_kv_full(v_st), v_ph)) { ok = false; break; }
           if (!wait_full(bar_p_full(0), i & 1)) { ok = false; break; }
           tc_fence_after();
           issue_pv(tO0, tS0, v_st, i > 0);
@@ -755,6 +774,34 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
       }
     }
     __syncwarp();
+  }
+
+  if (kDiff && (warp == 10 || warp == 11)) {
+    // =========================================================== V tiles: bf16 -> fp16, in place
+    // V tiles are the odd stages of the ring (it has an even number).  Thread = rows t and t + 64 of this CTA's 128 x 64 half;
+    // the chunk order follows the swizzle so that neighbouring rows use different banks.
+    static_assert(!kDiff || L::kStages % 2 == 0, "V tiles keep to the odd stages");
+    const int t = (warp - 10) * 32 + lane;
+    bool ok = true;
+    for (int i = 0; i < n_proc && ok; ++i) {
+      const int n = 2 * i + 1, stage = n % L::kStages;
+      ok = __all_sync(0xffffffffu, mbar_wait(bar_kv_full(stage), (n / L::kStages) & 1, limit));
+      if (!ok) break;
+      uint8_t* tile = smem + L::kOffKV + stage * L::kStageBytes + t * 128;
+#pragma unroll 1
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int ch = 0; ch < 8; ++ch) {
+          uint4* at = reinterpret_cast<uint4*>(tile + h * 64 * 128 + ((ch ^ (t & 7)) << 4));
+          const uint4 w = *at;
+          auto half2 = [](uint32_t x) { return pack_f16x2_sat(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u)); };
+          *at = make_uint4(half2(w.x), half2(w.y), half2(w.z), half2(w.w));
+        }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster_release(mapa_shared(bar_v_ready(stage), 0));
+    }
+    if (!ok && lane == 0) atomicCAS(p.status, 0u, kStatusTimeoutProducer);
   }
 
   // ---- teardown: everyone (of both CTAs) is done with tensor memory and shared memory before they are released
