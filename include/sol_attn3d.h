@@ -420,8 +420,8 @@ typedef struct {
 
 /*
  * Arguments as for sol_attn3d_forward (strides of the plan included); query_mask may be NULL (every row) or as for
- * sol_attn3d_forward_rect.  Rows of a sequence without a valid key are zeros.  K and V values at masked positions must be
- * finite.  Deterministic; may be captured.  Always runs on CTA pairs (SOL_ATTN3D_PAIR does not apply).
+ * sol_attn3d_forward_rect.  Rows of a sequence without a valid key are zeros.  K and V values at masked positions may be
+ * anything (infinities and NaN included).  Deterministic; may be captured.  Always runs on CTA pairs (SOL_ATTN3D_PAIR does not apply).
  * Errors: as for sol_attn3d_forward, UNSUPPORTED_SHAPE for head_dim 128 or an odd number of heads, INVALID_ARG for weights.
  */
 int sol_attn3d_forward_diff(sol_attn3d_plan_t plan, const void* q, const void* k, const void* v, void* out,

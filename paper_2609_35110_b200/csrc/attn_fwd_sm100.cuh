@@ -54,14 +54,15 @@ __device__ __forceinline__ float row_max128(const uint32_t (&r)[128]) {
   return max3(m0, m1, fmaxf(__uint_as_float(r[126]), __uint_as_float(r[127])));
 }
 
+// P of two neighbouring columns in the operand type of the second product.
+template <bool kF16>
+__device__ __forceinline__ uint32_t pack_p(float lo, float hi) { return kF16 ? pack_f16x2_sat(lo, hi) : pack_bf16x2(lo, hi); }
+
 // One pass over a 128-column score row held in registers: p = 2^(s*c - mc) packed to bf16 and the fp32
 // row sum of the un-rounded p.  Every exponential goes to the special-function unit: evaluating a share of them
 // with a polynomial on the FMA pipes was measured more than once (scalar and packed fp32x2 arithmetic, 1/8 to 1/2
 // of the elements) and lost every time: the polynomial costs 12 to 16 issue cycles per element against 8
 // special-function cycles, and the thread-per-row layout has no registers left to interleave enough of them.
-template <bool kF16>
-__device__ __forceinline__ uint32_t pack_p(float lo, float hi) { return kF16 ? pack_f16x2_sat(lo, hi) : pack_bf16x2(lo, hi); }
-
 template <bool kF16 = false>
 __device__ __forceinline__ void softmax_pass(const uint32_t (&r)[128], float c, float mc, uint32_t (&pk)[64],
                                              float& sum) {
@@ -779,7 +780,8 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
   if (kDiff && (warp == 10 || warp == 11)) {
     // =========================================================== V tiles: bf16 -> fp16, in place
     // V tiles are the odd stages of the ring (it has an even number).  Thread = rows t and t + 64 of this CTA's 128 x 64 half;
-    // the chunk order follows the swizzle so that neighbouring rows use different banks.
+    // the chunk order follows the swizzle so that neighbouring rows use different banks.  Rows of keys that do not count
+    // become zeros: 0 * (whatever stands there) would not be 0 for infinities and NaN.
     static_assert(!kDiff || L::kStages % 2 == 0, "V tiles keep to the odd stages");
     const int t = (warp - 10) * 32 + lane;
     bool ok = true;
@@ -788,15 +790,21 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
       ok = __all_sync(0xffffffffu, mbar_wait(bar_kv_full(stage), (n / L::kStages) & 1, limit));
       if (!ok) break;
       uint8_t* tile = smem + L::kOffKV + stage * L::kStageBytes + t * 128;
+      const int it = backwards ? n_proc - 1 - i : i;
+      const int jt = all_keys ? it : __ldg(&ktiles[it]);
+      const uint4 kb = all_keys ? tail_bits(sq.n_tokens - jt * 128) : __ldg(&keybits[jt]);
 #pragma unroll 1
-      for (int h = 0; h < 2; ++h)
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t bits = h == 0 ? (warp == 10 ? kb.x : kb.y) : (warp == 10 ? kb.z : kb.w);    // of rows 64 h + 32 (warp - 10) ..
+        const uint32_t keep = 0u - ((bits >> lane) & 1u);
 #pragma unroll
         for (int ch = 0; ch < 8; ++ch) {
           uint4* at = reinterpret_cast<uint4*>(tile + h * 64 * 128 + ((ch ^ (t & 7)) << 4));
           const uint4 w = *at;
           auto half2 = [](uint32_t x) { return pack_f16x2_sat(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u)); };
-          *at = make_uint4(half2(w.x), half2(w.y), half2(w.z), half2(w.w));
+          *at = make_uint4(half2(w.x) & keep, half2(w.y) & keep, half2(w.z) & keep, half2(w.w) & keep);
         }
+      }
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive_cluster_release(mapa_shared(bar_v_ready(stage), 0));

@@ -141,6 +141,28 @@ def test_masked_keys_do_not_matter():
     attn.close()
 
 
+def test_garbage_under_masks_and_in_the_neighbour_sequence():
+    """Infinities and NaN in K and V at masked positions, and in the sequence that shares the last key tile, have no effect."""
+    from paper_2609_35110_b200 import binding as B
+    seqs = [(300, 2, 6, 6), (70, 0, 1, 1)]
+    attn, (q, k, v), w, o = make(seqs, 2, 8)
+    mask = torch.ones(attn.total_tokens, dtype=torch.uint8)
+    mask[100:290] = 0
+    for m in (mask.cuda(), None):
+        off = torch.zeros(attn.total_tokens, dtype=torch.bool) if m is None else ~mask.bool()
+        off[372:] = True                                                       # the second sequence's rows end the first one's tile
+        a, b = torch.empty_like(q), torch.empty_like(q)
+        B.sol_attn3d_forward_diff(attn.plan, q, k, v, a, m, w)
+        k2, v2 = k.clone(), v.clone()
+        k2[off.cuda()] = float("nan")
+        v2[off.cuda()] = torch.tensor([float("nan"), float("inf")]).bfloat16().cuda().repeat(32)
+        B.sol_attn3d_forward_diff(attn.plan, q, k2, v2, b, m, w)
+        torch.cuda.synchronize()
+        assert attn.status() == 0
+        assert torch.isfinite(a).all() and torch.equal(a[:372], b[:372])
+    attn.close()
+
+
 def test_logit_ramp_moves_the_reference():
     """Logits that grow along the keys by far more than 2^8 per tile: both maps move their reference maximum."""
     from paper_2609_35110_b200 import binding as B
