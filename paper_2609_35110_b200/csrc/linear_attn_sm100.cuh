@@ -57,6 +57,8 @@ struct LinearParams {
   int n_seqs;
   int heads;
   int seg_tiles;              // tiles of a piece
+  int n_cut;                  // sequences of more than one piece: the first ones of the schedule, which is longest first
+  int cut_pieces;             // their pieces; then every sequence is one piece per unit
   const uint8_t* key_mask;    // uint8 [total_tokens] or nullptr
   const float* log_decay;     // [heads]
   float scale;
@@ -150,19 +152,26 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
   uint2* pairs = reinterpret_cast<uint2*>(smem + L::kOffPairs);
 
   // ---- which piece: sequences in schedule order, then segments, heads (or pairs) fastest: CTAs that run together read
-  //      neighbouring heads of the same tokens.  The state-only launch leaves out each sequence's last segment.
+  //      neighbouring heads of the same tokens.  The state-only launch leaves out each sequence's last segment.  Only the
+  //      sequences that are cut are walked over (there are few: cutting is for filling SMs).
   const int units = (p.heads + kHeads - 1) / kHeads;
-  int si = 0, first = 0, local_first = 0, n_seg = 0;
-  for (;; ++si) {
-    n_seg = (p.seqs[si].n_ktiles + p.seg_tiles - 1) / p.seg_tiles;
-    const int here = (kStateOnly ? n_seg - 1 : n_seg) * units;
-    if ((int)blockIdx.x < first + here || si + 1 >= p.n_seqs) break;
-    first += here;
-    local_first += (n_seg - 1) * units;
+  int si = 0, first = 0, local_first = 0, n_seg = 1;
+  if (!kStateOnly && (int)blockIdx.x >= p.cut_pieces) {
+    const int whole = ((int)blockIdx.x - p.cut_pieces) / units;
+    si = p.n_cut + whole;
+    first = p.cut_pieces + whole * units;
+  } else {
+    for (;; ++si) {
+      n_seg = (p.seqs[si].n_ktiles + p.seg_tiles - 1) / p.seg_tiles;
+      const int here = (kStateOnly ? n_seg - 1 : n_seg) * units;
+      if ((int)blockIdx.x < first + here || si + 1 >= p.n_cut) break;
+      first += here;
+      local_first += (n_seg - 1) * units;
+    }
   }
   const int rel = (int)blockIdx.x - first;
   const int seg = rel / units, unit = rel - seg * units, head = unit * kHeads;              // head: the (first) one
-  SOL_DEVICE_CHECK(p.status, rel >= 0 && seg < n_seg, kCheckWorkItem);
+  SOL_DEVICE_CHECK(p.status, si < p.n_seqs && rel >= 0 && seg < n_seg, kCheckWorkItem);
   const int n_tiles = min(p.seg_tiles, p.seqs[si].n_ktiles - seg * p.seg_tiles);
   const int tok0 = (int)p.seqs[si].tok_start + seg * p.seg_tiles * 128;     // first token of the piece in the packed tensors
   const int rem0 = p.seqs[si].n_tokens - seg * p.seg_tiles * 128;           // tokens from there to the sequence's end

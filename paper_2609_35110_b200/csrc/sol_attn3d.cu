@@ -50,8 +50,11 @@ struct sol_attn3d_plan_s {
   int total_quad_work = 0;            // work items when CTA pairs serve 512-row query blocks
   int pair_mode = 1;                  // CTA pairs (cta_group::2) where they apply: head_dim 128, not block-sparse
   int total_ktiles = 0;
-  int lin_seg_tiles = 1;              // linear attention: tiles per piece of a sequence, pieces, pieces with a successor
-  long long lin_pieces = 0, lin_local = 0;
+  // linear attention (0 until the first call that asks): tiles per piece of a sequence; pieces, pieces with a successor,
+  // pieces of the sequences that have more than one, those sequences
+  int lin_seg_tiles = 0;
+  long long lin_pieces = 0, lin_local = 0, lin_cut_pieces = 0;
+  int lin_cut = 0;
   std::vector<float2> tables;
   int tab_off[3] = {0, 0, 0};
 
@@ -149,7 +152,9 @@ int linear_units(sol_attn3d_plan_t p) { return p->head_dim == 64 ? (p->heads + 1
 // pieces to the SMs as the hardware does, in order, each to the SM that is free first.  The unit is a tile of the main launch
 // (3.7 us at head_dim 128); a tile of the state launch is 0.4, starting a piece 2, a predecessor's state 0.3, the extra launch 1.
 // 111,856 tokens x 40 heads x 128: 11 pieces are chosen and took 1.41 ms, its neighbours 8 and 15 1.54 and 1.52.
+// Up to some 30 ms of host time, once per plan and only for a plan that asks.
 void choose_linear_segments(sol_attn3d_plan_t p) {
+  if (p->lin_seg_tiles > 0) return;
   constexpr int kSms = 148;
   const int units = linear_units(p);
   int longest = 1;
@@ -157,11 +162,14 @@ void choose_linear_segments(sol_attn3d_plan_t p) {
   double best = 0.0;
   for (int n = 1; n <= std::min(longest, 64); ++n) {
     const int len = (longest + n - 1) / n;
-    long long pieces = 0, local = 0;
+    if (n > 1 && len == p->lin_seg_tiles) continue;
+    long long pieces = 0, local = 0, cut_pieces = 0;
+    int cut = 0;
     for (const SeqDev& q : p->sched) {
       const long long segs = (q.n_ktiles + len - 1) / len;
       pieces += segs * units;
       local += (segs - 1) * units;
+      if (segs > 1) { ++cut; cut_pieces += segs * units; }
     }
     if (n > 1 && pieces > 16384) break;
     double cost = local > 0 ? 1.0 : 0.0;
@@ -191,6 +199,8 @@ void choose_linear_segments(sol_attn3d_plan_t p) {
       p->lin_seg_tiles = len;
       p->lin_pieces = pieces;
       p->lin_local = local;
+      p->lin_cut = cut;
+      p->lin_cut_pieces = cut_pieces;
     }
   }
 }
@@ -314,7 +324,6 @@ int build_plan(sol_attn3d_plan_t* out, const sol_attn3d_desc* d) {
     p->total_quad_work = (int)quad_work;
     p->total_ktiles = (int)ktiles;
     p->total_pairs = (int)pairs;
-    choose_linear_segments(p);
 
     // cos/sin tables, built in fp64 and rounded once to fp32
     size_t n_entries = 0;
@@ -1386,7 +1395,9 @@ cudaError_t launch_linear(sol_attn3d_plan_t p, const CUtensorMap& tm_q, const CU
 
 size_t sol_attn3d_linear_workspace_bytes(sol_attn3d_plan_t p) {
   // one state per piece with a successor, and a copy of every initial state
-  if (p == nullptr || p->lin_local == 0) return 0;
+  if (p == nullptr) return 0;
+  choose_linear_segments(p);
+  if (p->lin_local == 0) return 0;
   return align_up(((size_t)p->lin_local + (size_t)p->n_seqs * linear_units(p)) * 128 * p->head_dim * sizeof(float));
 }
 
@@ -1399,6 +1410,7 @@ int sol_attn3d_forward_linear(sol_attn3d_plan_t p, const void* q, const void* k,
       (reinterpret_cast<uintptr_t>(log_decay) & 3u) != 0 || !std::isfinite(scale))
     return SOL_ATTN3D_ERR_INVALID_ARG;
   if (out == q || out == k || out == v) return SOL_ATTN3D_ERR_INVALID_ARG;
+  choose_linear_segments(p);
   if (p->lin_pieces >= (1ll << 31)) return SOL_ATTN3D_ERR_UNSUPPORTED_SHAPE;
   if (p->ws == nullptr || p->encode == nullptr) return SOL_ATTN3D_ERR_NO_WORKSPACE;
   if (p->lin_local > 0 && (linear_ws == nullptr || linear_ws_bytes < sol_attn3d_linear_workspace_bytes(p) ||
@@ -1415,6 +1427,8 @@ int sol_attn3d_forward_linear(sol_attn3d_plan_t p, const void* q, const void* k,
   lp.n_seqs = p->n_seqs;
   lp.heads = p->heads;
   lp.seg_tiles = p->lin_seg_tiles;
+  lp.n_cut = p->lin_cut;
+  lp.cut_pieces = (int)p->lin_cut_pieces;
   lp.key_mask = key_mask;
   lp.log_decay = log_decay;
   lp.scale = scale;

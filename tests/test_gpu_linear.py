@@ -250,3 +250,14 @@ def test_refusals():
     with pytest.raises(B.SolAttn3dError):
         B.sol_attn3d_forward_linear(attn.plan, q, k, v, v, None, d, 1.0, None, None, ws)
     attn.close()
+
+
+@pytest.mark.parametrize("seqs, heads, D", [
+    ([(5, 2, 4, 4)] * 700 + [(128, 8, 12, 12)], 3, 64),        # one long sequence that is cut, many short ones behind it
+    ([(1, 0, 1, 1)] * 1500, 1, 128),                           # single tokens
+    ([(0, 1, 1, 300)] * 3 + [(64, 9, 10, 12)] * 2, 2, 128),
+])
+def test_many_sequences(seqs, heads, D):
+    case = make(seqs, heads, D, 130)
+    out, dst = run(case, 0.5)
+    check(case, out, dst, 0.5)
