@@ -71,7 +71,7 @@ struct AttnParams {
   unsigned int* status;     // 0 = fine; written once on a wait time-out
   unsigned int* counters;   // [0]: (warp, key tile) events in which the softmax moved its reference maximum
   unsigned long long wait_limit_ns;
-  unsigned int fault_inject;  // test hooks: 1 = work item 0 never publishes S of query tile 1 (exercises the bounded
+  unsigned int fault_inject;  // test hooks: 1 = work item 0 never publishes S of query tile (or map) 1 (exercises the bounded
                               // waits); 2 = work item 0 fails a device-side check on purpose (debug build)
   unsigned int v_lbo, v_sbo;  // byte offsets of the V (MN-major) shared-memory descriptor
   // differential attention only (keybits == nullptr there: every token of a sequence is a valid key)

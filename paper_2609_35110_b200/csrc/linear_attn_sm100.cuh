@@ -70,6 +70,7 @@ struct LinearParams {
   long long o_tok_stride, o_head_stride;
   unsigned int* status;
   unsigned long long wait_limit_ns;
+  unsigned int fault_inject;  // test hook: 1 = CTA 0 never publishes its first K'^T V (exercises the bounded waits)
 };
 
 // Bits i and i + 1 of a word -> mask of a pair of 16-bit values (without a branch).
@@ -682,7 +683,7 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
 #pragma unroll 1
       for (int k = 0; k < 16; ++k)                                         // hi, then lo
         mma_ts_elect<false>(tmem_base + to, tmem_base + from + k * 8, v_lo + st * kStep + (k & 7) * (2048 >> 4), hi_desc, idesc_d, k);
-      tc_commit_elect(bar_t_full(kt));
+      if (!(p.fault_inject == 1u && blockIdx.x == 0 && kt == 0)) tc_commit_elect(bar_t_full(kt));
       if (!kPairs || kStateOnly) tc_commit_elect(bar_k_empty(st));         // (pairs: the second head's scores need K still)
     };
     if constexpr (kStateOnly) {

@@ -1441,6 +1441,7 @@ int sol_attn3d_forward_linear(sol_attn3d_plan_t p, const void* q, const void* k,
   lp.o_head_stride = p->so.head;
   lp.status = reinterpret_cast<unsigned int*>(p->ws + p->off_status);
   lp.wait_limit_ns = p->wait_limit_ns;
+  lp.fault_inject = p->fault_inject;
   p->launches = 0;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const cudaError_t e = p->head_dim == 128 ? launch_linear<false>(p, tm_q, tm_k, tm_v, tm_o, lp, st)
