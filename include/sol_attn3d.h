@@ -441,7 +441,7 @@ typedef struct {
   int64_t k_strides[3];
   int64_t v_strides[3];
   int64_t n_slots;
-  int64_t capacity;             /* tokens per slot */
+  int64_t capacity;             /* tokens per slot, below 2^31 */
   const uint8_t* key_mask;
   int64_t mask_slot_stride;
 } sol_attn3d_kv_cache;

@@ -1134,7 +1134,7 @@ int take_diff_weights(const sol_attn3d_diff_weights* w, int head_dim, sol::DiffW
     out->vec[i] = vec[i];
   }
   if (w->lambda_pair_stride != 0 && w->lambda_pair_stride < head_dim) return SOL_ATTN3D_ERR_INVALID_ARG;
-  if (!std::isfinite(w->lambda_init) || !(w->eps >= 0.f) || !aligned16(w->gain)) return SOL_ATTN3D_ERR_INVALID_ARG;
+  if (!std::isfinite(w->lambda_init) || !std::isfinite(w->eps) || w->eps < 0.f || !aligned16(w->gain)) return SOL_ATTN3D_ERR_INVALID_ARG;
   out->pair_stride = w->lambda_pair_stride;
   out->lambda_init = w->lambda_init;
   out->eps = w->eps;
@@ -1251,6 +1251,7 @@ int diff_step_splits(int batch, int pairs, long long capacity) {
 }
 bool diff_step_sizes_ok(int batch, int heads, int head_dim, long long capacity) {
   return batch >= 0 && heads >= 2 && heads % 2 == 0 && heads <= 65534 && head_dim == 64 && capacity >= 0 &&
+         capacity <= 0x7fffffffll &&                      // lengths are 32-bit
          (long long)batch * (heads / 2) * diff_step_splits(std::max(batch, 1), heads / 2, capacity) < (1ll << 31);
 }
 }  // namespace

@@ -65,6 +65,21 @@ def test_differential_workspace_leaves_the_builtin_scratch_limit_alone():
     assert total > 32 * 2 ** 20
 
 
+def test_infinite_eps_and_capacities_beyond_32_bits_are_refused():
+    lib = B._lib()
+    p = B.sol_attn3d_plan(1, 4, 64, 4, 8, 8, 0, (16, 24, 24))
+    w = _weights(eps=float("inf"))
+    assert lib.sol_attn3d_forward_diff(p, 16, 32, 48, 64, None, None, ctypes.byref(w), None) == B.ERR_INVALID_ARG
+    B.sol_attn3d_destroy(p)
+    w = _weights()
+    for capacity in (2 ** 31, 2 ** 40, 2 ** 62):
+        c = B._KvCache(ctypes.sizeof(B._KvCache), 32, 48, (0, 0, 0), (0, 0, 0), 3, capacity, None, 0)
+        assert lib.sol_attn3d_diff_step(16, _s2(), ctypes.byref(c), 4, None, 64, _s2(), 3, 4, 64, ctypes.byref(w), None, 0,
+                                        None) == B.ERR_UNSUPPORTED_SHAPE
+        assert B.sol_attn3d_diff_step_workspace_bytes(3, 4, 64, capacity) == 0
+    assert B.sol_attn3d_diff_step_workspace_bytes(3, 4, 64, 2 ** 31 - 1) > 0
+
+
 def _s2(a=0, b=0):
     return (ctypes.c_int64 * 2)(a, b)
 
