@@ -582,10 +582,20 @@ def sol_attn3d_diff_step_workspace_bytes(batch: int, heads: int, head_dim: int, 
     return int(_lib().sol_attn3d_diff_step_workspace_bytes(batch, heads, head_dim, capacity))
 
 
+def _row_strides(t: torch.Tensor, head_dim: int):
+    """_strides_of for calls that take 0 as "dense": an expanded axis is refused."""
+    st = _strides_of(t, head_dim)
+    if st[0] == 0 or st[1] == 0:
+        raise ValueError("expanded tensors (stride 0) are not supported")
+    return st
+
+
 def _cache_strides(t: torch.Tensor, shape):
     st = t.stride()
     if t.shape != shape or st[3] != 1:
         raise ValueError("caches: [slots, capacity, heads, head_dim] of one shape with contiguous head_dim")
+    if 0 in st and any(s == 0 and n > 1 for s, n in zip(st, shape)):
+        raise ValueError("expanded tensors (stride 0) are not supported")
     # the stride torch reports for an axis of extent 0 or 1 is arbitrary: 0 asks for the dense value there
     return _I64x3(st[0] if shape[0] > 1 else 0, st[1] if shape[1] > 1 else 0, st[2] if shape[2] > 1 else 0)
 
@@ -611,8 +621,8 @@ def sol_attn3d_diff_step(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.
     cache = _KvCache(_KV_CACHE_SIZE, k_cache.data_ptr(), v_cache.data_ptr(), _cache_strides(k_cache, shape),
                      _cache_strides(v_cache, shape), shape[0], shape[1], _ptr(key_mask), 0)
     nbytes = 0 if workspace is None else workspace.nbytes
-    _check(_lib().sol_attn3d_diff_step(_ptr(q), _strides_of(q, head_dim), ctypes.byref(cache), _ptr(lens), _ptr(slots), _ptr(out),
-                                       _strides_of(out, head_dim), batch, heads, head_dim, ctypes.byref(weights.struct),
+    _check(_lib().sol_attn3d_diff_step(_ptr(q), _row_strides(q, head_dim), ctypes.byref(cache), _ptr(lens), _ptr(slots), _ptr(out),
+                                       _row_strides(out, head_dim), batch, heads, head_dim, ctypes.byref(weights.struct),
                                        _ptr(workspace), nbytes, _stream(stream)), "sol_attn3d_diff_step")
 
 
@@ -657,8 +667,8 @@ def sol_attn3d_linear_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, ou
     _check_decay(log_decay, heads)
     _check_index(slots, batch, "slots")
     _check_on_device(q, k, v, out, log_decay, state_in, state_out, slots)
-    _check(_lib().sol_attn3d_linear_step(_ptr(q), _ptr(k), _ptr(v), _ptr(out), _strides_of(q, head_dim), _strides_of(k, head_dim),
-                                         _strides_of(v, head_dim), _strides_of(out, head_dim), batch, heads, head_dim,
+    _check(_lib().sol_attn3d_linear_step(_ptr(q), _ptr(k), _ptr(v), _ptr(out), _row_strides(q, head_dim), _row_strides(k, head_dim),
+                                         _row_strides(v, head_dim), _row_strides(out, head_dim), batch, heads, head_dim,
                                          _ptr(log_decay), scale, _ptr(state_in), _ptr(state_out),
                                          state_in.shape[0], _ptr(slots), _stream(stream)), "sol_attn3d_linear_step")
 

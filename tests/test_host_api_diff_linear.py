@@ -144,3 +144,18 @@ def test_forward_linear_refusals_and_scratch_size():
     n = B.sol_attn3d_linear_workspace_bytes(p)
     assert n % (128 * 128 * 4) == 0 and n // (128 * 128 * 4) > 4
     B.sol_attn3d_destroy(p)
+
+
+def test_expanded_tensors_are_refused():
+    """0 stands for the dense stride at the C entry, so an expanded axis (torch stride 0) must not get there."""
+    dense = torch.zeros(3, 4, 64, dtype=torch.bfloat16)
+    assert list(B._row_strides(dense, 64)) == [256, 64]
+    assert list(B._row_strides(dense[:1].expand(1, 4, 64), 64)) == [256, 64]      # an axis of one: any stride will do
+    for bad in (dense[:1].expand(3, 4, 64), dense[:, :1].expand(3, 4, 64)):
+        with pytest.raises(ValueError):
+            B._row_strides(bad, 64)
+    cache = torch.zeros(2, 5, 4, 64, dtype=torch.bfloat16)
+    assert list(B._cache_strides(cache, cache.shape)) == [1280, 256, 64]
+    for bad in (cache[:1].expand(2, 5, 4, 64), cache[:, :1].expand(2, 5, 4, 64), cache[:, :, :1].expand(2, 5, 4, 64)):
+        with pytest.raises(ValueError):
+            B._cache_strides(bad, cache.shape)
