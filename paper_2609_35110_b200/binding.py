@@ -245,6 +245,12 @@ def sol_attn3d_cu_seqlens(plan) -> list:
     return [int(p[i]) for i in range(n.value + 1)]
 
 
+def _n_seqs(plan) -> int:
+    n = ctypes.c_int()
+    _check(_lib().sol_attn3d_cu_seqlens(plan, ctypes.byref(ctypes.POINTER(ctypes.c_int64)()), ctypes.byref(n)), "sol_attn3d_cu_seqlens")
+    return n.value
+
+
 def sol_attn3d_workspace_bytes(plan) -> int:
     return int(_lib().sol_attn3d_workspace_bytes(plan))
 
@@ -644,6 +650,8 @@ def sol_attn3d_forward_linear(plan, q, k, v, out, key_mask, log_decay: torch.Ten
         if t is not None and (not t.is_cuda or t.dtype != torch.float32 or not t.is_contiguous() or t.dim() != 4 or
                               tuple(t.shape[1:]) != (heads, head_dim, head_dim)):
             raise ValueError("states must be contiguous CUDA float32 tensors [sequences, heads, D, D]")
+        if t is not None and t.shape[0] != _n_seqs(plan):
+            raise ValueError("states: one per sequence of the plan")
     _check_decay(log_decay, heads)
     _check_on_device(q, k, v, out, key_mask, log_decay, state_in, state_out, workspace)
     nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()

@@ -261,3 +261,14 @@ def test_many_sequences(seqs, heads, D):
     case = make(seqs, heads, D, 130)
     out, dst = run(case, 0.5)
     check(case, out, dst, 0.5)
+
+
+def test_states_of_another_number_of_sequences_are_refused():
+    from paper_2609_35110_b200 import binding as B
+    attn, (q, k, v), ld, state, ws = make([(5, 0, 1, 1), (9, 0, 1, 1)], 2, 64, 131)
+    out = torch.empty_like(q)
+    for a, b in ((state[:1], None), (None, state[:1]), (state, torch.cat([state, state]))):
+        a, b = (None if x is None else x.cuda() for x in (a, b))
+        with pytest.raises(ValueError):
+            B.sol_attn3d_forward_linear(attn.plan, q, k, v, out, None, ld.cuda(), 1.0, a, b, ws)
+    attn.close()
