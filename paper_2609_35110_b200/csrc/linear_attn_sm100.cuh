@@ -572,7 +572,8 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       // copy), so that the main launch may write state_out to the same memory at any time.
       float* copy = p.initial + (long long)(si * units + unit) * (128 * D);
       if (kStateOnly || n_seg == 1) {
-        if (has_state) read_state(p.state_in);
+        // a decay of 0 forgets whatever the state holds, infinities and NaN included: 0 * S would not
+        if (has_state && weight(1) != 0.f) read_state(p.state_in);
         asm volatile("bar.sync 1, 256;" ::: "memory");                     // the others' staging space is theirs until here
         if (kStateOnly) leave_piece(copy);
       } else {

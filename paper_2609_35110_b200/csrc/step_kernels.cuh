@@ -317,6 +317,10 @@ __global__ void __launch_bounds__(128) linear_step_kernel(const LinearStepArgs a
     if (__syncthreads_or(earlier)) return;
   }
   const float g = expf(fminf(a.log_decay[head], 0.f));
+  if (g == 0.f) {                                        // forgets whatever the state holds: 0 * infinity would be NaN
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) S[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+  }
   while (true) {
     if (tid < D) {
       s_q[tid] = __bfloat162float(a.x[0][(long long)b * a.row[0] + (long long)head * a.head[0] + tid]);

@@ -272,3 +272,25 @@ def test_states_of_another_number_of_sequences_are_refused():
         with pytest.raises(ValueError):
             B.sol_attn3d_forward_linear(attn.plan, q, k, v, out, None, ld.cuda(), 1.0, a, b, ws)
     attn.close()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("seqs", [[(5, 0, 1, 1)], [(256, 5, 30, 20)]])         # whole, and cut into pieces
+def test_a_decay_of_zero_forgets_a_state_that_holds_anything(seqs, D):
+    from paper_2609_35110_b200 import binding as B
+    decay = torch.tensor([-math.inf, -0.02])
+    case = make(seqs, 2, D, 132, decay=decay)
+    out, dst = run(case)
+    check(case, out, dst)
+    attn, qkv, ld, state, ws = case
+    state[:, 0] = torch.tensor([math.nan, math.inf]).repeat(D // 2)
+    out2, dst2 = run(case)
+    assert torch.equal(out, out2) and torch.equal(dst, dst2)
+    # one more token
+    q, k, v = (x[:1].contiguous() for x in qkv)
+    a, b = torch.empty_like(q), torch.empty_like(q)
+    s1, s2 = state.cuda(), torch.nan_to_num(state, posinf=0.0).cuda()
+    B.sol_attn3d_linear_step(q, k, v, a, ld.cuda(), 1.0, s1, s1)
+    B.sol_attn3d_linear_step(q, k, v, b, ld.cuda(), 1.0, s2, s2)
+    assert torch.equal(a, b) and torch.equal(s1, s2) and torch.isfinite(s1).all()
+    attn.close()
