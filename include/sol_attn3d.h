@@ -589,7 +589,7 @@ int sol_attn3d_debug_build(void);
  * around it).  enable != 0 creates four CUDA events owned by the plan; every later forward records
  * them on its stream around its three steps.  sol_attn3d_last_forward_ms blocks on the last event
  * (cudaEventSynchronize) and writes ms[0..2] = {key-validity bits, rotary prologue, attention kernel}
- * of the most recent forward (0 for a step that was skipped).  Returns INVALID_ARG if profiling is
+ * of the most recent forward (0, or next to it, for a step that was skipped; sol_attn3d_forward_linear has the third only).  Returns INVALID_ARG if profiling is
  * off or no forward ran.  enable == 0 destroys the events.
  */
 int sol_attn3d_set_profiling(sol_attn3d_plan_t plan, int enable);
@@ -599,7 +599,8 @@ int sol_attn3d_last_forward_ms(sol_attn3d_plan_t plan, float ms[3]);
  * Number of kernels the most recent forward-type call on this plan enqueued (any sol_attn3d_forward* entry point,
  * sol_attn3d_rope_qk, sol_attn3d_qknorm_rope), counted as they were launched: the dense forward launches 2 (rotary
  * prologue, attention) plus 1 when the key-validity bits are rebuilt; the block-sparse forward adds 3 per sequence,
- * the rectangular one 1, and sol_attn3d_forward_host launches one such set per head group.  Host-side counter, no
+ * the rectangular one 1, and sol_attn3d_forward_host launches one such set per head group.  The differential forward
+ * launches 2, plus 1 with a key mask and 1 with a query mask; the linear one 1, or 2 when sequences are cut.  Host-side counter, no
  * device access.  For launch accounting in benchmarks (Section 3.2 counts launches around "SDPA").
  */
 int sol_attn3d_last_launch_count(sol_attn3d_plan_t plan);

@@ -1445,9 +1445,21 @@ int sol_attn3d_forward_linear(sol_attn3d_plan_t p, const void* q, const void* k,
   lp.fault_inject = p->fault_inject;
   p->launches = 0;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const cudaError_t e = p->head_dim == 128 ? launch_linear<false>(p, tm_q, tm_k, tm_v, tm_o, lp, st)
-                                            : launch_linear<true>(p, tm_q, tm_k, tm_v, tm_o, lp, st);
-  return e == cudaSuccess ? SOL_ATTN3D_OK : fail_cuda(p, e);
+  cudaError_t e;
+  if (p->prof) {                                           // no bits and no rotary prologue: only the last interval counts
+    p->prof_valid = false;
+    p->prof_bits = false;
+    for (int i = 0; i < 3; ++i)
+      if ((e = cudaEventRecord(p->ev[i], st)) != cudaSuccess) return fail_cuda(p, e);
+  }
+  e = p->head_dim == 128 ? launch_linear<false>(p, tm_q, tm_k, tm_v, tm_o, lp, st)
+                         : launch_linear<true>(p, tm_q, tm_k, tm_v, tm_o, lp, st);
+  if (e != cudaSuccess) return fail_cuda(p, e);
+  if (p->prof) {
+    if ((e = cudaEventRecord(p->ev[3], st)) != cudaSuccess) return fail_cuda(p, e);
+    p->prof_valid = true;
+  }
+  return SOL_ATTN3D_OK;
 }
 
 int sol_attn3d_set_profiling(sol_attn3d_plan_t p, int enable) {

@@ -294,3 +294,21 @@ def test_a_decay_of_zero_forgets_a_state_that_holds_anything(seqs, D):
     B.sol_attn3d_linear_step(q, k, v, b, ld.cuda(), 1.0, s2, s2)
     assert torch.equal(a, b) and torch.equal(s1, s2) and torch.isfinite(s1).all()
     attn.close()
+
+
+def test_profiling_and_launch_count():
+    """Per-kernel times are those of the most recent call, the linear one included."""
+    from paper_2609_35110_b200 import binding as B
+    for seqs, launches in (([(5, 0, 1, 1)], 1), ([(256, 5, 30, 20)], 2)):
+        case = make(seqs, 2, 64, 133)
+        attn, (q, k, v) = case[:2]
+        ref, _ = run(case)
+        B.sol_attn3d_set_profiling(attn.plan, True)
+        with pytest.raises(B.SolAttn3dError):
+            B.sol_attn3d_last_forward_ms(attn.plan)
+        out, _ = run(case)
+        assert B.sol_attn3d_last_launch_count(attn.plan) == launches
+        ms = B.sol_attn3d_last_forward_ms(attn.plan)
+        assert ms[0] == 0 and 0 <= ms[1] < ms[2]
+        assert torch.equal(out, ref)
+        attn.close()
