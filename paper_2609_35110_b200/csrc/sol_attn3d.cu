@@ -1217,7 +1217,7 @@ int sol_attn3d_forward_diff(sol_attn3d_plan_t p, const void* q, const void* k, c
   ap.fault_inject = p->fault_inject;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)p->total_work, 1, 1);       // total_work = 256-row blocks x heads = 2 CTAs x blocks x pairs
-  cfg.blockDim = dim3(sol::kAttnThreads, 1, 1);
+  cfg.blockDim = dim3(sol::kDiffThreads, 1, 1);
   cfg.dynamicSmemBytes = sol::AttnSmem<128, 2, true>::kDynBytes;
   cfg.stream = st;
   cudaLaunchAttribute attr{};
