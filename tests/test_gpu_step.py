@@ -1,4 +1,5 @@
 """Single-token forms: differential attention of one query over a cache, recurrent step of the linear attention."""
+import gc
 import math
 
 import pytest
@@ -9,6 +10,15 @@ from oracle import diff_linear_oracle as dlo
 pytestmark = pytest.mark.gpu
 
 HALF_STEP = torch.finfo(torch.bfloat16).eps / 2
+
+
+@pytest.fixture(scope="module", autouse=True)
+def release_cached_memory():
+    """The long caches here leave gigabytes in torch's allocator, which later tests that watch the free memory would carve up."""
+    yield
+    gc.collect()
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
 
 
 def diff_case(lens, heads, capacity, seed, gain=True, mask=False, n_slots=None, strided=False):
