@@ -610,7 +610,7 @@ int sol_attn3d_last_launch_count(sol_attn3d_plan_t plan);
  * not describe it): the attention kernel exponentiates each 128-key tile against a reference maximum per query
  * row and moves that reference only when a tile's row maximum exceeds it by more than 2^8 (then the partial
  * output and row sum are rescaled).  *count receives how often that happened, in (warp of 32 query rows, key
- * tile) events, since the workspace was bound (sol_attn3d_set_workspace resets it).  Synchronous 4-byte copy;
+ * tile) events (the differential attention: 16 rows, 64 keys), since the workspace was bound (sol_attn3d_set_workspace resets it).  Synchronous 4-byte copy;
  * call after synchronising the stream.  Tests use it to prove that inputs built to move the maximum did so.
  */
 int sol_attn3d_softmax_rescale_count(sol_attn3d_plan_t plan, unsigned long long* count);

@@ -588,6 +588,9 @@ def sol_attn3d_diff_step_workspace_bytes(batch: int, heads: int, head_dim: int, 
     return int(_lib().sol_attn3d_diff_step_workspace_bytes(batch, heads, head_dim, capacity))
 
 
+_DENSE2, _DENSE3 = _I64x2(0, 0), _I64x3(0, 0, 0)         # strides of a contiguous tensor, for calls that take 0 as "dense"
+
+
 def _row_strides(t: torch.Tensor, head_dim: int):
     """_strides_of for calls that take 0 as "dense": an expanded axis is refused."""
     st = _strides_of(t, head_dim)
@@ -614,22 +617,23 @@ def sol_attn3d_diff_step(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.
     for t in (q, k_cache, v_cache, out):
         if not t.is_cuda or t.dtype != torch.bfloat16:
             raise ValueError("q, caches and out must be CUDA bf16 tensors")
-    if out.shape != q.shape or k_cache.dim() != 4 or k_cache.shape[2:] != q.shape[1:]:
+    shape = k_cache.shape
+    if out.shape != q.shape or len(shape) != 4 or shape[2:] != q.shape[1:] or v_cache.shape != shape:
         raise ValueError("q, out: [batch, heads, 64]; caches: [slots, capacity, heads, 64]")
     _check_index(lens, batch, "lens")
     _check_index(slots, batch, "slots")
-    shape = k_cache.shape
     if key_mask is not None and (not key_mask.is_cuda or key_mask.dtype != torch.uint8 or not key_mask.is_contiguous() or
                                  key_mask.shape != shape[:2]):
         raise ValueError("key_mask must be a contiguous CUDA uint8 tensor [slots, capacity]")
     _check_pairs(weights, heads)
     _check_on_device(q, k_cache, v_cache, lens, out, workspace, key_mask, slots, *weights.tensors)
-    cache = _KvCache(_KV_CACHE_SIZE, k_cache.data_ptr(), v_cache.data_ptr(), _cache_strides(k_cache, shape),
-                     _cache_strides(v_cache, shape), shape[0], shape[1], _ptr(key_mask), 0)
+    cache = _KvCache(_KV_CACHE_SIZE, k_cache.data_ptr(), v_cache.data_ptr(),
+                     _DENSE3 if k_cache.is_contiguous() else _cache_strides(k_cache, shape),
+                     _DENSE3 if v_cache.is_contiguous() else _cache_strides(v_cache, shape), shape[0], shape[1], _ptr(key_mask), 0)
     nbytes = 0 if workspace is None else workspace.nbytes
-    _check(_lib().sol_attn3d_diff_step(_ptr(q), _row_strides(q, head_dim), ctypes.byref(cache), _ptr(lens), _ptr(slots), _ptr(out),
-                                       _row_strides(out, head_dim), batch, heads, head_dim, ctypes.byref(weights.struct),
-                                       _ptr(workspace), nbytes, _stream(stream)), "sol_attn3d_diff_step")
+    _check(_lib().sol_attn3d_diff_step(_ptr(q), _DENSE2 if q.is_contiguous() else _row_strides(q, head_dim), ctypes.byref(cache), _ptr(lens), _ptr(slots), _ptr(out),
+                                       _DENSE2 if out.is_contiguous() else _row_strides(out, head_dim), batch, heads, head_dim,
+                                       ctypes.byref(weights.struct), _ptr(workspace), nbytes, _stream(stream)), "sol_attn3d_diff_step")
 
 
 def sol_attn3d_linear_workspace_bytes(plan) -> int:
@@ -675,10 +679,10 @@ def sol_attn3d_linear_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, ou
     _check_decay(log_decay, heads)
     _check_index(slots, batch, "slots")
     _check_on_device(q, k, v, out, log_decay, state_in, state_out, slots)
-    _check(_lib().sol_attn3d_linear_step(_ptr(q), _ptr(k), _ptr(v), _ptr(out), _row_strides(q, head_dim), _row_strides(k, head_dim),
-                                         _row_strides(v, head_dim), _row_strides(out, head_dim), batch, heads, head_dim,
-                                         _ptr(log_decay), scale, _ptr(state_in), _ptr(state_out),
-                                         state_in.shape[0], _ptr(slots), _stream(stream)), "sol_attn3d_linear_step")
+    st = [_DENSE2 if t.is_contiguous() else _row_strides(t, head_dim) for t in (q, k, v, out)]
+    _check(_lib().sol_attn3d_linear_step(_ptr(q), _ptr(k), _ptr(v), _ptr(out), *st, batch, heads, head_dim, _ptr(log_decay), scale,
+                                         _ptr(state_in), _ptr(state_out), want[0], _ptr(slots), _stream(stream)),
+           "sol_attn3d_linear_step")
 
 
 def _check_decay(log_decay: torch.Tensor, heads: int) -> None:
