@@ -9,8 +9,8 @@
 #include <cstdlib>
 #include <cstring>
 #include <functional>
+#include <mutex>
 #include <new>
-#include <queue>
 #include <vector>
 
 #include "attn_fwd_sm100.cuh"
@@ -50,8 +50,9 @@ struct sol_attn3d_plan_s {
   int total_quad_work = 0;            // work items when CTA pairs serve 512-row query blocks
   int pair_mode = 1;                  // CTA pairs (cta_group::2) where they apply: head_dim 128, not block-sparse
   int total_ktiles = 0;
-  // linear attention (0 until the first call that asks): tiles per piece of a sequence; pieces, pieces with a successor,
+  // linear attention, set by the first call that asks: tiles per piece of a sequence; pieces, pieces with a successor,
   // pieces of the sequences that have more than one, those sequences
+  std::once_flag lin_once;
   int lin_seg_tiles = 0;
   long long lin_pieces = 0, lin_local = 0, lin_cut_pieces = 0;
   int lin_cut = 0;
@@ -153,8 +154,7 @@ int linear_units(sol_attn3d_plan_t p) { return p->head_dim == 64 ? (p->heads + 1
 // (3.7 us at head_dim 128); a tile of the state launch is 0.4, starting a piece 2, a predecessor's state 0.3, the extra launch 1.
 // 111,856 tokens x 40 heads x 128: 11 pieces are chosen and took 1.41 ms, its neighbours 8 and 15 1.54 and 1.52.
 // Up to some 30 ms of host time, once per plan and only for a plan that asks.
-void choose_linear_segments(sol_attn3d_plan_t p) {
-  if (p->lin_seg_tiles > 0) return;
+void choose_linear_segments_now(sol_attn3d_plan_t p) {
   constexpr int kSms = 148;
   const int units = linear_units(p);
   int longest = 1;
@@ -175,8 +175,7 @@ void choose_linear_segments(sol_attn3d_plan_t p) {
     double cost = local > 0 ? 1.0 : 0.0;
     if (pieces <= 16384) {
       for (int state = local > 0 ? 1 : 0; state >= 0; --state) {
-        std::priority_queue<double, std::vector<double>, std::greater<double>> busy;   // when each SM is free, earliest first
-        for (int i = 0; i < kSms; ++i) busy.push(0.0);
+        double busy[kSms] = {};                                       // when each SM is free: a heap, earliest first
         double end = 0.0;
         for (const SeqDev& q : p->sched) {
           const int segs = (q.n_ktiles + len - 1) / len;
@@ -184,9 +183,9 @@ void choose_linear_segments(sol_attn3d_plan_t p) {
             const int tiles = std::min(len, q.n_ktiles - s * len);
             const double t = state ? 0.4 * tiles + 2.0 : tiles + 2.0 + 0.3 * s;
             for (int u = 0; u < units; ++u) {
-              const double done = busy.top() + t;
-              busy.pop();
-              busy.push(done);
+              std::pop_heap(busy, busy + kSms, std::greater<double>());
+              const double done = busy[kSms - 1] += t;
+              std::push_heap(busy, busy + kSms, std::greater<double>());
               end = std::max(end, done);
             }
           }
@@ -204,6 +203,8 @@ void choose_linear_segments(sol_attn3d_plan_t p) {
     }
   }
 }
+
+void choose_linear_segments(sol_attn3d_plan_t p) { std::call_once(p->lin_once, choose_linear_segments_now, p); }
 
 bool stride_ok(long long s) { return s > 0 && (s * 2) % 16 == 0 && (s * 2) < (1ll << 40); }
 

@@ -159,3 +159,24 @@ def test_expanded_tensors_are_refused():
     for bad in (cache[:1].expand(2, 5, 4, 64), cache[:, :1].expand(2, 5, 4, 64), cache[:, :, :1].expand(2, 5, 4, 64)):
         with pytest.raises(ValueError):
             B._cache_strides(bad, cache.shape)
+
+
+def test_first_questions_about_one_plan_from_several_threads_agree():
+    """The cutting of sequences is planned once per plan, whoever asks first."""
+    import threading
+    lib = B._lib()
+    for _ in range(20):
+        p = B.sol_attn3d_plan_ex([(256, 5, 30, 20), (256, 16, 30, 52)], 20, 128, (32, 48, 48))
+        start, got = threading.Barrier(4), []
+
+        def ask():
+            start.wait()
+            got.append(lib.sol_attn3d_linear_workspace_bytes(p))     # ctypes releases the interpreter lock
+
+        threads = [threading.Thread(target=ask) for _ in range(4)]
+        for t in threads:
+            t.start()
+        for t in threads:
+            t.join()
+        assert len(set(got)) == 1 and got[0] == B.sol_attn3d_linear_workspace_bytes(p)
+        B.sol_attn3d_destroy(p)
