@@ -239,10 +239,14 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     const int row = wq * 32 + lane;
     const uint32_t tm = tmem_base + (static_cast<uint32_t>(wq * 32) << 16);
     {
-      // The decay of a score, scale * g^{row - j}, without a table (shared memory is what this kernel is short of).  Columns
-      // above the diagonal get whatever comes out and are masked.  All loops over columns are rolled: unrolled, the five
-      // roles' code did not fit the instruction cache, and waiting for instructions was the largest stall.
-      const float l2s[2] = {fmaxf(powers_of(0).hi, -1e4f), kPairs ? fmaxf(powers_of(1).hi, -1e4f) : 0.f};
+      // The decay of a score, scale * g^{row - j}, without a table (shared memory is what this kernel is short of).  The
+      // exponent is the integer distance times log2(g), so that it is exactly 0 on the diagonal whatever log2(g) is: walked
+      // along the columns in steps of log2(g), what was left there of cancelling numbers put a token's own weight off by up
+      // to 3 % under strong decays.  From log2(g) = -256 on only the diagonal counts (2^-256 is 0 in fp32), and -infinity * 0
+      // would be NaN: hence the limit.  Columns above the diagonal get whatever comes out and are masked.  All loops over columns
+      // are rolled: unrolled, the five roles' code did not fit the instruction cache, and waiting for instructions was the
+      // largest stall.
+      const float l2s[2] = {fmaxf(powers_of(0).hi, -256.f), kPairs ? fmaxf(powers_of(1).hi, -256.f) : 0.f};
       const float g1 = p.scale * powers_of(kPairs ? half : 0)(row + 1);    // this thread's 64 columns are one head's
       const float2 g1_2 = make_float2(g1, g1);
       const float2 scale2 = make_float2(p.scale, p.scale);
@@ -278,14 +282,16 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             tmem_wait_ld();
           }
           uint32_t pk[16];
-          float x = l2 * (float)last;                                      // log2 of g^{row - j} at the block's first column
+          float2 dist = make_float2((float)last, (float)(last - 1));       // row - j of two columns
+          const float2 l2_2 = make_float2(l2, l2), minus2 = make_float2(-2.f, -2.f);
           if (cb <= wq) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-              const float2 w = mul_f32x2(scale2, make_float2(ex2_approx(x), ex2_approx(x - l2)));
+              const float2 x = mul_f32x2(l2_2, dist);
+              const float2 w = mul_f32x2(scale2, make_float2(ex2_approx(x.x), ex2_approx(x.y)));
               const float2 y = mul_f32x2(make_float2(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1])), w);
               pk[e] = pack_bf16x2(y.x, y.y);
-              x -= 2.f * l2;
+              dist = add_f32x2(dist, minus2);
             }
             if (cb == wq || mixed) {
 #pragma unroll
