@@ -66,9 +66,11 @@ constexpr int kStepPartial = 4 + 256;    // m1, m2, l1, l2, then 128 values per 
 // (m, l, acc) of two parts -> their union; a part without keys has m = -inf and counts for nothing
 __device__ __forceinline__ float part_weight(float m, float m_all) { return m == -CUDART_INF_F ? 0.f : exp2f(m - m_all); }
 
-// out rows of one (stream, pair) from the joined maps: thread e < 128 holds value e of both maps (already divided by l).
-__device__ __forceinline__ void diff_step_finish(const DiffStepArgs& a, int b, int pair, int e, float x, float* red) {
-  if (a.w.gain != nullptr) {
+// out rows of one (stream, pair) from the joined maps: thread e < 128 holds value e of the difference x.  A row without a
+// key (empty, the same in all threads) is zeros, with no lambda and no norm: 0 * infinity and 0 / sqrt(0) are not 0.
+__device__ __forceinline__ void diff_step_finish(const DiffStepArgs& a, int b, int pair, int e, float x, bool empty, float* red) {
+  if (empty) x = 0.f;
+  if (a.w.gain != nullptr && !empty) {
     float ss = x * x;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
@@ -215,8 +217,7 @@ __global__ void __launch_bounds__(kStepThreads, kStepResident) diff_step_kernel(
     return;
   }
   const float lam = diff_lambda(a.w, pair, e & 31);
-  const float x = ll[0] == 0.f ? 0.f : xx[0] / ll[0] - lam * (xx[1] / ll[1]);       // no key: zeros
-  diff_step_finish(a, b, pair, e, x, s_red);
+  diff_step_finish(a, b, pair, e, xx[0] / ll[0] - lam * (xx[1] / ll[1]), ll[0] == 0.f, s_red);
 }
 
 // Joins the splits of one (stream, pair): thread = one value of one map.  The weights of the splits are formed once, in
@@ -253,12 +254,12 @@ __global__ void __launch_bounds__(256) diff_step_join_kernel(const DiffStepArgs 
   const float* val = src + 4 + t * 128 + e;
 #pragma unroll 8
   for (int s = 0; s < a.n_split; ++s) x = fmaf(s_w[t][s], val[(long long)s * kStepPartial], x);
-  x = sl == 0.f ? 0.f : x / sl;                                            // no key: zeros (in both maps)
+  x /= sl;                                                                 // 0 / 0 without a key, in both maps
   if (t == 1) s_x[e] = x;
   __syncthreads();
   if (t == 1) return;
   const float lam = diff_lambda(a.w, pair, lane);
-  diff_step_finish(a, b, pair, e, x - lam * s_x[e], s_red);
+  diff_step_finish(a, b, pair, e, x - lam * s_x[e], sl == 0.f, s_red);
 }
 
 // ---------------------------------------------------------------------------------------------
