@@ -262,6 +262,7 @@ __device__ __forceinline__ uint4 tail_bits(int rem) {
 template <typename L>
 __device__ __forceinline__ void diff_epilogue(const AttnParams& p, const SeqDev& sq, int pair, int t, int h, int first_row, int lane,
                                               int wq, uint32_t tmem_lane, float lam, uint8_t* smem) {
+  const int v_exp = reinterpret_cast<const int*>(smem + L::kOffTmemPtr)[2];
   const float* xl = reinterpret_cast<const float*>(smem + L::kOffXchg);    // [map][row] row sums
   float* xs = reinterpret_cast<float*>(smem + L::kOffXchg) + 256;          // [map][half][row] sums of squares
   const int row = wq * 32 + lane;
@@ -284,13 +285,20 @@ __device__ __forceinline__ void diff_epilogue(const AttnParams& p, const SeqDev&
     xs[(2 * t + h) * 128 + row] = ss;
     softmax_warps_sync();
     ss = (xs[row] + xs[128 + row]) + (xs[256 + row] + xs[384 + row]);
-    const float f = (1.0f - p.diff.lambda_init) / sqrtf(ss * (1.0f / 128.0f) + p.diff.eps);
+    // x is held times 2^-v_exp; eps joins it in that scale.  If that leaves fp32's range upwards, eps is all that counts.
+    const float up = power_of_two(-v_exp), eps = p.diff.eps * up * up;
+    const float norm = eps < CUDART_INF_F ? sqrtf(fmaf(ss, 1.0f / 128.0f, eps)) : sqrtf(p.diff.eps) * up;
+    const float f = (1.0f - p.diff.lambda_init) / norm;
     const float4* g4 = reinterpret_cast<const float4*>(p.diff.gain + t * 64 + h * 32);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const float4 g = __ldg(g4 + e);
       x[4 * e] *= f * g.x; x[4 * e + 1] *= f * g.y; x[4 * e + 2] *= f * g.z; x[4 * e + 3] *= f * g.w;
     }
+  } else {
+    const float f = power_of_two(v_exp);
+#pragma unroll
+    for (int e = 0; e < 32; ++e) x[e] *= f;
   }
   // every MMA has completed: the Q tile is the staging buffer, 2 KB per warp
   uint8_t* stage = smem + L::kOffQ + ((2 * t + h) * 4 + wq) * 32 * 64;
@@ -466,7 +474,8 @@ __device__ __forceinline__ void diff_softmax_role(const AttnParams& p, const Seq
 //
 // Types: a difference of two maps amplifies their errors, so Q~, K~, P and V are fp16 operands (11 bits instead of 8).  P is
 // held times 2^7, so that its range, from 2^15 down to 2^-24, reaches 2^-31 of the reference; four warps turn each V tile from
-// bf16 into fp16 in shared memory, in place, tiles ahead of its use (values above 65504 saturate).  Error against fp64 at
+// bf16 into fp16 in shared memory, in place, tiles ahead of its use, times a power of two that fits fp16's range to the values
+// (value_exponent).  Error against fp64 at
 // 25,216 tokens: 0.0017, the rounding of the output itself (0.0026 with bf16 P and V, 0.0040 with bf16 Q~ and K~ too).
 //
 // Per key tile and CTA that is 2 x 16384 exponentials (2048 cycles of the special-function unit) against 1536 cycles of
@@ -513,6 +522,8 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
   auto bar_v_ready = [&](int s) { return bars + 8u * (8 + 2 * L::kStages + s); };   // kDiff: V of both CTAs is fp16
   volatile uint32_t* tmem_ptr_smem = reinterpret_cast<volatile uint32_t*>(smem + L::kOffTmemPtr);
 
+  // differential attention: the next call's words are larger than this one's, whatever this CTA does below
+  if (kDiff && blockIdx.x == 0 && threadIdx.x == 0) atomicAdd(p.value_range, 1ull);
   // ---- which work item (one per CTA, or one per CTA pair)
   const int unit = (int)blockIdx.x / kCtas + p.cta_offset;
   int si = 0;
@@ -573,6 +584,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
   }
   // A fault recorded by an earlier CTA stops later ones at the door (read once; made uniform over the pair below).
   if (threadIdx.x == 0) tmem_ptr_smem[1] = *reinterpret_cast<volatile unsigned int*>(p.status);
+  if (kDiff && warp == kTma + 3 && lane == 0) tmem_ptr_smem[2] = (uint32_t)value_exponent(p.value_range, si, p.heads, head);
   if (warp == kMma) {
     if (kPair) { tmem_alloc_pair(smem_u32(const_cast<uint32_t*>(tmem_ptr_smem)), 512); tmem_relinquish_pair(); }
     else       { tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_ptr_smem)), 512); tmem_relinquish(); }
@@ -989,6 +1001,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
     // 0 * (whatever stands there) would not be 0 for infinities and NaN.
     static_assert(!kDiff || L::kStages % 2 == 0, "V tiles keep to the odd stages");
     const int w4 = warp - (kTma + 4), r = w4 * 32 + lane;
+    const uint32_t scale2 = (127u - tmem_ptr_smem[2]) * 0x00800080u;       // 2^-v_exp in bf16, twice
     bool ok = true;
     for (int i = 0; i < n_proc && ok; ++i) {
       const int n = 2 * i + 1, stage = n % L::kStages;
@@ -1005,7 +1018,10 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
       for (int ch = 0; ch < 8; ++ch) w[ch] = *reinterpret_cast<const uint4*>(at + ((ch ^ (r & 7)) << 4));
 #pragma unroll
       for (int ch = 0; ch < 8; ++ch) {
-        auto half2 = [&](uint32_t x) { return pack_f16x2_sat(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u)); };
+        auto half2 = [&](uint32_t x) {                                     // a product with a power of two: exact
+          x = mul_bf16x2(x, scale2);
+          return pack_f16x2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u));
+        };
         if (!keep) w[ch] = make_uint4(0u, 0u, 0u, 0u);
         *reinterpret_cast<uint4*>(at + ((ch ^ (r & 7)) << 4)) = make_uint4(half2(w[ch].x), half2(w[ch].y), half2(w[ch].z), half2(w[ch].w));
       }

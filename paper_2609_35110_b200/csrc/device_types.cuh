@@ -51,6 +51,18 @@ struct DiffWeightsDev {
   const float* gain;        // 128 values, or nullptr: the difference itself is the output
 };
 
+// Differential attention holds V as fp16 times a power of two of its own for every (sequence, head pair), which puts the largest
+// finite magnitude among the valid keys into [2^14, 2^15): bf16's whole range passes, and what is 2^-28 of the largest
+// value still has all its bits.  words[0] counts the calls on the workspace; words[1 + sequence * pairs + pair] is
+// (call << 16) | bits of that magnitude, written with atomicMax: a word of an earlier call is smaller than any of this one's,
+// so nothing has to be cleared between calls.  (A call whose attention kernel was refused at its launch is not counted: its words
+// then stand beside the next call's, which can only be scaled by less than it could be.)
+__device__ __forceinline__ int value_exponent(const unsigned long long* words, int seq, int pairs, int pair) {
+  const int biased = (int)(words[1 + (long long)seq * pairs + pair] & 0xffffu) >> 7;
+  return (biased < 15 ? 15 : biased) - 141;                // V is held times 2^-this; 2^126 at most
+}
+__device__ __forceinline__ float power_of_two(int e) { return __int_as_float((e + 127) << 23); }        // -126 <= e <= 127
+
 struct AttnParams {
   const SeqDev* seqs;
   int n_seqs;
@@ -76,6 +88,7 @@ struct AttnParams {
   unsigned int v_lbo, v_sbo;  // byte offsets of the V (MN-major) shared-memory descriptor
   // differential attention only (keybits == nullptr there: every token of a sequence is a valid key)
   DiffWeightsDev diff;
+  unsigned long long* value_range;
 };
 
 // Status word: low byte = what happened (first event wins), upper bits = detail.

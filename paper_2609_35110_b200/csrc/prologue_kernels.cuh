@@ -96,13 +96,34 @@ struct RopeArgs {
   RopeGeom g;
   int head_begin, head_end;   // heads [head_begin, head_end) are produced by this launch
   unsigned int* status;       // status word (written by the index checks of the debug build only)
+  const __nv_bfloat16* v;     // kF16 only: V, the keys that count, and where the range of V goes (value_exponent)
+  long long v_tok_stride, v_head_stride;
+  const uint8_t* key_mask;
+  unsigned long long* value_range;
 };
 
-// kF16: the rotated values are rounded to fp16 instead of bf16 (differential attention: the difference of two softmax maps
+// The largest finite magnitude among eight bf16 values, as bits (they compare as integers), in either half of the result.
+__device__ __forceinline__ unsigned finite_top(const uint4& w) {
+  const unsigned x[4] = {w.x & 0x7fff7fffu, w.y & 0x7fff7fffu, w.z & 0x7fff7fffu, w.w & 0x7fff7fffu};
+  unsigned top = __vmaxu2(__vmaxu2(x[0], x[1]), __vmaxu2(x[2], x[3]));
+  if ((top & 0xffffu) >= 0x7f80u || (top >> 16) >= 0x7f80u) {              // rare: infinities and NaN do not count
+    top = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if ((x[i] & 0xffffu) < 0x7f80u) top = max(top, x[i] & 0xffffu);
+      if ((x[i] >> 16) < 0x7f80u) top = max(top, x[i] >> 16);
+    }
+  }
+  return top;
+}
+
+// kF16 (differential attention): the rotated values are rounded to fp16 instead of bf16 (the difference of two softmax maps
 // amplifies the error that rounding Q~ and K~ puts into the scores, and three more bits cost nothing on the tensor cores).
-// Magnitudes above 65504 saturate.
+// Magnitudes above 65504 saturate.  The same pass reads V and finds the largest finite magnitude among the valid keys of every
+// (sequence, head pair): a running maximum per thread and head, handed in when the sequence changes.  25,216 tokens x 40 heads:
+// 116 us without V, 140 us with its 129 MB (21 us at the copy bandwidth); blocks of their own for V beside the rotation took 186.
 template <bool kNorm, bool kF16 = false>
-__global__ void __launch_bounds__(256, 3) rope_qk_kernel(const RopeArgs a) {
+__global__ void __launch_bounds__(256, kF16 ? 2 : 3) rope_qk_kernel(const RopeArgs a) {
   const int chunks = a.g.head_dim >> 3;          // 16-byte chunks per head row (8 or 16: divides the warp)
   const int heads_per_pass = blockDim.x / chunks;
   const int chunk = threadIdx.x % chunks;
@@ -121,6 +142,26 @@ __global__ void __launch_bounds__(256, 3) rope_qk_kernel(const RopeArgs a) {
     else             { axis[u] = -1; tab[u] = 0; step[u] = 0; }
   }
 
+  constexpr int kBatch = 4;
+  // kF16: what this thread has seen of V of its heads hb + hsub + b * heads_per_pass in sequence top_seq
+  unsigned top[kBatch] = {};
+  int top_seq = -1;
+  const bool one_batch = a.head_end - a.head_begin <= kBatch * heads_per_pass;
+  const unsigned long long call = kF16 ? a.value_range[0] << 16 : 0ull;
+  const bool both = (heads_per_pass & 1) == 0;   // a pair's two heads are 16 neighbouring lanes
+  auto hand_in = [&](int h0) {                   // by all threads together
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b) {
+      unsigned t = max(top[b] & 0xffffu, top[b] >> 16);
+      for (int off = chunks >> 1; off > 0; off >>= 1) t = max(t, __shfl_xor_sync(warp_lanes, t, off));
+      if (both) t = max(t, __shfl_xor_sync(warp_lanes, t, 8));
+      const int h = h0 + b * heads_per_pass;
+      if (chunk == 0 && h < a.head_end && !(both && (h & 1)))
+        atomicMax(a.value_range + 1 + (long long)top_seq * (a.g.heads >> 1) + (h >> 1), call | t);
+      top[b] = 0;
+    }
+  };
+
   for (long long tok = blockIdx.x; tok < a.total_tokens; tok += gridDim.x) {
     // which sequence, which grid position
     int s = 0;
@@ -129,9 +170,11 @@ __global__ void __launch_bounds__(256, 3) rope_qk_kernel(const RopeArgs a) {
     const int local = (int)(tok - sq.tok_start);
     SOL_DEVICE_CHECK(a.status, local >= 0 && local < sq.n_tokens, kCheckTokenSequence);
     const bool rotate = local >= sq.text_len;
-    // heads in groups of kBatch per thread and tensor: the loads of Q AND K of a group are all issued before any is
+    const bool counts = kF16 && (a.key_mask == nullptr || a.key_mask[tok] != 0);
+    if (kF16 && one_batch && s != top_seq && top_seq >= 0) hand_in(hsub);
+    top_seq = s;
+    // heads in groups of kBatch per thread and tensor: the loads of Q AND K (and V) of a group are all issued before any is
     // used, and the table lookups travel with them
-    constexpr int kBatch = 4;
     for (int hb = a.head_begin; hb < a.head_end; hb += kBatch * heads_per_pass) {    // the same trip count for every thread
       const int h0 = hb + hsub;
       uint4 v[2][kBatch];
@@ -144,6 +187,16 @@ __global__ void __launch_bounds__(256, 3) rope_qk_kernel(const RopeArgs a) {
           const int h = h0 + b * heads_per_pass;
           if (kNorm)                v[which][b] = __ldg(reinterpret_cast<const uint4*>(src + min(h, a.head_end - 1) * a.x_head_stride[which]));
           else if (h < a.head_end)  v[which][b] = __ldg(reinterpret_cast<const uint4*>(src + h * a.x_head_stride[which]));
+        }
+      }
+      uint4 value[kBatch];
+      if (kF16) {
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b) {
+          const int h = h0 + b * heads_per_pass;
+          value[b] = counts && h < a.head_end
+                         ? __ldg(reinterpret_cast<const uint4*>(a.v + tok * a.v_tok_stride + h * a.v_head_stride + chunk * 8))
+                         : make_uint4(0, 0, 0, 0);
         }
       }
       float2 cs[4];
@@ -230,8 +283,14 @@ __global__ void __launch_bounds__(256, 3) rope_qk_kernel(const RopeArgs a) {
           if (h < a.head_end) *reinterpret_cast<uint4*>(dst + (long long)h * a.g.head_dim) = make_uint4(o[0], o[1], o[2], o[3]);
         }
       }
+      if (kF16) {
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b) top[b] = __vmaxu2(top[b], finite_top(value[b]));
+        if (!one_batch) hand_in(h0);
+      }
     }
   }
+  if (kF16 && one_batch && top_seq >= 0) hand_in(hsub);
 }
 
 // ---------------------------------------------------------------------------------------------

@@ -61,7 +61,7 @@ struct sol_attn3d_plan_s {
 
   // workspace layout (byte offsets)
   size_t off_status = 0, off_tables = 0, off_seqs = 0, off_keybits = 0, off_list = 0, off_count = 0, off_pairs = 0,
-         off_dbits = 0, off_dlist = 0, off_dcount = 0,
+         off_dbits = 0, off_dlist = 0, off_dcount = 0, off_drange = 0,
          off_qrot = 0, off_krot = 0, ws_bytes = 0;
   size_t ws_dense_bytes = 0;          // what every call but the differential attention uses (a prefix of the workspace)
   int total_pairs = 0;
@@ -205,6 +205,9 @@ void choose_linear_segments_now(sol_attn3d_plan_t p) {
 }
 
 void choose_linear_segments(sol_attn3d_plan_t p) { std::call_once(p->lin_once, choose_linear_segments_now, p); }
+
+// Differential attention: how large V is, per (sequence, head pair), and the count of calls (see value_exponent).
+size_t range_bytes(sol_attn3d_plan_t p) { return (1 + (size_t)p->n_seqs * (p->heads / 2)) * sizeof(unsigned long long); }
 
 bool stride_ok(long long s) { return s > 0 && (s * 2) % 16 == 0 && (s * 2) < (1ll << 40); }
 
@@ -362,6 +365,7 @@ int build_plan(sol_attn3d_plan_t* out, const sol_attn3d_desc* d) {
       p->off_dbits = off;   off = align_up(off + (size_t)p->total_ktiles * 16);
       p->off_dlist = off;   off = align_up(off + (size_t)p->total_ktiles * sizeof(int));
       p->off_dcount = off;  off = align_up(off + (size_t)p->n_seqs * sizeof(int));
+      p->off_drange = off;  off = align_up(off + range_bytes(p));
     }
     p->ws_bytes = off;
 
@@ -403,9 +407,10 @@ int encode_map(EncodeTiledFn fn, sol_attn3d_plan_t p, CUtensorMap* tm, const voi
 
 bool aligned16(const void* x) { return (reinterpret_cast<uintptr_t>(x) & 15u) == 0; }
 
+// v (differential attention): Q~ and K~ are rounded to fp16, and the range of V is found on the way.
 int launch_rope(sol_attn3d_plan_t p, const unsigned char* ws, const void* q, const void* k, void* qr, void* kr,
                 const float* q_gain, const float* k_gain, float eps, cudaStream_t st, int head_begin = 0,
-                int head_end = 0, bool f16 = false) {
+                int head_end = 0, const void* v = nullptr, const uint8_t* key_mask = nullptr) {
   sol::RopeArgs a{};
   a.gain[0] = q_gain;
   a.gain[1] = k_gain;
@@ -436,8 +441,16 @@ int launch_rope(sol_attn3d_plan_t p, const unsigned char* ws, const void* q, con
     if (n_heads % d == 0) { hpp = d; break; }
   const int threads = chunks * hpp;
   const long long blocks = std::min<long long>(p->total_tokens, 148ll * 16);
-  if (f16)  sol::rope_qk_kernel<false, true><<<(unsigned)blocks, threads, 0, st>>>(a);
-  else if (norm) sol::rope_qk_kernel<true><<<(unsigned)blocks, threads, 0, st>>>(a);
+  if (v != nullptr) {
+    // one wave of resident blocks: every block hands in the maxima it has seen, and few words take them
+    const long long wave = std::min<long long>(p->total_tokens, (long long)p->sm_count * std::min(16, 512 / threads));
+    a.v = static_cast<const __nv_bfloat16*>(v);
+    a.v_tok_stride = p->sv.tok;
+    a.v_head_stride = p->sv.head;
+    a.key_mask = key_mask;
+    a.value_range = reinterpret_cast<unsigned long long*>(p->ws + p->off_drange);
+    sol::rope_qk_kernel<false, true><<<(unsigned)wave, threads, 0, st>>>(a);
+  } else if (norm) sol::rope_qk_kernel<true><<<(unsigned)blocks, threads, 0, st>>>(a);
   else                                        sol::rope_qk_kernel<false><<<(unsigned)blocks, threads, 0, st>>>(a);
   const cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return fail_cuda(p, e);
@@ -519,6 +532,7 @@ int sol_attn3d_set_workspace(sol_attn3d_plan_t p, void* device_ptr, size_t bytes
   p->keybits_state = 0;
   p->v_cached = nullptr;
   if ((e = cudaMemset(p->ws + p->off_status, 0, 256)) != cudaSuccess) return fail_cuda(p, e);
+  if (p->off_drange != 0 && (e = cudaMemset(p->ws + p->off_drange, 0, range_bytes(p))) != cudaSuccess) return fail_cuda(p, e);
   if ((e = cudaMemcpy(p->ws + p->off_tables, p->tables.data(), p->tables.size() * sizeof(float2),
                       cudaMemcpyHostToDevice)) != cudaSuccess)
     return fail_cuda(p, e);
@@ -1181,8 +1195,8 @@ int sol_attn3d_forward_diff(sol_attn3d_plan_t p, const void* q, const void* k, c
   }
   if (p->prof && (e = cudaEventRecord(p->ev[1], st)) != cudaSuccess) return fail_cuda(p, e);
 
-  // (2) rotary prologue over all heads, rounding to fp16
-  rc = launch_rope(p, ws, q, k, ws + p->off_qrot, ws + p->off_krot, nullptr, nullptr, 0.f, st, 0, 0, true);
+  // (2) rotary prologue over all heads, rounding to fp16, and the range of V
+  rc = launch_rope(p, ws, q, k, ws + p->off_qrot, ws + p->off_krot, nullptr, nullptr, 0.f, st, 0, 0, v, key_mask);
   if (rc != SOL_ATTN3D_OK) return rc;
   if (query_mask != nullptr) {
     uint8_t* flags = ws + p->off_pairs;
@@ -1216,6 +1230,7 @@ int sol_attn3d_forward_diff(sol_attn3d_plan_t p, const void* q, const void* k, c
   ap.v_lbo = 16384u;
   ap.v_sbo = p->v_sbo;
   ap.fault_inject = p->fault_inject;
+  ap.value_range = reinterpret_cast<unsigned long long*>(ws + p->off_drange);
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)p->total_work, 1, 1);       // total_work = 256-row blocks x heads = 2 CTAs x blocks x pairs
   cfg.blockDim = dim3(sol::kDiffThreads, 1, 1);
