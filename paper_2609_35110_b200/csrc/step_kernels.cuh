@@ -77,7 +77,18 @@ __device__ __forceinline__ void diff_step_finish(const DiffStepArgs& a, int b, i
     if ((e & 31) == 0) red[e >> 5] = ss;
     asm volatile("bar.sync 2, 128;" ::: "memory");
     ss = (red[0] + red[1]) + (red[2] + red[3]);
-    x *= (1.0f - a.w.lambda_init) / sqrtf(ss * (1.0f / 128.0f) + a.w.eps) * __ldg(a.w.gain + e);
+    if (ss > 1e-30f && ss < 1e30f) {
+      x *= (1.0f - a.w.lambda_init) / sqrtf(ss * (1.0f / 128.0f) + a.w.eps) * __ldg(a.w.gain + e);
+    } else {                                               // rare: squares beyond fp32's range (the same in all threads)
+      __shared__ double wide[4];
+      double sq = (double)x * x;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
+      if ((e & 31) == 0) wide[e >> 5] = sq;
+      asm volatile("bar.sync 2, 128;" ::: "memory");
+      sq = (wide[0] + wide[1]) + (wide[2] + wide[3]);
+      x = (float)((1.0 - (double)a.w.lambda_init) * x / sqrt(sq * (1.0 / 128.0) + (double)a.w.eps)) * __ldg(a.w.gain + e);
+    }
   }
   a.out[(long long)b * a.o_row + (long long)(2 * pair + (e >> 6)) * a.o_head + (e & 63)] = __float2bfloat16_rn(x);
 }
