@@ -398,9 +398,10 @@ int sol_attn3d_sparse_selection(sol_attn3d_plan_t plan, const void* sparse_ws, i
  *     lambda = exp(lambda_q1 . lambda_k1) - exp(lambda_q2 . lambda_k2) + lambda_init
  *     out = (1 - lambda_init) * x / sqrt(mean over 128 of x^2 + eps) * gain         (gain == NULL: out = x)
  * with q~, k~ rotated per head as in sol_attn3d_forward; the 128 values of out go to heads 2i and 2i+1.  The difference
- * amplifies the errors of the maps, so sol_attn3d_forward_diff multiplies in fp16 instead of bf16.  Magnitudes of q~ and k~
+ * amplifies the errors of the maps, so sol_attn3d_forward_diff multiplies in fp16 instead of bf16.  Finite magnitudes of q~ and k~
  * above 65504 saturate, and those below 2^-14 are held to within 2^-25.  v keeps bf16's range: it is scaled by a power of two per
  * (sequence, pair), the largest valid value deciding; values below 2^-28 of that one are held to within 2^-39 of it.
+ * Infinities and NaN at valid places give what the formula gives.
  *   lambda_*            DEVICE pointers, fp32, 4-byte aligned: 64 values each, pair i's at i * lambda_pair_stride elements
  *                       (0: one set for all pairs; otherwise at least 64).
  *   gain                DEVICE pointer, 128 fp32, 16-byte aligned, shared by the pairs, or NULL.

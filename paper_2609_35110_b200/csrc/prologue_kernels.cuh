@@ -119,9 +119,10 @@ __device__ __forceinline__ unsigned finite_top(const uint4& w) {
 
 // kF16 (differential attention): the rotated values are rounded to fp16 instead of bf16 (the difference of two softmax maps
 // amplifies the error that rounding Q~ and K~ puts into the scores, and three more bits cost nothing on the tensor cores).
-// Magnitudes above 65504 saturate.  The same pass reads V and finds the largest finite magnitude among the valid keys of every
+// Finite magnitudes above 65504 saturate; infinities and NaN stay what they are.  The same pass reads V and finds the largest finite magnitude among the valid keys of every
 // (sequence, head pair): a running maximum per thread and head, handed in when the sequence changes.  25,216 tokens x 40 heads:
-// 116 us without V, 140 us with its 129 MB (21 us at the copy bandwidth); blocks of their own for V beside the rotation took 186.
+// 116 us for the plain rotation, 140 us with the 129 MB of V (21 us at the copy bandwidth), 150 us with the infinities; blocks of their
+// own for V beside the rotation took 71 us more than the rotation.
 template <bool kNorm, bool kF16 = false>
 __global__ void __launch_bounds__(256, kF16 ? 2 : 3) rope_qk_kernel(const RopeArgs a) {
   const int chunks = a.g.head_dim >> 3;          // 16-byte chunks per head row (8 or 16: divides the warp)
@@ -275,9 +276,21 @@ __global__ void __launch_bounds__(256, kF16 ? 2 : 3) rope_qk_kernel(const RopeAr
             }
             if (kF16) {
               o[u] = pack_f16x2_sat(re, ro);
+              f[2 * u] = re;
+              f[2 * u + 1] = ro;
             } else {
               const __nv_bfloat162 r2 = __floats2bfloat162_rn(re, ro);
               o[u] = *reinterpret_cast<const uint32_t*>(&r2);
+            }
+          }
+          if (kF16) {
+            // one test for the eight values: 0 * x is 0 for the finite ones only
+            float2 z = make_float2(0.f, 0.f);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) z = fma_f32x2(make_float2(f[2 * u], f[2 * u + 1]), make_float2(0.f, 0.f), z);
+            if (!(z.x + z.y == 0.f)) {           // rare: an infinity has become the largest value, whose successor in bits it is
+#pragma unroll
+              for (int u = 0; u < 4; ++u) o[u] += (isinf(f[2 * u]) ? 1u : 0u) + (isinf(f[2 * u + 1]) ? 0x10000u : 0u);
             }
           }
           if (h < a.head_end) *reinterpret_cast<uint4*>(dst + (long long)h * a.g.head_dim) = make_uint4(o[0], o[1], o[2], o[3]);

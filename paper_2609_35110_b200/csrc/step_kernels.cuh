@@ -63,7 +63,9 @@ constexpr int kStepThreads = 256, kStepResident = 3;          // CTAs on an SM (
 constexpr int kStepKeys = 4;             // keys a half-warp has in flight
 constexpr int kStepPartial = 4 + 256;    // m1, m2, l1, l2, then 128 values per map
 
-// (m, l, acc) of two parts -> their union; a part without keys has m = -inf and counts for nothing
+// (m, l, acc) of two parts -> their union; a part without keys has m = -inf and counts for nothing.  A part whose keys all have
+// a score of -infinity has m = -kStepLowest and l = 0: beside others it counts for nothing too, on its own it gives 0 / 0.
+constexpr float kStepLowest = 3.402823466e38f;
 __device__ __forceinline__ float part_weight(float m, float m_all) { return m == -CUDART_INF_F ? 0.f : exp2f(m - m_all); }
 
 // out rows of one (stream, pair) from the joined maps: thread e < 128 holds value e of the difference x.  A row without a
@@ -120,6 +122,7 @@ __global__ void __launch_bounds__(kStepThreads, kStepResident) diff_step_kernel(
   const uint8_t* mp = a.key_mask != nullptr ? a.key_mask + slot * a.mask_slot : nullptr;
 
   float m = -CUDART_INF_F, l = 0.f;      // of this lane's own map
+  bool seen = false;                     // this half-warp has had a valid key
   float2 acc0[4] = {}, acc1[4] = {};     // this lane's value dims, map 1 and map 2
   const int hw = warp * 2 + half;        // 16 half-warps
   const __nv_bfloat16* kc = kp + (k0 + hw) * a.k_tok;                      // this half-warp's next key
@@ -138,6 +141,7 @@ __global__ void __launch_bounds__(kStepThreads, kStepResident) diff_step_kernel(
       kc += k_step;
       vc += v_step;
       if (kMasked && on[u]) on[u] = __ldg(mp + first + u * 16) != 0;
+      seen = seen || on[u];
     }
     if (kMasked) {
       // a masked key has score -inf and value 0: whatever the cache holds there, infinities and NaN included, has no effect
@@ -198,6 +202,7 @@ __global__ void __launch_bounds__(kStepThreads, kStepResident) diff_step_kernel(
     for (; base + 16 * kStepKeys <= k1; base += 16 * kStepKeys) batch(base + hw, Flag<true>{}, Flag<true>{});
     if (base < k1) batch(base + hw, Flag<false>{}, Flag<true>{});
   }
+  if (seen) m = fmaxf(m, -kStepLowest);
   if ((l16 & 7) == 0) { s_m[map][hw] = m; s_l[map][hw] = l; }
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -228,7 +233,7 @@ __global__ void __launch_bounds__(kStepThreads, kStepResident) diff_step_kernel(
     return;
   }
   const float lam = diff_lambda(a.w, pair, e & 31);
-  diff_step_finish(a, b, pair, e, xx[0] / ll[0] - lam * (xx[1] / ll[1]), ll[0] == 0.f, s_red);
+  diff_step_finish(a, b, pair, e, xx[0] / ll[0] - lam * (xx[1] / ll[1]), mm[0] == -CUDART_INF_F, s_red);
 }
 
 // Joins the splits of one (stream, pair): thread = one value of one map.  The weights of the splits are formed once, in
@@ -270,7 +275,7 @@ __global__ void __launch_bounds__(256) diff_step_join_kernel(const DiffStepArgs 
   __syncthreads();
   if (t == 1) return;
   const float lam = diff_lambda(a.w, pair, lane);
-  diff_step_finish(a, b, pair, e, x - lam * s_x[e], sl == 0.f, s_red);
+  diff_step_finish(a, b, pair, e, x - lam * s_x[e], top == -CUDART_INF_F, s_red);
 }
 
 // ---------------------------------------------------------------------------------------------
