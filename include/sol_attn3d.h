@@ -479,7 +479,7 @@ int sol_attn3d_diff_step(const void* q, const int64_t q_strides[2], const sol_at
  *                 are: run sol_attn3d_rope_qk or sol_attn3d_qknorm_rope first where the model rotates them.  K and V
  *                 values at masked positions may be anything; values of the others must be finite.
  *   log_decay     DEVICE, fp32 [heads], natural logarithm of the decay; values above 0 count as 0, -infinity forgets all
- *                 (the state may then hold anything, NaN included).
+ *                 (the state may then hold anything, NaN included), NaN makes the head NaN.
  *   state_in      DEVICE, fp32 [n_seqs][heads][head_dim][head_dim] (sequences in the caller's order), 16-byte aligned:
  *                 the state before each sequence's first token; NULL = zeros.
  *   state_out     the same shape: the state after each sequence's last token; NULL = not wanted.  May equal state_in.
@@ -503,7 +503,7 @@ int sol_attn3d_forward_linear(sol_attn3d_plan_t plan, const void* q, const void*
  *   q, k, v, out  DEVICE, bf16 [batch, heads, head_dim] (64 or 128), element strides {row, head} ({0,0} = dense), 16-byte
  *                 aligned; out must not alias an input.  q and k are taken as they are (sol_attn3d_rope_qk rotates).
  *   log_decay     DEVICE, fp32 [heads], natural logarithm of the decay; values above 0 count as 0, -infinity forgets all
- *                 (the state may then hold anything, NaN included).
+ *                 (the state may then hold anything, NaN included), NaN makes the head NaN.
  *   state_in, state_out   DEVICE, fp32 [n_slots][heads][head_dim][head_dim], 16-byte aligned; the same pointer (in place)
  *                 or disjoint memory.  States of slots that no row names are not touched.
  *   slots         DEVICE, int32 [batch], or NULL: row b uses slot b (n_slots >= batch).  A row whose slot is outside

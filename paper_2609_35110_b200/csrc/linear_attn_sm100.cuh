@@ -86,7 +86,7 @@ __device__ __forceinline__ uint32_t pair_mask(uint32_t bits, int i) {
 struct DecayPowers {
   float hi, lo;
   __device__ __forceinline__ explicit DecayPowers(float log_decay) {
-    const double l = fmin((double)log_decay, 0.0) * 1.4426950408889634;
+    const double l = (log_decay > 0.f ? 0.0 : (double)log_decay) * 1.4426950408889634;      // NaN stays NaN
     hi = (float)l;
     lo = hi < -1e4f ? 0.f : (float)(l - (double)hi);
   }
@@ -246,7 +246,11 @@ linear_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       // would be NaN: hence the limit.  Columns above the diagonal get whatever comes out and are masked.  All loops over columns
       // are rolled: unrolled, the five roles' code did not fit the instruction cache, and waiting for instructions was the
       // largest stall.
-      const float l2s[2] = {fmaxf(powers_of(0).hi, -256.f), kPairs ? fmaxf(powers_of(1).hi, -256.f) : 0.f};
+      auto log2_decay = [&](int hd) {
+        const float l2 = powers_of(hd).hi;
+        return l2 < -256.f ? -256.f : l2;                                  // (fmaxf would lose a NaN)
+      };
+      const float l2s[2] = {log2_decay(0), kPairs ? log2_decay(1) : 0.f};
       const float g1 = p.scale * powers_of(kPairs ? half : 0)(row + 1);    // this thread's 64 columns are one head's
       const float2 g1_2 = make_float2(g1, g1);
       const float2 scale2 = make_float2(p.scale, p.scale);

@@ -333,7 +333,8 @@ __global__ void __launch_bounds__(128) linear_step_kernel(const LinearStepArgs a
       }
     if (__syncthreads_or(earlier)) return;
   }
-  const float g = expf(fminf(a.log_decay[head], 0.f));
+  const float log_decay = a.log_decay[head];
+  const float g = expf(log_decay > 0.f ? 0.f : log_decay);                // NaN stays NaN
   if (g == 0.f) {                                        // forgets whatever the state holds: 0 * infinity would be NaN
 #pragma unroll
     for (int i = 0; i < kRows; ++i) S[i] = make_float4(0.f, 0.f, 0.f, 0.f);
