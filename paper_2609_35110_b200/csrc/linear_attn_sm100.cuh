@@ -20,9 +20,10 @@
 // is fp32 and carried from tile to tile, keeps about 16 bits of every factor instead of 8; the running state itself is
 // never rounded below fp32 and never accumulated in tensor memory for longer than one tile.  The split needs three bf16x2
 // instructions for two values: with the weight as w = wb + wc (two bf16), hi = rn(k wb), lo = rn(k wc + rn(k wb - hi)),
-// where k wb - hi is exact before its rounding.  That is off by at most 2^-16 of |k w| (half a step, 2^-8, of two
-// quantities that are themselves at most 2^-8 of it, and of wc), against 5 instructions for one value in fp32.  Measured: the
-// state is within 2.5e-6 of fp64 in the 2-norm (fp32 arithmetic: 2.5e-7).  A third part would need 64 more columns of tensor
+// where k wb - hi is exact before its rounding.  Every rounding is off by at most 2^-8 of its result: w - wb - wc is at most 2^-16
+// of |w|, the rounded k wb - hi (2^-8 of |k w|) off by 2^-16 of |k w|, lo itself (2^-7 of |k w|) by 2^-15: 2^-14 of |k w| at
+// worst, reached to more than a half (2.2 * 2^-16 for k = 1.0703125, w = 0.5292931), against 5 instructions for one value in fp32.
+// Typically it is far less: measured, the state is within 4e-6 of fp64 in the 2-norm (fp32 arithmetic: 2.8e-7).  A third part would need 64 more columns of tensor
 // memory, and fp16 parts (11 bits each) a V in fp16, whose range is narrower than what a caller may pass.
 //
 // Warp roles:
