@@ -100,6 +100,11 @@ int sol_attn3d_plan_ex(sol_attn3d_plan_t* plan, const sol_attn3d_desc* desc);
 int sol_attn3d_cu_seqlens(sol_attn3d_plan_t plan, const int64_t** cu, int* n_seqs);
 
 /*
+ * What the tensors of a plan look like: dims = {n_seqs, heads, head_dim, total_tokens}.  For callers that check sizes.
+ */
+int sol_attn3d_plan_dims(sol_attn3d_plan_t plan, int64_t dims[4]);
+
+/*
  * Device scratch the caller must provide (the library never allocates device memory).  Holds the
  * rotated Q and K (the rotary prologue writes them once per forward), the rotary tables, the
  * per-128-key-tile validity bits and a status word.

@@ -155,6 +155,8 @@ def _lib():
     lib.sol_attn3d_sparse_stats.restype = i32
     lib.sol_attn3d_sparse_selection.argtypes = [vp, vp, i32, i32, i32, ctypes.POINTER(i32), i32, ctypes.POINTER(i32)]
     lib.sol_attn3d_sparse_selection.restype = i32
+    lib.sol_attn3d_plan_dims.argtypes = [vp, ctypes.POINTER(i64)]
+    lib.sol_attn3d_plan_dims.restype = i32
     lib.sol_attn3d_forward_diff.argtypes = [vp, vp, vp, vp, vp, vp, vp, ctypes.POINTER(_DiffWeights), vp]
     lib.sol_attn3d_forward_diff.restype = i32
     p64 = ctypes.POINTER(i64)
@@ -245,10 +247,14 @@ def sol_attn3d_cu_seqlens(plan) -> list:
     return [int(p[i]) for i in range(n.value + 1)]
 
 
-def _n_seqs(plan) -> int:
-    n = ctypes.c_int()
-    _check(_lib().sol_attn3d_cu_seqlens(plan, ctypes.byref(ctypes.POINTER(ctypes.c_int64)()), ctypes.byref(n)), "sol_attn3d_cu_seqlens")
-    return n.value
+_I64x4 = ctypes.c_int64 * 4
+
+
+def sol_attn3d_plan_dims(plan) -> Tuple[int, int, int, int]:
+    """(sequences, heads, head_dim, total tokens)"""
+    dims = _I64x4()
+    _check(_lib().sol_attn3d_plan_dims(plan, dims), "sol_attn3d_plan_dims")
+    return tuple(dims)
 
 
 def sol_attn3d_workspace_bytes(plan) -> int:
@@ -565,10 +571,22 @@ def sol_attn3d_forward_diff(plan, q, k, v, out, key_mask, weights: sol_attn3d_di
     for m, name in ((key_mask, "key_mask"), (query_mask, "query_mask")):
         if m is not None and (not m.is_cuda or m.dtype != torch.uint8 or not m.is_contiguous()):
             raise ValueError(f"{name} must be a contiguous CUDA uint8 tensor")
-    _check_pairs(weights, q.shape[-2])
+    _, heads, head_dim, tokens = sol_attn3d_plan_dims(plan)
+    _check_sizes(tokens, heads * head_dim, (q, k, v, out), (key_mask, query_mask))
+    _check_pairs(weights, heads)
     _check_on_device(q, k, v, out, key_mask, query_mask, *weights.tensors)
     _check(_lib().sol_attn3d_forward_diff(plan, _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(key_mask), _ptr(query_mask),
                                           ctypes.byref(weights.struct), _stream(stream)), "sol_attn3d_forward_diff")
+
+
+def _check_sizes(tokens: int, row: int, tensors, masks) -> None:
+    """The kernels go by the plan, whatever the tensors' shapes say: refuse what is too small for it."""
+    for t in tensors:
+        if t.numel() < tokens * row:
+            raise ValueError(f"q, k, v, out: the plan has {tokens} tokens of {row} values")
+    for m in masks:
+        if m is not None and m.numel() < tokens:
+            raise ValueError(f"masks: the plan has {tokens} tokens")
 
 
 def _check_on_device(*tensors) -> None:
@@ -649,13 +667,12 @@ def sol_attn3d_forward_linear(plan, q, k, v, out, key_mask, log_decay: torch.Ten
             raise ValueError("q, k, v, out must be CUDA bf16 tensors")
     if key_mask is not None and (not key_mask.is_cuda or key_mask.dtype != torch.uint8 or not key_mask.is_contiguous()):
         raise ValueError("key_mask must be a contiguous CUDA uint8 tensor")
-    heads, head_dim = q.shape[-2:]
+    n_seqs, heads, head_dim, tokens = sol_attn3d_plan_dims(plan)
+    _check_sizes(tokens, heads * head_dim, (q, k, v, out), (key_mask,))
     for t in (state_in, state_out):
-        if t is not None and (not t.is_cuda or t.dtype != torch.float32 or not t.is_contiguous() or t.dim() != 4 or
-                              tuple(t.shape[1:]) != (heads, head_dim, head_dim)):
-            raise ValueError("states must be contiguous CUDA float32 tensors [sequences, heads, D, D]")
-        if t is not None and t.shape[0] != _n_seqs(plan):
-            raise ValueError("states: one per sequence of the plan")
+        if t is not None and (not t.is_cuda or t.dtype != torch.float32 or not t.is_contiguous() or
+                              t.shape != (n_seqs, heads, head_dim, head_dim)):
+            raise ValueError(f"states must be contiguous CUDA float32 tensors, {[n_seqs, heads, head_dim, head_dim]} for this plan")
     _check_decay(log_decay, heads)
     _check_on_device(q, k, v, out, key_mask, log_decay, state_in, state_out, workspace)
     nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()

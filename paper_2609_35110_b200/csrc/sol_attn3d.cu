@@ -499,6 +499,15 @@ int sol_attn3d_cu_seqlens(sol_attn3d_plan_t plan, const int64_t** cu, int* n_seq
   return SOL_ATTN3D_OK;
 }
 
+int sol_attn3d_plan_dims(sol_attn3d_plan_t plan, int64_t dims[4]) {
+  if (plan == nullptr || dims == nullptr) return SOL_ATTN3D_ERR_INVALID_ARG;
+  dims[0] = plan->n_seqs;
+  dims[1] = plan->heads;
+  dims[2] = plan->head_dim;
+  dims[3] = plan->total_tokens;
+  return SOL_ATTN3D_OK;
+}
+
 size_t sol_attn3d_workspace_bytes(sol_attn3d_plan_t plan) { return plan ? plan->ws_bytes : 0; }
 
 int sol_attn3d_set_workspace(sol_attn3d_plan_t p, void* device_ptr, size_t bytes) {
