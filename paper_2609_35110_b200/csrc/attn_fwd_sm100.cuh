@@ -285,9 +285,11 @@ __device__ __forceinline__ void diff_epilogue(const AttnParams& p, const SeqDev&
     xs[(2 * t + h) * 128 + row] = ss;
     softmax_warps_sync();
     ss = (xs[row] + xs[128 + row]) + (xs[256 + row] + xs[384 + row]);
-    // x is held times 2^-v_exp; eps joins it in that scale.  If that leaves fp32's range upwards, eps is all that counts.
+    // x is held times 2^-v_exp; eps joins it in that scale.  If that leaves fp32's range upwards, eps is all that counts; if
+    // downwards, it still keeps a row of zeros from 0 / 0.
     const float up = power_of_two(-v_exp), eps = p.diff.eps * up * up;
-    const float norm = eps < CUDART_INF_F ? sqrtf(fmaf(ss, 1.0f / 128.0f, eps)) : sqrtf(p.diff.eps) * up;
+    float norm = eps < CUDART_INF_F ? sqrtf(fmaf(ss, 1.0f / 128.0f, eps)) : sqrtf(p.diff.eps) * up;
+    if (norm == 0.f && p.diff.eps > 0.f) norm = 1.f;
     const float f = (1.0f - p.diff.lambda_init) / norm;
     const float4* g4 = reinterpret_cast<const float4*>(p.diff.gain + t * 64 + h * 32);
 #pragma unroll

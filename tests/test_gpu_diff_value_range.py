@@ -105,6 +105,18 @@ def test_replays_see_the_values_of_their_time():
     attn.close()
 
 
+@pytest.mark.parametrize("large", [1e4, 1e15, 1e30, 3e38])
+def test_zero_rows_beside_a_large_value(large):
+    """One key with a large value and a weight of exp(-512), zeros elsewhere: x is 0 and eps keeps the norm from 0 / 0."""
+    attn, (q, k, v), w, o = make([(50, 0, 1, 1)], 2, 308, gain=True, eps=1e-5)
+    q[..., 0], k[..., 0] = 64.0, 0.0
+    k[7, :, 0] = -64.0
+    v.zero_()
+    v[7] = large
+    assert bool((forward(attn, q, k, v, w) == 0).all())
+    attn.close()
+
+
 def test_a_call_that_skips_its_first_rows_counts_too():
     """Large values in a call whose query mask leaves the first blocks without work, small ones in the next."""
     from paper_2609_35110_b200 import binding as B
