@@ -153,6 +153,7 @@ __global__ void __launch_bounds__(256, kF16 ? 2 : 3) rope_qk_kernel(const RopeAr
   auto hand_in = [&](int h0) {                   // by all threads together
 #pragma unroll
     for (int b = 0; b < kBatch; ++b) {
+      if (h0 - hsub + b * heads_per_pass >= a.head_end) break;            // (the same for all threads)
       unsigned t = max(top[b] & 0xffffu, top[b] >> 16);
       for (int off = chunks >> 1; off > 0; off >>= 1) t = max(t, __shfl_xor_sync(warp_lanes, t, off));
       if (both) t = max(t, __shfl_xor_sync(warp_lanes, t, 8));
