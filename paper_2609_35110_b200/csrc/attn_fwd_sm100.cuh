@@ -14,7 +14,7 @@
 //   warp  9     tcgen05.mma issuer: the whole warp runs the loop convergently, one elected lane issues each
 //               instruction (descriptors then stay in uniform registers); owns the TMEM allocation
 //   warps 10-11 idle (complete the third warpgroup)
-// (differential attention: 0-15 softmax, 16 producer, 17 and 18 issuers, 20-23 convert V; see kDiff below)
+// (differential attention: 0-15 softmax, 16 producer, 17 and 18 issuers, 19 looks up V's exponent, 20-23 convert V; see kDiff below)
 // The two query tiles ping-pong: while the softmax of one tile runs on the ALUs, the tensor core
 // works on the other tile's QK^T / PV.
 //
@@ -42,7 +42,7 @@ namespace sol {
 #ifndef SOL_REGS_OTHER
 #define SOL_REGS_OTHER 64
 #endif
-constexpr int kDiffThreads = 768;   // 16 softmax warps, producer, an MMA issuer per map, an idle warp, 4 warps that convert V
+constexpr int kDiffThreads = 768;   // 16 softmax warps, producer, an MMA issuer per map, a warp with little to do, 4 warps that convert V
 constexpr int kAttnThreads = 384;   // 8 softmax warps + producer + MMA issuer + 2 idle warps (a full third warpgroup)
 
 __device__ __forceinline__ float row_max128(const uint32_t (&r)[128]) {
@@ -477,17 +477,18 @@ __device__ __forceinline__ void diff_softmax_role(const AttnParams& p, const Seq
 // Types: a difference of two maps amplifies their errors, so Q~, K~, P and V are fp16 operands (11 bits instead of 8).  P is
 // held times 2^7, so that its range, from 2^15 down to 2^-24, reaches 2^-31 of the reference; four warps turn each V tile from
 // bf16 into fp16 in shared memory, in place, tiles ahead of its use, times a power of two that fits fp16's range to the values
-// (value_exponent).  Error against fp64 at
-// 25,216 tokens: 0.0017, the rounding of the output itself (0.0026 with bf16 P and V, 0.0040 with bf16 Q~ and K~ too).
+// (value_exponent; the product costs 0.6 %).  Error against fp64 at 25,216 tokens: 0.0017, the rounding of the output itself
+// (0.0026 with bf16 P and V, 0.0040 with bf16 Q~ and K~ too).
 //
 // Per key tile and CTA that is 2 x 16384 exponentials (2048 cycles of the special-function unit) against 1536 cycles of
 // tensor-core work, so the exponentials bound it.  With the plain kernel's shape (a warp per 32 rows, one score buffer per
 // map, one MMA issuer) the unit was busy 58 % of the time: a map waited 1,330 cycles per tile for its scores (P seen, two
 // products, scores seen), and a warp alone on its scheduler reached 70 % of the unit's rate.  Hence 64 keys per step and two
 // score buffers per map, an issuer per map, and sixteen softmax warps of 16 rows each: a row stays within one warp, whose
-// instructions, not the tensor core's latency, are what is left.  25,216 tokens x 20 pairs: 10.8 -> 10.3 ms, 950 TFLOP/s, at
-// 1.79 GHz under the power limit.  Two threads per row with 64 columns each and the plain kernel's buffers: 11.1 ms (the
-// agreement on a row's reference is a barrier per tile); double buffers with eight warps: 11.4.
+// instructions, not the tensor core's latency, are what is left: 2,990 cycles per tile.  25,216 tokens x 20 pairs: 10.35 ms with
+// the rotary pass, 943 TFLOP/s, in a long run, where the power limit holds the clock at 1.66 GHz (9.03 ms for a launch of its own).
+// Against 10.8 ms with the plain kernel's shape, two threads per row with 64 columns each and the plain kernel's buffers took 11.1
+// (the agreement on a row's reference is a barrier per tile), double buffers with eight warps 11.4.
 template <int D, int kCtas, bool kDiff = false>
 __global__ void __launch_bounds__(kDiff ? kDiffThreads : kAttnThreads, 1)
 attn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,

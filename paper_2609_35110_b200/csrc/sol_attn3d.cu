@@ -150,9 +150,11 @@ int linear_units(sol_attn3d_plan_t p) { return p->head_dim == 64 ? (p->heads + 1
 // Linear attention: into how many pieces the sequences are cut.  Whole sequences need one launch and read K and V once;
 // pieces keep more SMs busy, but every piece with a successor has its K and V read twice (a launch for the state it adds,
 // then the main one) and a piece starts by summing its predecessors' states.  Every count up to 64 is tried by dealing its
-// pieces to the SMs as the hardware does, in order, each to the SM that is free first.  The unit is a tile of the main launch
+// pieces to the 148 SMs as the hardware does, in order, each to the SM that is free first.  The unit is a tile of the main launch
 // (3.7 us at head_dim 128); a tile of the state launch is 0.4, starting a piece 2, a predecessor's state 0.3, the extra launch 1.
-// 111,856 tokens x 40 heads x 128: 11 pieces are chosen and took 1.41 ms, its neighbours 8 and 15 1.54 and 1.52.
+// These costs were measured at head_dim 128 and are used for pairs of 64-dim heads as they are, whose tile takes longer and whose
+// states are half as large; the choice was not compared with its neighbours there.  111,856 tokens x 40 heads x 128: 11 pieces
+// are chosen; they took 1.41 ms where 8 and 15 took 1.54 and 1.52 on the same box.
 // Up to some 30 ms of host time, once per plan and only for a plan that asks.
 void choose_linear_segments_now(sol_attn3d_plan_t p) {
   constexpr int kSms = 148;
