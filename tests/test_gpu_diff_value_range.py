@@ -63,6 +63,28 @@ def test_scales_of_sequences_and_pairs_are_their_own():
     attn.close()
 
 
+@pytest.mark.parametrize("masked", [False, True])
+@pytest.mark.parametrize("heads", [2, 18, 34, 74, 102, 130])
+def test_many_sequences_and_head_counts(heads, masked):
+    """Head counts that fill the rotary pass's blocks evenly, with an odd number of heads, with heads left over and in several goes;
+    many short sequences, each (sequence, pair) with a random order of magnitude."""
+    seqs = SEQS + [(3, 1, 2, 2)] * 40
+    attn, (q, k, v), w, _ = make(seqs, heads, 309, gain=False)
+    n = attn.total_tokens
+    g = torch.Generator().manual_seed(heads)
+    mask = (torch.rand(n, generator=g) < 0.7).to(torch.uint8).cuda() if masked else None
+    out = forward(attn, q, k, v, w, mask)
+    assert bool(torch.isfinite(out).all())
+    e = torch.randint(-100, 101, (len(seqs), heads // 2), generator=g)
+    lengths = torch.tensor([b - a for a, b in zip(attn.cu_seqlens, attn.cu_seqlens[1:])])
+    f = (2.0 ** e.float()).repeat_interleave(lengths, 0).repeat_interleave(2, 1)[:, :, None].cuda()
+    scaled = (v.float() * f).bfloat16()
+    if masked:
+        scaled[mask == 0] = torch.finfo(torch.bfloat16).max
+    assert torch.equal(forward(attn, q, k, scaled, w, mask).float(), out.float() * f)
+    attn.close()
+
+
 def test_values_that_do_not_count_do_not_set_the_scale():
     attn, (q, k, v), w, _ = make(SEQS, 4, 303, gain=False)
     v *= 2.0 ** -30
