@@ -119,10 +119,11 @@ __device__ __forceinline__ unsigned finite_top(const uint4& w) {
 
 // kF16 (differential attention): the rotated values are rounded to fp16 instead of bf16 (the difference of two softmax maps
 // amplifies the error that rounding Q~ and K~ puts into the scores, and three more bits cost nothing on the tensor cores).
-// Finite magnitudes above 65504 saturate; infinities and NaN stay what they are.  The same pass reads V and finds the largest finite magnitude among the valid keys of every
-// (sequence, head pair): a running maximum per thread and head, handed in when the sequence changes.  25,216 tokens x 40 heads:
-// 116 us for the plain rotation, 140 us with the 129 MB of V (21 us at the copy bandwidth), 150 us with the infinities; blocks of their
-// own for V beside the rotation took 71 us more than the rotation.
+// Finite magnitudes above 65504 saturate; infinities and NaN stay what they are.
+// The same pass reads V and finds the largest finite magnitude among the valid keys of every (sequence, head pair): a running
+// maximum per thread and head, handed in when the sequence changes; one wave of blocks, so that few words are not beset by many.
+// 25,216 tokens x 40 heads: 116 us for the plain rotation, 140 us with the 129 MB of V (21 us at the copy bandwidth), 150 us with
+// the infinities; blocks of their own for V beside the rotation took 71 us more than the rotation.
 template <bool kNorm, bool kF16 = false>
 __global__ void __launch_bounds__(256, kF16 ? 2 : 3) rope_qk_kernel(const RopeArgs a) {
   const int chunks = a.g.head_dim >> 3;          // 16-byte chunks per head row (8 or 16: divides the warp)
