@@ -523,6 +523,178 @@ int sol_attn3d_linear_step(const void* q, const void* k, const void* v, void* ou
                            float* state_out, int64_t n_slots, const int32_t* slots, sol_attn3d_stream_t stream);
 
 /*
+ * Streaming generation: a K/V cache in pages, and the attention of new tokens over it (the cached-K/V form of Section 3.2's "SDPA";
+ * cf. "Reference KV caching mechanism").  New frames are appended chunk by chunk, or token by token, to streams whose past stays
+ * in the cache; streams branch (guidance, candidates), drop what lies outside a window, and end.
+ *
+ * A cache is [n_layers][n_pages][page_size][kv_heads][head_dim] bf16 for K and for V, DEVICE, caller-owned; strides are element
+ * strides {layer, page, token, head}, 0 = dense, byte strides multiples of 16, offsets 64-bit.  K holds rotated keys.  Token j
+ * of stream s is row j % page_size of page table[s][j / page_size], the same in every layer; lens[s] is the number of tokens.
+ *   table     DEVICE, int32 [n_streams][table_width].  Entries at or beyond the pages that a stream's length needs are not read.
+ *             An entry within them that names no page reads as a page of zeros; nothing is written through it.
+ *   lens      DEVICE, int32 [n_streams].  Values are clamped to [0, table_width * page_size].
+ *   refs      DEVICE, int32 [n_pages]: how many streams hold a page; 0 = free.  NULL is fine for the calls that only read or
+ *             write tokens (append and the attention); the others keep it.
+ *   page_size a multiple of 16, at most 4096; n_pages * page_size and table_width * page_size below 2^31.
+ * The struct is read during the call, the arrays when the kernels run.
+ */
+typedef struct {
+  uint32_t size;                /* sizeof(sol_attn3d_paged_cache) */
+  int32_t n_layers;
+  int32_t page_size;
+  int32_t kv_heads;
+  int32_t head_dim;             /* 64 or 128 */
+  void* k;
+  void* v;
+  int64_t k_strides[4];
+  int64_t v_strides[4];
+  int64_t n_pages;
+  int32_t* table;
+  int32_t* lens;
+  int32_t* refs;
+  int64_t n_streams;
+  int64_t table_width;
+} sol_attn3d_paged_cache;
+
+/* What a bookkeeping call says of each request (DEVICE, int32 [n]). */
+#define SOL_ATTN3D_CACHE_OK 0
+#define SOL_ATTN3D_CACHE_BAD_STREAM 1 /* no such stream, or named by an earlier request of the call; a negative amount */
+#define SOL_ATTN3D_CACHE_NO_ROOM 2    /* the stream's row of the table is too short */
+#define SOL_ATTN3D_CACHE_NO_PAGES 3   /* not enough free pages */
+#define SOL_ATTN3D_CACHE_NOT_EMPTY 4  /* fork: the new stream holds tokens */
+
+/*
+ * Bookkeeping of streams.  All work is on the device, in stream order: no allocation, no synchronisation; may be captured.  The
+ * result depends on the arrays alone: requests are served in their order, new pages are the free ones of the lowest index, and the
+ * requests that need pages are served until the first one for which the free pages do not suffice.  A request that is not served
+ * changes nothing and says why in status (which may be NULL).  n = 0 is a no-op; n is at most 4096.  Calls that may overlap on the
+ * GPU must not touch the same cache.
+ *
+ * reserve  lens[streams[i]] grows by amount[i] >= 0 tokens, with the pages that they need.  (Then sol_attn3d_cache_append, once per
+ *          layer, fills them.)
+ * fork     stream streams[i], which must be empty, becomes a branch of parents[i]: it shares the full pages and has a copy of the
+ *          last one if that is partly filled (the rows that hold tokens, all layers).  Parents are as they were before the call.
+ * compact  of stream streams[i] the tokens j with keep[i][j] != 0 stay, in their order (uint8 [n][keep_width], rows keep_width
+ *          apart; tokens at or beyond keep_width go).  The pages before the one with the first dropped token stay; the rest of
+ *          what stays is copied to new pages, whether or not other streams hold the old ones, which lose a holder after all
+ *          requests have been served.  If what stays is a prefix nothing is copied, unless the page in which it now ends is
+ *          another stream's, too.
+ * free     the stream's pages lose a holder, its entries of the table become -1, its length 0.
+ *   workspace  DEVICE, 256-byte aligned, at least sol_attn3d_cache_workspace_bytes(cache, n) bytes, written and read by every call.
+ *              Calls that may overlap on the GPU need one each.
+ * One kernel (reserve, free), two (fork) or three (compact).
+ * Errors: INVALID_ARG, UNSUPPORTED_SHAPE, NO_WORKSPACE, CUDA.
+ */
+size_t sol_attn3d_cache_workspace_bytes(const sol_attn3d_paged_cache* cache, int n);
+int sol_attn3d_cache_reserve(const sol_attn3d_paged_cache* cache, int n, const int32_t* streams, const int32_t* amount,
+                             int32_t* status, sol_attn3d_stream_t stream);
+int sol_attn3d_cache_fork(const sol_attn3d_paged_cache* cache, int n, const int32_t* parents, const int32_t* streams,
+                          int32_t* status, void* workspace, size_t workspace_bytes, sol_attn3d_stream_t stream);
+int sol_attn3d_cache_compact(const sol_attn3d_paged_cache* cache, int n, const int32_t* streams, const uint8_t* keep,
+                             int64_t keep_width, int32_t* status, void* workspace, size_t workspace_bytes,
+                             sol_attn3d_stream_t stream);
+int sol_attn3d_cache_free(const sol_attn3d_paged_cache* cache, int n, const int32_t* streams, int32_t* status,
+                          sol_attn3d_stream_t stream);
+/*
+ * Copies whole pages in all layers, K and V: page dst_pages[i] = page src_pages[i] (DEVICE, int32 [n]); for programs that keep the
+ * table themselves.  Pairs that name no page, or one page twice, are left out; a page that is both a source and a destination, or
+ * a destination twice, holds either content.  One kernel; n is at most 2^20.
+ */
+int sol_attn3d_cache_copy_pages(const sol_attn3d_paged_cache* cache, int n, const int32_t* src_pages, const int32_t* dst_pages,
+                                sol_attn3d_stream_t stream);
+
+/*
+ * New tokens into one layer of a cache, in one pass: per-head RMS norm of Q and K with their gains, rotation, one rounding to bf16
+ * (the paper's fusion group (2), Section 3.5), K and V written to their pages.  The plan's sequences are chunks of new tokens:
+ * row i of sequence s, of n, becomes token lens - n + i of stream streams[s] (lens has been raised by sol_attn3d_cache_reserve);
+ * rows whose token would be before the first one are not written.
+ *   q, q_out       as in sol_attn3d_qknorm_rope (the plan's q strides; dense output), or both NULL.
+ *   k, v           DEVICE, bf16 [total_tokens, kv_heads, head_dim], element strides {token, head} ({0,0} = dense).
+ *   streams        DEVICE, int32 [n_seqs], or NULL: sequence s is stream s.  A sequence whose stream is outside [0, n_streams) is
+ *                  idle: nothing of it is read or written.  Of several sequences with one stream the first one's K and V count.
+ *   pos0           DEVICE, int32 [n_seqs][3], offsets of (t, h, w) of the sequence's grid, or NULL (0).  Angles are found in fp64, so
+ *                  far positions keep their phase.  Prefix tokens are not rotated.
+ *   q_gain, k_gain DEVICE, fp32 [head_dim], 16-byte aligned, or NULL: not normalised.  eps >= 0, finite.
+ * q_out must not alias an input.  One kernel; deterministic; may be captured.  The plan's workspace must be bound.
+ * Errors: INVALID_ARG, NO_WORKSPACE, UNSUPPORTED_SHAPE, CUDA.
+ */
+int sol_attn3d_cache_append(sol_attn3d_plan_t plan, const void* q, const void* k, const void* v, const int64_t k_strides[2],
+                            const int64_t v_strides[2], void* q_out, const sol_attn3d_paged_cache* cache, int layer,
+                            const int32_t* streams, const int32_t* pos0, const float* q_gain, const float* k_gain, float eps,
+                            sol_attn3d_stream_t stream);
+
+/*
+ * Attention of new tokens over one layer of a paged cache that already holds them: row i of sequence s, of n, is token lens - n + i
+ * of stream streams[s] and attends to
+ *     all tokens of the stream                                                    (causal_block = 0), or to
+ *     the tokens below  lens - n + (i / causal_block + 1) * causal_block          (causal_block > 0: every block of new tokens,
+ *                                                                                  a frame say, sees the past and itself; 1 = causal).
+ *   q, out       DEVICE, bf16 [total_tokens, heads, head_dim], the plan's q and out strides, 16-byte aligned; q is rotated.
+ *                heads must be a multiple of the cache's kv_heads; head h reads K/V head h / (heads / kv_heads).
+ *   key_mask     DEVICE, uint8 [n_streams][mask_width] by token, rows mask_width apart, nonzero = attend; or NULL.  Tokens at or beyond
+ *                mask_width do not count.
+ *   streams      as in sol_attn3d_cache_append; rows of an idle sequence are left as they were.  Several may name one stream.
+ *   workspace    DEVICE, 256-byte aligned, at least sol_attn3d_paged_workspace_bytes(plan, cache) bytes, which may be 0 (then NULL is
+ *                fine): results of key ranges that different CTAs handle, written and read by every call.  Calls that may overlap
+ *                on the GPU need one each.
+ * Rows without a valid key are zeros.  K and V of tokens that are masked, or beyond the stream's length, may be anything
+ * (infinities, NaN); those of tokens that some row sees must be finite where a mask or causal_block hides them from another.
+ * Deterministic; may be captured; one or two kernels.  The plan's workspace must be bound; time-outs are reported by
+ * sol_attn3d_status.
+ * Errors: INVALID_ARG, NO_WORKSPACE, UNSUPPORTED_SHAPE, CUDA.
+ */
+size_t sol_attn3d_paged_workspace_bytes(sol_attn3d_plan_t plan, const sol_attn3d_paged_cache* cache);
+int sol_attn3d_forward_paged(sol_attn3d_plan_t plan, const void* q, const sol_attn3d_paged_cache* cache, int layer, void* out,
+                             const int32_t* streams, const uint8_t* key_mask, int64_t mask_width, int causal_block,
+                             void* workspace, size_t workspace_bytes, sol_attn3d_stream_t stream);
+
+/*
+ * The same for one token per row without a plan: row b of q [batch, heads, head_dim] (element strides {row, head}, {0,0} = dense)
+ * is the last token of stream streams[b] (NULL: stream b) and sees all of the stream.  No device-side wait.
+ */
+size_t sol_attn3d_paged_step_workspace_bytes(const sol_attn3d_paged_cache* cache, int batch, int heads);
+int sol_attn3d_paged_step(const void* q, const int64_t q_strides[2], const sol_attn3d_paged_cache* cache, int layer,
+                          const int32_t* streams, void* out, const int64_t out_strides[2], int batch, int heads,
+                          const uint8_t* key_mask, int64_t mask_width, void* workspace, size_t workspace_bytes,
+                          sol_attn3d_stream_t stream);
+
+/*
+ * Cross attention: the queries of a plan's sequences over the states of an encoder (the paper's DiT attends to its prompt jointly,
+ * as a prefix; this is the same step for a block that keeps the prompt apart).  Sequence s attends to rows
+ * [begins[s], begins[s] + lens[s]) of k and v, of another length than its own; sequences may share a context.
+ *   k, v        DEVICE, bf16 [total_rows, kv_heads, head_dim], element strides {row, head} (0 = dense), 16-byte aligned.
+ *   begins, lens   DEVICE, int32 [n_seqs]; clamped to [0, total_rows].
+ *   max_len     no lens value is larger (it decides how the work is split; rows beyond it are still read, but not faster).
+ *   key_mask    DEVICE, uint8 [total_rows], nonzero = attend; or NULL.
+ */
+typedef struct {
+  uint32_t size;                /* sizeof(sol_attn3d_context) */
+  int32_t kv_heads;
+  int32_t head_dim;
+  const void* k;
+  const void* v;
+  int64_t k_strides[2];
+  int64_t v_strides[2];
+  int64_t total_rows;           /* below 2^31 */
+  const int32_t* begins;
+  const int32_t* lens;
+  int64_t max_len;
+  const uint8_t* key_mask;
+} sol_attn3d_context;
+
+/*
+ * q, out, workspace, masked values, rows without a key: as for sol_attn3d_forward_paged; q is taken as it is.  The step form takes one
+ * row per context, batch of them (begins and lens [batch]).
+ */
+size_t sol_attn3d_cross_workspace_bytes(sol_attn3d_plan_t plan, const sol_attn3d_context* context);
+int sol_attn3d_forward_cross(sol_attn3d_plan_t plan, const void* q, const sol_attn3d_context* context, void* out,
+                             void* workspace, size_t workspace_bytes, sol_attn3d_stream_t stream);
+size_t sol_attn3d_cross_step_workspace_bytes(const sol_attn3d_context* context, int batch, int heads);
+int sol_attn3d_cross_step(const void* q, const int64_t q_strides[2], const sol_attn3d_context* context, void* out,
+                          const int64_t out_strides[2], int batch, int heads, void* workspace, size_t workspace_bytes,
+                          sol_attn3d_stream_t stream);
+
+/*
  * sol_attn3d_forward for callers that must not allocate device memory.  (The paper has no counterpart:
  * this is a deployment variant of the call above, not a step of the method.)
  *

@@ -70,6 +70,43 @@ class _KvCache(ctypes.Structure):
     ]
 
 
+class _PagedCache(ctypes.Structure):
+    _fields_ = [
+        ("size", ctypes.c_uint32),
+        ("n_layers", ctypes.c_int32),
+        ("page_size", ctypes.c_int32),
+        ("kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("k", ctypes.c_void_p),
+        ("v", ctypes.c_void_p),
+        ("k_strides", ctypes.c_int64 * 4),
+        ("v_strides", ctypes.c_int64 * 4),
+        ("n_pages", ctypes.c_int64),
+        ("table", ctypes.c_void_p),
+        ("lens", ctypes.c_void_p),
+        ("refs", ctypes.c_void_p),
+        ("n_streams", ctypes.c_int64),
+        ("table_width", ctypes.c_int64),
+    ]
+
+
+class _Context(ctypes.Structure):
+    _fields_ = [
+        ("size", ctypes.c_uint32),
+        ("kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("k", ctypes.c_void_p),
+        ("v", ctypes.c_void_p),
+        ("k_strides", ctypes.c_int64 * 2),
+        ("v_strides", ctypes.c_int64 * 2),
+        ("total_rows", ctypes.c_int64),
+        ("begins", ctypes.c_void_p),
+        ("lens", ctypes.c_void_p),
+        ("max_len", ctypes.c_int64),
+        ("key_mask", ctypes.c_void_p),
+    ]
+
+
 _KV_CACHE_SIZE = ctypes.sizeof(_KvCache)
 
 
@@ -85,6 +122,13 @@ ERR_DEVICE_TIMEOUT = -7
 ERR_NO_MEMORY = -8
 ERR_SCRATCH_LIMIT = -9
 ERR_DEVICE_ASSERT = -10
+
+# what the bookkeeping calls of a paged cache say of each request
+CACHE_OK = 0
+CACHE_BAD_STREAM = 1
+CACHE_NO_ROOM = 2
+CACHE_NO_PAGES = 3
+CACHE_NOT_EMPTY = 4
 
 _LIB = None
 
@@ -172,6 +216,37 @@ def _lib():
     lib.sol_attn3d_linear_step.argtypes = [vp, vp, vp, vp, p64, p64, p64, p64, i32, i32, i32, vp, ctypes.c_float, vp, vp, i64,
                                            vp, vp]
     lib.sol_attn3d_linear_step.restype = i32
+    cache, context, size = ctypes.POINTER(_PagedCache), ctypes.POINTER(_Context), ctypes.c_size_t
+    lib.sol_attn3d_cache_workspace_bytes.argtypes = [cache, i32]
+    lib.sol_attn3d_cache_workspace_bytes.restype = size
+    lib.sol_attn3d_cache_reserve.argtypes = [cache, i32, vp, vp, vp, vp]
+    lib.sol_attn3d_cache_reserve.restype = i32
+    lib.sol_attn3d_cache_fork.argtypes = [cache, i32, vp, vp, vp, vp, size, vp]
+    lib.sol_attn3d_cache_fork.restype = i32
+    lib.sol_attn3d_cache_compact.argtypes = [cache, i32, vp, vp, i64, vp, vp, size, vp]
+    lib.sol_attn3d_cache_compact.restype = i32
+    lib.sol_attn3d_cache_free.argtypes = [cache, i32, vp, vp, vp]
+    lib.sol_attn3d_cache_free.restype = i32
+    lib.sol_attn3d_cache_copy_pages.argtypes = [cache, i32, vp, vp, vp]
+    lib.sol_attn3d_cache_copy_pages.restype = i32
+    lib.sol_attn3d_cache_append.argtypes = [vp, vp, vp, vp, p64, p64, vp, cache, i32, vp, vp, vp, vp, ctypes.c_float, vp]
+    lib.sol_attn3d_cache_append.restype = i32
+    lib.sol_attn3d_paged_workspace_bytes.argtypes = [vp, cache]
+    lib.sol_attn3d_paged_workspace_bytes.restype = size
+    lib.sol_attn3d_forward_paged.argtypes = [vp, vp, cache, i32, vp, vp, vp, i64, i32, vp, size, vp]
+    lib.sol_attn3d_forward_paged.restype = i32
+    lib.sol_attn3d_paged_step_workspace_bytes.argtypes = [cache, i32, i32]
+    lib.sol_attn3d_paged_step_workspace_bytes.restype = size
+    lib.sol_attn3d_paged_step.argtypes = [vp, p64, cache, i32, vp, vp, p64, i32, i32, vp, i64, vp, size, vp]
+    lib.sol_attn3d_paged_step.restype = i32
+    lib.sol_attn3d_cross_workspace_bytes.argtypes = [vp, context]
+    lib.sol_attn3d_cross_workspace_bytes.restype = size
+    lib.sol_attn3d_forward_cross.argtypes = [vp, vp, context, vp, vp, size, vp]
+    lib.sol_attn3d_forward_cross.restype = i32
+    lib.sol_attn3d_cross_step_workspace_bytes.argtypes = [context, i32, i32]
+    lib.sol_attn3d_cross_step_workspace_bytes.restype = size
+    lib.sol_attn3d_cross_step.argtypes = [vp, p64, context, vp, p64, i32, i32, vp, size, vp]
+    lib.sol_attn3d_cross_step.restype = i32
     lib.sol_attn3d_rope_qk.argtypes = [vp, vp, vp, vp, vp, vp]
     lib.sol_attn3d_rope_qk.restype = i32
     lib.sol_attn3d_status.argtypes = [vp]
@@ -705,6 +780,256 @@ def sol_attn3d_linear_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, ou
 def _check_decay(log_decay: torch.Tensor, heads: int) -> None:
     if not log_decay.is_cuda or log_decay.dtype != torch.float32 or not log_decay.is_contiguous() or log_decay.numel() != heads:
         raise ValueError("log_decay must be a contiguous CUDA float32 tensor with one element per head")
+
+
+def _pool_strides(t: torch.Tensor, extents, n: int):
+    """Element strides of all axes but the last; 0 (the dense value) where torch's is arbitrary (extent 0 or 1)."""
+    st = t.stride()
+    if st[-1] != 1 and extents[-1] > 1:
+        raise ValueError("head_dim must be contiguous")
+    if any(s == 0 and e > 1 for s, e in zip(st, extents)):
+        raise ValueError("expanded tensors (stride 0) are not supported")
+    return (ctypes.c_int64 * n)(*(s if e > 1 else 0 for s, e in zip(st[:-1], extents)))
+
+
+class sol_attn3d_paged_cache:
+    """A K/V cache in pages: keeps the tensors alive and marshals them.
+
+    k, v: CUDA bf16 [layers, pages, page_size, kv_heads, head_dim]; table: int32 [streams, columns], lens: int32 [streams],
+    refs: int32 [pages] (streams that hold a page), or None for a cache that is only read and appended to."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, refs: Optional[torch.Tensor] = None):
+        for t in (k, v):
+            if not t.is_cuda or t.dtype != torch.bfloat16 or t.dim() != 5 or t.shape != k.shape:
+                raise ValueError("k, v must be CUDA bf16 tensors [layers, pages, page_size, kv_heads, head_dim] of one shape")
+        for t, dims, name in ((table, 2, "table"), (lens, 1, "lens"), (refs, 1, "refs")):
+            if t is not None and (not t.is_cuda or t.dtype != torch.int32 or not t.is_contiguous() or t.dim() != dims):
+                raise ValueError(f"{name} must be a contiguous CUDA int32 tensor of {dims} dimension(s)")
+        if lens.shape[0] != table.shape[0] or (refs is not None and refs.shape[0] != k.shape[1]):
+            raise ValueError("lens has one element per row of the table, refs one per page")
+        layers, pages, page, kv_heads, head_dim = k.shape
+        self.k, self.v, self.table, self.lens, self.refs = k, v, table, lens, refs
+        self.tensors = (k, v, table, lens) + (() if refs is None else (refs,))
+        self.kv_heads, self.head_dim, self.n_streams = kv_heads, head_dim, table.shape[0]
+        self.struct = _PagedCache(ctypes.sizeof(_PagedCache), layers, page, kv_heads, head_dim, k.data_ptr(), v.data_ptr(),
+                                  _pool_strides(k, k.shape, 4), _pool_strides(v, v.shape, 4), pages, table.data_ptr(), lens.data_ptr(),
+                                  _ptr(refs), table.shape[0], table.shape[1])
+        self.ref = ctypes.byref(self.struct)
+
+
+class sol_attn3d_context:
+    """Encoder states to attend to: keeps the tensors alive and marshals them.
+
+    k, v: CUDA bf16 [rows, kv_heads, head_dim]; begins, lens: int32, one per sequence (or row, for the step form); no length is
+    larger than max_len; key_mask: uint8 [rows] or None."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, begins: torch.Tensor, lens: torch.Tensor, max_len: int,
+                 key_mask: Optional[torch.Tensor] = None):
+        for t in (k, v):
+            if not t.is_cuda or t.dtype != torch.bfloat16 or t.dim() != 3 or t.shape != k.shape:
+                raise ValueError("k, v must be CUDA bf16 tensors [rows, kv_heads, head_dim] of one shape")
+        _check_index(begins, begins.numel(), "begins")
+        _check_index(lens, begins.numel(), "lens")
+        if key_mask is not None and (not key_mask.is_cuda or key_mask.dtype != torch.uint8 or not key_mask.is_contiguous() or
+                                     key_mask.numel() != k.shape[0]):
+            raise ValueError("key_mask must be a contiguous CUDA uint8 tensor with one element per row")
+        self.tensors = (k, v, begins, lens) + (() if key_mask is None else (key_mask,))
+        self.k, self.v, self.begins, self.lens, self.key_mask = k, v, begins, lens, key_mask
+        self.kv_heads, self.head_dim, self.n = k.shape[1], k.shape[2], begins.numel()
+        self.struct = _Context(ctypes.sizeof(_Context), k.shape[1], k.shape[2], k.data_ptr(), v.data_ptr(), _pool_strides(k, k.shape, 2),
+                               _pool_strides(v, v.shape, 2), k.shape[0], begins.data_ptr(), lens.data_ptr(), max_len, _ptr(key_mask))
+        self.ref = ctypes.byref(self.struct)
+
+
+def _check_workspace(t: Optional[torch.Tensor]) -> int:
+    if t is None:
+        return 0
+    if not t.is_cuda or not t.is_contiguous():
+        raise ValueError("workspace must be a contiguous CUDA tensor")
+    return t.nbytes
+
+
+def _check_requests(cache: sol_attn3d_paged_cache, status, *lists) -> int:
+    n = lists[0].numel()
+    if cache.refs is None:
+        raise ValueError("this cache keeps no count of the streams that hold a page (refs)")
+    for t in lists + (status,):
+        _check_index(t, n, "streams, parents, amounts, status")
+    _check_on_device(*cache.tensors, *lists, status)
+    return n
+
+
+def sol_attn3d_cache_workspace_bytes(cache: sol_attn3d_paged_cache, n: int) -> int:
+    return int(_lib().sol_attn3d_cache_workspace_bytes(cache.ref, n))
+
+
+def sol_attn3d_cache_reserve(cache: sol_attn3d_paged_cache, streams: torch.Tensor, amount: torch.Tensor,
+                             status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Stream streams[i] grows by amount[i] tokens and the pages that they need; status[i] says whether it did (CACHE_*)."""
+    n = _check_requests(cache, status, streams, amount)
+    _check(_lib().sol_attn3d_cache_reserve(cache.ref, n, _ptr(streams), _ptr(amount), _ptr(status), _stream(stream)), "sol_attn3d_cache_reserve")
+
+
+def sol_attn3d_cache_fork(cache: sol_attn3d_paged_cache, parents: torch.Tensor, streams: torch.Tensor, status: Optional[torch.Tensor],
+                          workspace: torch.Tensor, stream=None) -> None:
+    """The empty stream streams[i] becomes a branch of parents[i]."""
+    n = _check_requests(cache, status, parents, streams)
+    nbytes = _check_workspace(workspace)
+    _check_on_device(workspace)
+    _check(_lib().sol_attn3d_cache_fork(cache.ref, n, _ptr(parents), _ptr(streams), _ptr(status), _ptr(workspace), nbytes, _stream(stream)),
+           "sol_attn3d_cache_fork")
+
+
+def sol_attn3d_cache_compact(cache: sol_attn3d_paged_cache, streams: torch.Tensor, keep: torch.Tensor, status: Optional[torch.Tensor],
+                             workspace: torch.Tensor, stream=None) -> None:
+    """Of stream streams[i] the tokens with keep[i] != 0 stay; keep: uint8 [len(streams), width], tokens beyond the width go."""
+    n = _check_requests(cache, status, streams)
+    if not keep.is_cuda or keep.dtype != torch.uint8 or not keep.is_contiguous() or keep.dim() != 2 or keep.shape[0] != n:
+        raise ValueError("keep must be a contiguous CUDA uint8 tensor with one row per stream")
+    nbytes = _check_workspace(workspace)
+    _check_on_device(keep, workspace)
+    _check(_lib().sol_attn3d_cache_compact(cache.ref, n, _ptr(streams), _ptr(keep), keep.shape[1], _ptr(status), _ptr(workspace), nbytes,
+                                           _stream(stream)), "sol_attn3d_cache_compact")
+
+
+def sol_attn3d_cache_free(cache: sol_attn3d_paged_cache, streams: torch.Tensor, status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """The streams give their pages back and are empty."""
+    n = _check_requests(cache, status, streams)
+    _check(_lib().sol_attn3d_cache_free(cache.ref, n, _ptr(streams), _ptr(status), _stream(stream)), "sol_attn3d_cache_free")
+
+
+def sol_attn3d_cache_copy_pages(cache: sol_attn3d_paged_cache, src_pages: torch.Tensor, dst_pages: torch.Tensor, stream=None) -> None:
+    """Page dst_pages[i] = page src_pages[i], in all layers."""
+    n = src_pages.numel()
+    _check_index(src_pages, n, "src_pages")
+    _check_index(dst_pages, n, "dst_pages")
+    _check_on_device(*cache.tensors, src_pages, dst_pages)
+    _check(_lib().sol_attn3d_cache_copy_pages(cache.ref, n, _ptr(src_pages), _ptr(dst_pages), _stream(stream)), "sol_attn3d_cache_copy_pages")
+
+
+def _check_bf16(*tensors) -> None:
+    for t in tensors:
+        if not t.is_cuda or t.dtype != torch.bfloat16:
+            raise ValueError("tensors must be CUDA bf16 tensors")
+
+
+def sol_attn3d_cache_append(plan, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, q_out: Optional[torch.Tensor],
+                            cache: sol_attn3d_paged_cache, layer: int, streams: Optional[torch.Tensor] = None,
+                            pos0: Optional[torch.Tensor] = None, q_gain: Optional[torch.Tensor] = None, k_gain: Optional[torch.Tensor] = None,
+                            eps: float = 0.0, stream=None) -> None:
+    """Norm and rotation of new tokens; K and V go to the last tokens of their streams, Q to q_out."""
+    n_seqs, heads, head_dim, tokens = sol_attn3d_plan_dims(plan)
+    both = [t for t in (q, q_out) if t is not None]
+    _check_bf16(k, v, *both)
+    _check_sizes(tokens, heads * head_dim, both, ())
+    if q_out is not None and not q_out.is_contiguous():
+        raise ValueError("q_out must be contiguous")
+    want = (tokens, cache.kv_heads, cache.head_dim)
+    if k.shape != want or v.shape != want:
+        raise ValueError(f"k, v: {list(want)} for this plan and cache")
+    _check_index(streams, n_seqs, "streams")
+    if pos0 is not None and (not pos0.is_cuda or pos0.dtype != torch.int32 or not pos0.is_contiguous() or pos0.shape != (n_seqs, 3)):
+        raise ValueError("pos0 must be a contiguous CUDA int32 tensor [sequences, 3]")
+    for g in (q_gain, k_gain):
+        if g is not None:
+            _check_gain(g)
+            if g.numel() != head_dim:
+                raise ValueError("gains have head_dim elements")
+    _check_on_device(*cache.tensors, k, v, *both, streams, pos0, q_gain, k_gain)
+    _check(_lib().sol_attn3d_cache_append(plan, _ptr(q), _ptr(k), _ptr(v), _row_strides(k, head_dim), _row_strides(v, head_dim), _ptr(q_out),
+                                          cache.ref, layer, _ptr(streams), _ptr(pos0), _ptr(q_gain), _ptr(k_gain), eps, _stream(stream)),
+           "sol_attn3d_cache_append")
+
+
+def _check_key_mask(cache: sol_attn3d_paged_cache, key_mask: Optional[torch.Tensor]) -> int:
+    if key_mask is None:
+        return 0
+    if not key_mask.is_cuda or key_mask.dtype != torch.uint8 or not key_mask.is_contiguous() or key_mask.dim() != 2 or \
+            key_mask.shape[0] != cache.n_streams:
+        raise ValueError("key_mask must be a contiguous CUDA uint8 tensor [streams, tokens]")
+    return key_mask.shape[1]
+
+
+def sol_attn3d_paged_workspace_bytes(plan, cache: sol_attn3d_paged_cache) -> int:
+    return int(_lib().sol_attn3d_paged_workspace_bytes(plan, cache.ref))
+
+
+def sol_attn3d_forward_paged(plan, q: torch.Tensor, cache: sol_attn3d_paged_cache, layer: int, out: torch.Tensor,
+                             streams: Optional[torch.Tensor] = None, key_mask: Optional[torch.Tensor] = None, causal_block: int = 0,
+                             workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """The plan's sequences are the last tokens of streams of the cache and attend to them; causal_block: see the header."""
+    n_seqs, heads, head_dim, tokens = sol_attn3d_plan_dims(plan)
+    _check_bf16(q, out)
+    _check_sizes(tokens, heads * head_dim, (q, out), ())
+    _check_index(streams, n_seqs, "streams")
+    width = _check_key_mask(cache, key_mask)
+    nbytes = _check_workspace(workspace)
+    _check_on_device(*cache.tensors, q, out, streams, key_mask, workspace)
+    _check(_lib().sol_attn3d_forward_paged(plan, _ptr(q), cache.ref, layer, _ptr(out), _ptr(streams), _ptr(key_mask), width, causal_block,
+                                           _ptr(workspace), nbytes, _stream(stream)), "sol_attn3d_forward_paged")
+
+
+def sol_attn3d_paged_step_workspace_bytes(cache: sol_attn3d_paged_cache, batch: int, heads: int) -> int:
+    return int(_lib().sol_attn3d_paged_step_workspace_bytes(cache.ref, batch, heads))
+
+
+def _check_rows(q: torch.Tensor, out: torch.Tensor, head_dim: int) -> None:
+    _check_bf16(q, out)
+    if q.dim() != 3 or q.shape != out.shape or q.shape[2] != head_dim:
+        raise ValueError(f"q, out: [batch, heads, {head_dim}]")
+
+
+def sol_attn3d_paged_step(q: torch.Tensor, cache: sol_attn3d_paged_cache, layer: int, out: torch.Tensor,
+                          streams: Optional[torch.Tensor] = None, key_mask: Optional[torch.Tensor] = None,
+                          workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """One token per row, q, out [batch, heads, D]: the last token of its stream, over all of the stream."""
+    head_dim = cache.head_dim
+    _check_rows(q, out, head_dim)
+    batch, heads = q.shape[0], q.shape[1]
+    _check_index(streams, batch, "streams")
+    width = _check_key_mask(cache, key_mask)
+    nbytes = _check_workspace(workspace)
+    _check_on_device(*cache.tensors, q, out, streams, key_mask, workspace)
+    _check(_lib().sol_attn3d_paged_step(_ptr(q), _DENSE2 if q.is_contiguous() else _row_strides(q, head_dim), cache.ref, layer, _ptr(streams),
+                                        _ptr(out), _DENSE2 if out.is_contiguous() else _row_strides(out, head_dim), batch, heads,
+                                        _ptr(key_mask), width, _ptr(workspace), nbytes, _stream(stream)), "sol_attn3d_paged_step")
+
+
+def sol_attn3d_cross_workspace_bytes(plan, context: sol_attn3d_context) -> int:
+    return int(_lib().sol_attn3d_cross_workspace_bytes(plan, context.ref))
+
+
+def sol_attn3d_forward_cross(plan, q: torch.Tensor, context: sol_attn3d_context, out: torch.Tensor,
+                             workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Cross attention of the plan's sequences, each to its context."""
+    n_seqs, heads, head_dim, tokens = sol_attn3d_plan_dims(plan)
+    _check_bf16(q, out)
+    _check_sizes(tokens, heads * head_dim, (q, out), ())
+    if context.n != n_seqs:
+        raise ValueError(f"{n_seqs} sequences need as many contexts")
+    nbytes = _check_workspace(workspace)
+    _check_on_device(*context.tensors, q, out, workspace)
+    _check(_lib().sol_attn3d_forward_cross(plan, _ptr(q), context.ref, _ptr(out), _ptr(workspace), nbytes, _stream(stream)),
+           "sol_attn3d_forward_cross")
+
+
+def sol_attn3d_cross_step_workspace_bytes(context: sol_attn3d_context, batch: int, heads: int) -> int:
+    return int(_lib().sol_attn3d_cross_step_workspace_bytes(context.ref, batch, heads))
+
+
+def sol_attn3d_cross_step(q: torch.Tensor, context: sol_attn3d_context, out: torch.Tensor, workspace: Optional[torch.Tensor] = None,
+                          stream=None) -> None:
+    """One row per context, q, out [batch, heads, D]."""
+    head_dim = context.head_dim
+    _check_rows(q, out, head_dim)
+    batch, heads = q.shape[0], q.shape[1]
+    if context.n != batch:
+        raise ValueError("one context per row")
+    nbytes = _check_workspace(workspace)
+    _check_on_device(*context.tensors, q, out, workspace)
+    _check(_lib().sol_attn3d_cross_step(_ptr(q), _DENSE2 if q.is_contiguous() else _row_strides(q, head_dim), context.ref, _ptr(out),
+                                        _DENSE2 if out.is_contiguous() else _row_strides(out, head_dim), batch, heads, _ptr(workspace), nbytes,
+                                        _stream(stream)), "sol_attn3d_cross_step")
 
 
 def sol_attn3d_rope_qk(plan, q, k, q_rot, k_rot, stream=None) -> None:

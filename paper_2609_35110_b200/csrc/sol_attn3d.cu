@@ -14,6 +14,8 @@
 #include <vector>
 
 #include "attn_fwd_sm100.cuh"
+#include "cache_kernels.cuh"
+#include "context_attn.cuh"
 #include "device_types.cuh"
 #include "linear_attn_sm100.cuh"
 #include "prologue_kernels.cuh"
@@ -45,6 +47,7 @@ struct sol_attn3d_plan_s {
   Strides sq{}, sk{}, sv{}, so{};
   std::vector<int64_t> cu;            // caller order
   std::vector<SeqDev> sched;          // schedule order (longest first)
+  std::vector<int> cum_tok;           // tokens of the sequences before each one in the schedule
   long long total_tokens = 0;
   int total_work = 0;
   int total_quad_work = 0;            // work items when CTA pairs serve 512-row query blocks
@@ -61,9 +64,9 @@ struct sol_attn3d_plan_s {
 
   // workspace layout (byte offsets)
   size_t off_status = 0, off_tables = 0, off_seqs = 0, off_keybits = 0, off_list = 0, off_count = 0, off_pairs = 0,
-         off_dbits = 0, off_dlist = 0, off_dcount = 0, off_drange = 0,
+         off_dbits = 0, off_dlist = 0, off_dcount = 0, off_drange = 0, off_cum = 0,
          off_qrot = 0, off_krot = 0, ws_bytes = 0;
-  size_t ws_dense_bytes = 0;          // what every call but the differential attention uses (a prefix of the workspace)
+  size_t ws_dense_bytes = 0;          // what sol_attn3d_forward and its variants use (a prefix of the workspace)
   int total_pairs = 0;
   unsigned char* ws = nullptr;
   // block-sparse scratch (passed per call): byte offsets
@@ -290,7 +293,10 @@ int build_plan(sol_attn3d_plan_t* out, const sol_attn3d_desc* d) {
     long long quad_work = 0;
     long long ktiles = 0;
     long long pairs = 0;
+    long long tokens = 0;
     for (SeqDev& q : seqs) {
+      p->cum_tok.push_back((int)tokens);
+      tokens += q.n_tokens;
       q.work_start = (int)work;
       q.quad_work_start = (int)quad_work;
       quad_work += (long long)((q.n_qpairs + 1) / 2) * d->heads;
@@ -369,6 +375,7 @@ int build_plan(sol_attn3d_plan_t* out, const sol_attn3d_desc* d) {
       p->off_dcount = off;  off = align_up(off + (size_t)p->n_seqs * sizeof(int));
       p->off_drange = off;  off = align_up(off + range_bytes(p));
     }
+    p->off_cum = off;       off = align_up(off + (size_t)p->n_seqs * sizeof(int));
     p->ws_bytes = off;
 
     if (const char* e = std::getenv("SOL_ATTN3D_WAIT_LIMIT_MS")) {
@@ -549,6 +556,8 @@ int sol_attn3d_set_workspace(sol_attn3d_plan_t p, void* device_ptr, size_t bytes
     return fail_cuda(p, e);
   if ((e = cudaMemcpy(p->ws + p->off_seqs, p->sched.data(), p->sched.size() * sizeof(SeqDev),
                       cudaMemcpyHostToDevice)) != cudaSuccess)
+    return fail_cuda(p, e);
+  if ((e = cudaMemcpy(p->ws + p->off_cum, p->cum_tok.data(), p->cum_tok.size() * sizeof(int), cudaMemcpyHostToDevice)) != cudaSuccess)
     return fail_cuda(p, e);
   const Strides dense{(long long)p->heads * p->head_dim, (long long)p->head_dim};
   int rc = encode_map(p->encode, p, &p->tm_q, p->ws + p->off_qrot, dense);
@@ -1488,6 +1497,8 @@ int sol_attn3d_forward_linear(sol_attn3d_plan_t p, const void* q, const void* k,
   }
   return SOL_ATTN3D_OK;
 }
+
+#include "streaming_host.cuh"
 
 int sol_attn3d_set_profiling(sol_attn3d_plan_t p, int enable) {
   if (p == nullptr) return SOL_ATTN3D_ERR_INVALID_ARG;

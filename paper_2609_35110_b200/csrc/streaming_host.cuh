@@ -1,0 +1,488 @@
+// Host side of streaming generation: paged cache, attention over it, cross attention.  Part of sol_attn3d.cu (inside extern "C").
+
+extern "C++" {
+namespace {
+
+bool aligned4(const void* x) { return (reinterpret_cast<uintptr_t>(x) & 3u) == 0; }
+
+// Checks a cache and, for a layer, fills in what the kernels see of it.
+int take_cache(const sol_attn3d_paged_cache* c, int layer, sol::PagedDev* out) {
+  if (c == nullptr || c->size != sizeof(sol_attn3d_paged_cache) || c->n_layers < 1 || c->page_size < 1 || c->kv_heads < 1 ||
+      c->head_dim < 1 || c->n_pages < 1 || c->n_streams < 1 || c->table_width < 1 || layer < 0 || layer >= c->n_layers)
+    return SOL_ATTN3D_ERR_INVALID_ARG;
+  if ((c->head_dim != 64 && c->head_dim != 128) || c->kv_heads > 65535 || c->page_size % 16 != 0 || c->page_size > 4096 ||
+      c->n_pages >= (1ll << 31) || c->table_width >= (1ll << 31) || c->n_streams >= (1ll << 31) ||
+      c->n_pages * c->page_size >= (1ll << 31) || c->table_width * c->page_size >= (1ll << 31))
+    return SOL_ATTN3D_ERR_UNSUPPORTED_SHAPE;
+  if (c->k == nullptr || c->v == nullptr || c->table == nullptr || c->lens == nullptr || !aligned16(c->k) || !aligned16(c->v) ||
+      !aligned4(c->table) || !aligned4(c->lens) || !aligned4(c->refs))
+    return SOL_ATTN3D_ERR_INVALID_ARG;
+  auto take = [&](const int64_t st[4], long long (&full)[4]) {
+    full[3] = st[3] == 0 ? c->head_dim : st[3];
+    full[2] = st[2] == 0 ? (long long)c->kv_heads * c->head_dim : st[2];
+    if (!stride_ok(full[3]) || !stride_ok(full[2])) return false;
+    full[1] = st[1] == 0 ? c->page_size * full[2] : st[1];
+    if (!stride_ok(full[1])) return false;
+    full[0] = st[0] == 0 ? c->n_pages * full[1] : st[0];
+    return full[0] > 0 && full[0] % 8 == 0 && full[0] < (1ll << 46);
+  };
+  long long ks[4], vs[4];
+  if (!take(c->k_strides, ks) || !take(c->v_strides, vs)) return SOL_ATTN3D_ERR_UNSUPPORTED_SHAPE;
+  out->k = static_cast<__nv_bfloat16*>(c->k) + layer * ks[0];
+  out->v = static_cast<__nv_bfloat16*>(c->v) + layer * vs[0];
+  for (int i = 0; i < 3; ++i) {
+    out->ks[i] = ks[i + 1];
+    out->vs[i] = vs[i + 1];
+  }
+  out->table = c->table;
+  out->lens = c->lens;
+  out->width = c->table_width;
+  out->n_streams = c->n_streams;
+  out->n_pages = c->n_pages;
+  out->page = c->page_size;
+  out->kv_heads = c->kv_heads;
+  return SOL_ATTN3D_OK;
+}
+
+int take_context(const sol_attn3d_context* x, sol::KeysDev* d) {
+  if (x == nullptr || x->size != sizeof(sol_attn3d_context) || x->kv_heads < 1 || x->head_dim < 1 || x->total_rows < 0 || x->max_len < 0)
+    return SOL_ATTN3D_ERR_INVALID_ARG;
+  if ((x->head_dim != 64 && x->head_dim != 128) || x->kv_heads > 65535 || x->total_rows >= (1ll << 31))
+    return SOL_ATTN3D_ERR_UNSUPPORTED_SHAPE;
+  if (x->begins == nullptr || x->lens == nullptr || !aligned4(x->begins) || !aligned4(x->lens) || !aligned16(x->k) || !aligned16(x->v) ||
+      (x->total_rows > 0 && (x->k == nullptr || x->v == nullptr)))
+    return SOL_ATTN3D_ERR_INVALID_ARG;
+  auto take = [&](const int64_t st[2], long long (&full)[3]) {
+    full[0] = 0;
+    full[2] = st[1] == 0 ? x->head_dim : st[1];
+    full[1] = st[0] == 0 ? (long long)x->kv_heads * x->head_dim : st[0];
+    return stride_ok(full[1]) && stride_ok(full[2]);
+  };
+  if (!take(x->k_strides, d->c.ks) || !take(x->v_strides, d->c.vs)) return SOL_ATTN3D_ERR_UNSUPPORTED_SHAPE;
+  d->c.k = static_cast<__nv_bfloat16*>(const_cast<void*>(x->k));
+  d->c.v = static_cast<__nv_bfloat16*>(const_cast<void*>(x->v));
+  d->c.kv_heads = x->kv_heads;
+  d->begins = x->begins;
+  d->lens = x->lens;
+  d->total_rows = x->total_rows;
+  d->mask = x->key_mask;
+  return SOL_ATTN3D_OK;
+}
+
+// ---- attention of few rows ------------------------------------------------------------------------------------------------
+// Splits of the keys: with few units, as many as make three whole waves of resident CTAs; with many, six waves, so that streams of
+// different length even out.  No split below 128 keys of the longest possible past.  Depends on the sizes of the call only (the
+// lengths live on the device).
+constexpr long long kFewWave = 148 * sol::kFewResident, kFewMinKeys = 128, kFewMaxSplit = 256;
+int few_splits(long long items, long long capacity) {
+  if (items < 1) return 1;
+  const long long want = 4 * items <= 3 * kFewWave ? 3 * kFewWave / items : (6 * kFewWave + items - 1) / items;
+  return (int)std::max<long long>(1, std::min<long long>(std::min<long long>(want, kFewMaxSplit), capacity / kFewMinKeys));
+}
+long long few_units(sol_attn3d_plan_t p, int batch, int group) {
+  return p != nullptr ? p->total_tokens * group / sol::kFewRows + p->n_seqs : (long long)batch * ((group + sol::kFewRows - 1) / sol::kFewRows);
+}
+size_t few_bytes(long long units, int kv_heads, int head_dim, long long capacity) {
+  const int n = few_splits(units * kv_heads, capacity);
+  return n == 1 ? 0 : align_up((size_t)units * kv_heads * n * sol::kFewRows * (head_dim + 4) * sizeof(float));
+}
+
+template <int D, bool kPaged>
+cudaError_t launch_few(const sol::FewArgs& f, cudaStream_t st, int* launches) {
+  const unsigned items = (unsigned)(f.units * f.d.c.kv_heads);
+  sol::few_rows_kernel<D, kPaged><<<items * (unsigned)f.n_split, sol::kFewThreads, 0, st>>>(f);
+  cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return e;
+  ++*launches;
+  if (f.partial != nullptr) {
+    const sol::JoinArgs j{f.a, f.d, f.n_split, sol::kFewRows, f.units, f.partial};
+    sol::join_rows_kernel<D, kPaged><<<items, 256, 0, st>>>(j);
+    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    ++*launches;
+  }
+  return cudaSuccess;
+}
+
+// Attention of `units` units of few rows; plan or batch as in few_units.
+int attend_few(sol::QueriesDev a, const sol::KeysDev& d, bool paged, int head_dim, long long units, long long capacity, void* workspace,
+               size_t workspace_bytes, cudaStream_t st, int* launches, int* cuda_error) {
+  sol::FewArgs f{};
+  f.a = a;
+  f.d = d;
+  f.units = units;
+  f.n_split = few_splits(units * d.c.kv_heads, capacity);
+  if (units * d.c.kv_heads * f.n_split >= (1ll << 31)) return SOL_ATTN3D_ERR_UNSUPPORTED_SHAPE;
+  if (f.n_split > 1) {
+    if (workspace == nullptr || workspace_bytes < few_bytes(units, d.c.kv_heads, head_dim, capacity) ||
+        (reinterpret_cast<uintptr_t>(workspace) % kAlign) != 0)
+      return SOL_ATTN3D_ERR_NO_WORKSPACE;
+    f.partial = static_cast<float*>(workspace);
+  }
+  const cudaError_t e = head_dim == 128 ? (paged ? launch_few<128, true>(f, st, launches) : launch_few<128, false>(f, st, launches))
+                                        : (paged ? launch_few<64, true>(f, st, launches) : launch_few<64, false>(f, st, launches));
+  if (e == cudaSuccess) return SOL_ATTN3D_OK;
+  *cuda_error = (int)e;
+  return SOL_ATTN3D_ERR_CUDA;
+}
+
+// ---- attention over a plan's sequences ---------------------------------------------------------------------------------------
+size_t context_bytes(sol_attn3d_plan_t p, int kv_heads, long long capacity) {
+  if (p == nullptr || p->heads % kv_heads != 0) return 0;
+  const int group = p->heads / kv_heads;
+  return few_bytes(few_units(p, 0, group), kv_heads, p->head_dim, capacity);
+}
+
+int forward_context(sol_attn3d_plan_t p, const void* q, void* out, const sol::KeysDev& d, bool paged, long long capacity, int causal,
+                    void* workspace, size_t workspace_bytes, sol_attn3d_stream_t stream) {
+  if (q == nullptr || out == nullptr || q == out || !aligned16(q) || !aligned16(out)) return SOL_ATTN3D_ERR_INVALID_ARG;
+  if (p->heads % d.c.kv_heads != 0) return SOL_ATTN3D_ERR_UNSUPPORTED_SHAPE;
+  if (p->ws == nullptr || p->encode == nullptr) return SOL_ATTN3D_ERR_NO_WORKSPACE;
+  sol::QueriesDev a{};
+  a.q = static_cast<const __nv_bfloat16*>(q);
+  a.out = static_cast<__nv_bfloat16*>(out);
+  a.q_tok = p->sq.tok; a.q_head = p->sq.head;
+  a.o_tok = p->so.tok; a.o_head = p->so.head;
+  a.seqs = reinterpret_cast<const SeqDev*>(p->ws + p->off_seqs);
+  a.cum_tok = reinterpret_cast<const int*>(p->ws + p->off_cum);
+  a.n_seqs = p->n_seqs;
+  a.group = p->heads / d.c.kv_heads;
+  a.causal = causal;
+  a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)p->head_dim));
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  cudaError_t e;
+  p->launches = 0;
+  if (p->prof) {                                           // no bits and no rotary prologue: only the last interval counts
+    p->prof_valid = false;
+    p->prof_bits = false;
+    for (int i = 0; i < 3; ++i)
+      if ((e = cudaEventRecord(p->ev[i], st)) != cudaSuccess) return fail_cuda(p, e);
+  }
+  const int rc = attend_few(a, d, paged, p->head_dim, few_units(p, 0, a.group), capacity, workspace, workspace_bytes, st, &p->launches, &p->last_cuda);
+  if (rc != SOL_ATTN3D_OK) return rc;
+  if (p->prof) {
+    if ((e = cudaEventRecord(p->ev[3], st)) != cudaSuccess) return fail_cuda(p, e);
+    p->prof_valid = true;
+  }
+  return SOL_ATTN3D_OK;
+}
+
+int step_context(const void* q, const int64_t q_strides[2], const sol::KeysDev& d, bool paged, void* out, const int64_t out_strides[2],
+                 int batch, int heads, int head_dim, long long capacity, void* workspace, size_t workspace_bytes, sol_attn3d_stream_t stream) {
+  if (batch < 0 || heads < 1) return SOL_ATTN3D_ERR_INVALID_ARG;
+  if (heads % d.c.kv_heads != 0 || heads > 65535) return SOL_ATTN3D_ERR_UNSUPPORTED_SHAPE;
+  if (batch == 0) return SOL_ATTN3D_OK;
+  if (q == nullptr || out == nullptr || q == out || !aligned16(q) || !aligned16(out) || q_strides == nullptr || out_strides == nullptr)
+    return SOL_ATTN3D_ERR_INVALID_ARG;
+  sol::QueriesDev a{};
+  const long long row = (long long)heads * head_dim;
+  a.q = static_cast<const __nv_bfloat16*>(q);
+  a.out = static_cast<__nv_bfloat16*>(out);
+  a.q_tok = q_strides[0] == 0 ? row : q_strides[0];
+  a.q_head = q_strides[1] == 0 ? head_dim : q_strides[1];
+  a.o_tok = out_strides[0] == 0 ? row : out_strides[0];
+  a.o_head = out_strides[1] == 0 ? head_dim : out_strides[1];
+  if (!stride_ok(a.q_tok) || !stride_ok(a.q_head) || !stride_ok(a.o_tok) || !stride_ok(a.o_head)) return SOL_ATTN3D_ERR_UNSUPPORTED_SHAPE;
+  a.n_seqs = batch;
+  a.group = heads / d.c.kv_heads;
+  a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)head_dim));
+  int launches = 0, cuda_error = 0;
+  return attend_few(a, d, paged, head_dim, few_units(nullptr, batch, a.group), capacity, workspace, workspace_bytes,
+                    static_cast<cudaStream_t>(stream), &launches, &cuda_error);
+}
+
+size_t step_bytes(int batch, int heads, int kv_heads, int head_dim, long long capacity) {
+  if (batch < 1 || heads < 1 || heads % kv_heads != 0) return 0;
+  return few_bytes(few_units(nullptr, batch, heads / kv_heads), kv_heads, head_dim, capacity);
+}
+
+// ---- bookkeeping --------------------------------------------------------------------------------------------------------------
+// Workspace of fork and compact: moves [n][capacity] | moved [n + 1] | kept [n] | first [n] | old_pages [n][table_width]
+struct BookSpace {
+  size_t moved, kept, first, old_pages, bytes;
+};
+BookSpace book_space(const sol_attn3d_paged_cache* c, int n) {
+  BookSpace s;
+  size_t o = align_up((size_t)n * c->table_width * c->page_size * sizeof(int2));
+  s.moved = o;     o = align_up(o + ((size_t)n + 1) * sizeof(long long));
+  s.kept = o;      o = align_up(o + (size_t)n * sizeof(int));
+  s.first = o;     o = align_up(o + (size_t)n * sizeof(int));
+  s.old_pages = o; o = align_up(o + (size_t)n * c->table_width * sizeof(int));
+  s.bytes = o;
+  return s;
+}
+
+int take_book(const sol_attn3d_paged_cache* c, int n, const int32_t* streams, int32_t* status, sol::BookArgs* b) {
+  sol::PagedDev layer{};
+  const int rc = take_cache(c, 0, &layer);
+  if (rc != SOL_ATTN3D_OK) return rc;
+  if (n < 0 || c->refs == nullptr || !aligned4(streams) || !aligned4(status) || (n > 0 && streams == nullptr)) return SOL_ATTN3D_ERR_INVALID_ARG;
+  if (n > sol::kMaxRequests) return SOL_ATTN3D_ERR_UNSUPPORTED_SHAPE;
+  b->table = c->table;
+  b->lens = c->lens;
+  b->refs = c->refs;
+  b->width = c->table_width;
+  b->n_streams = c->n_streams;
+  b->n_pages = c->n_pages;
+  b->page = c->page_size;
+  b->n = n;
+  b->streams = streams;
+  b->status = status;
+  return SOL_ATTN3D_OK;
+}
+
+int take_book_space(const sol_attn3d_paged_cache* c, int n, void* workspace, size_t bytes, sol::BookArgs* b) {
+  const BookSpace s = book_space(c, n);
+  if (workspace == nullptr || bytes < s.bytes || (reinterpret_cast<uintptr_t>(workspace) % kAlign) != 0) return SOL_ATTN3D_ERR_NO_WORKSPACE;
+  unsigned char* w = static_cast<unsigned char*>(workspace);
+  b->moves = reinterpret_cast<int2*>(w);
+  b->moves_cap = c->table_width * c->page_size;
+  b->moved = reinterpret_cast<long long*>(w + s.moved);
+  b->kept = reinterpret_cast<int*>(w + s.kept);
+  b->first = reinterpret_cast<int*>(w + s.first);
+  b->old_pages = reinterpret_cast<int*>(w + s.old_pages);
+  return SOL_ATTN3D_OK;
+}
+
+constexpr size_t kBookSmem = sizeof(sol::BookSmem) + sol::kMaxRequests * sizeof(int);
+
+template <typename K>
+int launch_book(K kernel, const sol::BookArgs& b, cudaStream_t st) {
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kBookSmem) != cudaSuccess) {
+    (void)cudaGetLastError();
+    return SOL_ATTN3D_ERR_CUDA;
+  }
+  kernel<<<1, sol::kBookThreads, kBookSmem, st>>>(b);
+  return cudaGetLastError() == cudaSuccess ? SOL_ATTN3D_OK : SOL_ATTN3D_ERR_CUDA;
+}
+
+template <bool kPages>
+int launch_move(const sol_attn3d_paged_cache* c, sol::MoveArgs m, cudaStream_t st) {
+  sol::PagedDev layer{};
+  int rc = take_cache(c, 0, &layer);
+  if (rc != SOL_ATTN3D_OK) return rc;
+  m.k = layer.k;
+  m.v = layer.v;
+  for (int i = 0; i < 3; ++i) {
+    m.ks[i + 1] = layer.ks[i];
+    m.vs[i + 1] = layer.vs[i];
+  }
+  m.ks[0] = c->k_strides[0] == 0 ? c->n_pages * m.ks[1] : c->k_strides[0];
+  m.vs[0] = c->v_strides[0] == 0 ? c->n_pages * m.vs[1] : c->v_strides[0];
+  m.layers = c->n_layers;
+  m.page = c->page_size;
+  m.kv_heads = c->kv_heads;
+  m.head_dim = c->head_dim;
+  m.n_pages = c->n_pages;
+  // the number of rows is on the device: eight resident blocks per SM walk over them
+  sol::cache_move_kernel<kPages><<<148 * 8, 256, 0, st>>>(m);
+  return cudaGetLastError() == cudaSuccess ? SOL_ATTN3D_OK : SOL_ATTN3D_ERR_CUDA;
+}
+
+}  // namespace
+}  // extern "C++"
+
+size_t sol_attn3d_cache_workspace_bytes(const sol_attn3d_paged_cache* cache, int n) {
+  sol::PagedDev layer{};
+  if (n < 1 || n > sol::kMaxRequests || take_cache(cache, 0, &layer) != SOL_ATTN3D_OK) return 0;
+  return book_space(cache, n).bytes;
+}
+
+int sol_attn3d_cache_reserve(const sol_attn3d_paged_cache* cache, int n, const int32_t* streams, const int32_t* amount, int32_t* status,
+                             sol_attn3d_stream_t stream) {
+  sol::BookArgs b{};
+  const int rc = take_book(cache, n, streams, status, &b);
+  if (rc != SOL_ATTN3D_OK || n == 0) return rc;
+  if (amount == nullptr || !aligned4(amount)) return SOL_ATTN3D_ERR_INVALID_ARG;
+  b.amount = amount;
+  return launch_book(sol::cache_reserve_kernel, b, static_cast<cudaStream_t>(stream));
+}
+
+int sol_attn3d_cache_fork(const sol_attn3d_paged_cache* cache, int n, const int32_t* parents, const int32_t* streams, int32_t* status,
+                          void* workspace, size_t workspace_bytes, sol_attn3d_stream_t stream) {
+  sol::BookArgs b{};
+  int rc = take_book(cache, n, streams, status, &b);
+  if (rc != SOL_ATTN3D_OK || n == 0) return rc;
+  if (parents == nullptr || !aligned4(parents)) return SOL_ATTN3D_ERR_INVALID_ARG;
+  if ((rc = take_book_space(cache, n, workspace, workspace_bytes, &b)) != SOL_ATTN3D_OK) return rc;
+  b.parents = parents;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if ((rc = launch_book(sol::cache_fork_kernel, b, st)) != SOL_ATTN3D_OK) return rc;
+  sol::MoveArgs m{};
+  m.n = n;
+  m.moves = b.moves;
+  m.moves_cap = b.moves_cap;
+  m.moved = b.moved;
+  return launch_move<false>(cache, m, st);
+}
+
+int sol_attn3d_cache_compact(const sol_attn3d_paged_cache* cache, int n, const int32_t* streams, const uint8_t* keep, int64_t keep_width,
+                             int32_t* status, void* workspace, size_t workspace_bytes, sol_attn3d_stream_t stream) {
+  sol::BookArgs b{};
+  int rc = take_book(cache, n, streams, status, &b);
+  if (rc != SOL_ATTN3D_OK || n == 0) return rc;
+  if (keep == nullptr || keep_width < 1) return SOL_ATTN3D_ERR_INVALID_ARG;
+  if ((rc = take_book_space(cache, n, workspace, workspace_bytes, &b)) != SOL_ATTN3D_OK) return rc;
+  b.keep = keep;
+  b.keep_stride = keep_width;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  sol::cache_keep_kernel<<<(unsigned)n, sol::kBookThreads, 0, st>>>(b);
+  if (cudaGetLastError() != cudaSuccess) return SOL_ATTN3D_ERR_CUDA;
+  if ((rc = launch_book(sol::cache_compact_kernel, b, st)) != SOL_ATTN3D_OK) return rc;
+  sol::MoveArgs m{};
+  m.n = n;
+  m.moves = b.moves;
+  m.moves_cap = b.moves_cap;
+  m.moved = b.moved;
+  m.first = b.first;
+  m.streams = streams;
+  m.table = cache->table;
+  m.width = cache->table_width;
+  return launch_move<false>(cache, m, st);
+}
+
+int sol_attn3d_cache_free(const sol_attn3d_paged_cache* cache, int n, const int32_t* streams, int32_t* status, sol_attn3d_stream_t stream) {
+  sol::BookArgs b{};
+  const int rc = take_book(cache, n, streams, status, &b);
+  if (rc != SOL_ATTN3D_OK || n == 0) return rc;
+  sol::cache_free_kernel<<<1, sol::kBookThreads, 0, static_cast<cudaStream_t>(stream)>>>(b);
+  return cudaGetLastError() == cudaSuccess ? SOL_ATTN3D_OK : SOL_ATTN3D_ERR_CUDA;
+}
+
+int sol_attn3d_cache_copy_pages(const sol_attn3d_paged_cache* cache, int n, const int32_t* src_pages, const int32_t* dst_pages,
+                                sol_attn3d_stream_t stream) {
+  sol::PagedDev layer{};
+  const int rc = take_cache(cache, 0, &layer);
+  if (rc != SOL_ATTN3D_OK) return rc;
+  if (n < 0) return SOL_ATTN3D_ERR_INVALID_ARG;
+  if (n > (1 << 20)) return SOL_ATTN3D_ERR_UNSUPPORTED_SHAPE;
+  if (n == 0) return SOL_ATTN3D_OK;
+  if (src_pages == nullptr || dst_pages == nullptr || !aligned4(src_pages) || !aligned4(dst_pages)) return SOL_ATTN3D_ERR_INVALID_ARG;
+  sol::MoveArgs m{};
+  m.n = n;
+  m.src_pages = src_pages;
+  m.dst_pages = dst_pages;
+  return launch_move<true>(cache, m, static_cast<cudaStream_t>(stream));
+}
+
+int sol_attn3d_cache_append(sol_attn3d_plan_t p, const void* q, const void* k, const void* v, const int64_t k_strides[2],
+                            const int64_t v_strides[2], void* q_out, const sol_attn3d_paged_cache* cache, int layer,
+                            const int32_t* streams, const int32_t* pos0, const float* q_gain, const float* k_gain, float eps,
+                            sol_attn3d_stream_t stream) {
+  if (p == nullptr || k == nullptr || v == nullptr || k_strides == nullptr || v_strides == nullptr) return SOL_ATTN3D_ERR_INVALID_ARG;
+  if ((q == nullptr) != (q_out == nullptr) || (q != nullptr && (q == q_out || k == q_out || v == q_out))) return SOL_ATTN3D_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out) || !aligned16(q_gain) || !aligned16(k_gain) || !aligned4(streams) ||
+      !aligned4(pos0) || !(eps >= 0.f) || !std::isfinite(eps))
+    return SOL_ATTN3D_ERR_INVALID_ARG;
+  sol::AppendArgs a{};
+  const int rc = take_cache(cache, layer, &a.c);
+  if (rc != SOL_ATTN3D_OK) return rc;
+  if (cache->head_dim != p->head_dim) return SOL_ATTN3D_ERR_UNSUPPORTED_SHAPE;
+  const long long dense = (long long)cache->kv_heads * cache->head_dim;
+  const int64_t* st[2] = {k_strides, v_strides};
+  a.x_tok[0] = p->sq.tok;
+  a.x_head[0] = p->sq.head;
+  for (int i = 0; i < 2; ++i) {
+    a.x_tok[i + 1] = st[i][0] == 0 ? dense : st[i][0];
+    a.x_head[i + 1] = st[i][1] == 0 ? cache->head_dim : st[i][1];
+    if (!stride_ok(a.x_tok[i + 1]) || !stride_ok(a.x_head[i + 1])) return SOL_ATTN3D_ERR_UNSUPPORTED_SHAPE;
+  }
+  if (p->ws == nullptr) return SOL_ATTN3D_ERR_NO_WORKSPACE;
+  a.x[0] = static_cast<const __nv_bfloat16*>(q);
+  a.x[1] = static_cast<const __nv_bfloat16*>(k);
+  a.x[2] = static_cast<const __nv_bfloat16*>(v);
+  a.q_out = static_cast<__nv_bfloat16*>(q_out);
+  a.gain[0] = q_gain;
+  a.gain[1] = k_gain;
+  a.eps = eps;
+  a.seqs = reinterpret_cast<const SeqDev*>(p->ws + p->off_seqs);
+  a.n_seqs = p->n_seqs;
+  a.total_tokens = p->total_tokens;
+  a.tables = reinterpret_cast<const float2*>(p->ws + p->off_tables);
+  for (int i = 0; i < 3; ++i) { a.g.rope[i] = p->rope[i]; a.g.tab_off[i] = p->tab_off[i]; }
+  a.g.head_dim = p->head_dim;
+  a.g.heads = p->heads;
+  a.streams = streams;
+  a.pos0 = pos0;
+  for (int axis = 0, pair = 0; axis < 3; ++axis)
+    for (int j = 0; j < p->rope[axis] / 2; ++j) a.omega[pair++] = std::exp(-(2.0 * j / p->rope[axis]) * std::log(p->theta));
+  const int chunks = p->head_dim / 8, rows = (q != nullptr ? p->heads : 0) + 2 * cache->kv_heads;
+  const int unit = 32 / chunks;                            // rows per warp
+  const int per_pass = std::min(256 / chunks, (rows + unit - 1) / unit * unit);
+  const long long blocks = std::min<long long>(p->total_tokens, 148ll * 16);
+  p->launches = 0;
+  sol::cache_append_kernel<<<(unsigned)blocks, chunks * per_pass, 0, static_cast<cudaStream_t>(stream)>>>(a);
+  const cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return fail_cuda(p, e);
+  ++p->launches;
+  return SOL_ATTN3D_OK;
+}
+
+size_t sol_attn3d_paged_workspace_bytes(sol_attn3d_plan_t plan, const sol_attn3d_paged_cache* cache) {
+  sol::PagedDev c{};
+  if (plan == nullptr || take_cache(cache, 0, &c) != SOL_ATTN3D_OK) return 0;
+  return context_bytes(plan, c.kv_heads, c.width * c.page);
+}
+
+int sol_attn3d_forward_paged(sol_attn3d_plan_t p, const void* q, const sol_attn3d_paged_cache* cache, int layer, void* out,
+                             const int32_t* streams, const uint8_t* key_mask, int64_t mask_width, int causal_block, void* workspace,
+                             size_t workspace_bytes, sol_attn3d_stream_t stream) {
+  if (p == nullptr || causal_block < 0 || (key_mask != nullptr && mask_width < 1) || !aligned4(streams)) return SOL_ATTN3D_ERR_INVALID_ARG;
+  sol::KeysDev d{};
+  const int rc = take_cache(cache, layer, &d.c);
+  if (rc != SOL_ATTN3D_OK) return rc;
+  if (cache->head_dim != p->head_dim) return SOL_ATTN3D_ERR_UNSUPPORTED_SHAPE;
+  d.streams = streams;
+  d.mask = key_mask;
+  d.mask_stride = mask_width;
+  return forward_context(p, q, out, d, true, d.c.width * d.c.page, causal_block, workspace, workspace_bytes, stream);
+}
+
+size_t sol_attn3d_paged_step_workspace_bytes(const sol_attn3d_paged_cache* cache, int batch, int heads) {
+  sol::PagedDev c{};
+  if (take_cache(cache, 0, &c) != SOL_ATTN3D_OK) return 0;
+  return step_bytes(batch, heads, c.kv_heads, cache->head_dim, c.width * c.page);
+}
+
+int sol_attn3d_paged_step(const void* q, const int64_t q_strides[2], const sol_attn3d_paged_cache* cache, int layer, const int32_t* streams,
+                          void* out, const int64_t out_strides[2], int batch, int heads, const uint8_t* key_mask, int64_t mask_width,
+                          void* workspace, size_t workspace_bytes, sol_attn3d_stream_t stream) {
+  if ((key_mask != nullptr && mask_width < 1) || !aligned4(streams)) return SOL_ATTN3D_ERR_INVALID_ARG;
+  sol::KeysDev d{};
+  const int rc = take_cache(cache, layer, &d.c);
+  if (rc != SOL_ATTN3D_OK) return rc;
+  d.streams = streams;
+  d.mask = key_mask;
+  d.mask_stride = mask_width;
+  return step_context(q, q_strides, d, true, out, out_strides, batch, heads, cache->head_dim, d.c.width * d.c.page, workspace, workspace_bytes, stream);
+}
+
+size_t sol_attn3d_cross_workspace_bytes(sol_attn3d_plan_t plan, const sol_attn3d_context* context) {
+  sol::KeysDev d{};
+  if (plan == nullptr || take_context(context, &d) != SOL_ATTN3D_OK) return 0;
+  return context_bytes(plan, context->kv_heads, std::min(context->max_len, context->total_rows));
+}
+
+int sol_attn3d_forward_cross(sol_attn3d_plan_t p, const void* q, const sol_attn3d_context* context, void* out, void* workspace,
+                             size_t workspace_bytes, sol_attn3d_stream_t stream) {
+  if (p == nullptr) return SOL_ATTN3D_ERR_INVALID_ARG;
+  sol::KeysDev d{};
+  const int rc = take_context(context, &d);
+  if (rc != SOL_ATTN3D_OK) return rc;
+  if (context->head_dim != p->head_dim) return SOL_ATTN3D_ERR_UNSUPPORTED_SHAPE;
+  return forward_context(p, q, out, d, false, std::min(context->max_len, context->total_rows), 0, workspace, workspace_bytes, stream);
+}
+
+size_t sol_attn3d_cross_step_workspace_bytes(const sol_attn3d_context* context, int batch, int heads) {
+  sol::KeysDev d{};
+  if (take_context(context, &d) != SOL_ATTN3D_OK) return 0;
+  return step_bytes(batch, heads, context->kv_heads, context->head_dim, std::min(context->max_len, context->total_rows));
+}
+
+int sol_attn3d_cross_step(const void* q, const int64_t q_strides[2], const sol_attn3d_context* context, void* out, const int64_t out_strides[2],
+                          int batch, int heads, void* workspace, size_t workspace_bytes, sol_attn3d_stream_t stream) {
+  sol::KeysDev d{};
+  const int rc = take_context(context, &d);
+  if (rc != SOL_ATTN3D_OK) return rc;
+  return step_context(q, q_strides, d, false, out, out_strides, batch, heads, context->head_dim, std::min(context->max_len, context->total_rows),
+                      workspace, workspace_bytes, stream);
+}

@@ -1,0 +1,103 @@
+"""Cross attention to an encoder's states, over a plan and one row per context, against the fp64 oracle."""
+import pytest
+import torch
+
+from oracle import streaming_oracle as so
+from test_gpu_paged import close, rope, size
+
+pytestmark = pytest.mark.gpu
+
+
+def contexts(lens, kv, d, seed, gap=3):
+    """Contexts one after another with rows of NaN between them, in a packed tensor."""
+    g = torch.Generator().manual_seed(seed)
+    begins, rows = [], 0
+    for n in lens:
+        begins.append(rows + gap)
+        rows += n + gap
+    kv_t = torch.full((rows + gap, 2, kv, d), float("nan"), dtype=torch.bfloat16)
+    for b, n in zip(begins, lens):
+        kv_t[b:b + n] = torch.randn(n, 2, kv, d, generator=g).bfloat16()
+    return kv_t, begins
+
+
+def ints(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def run(seqs, q, heads, d, ctx, step=False):
+    from paper_2609_35110_b200 import binding as B
+    out = torch.full((q.shape[0], heads, d), 7.0, dtype=torch.bfloat16, device="cuda")
+    if step:
+        ws = torch.full((B.sol_attn3d_cross_step_workspace_bytes(ctx, q.shape[0], heads),), 255, dtype=torch.uint8, device="cuda")
+        B.sol_attn3d_cross_step(q, ctx, out, workspace=ws)
+        return out.cpu()
+    attn = B.Attn3d(seqs, heads, d, rope(d), q_strides=(q.stride(0), q.stride(1)))
+    ws = torch.full((B.sol_attn3d_cross_workspace_bytes(attn.plan, ctx),), 255, dtype=torch.uint8, device="cuda")
+    B.sol_attn3d_forward_cross(attn.plan, q, ctx, out, workspace=ws)
+    torch.cuda.synchronize()
+    assert attn.status() == 0
+    return out.cpu()
+
+
+@pytest.mark.parametrize("heads,kv,d", [(4, 4, 64), (3, 3, 128), (6, 2, 128), (5, 1, 64), (40, 1, 128)])
+@pytest.mark.parametrize("masked", [False, True])
+def test_plan(heads, kv, d, masked):
+    from paper_2609_35110_b200 import binding as B
+    seqs = [(3, 2, 5, 7), (0, 1, 1, 1), (0, 2, 17, 20), (130, 0, 1, 1), (256, 0, 1, 1)]
+    lens = [77, 512, 129, 0, 1]
+    kv_t, begins = contexts(lens, kv, d, seed=heads)
+    begins[4], lens[4] = begins[0], lens[0]                             # two sequences with one context
+    g = torch.Generator().manual_seed(1)
+    mask = None
+    if masked:
+        mask = (torch.rand(kv_t.shape[0], generator=g) < 0.6).to(torch.uint8)
+        mask[begins[2]:begins[2] + lens[2]] = 0                         # nothing counts
+        kv_t[begins[1]:begins[1] + 512][mask[begins[1]:begins[1] + 512] == 0] = float("inf")
+    dev = kv_t.cuda()
+    ctx = B.sol_attn3d_context(dev[:, 0], dev[:, 1], ints(begins), ints(lens), 512, key_mask=None if mask is None else mask.cuda())
+    q = torch.randn(sum(map(size, seqs)), heads + 1, d, generator=g).bfloat16()
+    out = run(seqs, q.cuda()[:, :heads], heads, d, ctx)
+    at = 0
+    for s, b, n in zip(seqs, begins, lens):
+        m = size(s)
+        ref, mag = so.attend(q[at:at + m, :heads], kv_t[b:b + n, 0], kv_t[b:b + n, 1], so.key_limits(m, n, 0), None if mask is None else mask[b:b + n].bool())
+        close(out[at:at + m], ref, mag)
+        at += m
+
+
+@pytest.mark.parametrize("heads,kv,d", [(4, 4, 64), (6, 2, 128), (33, 1, 64)])
+def test_step(heads, kv, d):
+    from paper_2609_35110_b200 import binding as B
+    lens = [1, 0, 16, 77, 1500, 300]
+    kv_t, begins = contexts(lens, kv, d, seed=2)
+    dev = kv_t.cuda()
+    ctx = B.sol_attn3d_context(dev[:, 0], dev[:, 1], ints(begins), ints(lens), 1500)
+    q = torch.randn(len(lens), heads, d, generator=torch.Generator().manual_seed(3)).bfloat16()
+    out = run(None, q.cuda(), heads, d, ctx, step=True)
+    for i, (b, n) in enumerate(zip(begins, lens)):
+        ref, mag = so.attend(q[i:i + 1], kv_t[b:b + n, 0], kv_t[b:b + n, 1], so.key_limits(1, n, 0))
+        close(out[i:i + 1], ref, mag)
+
+
+def test_ranges_are_clamped():
+    """begins and lens outside the tensor, max_len below a length."""
+    from paper_2609_35110_b200 import binding as B
+    g = torch.Generator().manual_seed(4)
+    k, v = (torch.randn(200, 1, 64, generator=g).bfloat16() for _ in range(2))
+    ctx = B.sol_attn3d_context(k.cuda(), v.cuda(), ints([-4, 150, 500, 0]), ints([150, 1000, 3, -2]), 60)
+    seqs = [(140, 0, 1, 1), (2, 0, 1, 1), (3, 0, 1, 1), (1, 0, 1, 1)]
+    q = torch.randn(146, 2, 64, generator=g).bfloat16()
+    out = run(seqs, q.cuda(), 2, 64, ctx)
+    for a, b, lo, hi in ((0, 140, 0, 150), (140, 142, 150, 200), (142, 145, 0, 0), (145, 146, 0, 0)):
+        ref, mag = so.attend(q[a:b], k[lo:hi], v[lo:hi], so.key_limits(b - a, hi - lo, 0))
+        close(out[a:b], ref, mag)
+
+
+def test_no_states_at_all():
+    from paper_2609_35110_b200 import binding as B
+    empty = torch.empty(0, 2, 64, dtype=torch.bfloat16, device="cuda")
+    ctx = B.sol_attn3d_context(empty, empty, ints([0, 0]), ints([0, 5]), 0)
+    q = torch.randn(300, 2, 64, generator=torch.Generator().manual_seed(4)).bfloat16().cuda()
+    assert bool((run([(299, 0, 1, 1), (1, 0, 1, 1)], q, 2, 64, ctx) == 0).all())
+    assert bool((run(None, q[:2], 2, 64, ctx, step=True) == 0).all())
