@@ -1,0 +1,623 @@
+// Attention of many query rows over keys and values that live in the pages of a cache or in an encoder's states: tcgen05 tensor
+// cores, accumulators in tensor memory, online softmax in registers.  The two query tiles of a CTA ping-pong as in
+// attn_fwd_sm100.cuh; what differs is what surrounds them.
+//
+// A tile is 128 (token, head) rows of one K/V head: 128 / group tokens x the group's heads, head fastest, which one TMA box brings
+// side by side; so grouped heads share every K and V tile.  A unit is two such tiles, one K/V head and a range of key tiles (all of
+// them, or a part when there are few units; the parts are joined by join_rows_kernel).
+//
+// CTAs are persistent, one per SM, and take units from a counter, so that short contexts do not pay for a CTA's start (tensor
+// memory, barriers, the first loads) and its last stores per unit, and streams of different length even out.  A warp looks the
+// next unit up while the present one is computed: its Q, K and V are on their way, and its first scores are computed, while the
+// softmax warps still write the last one's rows.
+//   warps 0-3, 4-7  softmax and epilogue of tile 0, tile 1 (thread = row)
+//   warp 8          loads: Q by one box per tile half; K and V pages by one box per page part, a lane each
+//   warp 9          tcgen05.mma issuer
+//   warp 10         takes units
+//   warp 11         values of keys that do not count become zeros in shared memory (0 * NaN would not be 0)
+// Tensor memory: S0 | S1 | O0 | O1 as in attn_fwd_sm100.cuh.
+#pragma once
+#include "attn_fwd_sm100.cuh"
+#include "context_attn.cuh"
+
+namespace sol {
+
+struct UnitDev {
+  Span span;
+  long long tok0;               // first token of the sequence in the packed tensors
+  long long part;               // index of this unit's partial rows
+  int t0, n_tok;                // first new token of the unit; new tokens of the sequence
+  int kv_head;
+  int tile_begin, tile_end;     // key tiles
+  int n_tiles;                  // query tiles: 1 or 2
+  int lim[2];                   // keys below lim[t] count for every row of tile t
+  int last;                     // no more units
+};
+
+struct ContextParams {
+  QueriesDev a;
+  KeysDev d;
+  long long units;              // row units per K/V head
+  long long total;              // units * kv_heads * n_split
+  int n_split;
+  int tok_per_tile;             // 128 / group
+  int box_rows;                 // tokens of a K/V box: a power of two that divides the page size, at most 128
+  float* partial;               // [unit][kv_head][split][2 * tok_per_tile * group][D + 4], or nullptr: one split
+  unsigned int* counter;        // next unit; 0 between launches
+  unsigned int* status;
+  unsigned int* rescales;
+  unsigned long long wait_limit_ns;
+  unsigned int fault_inject;    // 1: the first unit withholds "scores of tile 1 (or the only one) are there"
+  unsigned int v_lbo, v_sbo;
+};
+
+template <int D>
+struct ContextSmem {
+  static constexpr int kTile = 128 * D * 2;
+  static constexpr int kHalves = D / 64;
+  static constexpr int kHalfBytes = 128 * 128;
+  static constexpr int kStages = D == 128 ? 4 : 10;       // K and V tiles alternate
+  static constexpr int kVRing = 8;                        // "V is clean" barriers: more than V tiles fit the ring
+  static constexpr int kOffQ = 0;
+  static constexpr int kOffKV = 2 * kTile;
+  static constexpr int kOffStage = kOffKV + kStages * kTile;   // 4 KB per softmax warp
+  static constexpr int kOffBars = kOffStage + 8 * 4096;
+  static constexpr int kNumBars = 2 * kStages + 4 + 6 + 4 + kVRing + 1;
+  static constexpr int kOffTmemPtr = kOffBars + kNumBars * 8;
+  static constexpr int kOffUnits = (kOffTmemPtr + 16 + 15) / 16 * 16;
+  static constexpr int kBytes = kOffUnits + 2 * (int)sizeof(UnitDev);
+  static constexpr int kDynBytes = kBytes + 1024;
+};
+
+// Validity of 32 keys from `first` on: those below `limit`.
+__device__ __forceinline__ uint32_t below(int limit, int first) {
+  const int n = limit - first;
+  return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u;
+}
+
+template <int D, bool kPaged>
+__global__ void __launch_bounds__(kAttnThreads, 1)
+context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
+                    const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ ContextParams p) {
+  using L = ContextSmem<D>;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw_addr = smem_u32(smem_raw);
+  const uint32_t sbase = (raw_addr + 1023u) & ~1023u;
+  uint8_t* smem = smem_raw + (sbase - raw_addr);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  const uint32_t sQ = sbase + L::kOffQ, sKV = sbase + L::kOffKV, bars = sbase + L::kOffBars;
+  auto bar_kv_full = [&](int s) { return bars + 8u * s; };
+  auto bar_kv_empty = [&](int s) { return bars + 8u * (L::kStages + s); };
+  constexpr int kB = 2 * L::kStages;
+  auto bar_q_full = [&](int t) { return bars + 8u * (kB + t); };
+  auto bar_q_empty = [&](int t) { return bars + 8u * (kB + 2 + t); };
+  auto bar_s_full = [&](int t) { return bars + 8u * (kB + 4 + t); };
+  auto bar_p_full = [&](int t) { return bars + 8u * (kB + 6 + t); };
+  auto bar_o_done = [&](int t) { return bars + 8u * (kB + 8 + t); };
+  auto bar_u_full = [&](int s) { return bars + 8u * (kB + 10 + s); };
+  auto bar_u_empty = [&](int s) { return bars + 8u * (kB + 12 + s); };
+  auto bar_v_clean = [&](uint32_t n) { return bars + 8u * (kB + 14 + (n & (L::kVRing - 1))); };
+  const uint32_t bar_drain = bars + 8u * (kB + 14 + L::kVRing);
+  volatile uint32_t* tmem_ptr_smem = reinterpret_cast<volatile uint32_t*>(smem + L::kOffTmemPtr);
+  UnitDev* units = reinterpret_cast<UnitDev*>(smem + L::kOffUnits);
+  const unsigned long long limit = p.wait_limit_ns;
+
+  if (warp == 8 && lane == 0) {
+    for (int s = 0; s < L::kStages; ++s) { mbar_init(bar_kv_full(s), 1); mbar_init(bar_kv_empty(s), 1); }
+    for (int t = 0; t < 2; ++t) {
+      mbar_init(bar_q_full(t), 1);
+      mbar_init(bar_q_empty(t), 1);
+      mbar_init(bar_s_full(t), 1);
+      mbar_init(bar_p_full(t), 4);
+      mbar_init(bar_o_done(t), 1);
+      mbar_init(bar_u_full(t), 1);
+      mbar_init(bar_u_empty(t), 11);                       // eight softmax warps, loads, issuer, cleaner
+    }
+    for (int n = 0; n < L::kVRing; ++n) mbar_init(bar_v_clean(n), 1);
+    mbar_init(bar_drain, 1);
+    fence_mbar_init();
+    prefetch_tensormap(&tm_q);
+    prefetch_tensormap(&tm_k);
+    prefetch_tensormap(&tm_v);
+  }
+  if (threadIdx.x == 0) tmem_ptr_smem[1] = *reinterpret_cast<volatile unsigned int*>(p.status);
+  if (warp == 9) {
+    tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_ptr_smem)), 512);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = tmem_ptr_smem[0];
+  if (tmem_ptr_smem[1] != 0) {                             // a fault was recorded earlier: nothing starts any more
+    if (warp == 9) tmem_dealloc(tmem_base, 512);
+    return;
+  }
+  // A role that is not part of a unit, or far ahead, waits for as long as the unit takes: it gives up once a wait somewhere else
+  // has run out, or after 64 limits.
+  auto wait_long = [&](uint32_t bar, uint32_t parity) {
+    for (int n = 0; n < 64; ++n) {
+      if (mbar_wait_warp(bar, parity, limit)) return true;
+      if (*reinterpret_cast<volatile unsigned int*>(p.status) != 0) return false;
+    }
+    return false;
+  };
+  auto release_unit = [&](uint32_t u) {
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar_u_empty(u & 1));
+  };
+
+  if (warp < 8) {
+    // =========================================================== softmax / epilogue
+    setmaxnreg_inc<SOL_REGS_SOFTMAX>();
+    const int t = warp >> 2, wq = warp & 3, row = wq * 32 + lane;
+    const uint32_t lane_off = static_cast<uint32_t>(wq * 32) << 16;
+    const uint32_t tS = tmem_base + lane_off + t * 128;
+    const uint32_t tO = tmem_base + lane_off + 256 + t * D;
+    const float c = p.a.scale_log2;
+    const int group = p.a.group;
+    const int tile_rows = p.tok_per_tile * group;
+    uint32_t n_s = 0;                                      // key tiles of this query tile so far
+    bool ok = true;
+    for (uint32_t u = 0;; ++u) {
+      if (!wait_long(bar_u_full(u & 1), (u >> 1) & 1)) { ok = false; break; }
+      const UnitDev& un = units[u & 1];
+      if (un.last) break;
+      if (t >= un.n_tiles) { release_unit(u); continue; }
+      const int tile_begin = un.tile_begin, tile_end = un.tile_end, lim_all = un.lim[t];
+      const uint8_t* mask = un.span.mask;
+      const int cap = un.span.cap;
+      const int tok = un.t0 + t * p.tok_per_tile + row / group;       // this thread's new token
+      const bool mine = row < tile_rows && tok < un.n_tok;
+      const int lim = mine ? key_limit(un.span, un.n_tok, tok, p.a.causal) : 0x7fffffff;
+      float m_ref = -CUDART_INF_F, l = 0.f;
+      bool seen = false, started = false;                  // started: every row of the warp has its reference
+      uint32_t next_mask = 0;                              // mask bytes of the next key tile: keys lane, + 32, + 64, + 96
+      auto fetch_mask = [&](int jt) {
+        uint32_t w = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int key = jt * 128 + e * 32 + lane;
+          if (key < cap && __ldg(mask + key) != 0) w |= 1u << e;
+        }
+        return w;
+      };
+      if (mask != nullptr && tile_begin < tile_end) next_mask = fetch_mask(tile_begin);
+
+      for (int jt = tile_begin; jt < tile_end; ++jt, ++n_s) {
+        const uint32_t mask_bits = next_mask;
+        if (mask != nullptr && jt + 1 < tile_end) next_mask = fetch_mask(jt + 1);
+        ok = mbar_wait_warp(bar_s_full(t), n_s & 1, limit);
+        if (!ok) break;
+        tc_fence_after();
+        const bool whole = mask == nullptr && (jt + 1) * 128 <= lim_all;
+        uint32_t r[128];
+        uint32_t pk[64];
+        float tile_sum;
+        bool first_half_stored = false;
+        if (whole && started) {
+          // Common case, in two halves: the second half of S is still on its way while the first is exponentiated, and the
+          // first half of P is on its way to tensor memory while the second is.
+          uint32_t (&r_lo)[64] = *reinterpret_cast<uint32_t(*)[64]>(&r[0]);
+          uint32_t (&r_hi)[64] = *reinterpret_cast<uint32_t(*)[64]>(&r[64]);
+          tmem_ld32(tS, *reinterpret_cast<uint32_t(*)[32]>(&r[0]));
+          tmem_ld32(tS + 32, *reinterpret_cast<uint32_t(*)[32]>(&r[32]));
+          tmem_wait_ld_dep64(r_lo);
+          tmem_ld32(tS + 64, *reinterpret_cast<uint32_t(*)[32]>(&r[64]));
+          tmem_ld32(tS + 96, *reinterpret_cast<uint32_t(*)[32]>(&r[96]));
+          float acc[4] = {0.f, 0.f, 0.f, 0.f};
+          const float mc = m_ref * c;
+          softmax_half(r_lo, c, mc, *reinterpret_cast<uint32_t(*)[32]>(&pk[0]), acc);
+          tmem_wait_ld_dep64(r_hi);
+          tmem_st32(tS, *reinterpret_cast<uint32_t(*)[32]>(&pk[0]));       // columns [0,32): their scores are in registers
+          first_half_stored = true;
+          softmax_half(r_hi, c, mc, *reinterpret_cast<uint32_t(*)[32]>(&pk[32]), acc);
+          tile_sum = (acc[0] + acc[1]) + (acc[2] + acc[3]);
+          seen = true;
+        } else {
+#pragma unroll
+          for (int cch = 0; cch < 4; ++cch) tmem_ld32(tS + cch * 32, *reinterpret_cast<uint32_t(*)[32]>(&r[cch * 32]));
+          tmem_wait_ld();
+          if (!whole) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              uint32_t valid = below(lim, jt * 128 + e * 32);
+              if (mask != nullptr) valid &= __ballot_sync(0xffffffffu, (mask_bits >> e) & 1u);
+              seen = seen || valid != 0;
+#pragma unroll
+              for (int cc = 0; cc < 32; ++cc)
+                if (((valid >> cc) & 1u) == 0) r[e * 32 + cc] = __float_as_uint(-CUDART_INF_F);
+            }
+          } else {
+            seen = true;
+          }
+          // a row takes its reference from its first tile with a valid key; before that every term is 2^-inf
+          if (m_ref == -CUDART_INF_F) m_ref = row_max128(r);
+          softmax_pass(r, c, m_ref == -CUDART_INF_F ? 0.f : m_ref * c, pk, tile_sum);
+          started = __all_sync(0xffffffffu, !mine || m_ref != -CUDART_INF_F);
+        }
+        // No row maximum was taken.  All terms are positive, so a sum <= 2^8 proves that every term is; otherwise, if the maximum
+        // has grown by more than 2^8, the reference moves and the tile is redone before its P is released.
+        if (__any_sync(0xffffffffu, mine && !(tile_sum <= 256.0f))) {
+          const float mx = row_max128(r);
+          const bool grow = mine && (mx - m_ref) * c > 8.0f;
+          if (__any_sync(0xffffffffu, grow)) {
+            if (lane == 0) atomicAdd(p.rescales, 1u);
+            const float f = grow ? ex2_approx((m_ref - mx) * c) : 1.0f;
+            if (grow) m_ref = mx;
+            l *= f;
+            if (jt > tile_begin) {
+              ok = mbar_wait_warp(bar_o_done(t), (n_s - 1) & 1, limit);
+              if (!ok) break;
+              tc_fence_after();
+#pragma unroll
+              for (int cch = 0; cch < D / 32; ++cch) {
+                uint32_t o[32];
+                tmem_ld32(tO + cch * 32, o);
+                tmem_wait_ld();
+#pragma unroll
+                for (int cc = 0; cc < 32; ++cc) o[cc] = __float_as_uint(__uint_as_float(o[cc]) * f);
+                tmem_st32(tO + cch * 32, o);
+              }
+            }
+            softmax_pass(r, c, m_ref == -CUDART_INF_F ? 0.f : m_ref * c, pk, tile_sum);
+            if (first_half_stored) tmem_wait_st();                       // the stale first half lands before its replacement
+            first_half_stored = false;
+          }
+        }
+        l += tile_sum;
+        if (!first_half_stored) tmem_st32(tS, *reinterpret_cast<uint32_t(*)[32]>(&pk[0]));
+        tmem_st32(tS + 32, *reinterpret_cast<uint32_t(*)[32]>(&pk[32]));
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar_p_full(t));
+      }
+      if (!ok) break;
+
+      // ---- epilogue
+      if (tile_begin < tile_end) {
+        ok = mbar_wait_warp(bar_o_done(t), (n_s - 1) & 1, limit);
+        if (!ok) break;
+        tc_fence_after();
+      }
+      if (p.partial != nullptr) {
+        float* dst = p.partial + (un.part * 2 * tile_rows + t * tile_rows + row) * (D + 4);
+#pragma unroll 1
+        for (int cch = 0; cch < D / 32; ++cch) {
+          uint32_t o[32];
+          if (tile_begin < tile_end) {
+            tmem_ld32(tO + cch * 32, o);
+            tmem_wait_ld();
+          } else {
+#pragma unroll
+            for (int cc = 0; cc < 32; ++cc) o[cc] = 0u;
+          }
+          if (mine) {
+#pragma unroll
+            for (int cc = 0; cc < 32; cc += 4) *reinterpret_cast<uint4*>(dst + cch * 32 + cc) = make_uint4(o[cc], o[cc + 1], o[cc + 2], o[cc + 3]);
+          }
+        }
+        if (mine) *reinterpret_cast<float4*>(dst + D) = make_float4(m_ref, l, seen ? 1.f : 0.f, 0.f);
+      } else {
+        // Rows are staged 64 columns at a time (16-byte chunks XOR-swizzled by row) and written with eight lanes per row.
+        const float inv = 1.0f / l;
+        uint8_t* stage = smem + L::kOffStage + warp * 4096;
+#pragma unroll 1
+        for (int hf = 0; hf < L::kHalves; ++hf) {
+          __syncwarp();
+#pragma unroll
+          for (int part = 0; part < 2; ++part) {
+            uint32_t o[32];
+            if (tile_begin < tile_end) {
+              tmem_ld32(tO + hf * 64 + part * 32, o);
+              tmem_wait_ld();
+            }
+#pragma unroll
+            for (int v4 = 0; v4 < 4; ++v4) {
+              uint4 w = make_uint4(0u, 0u, 0u, 0u);        // a row without a valid key is zeros
+              if (seen) {
+                w.x = pack_bf16x2(__uint_as_float(o[8 * v4 + 0]) * inv, __uint_as_float(o[8 * v4 + 1]) * inv);
+                w.y = pack_bf16x2(__uint_as_float(o[8 * v4 + 2]) * inv, __uint_as_float(o[8 * v4 + 3]) * inv);
+                w.z = pack_bf16x2(__uint_as_float(o[8 * v4 + 4]) * inv, __uint_as_float(o[8 * v4 + 5]) * inv);
+                w.w = pack_bf16x2(__uint_as_float(o[8 * v4 + 6]) * inv, __uint_as_float(o[8 * v4 + 7]) * inv);
+              }
+              *reinterpret_cast<uint4*>(stage + lane * 128 + (((part * 4 + v4) ^ (lane & 7)) << 4)) = w;
+            }
+          }
+          __syncwarp();
+          const uint64_t pol_once = l2_policy_evict_first();
+#pragma unroll
+          for (int r0 = 0; r0 < 32; r0 += 4) {
+            const int rr = r0 + (lane >> 3), ch = lane & 7;
+            const int tile_row = wq * 32 + rr;
+            const int tk = un.t0 + t * p.tok_per_tile + tile_row / group;
+            const uint4 w = *reinterpret_cast<const uint4*>(stage + rr * 128 + ((ch ^ (rr & 7)) << 4));
+            if (tile_row < tile_rows && tk < un.n_tok)
+              st_global_evict_first(p.a.out + (un.tok0 + tk) * p.a.o_tok + ((long long)un.kv_head * group + tile_row % group) * p.a.o_head +
+                                        hf * 64 + ch * 8, w, pol_once);
+          }
+        }
+      }
+      release_unit(u);
+    }
+    if (!ok && lane == 0) atomicCAS(p.status, 0u, kStatusTimeoutSoftmax);
+  } else {
+    setmaxnreg_dec<SOL_REGS_OTHER>();
+  }
+
+  if (warp == 8) {
+    // =========================================================== loads
+    const uint64_t pol_once = l2_policy_evict_first();
+    const uint32_t q_bytes = (uint32_t)(p.tok_per_tile * p.a.group * 128 * L::kHalves);
+    uint32_t it = 0, n_q[2] = {0, 0};
+    bool ok = true;
+    for (uint32_t u = 0;; ++u) {
+      if (!wait_long(bar_u_full(u & 1), (u >> 1) & 1)) { ok = false; break; }
+      const UnitDev& un = units[u & 1];
+      if (un.last) break;
+      const int tile_begin = un.tile_begin, tile_end = un.tile_end, kv_head = un.kv_head, n = un.span.cap;
+      const int* table = un.span.table;
+      const long long begin = un.span.begin;
+      if (tile_begin < tile_end) {
+        for (int t = 0; t < un.n_tiles && ok; ++t) {
+          ok = mbar_wait_warp(bar_q_empty(t), (n_q[t] & 1) ^ 1u, limit);
+          if (!ok) break;
+          ++n_q[t];
+          if (lane == 0) {
+            mbar_arrive_expect_tx(bar_q_full(t), q_bytes);
+#pragma unroll
+            for (int hf = 0; hf < L::kHalves; ++hf)
+              tma_load_3d_hint(sQ + t * L::kTile + hf * L::kHalfBytes, &tm_q, bar_q_full(t), hf * 64, kv_head * p.a.group,
+                               (int)un.tok0 + un.t0 + t * p.tok_per_tile, pol_once);
+          }
+          __syncwarp();
+        }
+        // a lane's page of a key tile; tokens beyond the keys, and entries that name no page, load zeros (a coordinate past the end)
+        auto page_of = [&](int jt) {
+          const int key = jt * 128 + lane * p.box_rows;
+          if (lane * p.box_rows >= 128 || key >= n) return (int)p.d.c.n_pages;
+          const int page = __ldg(table + key / p.d.c.page);
+          return page >= 0 && page < p.d.c.n_pages ? page : (int)p.d.c.n_pages;
+        };
+        int next_page = 0;
+        if (kPaged && ok) next_page = page_of(tile_begin);
+        for (int jt = tile_begin; jt < tile_end && ok; ++jt) {
+          const int page = next_page;
+          if (kPaged && jt + 1 < tile_end) next_page = page_of(jt + 1);
+#pragma unroll
+          for (int kv = 0; kv < 2; ++kv) {
+            const uint32_t stage = it % L::kStages;
+            ok = mbar_wait_warp(bar_kv_empty(stage), ((it / L::kStages) & 1) ^ 1u, limit);
+            if (!ok) break;
+            const uint32_t dst = sKV + stage * L::kTile;
+            const CUtensorMap* tm = kv ? &tm_v : &tm_k;
+            if (lane == 0) mbar_arrive_expect_tx(bar_kv_full(stage), L::kTile);
+            __syncwarp();
+            if (kPaged) {
+              if (lane * p.box_rows < 128) {
+                const int in_page = (jt * 128 + lane * p.box_rows) % p.d.c.page;
+#pragma unroll
+                for (int hf = 0; hf < L::kHalves; ++hf)
+                  tma_load_4d(dst + hf * L::kHalfBytes + lane * p.box_rows * 128, tm, bar_kv_full(stage), hf * 64, kv_head, in_page, page);
+              }
+            } else if (lane == 0) {
+#pragma unroll
+              for (int hf = 0; hf < L::kHalves; ++hf)
+                tma_load_3d(dst + hf * L::kHalfBytes, tm, bar_kv_full(stage), hf * 64, kv_head, (int)(begin + jt * 128));
+            }
+            __syncwarp();
+            ++it;
+          }
+        }
+      }
+      if (!ok) break;
+      release_unit(u);
+    }
+    if (!ok) {
+      if (lane == 0) atomicCAS(p.status, 0u, kStatusTimeoutProducer);
+      // copies in flight land before the shared memory is given back
+      for (int t = 0; t < 2; ++t)
+        if (n_q[t] > 0) mbar_wait_warp(bar_q_full(t), (n_q[t] - 1) & 1, limit);
+      const uint32_t first = it > (uint32_t)L::kStages ? it - L::kStages : 0u;
+      for (uint32_t j = first; j < it; ++j) mbar_wait_warp(bar_kv_full(j % L::kStages), (j / L::kStages) & 1u, limit);
+    }
+  } else if (warp == 9) {
+    // =========================================================== MMA issuer (the warp runs convergently, one elected lane issues)
+    constexpr uint32_t idesc_qk = idesc_bf16_f32(128, 128, false);
+    constexpr uint32_t idesc_pv = idesc_bf16_f32(128, D, true);
+    const uint32_t hi_k = smem_desc_hi_sw128(1024), hi_v = smem_desc_hi_sw128(p.v_sbo);
+    const uint32_t q_lo0 = smem_desc_lo(sQ, 16), q_lo1 = smem_desc_lo(sQ + L::kTile, 16);
+    const uint32_t k_lo_base = smem_desc_lo(sKV, 16), v_lo_base = smem_desc_lo(sKV, p.v_lbo);
+    constexpr uint32_t kStageStep = L::kTile >> 4;
+    const uint32_t tS0 = tmem_base, tS1 = tmem_base + 128, tO0 = tmem_base + 256, tO1 = tmem_base + 256 + D;
+    auto issue_qk = [&](uint32_t d_tmem, uint32_t q_lo, uint32_t stage) {
+      const uint32_t k_lo = k_lo_base + stage * kStageStep;
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k) {
+        const uint32_t off = ((k >> 2) * L::kHalfBytes + (k & 3) * 32) >> 4;
+        if (k == 0) mma_ss_elect<false>(d_tmem, q_lo + off, k_lo + off, hi_k, idesc_qk, 0u);
+        else        mma_ss_elect<true>(d_tmem, q_lo + off, k_lo + off, hi_k, idesc_qk, 1u);
+      }
+    };
+    auto issue_pv = [&](uint32_t d_tmem, uint32_t p_tmem, uint32_t stage, bool acc) {
+      const uint32_t v_lo = v_lo_base + stage * kStageStep;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        if (k == 0) mma_ts_elect<false>(d_tmem, p_tmem, v_lo, hi_v, idesc_pv, acc ? 1u : 0u);
+        else        mma_ts_elect<true>(d_tmem, p_tmem + k * 8, v_lo + k * (2048 >> 4), hi_v, idesc_pv, 1u);
+      }
+    };
+    uint32_t it = 0, n_v = 0, n_q[2] = {0, 0}, n_p[2] = {0, 0};
+    bool ok = true;
+    auto wait = [&](uint32_t bar, uint32_t parity) {
+      if (!mbar_wait_warp(bar, parity, limit)) { ok = false; return false; }
+      tc_fence_after();
+      return true;
+    };
+    auto stage_of = [&](uint32_t n) { return n % L::kStages; };
+    auto full = [&](uint32_t n) { return wait(bar_kv_full(n % L::kStages), (n / L::kStages) & 1); };
+    for (uint32_t u = 0; ok; ++u) {
+      if (!wait_long(bar_u_full(u & 1), (u >> 1) & 1)) { ok = false; break; }
+      const UnitDev& un = units[u & 1];
+      if (un.last) break;
+      const int n_proc = un.tile_end - un.tile_begin;
+      const bool two = un.n_tiles == 2;
+      release_unit(u);
+      if (n_proc <= 0) continue;
+      // (test hook: the first unit withholds a signal, so that the waits downstream run into their limit)
+      const bool withhold = p.fault_inject == 1u && blockIdx.x == 0 && u == 0;
+      uint32_t k_it = it;
+      if (!wait(bar_q_full(0), n_q[0] & 1) || !full(k_it)) break;
+      ++n_q[0];
+      issue_qk(tS0, q_lo0, stage_of(k_it));
+      if (two || !withhold) tc_commit_elect(bar_s_full(0));
+      if (n_proc == 1) tc_commit_elect(bar_q_empty(0));
+      if (two) {
+        if (!wait(bar_q_full(1), n_q[1] & 1)) break;
+        ++n_q[1];
+        issue_qk(tS1, q_lo1, stage_of(k_it));
+        if (!withhold) tc_commit_elect(bar_s_full(1));
+        if (n_proc == 1) tc_commit_elect(bar_q_empty(1));
+      }
+      tc_commit_elect(bar_kv_empty(stage_of(k_it)));
+      for (int i = 0; i < n_proc; ++i) {
+        const uint32_t v_it = it + 1, next = it + 2;
+        const bool more = i + 1 < n_proc, last_k = i + 2 == n_proc;
+        it += 2;
+        if (!full(v_it) || !wait(bar_v_clean(n_v), (n_v / L::kVRing) & 1)) break;
+        ++n_v;
+        if (!wait(bar_p_full(0), n_p[0] & 1)) break;
+        ++n_p[0];
+        issue_pv(tO0, tS0, stage_of(v_it), i > 0);
+        tc_commit_elect(bar_o_done(0));
+        if (more) {
+          if (!full(next)) break;
+          issue_qk(tS0, q_lo0, stage_of(next));
+          tc_commit_elect(bar_s_full(0));
+          if (last_k) tc_commit_elect(bar_q_empty(0));
+        }
+        if (two) {
+          if (!wait(bar_p_full(1), n_p[1] & 1)) break;
+          ++n_p[1];
+          issue_pv(tO1, tS1, stage_of(v_it), i > 0);
+          tc_commit_elect(bar_o_done(1));
+        }
+        tc_commit_elect(bar_kv_empty(stage_of(v_it)));
+        if (more) {
+          if (two) {
+            issue_qk(tS1, q_lo1, stage_of(next));
+            tc_commit_elect(bar_s_full(1));
+            if (last_k) tc_commit_elect(bar_q_empty(1));
+          }
+          tc_commit_elect(bar_kv_empty(stage_of(next)));
+        }
+      }
+    }
+    if (!ok) {
+      if (lane == 0) atomicCAS(p.status, 0u, kStatusTimeoutMma);
+      tc_commit_elect(bar_drain);                          // products in flight end before tensor memory is released
+      mbar_wait_warp(bar_drain, 0, limit);
+    }
+  } else if (warp == 10) {
+    // =========================================================== takes units
+    bool ok = true;
+    const int rows = 2 * p.tok_per_tile * p.a.group;
+    for (uint32_t u = 0;; ++u) {
+      if (u >= 2 && !wait_long(bar_u_empty(u & 1), ((u >> 1) & 1) ^ 1u)) { ok = false; break; }
+      int last = 0;
+      if (lane == 0) {
+        UnitDev un{};
+        for (;;) {
+          const unsigned int at = atomicAdd(p.counter, 1u);
+          if (at >= p.total) {
+            // every CTA draws one number past the units; the one that draws the last of them leaves the counter as it was found
+            if (at == p.total + gridDim.x - 1) *p.counter = 0u;
+            un.last = 1;
+            break;
+          }
+          const long long unit = at % p.units;
+          const long long rest = at / p.units;
+          const int split = (int)(rest % p.n_split);
+          un.kv_head = (int)(rest / p.n_split);
+          un.part = (unit * p.d.c.kv_heads + un.kv_head) * p.n_split + split;
+          long long first;
+          const SeqDev& sq = p.a.seqs[find_sequence(p.a, unit, rows, &first)];
+          const long long t0 = (unit - first) * 2 * p.tok_per_tile;
+          if (t0 >= sq.n_tokens) continue;
+          un.span = find_span<kPaged>(p.d, sq.seq_id);
+          if (un.span.idle) continue;
+          un.t0 = (int)t0;
+          un.n_tok = sq.n_tokens;
+          un.tok0 = sq.tok_start;
+          un.n_tiles = un.n_tok - un.t0 > p.tok_per_tile ? 2 : 1;
+          un.lim[0] = key_limit(un.span, un.n_tok, un.t0, p.a.causal);
+          un.lim[1] = key_limit(un.span, un.n_tok, un.t0 + p.tok_per_tile, p.a.causal);
+          const int most = key_limit(un.span, un.n_tok, min(un.n_tok, un.t0 + 2 * p.tok_per_tile) - 1, p.a.causal);
+          const int tiles = (most + 127) >> 7, per = (tiles + p.n_split - 1) / p.n_split;
+          un.tile_begin = min(tiles, split * per);
+          un.tile_end = min(tiles, un.tile_begin + per);
+          break;
+        }
+        units[u & 1] = un;
+        last = un.last;
+        mbar_arrive(bar_u_full(u & 1));
+      }
+      if (__shfl_sync(0xffffffffu, last, 0)) break;
+    }
+    if (!ok && lane == 0) atomicCAS(p.status, 0u, kStatusTimeoutProducer);
+  } else if (warp == 11) {
+    // =========================================================== values of keys that do not count
+    uint32_t it = 0, n_v = 0;
+    bool ok = true;
+    for (uint32_t u = 0; ok; ++u) {
+      if (!wait_long(bar_u_full(u & 1), (u >> 1) & 1)) { ok = false; break; }
+      const UnitDev& un = units[u & 1];
+      if (un.last) break;
+      const int tile_begin = un.tile_begin, tile_end = un.tile_end, cap = un.span.cap;
+      const uint8_t* mask = un.span.mask;
+      release_unit(u);
+      for (int jt = tile_begin; jt < tile_end; ++jt) {
+        const uint32_t v_it = it + 1, stage = v_it % L::kStages;
+        it += 2;
+        uint32_t drop = 0;                                 // bit e: key 32 e + lane of the tile does not count
+        if (mask != nullptr || (jt + 1) * 128 > cap) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int key = jt * 128 + e * 32 + lane;
+            if (key >= cap || (mask != nullptr && __ldg(mask + key) == 0)) drop |= 1u << e;
+          }
+        }
+        if (!mbar_wait_warp(bar_kv_full(stage), (v_it / L::kStages) & 1, limit)) { ok = false; break; }
+        if (__any_sync(0xffffffffu, drop != 0)) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if ((drop >> e) & 1u) {
+              uint8_t* at = smem + L::kOffKV + stage * L::kTile + (e * 32 + lane) * 128;
+#pragma unroll
+              for (int hf = 0; hf < L::kHalves; ++hf)
+#pragma unroll
+                for (int ch = 0; ch < 8; ++ch)             // (lanes start at different chunks: different banks)
+                  *reinterpret_cast<uint4*>(at + hf * L::kHalfBytes + (((ch + lane) & 7) << 4)) = make_uint4(0u, 0u, 0u, 0u);
+            }
+          fence_proxy_async_smem();
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar_v_clean(n_v));
+        ++n_v;
+      }
+    }
+    if (!ok && lane == 0) atomicCAS(p.status, 0u, kStatusTimeoutProducer);
+  }
+
+  // ---- everyone is done with tensor memory and shared memory before they are released
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 9) {
+    tc_fence_after();
+    tmem_dealloc(tmem_base, 512);
+  }
+}
+
+}  // namespace sol

@@ -16,6 +16,7 @@
 #include "attn_fwd_sm100.cuh"
 #include "cache_kernels.cuh"
 #include "context_attn.cuh"
+#include "context_attn_sm100.cuh"
 #include "device_types.cuh"
 #include "linear_attn_sm100.cuh"
 #include "prologue_kernels.cuh"

@@ -126,16 +126,145 @@ int attend_few(sol::QueriesDev a, const sol::KeysDev& d, bool paged, int head_di
 }
 
 // ---- attention over a plan's sequences ---------------------------------------------------------------------------------------
-size_t context_bytes(sol_attn3d_plan_t p, int kv_heads, long long capacity) {
+constexpr size_t kUnitCounterOffset = 128;   // next unit of context_attn_kernel inside the 256-byte status block of a workspace
+
+// How a plan's rows are served for `kv_heads` K/V heads and pasts of up to `capacity` keys.  Few rows per K/V head (one unit of
+// few_rows_kernel in every sequence) go to that kernel; more to the tensor-core kernel, whose tile is 128 rows high.
+struct ContextRoute {
+  bool few;
+  int group, tok_per_tile, n_split;
+  long long units;              // per K/V head
+};
+ContextRoute choose_route(sol_attn3d_plan_t p, int kv_heads, long long capacity, long long total_rows) {
+  ContextRoute r{};
+  r.group = p->heads / kv_heads;
+  const long long longest = p->sched.front().n_tokens;
+  r.few = longest * r.group <= sol::kFewRows || r.group > 128 || total_rows == 0;
+  if (r.few) {
+    r.units = few_units(p, 0, r.group);
+    r.n_split = few_splits(r.units * kv_heads, capacity);
+    return r;
+  }
+  r.tok_per_tile = 128 / r.group;
+  const int per_unit = 2 * r.tok_per_tile;
+  r.units = p->total_tokens / per_unit + p->n_seqs;
+  // Splits of the keys, where the units do not fill the SMs: the number that costs least when the units are dealt to 148 SMs in
+  // waves.  The cost of a unit is its key tiles (about 1.9 us each) and some 2 tiles' time for its start and end; joining costs a
+  // launch and the partial rows' way through memory.
+  long long busy = 0;
+  for (const SeqDev& q : p->sched) busy += (q.n_tokens + per_unit - 1) / per_unit;
+  busy *= kv_heads;
+  const long long tiles = (capacity + 127) / 128;
+  r.n_split = 1;
+  double best = 0.0;
+  for (int n = 1; n <= std::max<long long>(1, std::min<long long>(64, tiles / 2)); ++n) {
+    const double waves = (double)((busy * n + 147) / 148);
+    const double cost = waves * ((tiles + n - 1) / n + 2.0) + (n > 1 ? 2.0 + 0.01 * busy * n : 0.0);
+    if (n == 1 || cost < 0.95 * best) {
+      best = cost;
+      r.n_split = n;
+    }
+  }
+  return r;
+}
+
+size_t context_bytes(sol_attn3d_plan_t p, int kv_heads, long long capacity, long long total_rows) {
   if (p == nullptr || p->heads % kv_heads != 0) return 0;
-  const int group = p->heads / kv_heads;
-  return few_bytes(few_units(p, 0, group), kv_heads, p->head_dim, capacity);
+  const ContextRoute r = choose_route(p, kv_heads, capacity, total_rows);
+  if (r.few) return few_bytes(r.units, kv_heads, p->head_dim, capacity);
+  return r.n_split == 1 ? 0 : align_up((size_t)r.units * kv_heads * r.n_split * 2 * r.tok_per_tile * r.group * (p->head_dim + 4) * sizeof(float));
+}
+
+// Any tensor as a tiled map of bf16 boxes 64 elements wide, 128-byte swizzle; strides of the outer dimensions in elements.
+int encode_boxes(sol_attn3d_plan_t p, CUtensorMap* tm, const void* base, int rank, const long long* dims, const long long* strides, const int* box) {
+  cuuint64_t d[4], s[3];
+  cuuint32_t b[4];
+  const cuuint32_t estr[4] = {1, 1, 1, 1};
+  for (int i = 0; i < rank; ++i) {
+    d[i] = (cuuint64_t)dims[i];
+    b[i] = (cuuint32_t)box[i];
+    if (i > 0) s[i - 1] = (cuuint64_t)strides[i - 1] * 2;
+  }
+  const CUresult r = p->encode(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void*>(base), d, s, b, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r == CUDA_SUCCESS) return SOL_ATTN3D_OK;
+  p->last_cuda = (int)r;
+  return SOL_ATTN3D_ERR_CUDA;
+}
+
+template <int D, bool kPaged>
+cudaError_t launch_context(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const sol::ContextParams& c, int sms, cudaStream_t st, int* launches) {
+  cudaError_t e = cudaFuncSetAttribute(sol::context_attn_kernel<D, kPaged>, cudaFuncAttributeMaxDynamicSharedMemorySize, sol::ContextSmem<D>::kDynBytes);
+  if (e != cudaSuccess) return e;
+  sol::context_attn_kernel<D, kPaged><<<(unsigned)std::min<long long>(c.total, sms), sol::kAttnThreads, sol::ContextSmem<D>::kDynBytes, st>>>(q, k, v, c);
+  if ((e = cudaGetLastError()) != cudaSuccess) return e;
+  ++*launches;
+  if (c.partial != nullptr) {
+    const sol::JoinArgs j{c.a, c.d, c.n_split, 2 * c.tok_per_tile * c.a.group, c.units, c.partial};
+    sol::join_rows_kernel<D, kPaged><<<(unsigned)(c.units * c.d.c.kv_heads), 256, 0, st>>>(j);
+    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    ++*launches;
+  }
+  return cudaSuccess;
+}
+
+int attend_many(sol_attn3d_plan_t p, const sol::QueriesDev& a, const sol::KeysDev& d, bool paged, const ContextRoute& r, void* workspace,
+                size_t workspace_bytes, size_t need, cudaStream_t st) {
+  sol::ContextParams c{};
+  c.a = a;
+  c.d = d;
+  c.units = r.units;
+  c.n_split = r.n_split;
+  c.total = r.units * d.c.kv_heads * r.n_split;
+  if (c.total >= (1ll << 31)) return SOL_ATTN3D_ERR_UNSUPPORTED_SHAPE;
+  c.tok_per_tile = r.tok_per_tile;
+  if (r.n_split > 1) {
+    if (workspace == nullptr || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) % kAlign) != 0) return SOL_ATTN3D_ERR_NO_WORKSPACE;
+    c.partial = static_cast<float*>(workspace);
+  }
+  c.counter = reinterpret_cast<unsigned int*>(p->ws + p->off_status + kUnitCounterOffset);
+  c.status = reinterpret_cast<unsigned int*>(p->ws + p->off_status);
+  c.rescales = reinterpret_cast<unsigned int*>(p->ws + p->off_status + kCountersOffset);
+  c.wait_limit_ns = p->wait_limit_ns;
+  c.fault_inject = p->fault_inject;
+  c.v_lbo = p->v_lbo;
+  c.v_sbo = p->v_sbo;
+  CUtensorMap tm_q, tm_k, tm_v;
+  const long long q_dims[3] = {p->head_dim, p->heads, p->total_tokens}, q_strides[2] = {a.q_head, a.q_tok};
+  const int q_box[3] = {64, r.group, r.tok_per_tile};
+  int rc = encode_boxes(p, &tm_q, a.q, 3, q_dims, q_strides, q_box);
+  for (int kv = 0; kv < 2 && rc == SOL_ATTN3D_OK; ++kv) {
+    CUtensorMap* tm = kv ? &tm_v : &tm_k;
+    const void* base = kv ? d.c.v : d.c.k;
+    const long long* s = kv ? d.c.vs : d.c.ks;
+    if (paged) {
+      c.box_rows = 16;
+      while (c.box_rows < 128 && d.c.page % (2 * c.box_rows) == 0) c.box_rows *= 2;
+      const long long dims[4] = {p->head_dim, d.c.kv_heads, d.c.page, d.c.n_pages}, strides[3] = {s[2], s[1], s[0]};
+      const int box[4] = {64, 1, c.box_rows, 1};
+      rc = encode_boxes(p, tm, base, 4, dims, strides, box);
+    } else {
+      c.box_rows = 128;
+      const long long dims[3] = {p->head_dim, d.c.kv_heads, d.total_rows}, strides[2] = {s[2], s[1]};
+      const int box[3] = {64, 1, 128};
+      rc = encode_boxes(p, tm, base, 3, dims, strides, box);
+    }
+  }
+  if (rc != SOL_ATTN3D_OK) return rc;
+  const cudaError_t e = p->head_dim == 128 ? (paged ? launch_context<128, true>(tm_q, tm_k, tm_v, c, p->sm_count, st, &p->launches)
+                                                    : launch_context<128, false>(tm_q, tm_k, tm_v, c, p->sm_count, st, &p->launches))
+                                           : (paged ? launch_context<64, true>(tm_q, tm_k, tm_v, c, p->sm_count, st, &p->launches)
+                                                    : launch_context<64, false>(tm_q, tm_k, tm_v, c, p->sm_count, st, &p->launches));
+  return e == cudaSuccess ? SOL_ATTN3D_OK : fail_cuda(p, e);
 }
 
 int forward_context(sol_attn3d_plan_t p, const void* q, void* out, const sol::KeysDev& d, bool paged, long long capacity, int causal,
                     void* workspace, size_t workspace_bytes, sol_attn3d_stream_t stream) {
   if (q == nullptr || out == nullptr || q == out || !aligned16(q) || !aligned16(out)) return SOL_ATTN3D_ERR_INVALID_ARG;
   if (p->heads % d.c.kv_heads != 0) return SOL_ATTN3D_ERR_UNSUPPORTED_SHAPE;
+  const long long total_rows = paged ? 1 : d.total_rows;
+  const ContextRoute r = choose_route(p, d.c.kv_heads, capacity, total_rows);
+  if ((long long)p->sched.front().n_tokens * r.group >= (1ll << 31)) return SOL_ATTN3D_ERR_UNSUPPORTED_SHAPE;   // rows are counted in 32 bits
   if (p->ws == nullptr || p->encode == nullptr) return SOL_ATTN3D_ERR_NO_WORKSPACE;
   sol::QueriesDev a{};
   a.q = static_cast<const __nv_bfloat16*>(q);
@@ -145,7 +274,7 @@ int forward_context(sol_attn3d_plan_t p, const void* q, void* out, const sol::Ke
   a.seqs = reinterpret_cast<const SeqDev*>(p->ws + p->off_seqs);
   a.cum_tok = reinterpret_cast<const int*>(p->ws + p->off_cum);
   a.n_seqs = p->n_seqs;
-  a.group = p->heads / d.c.kv_heads;
+  a.group = r.group;
   a.causal = causal;
   a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)p->head_dim));
   cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -157,7 +286,8 @@ int forward_context(sol_attn3d_plan_t p, const void* q, void* out, const sol::Ke
     for (int i = 0; i < 3; ++i)
       if ((e = cudaEventRecord(p->ev[i], st)) != cudaSuccess) return fail_cuda(p, e);
   }
-  const int rc = attend_few(a, d, paged, p->head_dim, few_units(p, 0, a.group), capacity, workspace, workspace_bytes, st, &p->launches, &p->last_cuda);
+  const int rc = r.few ? attend_few(a, d, paged, p->head_dim, r.units, capacity, workspace, workspace_bytes, st, &p->launches, &p->last_cuda)
+                       : attend_many(p, a, d, paged, r, workspace, workspace_bytes, context_bytes(p, d.c.kv_heads, capacity, total_rows), st);
   if (rc != SOL_ATTN3D_OK) return rc;
   if (p->prof) {
     if ((e = cudaEventRecord(p->ev[3], st)) != cudaSuccess) return fail_cuda(p, e);
@@ -420,7 +550,7 @@ int sol_attn3d_cache_append(sol_attn3d_plan_t p, const void* q, const void* k, c
 size_t sol_attn3d_paged_workspace_bytes(sol_attn3d_plan_t plan, const sol_attn3d_paged_cache* cache) {
   sol::PagedDev c{};
   if (plan == nullptr || take_cache(cache, 0, &c) != SOL_ATTN3D_OK) return 0;
-  return context_bytes(plan, c.kv_heads, c.width * c.page);
+  return context_bytes(plan, c.kv_heads, c.width * c.page, 1);
 }
 
 int sol_attn3d_forward_paged(sol_attn3d_plan_t p, const void* q, const sol_attn3d_paged_cache* cache, int layer, void* out,
@@ -459,7 +589,7 @@ int sol_attn3d_paged_step(const void* q, const int64_t q_strides[2], const sol_a
 size_t sol_attn3d_cross_workspace_bytes(sol_attn3d_plan_t plan, const sol_attn3d_context* context) {
   sol::KeysDev d{};
   if (plan == nullptr || take_context(context, &d) != SOL_ATTN3D_OK) return 0;
-  return context_bytes(plan, context->kv_heads, std::min(context->max_len, context->total_rows));
+  return context_bytes(plan, context->kv_heads, std::min(context->max_len, context->total_rows), context->total_rows);
 }
 
 int sol_attn3d_forward_cross(sol_attn3d_plan_t p, const void* q, const sol_attn3d_context* context, void* out, void* workspace,
