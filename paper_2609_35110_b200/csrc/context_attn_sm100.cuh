@@ -192,33 +192,19 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         if (!ok) break;
         tc_fence_after();
         const bool whole = mask == nullptr && (jt + 1) * 128 <= lim_all;
+        // In two halves: the second half of S is still on its way while the first is exponentiated, and the first half of P is on
+        // its way to tensor memory while the second is.  (Also fewer registers: 128 scores and 32 packed pairs at a time.)
         uint32_t r[128];
-        uint32_t pk[64];
-        float tile_sum;
-        bool first_half_stored = false;
-        if (whole && started) {
-          // Common case, in two halves: the second half of S is still on its way while the first is exponentiated, and the
-          // first half of P is on its way to tensor memory while the second is.
-          uint32_t (&r_lo)[64] = *reinterpret_cast<uint32_t(*)[64]>(&r[0]);
-          uint32_t (&r_hi)[64] = *reinterpret_cast<uint32_t(*)[64]>(&r[64]);
-          tmem_ld32(tS, *reinterpret_cast<uint32_t(*)[32]>(&r[0]));
-          tmem_ld32(tS + 32, *reinterpret_cast<uint32_t(*)[32]>(&r[32]));
-          tmem_wait_ld_dep64(r_lo);
-          tmem_ld32(tS + 64, *reinterpret_cast<uint32_t(*)[32]>(&r[64]));
-          tmem_ld32(tS + 96, *reinterpret_cast<uint32_t(*)[32]>(&r[96]));
-          float acc[4] = {0.f, 0.f, 0.f, 0.f};
-          const float mc = m_ref * c;
-          softmax_half(r_lo, c, mc, *reinterpret_cast<uint32_t(*)[32]>(&pk[0]), acc);
+        uint32_t (&r_lo)[64] = *reinterpret_cast<uint32_t(*)[64]>(&r[0]);
+        uint32_t (&r_hi)[64] = *reinterpret_cast<uint32_t(*)[64]>(&r[64]);
+        uint32_t pk[32];
+        tmem_ld32(tS, *reinterpret_cast<uint32_t(*)[32]>(&r[0]));
+        tmem_ld32(tS + 32, *reinterpret_cast<uint32_t(*)[32]>(&r[32]));
+        tmem_wait_ld_dep64(r_lo);
+        tmem_ld32(tS + 64, *reinterpret_cast<uint32_t(*)[32]>(&r[64]));
+        tmem_ld32(tS + 96, *reinterpret_cast<uint32_t(*)[32]>(&r[96]));
+        if (!whole || !started) {
           tmem_wait_ld_dep64(r_hi);
-          tmem_st32(tS, *reinterpret_cast<uint32_t(*)[32]>(&pk[0]));       // columns [0,32): their scores are in registers
-          first_half_stored = true;
-          softmax_half(r_hi, c, mc, *reinterpret_cast<uint32_t(*)[32]>(&pk[32]), acc);
-          tile_sum = (acc[0] + acc[1]) + (acc[2] + acc[3]);
-          seen = true;
-        } else {
-#pragma unroll
-          for (int cch = 0; cch < 4; ++cch) tmem_ld32(tS + cch * 32, *reinterpret_cast<uint32_t(*)[32]>(&r[cch * 32]));
-          tmem_wait_ld();
           if (!whole) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -229,17 +215,27 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
               for (int cc = 0; cc < 32; ++cc)
                 if (((valid >> cc) & 1u) == 0) r[e * 32 + cc] = __float_as_uint(-CUDART_INF_F);
             }
-          } else {
-            seen = true;
           }
           // a row takes its reference from its first tile with a valid key; before that every term is 2^-inf
           if (m_ref == -CUDART_INF_F) m_ref = row_max128(r);
-          softmax_pass(r, c, m_ref == -CUDART_INF_F ? 0.f : m_ref * c, pk, tile_sum);
           started = __all_sync(0xffffffffu, !mine || m_ref != -CUDART_INF_F);
+        }
+        seen = seen || whole;
+        float acc[4];
+        auto first_half = [&](float mc) {
+          acc[0] = acc[1] = acc[2] = acc[3] = 0.f;
+          softmax_half(r_lo, c, mc, pk, acc);
+          tmem_wait_ld_dep64(r_hi);
+          tmem_st32(tS, pk);                               // columns [0,32): their scores are in registers
+        };
+        {
+          const float mc = m_ref == -CUDART_INF_F ? 0.f : m_ref * c;
+          first_half(mc);
+          softmax_half(r_hi, c, mc, pk, acc);
         }
         // No row maximum was taken.  All terms are positive, so a sum <= 2^8 proves that every term is; otherwise, if the maximum
         // has grown by more than 2^8, the reference moves and the tile is redone before its P is released.
-        if (__any_sync(0xffffffffu, mine && !(tile_sum <= 256.0f))) {
+        if (__any_sync(0xffffffffu, mine && !((acc[0] + acc[1]) + (acc[2] + acc[3]) <= 256.0f))) {
           const float mx = row_max128(r);
           const bool grow = mine && (mx - m_ref) * c > 8.0f;
           if (__any_sync(0xffffffffu, grow)) {
@@ -251,24 +247,24 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
               ok = mbar_wait_warp(bar_o_done(t), (n_s - 1) & 1, limit);
               if (!ok) break;
               tc_fence_after();
-#pragma unroll
-              for (int cch = 0; cch < D / 32; ++cch) {
-                uint32_t o[32];
-                tmem_ld32(tO + cch * 32, o);
+#pragma unroll 1
+              for (int cch = 0; cch < D / 16; ++cch) {
+                uint32_t o[16];
+                tmem_ld16(tO + cch * 16, o);
                 tmem_wait_ld();
 #pragma unroll
-                for (int cc = 0; cc < 32; ++cc) o[cc] = __float_as_uint(__uint_as_float(o[cc]) * f);
-                tmem_st32(tO + cch * 32, o);
+                for (int cc = 0; cc < 16; ++cc) o[cc] = __float_as_uint(__uint_as_float(o[cc]) * f);
+                tmem_st16(tO + cch * 16, o);
               }
             }
-            softmax_pass(r, c, m_ref == -CUDART_INF_F ? 0.f : m_ref * c, pk, tile_sum);
-            if (first_half_stored) tmem_wait_st();                       // the stale first half lands before its replacement
-            first_half_stored = false;
+            tmem_wait_st();                                // the stale first half lands before its replacement
+            const float mc = m_ref == -CUDART_INF_F ? 0.f : m_ref * c;
+            first_half(mc);
+            softmax_half(r_hi, c, mc, pk, acc);
           }
         }
-        l += tile_sum;
-        if (!first_half_stored) tmem_st32(tS, *reinterpret_cast<uint32_t(*)[32]>(&pk[0]));
-        tmem_st32(tS + 32, *reinterpret_cast<uint32_t(*)[32]>(&pk[32]));
+        l += (acc[0] + acc[1]) + (acc[2] + acc[3]);
+        tmem_st32(tS + 32, pk);
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
