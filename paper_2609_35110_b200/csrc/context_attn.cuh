@@ -110,7 +110,7 @@ struct FewArgs {
   KeysDev d;
   int n_split;
   long long units;              // per K/V head
-  float* partial;               // [unit][kv_head][split][16][D + 2], or nullptr: one split
+  float* partial;               // [kv_head][unit][split][16][D + 4], or nullptr: one split
 };
 
 __device__ __forceinline__ void mma_bf16_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -343,7 +343,7 @@ __global__ void __launch_bounds__(kFewThreads, kFewResident) few_rows_kernel(con
       for (int e = 0; e < 8; ++e) acc[e] = fmaf(s_o[w][row][d0 + e], f, acc[e]);
     }
     if (p.partial != nullptr) {
-      float* dst = p.partial + (((unit * p.d.c.kv_heads + kv_head) * p.n_split + split) * kFewRows + row) * (D + 4);
+      float* dst = p.partial + (((kv_head * p.units + unit) * p.n_split + split) * kFewRows + row) * (D + 4);
       *reinterpret_cast<float4*>(dst + d0) = make_float4(acc[0], acc[1], acc[2], acc[3]);
       *reinterpret_cast<float4*>(dst + d0 + 4) = make_float4(acc[4], acc[5], acc[6], acc[7]);
       if (d0 == 0) *reinterpret_cast<float4*>(dst + D) = make_float4(top, sum, any ? 1.f : 0.f, 0.f);
@@ -360,43 +360,60 @@ __global__ void __launch_bounds__(kFewThreads, kFewResident) few_rows_kernel(con
 }
 
 // Joins the parts of split keys, in the order of the splits.  Rows of partial results: D values, maximum, sum, "has a valid key".
-// One thread per 8 dims of a row; a CTA per unit and K/V head.
+// One thread per 8 dims of a row; a CTA per unit and K/V head.  Whose rows a unit holds follows from its number (few rows), or was
+// written down by who made them (kListed).
+struct JoinUnit {
+  long long tok0;
+  int t0, n_tok;                // first new token of the unit; new tokens of the sequence (0: nothing to join)
+  int kv_head;
+  int unused;
+};
 struct JoinArgs {
   QueriesDev a;
   KeysDev d;
   int n_split, rows_per_unit;
   long long units;
   const float* partial;
+  const JoinUnit* list;
 };
 
-template <int D, bool kPaged>
+template <int D, bool kPaged, bool kListed>
 __global__ void __launch_bounds__(256) join_rows_kernel(const __grid_constant__ JoinArgs p) {
-  const int kv_head = (int)(blockIdx.x % p.d.c.kv_heads);
-  const long long unit = blockIdx.x / p.d.c.kv_heads;
-  int entry, n_tok, row0;
-  long long tok0;
-  if (p.a.seqs != nullptr) {
-    long long first;
-    const SeqDev& sq = p.a.seqs[find_sequence(p.a, unit, p.rows_per_unit, &first)];
-    entry = sq.seq_id;
-    n_tok = sq.n_tokens;
-    tok0 = sq.tok_start;
-    row0 = (int)(unit - first) * p.rows_per_unit;
+  int kv_head, n_tok;
+  long long tok0, row0;
+  if (kListed) {
+    const JoinUnit u = p.list[blockIdx.x];
+    kv_head = u.kv_head;
+    n_tok = u.n_tok;
+    tok0 = u.tok0;
+    row0 = (long long)u.t0 * p.a.group;
   } else {
-    const int per = (p.a.group + p.rows_per_unit - 1) / p.rows_per_unit;
-    entry = (int)(unit / per);
-    n_tok = 1;
-    tok0 = entry;
-    row0 = (int)(unit % per) * p.rows_per_unit;
+    int entry;
+    kv_head = (int)(blockIdx.x / p.units);
+    const long long unit = blockIdx.x % p.units;
+    if (p.a.seqs != nullptr) {
+      long long first;
+      const SeqDev& sq = p.a.seqs[find_sequence(p.a, unit, p.rows_per_unit, &first)];
+      entry = sq.seq_id;
+      n_tok = sq.n_tokens;
+      tok0 = sq.tok_start;
+      row0 = (unit - first) * p.rows_per_unit;
+    } else {
+      const int per = (p.a.group + p.rows_per_unit - 1) / p.rows_per_unit;
+      entry = (int)(unit / per);
+      n_tok = 1;
+      tok0 = entry;
+      row0 = (unit % per) * p.rows_per_unit;
+    }
+    if (kPaged) {
+      const long long stream = p.d.streams != nullptr ? p.d.streams[entry] : entry;
+      if (stream < 0 || stream >= p.d.c.n_streams) return;
+    }
   }
   const long long n_rows = min((long long)p.rows_per_unit, (long long)n_tok * p.a.group - row0);
   if (n_rows <= 0) return;
-  if (kPaged) {
-    const long long stream = p.d.streams != nullptr ? p.d.streams[entry] : entry;
-    if (stream < 0 || stream >= p.d.c.n_streams) return;
-  }
   constexpr int kChunks = D / 8;
-  const float* part = p.partial + (unit * p.d.c.kv_heads + kv_head) * p.n_split * (long long)p.rows_per_unit * (D + 4);
+  const float* part = p.partial + (long long)blockIdx.x * p.n_split * p.rows_per_unit * (D + 4);
   for (int x = threadIdx.x; x < n_rows * kChunks; x += blockDim.x) {
     const int row = x / kChunks, d0 = (x % kChunks) * 8;
     const float* mine = part + (long long)row * (D + 4);
@@ -420,7 +437,7 @@ __global__ void __launch_bounds__(256) join_rows_kernel(const __grid_constant__ 
       acc[4] = fmaf(v.x, f, acc[4]); acc[5] = fmaf(v.y, f, acc[5]); acc[6] = fmaf(v.z, f, acc[6]); acc[7] = fmaf(v.w, f, acc[7]);
     }
     const float inv = 1.f / sum;
-    const int r = row0 + row;
+    const long long r = row0 + row;
     __nv_bfloat16* dst = p.a.out + (tok0 + r / p.a.group) * p.a.o_tok + ((long long)kv_head * p.a.group + r % p.a.group) * p.a.o_head + d0;
     uint4 y = make_uint4(0, 0, 0, 0);
     if (any) y = make_uint4(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv),

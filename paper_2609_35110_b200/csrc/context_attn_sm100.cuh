@@ -25,7 +25,7 @@ namespace sol {
 struct UnitDev {
   Span span;
   long long tok0;               // first token of the sequence in the packed tensors
-  long long part;               // index of this unit's partial rows
+  long long part;               // index of this unit's partial rows, or -1: the rows themselves are written
   int t0, n_tok;                // first new token of the unit; new tokens of the sequence
   int kv_head;
   int tile_begin, tile_end;     // key tiles
@@ -37,12 +37,16 @@ struct UnitDev {
 struct ContextParams {
   QueriesDev a;
   KeysDev d;
-  long long units;              // row units per K/V head
-  long long total;              // units * kv_heads * n_split
+  long long units;              // row units per K/V head (more than kSortedSeqs sequences: with room for empty ones, find_sequence)
+  long long n_whole, n_tail;    // units that take all of their keys, then units whose keys are split
+  long long total;              // n_whole + n_tail * n_split
   int n_split;
+  int lookahead;                // units that a CTA draws before it has finished with the one in work: 2 or 4
   int tok_per_tile;             // 128 / group
+  unsigned int inv_group;       // ceil(2^16 / group): x / group = x * inv_group >> 16 for x < 128
   int box_rows;                 // tokens of a K/V box: a power of two that divides the page size, at most 128
-  float* partial;               // [unit][kv_head][split][2 * tok_per_tile * group][D + 4], or nullptr: one split
+  float* partial;               // [n_tail][n_split][2 * tok_per_tile * group][D + 4]
+  JoinUnit* join;               // [n_tail]: whose rows these are
   unsigned int* counter;        // next unit; 0 between launches
   unsigned int* status;
   unsigned int* rescales;
@@ -50,6 +54,10 @@ struct ContextParams {
   unsigned int fault_inject;    // 1: the first unit withholds "scores of tile 1 (or the only one) are there"
   unsigned int v_lbo, v_sbo;
 };
+
+// Up to so many sequences are taken in the order of their keys, most first, so that long units do not come last.
+constexpr int kSortedSeqs = 32;
+constexpr int kUnitRing = 4;
 
 template <int D>
 struct ContextSmem {
@@ -62,10 +70,11 @@ struct ContextSmem {
   static constexpr int kOffKV = 2 * kTile;
   static constexpr int kOffStage = kOffKV + kStages * kTile;   // 4 KB per softmax warp
   static constexpr int kOffBars = kOffStage + 8 * 4096;
-  static constexpr int kNumBars = 2 * kStages + 4 + 6 + 4 + kVRing + 1;
+  static constexpr int kNumBars = 2 * kStages + 4 + 6 + 2 * kUnitRing + kVRing + 1;
   static constexpr int kOffTmemPtr = kOffBars + kNumBars * 8;
   static constexpr int kOffUnits = (kOffTmemPtr + 16 + 15) / 16 * 16;
-  static constexpr int kBytes = kOffUnits + 2 * (int)sizeof(UnitDev);
+  static constexpr int kOffOrder = kOffUnits + kUnitRing * (int)sizeof(UnitDev);   // sequence, first unit: kSortedSeqs each
+  static constexpr int kBytes = kOffOrder + 2 * kSortedSeqs * 4;
   static constexpr int kDynBytes = kBytes + 1024;
 };
 
@@ -95,10 +104,11 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
   auto bar_s_full = [&](int t) { return bars + 8u * (kB + 4 + t); };
   auto bar_p_full = [&](int t) { return bars + 8u * (kB + 6 + t); };
   auto bar_o_done = [&](int t) { return bars + 8u * (kB + 8 + t); };
-  auto bar_u_full = [&](int s) { return bars + 8u * (kB + 10 + s); };
-  auto bar_u_empty = [&](int s) { return bars + 8u * (kB + 12 + s); };
-  auto bar_v_clean = [&](uint32_t n) { return bars + 8u * (kB + 14 + (n & (L::kVRing - 1))); };
-  const uint32_t bar_drain = bars + 8u * (kB + 14 + L::kVRing);
+  auto bar_u_full = [&](uint32_t u) { return bars + 8u * (kB + 10 + (u & (kUnitRing - 1))); };
+  auto bar_u_empty = [&](uint32_t u) { return bars + 8u * (kB + 10 + kUnitRing + (u & (kUnitRing - 1))); };
+  auto bar_v_clean = [&](uint32_t n) { return bars + 8u * (kB + 10 + 2 * kUnitRing + (n & (L::kVRing - 1))); };
+  const uint32_t bar_drain = bars + 8u * (kB + 10 + 2 * kUnitRing + L::kVRing);
+  auto round_of = [](uint32_t u) { return (u / kUnitRing) & 1u; };
   volatile uint32_t* tmem_ptr_smem = reinterpret_cast<volatile uint32_t*>(smem + L::kOffTmemPtr);
   UnitDev* units = reinterpret_cast<UnitDev*>(smem + L::kOffUnits);
   const unsigned long long limit = p.wait_limit_ns;
@@ -111,8 +121,10 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       mbar_init(bar_s_full(t), 1);
       mbar_init(bar_p_full(t), 4);
       mbar_init(bar_o_done(t), 1);
-      mbar_init(bar_u_full(t), 1);
-      mbar_init(bar_u_empty(t), 11);                       // eight softmax warps, loads, issuer, cleaner
+    }
+    for (int u = 0; u < kUnitRing; ++u) {
+      mbar_init(bar_u_full(u), 1);
+      mbar_init(bar_u_empty(u), 11);                       // eight softmax warps, loads, issuer, cleaner
     }
     for (int n = 0; n < L::kVRing; ++n) mbar_init(bar_v_clean(n), 1);
     mbar_init(bar_drain, 1);
@@ -145,7 +157,7 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
   };
   auto release_unit = [&](uint32_t u) {
     __syncwarp();
-    if (lane == 0) mbar_arrive(bar_u_empty(u & 1));
+    if (lane == 0) mbar_arrive(bar_u_empty(u));
   };
 
   if (warp < 8) {
@@ -161,14 +173,14 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     uint32_t n_s = 0;                                      // key tiles of this query tile so far
     bool ok = true;
     for (uint32_t u = 0;; ++u) {
-      if (!wait_long(bar_u_full(u & 1), (u >> 1) & 1)) { ok = false; break; }
-      const UnitDev& un = units[u & 1];
+      if (!wait_long(bar_u_full(u), round_of(u))) { ok = false; break; }
+      const UnitDev& un = units[u & (kUnitRing - 1)];
       if (un.last) break;
       if (t >= un.n_tiles) { release_unit(u); continue; }
       const int tile_begin = un.tile_begin, tile_end = un.tile_end, lim_all = un.lim[t];
       const uint8_t* mask = un.span.mask;
       const int cap = un.span.cap;
-      const int tok = un.t0 + t * p.tok_per_tile + row / group;       // this thread's new token
+      const int tok = un.t0 + t * p.tok_per_tile + (int)(row * p.inv_group >> 16);       // this thread's new token
       const bool mine = row < tile_rows && tok < un.n_tok;
       const int lim = mine ? key_limit(un.span, un.n_tok, tok, p.a.causal) : 0x7fffffff;
       float m_ref = -CUDART_INF_F, l = 0.f;
@@ -278,7 +290,7 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         if (!ok) break;
         tc_fence_after();
       }
-      if (p.partial != nullptr) {
+      if (un.part >= 0) {
         float* dst = p.partial + (un.part * 2 * tile_rows + t * tile_rows + row) * (D + 4);
 #pragma unroll 1
         for (int cch = 0; cch < D / 32; ++cch) {
@@ -328,10 +340,11 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
           for (int r0 = 0; r0 < 32; r0 += 4) {
             const int rr = r0 + (lane >> 3), ch = lane & 7;
             const int tile_row = wq * 32 + rr;
-            const int tk = un.t0 + t * p.tok_per_tile + tile_row / group;
+            const int in_tile = (int)(tile_row * p.inv_group >> 16);       // token of the tile
+            const int tk = un.t0 + t * p.tok_per_tile + in_tile;
             const uint4 w = *reinterpret_cast<const uint4*>(stage + rr * 128 + ((ch ^ (rr & 7)) << 4));
             if (tile_row < tile_rows && tk < un.n_tok)
-              st_global_evict_first(p.a.out + (un.tok0 + tk) * p.a.o_tok + ((long long)un.kv_head * group + tile_row % group) * p.a.o_head +
+              st_global_evict_first(p.a.out + (un.tok0 + tk) * p.a.o_tok + (long long)(un.kv_head * group + tile_row - in_tile * group) * p.a.o_head +
                                         hf * 64 + ch * 8, w, pol_once);
           }
         }
@@ -350,8 +363,8 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     uint32_t it = 0, n_q[2] = {0, 0};
     bool ok = true;
     for (uint32_t u = 0;; ++u) {
-      if (!wait_long(bar_u_full(u & 1), (u >> 1) & 1)) { ok = false; break; }
-      const UnitDev& un = units[u & 1];
+      if (!wait_long(bar_u_full(u), round_of(u))) { ok = false; break; }
+      const UnitDev& un = units[u & (kUnitRing - 1)];
       if (un.last) break;
       const int tile_begin = un.tile_begin, tile_end = un.tile_end, kv_head = un.kv_head, n = un.span.cap;
       const int* table = un.span.table;
@@ -454,62 +467,96 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     };
     auto stage_of = [&](uint32_t n) { return n % L::kStages; };
     auto full = [&](uint32_t n) { return wait(bar_kv_full(n % L::kStages), (n / L::kStages) & 1); };
-    for (uint32_t u = 0; ok; ++u) {
-      if (!wait_long(bar_u_full(u & 1), (u >> 1) & 1)) { ok = false; break; }
-      const UnitDev& un = units[u & 1];
-      if (un.last) break;
-      const int n_proc = un.tile_end - un.tile_begin;
-      const bool two = un.n_tiles == 2;
-      release_unit(u);
-      if (n_proc <= 0) continue;
-      // (test hook: the first unit withholds a signal, so that the waits downstream run into their limit)
-      const bool withhold = p.fault_inject == 1u && blockIdx.x == 0 && u == 0;
-      uint32_t k_it = it;
-      if (!wait(bar_q_full(0), n_q[0] & 1) || !full(k_it)) break;
-      ++n_q[0];
-      issue_qk(tS0, q_lo0, stage_of(k_it));
-      if (two || !withhold) tc_commit_elect(bar_s_full(0));
-      if (n_proc == 1) tc_commit_elect(bar_q_empty(0));
-      if (two) {
-        if (!wait(bar_q_full(1), n_q[1] & 1)) break;
-        ++n_q[1];
-        issue_qk(tS1, q_lo1, stage_of(k_it));
-        if (!withhold) tc_commit_elect(bar_s_full(1));
-        if (n_proc == 1) tc_commit_elect(bar_q_empty(1));
+    // The next unit: kNone, kEmpty (it has no key tiles, the softmax warps see to its rows) or kTiles.
+    enum { kNone, kEmpty, kTiles };
+    uint32_t u = 0;
+    int n_proc = 0;
+    bool two = false, withhold = p.fault_inject == 1u && blockIdx.x == 0;
+    auto draw = [&]() {
+      if (!wait_long(bar_u_full(u), round_of(u))) { ok = false; return (int)kNone; }
+      const UnitDev& un = units[u & (kUnitRing - 1)];
+      if (un.last) return (int)kNone;
+      n_proc = un.tile_end - un.tile_begin;
+      two = un.n_tiles == 2;
+      release_unit(u++);
+      return (int)(n_proc > 0 ? kTiles : kEmpty);
+    };
+    // One stream of key tiles through units that follow one another: scores of tile 0 for the next key tile, which may be the next
+    // unit's first, follow the product of this one, so that a unit's end looks to the tensor core like its middle.  (An empty unit
+    // ends the stream: looking past it could wait for this unit's own end.)
+    while (ok) {
+      int what = draw();
+      while (what == kEmpty) what = draw();
+      if (what != kTiles) break;
+      // (withhold, a test hook: the first unit withholds a signal, so that the waits downstream run into their limit)
+      {
+        const uint32_t k_st = stage_of(it);
+        if (!wait(bar_q_full(0), n_q[0] & 1) || !full(it)) break;
+        ++n_q[0];
+        issue_qk(tS0, q_lo0, k_st);
+        if (two || !withhold) tc_commit_elect(bar_s_full(0));
+        if (n_proc == 1) tc_commit_elect(bar_q_empty(0));
+        if (two) {
+          if (!wait(bar_q_full(1), n_q[1] & 1)) break;
+          ++n_q[1];
+          issue_qk(tS1, q_lo1, k_st);
+          if (!withhold) tc_commit_elect(bar_s_full(1));
+          if (n_proc == 1) tc_commit_elect(bar_q_empty(1));
+        }
+        tc_commit_elect(bar_kv_empty(k_st));
+        withhold = false;
       }
-      tc_commit_elect(bar_kv_empty(stage_of(k_it)));
-      for (int i = 0; i < n_proc; ++i) {
+      bool have = true;
+      int i = 0;
+      while (have && ok) {
         const uint32_t v_it = it + 1, next = it + 2;
-        const bool more = i + 1 < n_proc, last_k = i + 2 == n_proc;
+        const bool now_two = two, first = i == 0;
         it += 2;
         if (!full(v_it) || !wait(bar_v_clean(n_v), (n_v / L::kVRing) & 1)) break;
         ++n_v;
         if (!wait(bar_p_full(0), n_p[0] & 1)) break;
         ++n_p[0];
-        issue_pv(tO0, tS0, stage_of(v_it), i > 0);
+        issue_pv(tO0, tS0, stage_of(v_it), !first);
         tc_commit_elect(bar_o_done(0));
-        if (more) {
+        bool fresh = false;                                  // the next key tile is the first of another unit
+        if (++i == n_proc) {
+          what = draw();
+          if (!ok) break;
+          have = what == kTiles;
+          fresh = true;
+          i = 0;
+        }
+        if (have) {
+          if (fresh) {
+            if (!wait(bar_q_full(0), n_q[0] & 1)) break;
+            ++n_q[0];
+          }
           if (!full(next)) break;
           issue_qk(tS0, q_lo0, stage_of(next));
           tc_commit_elect(bar_s_full(0));
-          if (last_k) tc_commit_elect(bar_q_empty(0));
+          if (i + 1 == n_proc) tc_commit_elect(bar_q_empty(0));
         }
-        if (two) {
+        if (now_two) {
           if (!wait(bar_p_full(1), n_p[1] & 1)) break;
           ++n_p[1];
-          issue_pv(tO1, tS1, stage_of(v_it), i > 0);
+          issue_pv(tO1, tS1, stage_of(v_it), !first);
           tc_commit_elect(bar_o_done(1));
         }
         tc_commit_elect(bar_kv_empty(stage_of(v_it)));
-        if (more) {
+        if (have) {
           if (two) {
+            if (fresh) {
+              if (!wait(bar_q_full(1), n_q[1] & 1)) break;
+              ++n_q[1];
+            }
             issue_qk(tS1, q_lo1, stage_of(next));
             tc_commit_elect(bar_s_full(1));
-            if (last_k) tc_commit_elect(bar_q_empty(1));
+            if (i + 1 == n_proc) tc_commit_elect(bar_q_empty(1));
           }
           tc_commit_elect(bar_kv_empty(stage_of(next)));
         }
       }
+      if (what == kNone) break;
     }
     if (!ok) {
       if (lane == 0) atomicCAS(p.status, 0u, kStatusTimeoutMma);
@@ -519,48 +566,104 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
   } else if (warp == 10) {
     // =========================================================== takes units
     bool ok = true;
-    const int rows = 2 * p.tok_per_tile * p.a.group;
+    const int per_unit = 2 * p.tok_per_tile;
+    int* order = reinterpret_cast<int*>(smem + L::kOffOrder);              // sequences, most keys first
+    unsigned int* start = reinterpret_cast<unsigned int*>(order) + kSortedSeqs;   // first unit of each
+    const bool sorted = p.a.n_seqs <= kSortedSeqs;
+    unsigned int n_units = 0;
+    if (sorted) {
+      int keys = -1;
+      unsigned int mine = 0;
+      if (lane < p.a.n_seqs) {
+        const SeqDev& sq = p.a.seqs[lane];
+        const Span sp = find_span<kPaged>(p.d, sq.seq_id);
+        keys = sp.idle ? -1 : sp.n;
+        mine = sp.idle ? 0u : (unsigned int)((sq.n_tokens + per_unit - 1) / per_unit) * (unsigned int)p.d.c.kv_heads;
+      }
+      int rank = 0;
+      for (int j = 0; j < kSortedSeqs; ++j) {
+        const int other = __shfl_sync(0xffffffffu, keys, j);
+        rank += other > keys || (other == keys && j < lane) ? 1 : 0;
+      }
+      order[rank] = lane;
+      start[rank] = mine;
+      __syncwarp();
+      const unsigned int own = start[lane];
+      unsigned int upto = own;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const unsigned int y = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += y;
+      }
+      n_units = __shfl_sync(0xffffffffu, upto, 31);
+      __syncwarp();
+      start[lane] = upto - own;
+      __syncwarp();
+    }
     for (uint32_t u = 0;; ++u) {
-      if (u >= 2 && !wait_long(bar_u_empty(u & 1), ((u >> 1) & 1) ^ 1u)) { ok = false; break; }
+      if (u >= (uint32_t)p.lookahead && !wait_long(bar_u_empty(u - p.lookahead), round_of(u - p.lookahead))) { ok = false; break; }
       int last = 0;
-      if (lane == 0) {
-        UnitDev un{};
-        for (;;) {
-          const unsigned int at = atomicAdd(p.counter, 1u);
-          if (at >= p.total) {
-            // every CTA draws one number past the units; the one that draws the last of them leaves the counter as it was found
-            if (at == p.total + gridDim.x - 1) *p.counter = 0u;
-            un.last = 1;
-            break;
+      for (;;) {
+        unsigned int at = 0;
+        if (lane == 0) at = atomicAdd(p.counter, 1u);
+        at = __shfl_sync(0xffffffffu, at, 0);
+        if (at >= p.total) {
+          // every CTA draws one number past the units; the one that draws the last of them leaves the counter as it was found
+          if (lane == 0 && at == p.total + gridDim.x - 1) *p.counter = 0u;
+          last = 1;
+          break;
+        }
+        const bool tail = at >= p.n_whole;
+        const long long in_tail = tail ? (at - p.n_whole) % p.n_tail : 0;
+        const int split = tail ? (int)((at - p.n_whole) / p.n_tail) : 0, n_split = tail ? p.n_split : 1;
+        const long long flat = tail ? p.n_whole + in_tail : at;
+        // ---- which sequence, K/V head and rows
+        int si = 0, kv_head = 0;
+        long long t0 = -1;
+        if (sorted) {
+          if (flat < n_units) {
+            const int slot = 31 - __clz(__ballot_sync(0xffffffffu, start[lane] <= flat && lane < p.a.n_seqs));
+            si = order[slot];
+            const unsigned int n = (unsigned int)((p.a.seqs[si].n_tokens + per_unit - 1) / per_unit);
+            const unsigned int local = (unsigned int)flat - start[slot];
+            kv_head = (int)(local / n);
+            t0 = (long long)(local % n) * per_unit;
           }
-          const long long unit = at % p.units;
-          const long long rest = at / p.units;
-          const int split = (int)(rest % p.n_split);
-          un.kv_head = (int)(rest / p.n_split);
-          un.part = (unit * p.d.c.kv_heads + un.kv_head) * p.n_split + split;
+        } else {
           long long first;
-          const SeqDev& sq = p.a.seqs[find_sequence(p.a, unit, rows, &first)];
-          const long long t0 = (unit - first) * 2 * p.tok_per_tile;
-          if (t0 >= sq.n_tokens) continue;
+          kv_head = (int)(flat / p.units);
+          si = find_sequence(p.a, flat % p.units, per_unit * p.a.group, &first);
+          t0 = (flat % p.units - first) * per_unit;
+          if (t0 >= p.a.seqs[si].n_tokens) t0 = -1;
+        }
+        UnitDev un{};
+        if (t0 >= 0) {
+          const SeqDev& sq = p.a.seqs[si];
           un.span = find_span<kPaged>(p.d, sq.seq_id);
-          if (un.span.idle) continue;
           un.t0 = (int)t0;
           un.n_tok = sq.n_tokens;
           un.tok0 = sq.tok_start;
-          un.n_tiles = un.n_tok - un.t0 > p.tok_per_tile ? 2 : 1;
-          un.lim[0] = key_limit(un.span, un.n_tok, un.t0, p.a.causal);
-          un.lim[1] = key_limit(un.span, un.n_tok, un.t0 + p.tok_per_tile, p.a.causal);
-          const int most = key_limit(un.span, un.n_tok, min(un.n_tok, un.t0 + 2 * p.tok_per_tile) - 1, p.a.causal);
-          const int tiles = (most + 127) >> 7, per = (tiles + p.n_split - 1) / p.n_split;
-          un.tile_begin = min(tiles, split * per);
-          un.tile_end = min(tiles, un.tile_begin + per);
-          break;
+          un.kv_head = kv_head;
         }
-        units[u & 1] = un;
-        last = un.last;
-        mbar_arrive(bar_u_full(u & 1));
+        const bool none = t0 < 0 || un.span.idle;
+        if (tail && n_split > 1 && split == 0 && lane == 0) p.join[in_tail] = JoinUnit{un.tok0, un.t0, none ? 0 : un.n_tok, kv_head, 0};
+        if (none) continue;
+        un.part = n_split > 1 ? in_tail * n_split + split : -1;
+        un.n_tiles = un.n_tok - un.t0 > p.tok_per_tile ? 2 : 1;
+        un.lim[0] = key_limit(un.span, un.n_tok, un.t0, p.a.causal);
+        un.lim[1] = key_limit(un.span, un.n_tok, un.t0 + p.tok_per_tile, p.a.causal);
+        const int most = key_limit(un.span, un.n_tok, min(un.n_tok, un.t0 + per_unit) - 1, p.a.causal);
+        const int tiles = (most + 127) >> 7, per = (tiles + n_split - 1) / n_split;
+        un.tile_begin = min(tiles, split * per);
+        un.tile_end = min(tiles, un.tile_begin + per);
+        if (lane == 0) units[u & (kUnitRing - 1)] = un;
+        break;
       }
-      if (__shfl_sync(0xffffffffu, last, 0)) break;
+      if (lane == 0) {
+        if (last) units[u & (kUnitRing - 1)].last = 1;
+        mbar_arrive(bar_u_full(u));
+      }
+      if (last) break;
     }
     if (!ok && lane == 0) atomicCAS(p.status, 0u, kStatusTimeoutProducer);
   } else if (warp == 11) {
@@ -568,8 +671,8 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     uint32_t it = 0, n_v = 0;
     bool ok = true;
     for (uint32_t u = 0; ok; ++u) {
-      if (!wait_long(bar_u_full(u & 1), (u >> 1) & 1)) { ok = false; break; }
-      const UnitDev& un = units[u & 1];
+      if (!wait_long(bar_u_full(u), round_of(u))) { ok = false; break; }
+      const UnitDev& un = units[u & (kUnitRing - 1)];
       if (un.last) break;
       const int tile_begin = un.tile_begin, tile_end = un.tile_end, cap = un.span.cap;
       const uint8_t* mask = un.span.mask;

@@ -95,8 +95,8 @@ cudaError_t launch_few(const sol::FewArgs& f, cudaStream_t st, int* launches) {
   if (e != cudaSuccess) return e;
   ++*launches;
   if (f.partial != nullptr) {
-    const sol::JoinArgs j{f.a, f.d, f.n_split, sol::kFewRows, f.units, f.partial};
-    sol::join_rows_kernel<D, kPaged><<<items, 256, 0, st>>>(j);
+    const sol::JoinArgs j{f.a, f.d, f.n_split, sol::kFewRows, f.units, f.partial, nullptr};
+    sol::join_rows_kernel<D, kPaged, false><<<items, 256, 0, st>>>(j);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
     ++*launches;
   }
@@ -134,6 +134,7 @@ struct ContextRoute {
   bool few;
   int group, tok_per_tile, n_split;
   long long units;              // per K/V head
+  long long n_whole, n_tail;    // units of all heads that take all of their keys; units whose keys are split
 };
 ContextRoute choose_route(sol_attn3d_plan_t p, int kv_heads, long long capacity, long long total_rows) {
   ContextRoute r{};
@@ -147,32 +148,38 @@ ContextRoute choose_route(sol_attn3d_plan_t p, int kv_heads, long long capacity,
   }
   r.tok_per_tile = 128 / r.group;
   const int per_unit = 2 * r.tok_per_tile;
-  r.units = p->total_tokens / per_unit + p->n_seqs;
-  // Splits of the keys, where the units do not fill the SMs: the number that costs least when the units are dealt to 148 SMs in
-  // waves.  The cost of a unit is its key tiles (about 1.9 us each) and some 2 tiles' time for its start and end; joining costs a
-  // launch and the partial rows' way through memory.
-  long long busy = 0;
-  for (const SeqDev& q : p->sched) busy += (q.n_tokens + per_unit - 1) / per_unit;
-  busy *= kv_heads;
-  const long long tiles = (capacity + 127) / 128;
-  r.n_split = 1;
+  // (sequences are sorted on the device up to kSortedSeqs; more are numbered with room for one empty unit each, see find_sequence)
+  for (const SeqDev& q : p->sched) r.units += (q.n_tokens + per_unit - 1) / per_unit;
+  if (p->n_seqs > sol::kSortedSeqs) r.units = p->total_tokens / per_unit + p->n_seqs;
+  // Units are dealt to 148 SMs.  What is left after the last whole wave, or all of them if there are few, is split by keys so that it
+  // ends as one wave of short units.  The cost of a unit is its key tiles (about 2 us each; the longest possible past is assumed) and
+  // 2 tiles' time for its start and end; a part's partial rows go through memory for 0.03, and joining is a launch: 1.5.
+  const long long flat = r.units * kv_heads, tiles = (capacity + 127) / 128, waves = flat / 148;
   double best = 0.0;
-  for (int n = 1; n <= std::max<long long>(1, std::min<long long>(64, tiles / 2)); ++n) {
-    const double waves = (double)((busy * n + 147) / 148);
-    const double cost = waves * ((tiles + n - 1) / n + 2.0) + (n > 1 ? 2.0 + 0.01 * busy * n : 0.0);
-    if (n == 1 || cost < 0.95 * best) {
-      best = cost;
-      r.n_split = n;
+  for (long long back = 0; back <= 2 && back <= waves; ++back) {
+    const long long whole = (waves - back) * 148, tail = flat - whole;
+    for (int n = 1; n <= std::max<long long>(1, std::min<long long>(64, tiles / 2)); ++n) {
+      const double cost = (double)(waves - back) * (tiles + 2.0) + (double)((tail * n + 147) / 148) * ((tiles + n - 1) / n + 2.0) +
+                          (n > 1 ? 1.5 + 0.03 * (double)(tail * n) : 0.0);
+      if ((back == 0 && n == 1) || cost < 0.97 * best) {
+        best = cost;
+        r.n_split = n;
+        r.n_whole = n > 1 ? whole : flat;
+        r.n_tail = flat - r.n_whole;
+      }
     }
   }
   return r;
 }
 
+size_t join_list_bytes(const ContextRoute& r) { return align_up((size_t)r.n_tail * sizeof(sol::JoinUnit)); }
+
 size_t context_bytes(sol_attn3d_plan_t p, int kv_heads, long long capacity, long long total_rows) {
   if (p == nullptr || p->heads % kv_heads != 0) return 0;
   const ContextRoute r = choose_route(p, kv_heads, capacity, total_rows);
   if (r.few) return few_bytes(r.units, kv_heads, p->head_dim, capacity);
-  return r.n_split == 1 ? 0 : align_up((size_t)r.units * kv_heads * r.n_split * 2 * r.tok_per_tile * r.group * (p->head_dim + 4) * sizeof(float));
+  if (r.n_split == 1) return 0;
+  return join_list_bytes(r) + align_up((size_t)r.n_tail * r.n_split * 2 * r.tok_per_tile * r.group * (p->head_dim + 4) * sizeof(float));
 }
 
 // Any tensor as a tiled map of bf16 boxes 64 elements wide, 128-byte swizzle; strides of the outer dimensions in elements.
@@ -200,8 +207,8 @@ cudaError_t launch_context(const CUtensorMap& q, const CUtensorMap& k, const CUt
   if ((e = cudaGetLastError()) != cudaSuccess) return e;
   ++*launches;
   if (c.partial != nullptr) {
-    const sol::JoinArgs j{c.a, c.d, c.n_split, 2 * c.tok_per_tile * c.a.group, c.units, c.partial};
-    sol::join_rows_kernel<D, kPaged><<<(unsigned)(c.units * c.d.c.kv_heads), 256, 0, st>>>(j);
+    const sol::JoinArgs j{c.a, c.d, c.n_split, 2 * c.tok_per_tile * c.a.group, c.units, c.partial, c.join};
+    sol::join_rows_kernel<D, kPaged, true><<<(unsigned)c.n_tail, 256, 0, st>>>(j);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
     ++*launches;
   }
@@ -209,18 +216,23 @@ cudaError_t launch_context(const CUtensorMap& q, const CUtensorMap& k, const CUt
 }
 
 int attend_many(sol_attn3d_plan_t p, const sol::QueriesDev& a, const sol::KeysDev& d, bool paged, const ContextRoute& r, void* workspace,
-                size_t workspace_bytes, size_t need, cudaStream_t st) {
+                size_t workspace_bytes, size_t need, int lookahead, cudaStream_t st) {
   sol::ContextParams c{};
   c.a = a;
   c.d = d;
   c.units = r.units;
   c.n_split = r.n_split;
-  c.total = r.units * d.c.kv_heads * r.n_split;
+  c.n_whole = r.n_whole;
+  c.n_tail = r.n_tail;
+  c.total = r.n_whole + r.n_tail * r.n_split;
   if (c.total >= (1ll << 31)) return SOL_ATTN3D_ERR_UNSUPPORTED_SHAPE;
   c.tok_per_tile = r.tok_per_tile;
+  c.inv_group = (65536u + r.group - 1) / r.group;
+  c.lookahead = lookahead;
   if (r.n_split > 1) {
     if (workspace == nullptr || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) % kAlign) != 0) return SOL_ATTN3D_ERR_NO_WORKSPACE;
-    c.partial = static_cast<float*>(workspace);
+    c.join = static_cast<sol::JoinUnit*>(workspace);
+    c.partial = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + join_list_bytes(r));
   }
   c.counter = reinterpret_cast<unsigned int*>(p->ws + p->off_status + kUnitCounterOffset);
   c.status = reinterpret_cast<unsigned int*>(p->ws + p->off_status);
@@ -287,7 +299,8 @@ int forward_context(sol_attn3d_plan_t p, const void* q, void* out, const sol::Ke
       if ((e = cudaEventRecord(p->ev[i], st)) != cudaSuccess) return fail_cuda(p, e);
   }
   const int rc = r.few ? attend_few(a, d, paged, p->head_dim, r.units, capacity, workspace, workspace_bytes, st, &p->launches, &p->last_cuda)
-                       : attend_many(p, a, d, paged, r, workspace, workspace_bytes, context_bytes(p, d.c.kv_heads, capacity, total_rows), st);
+                       : attend_many(p, a, d, paged, r, workspace, workspace_bytes, context_bytes(p, d.c.kv_heads, capacity, total_rows),
+                                     capacity <= 2048 ? 4 : 2, st);   // short units: looking one up must not hold the next ones back
   if (rc != SOL_ATTN3D_OK) return rc;
   if (p->prof) {
     if ((e = cudaEventRecord(p->ev[3], st)) != cudaSuccess) return fail_cuda(p, e);

@@ -101,3 +101,28 @@ def test_no_states_at_all():
     q = torch.randn(300, 2, 64, generator=torch.Generator().manual_seed(4)).bfloat16().cuda()
     assert bool((run([(299, 0, 1, 1), (1, 0, 1, 1)], q, 2, 64, ctx) == 0).all())
     assert bool((run(None, q[:2], 2, 64, ctx, step=True) == 0).all())
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("masked", [False, True])
+def test_many_sequences_most_without_states(d, masked):
+    """Units without any key among units with some, more of them than are drawn ahead; fewer and more sequences than are sorted."""
+    from paper_2609_35110_b200 import binding as B
+    for n_seqs in (6, 32, 33, 50):
+        sizes = [40, 1, 700, 300, 129, 2000][:6] + [((37 * i) % 300) + 1 for i in range(n_seqs - 6)]
+        lens = [130, 5, 0, 300, 0, 0] + [0 if i % 3 else 20 + i for i in range(n_seqs - 6)]
+        kv_t, begins = contexts(lens, 2, d, seed=n_seqs)
+        mask = None
+        if masked:
+            mask = torch.ones(kv_t.shape[0], dtype=torch.uint8)
+            mask[begins[0]:begins[0] + 130] = 0
+            mask[begins[3]:begins[3] + 290] = 0
+        dev = kv_t.cuda()
+        ctx = B.sol_attn3d_context(dev[:, 0], dev[:, 1], ints(begins), ints(lens), max(lens), key_mask=None if mask is None else mask.cuda())
+        q = torch.randn(sum(sizes), 4, d, generator=torch.Generator().manual_seed(1)).bfloat16()
+        out = run([(n, 0, 1, 1) for n in sizes], q.cuda(), 4, d, ctx)
+        at = 0
+        for m, b, n in zip(sizes, begins, lens):
+            ref, mag = so.attend(q[at:at + m], kv_t[b:b + n, 0], kv_t[b:b + n, 1], so.key_limits(m, n, 0), None if mask is None else mask[b:b + n].bool())
+            close(out[at:at + m], ref, mag)
+            at += m

@@ -305,3 +305,13 @@ def test_pages_beyond_4_gib(n_new):
     out = run_chunk([(n_new, 0, 1, 1)], [0], c, kv, q.cuda())
     ref, mag = so.attend(q, kr[:250], vr[:250], so.key_limits(n_new, 250, 0))
     close(out, ref, mag)
+
+
+def test_many_streams_with_split_keys():
+    """A whole wave of units and a rest whose keys are split; some streams empty, some idle, rows that see nothing."""
+    lens = [4000, 0, 2500, 700, 3000, 20]
+    seqs = [(700, 0, 1, 1), (40, 0, 1, 1), (300, 0, 1, 1), (130, 0, 1, 1), (1, 0, 1, 1), (100, 0, 1, 1), (257, 0, 1, 1)]
+    for heads, kv, d in ((24, 24, 64), (30, 6, 128), (3, 1, 64)):
+        c = Cache(lens, 32, kv, d, seed=heads, layers=1, layer=0)
+        check_chunk(seqs, [2, 1, 0, 9, 4, 5, 3], c, heads, 0)
+        check_chunk(seqs, [2, 1, 0, 9, 4, 5, 3], c, heads, 130)
