@@ -360,7 +360,7 @@ __global__ void __launch_bounds__(kFewThreads, kFewResident) few_rows_kernel(con
 }
 
 // Joins the parts of split keys, in the order of the splits.  Rows of partial results: D values, maximum, sum, "has a valid key".
-// One thread per 8 dims of a row; a CTA per unit and K/V head.  Whose rows a unit holds follows from its number (few rows), or was
+// One thread per 8 dims of a row; CTAs (unit and K/V head, 256 such pieces).  Whose rows a unit holds follows from its number (few rows), or was
 // written down by who made them (kListed).
 struct JoinUnit {
   long long tok0;
@@ -414,7 +414,8 @@ __global__ void __launch_bounds__(256) join_rows_kernel(const __grid_constant__ 
   if (n_rows <= 0) return;
   constexpr int kChunks = D / 8;
   const float* part = p.partial + (long long)blockIdx.x * p.n_split * p.rows_per_unit * (D + 4);
-  for (int x = threadIdx.x; x < n_rows * kChunks; x += blockDim.x) {
+  const int x = blockIdx.y * 256 + threadIdx.x;
+  if (x < n_rows * kChunks) {
     const int row = x / kChunks, d0 = (x % kChunks) * 8;
     const float* mine = part + (long long)row * (D + 4);
     const long long step = (long long)p.rows_per_unit * (D + 4);

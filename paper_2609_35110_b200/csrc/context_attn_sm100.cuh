@@ -84,7 +84,7 @@ __device__ __forceinline__ uint32_t below(int limit, int first) {
   return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u;
 }
 
-template <int D, bool kPaged>
+template <int D, bool kPaged, bool kMask>
 __global__ void __launch_bounds__(kAttnThreads, 1)
 context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                     const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ ContextParams p) {
@@ -178,7 +178,7 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       if (un.last) break;
       if (t >= un.n_tiles) { release_unit(u); continue; }
       const int tile_begin = un.tile_begin, tile_end = un.tile_end, lim_all = un.lim[t];
-      const uint8_t* mask = un.span.mask;
+      const uint8_t* mask = kMask ? un.span.mask : nullptr;
       const int cap = un.span.cap;
       const int tok = un.t0 + t * p.tok_per_tile + (int)(row * p.inv_group >> 16);       // this thread's new token
       const bool mine = row < tile_rows && tok < un.n_tok;
@@ -195,17 +195,24 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         }
         return w;
       };
-      if (mask != nullptr && tile_begin < tile_end) next_mask = fetch_mask(tile_begin);
+      if (kMask && tile_begin < tile_end) next_mask = fetch_mask(tile_begin);
 
       for (int jt = tile_begin; jt < tile_end; ++jt, ++n_s) {
         const uint32_t mask_bits = next_mask;
-        if (mask != nullptr && jt + 1 < tile_end) next_mask = fetch_mask(jt + 1);
+        if (kMask && jt + 1 < tile_end) next_mask = fetch_mask(jt + 1);
         ok = mbar_wait_warp(bar_s_full(t), n_s & 1, limit);
         if (!ok) break;
         tc_fence_after();
-        const bool whole = mask == nullptr && (jt + 1) * 128 <= lim_all;
+        bool whole = (jt + 1) * 128 <= lim_all;            // all 128 keys count for all rows of the tile
+        uint32_t bits[4] = {~0u, ~0u, ~0u, ~0u};           // the mask's word on them
+        if (kMask) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) bits[e] = __ballot_sync(0xffffffffu, (mask_bits >> e) & 1u);
+          whole = whole && (bits[0] & bits[1] & bits[2] & bits[3]) == ~0u;
+        }
         // In two halves: the second half of S is still on its way while the first is exponentiated, and the first half of P is on
-        // its way to tensor memory while the second is.  (Also fewer registers: 128 scores and 32 packed pairs at a time.)
+        // its way to tensor memory while the second is.  (Also fewer registers: 128 scores and 32 packed pairs at a time.)  The common
+        // case has a copy of its own, and so has the redo: with one copy for all the kernel took 5 % longer, as a loop 30 %.
         uint32_t r[128];
         uint32_t (&r_lo)[64] = *reinterpret_cast<uint32_t(*)[64]>(&r[0]);
         uint32_t (&r_hi)[64] = *reinterpret_cast<uint32_t(*)[64]>(&r[64]);
@@ -215,13 +222,21 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         tmem_wait_ld_dep64(r_lo);
         tmem_ld32(tS + 64, *reinterpret_cast<uint32_t(*)[32]>(&r[64]));
         tmem_ld32(tS + 96, *reinterpret_cast<uint32_t(*)[32]>(&r[96]));
-        if (!whole || !started) {
+        float acc[4];
+        if (whole && started) {
+          const float mc = m_ref * c;
+          acc[0] = acc[1] = acc[2] = acc[3] = 0.f;
+          softmax_half(r_lo, c, mc, pk, acc);
+          tmem_wait_ld_dep64(r_hi);
+          tmem_st32(tS, pk);
+          softmax_half(r_hi, c, mc, pk, acc);
+          seen = true;
+        } else {
           tmem_wait_ld_dep64(r_hi);
           if (!whole) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              uint32_t valid = below(lim, jt * 128 + e * 32);
-              if (mask != nullptr) valid &= __ballot_sync(0xffffffffu, (mask_bits >> e) & 1u);
+              const uint32_t valid = below(lim, jt * 128 + e * 32) & bits[e];
               seen = seen || valid != 0;
 #pragma unroll
               for (int cc = 0; cc < 32; ++cc)
@@ -231,18 +246,11 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
           // a row takes its reference from its first tile with a valid key; before that every term is 2^-inf
           if (m_ref == -CUDART_INF_F) m_ref = row_max128(r);
           started = __all_sync(0xffffffffu, !mine || m_ref != -CUDART_INF_F);
-        }
-        seen = seen || whole;
-        float acc[4];
-        auto first_half = [&](float mc) {
+          seen = seen || whole;
+          const float mc = m_ref == -CUDART_INF_F ? 0.f : m_ref * c;
           acc[0] = acc[1] = acc[2] = acc[3] = 0.f;
           softmax_half(r_lo, c, mc, pk, acc);
-          tmem_wait_ld_dep64(r_hi);
-          tmem_st32(tS, pk);                               // columns [0,32): their scores are in registers
-        };
-        {
-          const float mc = m_ref == -CUDART_INF_F ? 0.f : m_ref * c;
-          first_half(mc);
+          tmem_st32(tS, pk);
           softmax_half(r_hi, c, mc, pk, acc);
         }
         // No row maximum was taken.  All terms are positive, so a sum <= 2^8 proves that every term is; otherwise, if the maximum
@@ -269,14 +277,16 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 tmem_st16(tO + cch * 16, o);
               }
             }
-            tmem_wait_st();                                // the stale first half lands before its replacement
+            tmem_wait_st();                                // the stale P lands before its replacement
             const float mc = m_ref == -CUDART_INF_F ? 0.f : m_ref * c;
-            first_half(mc);
+            acc[0] = acc[1] = acc[2] = acc[3] = 0.f;
+            softmax_half(r_lo, c, mc, pk, acc);
+            tmem_st32(tS, pk);
             softmax_half(r_hi, c, mc, pk, acc);
           }
         }
-        l += (acc[0] + acc[1]) + (acc[2] + acc[3]);
         tmem_st32(tS + 32, pk);
+        l += (acc[0] + acc[1]) + (acc[2] + acc[3]);
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
@@ -309,44 +319,50 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         }
         if (mine) *reinterpret_cast<float4*>(dst + D) = make_float4(m_ref, l, seen ? 1.f : 0.f, 0.f);
       } else {
-        // Rows are staged 64 columns at a time (16-byte chunks XOR-swizzled by row) and written with eight lanes per row.
+        // Rows are staged 64 columns at a time (16-byte chunks XOR-swizzled by row) and written with eight lanes per row, four rows
+        // at a time; a lane's eight places are found first, so that its stores follow one another.
         const float inv = 1.0f / l;
         uint8_t* stage = smem + L::kOffStage + warp * 4096;
+        int own = lane;
+        asm volatile("" : "+r"(own));                      // keeps what follows from it out of the registers of the main loop
+        const int first_tok = un.t0 + t * p.tok_per_tile, left = un.n_tok - first_tok, ch = own & 7;
+        __nv_bfloat16* base = p.a.out + (un.tok0 + first_tok) * p.a.o_tok + (long long)(un.kv_head * group) * p.a.o_head + ch * 8;
+        __nv_bfloat16* place[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int tile_row = wq * 32 + 4 * e + (own >> 3);
+          const int in_tile = (int)(tile_row * p.inv_group >> 16);         // token of the tile
+          place[e] = tile_row < tile_rows && in_tile < left ? base + in_tile * p.a.o_tok + (tile_row - in_tile * group) * p.a.o_head : nullptr;
+        }
+        const uint64_t pol_once = l2_policy_evict_first();
 #pragma unroll 1
         for (int hf = 0; hf < L::kHalves; ++hf) {
+          uint32_t o[64];                                  // (without key tiles: whatever is there, and not used)
+          tmem_ld32(tO + hf * 64, *reinterpret_cast<uint32_t(*)[32]>(&o[0]));
+          tmem_ld32(tO + hf * 64 + 32, *reinterpret_cast<uint32_t(*)[32]>(&o[32]));
+          tmem_wait_ld_dep64(o);
           __syncwarp();
 #pragma unroll
-          for (int part = 0; part < 2; ++part) {
-            uint32_t o[32];
-            if (tile_begin < tile_end) {
-              tmem_ld32(tO + hf * 64 + part * 32, o);
-              tmem_wait_ld();
+          for (int v = 0; v < 8; ++v) {
+            uint4 w = make_uint4(0u, 0u, 0u, 0u);          // a row without a valid key is zeros
+            if (seen) {
+              w.x = pack_bf16x2(__uint_as_float(o[8 * v + 0]) * inv, __uint_as_float(o[8 * v + 1]) * inv);
+              w.y = pack_bf16x2(__uint_as_float(o[8 * v + 2]) * inv, __uint_as_float(o[8 * v + 3]) * inv);
+              w.z = pack_bf16x2(__uint_as_float(o[8 * v + 4]) * inv, __uint_as_float(o[8 * v + 5]) * inv);
+              w.w = pack_bf16x2(__uint_as_float(o[8 * v + 6]) * inv, __uint_as_float(o[8 * v + 7]) * inv);
             }
-#pragma unroll
-            for (int v4 = 0; v4 < 4; ++v4) {
-              uint4 w = make_uint4(0u, 0u, 0u, 0u);        // a row without a valid key is zeros
-              if (seen) {
-                w.x = pack_bf16x2(__uint_as_float(o[8 * v4 + 0]) * inv, __uint_as_float(o[8 * v4 + 1]) * inv);
-                w.y = pack_bf16x2(__uint_as_float(o[8 * v4 + 2]) * inv, __uint_as_float(o[8 * v4 + 3]) * inv);
-                w.z = pack_bf16x2(__uint_as_float(o[8 * v4 + 4]) * inv, __uint_as_float(o[8 * v4 + 5]) * inv);
-                w.w = pack_bf16x2(__uint_as_float(o[8 * v4 + 6]) * inv, __uint_as_float(o[8 * v4 + 7]) * inv);
-              }
-              *reinterpret_cast<uint4*>(stage + lane * 128 + (((part * 4 + v4) ^ (lane & 7)) << 4)) = w;
-            }
+            *reinterpret_cast<uint4*>(stage + own * 128 + ((v ^ ch) << 4)) = w;
           }
           __syncwarp();
-          const uint64_t pol_once = l2_policy_evict_first();
+          uint4 w[8];
 #pragma unroll
-          for (int r0 = 0; r0 < 32; r0 += 4) {
-            const int rr = r0 + (lane >> 3), ch = lane & 7;
-            const int tile_row = wq * 32 + rr;
-            const int in_tile = (int)(tile_row * p.inv_group >> 16);       // token of the tile
-            const int tk = un.t0 + t * p.tok_per_tile + in_tile;
-            const uint4 w = *reinterpret_cast<const uint4*>(stage + rr * 128 + ((ch ^ (rr & 7)) << 4));
-            if (tile_row < tile_rows && tk < un.n_tok)
-              st_global_evict_first(p.a.out + (un.tok0 + tk) * p.a.o_tok + (long long)(un.kv_head * group + tile_row - in_tile * group) * p.a.o_head +
-                                        hf * 64 + ch * 8, w, pol_once);
+          for (int e = 0; e < 8; ++e) {
+            const int rr = 4 * e + (own >> 3);
+            w[e] = *reinterpret_cast<const uint4*>(stage + rr * 128 + ((ch ^ (rr & 7)) << 4));
           }
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (place[e] != nullptr) st_global_evict_first(place[e] + hf * 64, w[e], pol_once);
         }
       }
       release_unit(u);
@@ -675,17 +691,17 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       const UnitDev& un = units[u & (kUnitRing - 1)];
       if (un.last) break;
       const int tile_begin = un.tile_begin, tile_end = un.tile_end, cap = un.span.cap;
-      const uint8_t* mask = un.span.mask;
+      const uint8_t* mask = kMask ? un.span.mask : nullptr;
       release_unit(u);
       for (int jt = tile_begin; jt < tile_end; ++jt) {
         const uint32_t v_it = it + 1, stage = v_it % L::kStages;
         it += 2;
         uint32_t drop = 0;                                 // bit e: key 32 e + lane of the tile does not count
-        if (mask != nullptr || (jt + 1) * 128 > cap) {
+        if (kMask || (jt + 1) * 128 > cap) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int key = jt * 128 + e * 32 + lane;
-            if (key >= cap || (mask != nullptr && __ldg(mask + key) == 0)) drop |= 1u << e;
+            if (key >= cap || (kMask && __ldg(mask + key) == 0)) drop |= 1u << e;
           }
         }
         if (!mbar_wait_warp(bar_kv_full(stage), (v_it / L::kStages) & 1, limit)) { ok = false; break; }

@@ -96,7 +96,7 @@ cudaError_t launch_few(const sol::FewArgs& f, cudaStream_t st, int* launches) {
   ++*launches;
   if (f.partial != nullptr) {
     const sol::JoinArgs j{f.a, f.d, f.n_split, sol::kFewRows, f.units, f.partial, nullptr};
-    sol::join_rows_kernel<D, kPaged, false><<<items, 256, 0, st>>>(j);
+    sol::join_rows_kernel<D, kPaged, false><<<dim3(items, (sol::kFewRows * D / 8 + 255) / 256), 256, 0, st>>>(j);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
     ++*launches;
   }
@@ -199,20 +199,25 @@ int encode_boxes(sol_attn3d_plan_t p, CUtensorMap* tm, const void* base, int ran
   return SOL_ATTN3D_ERR_CUDA;
 }
 
-template <int D, bool kPaged>
-cudaError_t launch_context(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const sol::ContextParams& c, int sms, cudaStream_t st, int* launches) {
-  cudaError_t e = cudaFuncSetAttribute(sol::context_attn_kernel<D, kPaged>, cudaFuncAttributeMaxDynamicSharedMemorySize, sol::ContextSmem<D>::kDynBytes);
+template <int D, bool kPaged, bool kMask>
+cudaError_t launch_context_as(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const sol::ContextParams& c, int sms, cudaStream_t st, int* launches) {
+  cudaError_t e = cudaFuncSetAttribute(sol::context_attn_kernel<D, kPaged, kMask>, cudaFuncAttributeMaxDynamicSharedMemorySize, sol::ContextSmem<D>::kDynBytes);
   if (e != cudaSuccess) return e;
-  sol::context_attn_kernel<D, kPaged><<<(unsigned)std::min<long long>(c.total, sms), sol::kAttnThreads, sol::ContextSmem<D>::kDynBytes, st>>>(q, k, v, c);
+  sol::context_attn_kernel<D, kPaged, kMask><<<(unsigned)std::min<long long>(c.total, sms), sol::kAttnThreads, sol::ContextSmem<D>::kDynBytes, st>>>(q, k, v, c);
   if ((e = cudaGetLastError()) != cudaSuccess) return e;
   ++*launches;
   if (c.partial != nullptr) {
     const sol::JoinArgs j{c.a, c.d, c.n_split, 2 * c.tok_per_tile * c.a.group, c.units, c.partial, c.join};
-    sol::join_rows_kernel<D, kPaged, true><<<(unsigned)c.n_tail, 256, 0, st>>>(j);
+    sol::join_rows_kernel<D, kPaged, true><<<dim3((unsigned)c.n_tail, (unsigned)(j.rows_per_unit * D / 8 + 255) / 256), 256, 0, st>>>(j);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
     ++*launches;
   }
   return cudaSuccess;
+}
+
+template <int D, bool kPaged>
+cudaError_t launch_context(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const sol::ContextParams& c, int sms, cudaStream_t st, int* launches) {
+  return c.d.mask != nullptr ? launch_context_as<D, kPaged, true>(q, k, v, c, sms, st, launches) : launch_context_as<D, kPaged, false>(q, k, v, c, sms, st, launches);
 }
 
 int attend_many(sol_attn3d_plan_t p, const sol::QueriesDev& a, const sol::KeysDev& d, bool paged, const ContextRoute& r, void* workspace,
