@@ -94,16 +94,28 @@ __device__ __forceinline__ int find_sequence(const QueriesDev& a, long long unit
 // 256 operations per key and bind long before HBM does; a tcgen05 tile has 128 rows, of which 16 or fewer would be filled, and
 // its operands would have to go through shared memory.
 //
-// Nothing is staged: lanes load 16 bytes of global memory straight into operand registers.  A product does not care for the order
-// of the index that it sums over, so the K dims of a 32-dim step are assigned such that a lane's operand registers are eight
-// neighbouring dims of one key: lane 4 g + c has dims 8 c .. 8 c + 7 of keys g and g + 8.  For P V the summed index is the key, two
-// to a register: lane 4 g + c loads dims 8 g .. 8 g + 7 of keys 2 c, 2 c + 1, 2 c + 8, 2 c + 9 and pairs them with byte permutes; output
-// column g of product e is dim 8 g + e, which leaves a lane with 16 neighbouring dims of its two rows.
+// Every warp has a ring of its own in shared memory that cp.async fills, some blocks ahead (rows padded by 16 bytes, so that the eight
+// rows of an ldmatrix lie in different banks); no barrier but the warp's.  Masked keys are not read: their place is zeros, whatever
+// the cache holds there.  K goes to the tensor core as it lies, V through the transposing ldmatrix.
 //
-// Softmax in fp32 with a running maximum per row; P is rounded to bf16 for the product (its row sum is of the unrounded values), as
-// in the dense kernel.  Keys are split over CTAs when there are few units; the parts are joined in a fixed order.
+// Softmax in fp32 with a running maximum per row.  P is held as two bf16 parts, most of p and what that leaves, whose products with V are
+// added: the tensor core has time (48 of its instructions per 16 keys; HBM allows 350 cycles for them), and the error is then the
+// output's own rounding (0.0017 relative, 0.0020 with one part).  Keys are split over CTAs when there are few units; the parts are
+// joined in a fixed order.
 // ---------------------------------------------------------------------------------------------
 constexpr int kFewRows = 16, kFewWarps = 4, kFewThreads = 32 * kFewWarps, kFewResident = 3;
+
+template <int D>
+struct FewSmem {
+  static constexpr int kPitch = D * 2 + 16;               // bytes of a row
+  static constexpr int kBlock = 16 * kPitch;              // 16 keys of K, or of V
+  static constexpr int kStages = D == 128 ? 2 : 4;
+  static constexpr int kRing = kStages * 2 * kBlock;      // per warp
+  static constexpr int kOffValid = kFewWarps * kRing;     // validity of the keys of a stage, 32 bits per warp and stage
+  static constexpr int kOffStats = kOffValid + kFewWarps * kStages * 4;
+  static constexpr int kBytes = (kOffStats + kFewWarps * kFewRows * 12 + 15) / 16 * 16;
+  static_assert(kRing >= kFewRows * (D + 4) * 4, "a warp's partial rows replace its ring at the end");
+};
 
 struct FewArgs {
   QueriesDev a;
@@ -118,14 +130,11 @@ __device__ __forceinline__ void mma_bf16_16816(float (&c)[4], uint32_t a0, uint3
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
 template <int D, bool kPaged>
 __global__ void __launch_bounds__(kFewThreads, kFewResident) few_rows_kernel(const __grid_constant__ FewArgs p) {
-  constexpr int kK = D / 32, kV = D / 64;               // 16-byte loads per key: of K by a quad, of V by eight lanes
-  __shared__ float s_o[kFewWarps][kFewRows][D + 4];
-  __shared__ float s_m[kFewWarps][kFewRows], s_l[kFewWarps][kFewRows];
-  __shared__ int s_seen[kFewWarps][kFewRows];
+  using L = FewSmem<D>;
+  extern __shared__ __align__(16) uint8_t few_smem[];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
 
   // ---- which rows, which keys
@@ -156,16 +165,19 @@ __global__ void __launch_bounds__(kFewThreads, kFewResident) few_rows_kernel(con
 
   // ---- the two rows of this lane's quad: tile rows g and g + 8
   int limit[2];
-  uint4 q[2][kK];
+  uint32_t q[D / 16][4];                                // operand registers: [dims 16 k + 2 c, + 1, then + 8][row]
 #pragma unroll
   for (int r = 0; r < 2; ++r) {
     const int row = row0 + g + 8 * r;
     const bool there = g + 8 * r < n_rows;
     const int tok = there ? row / p.a.group : 0, h = there ? row % p.a.group : 0;
     limit[r] = there ? key_limit(sp, n_tok, tok, p.a.causal) : 0;
-    const __nv_bfloat16* src = p.a.q + (tok0 + tok) * p.a.q_tok + ((long long)kv_head * p.a.group + h) * p.a.q_head + c * 8;
+    const __nv_bfloat16* src = p.a.q + (tok0 + tok) * p.a.q_tok + ((long long)kv_head * p.a.group + h) * p.a.q_head + 2 * c;
 #pragma unroll
-    for (int j = 0; j < kK; ++j) q[r][j] = there ? __ldg(reinterpret_cast<const uint4*>(src + j * 32)) : make_uint4(0, 0, 0, 0);
+    for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+        q[k][2 * half + r] = there ? __ldg(reinterpret_cast<const unsigned int*>(src + 16 * k + 8 * half)) : 0u;
   }
   const int last_tok = (row0 + n_rows - 1) / p.a.group;
   const int most = key_limit(sp, n_tok, last_tok, p.a.causal);            // limits grow with the token
@@ -175,74 +187,118 @@ __global__ void __launch_bounds__(kFewThreads, kFewResident) few_rows_kernel(con
   const int per_split = ((blocks + p.n_split - 1) / p.n_split + kFewWarps - 1) / kFewWarps * kFewWarps;
   const int b_end = (int)min((long long)blocks, (long long)(split + 1) * per_split);
 
-  float o[kV * 8][4];
+  // ---- the warp's ring
+  const uint32_t ring = smem_u32(few_smem) + warp * L::kRing;
+  uint32_t* valid_of = reinterpret_cast<uint32_t*>(few_smem + L::kOffValid) + warp * L::kStages;
+  const int b_first = split * per_split + warp;
+  constexpr int kChunks16 = D / 8;                      // 16-byte chunks of a row
+  const int chunk = lane % kChunks16, row_first = lane / kChunks16;
+  constexpr int kRowStep = 32 / kChunks16;
+  const __nv_bfloat16* kh = p.d.c.k + kv_head * p.d.c.ks[2] + chunk * 8;
+  const __nv_bfloat16* vh = p.d.c.v + kv_head * p.d.c.vs[2] + chunk * 8;
+  const long long k_step = kRowStep * p.d.c.ks[1], v_step = kRowStep * p.d.c.vs[1];
+  // What a block needs before its loads can start is fetched a turn earlier: its page, and the mask's word on its keys.  Its place among
+  // the pages moves with it (four blocks a turn), without a division.
+  const int page = kPaged ? p.d.c.page : 1, page_cols = 16 * kFewWarps / page, page_rows = 16 * kFewWarps % page;
+  int col = kPaged ? b_first * 16 / page : 0, in_page = kPaged ? b_first * 16 % page : 0;
+  int page_ahead = 0, row_ahead = 0;
+  bool on_ahead = false;
+  auto look_up = [&](int b) {
+    if (b >= b_end) return;
+    if (kPaged) {
+      page_ahead = __ldg(sp.table + col);
+      row_ahead = in_page;
+      col += page_cols;
+      in_page += page_rows;
+      if (in_page >= page) { in_page -= page; ++col; }
+    }
+    const int key = b * 16 + (lane & 15);
+    on_ahead = key < most && (sp.mask == nullptr || __ldg(sp.mask + key) != 0);
+  };
+  auto fetch = [&](int b, int stage) {                  // block b of 16 keys into a stage; the next one's look-up
+    if (b < b_end) {
+      uint32_t valid = __ballot_sync(0xffffffffu, on_ahead) & 0xffffu;
+      if (lane == 0) valid_of[stage] = valid;
+      long long krow, vrow;
+      if (kPaged) {                                     // (a page holds whole blocks: its size is a multiple of 16)
+        const bool there = page_ahead >= 0 && page_ahead < p.d.c.n_pages;
+        const long long at = there ? page_ahead : 0;    // no such page: zeros, and an address that there is
+        krow = at * p.d.c.ks[0] + row_ahead * p.d.c.ks[1];
+        vrow = at * p.d.c.vs[0] + row_ahead * p.d.c.vs[1];
+        if (!there) valid = 0;
+      } else {
+        krow = (sp.begin + b * 16) * p.d.c.ks[1];
+        vrow = (sp.begin + b * 16) * p.d.c.vs[1];
+      }
+      const __nv_bfloat16* ksrc = kh + krow + row_first * p.d.c.ks[1];
+      const __nv_bfloat16* vsrc = vh + vrow + row_first * p.d.c.vs[1];
+      const uint32_t dst = ring + stage * 2 * L::kBlock + row_first * L::kPitch + chunk * 16;
+      if (valid == 0xffffu) {
 #pragma unroll
-  for (int t = 0; t < kV * 8; ++t)
+        for (int i = 0; i < 16 / kRowStep; ++i, ksrc += k_step, vsrc += v_step) {
+          cp_async_16(dst + i * kRowStep * L::kPitch, ksrc, 16);
+          cp_async_16(dst + L::kBlock + i * kRowStep * L::kPitch, vsrc, 16);
+        }
+      } else {
+        valid >>= row_first;
+#pragma unroll
+        for (int i = 0; i < 16 / kRowStep; ++i, ksrc += k_step, vsrc += v_step) {
+          const bool on = (valid >> (i * kRowStep)) & 1u;
+          // (a key that is not read keeps its address inside a page; behind the last row of a context there may be no memory)
+          cp_async_16(dst + i * kRowStep * L::kPitch, kPaged || on ? ksrc : p.d.c.k, on ? 16 : 0);
+          cp_async_16(dst + L::kBlock + i * kRowStep * L::kPitch, kPaged || on ? vsrc : p.d.c.v, on ? 16 : 0);
+        }
+      }
+      look_up(b + kFewWarps);
+    }
+    cp_async_commit();
+  };
+  look_up(b_first);
+#pragma unroll
+  for (int s = 0; s < L::kStages - 1; ++s) fetch(b_first + s * kFewWarps, s);
+
+  float o[D / 8][4];
+#pragma unroll
+  for (int t = 0; t < D / 8; ++t)
 #pragma unroll
     for (int e = 0; e < 4; ++e) o[t][e] = 0.f;
   float m[2] = {-CUDART_INF_F, -CUDART_INF_F}, l[2] = {0.f, 0.f};
   bool seen[2] = {false, false};
   const float sc = p.a.scale_log2;
-  const __nv_bfloat16* kh = p.d.c.k + kv_head * p.d.c.ks[2] + c * 8;
-  const __nv_bfloat16* vh = p.d.c.v + kv_head * p.d.c.vs[2] + g * 8;
+  // an ldmatrix lane's row: of K, keys (lane & 7) + 8 (lane >> 4), dims + 8 for odd (lane >> 3); of V, keys lane & 15, dims + 8 (lane >> 4)
+  const uint32_t k_lane = ((lane & 7) + 8 * (lane >> 4)) * L::kPitch + ((lane >> 3) & 1) * 16;
+  const uint32_t v_lane = (lane & 15) * L::kPitch + (lane >> 4) * 16;
 
-  for (int b = split * per_split + warp; b < b_end; b += kFewWarps) {
+  int stage = 0;
+  for (int b = b_first; b < b_end; b += kFewWarps) {
+    fetch(b + (L::kStages - 1) * kFewWarps, stage == 0 ? L::kStages - 1 : stage - 1);
+    cp_async_wait<L::kStages - 1>();
+    __syncwarp();
     const int key0 = b * 16;
-    // ---- where these 16 keys are (a page holds whole blocks: its size is a multiple of 16)
-    long long krow, vrow;
-    bool there = true;
-    if (kPaged) {
-      const int page = __ldg(sp.table + key0 / p.d.c.page), in_page = key0 % p.d.c.page;
-      there = page >= 0 && page < p.d.c.n_pages;
-      krow = page * p.d.c.ks[0] + in_page * p.d.c.ks[1];
-      vrow = page * p.d.c.vs[0] + in_page * p.d.c.vs[1];
-    } else {
-      krow = (sp.begin + key0) * p.d.c.ks[1];
-      vrow = (sp.begin + key0) * p.d.c.vs[1];
-    }
-    const bool whole = key0 + 16 <= most;
-    uint4 kx[2][kK], vx[4][kV];
+    const uint32_t k_at = ring + stage * 2 * L::kBlock + k_lane, v_at = ring + stage * 2 * L::kBlock + L::kBlock + v_lane;
+    const uint32_t valid = valid_of[stage];
+    // ---- scores: [t] keys 8 t + 2 c, + 1; entries 0, 1 of row g, 2, 3 of row g + 8 (two chains of products each)
+    float s[2][4], s2[2][4];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const int key = g + 8 * t;
-      const bool on = there && (whole || key0 + key < most);
-      const __nv_bfloat16* src = kh + krow + key * p.d.c.ks[1];
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int j = 0; j < kK; ++j) kx[t][j] = on ? __ldg(reinterpret_cast<const uint4*>(src + j * 32)) : make_uint4(0, 0, 0, 0);
-    }
+      for (int e = 0; e < 4; ++e) s[t][e] = s2[t][e] = 0.f;
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const int key = 2 * c + (t & 1) + 8 * (t >> 1);
-      const bool on = there && (whole || key0 + key < most);
-      const __nv_bfloat16* src = vh + vrow + key * p.d.c.vs[1];
+    for (int k = 0; k < D / 16; k += 2) {
+      uint32_t x[4], y[4];
+      ldmatrix_x4(k_at + k * 32, x);
+      ldmatrix_x4(k_at + k * 32 + 32, y);
 #pragma unroll
-      for (int j = 0; j < kV; ++j) vx[t][j] = on ? __ldg(reinterpret_cast<const uint4*>(src + j * 64)) : make_uint4(0, 0, 0, 0);
-    }
-    uint32_t valid = 0xffffu;
-    if (sp.mask != nullptr) {
-      const bool on = key0 + (lane & 15) < most && __ldg(sp.mask + key0 + (lane & 15)) != 0;
-      valid = __ballot_sync(0xffffffffu, on) & 0xffffu;
-      if (valid == 0) continue;
-      // values of keys that do not count may be anything: they become zeros
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-        if (((valid >> (2 * c + (t & 1) + 8 * (t >> 1))) & 1u) == 0)
-#pragma unroll
-          for (int j = 0; j < kV; ++j) vx[t][j] = make_uint4(0, 0, 0, 0);
-    }
-    // ---- scores: [t] keys 8 t + 2 c, + 1; entries 0, 1 of row g, 2, 3 of row g + 8
-    float s[2][4];
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) s[t][e] = 0.f;
-#pragma unroll
-      for (int j = 0; j < kK; ++j) {
-        mma_bf16_16816(s[t], q[0][j].x, q[1][j].x, q[0][j].y, q[1][j].y, kx[t][j].x, kx[t][j].y);
-        mma_bf16_16816(s[t], q[0][j].z, q[1][j].z, q[0][j].w, q[1][j].w, kx[t][j].z, kx[t][j].w);
+      for (int t = 0; t < 2; ++t) {
+        mma_bf16_16816(s[t], q[k][0], q[k][1], q[k][2], q[k][3], x[2 * t], x[2 * t + 1]);
+        mma_bf16_16816(s2[t], q[k + 1][0], q[k + 1][1], q[k + 1][2], q[k + 1][3], y[2 * t], y[2 * t + 1]);
       }
     }
-    if (valid != 0xffffu || key0 + 16 > least) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[t][e] += s2[t][e];
+    if (key0 + 16 > least && least < most) {            // the rows do not see the same keys
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -253,7 +309,15 @@ __global__ void __launch_bounds__(kFewThreads, kFewResident) few_rows_kernel(con
           seen[e >> 1] = seen[e >> 1] || on;
         }
     } else {
-      seen[0] = seen[1] = true;
+      if (valid != 0xffffu) {
+        const uint32_t mine = valid >> (2 * c);         // bits 0, 1, 8, 9: this lane's keys
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+            if (((mine >> (8 * t + e)) & 1u) == 0) s[t][e] = s[t][2 + e] = -CUDART_INF_F;
+      }
+      seen[0] = seen[1] = seen[0] || valid != 0;        // (rows that the unit does not have: not written)
     }
     // ---- running maximum of the row, over the quad
     float scale[2];
@@ -270,35 +334,46 @@ __global__ void __launch_bounds__(kFewThreads, kFewResident) few_rows_kernel(con
     }
     if (__any_sync(0xffffffffu, scale[0] != 1.f || scale[1] != 1.f)) {
 #pragma unroll
-      for (int t = 0; t < kV * 8; ++t) {
+      for (int t = 0; t < D / 8; ++t) {
         o[t][0] *= scale[0]; o[t][1] *= scale[0];
         o[t][2] *= scale[1]; o[t][3] *= scale[1];
       }
       l[0] *= scale[0];
       l[1] *= scale[1];
     }
-    uint32_t pa[4];
+    uint32_t hi[4], lo[4];
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
         const float p0 = ex2_approx(fmaf(s[t][2 * r], sc, -base[r])), p1 = ex2_approx(fmaf(s[t][2 * r + 1], sc, -base[r]));
         l[r] += p0 + p1;
-        pa[2 * t + r] = pack_bf16x2(p0, p1);
+        // (the larger part stays below p, so that both are positive: an infinite value times them is not inf - inf, nor inf * 0)
+        const uint32_t h0 = __float_as_uint(p0 * 0.99609375f) & 0xffff0000u, h1 = __float_as_uint(p1 * 0.99609375f) & 0xffff0000u;
+        hi[2 * t + r] = __byte_perm(h0, h1, 0x7632);
+        lo[2 * t + r] = pack_bf16x2(p0 - __uint_as_float(h0), p1 - __uint_as_float(h1));
       }
     // ---- O += P V
 #pragma unroll
-    for (int j = 0; j < kV; ++j)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const uint32_t pick = (e & 1) ? 0x7632u : 0x5410u;
-        const uint32_t b0 = __byte_perm(word(vx[0][j], e >> 1), word(vx[1][j], e >> 1), pick);
-        const uint32_t b1 = __byte_perm(word(vx[2][j], e >> 1), word(vx[3][j], e >> 1), pick);
-        mma_bf16_16816(o[j * 8 + e], pa[0], pa[1], pa[2], pa[3], b0, b1);
-      }
+    for (int j = 0; j < D / 8; j += 2) {
+      uint32_t x[4];
+      ldmatrix_x4_trans(v_at + j * 16, x);
+      mma_bf16_16816(o[j], hi[0], hi[1], hi[2], hi[3], x[0], x[1]);
+      mma_bf16_16816(o[j + 1], hi[0], hi[1], hi[2], hi[3], x[2], x[3]);
+      mma_bf16_16816(o[j], lo[0], lo[1], lo[2], lo[3], x[0], x[1]);
+      mma_bf16_16816(o[j + 1], lo[0], lo[1], lo[2], lo[3], x[2], x[3]);
+    }
+    __syncwarp();                                       // the stage is filled again in the next turn
+    if (++stage == L::kStages) stage = 0;
   }
+  cp_async_wait<0>();
+  __syncwarp();
 
-  // ---- the four warps' parts
+  // ---- the four warps' parts: rows in place of the warp's ring, statistics beside them
+  auto rows_of = [&](int w) { return reinterpret_cast<float*>(few_smem + w * L::kRing); };
+  float* s_m = reinterpret_cast<float*>(few_smem + L::kOffStats);
+  float* s_l = s_m + kFewWarps * kFewRows;
+  int* s_seen = reinterpret_cast<int*>(s_l + kFewWarps * kFewRows);
 #pragma unroll
   for (int r = 0; r < 2; ++r) {
     l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
@@ -308,19 +383,14 @@ __global__ void __launch_bounds__(kFewThreads, kFewResident) few_rows_kernel(con
     any |= __shfl_xor_sync(0xffffffffu, any, 2);
     const int row = g + 8 * r;
     if (c == 0) {
-      s_m[warp][row] = m[r];
-      s_l[warp][row] = l[r];
-      s_seen[warp][row] = any;
+      s_m[warp * kFewRows + row] = m[r];
+      s_l[warp * kFewRows + row] = l[r];
+      s_seen[warp * kFewRows + row] = any;
     }
     if (row < n_rows)
 #pragma unroll
-      for (int j = 0; j < kV; ++j)
-#pragma unroll
-        for (int half = 0; half < 2; ++half)
-#pragma unroll
-          for (int e = 0; e < 8; e += 4)
-            *reinterpret_cast<float4*>(&s_o[warp][row][j * 64 + (2 * c + half) * 8 + e]) =
-                make_float4(o[j * 8 + e][2 * r + half], o[j * 8 + e + 1][2 * r + half], o[j * 8 + e + 2][2 * r + half], o[j * 8 + e + 3][2 * r + half]);
+      for (int j = 0; j < D / 8; ++j)
+        *reinterpret_cast<float2*>(rows_of(warp) + row * (D + 4) + 8 * j + 2 * c) = make_float2(o[j][2 * r], o[j][2 * r + 1]);
   }
   __syncthreads();
   constexpr int kChunks = D / 8;                                            // a thread takes 8 dims of a row
@@ -330,17 +400,18 @@ __global__ void __launch_bounds__(kFewThreads, kFewResident) few_rows_kernel(con
     int any = 0;
 #pragma unroll
     for (int w = 0; w < kFewWarps; ++w) {
-      top = fmaxf(top, s_m[w][row]);
-      any |= s_seen[w][row];
+      top = fmaxf(top, s_m[w * kFewRows + row]);
+      any |= s_seen[w * kFewRows + row];
     }
     float sum = 0.f, acc[8] = {};
 #pragma unroll
     for (int w = 0; w < kFewWarps; ++w) {
-      if (!s_seen[w][row]) continue;
-      const float f = s_m[w][row] == top ? 1.f : ex2_approx((s_m[w][row] - top) * sc);
-      sum = fmaf(s_l[w][row], f, sum);
+      if (!s_seen[w * kFewRows + row]) continue;
+      const float mw = s_m[w * kFewRows + row], f = mw == top ? 1.f : ex2_approx((mw - top) * sc);
+      sum = fmaf(s_l[w * kFewRows + row], f, sum);
+      const float* src = rows_of(w) + row * (D + 4) + d0;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) acc[e] = fmaf(s_o[w][row][d0 + e], f, acc[e]);
+      for (int e = 0; e < 8; ++e) acc[e] = fmaf(src[e], f, acc[e]);
     }
     if (p.partial != nullptr) {
       float* dst = p.partial + (((kv_head * p.units + unit) * p.n_split + split) * kFewRows + row) * (D + 4);

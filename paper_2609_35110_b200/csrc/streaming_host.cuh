@@ -70,14 +70,15 @@ int take_context(const sol_attn3d_context* x, sol::KeysDev* d) {
 }
 
 // ---- attention of few rows ------------------------------------------------------------------------------------------------
-// Splits of the keys: with few units, as many as make three whole waves of resident CTAs; with many, six waves, so that streams of
-// different length even out.  No split below 128 keys of the longest possible past.  Depends on the sizes of the call only (the
-// lengths live on the device).
-constexpr long long kFewWave = 148 * sol::kFewResident, kFewMinKeys = 128, kFewMaxSplit = 256;
+// Splits of the keys: about 1,024 keys of the longest possible past per CTA, so that streams of different length even out; at least
+// what makes three waves of resident CTAs when there are few units, at most eight waves (a table may be far wider than its streams are
+// long, and a CTA without keys still costs its start); never below 256 keys.  Depends on the sizes of the call only (the lengths live
+// on the device).
+constexpr long long kFewWave = 148 * sol::kFewResident, kFewMinKeys = 256, kFewMaxSplit = 256;
 int few_splits(long long items, long long capacity) {
   if (items < 1) return 1;
-  const long long want = 4 * items <= 3 * kFewWave ? 3 * kFewWave / items : (6 * kFewWave + items - 1) / items;
-  return (int)std::max<long long>(1, std::min<long long>(std::min<long long>(want, kFewMaxSplit), capacity / kFewMinKeys));
+  const long long want = std::min(std::max((capacity + 1023) / 1024, 3 * kFewWave / items), (8 * kFewWave + items - 1) / items);
+  return (int)std::max<long long>(1, std::min(std::min(want, kFewMaxSplit), capacity / kFewMinKeys));
 }
 long long few_units(sol_attn3d_plan_t p, int batch, int group) {
   return p != nullptr ? p->total_tokens * group / sol::kFewRows + p->n_seqs : (long long)batch * ((group + sol::kFewRows - 1) / sol::kFewRows);
@@ -90,9 +91,10 @@ size_t few_bytes(long long units, int kv_heads, int head_dim, long long capacity
 template <int D, bool kPaged>
 cudaError_t launch_few(const sol::FewArgs& f, cudaStream_t st, int* launches) {
   const unsigned items = (unsigned)(f.units * f.d.c.kv_heads);
-  sol::few_rows_kernel<D, kPaged><<<items * (unsigned)f.n_split, sol::kFewThreads, 0, st>>>(f);
-  cudaError_t e = cudaGetLastError();
+  cudaError_t e = cudaFuncSetAttribute(sol::few_rows_kernel<D, kPaged>, cudaFuncAttributeMaxDynamicSharedMemorySize, sol::FewSmem<D>::kBytes);
   if (e != cudaSuccess) return e;
+  sol::few_rows_kernel<D, kPaged><<<items * (unsigned)f.n_split, sol::kFewThreads, sol::FewSmem<D>::kBytes, st>>>(f);
+  if ((e = cudaGetLastError()) != cudaSuccess) return e;
   ++*launches;
   if (f.partial != nullptr) {
     const sol::JoinArgs j{f.a, f.d, f.n_split, sol::kFewRows, f.units, f.partial, nullptr};
