@@ -98,7 +98,7 @@ __device__ __forceinline__ int find_sequence(const QueriesDev& a, long long unit
 // rows of an ldmatrix lie in different banks); no barrier but the warp's.  Masked keys are not read: their place is zeros, whatever
 // the cache holds there.  K goes to the tensor core as it lies, V through the transposing ldmatrix.
 //
-// Softmax in fp32 with a running maximum per row.  P is held as two bf16 parts, most of p and what that leaves, whose products with V are
+// Softmax in fp32 against a reference per row that moves only when a score exceeds it by more than 2^8.  P is held as two bf16 parts, most of p and what that leaves, whose products with V are
 // added: the tensor core has time (48 of its instructions per 16 keys; HBM allows 350 cycles for them), and the error is then the
 // output's own rounding (0.0017 relative, 0.0020 with one part).  Keys are split over CTAs when there are few units; the parts are
 // joined in a fixed order.
@@ -215,7 +215,24 @@ __global__ void __launch_bounds__(kFewThreads, kFewResident) few_rows_kernel(con
     const int key = b * 16 + (lane & 15);
     on_ahead = key < most && (sp.mask == nullptr || __ldg(sp.mask + key) != 0);
   };
-  auto fetch = [&](int b, int stage) {                  // block b of 16 keys into a stage; the next one's look-up
+  // K of block b into a stage, then V of the same block: two steps, because K's place is free as soon as the scores are computed
+  uint32_t v_valid = 0;
+  const __nv_bfloat16* v_next = nullptr;
+  auto copy_rows = [&](uint32_t dst, const __nv_bfloat16* src, long long step, uint32_t valid, const __nv_bfloat16* safe) {
+    if (valid == 0xffffu) {
+#pragma unroll
+      for (int i = 0; i < 16 / kRowStep; ++i, src += step) cp_async_16(dst + i * kRowStep * L::kPitch, src, 16);
+    } else {
+      valid >>= row_first;
+#pragma unroll
+      for (int i = 0; i < 16 / kRowStep; ++i, src += step) {
+        const bool on = (valid >> (i * kRowStep)) & 1u;
+        // (a key that is not read keeps its address inside a page; behind the last row of a context there may be no memory)
+        cp_async_16(dst + i * kRowStep * L::kPitch, kPaged || on ? src : safe, on ? 16 : 0);
+      }
+    }
+  };
+  auto fetch_k = [&](int b, int stage) {
     if (b < b_end) {
       uint32_t valid = __ballot_sync(0xffffffffu, on_ahead) & 0xffffu;
       if (lane == 0) valid_of[stage] = valid;
@@ -230,32 +247,25 @@ __global__ void __launch_bounds__(kFewThreads, kFewResident) few_rows_kernel(con
         krow = (sp.begin + b * 16) * p.d.c.ks[1];
         vrow = (sp.begin + b * 16) * p.d.c.vs[1];
       }
-      const __nv_bfloat16* ksrc = kh + krow + row_first * p.d.c.ks[1];
-      const __nv_bfloat16* vsrc = vh + vrow + row_first * p.d.c.vs[1];
-      const uint32_t dst = ring + stage * 2 * L::kBlock + row_first * L::kPitch + chunk * 16;
-      if (valid == 0xffffu) {
-#pragma unroll
-        for (int i = 0; i < 16 / kRowStep; ++i, ksrc += k_step, vsrc += v_step) {
-          cp_async_16(dst + i * kRowStep * L::kPitch, ksrc, 16);
-          cp_async_16(dst + L::kBlock + i * kRowStep * L::kPitch, vsrc, 16);
-        }
-      } else {
-        valid >>= row_first;
-#pragma unroll
-        for (int i = 0; i < 16 / kRowStep; ++i, ksrc += k_step, vsrc += v_step) {
-          const bool on = (valid >> (i * kRowStep)) & 1u;
-          // (a key that is not read keeps its address inside a page; behind the last row of a context there may be no memory)
-          cp_async_16(dst + i * kRowStep * L::kPitch, kPaged || on ? ksrc : p.d.c.k, on ? 16 : 0);
-          cp_async_16(dst + L::kBlock + i * kRowStep * L::kPitch, kPaged || on ? vsrc : p.d.c.v, on ? 16 : 0);
-        }
-      }
+      v_valid = valid;
+      v_next = vh + vrow + row_first * p.d.c.vs[1];
+      copy_rows(ring + stage * 2 * L::kBlock + row_first * L::kPitch + chunk * 16, kh + krow + row_first * p.d.c.ks[1], k_step, valid, p.d.c.k);
+    }
+    cp_async_commit();
+  };
+  auto fetch_v = [&](int b, int stage) {
+    if (b < b_end) {
+      copy_rows(ring + stage * 2 * L::kBlock + L::kBlock + row_first * L::kPitch + chunk * 16, v_next, v_step, v_valid, p.d.c.v);
       look_up(b + kFewWarps);
     }
     cp_async_commit();
   };
   look_up(b_first);
 #pragma unroll
-  for (int s = 0; s < L::kStages - 1; ++s) fetch(b_first + s * kFewWarps, s);
+  for (int s = 0; s < L::kStages; ++s) {
+    fetch_k(b_first + s * kFewWarps, s);
+    fetch_v(b_first + s * kFewWarps, s);
+  }
 
   float o[D / 8][4];
 #pragma unroll
@@ -270,9 +280,9 @@ __global__ void __launch_bounds__(kFewThreads, kFewResident) few_rows_kernel(con
   const uint32_t v_lane = (lane & 15) * L::kPitch + (lane >> 4) * 16;
 
   int stage = 0;
+#pragma unroll 1
   for (int b = b_first; b < b_end; b += kFewWarps) {
-    fetch(b + (L::kStages - 1) * kFewWarps, stage == 0 ? L::kStages - 1 : stage - 1);
-    cp_async_wait<L::kStages - 1>();
+    cp_async_wait<2 * L::kStages - 1>();                // K of this block is there
     __syncwarp();
     const int key0 = b * 16;
     const uint32_t k_at = ring + stage * 2 * L::kBlock + k_lane, v_at = ring + stage * 2 * L::kBlock + L::kBlock + v_lane;
@@ -294,6 +304,8 @@ __global__ void __launch_bounds__(kFewThreads, kFewResident) few_rows_kernel(con
         mma_bf16_16816(s2[t], q[k + 1][0], q[k + 1][1], q[k + 1][2], q[k + 1][3], y[2 * t], y[2 * t + 1]);
       }
     }
+    __syncwarp();
+    fetch_k(b + L::kStages * kFewWarps, stage);
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -319,28 +331,28 @@ __global__ void __launch_bounds__(kFewThreads, kFewResident) few_rows_kernel(con
       }
       seen[0] = seen[1] = seen[0] || valid != 0;        // (rows that the unit does not have: not written)
     }
-    // ---- running maximum of the row, over the quad
-    float scale[2];
-    float base[2];
+    // ---- the rows' references: the largest score of the first block with a valid key, moved when one exceeds it by more than 2^8
+    float x[2];
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
-      float x = fmaxf(fmaxf(s[0][2 * r], s[0][2 * r + 1]), fmaxf(s[1][2 * r], s[1][2 * r + 1]));
-      x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
-      x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
-      x = fmaxf(x, m[r]);
-      base[r] = x == -CUDART_INF_F ? 0.f : x * sc;                          // (nothing valid yet: every term below is 2^-inf)
-      scale[r] = x == m[r] ? 1.f : ex2_approx(m[r] * sc - base[r]);
-      m[r] = x;
+      x[r] = fmaxf(fmaxf(s[0][2 * r], s[0][2 * r + 1]), fmaxf(s[1][2 * r], s[1][2 * r + 1]));
+      x[r] = fmaxf(x[r], __shfl_xor_sync(0xffffffffu, x[r], 1));
+      x[r] = fmaxf(x[r], __shfl_xor_sync(0xffffffffu, x[r], 2));
     }
-    if (__any_sync(0xffffffffu, scale[0] != 1.f || scale[1] != 1.f)) {
+    const bool move0 = (x[0] - m[0]) * sc > 8.f, move1 = (x[1] - m[1]) * sc > 8.f;
+    if (__any_sync(0xffffffffu, move0 || move1)) {
+      const float f0 = move0 ? ex2_approx((m[0] - x[0]) * sc) : 1.f, f1 = move1 ? ex2_approx((m[1] - x[1]) * sc) : 1.f;
+      if (move0) m[0] = x[0];
+      if (move1) m[1] = x[1];
 #pragma unroll
       for (int t = 0; t < D / 8; ++t) {
-        o[t][0] *= scale[0]; o[t][1] *= scale[0];
-        o[t][2] *= scale[1]; o[t][3] *= scale[1];
+        o[t][0] *= f0; o[t][1] *= f0;
+        o[t][2] *= f1; o[t][3] *= f1;
       }
-      l[0] *= scale[0];
-      l[1] *= scale[1];
+      l[0] *= f0;
+      l[1] *= f1;
     }
+    const float base[2] = {m[0] == -CUDART_INF_F ? 0.f : m[0] * sc, m[1] == -CUDART_INF_F ? 0.f : m[1] * sc};   // (nothing valid yet: 2^-inf)
     uint32_t hi[4], lo[4];
 #pragma unroll
     for (int t = 0; t < 2; ++t)
@@ -354,6 +366,8 @@ __global__ void __launch_bounds__(kFewThreads, kFewResident) few_rows_kernel(con
         lo[2 * t + r] = pack_bf16x2(p0 - __uint_as_float(h0), p1 - __uint_as_float(h1));
       }
     // ---- O += P V
+    cp_async_wait<2 * L::kStages - 1>();                // V of this block is there
+    __syncwarp();
 #pragma unroll
     for (int j = 0; j < D / 8; j += 2) {
       uint32_t x[4];
@@ -363,7 +377,8 @@ __global__ void __launch_bounds__(kFewThreads, kFewResident) few_rows_kernel(con
       mma_bf16_16816(o[j], lo[0], lo[1], lo[2], lo[3], x[0], x[1]);
       mma_bf16_16816(o[j + 1], lo[0], lo[1], lo[2], lo[3], x[2], x[3]);
     }
-    __syncwarp();                                       // the stage is filled again in the next turn
+    __syncwarp();
+    fetch_v(b + L::kStages * kFewWarps, stage);
     if (++stage == L::kStages) stage = 0;
   }
   cp_async_wait<0>();
