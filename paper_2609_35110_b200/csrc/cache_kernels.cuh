@@ -34,10 +34,11 @@ __device__ __forceinline__ long long stream_tokens(const PagedDev& c, long long 
 // the token's (t, h, w), offset per sequence, and rounded once; V is copied.  Row i of a chunk of n tokens becomes token
 // N - n + i of a stream of N.  Bound by HBM: every value is read and written once.
 //
-// A thread owns a 16-byte chunk (8 dims) of a token's rows: Q heads, then K heads, then V heads, `blockDim.x / chunks` rows
-// apart, four of them in flight.  The angles of its four pairs are found once per token: from the plan's tables, or, where
-// positions are offset, as position times frequency in fp64 (the tables end with the grid, and fp32 loses far positions), which
-// B200 does at half its fp32 rate.
+// A block takes a range of neighbouring tokens.  A thread owns a 16-byte chunk (8 dims) of a token's rows: Q heads, then K heads, then
+// V heads, `blockDim.x / chunks` rows apart, four of them in flight.  While a token's first loads are on their way, 64 threads find
+// the angles of its pairs, once for all heads: from the plan's tables, or, where positions are offset, from position times frequency
+// in fp64, brought to (-pi, pi] there (the tables end with the grid, and fp32 loses far positions).  (Every thread finding its own in
+// fp64: 106 us for 4,680 tokens x 40 heads, of which the angles took more than half.)
 // ---------------------------------------------------------------------------------------------
 struct AppendArgs {
   const __nv_bfloat16* x[3];    // q, k, v of the new tokens (q may be nullptr)
@@ -57,6 +58,7 @@ struct AppendArgs {
 };
 
 __global__ void __launch_bounds__(256, 3) cache_append_kernel(const __grid_constant__ AppendArgs a) {
+  __shared__ float2 angle[2][64];
   __shared__ int found;
   const int D = a.g.head_dim, chunks = D >> 3;
   const int rows_per_pass = blockDim.x / chunks;
@@ -64,54 +66,48 @@ __global__ void __launch_bounds__(256, 3) cache_append_kernel(const __grid_const
   const unsigned lanes = __activemask();
   const float inv_d = 1.0f / (float)D;
   const int n_q = a.x[0] != nullptr ? a.g.heads : 0, n_k = a.c.kv_heads, n_rows = n_q + 2 * n_k;
+  const int d1 = a.g.rope[0], d2 = d1 + a.g.rope[1], d3 = d2 + a.g.rope[2];
   constexpr int kBatch = 4;
 
-  for (long long tok = blockIdx.x; tok < a.total_tokens; tok += gridDim.x) {
-    for (int s = threadIdx.x; s < a.n_seqs; s += blockDim.x)
-      if (tok >= a.seqs[s].tok_start && tok < a.seqs[s].tok_start + a.seqs[s].n_tokens) found = s;
-    __syncthreads();
-    const SeqDev sq = a.seqs[found];
-    __syncthreads();
-    const int local = (int)(tok - sq.tok_start);
-    const long long stream = a.streams != nullptr ? a.streams[sq.seq_id] : sq.seq_id;
-    if (stream < 0 || stream >= a.c.n_streams) continue;                   // an idle sequence (the same for the whole block)
-    // Of several sequences with one stream the first counts: they would write the same rows.
-    bool again = false;
-    if (a.streams != nullptr) {
-      for (int s = threadIdx.x; s < sq.seq_id; s += blockDim.x) again = again || a.streams[s] == stream;
-      again = __syncthreads_or(again) != 0;
-    }
-    const long long at = stream_tokens(a.c, stream) - sq.n_tokens + local;
-    long long page = -1;
-    if (at >= 0 && !again) page = a.c.table[stream * a.c.width + at / a.c.page];
-    const bool write = page >= 0 && page < a.c.n_pages;                    // (a table that names no page there: nothing is written)
-    const int in_page = write ? (int)(at % a.c.page) : 0;
-    const bool rotate = local >= sq.text_len;
-    float2 cs[4];
-    if (rotate) {
-      const int p = local - sq.text_len, hw = sq.H * sq.W;
-      const int pos[3] = {p / hw, (p / sq.W) % sq.H, p % sq.W};
-      const int d1 = a.g.rope[0], d2 = d1 + a.g.rope[1], d3 = d2 + a.g.rope[2];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int d = chunk * 8 + 2 * u;                                   // first head dim of the pair
-        const int axis = d < d1 ? 0 : d < d2 ? 1 : 2;
-        const int x = axis == 0 ? pos[0] : axis == 1 ? pos[1] : pos[2];
-        if (d >= d3) {
-          cs[u] = make_float2(1.f, 0.f);
-        } else if (a.pos0 != nullptr) {
-          double s, c;
-          sincos((double)((long long)x + a.pos0[3 * sq.seq_id + axis]) * a.omega[d >> 1], &s, &c);
-          cs[u] = make_float2((float)c, (float)s);
-        } else {
-          const int first = axis == 0 ? 0 : axis == 1 ? d1 : d2;
-          cs[u] = __ldg(&a.tables[a.g.tab_off[axis] + x * (a.g.rope[axis] >> 1) + ((d - first) >> 1)]);
+  // the sequence that the block is in, and what follows from it; all of it the same for the whole block
+  SeqDev sq{};
+  long long seq_end = -1, first_at = 0;                    // end of its tokens; place of its first token in the stream
+  const int* table = nullptr;                              // nullptr: nothing of it is written to the cache
+  bool idle = false;
+  int turn = 0;
+
+  const long long begin = a.total_tokens * blockIdx.x / gridDim.x, end = a.total_tokens * (blockIdx.x + 1) / gridDim.x;
+  for (long long tok = begin; tok < end; ++tok) {
+    if (tok >= seq_end) {
+      for (int s = threadIdx.x; s < a.n_seqs; s += blockDim.x)
+        if (tok >= a.seqs[s].tok_start && tok < a.seqs[s].tok_start + a.seqs[s].n_tokens) found = s;
+      __syncthreads();
+      sq = a.seqs[found];
+      __syncthreads();
+      seq_end = sq.tok_start + sq.n_tokens;
+      const long long stream = a.streams != nullptr ? a.streams[sq.seq_id] : sq.seq_id;
+      idle = stream < 0 || stream >= a.c.n_streams;
+      table = nullptr;
+      if (!idle) {
+        // Of several sequences with one stream the first counts: they would write the same rows.
+        bool again = false;
+        if (a.streams != nullptr) {
+          for (int s = threadIdx.x; s < sq.seq_id; s += blockDim.x) again = again || a.streams[s] == stream;
+          again = __syncthreads_or(again) != 0;
         }
+        if (!again) table = a.c.table + stream * a.c.width;
+        first_at = stream_tokens(a.c, stream) - sq.n_tokens;
       }
     }
-    for (int r0 = 0; r0 < n_rows; r0 += kBatch * rows_per_pass) {          // the same trip count for every thread
-      uint4 w[kBatch];
-      int which[kBatch], head[kBatch];
+    if (idle) {
+      tok = seq_end - 1;
+      continue;
+    }
+    const int local = (int)(tok - sq.tok_start);
+    const bool rotate = local >= sq.text_len;
+    uint4 w[kBatch];
+    int which[kBatch], head[kBatch];
+    auto load = [&](int r0) {
 #pragma unroll
       for (int b = 0; b < kBatch; ++b) {
         const int r = r0 + sub + b * rows_per_pass;
@@ -126,6 +122,41 @@ __global__ void __launch_bounds__(256, 3) cache_append_kernel(const __grid_const
           w[b] = make_uint4(0, 0, 0, 0);
         }
       }
+    };
+    load(0);
+    const long long at = first_at + local;
+    long long page = -1;
+    if (table != nullptr && at >= 0) page = table[at / a.c.page];
+    for (int j = threadIdx.x; rotate && j < (D >> 1); j += blockDim.x) {
+      const int p = local - sq.text_len, hw = sq.H * sq.W;
+      const int d = 2 * j;                       // first head dim of the pair
+      const int axis = d < d1 ? 0 : d < d2 ? 1 : 2;
+      const int x = axis == 0 ? p / hw : axis == 1 ? (p / sq.W) % sq.H : p % sq.W;
+      float2 cs = make_float2(1.f, 0.f);
+      if (d < d3) {
+        if (a.pos0 != nullptr) {
+          const double phi = (double)((long long)x + a.pos0[3 * sq.seq_id + axis]) * a.omega[j];
+          const double turns = rint(phi * 0.15915494309189535);             // 1 / (2 pi)
+          const double rest = fma(-turns, 2.4492935982947064e-16, fma(-turns, 6.283185307179586, phi));   // 2 pi in two parts
+          sincosf((float)rest, &cs.y, &cs.x);
+        } else {
+          const int first = axis == 0 ? 0 : axis == 1 ? d1 : d2;
+          cs = __ldg(&a.tables[a.g.tab_off[axis] + x * (a.g.rope[axis] >> 1) + ((d - first) >> 1)]);
+        }
+      }
+      angle[turn][j] = cs;
+    }
+    __syncthreads();                                       // (two buffers: the next token's angles may come before the last reader is done)
+    float2 cs[4];
+    if (rotate) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) cs[u] = angle[turn][chunk * 4 + u];
+    }
+    turn ^= 1;
+    const bool write = page >= 0 && page < a.c.n_pages;                    // (a table that names no page there: nothing is written)
+    const int in_page = write ? (int)(at % a.c.page) : 0;
+    for (int r0 = 0; r0 < n_rows; r0 += kBatch * rows_per_pass) {          // the same trip count for every thread
+      if (r0 > 0) load(r0);
       float rinv[kBatch];
       if (a.gain[0] != nullptr || a.gain[1] != nullptr) {
         // Sums of squares of the rows, by shuffles over a row's chunks; where they leave fp32's range, once more on scaled values.
@@ -219,7 +250,7 @@ __global__ void __launch_bounds__(256, 3) cache_append_kernel(const __grid_const
 // ---------------------------------------------------------------------------------------------
 enum : int { kCacheOk = 0, kCacheBadStream = 1, kCacheNoRoom = 2, kCacheNoPages = 3, kCacheNotEmpty = 4 };
 constexpr int kMaxRequests = 4096;
-constexpr int kBookThreads = 1024;
+constexpr int kBookThreads = 512, kKeepThreads = 1024;
 
 struct BookArgs {
   int* table;
@@ -250,110 +281,124 @@ __device__ __forceinline__ int stream_length(const BookArgs& a, long long stream
   const long long n = a.lens[stream], cap = a.width * a.page;
   return (int)(n < 0 ? 0 : n < cap ? n : cap);
 }
-// Is the stream of request i there, and not named by an earlier request?
-__device__ __forceinline__ bool named_first(const BookArgs& a, int i) {
-  const int s = a.streams[i];
-  if (s < 0 || s >= a.n_streams) return false;
-  for (int j = 0; j < i; ++j)
-    if (a.streams[j] == s) return false;
-  return true;
-}
-
-// Inclusive sums over the block's threads; `warp_sum` has 32 entries.  All threads call it.
-__device__ __forceinline__ long long block_scan(long long x, long long* warp_sum) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+// Sums over the block's threads, inclusive; `warp_sum` has 32 entries.  All threads call it; two barriers.
+template <typename T>
+__device__ __forceinline__ T block_scan(T x, long long* warp_sum) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const long long y = __shfl_up_sync(0xffffffffu, x, o);
+    const T y = __shfl_up_sync(0xffffffffu, x, o);
     if (lane >= o) x += y;
   }
+  __syncthreads();                                         // (the last call's sums have been read)
   if (lane == 31) warp_sum[warp] = x;
   __syncthreads();
-  if (warp == 0) {
-    long long t = lane < (int)(blockDim.x >> 5) ? warp_sum[lane] : 0;
+  T t = lane < warp && lane < warps ? (T)warp_sum[lane] : (T)0;            // every warp sums the warps before it
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const long long y = __shfl_up_sync(0xffffffffu, t, o);
-      if (lane >= o) t += y;
-    }
-    warp_sum[lane] = t;
-  }
-  __syncthreads();
-  if (warp > 0) x += warp_sum[warp - 1];
-  __syncthreads();
-  return x;
+  for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
+  return x + t;
 }
 
 struct BookSmem {
   long long warp_sum[32];
-  long long ends[kMaxRequests];  // need of the requests up to and including i
+  int streams[kMaxRequests];     // as named
   int need[kMaxRequests];        // pages, or -1: refused
+  int ends[kMaxRequests];        // need of the requests up to and including i (2^30 for all above that); later, rows to copy
+  int extra[kMaxRequests];       // per request, as the kernel uses it
 };
 
-// Turns need[] into running sums and refuses what does not fit the free pages; returns the number of pages to hand out.
-__device__ __forceinline__ long long admit(const BookArgs& a, BookSmem& sm) {
-  long long wanted = 0;
-  for (int i0 = 0; i0 < a.n; i0 += blockDim.x) {
-    const int i = i0 + threadIdx.x;
-    const long long x = i < a.n && sm.need[i] > 0 ? sm.need[i] : 0;
-    const long long s = block_scan(x, sm.warp_sum);
-    if (i < a.n) sm.ends[i] = wanted + s;
-    __syncthreads();
-    wanted = sm.ends[min(i0 + (int)blockDim.x, a.n) - 1];
-  }
-  return wanted;
+__device__ __forceinline__ void load_streams(const BookArgs& a, BookSmem& sm) {
+  for (int i = threadIdx.x; i < a.n; i += blockDim.x) sm.streams[i] = a.streams[i];
+  __syncthreads();
+}
+// Is the stream of request i there, and not named by an earlier request?
+__device__ __forceinline__ bool named_first(const BookArgs& a, const BookSmem& sm, int i) {
+  const int s = sm.streams[i];
+  if (s < 0 || s >= a.n_streams) return false;
+  for (int j = 0; j < i; ++j)
+    if (sm.streams[j] == s) return false;
+  return true;
 }
 
-// Hands out `wanted` free pages, lowest index first: calls give(request, k, page) for the k-th page of a request.  Returns how many
-// there were.  A request gets all its pages or none: admit_found below says which.
-template <typename Give>
-__device__ __forceinline__ long long hand_out(const BookArgs& a, BookSmem& sm, long long wanted, const Give& give) {
-  long long found = 0;
-  for (long long p0 = 0; p0 < a.n_pages && found < wanted; p0 += blockDim.x) {
-    const long long p = p0 + threadIdx.x;
-    const bool is_free = p < a.n_pages && a.refs[p] == 0;
-    const long long rank = block_scan(is_free ? 1 : 0, sm.warp_sum) - 1 + found;        // among all free pages
-    if (is_free && rank < wanted) {
-      int lo = 0, hi = a.n - 1;                                            // the first request whose running sum exceeds the rank
-      while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (sm.ends[mid] > rank) hi = mid; else lo = mid + 1;
-      }
-      give(lo, (int)(rank - (sm.ends[lo] - sm.need[lo])), (int)p);
-    }
-    found += __syncthreads_count(is_free);
+// Running sums of `of(i)` over the requests, into ends[]; returns the whole.  (Requests may ask for far more than there is.)
+template <typename Of>
+__device__ __forceinline__ int sum_up(const BookArgs& a, BookSmem& sm, const Of& of) {
+  int before = 0;
+  for (int i0 = 0; i0 < a.n; i0 += blockDim.x) {
+    const int i = i0 + threadIdx.x;
+    const long long s = before + block_scan<long long>(i < a.n ? of(i) : 0, sm.warp_sum);
+    if (i < a.n) sm.ends[i] = (int)min(s, 1ll << 30);
+    __syncthreads();
+    before = sm.ends[min(i0 + (int)blockDim.x, a.n) - 1];
   }
-  return found < wanted ? found : wanted;
+  return before;
 }
-// The free pages are counted first (up to what is wanted), so that a request that cannot be served takes none.
-__device__ __forceinline__ long long count_free(const BookArgs& a, long long wanted) {
-  long long found = 0;
-  for (long long p0 = 0; p0 < a.n_pages && found < wanted; p0 += 8ll * blockDim.x) {
-    int mine = 0;
+
+// Walks over the free pages, lowest index first, until `wanted` have been seen: take(rank, page).  Returns how many there were.
+template <typename Take>
+__device__ __forceinline__ int walk_free(const BookArgs& a, BookSmem& sm, int wanted, const Take& take) {
+  constexpr int kEach = 8;                                 // neighbouring pages per thread and turn
+  int found = 0;
+  for (long long p0 = 0; p0 < a.n_pages && found < wanted; p0 += kEach * blockDim.x) {
+    const long long first = p0 + kEach * threadIdx.x;
+    unsigned bits = 0;
 #pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      const long long p = p0 + u * (long long)blockDim.x + threadIdx.x;
-      mine += p < a.n_pages && a.refs[p] == 0 ? 1 : 0;
-    }
-    // 0 .. 8 free pages per thread: four counts of one bit
-#pragma unroll
-    for (int bit = 0; bit < 4; ++bit) found += (long long)__syncthreads_count((mine >> bit) & 1) << bit;
+    for (int e = 0; e < kEach; ++e)
+      if (first + e < a.n_pages && a.refs[first + e] == 0) bits |= 1u << e;
+    const int mine = __popc(bits), upto = block_scan<int>(mine, sm.warp_sum);
+    int rank = found + upto - mine;
+    for (; bits != 0; bits &= bits - 1, ++rank)
+      if (rank < wanted) take(rank, (int)(first + __ffs(bits) - 1));
+    if (threadIdx.x == blockDim.x - 1) sm.warp_sum[31] = upto;             // (read by no scan: there are fewer than 32 warps)
+    __syncthreads();
+    found += (int)sm.warp_sum[31];
   }
-  return found;
+  return min(found, wanted);
+}
+static_assert(kBookThreads / 32 < 32, "walk_free keeps a sum in the last entry");
+
+// Pages for requests with need[i] > 0, in their order: served(i) tells which get theirs, give(i, k, page) hands request i its k-th.
+// The free pages are counted first, so that a request that cannot be served takes none.
+struct Served {
+  int there;
+  __device__ __forceinline__ bool operator()(const BookSmem& sm, int i) const { return sm.need[i] >= 0 && !(sm.need[i] > 0 && sm.ends[i] > there); }
+};
+template <typename Give>
+__device__ __forceinline__ Served allocate(const BookArgs& a, BookSmem& sm, const Give& give) {
+  __syncthreads();
+  const int wanted = sum_up(a, sm, [&](int i) { return max(sm.need[i], 0); });
+  const Served served{walk_free(a, sm, wanted, [](int, int) {})};
+  for (int i = threadIdx.x; i < a.n; i += blockDim.x)
+    if (sm.need[i] > 0 && !served(sm, i) && a.status != nullptr) a.status[i] = kCacheNoPages;
+  __syncthreads();
+  walk_free(a, sm, served.there, [&](int rank, int p) {
+    int lo = 0, hi = a.n - 1;                                              // the first request whose running sum exceeds the rank
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (sm.ends[mid] > rank) hi = mid; else lo = mid + 1;
+    }
+    if (sm.ends[lo] > served.there) return;
+    give(lo, rank - (sm.ends[lo] - sm.need[lo]), p);
+    a.refs[p] = 1;
+  });
+  __syncthreads();
+  return served;
 }
 
 // Closing streams: their pages lose a holder.
 __global__ void __launch_bounds__(kBookThreads) cache_free_kernel(const BookArgs a) {
-  __shared__ int ok[kMaxRequests];
-  for (int i = threadIdx.x; i < a.n; i += blockDim.x) {
-    ok[i] = named_first(a, i);
-    if (a.status != nullptr) a.status[i] = ok[i] ? kCacheOk : kCacheBadStream;
-  }
-  __syncthreads();
+  extern __shared__ __align__(16) unsigned char book_raw[];
+  BookSmem& sm = *reinterpret_cast<BookSmem*>(book_raw);
+  load_streams(a, sm);
   const int lane = threadIdx.x & 31;
-  for (int i = threadIdx.x >> 5; i < a.n; i += blockDim.x >> 5) {
-    if (!ok[i]) continue;
-    const long long s = a.streams[i];
+  for (int i = threadIdx.x >> 5; i < a.n; i += blockDim.x >> 5) {          // a warp per request
+    bool ok = false;
+    if (lane == 0) {
+      ok = named_first(a, sm, i);
+      if (a.status != nullptr) a.status[i] = ok ? kCacheOk : kCacheBadStream;
+    }
+    if (!__any_sync(0xffffffffu, ok)) continue;
+    const long long s = sm.streams[i];
     const int held = pages_of(stream_length(a, s), a.page);
     for (int c = lane; c < held; c += 32) {
       const int p = a.table[s * a.width + c];
@@ -369,76 +414,55 @@ __global__ void __launch_bounds__(kBookThreads) cache_free_kernel(const BookArgs
 __global__ void __launch_bounds__(kBookThreads) cache_reserve_kernel(const BookArgs a) {
   extern __shared__ __align__(16) unsigned char book_raw[];
   BookSmem& sm = *reinterpret_cast<BookSmem*>(book_raw);
+  load_streams(a, sm);
   for (int i = threadIdx.x; i < a.n; i += blockDim.x) {
     int need = -1, st = kCacheBadStream;
-    if (named_first(a, i) && a.amount[i] >= 0) {
-      const int len = stream_length(a, a.streams[i]);
+    if (named_first(a, sm, i) && a.amount[i] >= 0) {
+      const int len = stream_length(a, sm.streams[i]);
       const long long want = (long long)len + a.amount[i];
+      sm.extra[i] = pages_of(len, a.page);
       st = kCacheNoRoom;
       if (want <= a.width * a.page && want <= 0x7fffffffll) {
         st = kCacheOk;
-        need = pages_of((int)want, a.page) - pages_of(len, a.page);
+        need = pages_of((int)want, a.page) - sm.extra[i];
       }
     }
     sm.need[i] = need;
     if (a.status != nullptr) a.status[i] = st;
   }
-  __syncthreads();
-  const long long wanted = admit(a, sm), there = count_free(a, wanted);
+  const Served served = allocate(a, sm, [&](int i, int k, int p) { a.table[sm.streams[i] * a.width + sm.extra[i] + k] = p; });
   for (int i = threadIdx.x; i < a.n; i += blockDim.x)
-    if (sm.need[i] > 0 && sm.ends[i] > there) {
-      if (a.status != nullptr) a.status[i] = kCacheNoPages;
-    }
-  __syncthreads();
-  hand_out(a, sm, wanted < there ? wanted : there, [&](int i, int k, int p) {
-    if (sm.ends[i] > there) return;
-    const long long s = a.streams[i];
-    a.table[s * a.width + pages_of(stream_length(a, s), a.page) + k] = p;
-    a.refs[p] = 1;
-  });
-  __syncthreads();
-  for (int i = threadIdx.x; i < a.n; i += blockDim.x)
-    if (sm.need[i] >= 0 && !(sm.need[i] > 0 && sm.ends[i] > there)) a.lens[a.streams[i]] = stream_length(a, a.streams[i]) + a.amount[i];
+    if (served(sm, i)) a.lens[sm.streams[i]] = stream_length(a, sm.streams[i]) + a.amount[i];
 }
 
 // Opening streams as branches of others: full pages are shared, the last, partly filled one is copied (by cache_move_kernel).
 __global__ void __launch_bounds__(kBookThreads) cache_fork_kernel(const BookArgs a) {
   extern __shared__ __align__(16) unsigned char book_raw[];
   BookSmem& sm = *reinterpret_cast<BookSmem*>(book_raw);
-  int* len = reinterpret_cast<int*>(book_raw + sizeof(BookSmem));          // of the parents, before anything changes
+  int* len = sm.extra;                                     // of the parents, before anything changes
+  load_streams(a, sm);
   for (int i = threadIdx.x; i < a.n; i += blockDim.x) {
     int st = kCacheBadStream, need = -1;
     const int parent = a.parents[i];
     len[i] = 0;
-    if (named_first(a, i) && parent >= 0 && parent < a.n_streams) {
+    if (parent >= 0 && parent < a.n_streams && named_first(a, sm, i)) {
       st = kCacheNotEmpty;
-      if (stream_length(a, a.streams[i]) == 0) {
+      const int old = stream_length(a, parent);
+      if (stream_length(a, sm.streams[i]) == 0) {
         st = kCacheOk;
-        len[i] = stream_length(a, parent);
-        need = len[i] % a.page != 0 ? 1 : 0;
+        len[i] = old;
+        need = old % a.page != 0 ? 1 : 0;
       }
     }
     sm.need[i] = need;
     if (a.status != nullptr) a.status[i] = st;
   }
-  __syncthreads();
-  const long long wanted = admit(a, sm), there = count_free(a, wanted);
-  for (int i = threadIdx.x; i < a.n; i += blockDim.x)
-    if (sm.need[i] > 0 && sm.ends[i] > there) {
-      if (a.status != nullptr) a.status[i] = kCacheNoPages;
-    }
-  __syncthreads();
-  hand_out(a, sm, wanted < there ? wanted : there, [&](int i, int k, int p) {
-    if (sm.ends[i] > there) return;
-    a.table[a.streams[i] * a.width + len[i] / a.page] = p;
-    a.refs[p] = 1;
-  });
-  __syncthreads();
+  const Served served = allocate(a, sm, [&](int i, int, int p) { a.table[sm.streams[i] * a.width + len[i] / a.page] = p; });
   // one warp per request: the shared pages, and which rows of the last one have to be copied
   const int lane = threadIdx.x & 31;
   for (int i = threadIdx.x >> 5; i < a.n; i += blockDim.x >> 5) {
-    if (sm.need[i] < 0 || (sm.need[i] > 0 && sm.ends[i] > there)) continue;
-    const long long s = a.streams[i], parent = a.parents[i];
+    if (!served(sm, i)) continue;
+    const long long s = sm.streams[i], parent = a.parents[i];
     const int full = len[i] / a.page, rest = len[i] % a.page;
     for (int c = lane; c < full; c += 32) {
       const int p = a.table[parent * a.width + c];
@@ -454,78 +478,63 @@ __global__ void __launch_bounds__(kBookThreads) cache_fork_kernel(const BookArgs
     __syncwarp();
     if (lane == 0) a.lens[s] = len[i];
   }
+  __syncthreads();
   // rows to copy before request i
-  long long before = 0;
-  for (int i0 = 0; i0 < a.n; i0 += blockDim.x) {
-    const int i = i0 + threadIdx.x;
-    long long x = 0;
-    if (i < a.n && sm.need[i] > 0 && sm.ends[i] <= there) x = len[i] % a.page;
-    const long long s = block_scan(x, sm.warp_sum);
-    if (i < a.n) {
-      a.moved[i + 1] = before + s;
-      sm.ends[i] = before + s;
-    }
-    __syncthreads();
-    before = sm.ends[min(i0 + (int)blockDim.x, a.n) - 1];
-  }
+  for (int i = threadIdx.x; i < a.n; i += blockDim.x) sm.need[i] = sm.need[i] > 0 && served(sm, i) ? len[i] % a.page : 0;
+  __syncthreads();
+  sum_up(a, sm, [&](int i) { return sm.need[i]; });
+  for (int i = threadIdx.x; i < a.n; i += blockDim.x) a.moved[i + 1] = sm.ends[i];
   if (threadIdx.x == 0) a.moved[0] = 0;
 }
 
 // Thinning streams, first step: one block per request counts what stays, finds the first dropped token and lists where the rows
 // that stay are now.
-__global__ void __launch_bounds__(kBookThreads) cache_keep_kernel(const BookArgs a) {
+__global__ void __launch_bounds__(kKeepThreads) cache_keep_kernel(const BookArgs a) {
   __shared__ long long warp_sum[32];
-  __shared__ int in_order;
-  __shared__ int lowest;
+  __shared__ int lowest, whole;
   const int i = blockIdx.x;
   if (threadIdx.x == 0) lowest = 0x7fffffff;
-  {
-    const int s = a.streams[i];
-    bool bad = s < 0 || s >= a.n_streams;
-    for (int j = threadIdx.x; j < i; j += blockDim.x) bad = bad || a.streams[j] == s;
-    bad = __syncthreads_or(bad) != 0;
-    if (threadIdx.x == 0) in_order = !bad;
-  }
-  __syncthreads();
-  if (!in_order) {
+  const int s = a.streams[i];
+  bool bad = s < 0 || s >= a.n_streams;
+  for (int j = threadIdx.x; j < i; j += blockDim.x) bad = bad || a.streams[j] == s;
+  if (__syncthreads_or(bad) != 0) {
     if (threadIdx.x == 0) a.kept[i] = -1;
     return;
   }
-  const long long s = a.streams[i];
   const int len = stream_length(a, s), held = pages_of(len, a.page);
   const int* row = a.table + s * a.width;
   for (int c = threadIdx.x; c < held; c += blockDim.x) a.old_pages[i * a.width + c] = row[c];
   const uint8_t* keep = a.keep + i * a.keep_stride;
-  constexpr int kEach = 8;                                                 // neighbouring tokens per thread and turn
-  long long before = 0;
-  for (long long t0 = 0; t0 < len; t0 += kEach * kBookThreads) {
+  int2* moves = a.moves + i * a.moves_cap;
+  constexpr int kEach = 16;                                                // neighbouring tokens per thread and turn
+  int before = 0;
+  for (long long t0 = 0; t0 < len; t0 += kEach * kKeepThreads) {
     const long long t = t0 + kEach * threadIdx.x;
-    unsigned bits = 0;
-    int drop = 0x7fffffff;
+    unsigned bits = 0, there = 0;
 #pragma unroll
     for (int e = 0; e < kEach; ++e)
       if (t + e < len) {
+        there |= 1u << e;
         if (t + e < a.keep_stride && keep[t + e] != 0) bits |= 1u << e;
-        else if (drop == 0x7fffffff) drop = (int)(t + e);
       }
-    drop = __reduce_min_sync(0xffffffffu, drop);
+    const unsigned dropped = there & ~bits;
+    const int drop = __reduce_min_sync(0xffffffffu, dropped != 0 ? (int)(t + __ffs(dropped) - 1) : 0x7fffffff);
     if ((threadIdx.x & 31) == 0 && drop != 0x7fffffff) atomicMin(&lowest, drop);
-    const int mine = __popc(bits);
-    const long long upto = block_scan(mine, warp_sum);
-    long long at = before + upto - mine;
+    const int mine = __popc(bits), upto = block_scan<int>(mine, warp_sum);
+    int at = before + upto - mine;
+    // 16 tokens may span two pages (a page holds whole groups of 16, and t is a multiple of 16: they do not)
+    const int page = bits != 0 ? row[t / a.page] : -1;
+    const int place = page >= 0 && page < a.n_pages ? page * a.page + (int)(t % a.page) : -1;
 #pragma unroll
     for (int e = 0; e < kEach; ++e)
-      if ((bits >> e) & 1u) {
-        const int p = row[(t + e) / a.page];
-        a.moves[i * a.moves_cap + at++].x = p >= 0 && p < a.n_pages ? p * a.page + (int)((t + e) % a.page) : -1;
-      }
-    if (threadIdx.x == blockDim.x - 1) warp_sum[0] = upto;
+      if ((bits >> e) & 1u) moves[at++].x = place >= 0 ? place + e : -1;
+    if (threadIdx.x == blockDim.x - 1) whole = upto;
     __syncthreads();
-    before += warp_sum[0];
+    before += whole;
     __syncthreads();
   }
   if (threadIdx.x == 0) {
-    a.kept[i] = (int)before;
+    a.kept[i] = before;
     a.first[i] = lowest < len ? lowest : len;
   }
 }
@@ -535,12 +544,14 @@ __global__ void __launch_bounds__(kBookThreads) cache_keep_kernel(const BookArgs
 __global__ void __launch_bounds__(kBookThreads) cache_compact_kernel(const BookArgs a) {
   extern __shared__ __align__(16) unsigned char book_raw[];
   BookSmem& sm = *reinterpret_cast<BookSmem*>(book_raw);
-  int* begin = reinterpret_cast<int*>(book_raw + sizeof(BookSmem));        // the first page that does not stay
+  int* begin = sm.extra;                                   // the first page that does not stay
+  load_streams(a, sm);
   for (int i = threadIdx.x; i < a.n; i += blockDim.x) {
     int need = -1, st = kCacheBadStream;
     begin[i] = 0;
-    if (a.kept[i] >= 0) {
-      const int kept = a.kept[i], first = a.first[i];
+    const int kept = a.kept[i];
+    if (kept >= 0) {
+      const int first = a.first[i];
       begin[i] = first / a.page;
       if (kept == first) {
         // a prefix stays: nothing moves, unless a page that becomes partly filled is another stream's, too
@@ -553,22 +564,11 @@ __global__ void __launch_bounds__(kBookThreads) cache_compact_kernel(const BookA
     sm.need[i] = need;
     if (a.status != nullptr) a.status[i] = st;
   }
-  __syncthreads();
-  const long long wanted = admit(a, sm), there = count_free(a, wanted);
-  auto served = [&](int i) { return sm.need[i] >= 0 && !(sm.need[i] > 0 && sm.ends[i] > there); };
-  for (int i = threadIdx.x; i < a.n; i += blockDim.x)
-    if (sm.need[i] > 0 && !served(i) && a.status != nullptr) a.status[i] = kCacheNoPages;
-  __syncthreads();
-  hand_out(a, sm, wanted < there ? wanted : there, [&](int i, int k, int p) {
-    if (sm.ends[i] > there) return;
-    a.table[a.streams[i] * a.width + begin[i] + k] = p;
-    a.refs[p] = 1;
-  });
-  __syncthreads();
+  const Served served = allocate(a, sm, [&](int i, int k, int p) { a.table[sm.streams[i] * a.width + begin[i] + k] = p; });
   const int lane = threadIdx.x & 31;
   for (int i = threadIdx.x >> 5; i < a.n; i += blockDim.x >> 5) {
-    if (!served(i)) continue;
-    const long long s = a.streams[i];
+    if (!served(sm, i)) continue;
+    const long long s = sm.streams[i];
     const int held = pages_of(stream_length(a, s), a.page);
     for (int c = begin[i] + lane; c < held; c += 32) {
       const int p = a.old_pages[i * a.width + c];
@@ -578,18 +578,15 @@ __global__ void __launch_bounds__(kBookThreads) cache_compact_kernel(const BookA
     __syncwarp();
     if (lane == 0) a.lens[s] = a.kept[i];
   }
-  long long before = 0;
-  for (int i0 = 0; i0 < a.n; i0 += blockDim.x) {
-    const int i = i0 + threadIdx.x;
-    long long x = 0;
-    if (i < a.n && sm.need[i] > 0 && served(i)) x = a.kept[i] - (long long)begin[i] * a.page;
-    if (i < a.n) a.first[i] = begin[i] * a.page;                           // what the copying kernel starts from
-    __syncthreads();
-    const long long sum = block_scan(x, sm.warp_sum);
-    if (i < a.n) a.moved[i + 1] = before + sum;
-    __syncthreads();
-    before = a.moved[min(i0 + (int)blockDim.x, a.n)];
+  __syncthreads();
+  // rows to copy before request i, and the token that the copy of a request starts from
+  for (int i = threadIdx.x; i < a.n; i += blockDim.x) {
+    sm.need[i] = sm.need[i] > 0 && served(sm, i) ? a.kept[i] - begin[i] * a.page : 0;
+    a.first[i] = begin[i] * a.page;
   }
+  __syncthreads();
+  sum_up(a, sm, [&](int i) { return sm.need[i]; });
+  for (int i = threadIdx.x; i < a.n; i += blockDim.x) a.moved[i + 1] = sm.ends[i];
   if (threadIdx.x == 0) a.moved[0] = 0;
 }
 

@@ -393,7 +393,7 @@ int take_book_space(const sol_attn3d_paged_cache* c, int n, void* workspace, siz
   return SOL_ATTN3D_OK;
 }
 
-constexpr size_t kBookSmem = sizeof(sol::BookSmem) + sol::kMaxRequests * sizeof(int);
+constexpr size_t kBookSmem = sizeof(sol::BookSmem);
 
 template <typename K>
 int launch_book(K kernel, const sol::BookArgs& b, cudaStream_t st) {
@@ -475,7 +475,7 @@ int sol_attn3d_cache_compact(const sol_attn3d_paged_cache* cache, int n, const i
   b.keep = keep;
   b.keep_stride = keep_width;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  sol::cache_keep_kernel<<<(unsigned)n, sol::kBookThreads, 0, st>>>(b);
+  sol::cache_keep_kernel<<<(unsigned)n, sol::kKeepThreads, 0, st>>>(b);
   if (cudaGetLastError() != cudaSuccess) return SOL_ATTN3D_ERR_CUDA;
   if ((rc = launch_book(sol::cache_compact_kernel, b, st)) != SOL_ATTN3D_OK) return rc;
   sol::MoveArgs m{};
@@ -494,8 +494,7 @@ int sol_attn3d_cache_free(const sol_attn3d_paged_cache* cache, int n, const int3
   sol::BookArgs b{};
   const int rc = take_book(cache, n, streams, status, &b);
   if (rc != SOL_ATTN3D_OK || n == 0) return rc;
-  sol::cache_free_kernel<<<1, sol::kBookThreads, 0, static_cast<cudaStream_t>(stream)>>>(b);
-  return cudaGetLastError() == cudaSuccess ? SOL_ATTN3D_OK : SOL_ATTN3D_ERR_CUDA;
+  return launch_book(sol::cache_free_kernel, b, static_cast<cudaStream_t>(stream));
 }
 
 int sol_attn3d_cache_copy_pages(const sol_attn3d_paged_cache* cache, int n, const int32_t* src_pages, const int32_t* dst_pages,
@@ -558,7 +557,7 @@ int sol_attn3d_cache_append(sol_attn3d_plan_t p, const void* q, const void* k, c
   const int chunks = p->head_dim / 8, rows = (q != nullptr ? p->heads : 0) + 2 * cache->kv_heads;
   const int unit = 32 / chunks;                            // rows per warp
   const int per_pass = std::min(256 / chunks, (rows + unit - 1) / unit * unit);
-  const long long blocks = std::min<long long>(p->total_tokens, 148ll * 16);
+  const long long blocks = std::min<long long>(p->total_tokens, 148ll * 3);   // one wave of resident blocks, a range of tokens each
   p->launches = 0;
   sol::cache_append_kernel<<<(unsigned)blocks, chunks * per_pass, 0, static_cast<cudaStream_t>(stream)>>>(a);
   const cudaError_t e = cudaGetLastError();

@@ -107,6 +107,7 @@ def test_append_edges():
     check_append([(0, 1, 4, 10), (5, 0, 1, 1), (0, 1, 2, 2)], [1, 0, 1], [33, 50], 2, 2, 128, 16, False, [[1, 2, 3]] * 3)
     check_append([(0, 2, 3, 5)], None, [30], 3, 3, 128, 64, True, [[5, 6, 7]], dims=(20, 0, 40))
     check_append([(0, 2, 3, 5)], None, [31], 3, 3, 64, 64, True, None, q=False)
+    check_append([(0, 2, 3, 5), (1, 3, 1, 1)], None, [31, 4], 1, 1, 128, 64, True, [[9, 8, 7]] * 2, q=False)
     one = torch.ones(64) * 3
     check_append([(0, 2, 3, 5)], None, [31], 3, 3, 64, 64, True, None, gains=[None, one])
     check_append([(0, 2, 3, 5)], None, [31], 3, 3, 64, 64, True, None, gains=[one, None])
@@ -208,6 +209,20 @@ def test_life_of_streams(page, kv, d):
     assert m.call("fork", [6, 8], [1, 9]) == [0, 0]
     assert m.call("free", list(range(10))) == [0] * 10
     assert set(m.book.refs) == {0} and set(m.book.lens) == {0}
+
+
+def test_requests_for_more_than_there_is():
+    """Sums of what is asked for pass 32 bits; nothing of it is served, what needs no page is."""
+    m = Model([1, 0, 16, 5], 16, 6, 1 << 20, layers=1)
+    big = (1 << 24) - 32
+    from paper_2609_35110_b200 import binding as B
+    n = 300
+    m2 = Model([1] + [0] * n, 16, 3, 1 << 16, layers=1)
+    status = torch.full((n,), -1, dtype=torch.int32, device="cuda")
+    B.sol_attn3d_cache_reserve(m2.cache, ints(list(range(1, n + 1))), ints([(1 << 20) - 5] * (n - 1) + [0]), status)
+    assert status.tolist() == [3] * (n - 1) + [0]
+    assert m2.cache.lens.tolist() == [1] + [0] * n and m2.cache.refs.tolist() == m2.book.refs
+    assert m.call("reserve", [0, 1, 2, 3], [big, big, 0, 11]) == [3, 3, 0, 0]
 
 
 @pytest.mark.parametrize("free", [0, 1, 2, 3, 5])
