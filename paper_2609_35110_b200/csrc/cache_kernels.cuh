@@ -23,6 +23,11 @@ struct PagedDev {
   int page, kv_heads;
 };
 
+// Kernels of this family may be launched while their predecessor in the stream still runs (programmatic dependent launch): each waits
+// for it here before it touches memory, and lets its own successor be launched at once, which saves some 3 us between short kernels.
+__device__ __forceinline__ void chained_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void chained_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 // Tokens of a stream that the table has room for.
 __device__ __forceinline__ long long stream_tokens(const PagedDev& c, long long stream) {
   const long long n = c.lens[stream], cap = c.width * c.page;
@@ -34,11 +39,12 @@ __device__ __forceinline__ long long stream_tokens(const PagedDev& c, long long 
 // the token's (t, h, w), offset per sequence, and rounded once; V is copied.  Row i of a chunk of n tokens becomes token
 // N - n + i of a stream of N.  Bound by HBM: every value is read and written once.
 //
-// A block takes a range of neighbouring tokens.  A thread owns a 16-byte chunk (8 dims) of a token's rows: Q heads, then K heads, then
-// V heads, `blockDim.x / chunks` rows apart, four of them in flight.  While a token's first loads are on their way, 64 threads find
-// the angles of its pairs, once for all heads: from the plan's tables, or, where positions are offset, from position times frequency
-// in fp64, brought to (-pi, pi] there (the tables end with the grid, and fp32 loses far positions).  (Every thread finding its own in
-// fp64: 106 us for 4,680 tokens x 40 heads, of which the angles took more than half.)
+// A block takes up to four neighbouring tokens at a time.  Its threads first find the angles of the tokens' pairs, one each, and the
+// tokens' places in the cache: the angles from the plan's tables, or, where positions are offset, from position times frequency in
+// fp64, brought to (-pi, pi] there (the tables end with the grid, and fp32 loses far positions).  Then a thread owns 16-byte chunks (8
+// dims) of the tokens' rows (Q heads, K heads, V heads), four at a time, the next four on their way.  (With every thread finding its own
+// angles, 4,680 tokens x 40 heads took 106 us; token by token, 93 us: a token's angles, table look-up and first loads then wait
+// for one another.)
 // ---------------------------------------------------------------------------------------------
 struct AppendArgs {
   const __nv_bfloat16* x[3];    // q, k, v of the new tokens (q may be nullptr)
@@ -54,12 +60,14 @@ struct AppendArgs {
   const int* streams;           // per sequence (caller's order), or nullptr: sequence s is stream s
   const int* pos0;              // [n_seqs][3] offsets of (t, h, w), or nullptr
   PagedDev c;
-  double omega[64];             // frequency of pair j of head_dim / 2, 0 where nothing rotates
+  const double* omega;          // frequency of pair j of head_dim / 2
 };
 
-__global__ void __launch_bounds__(256, 3) cache_append_kernel(const __grid_constant__ AppendArgs a) {
-  __shared__ float2 angle[2][64];
-  __shared__ int found;
+__global__ void __launch_bounds__(256, 3) cache_append_kernel(const __grid_constant__ AppendArgs a, int group) {
+  constexpr int kGroup = 4, kBatch = 4;
+  __shared__ float2 angle[kGroup][64];
+  __shared__ long long k_place[kGroup], v_place[kGroup];   // element offset of a token's first K and V head, -1: it is not written
+  __shared__ int found[kGroup], again[kGroup];
   const int D = a.g.head_dim, chunks = D >> 3;
   const int rows_per_pass = blockDim.x / chunks;
   const int chunk = threadIdx.x % chunks, sub = threadIdx.x / chunks;
@@ -67,75 +75,52 @@ __global__ void __launch_bounds__(256, 3) cache_append_kernel(const __grid_const
   const float inv_d = 1.0f / (float)D;
   const int n_q = a.x[0] != nullptr ? a.g.heads : 0, n_k = a.c.kv_heads, n_rows = n_q + 2 * n_k;
   const int d1 = a.g.rope[0], d2 = d1 + a.g.rope[1], d3 = d2 + a.g.rope[2];
-  constexpr int kBatch = 4;
+  chained_wait();
+  chained_next();
 
-  // the sequence that the block is in, and what follows from it; all of it the same for the whole block
-  SeqDev sq{};
-  long long seq_end = -1, first_at = 0;                    // end of its tokens; place of its first token in the stream
-  const int* table = nullptr;                              // nullptr: nothing of it is written to the cache
-  bool idle = false;
-  int turn = 0;
-
-  const long long begin = a.total_tokens * blockIdx.x / gridDim.x, end = a.total_tokens * (blockIdx.x + 1) / gridDim.x;
-  for (long long tok = begin; tok < end; ++tok) {
-    if (tok >= seq_end) {
-      for (int s = threadIdx.x; s < a.n_seqs; s += blockDim.x)
-        if (tok >= a.seqs[s].tok_start && tok < a.seqs[s].tok_start + a.seqs[s].n_tokens) found = s;
-      __syncthreads();
-      sq = a.seqs[found];
-      __syncthreads();
-      seq_end = sq.tok_start + sq.n_tokens;
-      const long long stream = a.streams != nullptr ? a.streams[sq.seq_id] : sq.seq_id;
-      idle = stream < 0 || stream >= a.c.n_streams;
-      table = nullptr;
-      if (!idle) {
-        // Of several sequences with one stream the first counts: they would write the same rows.
-        bool again = false;
-        if (a.streams != nullptr) {
-          for (int s = threadIdx.x; s < sq.seq_id; s += blockDim.x) again = again || a.streams[s] == stream;
-          again = __syncthreads_or(again) != 0;
-        }
-        if (!again) table = a.c.table + stream * a.c.width;
-        first_at = stream_tokens(a.c, stream) - sq.n_tokens;
-      }
-    }
-    if (idle) {
-      tok = seq_end - 1;
-      continue;
-    }
-    const int local = (int)(tok - sq.tok_start);
-    const bool rotate = local >= sq.text_len;
-    uint4 w[kBatch];
-    int which[kBatch], head[kBatch];
-    auto load = [&](int r0) {
+  for (long long tok0 = (long long)blockIdx.x * group; tok0 < a.total_tokens; tok0 += (long long)gridDim.x * group) {
+    const int n_tok = (int)min((long long)group, a.total_tokens - tok0);
+    // Item: (token, row).  token < 0: past the end.
+    auto item = [&](int idx, int& token, int& which, int& head) {
+      token = (idx >= n_rows) + (idx >= 2 * n_rows) + (idx >= 3 * n_rows);
+      const int r = idx - token * n_rows;
+      if (token >= n_tok || r >= n_rows) token = -1;
+      which = r < n_q ? 0 : r < n_q + n_k ? 1 : 2;
+      head = which == 0 ? r : which == 1 ? r - n_q : r - n_q - n_k;
+    };
+    auto load = [&](int base, uint4 (&w)[kBatch]) {
 #pragma unroll
       for (int b = 0; b < kBatch; ++b) {
-        const int r = r0 + sub + b * rows_per_pass;
-        which[b] = r < n_q ? 0 : r < n_q + n_k ? 1 : r < n_rows ? 2 : 3;
-        head[b] = which[b] == 0 ? r : which[b] == 1 ? r - n_q : r - n_q - n_k;
-        if (which[b] < 3) {
-          const long long x_tok = which[b] == 0 ? a.x_tok[0] : which[b] == 1 ? a.x_tok[1] : a.x_tok[2];
-          const long long x_head = which[b] == 0 ? a.x_head[0] : which[b] == 1 ? a.x_head[1] : a.x_head[2];
-          const __nv_bfloat16* x = which[b] == 0 ? a.x[0] : which[b] == 1 ? a.x[1] : a.x[2];
-          w[b] = __ldg(reinterpret_cast<const uint4*>(x + tok * x_tok + head[b] * x_head + chunk * 8));
-        } else {
-          w[b] = make_uint4(0, 0, 0, 0);
+        int token, which, head;
+        item(base + sub + b * rows_per_pass, token, which, head);
+        w[b] = make_uint4(0, 0, 0, 0);
+        if (token >= 0) {
+          const long long x_tok = which == 0 ? a.x_tok[0] : which == 1 ? a.x_tok[1] : a.x_tok[2];
+          const long long x_head = which == 0 ? a.x_head[0] : which == 1 ? a.x_head[1] : a.x_head[2];
+          const __nv_bfloat16* x = which == 0 ? a.x[0] : which == 1 ? a.x[1] : a.x[2];
+          w[b] = __ldg(reinterpret_cast<const uint4*>(x + (tok0 + token) * x_tok + head * x_head + chunk * 8));
         }
       }
     };
-    load(0);
-    const long long at = first_at + local;
-    long long page = -1;
-    if (table != nullptr && at >= 0) page = table[at / a.c.page];
-    for (int j = threadIdx.x; rotate && j < (D >> 1); j += blockDim.x) {
-      const int p = local - sq.text_len, hw = sq.H * sq.W;
-      const int d = 2 * j;                       // first head dim of the pair
-      const int axis = d < d1 ? 0 : d < d2 ? 1 : 2;
-      const int x = axis == 0 ? p / hw : axis == 1 ? (p / sq.W) % sq.H : p % sq.W;
+    uint4 w[kBatch];
+    load(0, w);
+    // ---- the tokens' sequences, places and angles
+    for (int g = 0; g < n_tok; ++g)
+      for (int s = threadIdx.x; s < a.n_seqs; s += blockDim.x)
+        if (tok0 + g >= a.seqs[s].tok_start && tok0 + g < a.seqs[s].tok_start + a.seqs[s].n_tokens) found[g] = s;
+    if (threadIdx.x < kGroup) again[threadIdx.x] = 0;
+    __syncthreads();
+    for (int j = threadIdx.x; j < n_tok * 64; j += blockDim.x) {
+      const int g = j >> 6, pair = j & 63;
+      const SeqDev& sq = a.seqs[found[g]];
+      const int local = (int)(tok0 + g - sq.tok_start), p = local - sq.text_len;
+      const int d = 2 * pair;                              // first head dim of the pair
       float2 cs = make_float2(1.f, 0.f);
-      if (d < d3) {
+      if (p >= 0 && d < d3) {
+        const int axis = d < d1 ? 0 : d < d2 ? 1 : 2;
+        const int x = axis == 0 ? p / (sq.H * sq.W) : axis == 1 ? (p / sq.W) % sq.H : p % sq.W;
         if (a.pos0 != nullptr) {
-          const double phi = (double)((long long)x + a.pos0[3 * sq.seq_id + axis]) * a.omega[j];
+          const double phi = (double)((long long)x + a.pos0[3 * sq.seq_id + axis]) * __ldg(a.omega + pair);
           const double turns = rint(phi * 0.15915494309189535);             // 1 / (2 pi)
           const double rest = fma(-turns, 2.4492935982947064e-16, fma(-turns, 6.283185307179586, phi));   // 2 pi in two parts
           sincosf((float)rest, &cs.y, &cs.x);
@@ -144,19 +129,43 @@ __global__ void __launch_bounds__(256, 3) cache_append_kernel(const __grid_const
           cs = __ldg(&a.tables[a.g.tab_off[axis] + x * (a.g.rope[axis] >> 1) + ((d - first) >> 1)]);
         }
       }
-      angle[turn][j] = cs;
+      angle[g][pair] = cs;
     }
-    __syncthreads();                                       // (two buffers: the next token's angles may come before the last reader is done)
-    float2 cs[4];
-    if (rotate) {
-#pragma unroll
-      for (int u = 0; u < 4; ++u) cs[u] = angle[turn][chunk * 4 + u];
+    if (threadIdx.x >= blockDim.x - 32) {                  // the last warp: a lane per token (the first ones may have more angles to find)
+      const int g = threadIdx.x - (blockDim.x - 32);
+      if (g < n_tok) {
+        const SeqDev& sq = a.seqs[found[g]];
+        const long long stream = a.streams != nullptr ? a.streams[sq.seq_id] : sq.seq_id;
+        long long k_at = -2, v_at = -2;                    // -2: an idle sequence
+        if (stream >= 0 && stream < a.c.n_streams) {
+          k_at = v_at = -1;
+          const long long at = stream_tokens(a.c, stream) - sq.n_tokens + (tok0 + g - sq.tok_start);
+          if (at >= 0) {
+            const int page = a.c.table[stream * a.c.width + at / a.c.page];
+            if (page >= 0 && page < a.c.n_pages) {         // (a table that names no page there: nothing is written)
+              k_at = page * a.c.ks[0] + (at % a.c.page) * a.c.ks[1];
+              v_at = page * a.c.vs[0] + (at % a.c.page) * a.c.vs[1];
+            }
+          }
+        }
+        k_place[g] = k_at;
+        v_place[g] = v_at;
+      }
     }
-    turn ^= 1;
-    const bool write = page >= 0 && page < a.c.n_pages;                    // (a table that names no page there: nothing is written)
-    const int in_page = write ? (int)(at % a.c.page) : 0;
-    for (int r0 = 0; r0 < n_rows; r0 += kBatch * rows_per_pass) {          // the same trip count for every thread
-      if (r0 > 0) load(r0);
+    // Of several sequences with one stream the first counts: they would write the same rows.
+    if (a.streams != nullptr)
+      for (int g = 0; g < n_tok; ++g) {
+        const int id = a.seqs[found[g]].seq_id, stream = a.streams[id];
+        for (int s = threadIdx.x; s < id; s += blockDim.x)
+          if (a.streams[s] == stream) again[g] = 1;
+      }
+    __syncthreads();
+
+    // ---- the rows
+    const int n_items = n_tok * n_rows, step = kBatch * rows_per_pass;
+    for (int base = 0; base < n_items; base += step) {     // the same trip count for every thread
+      uint4 ahead[kBatch];
+      if (base + step < n_items) load(base + step, ahead);
       float rinv[kBatch];
       if (a.gain[0] != nullptr || a.gain[1] != nullptr) {
         // Sums of squares of the rows, by shuffles over a row's chunks; where they leave fp32's range, once more on scaled values.
@@ -202,9 +211,11 @@ __global__ void __launch_bounds__(256, 3) cache_append_kernel(const __grid_const
       }
 #pragma unroll
       for (int b = 0; b < kBatch; ++b) {
-        if (which[b] == 3) break;
+        int token, which, head;
+        item(base + sub + b * rows_per_pass, token, which, head);
+        if (token < 0 || k_place[token] == -2) continue;
         uint4 y = w[b];
-        if (which[b] < 2) {
+        if (which < 2) {
           const uint32_t x[4] = {w[b].x, w[b].y, w[b].z, w[b].w};
           float f[8];
 #pragma unroll
@@ -212,7 +223,7 @@ __global__ void __launch_bounds__(256, 3) cache_append_kernel(const __grid_const
             f[2 * u] = __uint_as_float(x[u] << 16);
             f[2 * u + 1] = __uint_as_float(x[u] & 0xffff0000u);
           }
-          const float* gain = which[b] == 0 ? a.gain[0] : a.gain[1];
+          const float* gain = which == 0 ? a.gain[0] : a.gain[1];
           if (gain != nullptr) {
             const float4 g0 = __ldg(reinterpret_cast<const float4*>(gain + chunk * 8));
             const float4 g1 = __ldg(reinterpret_cast<const float4*>(gain + chunk * 8) + 1);
@@ -220,26 +231,27 @@ __global__ void __launch_bounds__(256, 3) cache_append_kernel(const __grid_const
             f[0] = f[0] * r * g0.x; f[1] = f[1] * r * g0.y; f[2] = f[2] * r * g0.z; f[3] = f[3] * r * g0.w;
             f[4] = f[4] * r * g1.x; f[5] = f[5] * r * g1.y; f[6] = f[6] * r * g1.z; f[7] = f[7] * r * g1.w;
           }
-          if (rotate) {
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-              if (cs[u].x == 1.f && cs[u].y == 0.f) continue;              // (keeps infinities in dims that do not rotate)
-              const float re = f[2 * u], ro = f[2 * u + 1];
-              f[2 * u] = re * cs[u].x - ro * cs[u].y;
-              f[2 * u + 1] = re * cs[u].y + ro * cs[u].x;
-            }
+          for (int u = 0; u < 4; ++u) {
+            const float2 cs = angle[token][chunk * 4 + u];
+            if (cs.x == 1.f && cs.y == 0.f) continue;                      // (keeps infinities in dims that do not rotate)
+            const float re = f[2 * u], ro = f[2 * u + 1];
+            f[2 * u] = re * cs.x - ro * cs.y;
+            f[2 * u + 1] = re * cs.y + ro * cs.x;
           }
           y = make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
         }
-        if (which[b] == 0) {
-          *reinterpret_cast<uint4*>(a.q_out + (tok * a.g.heads + head[b]) * (long long)D + chunk * 8) = y;
-        } else if (write) {
-          __nv_bfloat16* dst = which[b] == 1 ? a.c.k + page * a.c.ks[0] + in_page * a.c.ks[1] + head[b] * a.c.ks[2]
-                                             : a.c.v + page * a.c.vs[0] + in_page * a.c.vs[1] + head[b] * a.c.vs[2];
+        if (which == 0) {
+          *reinterpret_cast<uint4*>(a.q_out + ((tok0 + token) * a.g.heads + head) * (long long)D + chunk * 8) = y;
+        } else if (k_place[token] >= 0 && again[token] == 0) {
+          __nv_bfloat16* dst = which == 1 ? a.c.k + k_place[token] + head * a.c.ks[2] : a.c.v + v_place[token] + head * a.c.vs[2];
           *reinterpret_cast<uint4*>(dst + chunk * 8) = y;
         }
       }
+#pragma unroll
+      for (int b = 0; b < kBatch; ++b) w[b] = ahead[b];
     }
+    __syncthreads();                                       // places and angles are found anew for the next tokens
   }
 }
 
@@ -389,6 +401,8 @@ __device__ __forceinline__ Served allocate(const BookArgs& a, BookSmem& sm, cons
 __global__ void __launch_bounds__(kBookThreads) cache_free_kernel(const BookArgs a) {
   extern __shared__ __align__(16) unsigned char book_raw[];
   BookSmem& sm = *reinterpret_cast<BookSmem*>(book_raw);
+  chained_wait();
+  chained_next();
   load_streams(a, sm);
   const int lane = threadIdx.x & 31;
   for (int i = threadIdx.x >> 5; i < a.n; i += blockDim.x >> 5) {          // a warp per request
@@ -414,6 +428,8 @@ __global__ void __launch_bounds__(kBookThreads) cache_free_kernel(const BookArgs
 __global__ void __launch_bounds__(kBookThreads) cache_reserve_kernel(const BookArgs a) {
   extern __shared__ __align__(16) unsigned char book_raw[];
   BookSmem& sm = *reinterpret_cast<BookSmem*>(book_raw);
+  chained_wait();
+  chained_next();
   load_streams(a, sm);
   for (int i = threadIdx.x; i < a.n; i += blockDim.x) {
     int need = -1, st = kCacheBadStream;
@@ -440,6 +456,8 @@ __global__ void __launch_bounds__(kBookThreads) cache_fork_kernel(const BookArgs
   extern __shared__ __align__(16) unsigned char book_raw[];
   BookSmem& sm = *reinterpret_cast<BookSmem*>(book_raw);
   int* len = sm.extra;                                     // of the parents, before anything changes
+  chained_wait();
+  chained_next();
   load_streams(a, sm);
   for (int i = threadIdx.x; i < a.n; i += blockDim.x) {
     int st = kCacheBadStream, need = -1;
@@ -492,6 +510,8 @@ __global__ void __launch_bounds__(kBookThreads) cache_fork_kernel(const BookArgs
 __global__ void __launch_bounds__(kKeepThreads) cache_keep_kernel(const BookArgs a) {
   __shared__ long long warp_sum[32];
   __shared__ int lowest, whole;
+  chained_wait();
+  chained_next();
   const int i = blockIdx.x;
   if (threadIdx.x == 0) lowest = 0x7fffffff;
   const int s = a.streams[i];
@@ -545,6 +565,8 @@ __global__ void __launch_bounds__(kBookThreads) cache_compact_kernel(const BookA
   extern __shared__ __align__(16) unsigned char book_raw[];
   BookSmem& sm = *reinterpret_cast<BookSmem*>(book_raw);
   int* begin = sm.extra;                                   // the first page that does not stay
+  chained_wait();
+  chained_next();
   load_streams(a, sm);
   for (int i = threadIdx.x; i < a.n; i += blockDim.x) {
     int need = -1, st = kCacheBadStream;
@@ -616,6 +638,8 @@ struct MoveArgs {
 
 template <bool kPages>
 __global__ void __launch_bounds__(256) cache_move_kernel(const MoveArgs a) {
+  chained_wait();
+  chained_next();
   const int lane = threadIdx.x & 31;
   const long long rows = kPages ? (long long)a.n * a.page : a.moved[a.n];
   const long long items = rows * a.layers;

@@ -135,6 +135,8 @@ template <int D, bool kPaged>
 __global__ void __launch_bounds__(kFewThreads, kFewResident) few_rows_kernel(const __grid_constant__ FewArgs p) {
   using L = FewSmem<D>;
   extern __shared__ __align__(16) uint8_t few_smem[];
+  chained_wait();
+  chained_next();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
 
   // ---- which rows, which keys
@@ -467,6 +469,8 @@ template <int D, bool kPaged, bool kListed>
 __global__ void __launch_bounds__(256) join_rows_kernel(const __grid_constant__ JoinArgs p) {
   int kv_head, n_tok;
   long long tok0, row0;
+  chained_wait();
+  chained_next();
   if (kListed) {
     const JoinUnit u = p.list[blockIdx.x];
     kv_head = u.kv_head;
@@ -501,27 +505,45 @@ __global__ void __launch_bounds__(256) join_rows_kernel(const __grid_constant__ 
   constexpr int kChunks = D / 8;
   const float* part = p.partial + (long long)blockIdx.x * p.n_split * p.rows_per_unit * (D + 4);
   const int x = blockIdx.y * 256 + threadIdx.x;
-  if (x < n_rows * kChunks) {
-    const int row = x / kChunks, d0 = (x % kChunks) * 8;
+  const int row = x / kChunks, d0 = (x % kChunks) * 8;
+  const unsigned team = __ballot_sync(0xffffffffu, row < n_rows);          // whole teams of kChunks threads, one per row
+  if (row < n_rows) {
     const float* mine = part + (long long)row * (D + 4);
     const long long step = (long long)p.rows_per_unit * (D + 4);
+    // The team's threads look at a part's statistics each, kChunks parts at a time; the weights then come by shuffle, so that the loads
+    // of the values do not wait for them one by one.
+    const int lane = threadIdx.x % kChunks;
     float top = -CUDART_INF_F;
     bool any = false;
-    for (int s = 0; s < p.n_split; ++s) {
-      const float4 t = __ldg(reinterpret_cast<const float4*>(mine + s * step + D));
-      top = fmaxf(top, t.x);
-      any = any || t.z != 0.f;
+    for (int s0 = 0; s0 < p.n_split; s0 += kChunks)
+      if (s0 + lane < p.n_split) {
+        const float4 t = __ldg(reinterpret_cast<const float4*>(mine + (s0 + lane) * step + D));
+        top = fmaxf(top, t.x);
+        any = any || t.z != 0.f;
+      }
+#pragma unroll
+    for (int o = kChunks / 2; o > 0; o >>= 1) {
+      top = fmaxf(top, __shfl_xor_sync(team, top, o));
+      any = __shfl_xor_sync(team, (int)any, o) != 0 || any;
     }
     float sum = 0.f, acc[8] = {};
+    for (int s0 = 0; s0 < p.n_split; s0 += kChunks) {
+      float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (s0 + lane < p.n_split) t = __ldg(reinterpret_cast<const float4*>(mine + (s0 + lane) * step + D));
+      const float weight = t.z == 0.f ? 0.f : t.x == top ? 1.f : ex2_approx((t.x - top) * p.a.scale_log2);
+      const float share = t.z == 0.f ? 0.f : t.y * weight;
 #pragma unroll 4
-    for (int s = 0; s < p.n_split; ++s) {
-      const float4 t = __ldg(reinterpret_cast<const float4*>(mine + s * step + D));
-      const float4 u = __ldg(reinterpret_cast<const float4*>(mine + s * step + d0)), v = __ldg(reinterpret_cast<const float4*>(mine + s * step + d0 + 4));
-      if (t.z == 0.f) continue;
-      const float f = t.x == top ? 1.f : ex2_approx((t.x - top) * p.a.scale_log2);
-      sum = fmaf(t.y, f, sum);
-      acc[0] = fmaf(u.x, f, acc[0]); acc[1] = fmaf(u.y, f, acc[1]); acc[2] = fmaf(u.z, f, acc[2]); acc[3] = fmaf(u.w, f, acc[3]);
-      acc[4] = fmaf(v.x, f, acc[4]); acc[5] = fmaf(v.y, f, acc[5]); acc[6] = fmaf(v.z, f, acc[6]); acc[7] = fmaf(v.w, f, acc[7]);
+      for (int s = 0; s < kChunks; ++s) {
+        if (s0 + s >= p.n_split) break;
+        const float4 u = __ldg(reinterpret_cast<const float4*>(mine + (s0 + s) * step + d0)), v = __ldg(reinterpret_cast<const float4*>(mine + (s0 + s) * step + d0 + 4));
+        const float f = __shfl_sync(team, weight, s, kChunks);
+        const bool there = __shfl_sync(team, t.z, s, kChunks) != 0.f;
+        sum += __shfl_sync(team, share, s, kChunks);
+        if (there) {
+          acc[0] = fmaf(u.x, f, acc[0]); acc[1] = fmaf(u.y, f, acc[1]); acc[2] = fmaf(u.z, f, acc[2]); acc[3] = fmaf(u.w, f, acc[3]);
+          acc[4] = fmaf(v.x, f, acc[4]); acc[5] = fmaf(v.y, f, acc[5]); acc[6] = fmaf(v.z, f, acc[6]); acc[7] = fmaf(v.w, f, acc[7]);
+        }
+      }
     }
     const float inv = 1.f / sum;
     const long long r = row0 + row;

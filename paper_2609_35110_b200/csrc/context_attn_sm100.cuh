@@ -113,6 +113,8 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
   UnitDev* units = reinterpret_cast<UnitDev*>(smem + L::kOffUnits);
   const unsigned long long limit = p.wait_limit_ns;
 
+  chained_wait();
+  chained_next();
   if (warp == 8 && lane == 0) {
     for (int s = 0; s < L::kStages; ++s) { mbar_init(bar_kv_full(s), 1); mbar_init(bar_kv_empty(s), 1); }
     for (int t = 0; t < 2; ++t) {

@@ -65,7 +65,7 @@ struct sol_attn3d_plan_s {
 
   // workspace layout (byte offsets)
   size_t off_status = 0, off_tables = 0, off_seqs = 0, off_keybits = 0, off_list = 0, off_count = 0, off_pairs = 0,
-         off_dbits = 0, off_dlist = 0, off_dcount = 0, off_drange = 0, off_cum = 0,
+         off_dbits = 0, off_dlist = 0, off_dcount = 0, off_drange = 0, off_cum = 0, off_omega = 0,
          off_qrot = 0, off_krot = 0, ws_bytes = 0;
   size_t ws_dense_bytes = 0;          // what sol_attn3d_forward and its variants use (a prefix of the workspace)
   int total_pairs = 0;
@@ -377,6 +377,7 @@ int build_plan(sol_attn3d_plan_t* out, const sol_attn3d_desc* d) {
       p->off_drange = off;  off = align_up(off + range_bytes(p));
     }
     p->off_cum = off;       off = align_up(off + (size_t)p->n_seqs * sizeof(int));
+    p->off_omega = off;     off = align_up(off + 64 * sizeof(double));
     p->ws_bytes = off;
 
     if (const char* e = std::getenv("SOL_ATTN3D_WAIT_LIMIT_MS")) {
@@ -560,6 +561,10 @@ int sol_attn3d_set_workspace(sol_attn3d_plan_t p, void* device_ptr, size_t bytes
     return fail_cuda(p, e);
   if ((e = cudaMemcpy(p->ws + p->off_cum, p->cum_tok.data(), p->cum_tok.size() * sizeof(int), cudaMemcpyHostToDevice)) != cudaSuccess)
     return fail_cuda(p, e);
+  double omega[64] = {};                                   // frequency of pair j of a row, over the three axes
+  for (int axis = 0, pair = 0; axis < 3; ++axis)
+    for (int j = 0; j < p->rope[axis] / 2; ++j) omega[pair++] = std::exp(-(2.0 * j / p->rope[axis]) * std::log(p->theta));
+  if ((e = cudaMemcpy(p->ws + p->off_omega, omega, sizeof(omega), cudaMemcpyHostToDevice)) != cudaSuccess) return fail_cuda(p, e);
   const Strides dense{(long long)p->heads * p->head_dim, (long long)p->head_dim};
   int rc = encode_map(p->encode, p, &p->tm_q, p->ws + p->off_qrot, dense);
   if (rc == SOL_ATTN3D_OK) rc = encode_map(p->encode, p, &p->tm_k, p->ws + p->off_krot, dense);

@@ -5,6 +5,24 @@ namespace {
 
 bool aligned4(const void* x) { return (reinterpret_cast<uintptr_t>(x) & 3u) == 0; }
 
+// Launches a kernel that begins with chained_wait(): it may be placed on the GPU while its predecessor in the stream still runs.
+template <typename... Params, typename... Args>
+cudaError_t launch_chained(void (*kernel)(Params...), dim3 grid, unsigned threads, size_t smem, cudaStream_t st, const Args&... args) {
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, args...);
+  if (e != cudaSuccess) (void)cudaGetLastError();
+  return e;
+}
+
 // Checks a cache and, for a layer, fills in what the kernels see of it.
 int take_cache(const sol_attn3d_paged_cache* c, int layer, sol::PagedDev* out) {
   if (c == nullptr || c->size != sizeof(sol_attn3d_paged_cache) || c->n_layers < 1 || c->page_size < 1 || c->kv_heads < 1 ||
@@ -93,13 +111,11 @@ cudaError_t launch_few(const sol::FewArgs& f, cudaStream_t st, int* launches) {
   const unsigned items = (unsigned)(f.units * f.d.c.kv_heads);
   cudaError_t e = cudaFuncSetAttribute(sol::few_rows_kernel<D, kPaged>, cudaFuncAttributeMaxDynamicSharedMemorySize, sol::FewSmem<D>::kBytes);
   if (e != cudaSuccess) return e;
-  sol::few_rows_kernel<D, kPaged><<<items * (unsigned)f.n_split, sol::kFewThreads, sol::FewSmem<D>::kBytes, st>>>(f);
-  if ((e = cudaGetLastError()) != cudaSuccess) return e;
+  if ((e = launch_chained(sol::few_rows_kernel<D, kPaged>, items * (unsigned)f.n_split, sol::kFewThreads, sol::FewSmem<D>::kBytes, st, f)) != cudaSuccess) return e;
   ++*launches;
   if (f.partial != nullptr) {
     const sol::JoinArgs j{f.a, f.d, f.n_split, sol::kFewRows, f.units, f.partial, nullptr};
-    sol::join_rows_kernel<D, kPaged, false><<<dim3(items, (sol::kFewRows * D / 8 + 255) / 256), 256, 0, st>>>(j);
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    if ((e = launch_chained(sol::join_rows_kernel<D, kPaged, false>, dim3(items, (sol::kFewRows * D / 8 + 255) / 256), 256, 0, st, j)) != cudaSuccess) return e;
     ++*launches;
   }
   return cudaSuccess;
@@ -205,13 +221,13 @@ template <int D, bool kPaged, bool kMask>
 cudaError_t launch_context_as(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const sol::ContextParams& c, int sms, cudaStream_t st, int* launches) {
   cudaError_t e = cudaFuncSetAttribute(sol::context_attn_kernel<D, kPaged, kMask>, cudaFuncAttributeMaxDynamicSharedMemorySize, sol::ContextSmem<D>::kDynBytes);
   if (e != cudaSuccess) return e;
-  sol::context_attn_kernel<D, kPaged, kMask><<<(unsigned)std::min<long long>(c.total, sms), sol::kAttnThreads, sol::ContextSmem<D>::kDynBytes, st>>>(q, k, v, c);
-  if ((e = cudaGetLastError()) != cudaSuccess) return e;
+  if ((e = launch_chained(sol::context_attn_kernel<D, kPaged, kMask>, (unsigned)std::min<long long>(c.total, sms), sol::kAttnThreads, sol::ContextSmem<D>::kDynBytes, st,
+                          q, k, v, c)) != cudaSuccess) return e;
   ++*launches;
   if (c.partial != nullptr) {
     const sol::JoinArgs j{c.a, c.d, c.n_split, 2 * c.tok_per_tile * c.a.group, c.units, c.partial, c.join};
-    sol::join_rows_kernel<D, kPaged, true><<<dim3((unsigned)c.n_tail, (unsigned)(j.rows_per_unit * D / 8 + 255) / 256), 256, 0, st>>>(j);
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    if ((e = launch_chained(sol::join_rows_kernel<D, kPaged, true>, dim3((unsigned)c.n_tail, (unsigned)(j.rows_per_unit * D / 8 + 255) / 256), 256, 0, st, j)) != cudaSuccess)
+      return e;
     ++*launches;
   }
   return cudaSuccess;
@@ -401,8 +417,7 @@ int launch_book(K kernel, const sol::BookArgs& b, cudaStream_t st) {
     (void)cudaGetLastError();
     return SOL_ATTN3D_ERR_CUDA;
   }
-  kernel<<<1, sol::kBookThreads, kBookSmem, st>>>(b);
-  return cudaGetLastError() == cudaSuccess ? SOL_ATTN3D_OK : SOL_ATTN3D_ERR_CUDA;
+  return launch_chained(kernel, 1, sol::kBookThreads, kBookSmem, st, b) == cudaSuccess ? SOL_ATTN3D_OK : SOL_ATTN3D_ERR_CUDA;
 }
 
 template <bool kPages>
@@ -424,8 +439,7 @@ int launch_move(const sol_attn3d_paged_cache* c, sol::MoveArgs m, cudaStream_t s
   m.head_dim = c->head_dim;
   m.n_pages = c->n_pages;
   // the number of rows is on the device: eight resident blocks per SM walk over them
-  sol::cache_move_kernel<kPages><<<148 * 8, 256, 0, st>>>(m);
-  return cudaGetLastError() == cudaSuccess ? SOL_ATTN3D_OK : SOL_ATTN3D_ERR_CUDA;
+  return launch_chained(sol::cache_move_kernel<kPages>, 148 * 8, 256, 0, st, m) == cudaSuccess ? SOL_ATTN3D_OK : SOL_ATTN3D_ERR_CUDA;
 }
 
 }  // namespace
@@ -475,8 +489,7 @@ int sol_attn3d_cache_compact(const sol_attn3d_paged_cache* cache, int n, const i
   b.keep = keep;
   b.keep_stride = keep_width;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  sol::cache_keep_kernel<<<(unsigned)n, sol::kKeepThreads, 0, st>>>(b);
-  if (cudaGetLastError() != cudaSuccess) return SOL_ATTN3D_ERR_CUDA;
+  if (launch_chained(sol::cache_keep_kernel, (unsigned)n, sol::kKeepThreads, 0, st, b) != cudaSuccess) return SOL_ATTN3D_ERR_CUDA;
   if ((rc = launch_book(sol::cache_compact_kernel, b, st)) != SOL_ATTN3D_OK) return rc;
   sol::MoveArgs m{};
   m.n = n;
@@ -552,15 +565,15 @@ int sol_attn3d_cache_append(sol_attn3d_plan_t p, const void* q, const void* k, c
   a.g.heads = p->heads;
   a.streams = streams;
   a.pos0 = pos0;
-  for (int axis = 0, pair = 0; axis < 3; ++axis)
-    for (int j = 0; j < p->rope[axis] / 2; ++j) a.omega[pair++] = std::exp(-(2.0 * j / p->rope[axis]) * std::log(p->theta));
+  a.omega = reinterpret_cast<const double*>(p->ws + p->off_omega);
   const int chunks = p->head_dim / 8, rows = (q != nullptr ? p->heads : 0) + 2 * cache->kv_heads;
   const int unit = 32 / chunks;                            // rows per warp
-  const int per_pass = std::min(256 / chunks, (rows + unit - 1) / unit * unit);
-  const long long blocks = std::min<long long>(p->total_tokens, 148ll * 3);   // one wave of resident blocks, a range of tokens each
+  // four tokens at a time, unless that leaves SMs idle
+  const int group = p->total_tokens >= 148 * 3 * 4 ? 4 : 1;
+  const int per_pass = std::min(256 / chunks, (rows * group + unit - 1) / unit * unit);
+  const long long blocks = std::min<long long>((p->total_tokens + group - 1) / group, 148ll * 3 * 8);
   p->launches = 0;
-  sol::cache_append_kernel<<<(unsigned)blocks, chunks * per_pass, 0, static_cast<cudaStream_t>(stream)>>>(a);
-  const cudaError_t e = cudaGetLastError();
+  const cudaError_t e = launch_chained(sol::cache_append_kernel, (unsigned)blocks, (unsigned)(chunks * per_pass), 0, static_cast<cudaStream_t>(stream), a, group);
   if (e != cudaSuccess) return fail_cuda(p, e);
   ++p->launches;
   return SOL_ATTN3D_OK;
