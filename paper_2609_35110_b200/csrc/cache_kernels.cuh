@@ -8,6 +8,7 @@
 #include <cuda_runtime.h>
 
 #include "device_types.cuh"
+#include "ptx_sm100.cuh"
 
 namespace sol {
 
@@ -42,9 +43,9 @@ __device__ __forceinline__ long long stream_tokens(const PagedDev& c, long long 
 // A block takes up to four neighbouring tokens at a time.  Its threads first find the angles of the tokens' pairs, one each, and the
 // tokens' places in the cache: the angles from the plan's tables, or, where positions are offset, from position times frequency in
 // fp64, brought to (-pi, pi] there (the tables end with the grid, and fp32 loses far positions).  Then a thread owns 16-byte chunks (8
-// dims) of the tokens' rows (Q heads, K heads, V heads), four at a time, the next four on their way.  (With every thread finding its own
-// angles, 4,680 tokens x 40 heads took 106 us; token by token, 93 us: a token's angles, table look-up and first loads then wait
-// for one another.)
+// dims) of rows, four rows at a time: the same head of the four tokens (kTokens = 4), or four heads of one (kTokens = 1: few tokens);
+// all Q heads, then all K heads, then V.  Issuing the instructions bounds it, so a row's address is a base per token and an offset per
+// head (found row by row they made 183 instructions per 8 values of a lane: 98 us for 4,680 tokens x 40 heads).
 // ---------------------------------------------------------------------------------------------
 struct AppendArgs {
   const __nv_bfloat16* x[3];    // q, k, v of the new tokens (q may be nullptr)
@@ -63,55 +64,52 @@ struct AppendArgs {
   const double* omega;          // frequency of pair j of head_dim / 2
 };
 
-__global__ void __launch_bounds__(256, 3) cache_append_kernel(const __grid_constant__ AppendArgs a, int group) {
-  constexpr int kGroup = 4, kBatch = 4;
-  __shared__ float2 angle[kGroup][64];
-  __shared__ long long k_place[kGroup], v_place[kGroup];   // element offset of a token's first K and V head, -1: it is not written
-  __shared__ int found[kGroup], again[kGroup];
-  const int D = a.g.head_dim, chunks = D >> 3;
-  const int rows_per_pass = blockDim.x / chunks;
-  const int chunk = threadIdx.x % chunks, sub = threadIdx.x / chunks;
+template <int D, int kTokens>
+__global__ void __launch_bounds__(256, 3) cache_append_kernel(const __grid_constant__ AppendArgs a) {
+  constexpr int kBatch = 4, kChunks = D / 8;
+  __shared__ __align__(16) float2 angle[kTokens][D / 2];
+  __shared__ __nv_bfloat16* place[3][kTokens];             // where a token's first Q, K and V head go; nullptr: nowhere
+  __shared__ int found[kTokens], rotates[kTokens];
+  const int rows_per_pass = blockDim.x / kChunks;
+  const int chunk = threadIdx.x % kChunks, sub = threadIdx.x / kChunks;
   const unsigned lanes = __activemask();
-  const float inv_d = 1.0f / (float)D;
-  const int n_q = a.x[0] != nullptr ? a.g.heads : 0, n_k = a.c.kv_heads, n_rows = n_q + 2 * n_k;
   const int d1 = a.g.rope[0], d2 = d1 + a.g.rope[1], d3 = d2 + a.g.rope[2];
+  // Step: a tensor and a batch of its heads.
+  constexpr int kHeads = kBatch / kTokens;
+  const int head_step = kHeads * rows_per_pass;
+  const int q_steps = a.x[0] != nullptr ? (a.g.heads + head_step - 1) / head_step : 0, k_steps = (a.c.kv_heads + head_step - 1) / head_step;
+  const int steps = q_steps + 2 * k_steps;
+  auto step_of = [&](int it, int& which, int& n, int& h0) {
+    which = it < q_steps ? 0 : it < q_steps + k_steps ? 1 : 2;
+    n = which == 0 ? a.g.heads : a.c.kv_heads;
+    h0 = (which == 0 ? it : which == 1 ? it - q_steps : it - q_steps - k_steps) * head_step + sub;
+  };
   chained_wait();
   chained_next();
 
-  for (long long tok0 = (long long)blockIdx.x * group; tok0 < a.total_tokens; tok0 += (long long)gridDim.x * group) {
-    const int n_tok = (int)min((long long)group, a.total_tokens - tok0);
-    // Item: (token, row).  token < 0: past the end.
-    auto item = [&](int idx, int& token, int& which, int& head) {
-      token = (idx >= n_rows) + (idx >= 2 * n_rows) + (idx >= 3 * n_rows);
-      const int r = idx - token * n_rows;
-      if (token >= n_tok || r >= n_rows) token = -1;
-      which = r < n_q ? 0 : r < n_q + n_k ? 1 : 2;
-      head = which == 0 ? r : which == 1 ? r - n_q : r - n_q - n_k;
-    };
-    auto load = [&](int base, uint4 (&w)[kBatch]) {
+  for (long long tok0 = (long long)blockIdx.x * kTokens; tok0 < a.total_tokens; tok0 += (long long)gridDim.x * kTokens) {
+    const int n_tok = (int)min((long long)kTokens, a.total_tokens - tok0);
+    uint4 ahead[kBatch];
+    auto load = [&](int it) {                              // (past the end: the last head or token again, not stored)
+      int which, n, h0;
+      step_of(it, which, n, h0);
+      const long long x_tok = a.x_tok[which];
+      const int x_head = (int)a.x_head[which];
+      const __nv_bfloat16* src = a.x[which] + tok0 * x_tok + chunk * 8;
 #pragma unroll
       for (int b = 0; b < kBatch; ++b) {
-        int token, which, head;
-        item(base + sub + b * rows_per_pass, token, which, head);
-        w[b] = make_uint4(0, 0, 0, 0);
-        if (token >= 0) {
-          const long long x_tok = which == 0 ? a.x_tok[0] : which == 1 ? a.x_tok[1] : a.x_tok[2];
-          const long long x_head = which == 0 ? a.x_head[0] : which == 1 ? a.x_head[1] : a.x_head[2];
-          const __nv_bfloat16* x = which == 0 ? a.x[0] : which == 1 ? a.x[1] : a.x[2];
-          w[b] = __ldg(reinterpret_cast<const uint4*>(x + (tok0 + token) * x_tok + head * x_head + chunk * 8));
-        }
+        const int h = min(h0 + b / kTokens * rows_per_pass, n - 1);
+        ahead[b] = __ldg(reinterpret_cast<const uint4*>(src + min(b % kTokens, n_tok - 1) * x_tok + (long long)h * x_head));
       }
     };
-    uint4 w[kBatch];
-    load(0, w);
+    load(0);
     // ---- the tokens' sequences, places and angles
     for (int g = 0; g < n_tok; ++g)
       for (int s = threadIdx.x; s < a.n_seqs; s += blockDim.x)
         if (tok0 + g >= a.seqs[s].tok_start && tok0 + g < a.seqs[s].tok_start + a.seqs[s].n_tokens) found[g] = s;
-    if (threadIdx.x < kGroup) again[threadIdx.x] = 0;
     __syncthreads();
-    for (int j = threadIdx.x; j < n_tok * 64; j += blockDim.x) {
-      const int g = j >> 6, pair = j & 63;
+    for (int j = threadIdx.x; j < n_tok * (D / 2); j += blockDim.x) {
+      const int g = j / (D / 2), pair = j % (D / 2);
       const SeqDev& sq = a.seqs[found[g]];
       const int local = (int)(tok0 + g - sq.tok_start), p = local - sq.text_len;
       const int d = 2 * pair;                              // first head dim of the pair
@@ -131,125 +129,122 @@ __global__ void __launch_bounds__(256, 3) cache_append_kernel(const __grid_const
       }
       angle[g][pair] = cs;
     }
-    if (threadIdx.x >= blockDim.x - 32) {                  // the last warp: a lane per token (the first ones may have more angles to find)
-      const int g = threadIdx.x - (blockDim.x - 32);
-      if (g < n_tok) {
+    if (threadIdx.x >= blockDim.x - 32) {                  // the last warp: places (the first ones may have more angles to find)
+      const int lane = threadIdx.x & 31;
+      for (int g = 0; g < n_tok; ++g) {
         const SeqDev& sq = a.seqs[found[g]];
         const long long stream = a.streams != nullptr ? a.streams[sq.seq_id] : sq.seq_id;
-        long long k_at = -2, v_at = -2;                    // -2: an idle sequence
-        if (stream >= 0 && stream < a.c.n_streams) {
-          k_at = v_at = -1;
-          const long long at = stream_tokens(a.c, stream) - sq.n_tokens + (tok0 + g - sq.tok_start);
-          if (at >= 0) {
-            const int page = a.c.table[stream * a.c.width + at / a.c.page];
-            if (page >= 0 && page < a.c.n_pages) {         // (a table that names no page there: nothing is written)
-              k_at = page * a.c.ks[0] + (at % a.c.page) * a.c.ks[1];
-              v_at = page * a.c.vs[0] + (at % a.c.page) * a.c.vs[1];
+        // Of several sequences with one stream the first counts: they would write the same rows.
+        bool again = false;
+        if (a.streams != nullptr)
+          for (int s = lane; s < sq.seq_id; s += 32) again = again || a.streams[s] == stream;
+        again = __any_sync(0xffffffffu, again);
+        if (lane == 0) {
+          place[0][g] = place[1][g] = place[2][g] = nullptr;
+          if (stream >= 0 && stream < a.c.n_streams) {     // (otherwise an idle sequence)
+            place[0][g] = a.q_out + (tok0 + g) * a.g.heads * (long long)D;
+            const long long at = stream_tokens(a.c, stream) - sq.n_tokens + (tok0 + g - sq.tok_start);
+            if (at >= 0 && !again) {
+              const int page = a.c.table[stream * a.c.width + (int)at / a.c.page], row = (int)at % a.c.page;
+              if (page >= 0 && page < a.c.n_pages) {       // (a table that names no page there: nothing is written)
+                place[1][g] = a.c.k + page * a.c.ks[0] + row * a.c.ks[1];
+                place[2][g] = a.c.v + page * a.c.vs[0] + row * a.c.vs[1];
+              }
             }
           }
+          rotates[g] = tok0 + g - sq.tok_start >= sq.text_len;
         }
-        k_place[g] = k_at;
-        v_place[g] = v_at;
       }
     }
-    // Of several sequences with one stream the first counts: they would write the same rows.
-    if (a.streams != nullptr)
-      for (int g = 0; g < n_tok; ++g) {
-        const int id = a.seqs[found[g]].seq_id, stream = a.streams[id];
-        for (int s = threadIdx.x; s < id; s += blockDim.x)
-          if (a.streams[s] == stream) again[g] = 1;
-      }
     __syncthreads();
 
-    // ---- the rows
-    const int n_items = n_tok * n_rows, step = kBatch * rows_per_pass;
-    for (int base = 0; base < n_items; base += step) {     // the same trip count for every thread
-      uint4 ahead[kBatch];
-      if (base + step < n_items) load(base + step, ahead);
-      float rinv[kBatch];
-      if (a.gain[0] != nullptr || a.gain[1] != nullptr) {
-        // Sums of squares of the rows, by shuffles over a row's chunks; where they leave fp32's range, once more on scaled values.
-        auto squares = [&](float scale, float (&ss)[kBatch]) {
+    // ---- the rows: Q, then K, with norm and rotation, then V as it is; the next step's loads are on their way during a step
+#pragma unroll 1
+    for (int it = 0; it < steps; ++it) {
+      uint4 w[kBatch];
+#pragma unroll
+      for (int b = 0; b < kBatch; ++b) w[b] = ahead[b];
+      if (it + 1 < steps) load(it + 1);
+      int which, n, h0;
+      step_of(it, which, n, h0);
+      const int out_head = which == 0 ? D : which == 1 ? (int)a.c.ks[2] : (int)a.c.vs[2];
+      float rinv[kBatch], gains[8];
+      const bool norm = which < 2 && a.gain[which & 1] != nullptr;
+      if (norm) {
+          *reinterpret_cast<float4*>(&gains[0]) = __ldg(reinterpret_cast<const float4*>(a.gain[which & 1] + chunk * 8));
+          *reinterpret_cast<float4*>(&gains[4]) = __ldg(reinterpret_cast<const float4*>(a.gain[which & 1] + chunk * 8) + 1);
+          // Sums of squares of the rows, by shuffles over a row's chunks; where they leave fp32's range, once more on scaled values.
+          auto squares = [&](float scale, float (&ss)[kBatch]) {
+#pragma unroll
+            for (int b = 0; b < kBatch; ++b) {
+              const uint32_t v[4] = {w[b].x, w[b].y, w[b].z, w[b].w};
+              ss[b] = 0.f;
+#pragma unroll
+              for (int u = 0; u < 4; ++u) {
+                float lo = __uint_as_float(v[u] << 16), hi = __uint_as_float(v[u] & 0xffff0000u);
+                if (scale != 1.0f) { lo *= scale; hi *= scale; }
+                ss[b] = fmaf(lo, lo, ss[b]);
+                ss[b] = fmaf(hi, hi, ss[b]);
+              }
+            }
+#pragma unroll
+            for (int off = kChunks / 2; off > 0; off >>= 1)
+#pragma unroll
+              for (int b = 0; b < kBatch; ++b) ss[b] += __shfl_xor_sync(lanes, ss[b], off);
+          };
+          float ss[kBatch];
+          squares(1.0f, ss);
+          bool odd = false;
 #pragma unroll
           for (int b = 0; b < kBatch; ++b) {
-            const uint32_t x[4] = {w[b].x, w[b].y, w[b].z, w[b].w};
-            ss[b] = 0.f;
+            rinv[b] = rsqrtf(fmaf(ss[b], 1.0f / D, a.eps));
+            odd = odd || !(ss[b] < 1e37f) || ss[b] < 1e-25f;
+          }
+          if (__any_sync(lanes, odd)) {
+            float big[kBatch], tiny[kBatch];
+            squares(0x1p-70f, big);
+            squares(0x1p60f, tiny);
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-              const float lo = __uint_as_float(x[u] << 16) * scale, hi = __uint_as_float(x[u] & 0xffff0000u) * scale;
-              ss[b] = fmaf(lo, lo, ss[b]);
-              ss[b] = fmaf(hi, hi, ss[b]);
+            for (int b = 0; b < kBatch; ++b) {             // (eps is nothing beside squares of 1e37 / D)
+              if (!(ss[b] < 1e37f)) rinv[b] = rsqrtf(big[b] * (1.0f / D) + a.eps * 0x1p-120f * 0x1p-20f) * 0x1p-70f;
+              else if (ss[b] < 1e-25f && a.eps < 1e-20f) rinv[b] = rsqrtf(tiny[b] * (1.0f / D) + a.eps * 0x1p120f) * 0x1p60f;
             }
           }
-          for (int off = chunks >> 1; off > 0; off >>= 1)
-#pragma unroll
-            for (int b = 0; b < kBatch; ++b) ss[b] += __shfl_xor_sync(lanes, ss[b], off);
-        };
-        float ss[kBatch];
-        squares(1.0f, ss);
-        bool large = false, small = false;
-#pragma unroll
-        for (int b = 0; b < kBatch; ++b) {
-          rinv[b] = rsqrtf(ss[b] * inv_d + a.eps);
-          large = large || !(ss[b] < 1e37f);
-          small = small || (ss[b] < 1e-25f && a.eps < 1e-20f);
         }
-        if (__any_sync(lanes, large)) {
-          float s2[kBatch];
-          squares(0x1p-70f, s2);
-#pragma unroll
-          for (int b = 0; b < kBatch; ++b)                                 // 2^-70 is a factor of the root; eps is beside 1e37 / D nothing
-            if (!(ss[b] < 1e37f)) rinv[b] = rsqrtf(s2[b] * inv_d + a.eps * 0x1p-120f * 0x1p-20f) * 0x1p-70f;
-        }
-        if (__any_sync(lanes, small)) {
-          float s2[kBatch];
-          squares(0x1p60f, s2);
-#pragma unroll
-          for (int b = 0; b < kBatch; ++b)
-            if (ss[b] < 1e-25f && a.eps < 1e-20f) rinv[b] = rsqrtf(s2[b] * inv_d + a.eps * 0x1p120f) * 0x1p60f;
-        }
-      }
 #pragma unroll
       for (int b = 0; b < kBatch; ++b) {
-        int token, which, head;
-        item(base + sub + b * rows_per_pass, token, which, head);
-        if (token < 0 || k_place[token] == -2) continue;
+        const int h = h0 + b / kTokens * rows_per_pass;
+        __nv_bfloat16* dst = place[which][b % kTokens];
+        if (h >= n || b % kTokens >= n_tok || dst == nullptr) continue;
         uint4 y = w[b];
         if (which < 2) {
-          const uint32_t x[4] = {w[b].x, w[b].y, w[b].z, w[b].w};
+          const uint32_t v[4] = {w[b].x, w[b].y, w[b].z, w[b].w};
           float f[8];
 #pragma unroll
           for (int u = 0; u < 4; ++u) {
-            f[2 * u] = __uint_as_float(x[u] << 16);
-            f[2 * u + 1] = __uint_as_float(x[u] & 0xffff0000u);
+            f[2 * u] = __uint_as_float(v[u] << 16);
+            f[2 * u + 1] = __uint_as_float(v[u] & 0xffff0000u);
           }
-          const float* gain = which == 0 ? a.gain[0] : a.gain[1];
-          if (gain != nullptr) {
-            const float4 g0 = __ldg(reinterpret_cast<const float4*>(gain + chunk * 8));
-            const float4 g1 = __ldg(reinterpret_cast<const float4*>(gain + chunk * 8) + 1);
-            const float r = rinv[b];
-            f[0] = f[0] * r * g0.x; f[1] = f[1] * r * g0.y; f[2] = f[2] * r * g0.z; f[3] = f[3] * r * g0.w;
-            f[4] = f[4] * r * g1.x; f[5] = f[5] * r * g1.y; f[6] = f[6] * r * g1.z; f[7] = f[7] * r * g1.w;
-          }
+          if (norm) {
 #pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            const float2 cs = angle[token][chunk * 4 + u];
-            if (cs.x == 1.f && cs.y == 0.f) continue;                      // (keeps infinities in dims that do not rotate)
-            const float re = f[2 * u], ro = f[2 * u + 1];
-            f[2 * u] = re * cs.x - ro * cs.y;
-            f[2 * u + 1] = re * cs.y + ro * cs.x;
+            for (int e = 0; e < 8; ++e) f[e] *= rinv[b] * gains[e];
+          }
+          if (rotates[b % kTokens] != 0) {
+            const float4* cs = reinterpret_cast<const float4*>(&angle[b % kTokens][chunk * 4]);
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {                  // two pairs: cos, sin, cos, sin
+              const float4 t = cs[u];
+              const float e0 = f[4 * u], o0 = f[4 * u + 1], e1 = f[4 * u + 2], o1 = f[4 * u + 3];
+              f[4 * u] = fmaf(e0, t.x, -(o0 * t.y));
+              f[4 * u + 1] = fmaf(e0, t.y, o0 * t.x);
+              f[4 * u + 2] = fmaf(e1, t.z, -(o1 * t.w));
+              f[4 * u + 3] = fmaf(e1, t.w, o1 * t.z);
+            }
           }
           y = make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
         }
-        if (which == 0) {
-          *reinterpret_cast<uint4*>(a.q_out + ((tok0 + token) * a.g.heads + head) * (long long)D + chunk * 8) = y;
-        } else if (k_place[token] >= 0 && again[token] == 0) {
-          __nv_bfloat16* dst = which == 1 ? a.c.k + k_place[token] + head * a.c.ks[2] : a.c.v + v_place[token] + head * a.c.vs[2];
-          *reinterpret_cast<uint4*>(dst + chunk * 8) = y;
-        }
+        *reinterpret_cast<uint4*>(dst + (long long)h * out_head + chunk * 8) = y;
       }
-#pragma unroll
-      for (int b = 0; b < kBatch; ++b) w[b] = ahead[b];
     }
     __syncthreads();                                       // places and angles are found anew for the next tokens
   }

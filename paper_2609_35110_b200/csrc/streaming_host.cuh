@@ -548,6 +548,8 @@ int sol_attn3d_cache_append(sol_attn3d_plan_t p, const void* q, const void* k, c
     a.x_head[i + 1] = st[i][1] == 0 ? cache->head_dim : st[i][1];
     if (!stride_ok(a.x_tok[i + 1]) || !stride_ok(a.x_head[i + 1])) return SOL_ATTN3D_ERR_UNSUPPORTED_SHAPE;
   }
+  for (long long st : {a.x_head[0], a.x_head[1], a.x_head[2], a.c.ks[2], a.c.vs[2]})
+    if (st > 0x7fffffffll) return SOL_ATTN3D_ERR_UNSUPPORTED_SHAPE;
   if (p->ws == nullptr) return SOL_ATTN3D_ERR_NO_WORKSPACE;
   a.x[0] = static_cast<const __nv_bfloat16*>(q);
   a.x[1] = static_cast<const __nv_bfloat16*>(k);
@@ -566,14 +568,15 @@ int sol_attn3d_cache_append(sol_attn3d_plan_t p, const void* q, const void* k, c
   a.streams = streams;
   a.pos0 = pos0;
   a.omega = reinterpret_cast<const double*>(p->ws + p->off_omega);
-  const int chunks = p->head_dim / 8, rows = (q != nullptr ? p->heads : 0) + 2 * cache->kv_heads;
+  const int chunks = p->head_dim / 8, rows = std::max(q != nullptr ? p->heads : 0, (int)cache->kv_heads);
   const int unit = 32 / chunks;                            // rows per warp
-  // four tokens at a time, unless that leaves SMs idle
-  const int group = p->total_tokens >= 148 * 3 * 4 ? 4 : 1;
-  const int per_pass = std::min(256 / chunks, (rows * group + unit - 1) / unit * unit);
-  const long long blocks = std::min<long long>((p->total_tokens + group - 1) / group, 148ll * 3 * 8);
+  const bool many = p->total_tokens >= 148 * 3 * 4;        // four tokens at a time, unless that leaves SMs idle
+  const int per_pass = std::min(256 / chunks, ((many ? rows : (rows + 3) / 4) + unit - 1) / unit * unit);
+  const long long blocks = std::min<long long>((p->total_tokens + (many ? 3 : 0)) / (many ? 4 : 1), 148ll * 3 * 8);
   p->launches = 0;
-  const cudaError_t e = launch_chained(sol::cache_append_kernel, (unsigned)blocks, (unsigned)(chunks * per_pass), 0, static_cast<cudaStream_t>(stream), a, group);
+  const cudaError_t e = launch_chained(p->head_dim == 128 ? (many ? sol::cache_append_kernel<128, 4> : sol::cache_append_kernel<128, 1>)
+                                                          : (many ? sol::cache_append_kernel<64, 4> : sol::cache_append_kernel<64, 1>),
+                                       (unsigned)blocks, (unsigned)(chunks * per_pass), 0, static_cast<cudaStream_t>(stream), a);
   if (e != cudaSuccess) return fail_cuda(p, e);
   ++p->launches;
   return SOL_ATTN3D_OK;
