@@ -28,7 +28,8 @@ struct UnitDev {
   long long part;               // index of this unit's partial rows, or -1: the rows themselves are written
   int t0, n_tok;                // first new token of the unit; new tokens of the sequence
   int kv_head;
-  int tile_begin, tile_end;     // key tiles
+  int tile_begin, n_keys;       // key tiles: the first one (where all are taken), how many
+  uint32_t live;                // with a mask and no more than 32 key tiles: those that hold a valid key; else 0
   int n_tiles;                  // query tiles: 1 or 2
   int lim[2];                   // keys below lim[t] count for every row of tile t
   int last;                     // no more units
@@ -76,6 +77,26 @@ struct ContextSmem {
   static constexpr int kOffOrder = kOffUnits + kUnitRing * (int)sizeof(UnitDev);   // sequence, first unit: kSortedSeqs each
   static constexpr int kBytes = kOffOrder + 2 * kSortedSeqs * 4;
   static constexpr int kDynBytes = kBytes + 1024;
+};
+
+// A unit's key tiles, one after another.
+template <bool kMask>
+struct TileWalk {
+  int jt, left;
+  uint32_t live;
+  __device__ __forceinline__ explicit TileWalk(const UnitDev& un) : jt(un.tile_begin), left(un.n_keys), live(kMask ? un.live : 0u) {
+    if (kMask && live != 0) jt = __ffs(live) - 1;
+  }
+  __device__ __forceinline__ bool more() const { return left > 0; }
+  __device__ __forceinline__ void next() {
+    --left;
+    if (kMask && live != 0) {
+      live &= live - 1;
+      jt = __ffs(live) - 1;
+    } else {
+      ++jt;
+    }
+  }
 };
 
 // Validity of 32 keys from `first` on: those below `limit`.
@@ -174,12 +195,30 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     const int tile_rows = p.tok_per_tile * group;
     uint32_t n_s = 0;                                      // key tiles of this query tile so far
     bool ok = true;
+    // Sequences without any key have no units (where they are sorted): their rows are zeros, which all CTAs write together.
+    if (p.a.n_seqs <= kSortedSeqs) {
+      bool empty = false;
+      if (lane < p.a.n_seqs) {
+        const Span sp = find_span<kPaged>(p.d, p.a.seqs[lane].seq_id);
+        empty = !sp.idle && sp.n == 0;
+      }
+      for (unsigned which = __ballot_sync(0xffffffffu, empty); which != 0; which &= which - 1) {
+        const SeqDev& sq = p.a.seqs[__ffs(which) - 1];
+        const int chunks = p.d.c.kv_heads * group * (D / 8);
+        for (long long tok = (long long)blockIdx.x * 8 + warp; tok < sq.n_tokens; tok += (long long)gridDim.x * 8) {
+          __nv_bfloat16* dst = p.a.out + (sq.tok_start + tok) * p.a.o_tok;
+          for (int x = lane; x < chunks; x += 32)
+            *reinterpret_cast<uint4*>(dst + (long long)(x / (D / 8)) * p.a.o_head + x % (D / 8) * 8) = make_uint4(0u, 0u, 0u, 0u);
+        }
+      }
+    }
     for (uint32_t u = 0;; ++u) {
       if (!wait_long(bar_u_full(u), round_of(u))) { ok = false; break; }
       const UnitDev& un = units[u & (kUnitRing - 1)];
       if (un.last) break;
       if (t >= un.n_tiles) { release_unit(u); continue; }
-      const int tile_begin = un.tile_begin, tile_end = un.tile_end, lim_all = un.lim[t];
+      const int lim_all = un.lim[t];
+      const bool any_keys = un.n_keys > 0;
       const uint8_t* mask = kMask ? un.span.mask : nullptr;
       const int cap = un.span.cap;
       const int tok = un.t0 + t * p.tok_per_tile + (int)(row * p.inv_group >> 16);       // this thread's new token
@@ -197,11 +236,14 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         }
         return w;
       };
-      if (kMask && tile_begin < tile_end) next_mask = fetch_mask(tile_begin);
+      TileWalk<kMask> walk(un);
+      if (kMask && any_keys) next_mask = fetch_mask(walk.jt);
 
-      for (int jt = tile_begin; jt < tile_end; ++jt, ++n_s) {
+      for (bool first = true; walk.more(); first = false, ++n_s) {
+        const int jt = walk.jt;
         const uint32_t mask_bits = next_mask;
-        if (kMask && jt + 1 < tile_end) next_mask = fetch_mask(jt + 1);
+        walk.next();
+        if (kMask && walk.more()) next_mask = fetch_mask(walk.jt);
         ok = mbar_wait_warp(bar_s_full(t), n_s & 1, limit);
         if (!ok) break;
         tc_fence_after();
@@ -265,7 +307,7 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             const float f = grow ? ex2_approx((m_ref - mx) * c) : 1.0f;
             if (grow) m_ref = mx;
             l *= f;
-            if (jt > tile_begin) {
+            if (!first) {
               ok = mbar_wait_warp(bar_o_done(t), (n_s - 1) & 1, limit);
               if (!ok) break;
               tc_fence_after();
@@ -297,7 +339,7 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       if (!ok) break;
 
       // ---- epilogue
-      if (tile_begin < tile_end) {
+      if (any_keys) {
         ok = mbar_wait_warp(bar_o_done(t), (n_s - 1) & 1, limit);
         if (!ok) break;
         tc_fence_after();
@@ -306,14 +348,9 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         float* dst = p.partial + (un.part * 2 * tile_rows + t * tile_rows + row) * (D + 4);
 #pragma unroll 1
         for (int cch = 0; cch < D / 32; ++cch) {
-          uint32_t o[32];
-          if (tile_begin < tile_end) {
-            tmem_ld32(tO + cch * 32, o);
-            tmem_wait_ld();
-          } else {
-#pragma unroll
-            for (int cc = 0; cc < 32; ++cc) o[cc] = 0u;
-          }
+          uint32_t o[32];                                  // (without a valid key: whatever is there, and not used)
+          tmem_ld32(tO + cch * 32, o);
+          tmem_wait_ld();
           if (mine) {
 #pragma unroll
             for (int cc = 0; cc < 32; cc += 4) *reinterpret_cast<uint4*>(dst + cch * 32 + cc) = make_uint4(o[cc], o[cc + 1], o[cc + 2], o[cc + 3]);
@@ -384,10 +421,10 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       if (!wait_long(bar_u_full(u), round_of(u))) { ok = false; break; }
       const UnitDev& un = units[u & (kUnitRing - 1)];
       if (un.last) break;
-      const int tile_begin = un.tile_begin, tile_end = un.tile_end, kv_head = un.kv_head, n = un.span.cap;
+      const int kv_head = un.kv_head, n = un.span.cap;
       const int* table = un.span.table;
       const long long begin = un.span.begin;
-      if (tile_begin < tile_end) {
+      if (un.n_keys > 0) {
         for (int t = 0; t < un.n_tiles && ok; ++t) {
           ok = mbar_wait_warp(bar_q_empty(t), (n_q[t] & 1) ^ 1u, limit);
           if (!ok) break;
@@ -409,10 +446,13 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
           return page >= 0 && page < p.d.c.n_pages ? page : (int)p.d.c.n_pages;
         };
         int next_page = 0;
-        if (kPaged && ok) next_page = page_of(tile_begin);
-        for (int jt = tile_begin; jt < tile_end && ok; ++jt) {
+        TileWalk<kMask> walk(un);
+        if (kPaged && ok) next_page = page_of(walk.jt);
+        while (walk.more() && ok) {
+          const int jt = walk.jt;
+          walk.next();
           const int page = next_page;
-          if (kPaged && jt + 1 < tile_end) next_page = page_of(jt + 1);
+          if (kPaged && walk.more()) next_page = page_of(walk.jt);
 #pragma unroll
           for (int kv = 0; kv < 2; ++kv) {
             const uint32_t stage = it % L::kStages;
@@ -494,7 +534,7 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       if (!wait_long(bar_u_full(u), round_of(u))) { ok = false; return (int)kNone; }
       const UnitDev& un = units[u & (kUnitRing - 1)];
       if (un.last) return (int)kNone;
-      n_proc = un.tile_end - un.tile_begin;
+      n_proc = un.n_keys;
       two = un.n_tiles == 2;
       release_unit(u++);
       return (int)(n_proc > 0 ? kTiles : kEmpty);
@@ -588,6 +628,8 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     int* order = reinterpret_cast<int*>(smem + L::kOffOrder);              // sequences, most keys first
     unsigned int* start = reinterpret_cast<unsigned int*>(order) + kSortedSeqs;   // first unit of each
     const bool sorted = p.a.n_seqs <= kSortedSeqs;
+    int looked_at = -1;                                    // the sequence whose live key tiles these are
+    uint32_t live = 0;
     unsigned int n_units = 0;
     if (sorted) {
       int keys = -1;
@@ -596,7 +638,7 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         const SeqDev& sq = p.a.seqs[lane];
         const Span sp = find_span<kPaged>(p.d, sq.seq_id);
         keys = sp.idle ? -1 : sp.n;
-        mine = sp.idle ? 0u : (unsigned int)((sq.n_tokens + per_unit - 1) / per_unit) * (unsigned int)p.d.c.kv_heads;
+        mine = sp.idle || sp.n == 0 ? 0u : (unsigned int)((sq.n_tokens + per_unit - 1) / per_unit) * (unsigned int)p.d.c.kv_heads;
       }
       int rank = 0;
       for (int j = 0; j < kSortedSeqs; ++j) {
@@ -673,7 +715,26 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         const int most = key_limit(un.span, un.n_tok, min(un.n_tok, un.t0 + per_unit) - 1, p.a.causal);
         const int tiles = (most + 127) >> 7, per = (tiles + n_split - 1) / n_split;
         un.tile_begin = min(tiles, split * per);
-        un.tile_end = min(tiles, un.tile_begin + per);
+        un.n_keys = min(tiles, un.tile_begin + per) - un.tile_begin;
+        if (kMask && tiles <= 32) {
+          // a tile without a valid key (the padding of a prompt, say) is left out; looked up once per sequence
+          if (si != looked_at) {
+            looked_at = si;
+            live = 0;
+            for (int jt = 0; jt * 128 < un.span.cap && jt < 32; ++jt) {
+              bool on = false;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const int key = jt * 128 + e * 32 + lane;
+                on = on || (key < un.span.cap && __ldg(un.span.mask + key) != 0);
+              }
+              live |= (__any_sync(0xffffffffu, on) ? 1u : 0u) << jt;
+            }
+          }
+          const uint32_t mine = live & (un.n_keys > 0 ? (0xffffffffu >> (32 - un.n_keys)) << un.tile_begin : 0u);
+          un.live = mine;
+          un.n_keys = __popc(mine);
+        }
         if (lane == 0) units[u & (kUnitRing - 1)] = un;
         break;
       }
@@ -692,10 +753,12 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       if (!wait_long(bar_u_full(u), round_of(u))) { ok = false; break; }
       const UnitDev& un = units[u & (kUnitRing - 1)];
       if (un.last) break;
-      const int tile_begin = un.tile_begin, tile_end = un.tile_end, cap = un.span.cap;
+      TileWalk<kMask> walk(un);
+      const int cap = un.span.cap;
       const uint8_t* mask = kMask ? un.span.mask : nullptr;
       release_unit(u);
-      for (int jt = tile_begin; jt < tile_end; ++jt) {
+      for (; walk.more(); walk.next()) {
+        const int jt = walk.jt;
         const uint32_t v_it = it + 1, stage = v_it % L::kStages;
         it += 2;
         uint32_t drop = 0;                                 // bit e: key 32 e + lane of the tile does not count

@@ -126,3 +126,45 @@ def test_many_sequences_most_without_states(d, masked):
             ref, mag = so.attend(q[at:at + m], kv_t[b:b + n, 0], kv_t[b:b + n, 1], so.key_limits(m, n, 0), None if mask is None else mask[b:b + n].bool())
             close(out[at:at + m], ref, mag)
             at += m
+
+
+@pytest.mark.parametrize("heads,d", [(2, 128), (4, 64)])
+def test_padded_contexts(heads, d):
+    """Key tiles without a valid key, at the end, in the middle, at the start; contexts of more than 32 tiles; split keys."""
+    from paper_2609_35110_b200 import binding as B
+    lens = [1000, 700, 4500, 4096, 300, 130]
+    kv_t, begins = contexts(lens, heads, d, seed=7)
+    mask = torch.zeros(kv_t.shape[0], dtype=torch.uint8)
+    for i, spans in enumerate([[(0, 100)], [(300, 301), (600, 640)], [(0, 50), (4400, 4500)], [(4095, 4096)], [], [(128, 130)]]):
+        for a, b in spans:
+            mask[begins[i] + a:begins[i] + b] = 1
+    kv_t[mask == 0] = float("nan")
+    dev = kv_t.cuda()
+    ctx = B.sol_attn3d_context(dev[:, 0], dev[:, 1], ints(begins), ints(lens), 4500, key_mask=mask.cuda())
+    for sizes in ([300, 20, 257, 513, 40, 1], [17] * 6, [2000, 300, 1000, 128, 700, 900]):
+        q = torch.randn(sum(sizes), heads, d, generator=torch.Generator().manual_seed(1)).bfloat16()
+        out = run([(n, 0, 1, 1) for n in sizes], q.cuda(), heads, d, ctx)
+        at = 0
+        for m, b, n in zip(sizes, begins, lens):
+            ref, mag = so.attend(q[at:at + m], kv_t[b:b + n, 0], kv_t[b:b + n, 1], so.key_limits(m, n, 0), mask[b:b + n].bool())
+            close(out[at:at + m], ref, mag)
+            at += m
+
+
+def test_strided_outputs():
+    """Rows of another tensor's output are left as they were, also where a sequence has no key."""
+    from paper_2609_35110_b200 import binding as B
+    kv_t, begins = contexts([300, 0], 2, 64, seed=3)
+    dev = kv_t.cuda()
+    ctx = B.sol_attn3d_context(dev[:, 0], dev[:, 1], ints(begins), ints([300, 0]), 300)
+    attn = B.Attn3d([(200, 0, 1, 1), (150, 0, 1, 1)], 2, 64, rope(64), out_strides=(5 * 64, 128))
+    q = torch.randn(350, 2, 64, generator=torch.Generator().manual_seed(1)).bfloat16()
+    buf = torch.full((350, 5, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    out = buf.view(350, 5 * 64).as_strided((350, 2, 64), (5 * 64, 128, 1))
+    ws = torch.empty(B.sol_attn3d_cross_workspace_bytes(attn.plan, ctx), dtype=torch.uint8, device="cuda")
+    B.sol_attn3d_forward_cross(attn.plan, q.cuda(), ctx, buf, workspace=ws)
+    torch.cuda.synchronize()
+    assert attn.status() == 0
+    ref, mag = so.attend(q[:200], kv_t[begins[0]:begins[0] + 300, 0], kv_t[begins[0]:begins[0] + 300, 1], so.key_limits(200, 300, 0))
+    close(out[:200].cpu(), ref, mag)
+    assert bool((out[200:] == 0).all()) and bool((buf[:, 1::2] == 7.0).all()) and bool((buf[:, 4] == 7.0).all())
