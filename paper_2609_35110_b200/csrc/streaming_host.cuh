@@ -192,12 +192,15 @@ ContextRoute choose_route(sol_attn3d_plan_t p, int kv_heads, long long capacity,
 
 size_t join_list_bytes(const ContextRoute& r) { return align_up((size_t)r.n_tail * sizeof(sol::JoinUnit)); }
 
+size_t many_bytes(const ContextRoute& r, int head_dim) {
+  if (r.n_split == 1) return 0;
+  return join_list_bytes(r) + align_up((size_t)r.n_tail * r.n_split * 2 * r.tok_per_tile * r.group * (head_dim + 4) * sizeof(float));
+}
+
 size_t context_bytes(sol_attn3d_plan_t p, int kv_heads, long long capacity, long long total_rows) {
   if (p == nullptr || p->heads % kv_heads != 0) return 0;
   const ContextRoute r = choose_route(p, kv_heads, capacity, total_rows);
-  if (r.few) return few_bytes(r.units, kv_heads, p->head_dim, capacity);
-  if (r.n_split == 1) return 0;
-  return join_list_bytes(r) + align_up((size_t)r.n_tail * r.n_split * 2 * r.tok_per_tile * r.group * (p->head_dim + 4) * sizeof(float));
+  return r.few ? few_bytes(r.units, kv_heads, p->head_dim, capacity) : many_bytes(r, p->head_dim);
 }
 
 // Any tensor as a tiled map of bf16 boxes 64 elements wide, 128-byte swizzle; strides of the outer dimensions in elements.
@@ -239,7 +242,7 @@ cudaError_t launch_context(const CUtensorMap& q, const CUtensorMap& k, const CUt
 }
 
 int attend_many(sol_attn3d_plan_t p, const sol::QueriesDev& a, const sol::KeysDev& d, bool paged, const ContextRoute& r, void* workspace,
-                size_t workspace_bytes, size_t need, int lookahead, cudaStream_t st) {
+                size_t workspace_bytes, int lookahead, cudaStream_t st) {
   sol::ContextParams c{};
   c.a = a;
   c.d = d;
@@ -253,7 +256,7 @@ int attend_many(sol_attn3d_plan_t p, const sol::QueriesDev& a, const sol::KeysDe
   c.inv_group = (65536u + r.group - 1) / r.group;
   c.lookahead = lookahead;
   if (r.n_split > 1) {
-    if (workspace == nullptr || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) % kAlign) != 0) return SOL_ATTN3D_ERR_NO_WORKSPACE;
+    if (workspace == nullptr || workspace_bytes < many_bytes(r, p->head_dim) || (reinterpret_cast<uintptr_t>(workspace) % kAlign) != 0) return SOL_ATTN3D_ERR_NO_WORKSPACE;
     c.join = static_cast<sol::JoinUnit*>(workspace);
     c.partial = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + join_list_bytes(r));
   }
@@ -322,8 +325,7 @@ int forward_context(sol_attn3d_plan_t p, const void* q, void* out, const sol::Ke
       if ((e = cudaEventRecord(p->ev[i], st)) != cudaSuccess) return fail_cuda(p, e);
   }
   const int rc = r.few ? attend_few(a, d, paged, p->head_dim, r.units, capacity, workspace, workspace_bytes, st, &p->launches, &p->last_cuda)
-                       : attend_many(p, a, d, paged, r, workspace, workspace_bytes, context_bytes(p, d.c.kv_heads, capacity, total_rows),
-                                     capacity <= 2048 ? 4 : 2, st);   // short units: looking one up must not hold the next ones back
+                       : attend_many(p, a, d, paged, r, workspace, workspace_bytes, capacity <= 2048 ? 4 : 2, st);   // short units: looking one up must not hold the next ones back
   if (rc != SOL_ATTN3D_OK) return rc;
   if (p->prof) {
     if ((e = cudaEventRecord(p->ev[3], st)) != cudaSuccess) return fail_cuda(p, e);

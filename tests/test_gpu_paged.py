@@ -315,3 +315,9 @@ def test_many_streams_with_split_keys():
         c = Cache(lens, 32, kv, d, seed=heads, layers=1, layer=0)
         check_chunk(seqs, [2, 1, 0, 9, 4, 5, 3], c, heads, 0)
         check_chunk(seqs, [2, 1, 0, 9, 4, 5, 3], c, heads, 130)
+
+
+@pytest.mark.parametrize("heads,kv", [(130, 1), (300, 2)])
+def test_more_heads_per_key_head_than_a_tile_has_rows(heads, kv):
+    c = Cache([500, 90], 32, kv, 64, seed=1)
+    check_chunk([(20, 0, 1, 1), (1, 0, 1, 1)], None, c, heads, 1)
