@@ -447,111 +447,122 @@ __global__ void __launch_bounds__(kFewThreads, kFewResident) few_rows_kernel(con
   }
 }
 
-// Joins the parts of split keys, in the order of the splits.  Rows of partial results: D values, maximum, sum, "has a valid key".
-// One thread per 8 dims of a row; CTAs (unit and K/V head, 256 such pieces).  Whose rows a unit holds follows from its number (few rows), or was
-// written down by who made them (kListed).
+// Joins the parts of split keys.  Rows of partial results: D values, maximum, sum, "has a valid key".  A warp per row: its lanes look at
+// the statistics of 32 parts at once; then a lane sums 8 dims over every second (D = 128) or fourth part, with weights that come by
+// shuffle, so that the loads of the values do not wait for one another.  All sums are in a fixed order.
+template <int D>
+__device__ __forceinline__ void join_row(const float* mine, long long step, int n_parts, float scale_log2, __nv_bfloat16* dst) {
+  constexpr int kChunks = D / 8, kTeams = 32 / kChunks;
+  const int lane = threadIdx.x & 31, d0 = lane % kChunks * 8, team = lane / kChunks;
+  float top = -CUDART_INF_F;
+  bool any = false;
+  for (int s = lane; s < n_parts; s += 32) {
+    const float4 t = __ldg(reinterpret_cast<const float4*>(mine + s * step + D));
+    top = fmaxf(top, t.x);
+    any = any || t.z != 0.f;
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  any = __any_sync(0xffffffffu, any);
+  float sum = 0.f, acc[8] = {};
+  for (int s0 = 0; s0 < n_parts; s0 += 32) {
+    float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (s0 + lane < n_parts) t = __ldg(reinterpret_cast<const float4*>(mine + (s0 + lane) * step + D));
+    const float weight = t.z == 0.f ? 0.f : t.x == top ? 1.f : ex2_approx((t.x - top) * scale_log2);
+    if (t.z != 0.f) sum = fmaf(t.y, weight, sum);
+    const unsigned there = __ballot_sync(0xffffffffu, t.z != 0.f);         // (what a part without a valid key holds is not looked at)
+#pragma unroll 4
+    for (int j = 0; j < 32; j += kTeams) {
+      if (s0 + j >= n_parts) break;
+      const float f = __shfl_sync(0xffffffffu, weight, j + team);
+      if ((there >> (j + team)) & 1u) {
+        const float* v = mine + (s0 + j + team) * step + d0;
+        const float4 a = __ldg(reinterpret_cast<const float4*>(v)), b = __ldg(reinterpret_cast<const float4*>(v + 4));
+        acc[0] = fmaf(a.x, f, acc[0]); acc[1] = fmaf(a.y, f, acc[1]); acc[2] = fmaf(a.z, f, acc[2]); acc[3] = fmaf(a.w, f, acc[3]);
+        acc[4] = fmaf(b.x, f, acc[4]); acc[5] = fmaf(b.y, f, acc[5]); acc[6] = fmaf(b.z, f, acc[6]); acc[7] = fmaf(b.w, f, acc[7]);
+      }
+    }
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (o >= kChunks)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] += __shfl_xor_sync(0xffffffffu, acc[e], o);
+  }
+  const float inv = 1.f / sum;
+  uint4 y = make_uint4(0, 0, 0, 0);                        // no valid key: zeros
+  if (any) y = make_uint4(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv),
+                          pack_bf16x2(acc[4] * inv, acc[5] * inv), pack_bf16x2(acc[6] * inv, acc[7] * inv));
+  if (team == 0) *reinterpret_cast<uint4*>(dst + d0) = y;
+}
+
+constexpr int kJoinWarps = 8;
+
+// After few_rows_kernel: a CTA per unit and K/V head.
+template <int D, bool kPaged>
+__global__ void __launch_bounds__(32 * kJoinWarps) join_few_kernel(const __grid_constant__ FewArgs p) {
+  chained_wait();
+  chained_next();
+  const int kv_head = (int)(blockIdx.x / p.units);
+  const long long unit = blockIdx.x % p.units;
+  int entry, n_tok, row0;
+  long long tok0;
+  if (p.a.seqs != nullptr) {
+    long long first;
+    const SeqDev& sq = p.a.seqs[find_sequence(p.a, unit, kFewRows, &first)];
+    entry = sq.seq_id;
+    n_tok = sq.n_tokens;
+    tok0 = sq.tok_start;
+    row0 = (int)(unit - first) * kFewRows;
+  } else {
+    const int per = (p.a.group + kFewRows - 1) / kFewRows;
+    entry = (int)(unit / per);
+    n_tok = 1;
+    tok0 = entry;
+    row0 = (int)(unit % per) * kFewRows;
+  }
+  if (kPaged) {
+    const long long stream = p.d.streams != nullptr ? p.d.streams[entry] : entry;
+    if (stream < 0 || stream >= p.d.c.n_streams) return;
+  }
+  const int n_rows = min(kFewRows, n_tok * p.a.group - row0);
+  const float* part = p.partial + (long long)blockIdx.x * p.n_split * kFewRows * (D + 4);
+  for (int row = threadIdx.x >> 5; row < n_rows; row += kJoinWarps) {
+    const int r = row0 + row;
+    join_row<D>(part + row * (D + 4), (long long)kFewRows * (D + 4), p.n_split, p.a.scale_log2,
+                p.a.out + (tok0 + r / p.a.group) * p.a.o_tok + ((long long)kv_head * p.a.group + r % p.a.group) * p.a.o_head);
+  }
+}
+
+// After context_attn_kernel: the units whose keys it split are listed on the device.  A warp per row of one.
 struct JoinUnit {
   long long tok0;
   int t0, n_tok;                // first new token of the unit; new tokens of the sequence (0: nothing to join)
   int kv_head;
+  int first_part, n_parts;      // its partial rows
   int unused;
 };
 struct JoinArgs {
   QueriesDev a;
-  KeysDev d;
-  int n_split, rows_per_unit;
-  long long units;
+  int rows_per_unit;
   const float* partial;
   const JoinUnit* list;
+  const int* count;
 };
 
-template <int D, bool kPaged, bool kListed>
-__global__ void __launch_bounds__(256) join_rows_kernel(const __grid_constant__ JoinArgs p) {
-  int kv_head, n_tok;
-  long long tok0, row0;
+template <int D>
+__global__ void __launch_bounds__(32 * kJoinWarps) join_units_kernel(const __grid_constant__ JoinArgs p) {
   chained_wait();
   chained_next();
-  if (kListed) {
-    const JoinUnit u = p.list[blockIdx.x];
-    kv_head = u.kv_head;
-    n_tok = u.n_tok;
-    tok0 = u.tok0;
-    row0 = (long long)u.t0 * p.a.group;
-  } else {
-    int entry;
-    kv_head = (int)(blockIdx.x / p.units);
-    const long long unit = blockIdx.x % p.units;
-    if (p.a.seqs != nullptr) {
-      long long first;
-      const SeqDev& sq = p.a.seqs[find_sequence(p.a, unit, p.rows_per_unit, &first)];
-      entry = sq.seq_id;
-      n_tok = sq.n_tokens;
-      tok0 = sq.tok_start;
-      row0 = (unit - first) * p.rows_per_unit;
-    } else {
-      const int per = (p.a.group + p.rows_per_unit - 1) / p.rows_per_unit;
-      entry = (int)(unit / per);
-      n_tok = 1;
-      tok0 = entry;
-      row0 = (unit % per) * p.rows_per_unit;
-    }
-    if (kPaged) {
-      const long long stream = p.d.streams != nullptr ? p.d.streams[entry] : entry;
-      if (stream < 0 || stream >= p.d.c.n_streams) return;
-    }
-  }
-  const long long n_rows = min((long long)p.rows_per_unit, (long long)n_tok * p.a.group - row0);
-  if (n_rows <= 0) return;
-  constexpr int kChunks = D / 8;
-  const float* part = p.partial + (long long)blockIdx.x * p.n_split * p.rows_per_unit * (D + 4);
-  const int x = blockIdx.y * 256 + threadIdx.x;
-  const int row = x / kChunks, d0 = (x % kChunks) * 8;
-  const unsigned team = __ballot_sync(0xffffffffu, row < n_rows);          // whole teams of kChunks threads, one per row
-  if (row < n_rows) {
-    const float* mine = part + (long long)row * (D + 4);
+  const long long all = (long long)*p.count * p.rows_per_unit;
+  for (long long x = (long long)blockIdx.x * kJoinWarps + (threadIdx.x >> 5); x < all; x += (long long)gridDim.x * kJoinWarps) {
+    const JoinUnit u = p.list[x / p.rows_per_unit];
+    const int row = (int)(x % p.rows_per_unit), tok = u.t0 + row / p.a.group;
+    if (tok >= u.n_tok) continue;
     const long long step = (long long)p.rows_per_unit * (D + 4);
-    // The team's threads look at a part's statistics each, kChunks parts at a time; the weights then come by shuffle, so that the loads
-    // of the values do not wait for them one by one.
-    const int lane = threadIdx.x % kChunks;
-    float top = -CUDART_INF_F;
-    bool any = false;
-    for (int s0 = 0; s0 < p.n_split; s0 += kChunks)
-      if (s0 + lane < p.n_split) {
-        const float4 t = __ldg(reinterpret_cast<const float4*>(mine + (s0 + lane) * step + D));
-        top = fmaxf(top, t.x);
-        any = any || t.z != 0.f;
-      }
-#pragma unroll
-    for (int o = kChunks / 2; o > 0; o >>= 1) {
-      top = fmaxf(top, __shfl_xor_sync(team, top, o));
-      any = __shfl_xor_sync(team, (int)any, o) != 0 || any;
-    }
-    float sum = 0.f, acc[8] = {};
-    for (int s0 = 0; s0 < p.n_split; s0 += kChunks) {
-      float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (s0 + lane < p.n_split) t = __ldg(reinterpret_cast<const float4*>(mine + (s0 + lane) * step + D));
-      const float weight = t.z == 0.f ? 0.f : t.x == top ? 1.f : ex2_approx((t.x - top) * p.a.scale_log2);
-      const float share = t.z == 0.f ? 0.f : t.y * weight;
-#pragma unroll 4
-      for (int s = 0; s < kChunks; ++s) {
-        if (s0 + s >= p.n_split) break;
-        const float4 u = __ldg(reinterpret_cast<const float4*>(mine + (s0 + s) * step + d0)), v = __ldg(reinterpret_cast<const float4*>(mine + (s0 + s) * step + d0 + 4));
-        const float f = __shfl_sync(team, weight, s, kChunks);
-        const bool there = __shfl_sync(team, t.z, s, kChunks) != 0.f;
-        sum += __shfl_sync(team, share, s, kChunks);
-        if (there) {
-          acc[0] = fmaf(u.x, f, acc[0]); acc[1] = fmaf(u.y, f, acc[1]); acc[2] = fmaf(u.z, f, acc[2]); acc[3] = fmaf(u.w, f, acc[3]);
-          acc[4] = fmaf(v.x, f, acc[4]); acc[5] = fmaf(v.y, f, acc[5]); acc[6] = fmaf(v.z, f, acc[6]); acc[7] = fmaf(v.w, f, acc[7]);
-        }
-      }
-    }
-    const float inv = 1.f / sum;
-    const long long r = row0 + row;
-    __nv_bfloat16* dst = p.a.out + (tok0 + r / p.a.group) * p.a.o_tok + ((long long)kv_head * p.a.group + r % p.a.group) * p.a.o_head + d0;
-    uint4 y = make_uint4(0, 0, 0, 0);
-    if (any) y = make_uint4(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv),
-                            pack_bf16x2(acc[4] * inv, acc[5] * inv), pack_bf16x2(acc[6] * inv, acc[7] * inv));
-    *reinterpret_cast<uint4*>(dst) = y;
+    join_row<D>(p.partial + u.first_part * step + row * (D + 4), step, u.n_parts, p.a.scale_log2,
+                p.a.out + (u.tok0 + tok) * p.a.o_tok + ((long long)u.kv_head * p.a.group + row % p.a.group) * p.a.o_head);
   }
 }
 

@@ -33,31 +33,43 @@ struct UnitDev {
   int n_tiles;                  // query tiles: 1 or 2
   int lim[2];                   // keys below lim[t] count for every row of tile t
   int last;                     // no more units
+  int withhold;                 // test hook: "the scores of the last tile are there" is not said
 };
 
 struct ContextParams {
   QueriesDev a;
   KeysDev d;
-  long long units;              // row units per K/V head (more than kSortedSeqs sequences: with room for empty ones, find_sequence)
-  long long n_whole, n_tail;    // units that take all of their keys, then units whose keys are split
-  long long total;              // n_whole + n_tail * n_split
+  // Up to kSortedSeqs sequences are planned on the device, where their keys are known, into at most max_parts parts of split units.
+  int max_parts;
+  // More sequences: row units per K/V head, numbered with room for empty ones (find_sequence); all heads' units, of which the first
+  // n_whole take all of their keys and the others' keys are split.
+  long long units, n_whole, n_tail;
   int n_split;
   int lookahead;                // units that a CTA draws before it has finished with the one in work: 2 or 4
   int tok_per_tile;             // 128 / group
   unsigned int inv_group;       // ceil(2^16 / group): x / group = x * inv_group >> 16 for x < 128
   int box_rows;                 // tokens of a K/V box: a power of two that divides the page size, at most 128
-  float* partial;               // [n_tail][n_split][2 * tok_per_tile * group][D + 4]
-  JoinUnit* join;               // [n_tail]: whose rows these are
+  float* partial;               // [part][2 * tok_per_tile * group][D + 4]
+  JoinUnit* join;               // whose rows the parts hold, a unit each
+  int* join_count;
   unsigned int* counter;        // next unit; 0 between launches
   unsigned int* status;
   unsigned int* rescales;
   unsigned long long wait_limit_ns;
-  unsigned int fault_inject;    // 1: the first unit withholds "scores of tile 1 (or the only one) are there"
+  unsigned int fault_inject;    // 1: item 0 withholds "the scores of the last tile are there"
   unsigned int v_lbo, v_sbo;
 };
 
-// Up to so many sequences are taken in the order of their keys, most first, so that long units do not come last.
+// Up to so many sequences are planned on the device: taken in the order of their keys, most first, so that long units do not come
+// last, and their keys split where that evens the work out.
 constexpr int kSortedSeqs = 32;
+constexpr int kPlanSms = 148;
+// What a unit needs to know of its sequence, looked up once.
+struct SeqNote {
+  int at;                       // stream, or first row of the context
+  int n, cap;                   // as in Span; n < 0: idle
+  int tok0, n_tok;              // first token in the packed tensors; new tokens
+};
 constexpr int kUnitRing = 4;
 
 template <int D>
@@ -65,7 +77,7 @@ struct ContextSmem {
   static constexpr int kTile = 128 * D * 2;
   static constexpr int kHalves = D / 64;
   static constexpr int kHalfBytes = 128 * 128;
-  static constexpr int kStages = D == 128 ? 4 : 10;       // K and V tiles alternate
+  static constexpr int kStages = D == 128 ? 4 : 9;       // K and V tiles alternate
   static constexpr int kVRing = 8;                        // "V is clean" barriers: more than V tiles fit the ring
   static constexpr int kOffQ = 0;
   static constexpr int kOffKV = 2 * kTile;
@@ -74,9 +86,11 @@ struct ContextSmem {
   static constexpr int kNumBars = 2 * kStages + 4 + 6 + 2 * kUnitRing + kVRing + 1;
   static constexpr int kOffTmemPtr = kOffBars + kNumBars * 8;
   static constexpr int kOffUnits = (kOffTmemPtr + 16 + 15) / 16 * 16;
-  static constexpr int kOffOrder = kOffUnits + kUnitRing * (int)sizeof(UnitDev);   // sequence, first unit: kSortedSeqs each
-  static constexpr int kBytes = kOffOrder + 2 * kSortedSeqs * 4;
+  static constexpr int kOffOrder = kOffUnits + kUnitRing * (int)sizeof(UnitDev);   // sequence, first item, units, parts, first part: kSortedSeqs each
+  static constexpr int kOffSeqs = kOffOrder + 5 * kSortedSeqs * 4;
+  static constexpr int kBytes = kOffSeqs + kSortedSeqs * (int)sizeof(SeqNote);
   static constexpr int kDynBytes = kBytes + 1024;
+  static_assert(kDynBytes <= 227 * 1024, "what a CTA may have");
 };
 
 // A unit's key tiles, one after another.
@@ -529,13 +543,14 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     enum { kNone, kEmpty, kTiles };
     uint32_t u = 0;
     int n_proc = 0;
-    bool two = false, withhold = p.fault_inject == 1u && blockIdx.x == 0;
+    bool two = false, withhold = false;
     auto draw = [&]() {
       if (!wait_long(bar_u_full(u), round_of(u))) { ok = false; return (int)kNone; }
       const UnitDev& un = units[u & (kUnitRing - 1)];
       if (un.last) return (int)kNone;
       n_proc = un.n_keys;
       two = un.n_tiles == 2;
+      withhold = un.withhold != 0;
       release_unit(u++);
       return (int)(n_proc > 0 ? kTiles : kEmpty);
     };
@@ -546,7 +561,7 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       int what = draw();
       while (what == kEmpty) what = draw();
       if (what != kTiles) break;
-      // (withhold, a test hook: the first unit withholds a signal, so that the waits downstream run into their limit)
+      // (withhold, a test hook: a signal is left out, so that the waits downstream run into their limit)
       {
         const uint32_t k_st = stage_of(it);
         if (!wait(bar_q_full(0), n_q[0] & 1) || !full(it)) break;
@@ -562,7 +577,6 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
           if (n_proc == 1) tc_commit_elect(bar_q_empty(1));
         }
         tc_commit_elect(bar_kv_empty(k_st));
-        withhold = false;
       }
       bool have = true;
       int i = 0;
@@ -625,70 +639,151 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     // =========================================================== takes units
     bool ok = true;
     const int per_unit = 2 * p.tok_per_tile;
-    int* order = reinterpret_cast<int*>(smem + L::kOffOrder);              // sequences, most keys first
-    unsigned int* start = reinterpret_cast<unsigned int*>(order) + kSortedSeqs;   // first unit of each
+    int* order = reinterpret_cast<int*>(smem + L::kOffOrder);              // by rank, most keys first: sequence,
+    unsigned int* start = reinterpret_cast<unsigned int*>(order) + kSortedSeqs;   // its first item,
+    int* n_unit = order + 2 * kSortedSeqs;                                 // its units, all heads,
+    int* n_part = order + 3 * kSortedSeqs;                                 // parts of each,
+    int* part0 = order + 4 * kSortedSeqs;                                  // its first partial rows (where there are several)
     const bool sorted = p.a.n_seqs <= kSortedSeqs;
+    SeqNote* notes = reinterpret_cast<SeqNote*>(smem + L::kOffSeqs);       // by place in the schedule
     int looked_at = -1;                                    // the sequence whose live key tiles these are
     uint32_t live = 0;
-    unsigned int n_units = 0;
+    // whole units, then `tail` units of `tail_split` parts (one kind of units, or more sequences than are sorted)
+    long long n_whole = p.n_whole, tail = p.n_tail, n_items = p.n_whole + p.n_tail * p.n_split;
+    int tail_split = p.n_split, joins = p.n_split > 1 ? (int)p.n_tail : 0;
     if (sorted) {
-      int keys = -1;
-      unsigned int mine = 0;
+      int keys = -1, units = 0;
       if (lane < p.a.n_seqs) {
         const SeqDev& sq = p.a.seqs[lane];
         const Span sp = find_span<kPaged>(p.d, sq.seq_id);
         keys = sp.idle ? -1 : sp.n;
-        mine = sp.idle || sp.n == 0 ? 0u : (unsigned int)((sq.n_tokens + per_unit - 1) / per_unit) * (unsigned int)p.d.c.kv_heads;
+        notes[lane] = SeqNote{kPaged ? (p.d.streams != nullptr ? p.d.streams[sq.seq_id] : sq.seq_id) : (int)sp.begin, keys, sp.cap, (int)sq.tok_start, sq.n_tokens};
+        units = sp.idle || sp.n == 0 ? 0 : (sq.n_tokens + per_unit - 1) / per_unit * p.d.c.kv_heads;
       }
       int rank = 0;
-      for (int j = 0; j < kSortedSeqs; ++j) {
+      for (int j = 0; j < p.a.n_seqs; ++j) {
         const int other = __shfl_sync(0xffffffffu, keys, j);
         rank += other > keys || (other == keys && j < lane) ? 1 : 0;
       }
+      if (lane >= p.a.n_seqs) rank = lane;
+      const int tiles = keys > 0 ? (keys + 127) >> 7 : 0;
+      // How to split the keys: lane i weighs parts of 1 / (i + 1) of the longest sequence's key tiles.  The unit of cost is a key tile
+      // (some 2 us); a part costs 2 for its start and end, its partial rows 0.03 on their way through memory, a join 1.5.  Units of
+      // one kind are dealt in whole waves; a mixture, largest first, ends 0.15 of a part late and
+      // has whole waves of its large parts.  (Four streams of 7 to 100 tiles: 342 us
+      // unsplit, 377 us in thirds of the longest; 40 units of 147 tiles beside small ones: 372 and 150 us.)
+      const int most = __shfl_sync(0xffffffffu, tiles, __ffs(__ballot_sync(0xffffffffu, rank == 0)) - 1);
+      const int chunk = max(1, (most + lane) / (lane + 1));
+      int flat = 0, items = 0, split_items = 0, large = 0;  // large: parts of more than half of the largest
+      float work = 0.f, large_work = 0.f;
+      bool one_kind = true;
+      for (int j = 0; j < p.a.n_seqs; ++j) {
+        const int t = __shfl_sync(0xffffffffu, tiles, j), n = __shfl_sync(0xffffffffu, units, j);
+        const int parts = (t + chunk - 1) / chunk;
+        flat += n;
+        items += n * max(parts, 1);
+        if (parts > 1) split_items += n * parts;
+        const float w = (float)n * (float)(t + 2 * max(parts, 1));
+        work += w;
+        if (2 * t > chunk * max(parts, 1)) {
+          large += n * max(parts, 1);
+          large_work += w;
+        }
+        one_kind = one_kind && (n == 0 || t == most);
+      }
+      const float joining = split_items > 0 ? 1.5f + 0.03f * split_items : 0.f;
+      float cost = one_kind ? (float)((items + kPlanSms - 1) / kPlanSms) * (chunk + 2) : fmaxf(fmaxf(work * (1.f / kPlanSms), (float)(chunk + 2)), large_work / max(large, 1) * (float)((large + kPlanSms - 1) / kPlanSms)) + 0.15f * (chunk + 2);
+      cost += joining;
+      if (split_items > p.max_parts || (lane > 0 && chunk < 4)) cost = CUDART_INF_F;
+      // ... or, for units of one kind, whole ones in whole waves and the rest in i + 1 parts each
+      const int waves = flat / kPlanSms, rest = flat - waves * kPlanSms, rest_chunk = (most + lane) / (lane + 1);
+      float tail_cost = (float)waves * (most + 2) + (float)((rest * (lane + 1) + kPlanSms - 1) / kPlanSms) * (rest_chunk + 2) + 1.5f + 0.03f * rest * (lane + 1);
+      if (!one_kind || waves == 0 || rest == 0 || lane == 0 || rest_chunk < 4 || rest * (lane + 1) > p.max_parts) tail_cost = CUDART_INF_F;
+      int pick = tail_cost < cost ? lane + 32 : lane;
+      float best = fminf(cost, tail_cost);
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) {
+        const float c = __shfl_xor_sync(0xffffffffu, best, o);
+        const int w = __shfl_xor_sync(0xffffffffu, pick, o);
+        if (c < best || (c == best && w < pick)) { best = c; pick = w; }
+      }
+      const bool by_tail = pick >= 32;
+      const int by_chunk = by_tail ? 0x7fffffff : __shfl_sync(0xffffffffu, chunk, pick & 31);
+      const int parts = by_tail || tiles == 0 ? 1 : (tiles - 1) / by_chunk + 1;
+      // the items in rank order
       order[rank] = lane;
-      start[rank] = mine;
+      n_unit[rank] = units;
+      n_part[rank] = parts;
       __syncwarp();
-      const unsigned int own = start[lane];
-      unsigned int upto = own;
+      const int my_items = n_unit[lane] * n_part[lane], my_parts = n_part[lane] > 1 ? my_items : 0;
+      int upto = my_items, parts_upto = my_parts, joins_upto = n_part[lane] > 1 ? n_unit[lane] : 0;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
-        const unsigned int y = __shfl_up_sync(0xffffffffu, upto, o);
-        if (lane >= o) upto += y;
+        const int x = __shfl_up_sync(0xffffffffu, upto, o), y = __shfl_up_sync(0xffffffffu, parts_upto, o), z = __shfl_up_sync(0xffffffffu, joins_upto, o);
+        if (lane >= o) { upto += x; parts_upto += y; joins_upto += z; }
       }
-      n_units = __shfl_sync(0xffffffffu, upto, 31);
+      start[lane] = (unsigned int)(upto - my_items);
+      part0[lane] = parts_upto - my_parts;
       __syncwarp();
-      start[lane] = upto - own;
-      __syncwarp();
+      n_whole = __shfl_sync(0xffffffffu, upto, 31);
+      joins = __shfl_sync(0xffffffffu, joins_upto, 31);
+      tail = 0;
+      tail_split = 1;
+      n_items = n_whole;
+      if (by_tail) {
+        n_whole = (long long)waves * kPlanSms;
+        tail = rest;
+        tail_split = (pick & 31) + 1;
+        n_items = n_whole + tail * tail_split;
+        joins = rest;
+      }
     }
+    if (p.join_count != nullptr && blockIdx.x == 0 && lane == 0) *p.join_count = joins;
+    bool drawn = false;
     for (uint32_t u = 0;; ++u) {
       if (u >= (uint32_t)p.lookahead && !wait_long(bar_u_empty(u - p.lookahead), round_of(u - p.lookahead))) { ok = false; break; }
       int last = 0;
       for (;;) {
-        unsigned int at = 0;
-        if (lane == 0) at = atomicAdd(p.counter, 1u);
-        at = __shfl_sync(0xffffffffu, at, 0);
-        if (at >= p.total) {
-          // every CTA draws one number past the units; the one that draws the last of them leaves the counter as it was found
-          if (lane == 0 && at == p.total + gridDim.x - 1) *p.counter = 0u;
+        // the first item of a CTA is its own number; the others come from the counter
+        unsigned int at = blockIdx.x;
+        if (drawn) {
+          if (lane == 0) at = atomicAdd(p.counter, 1u);
+          at = __shfl_sync(0xffffffffu, at, 0) + gridDim.x;
+        }
+        if (at >= n_items) {
+          // every CTA draws one number past the items; the one that draws the last of them leaves the counter as it was found
+          if (lane == 0) {
+            const unsigned int draws = (n_items > gridDim.x ? (unsigned int)n_items - gridDim.x : 0u) + gridDim.x;
+            const unsigned int mine = drawn ? at - gridDim.x : atomicAdd(p.counter, 1u);
+            if (mine + 1 == draws) *p.counter = 0u;
+          }
           last = 1;
           break;
         }
-        const bool tail = at >= p.n_whole;
-        const long long in_tail = tail ? (at - p.n_whole) % p.n_tail : 0;
-        const int split = tail ? (int)((at - p.n_whole) / p.n_tail) : 0, n_split = tail ? p.n_split : 1;
-        const long long flat = tail ? p.n_whole + in_tail : at;
+        drawn = true;
+        const bool in_tail = at >= n_whole;
+        const long long tail_unit = in_tail ? (at - n_whole) % tail : 0;
+        const long long flat = in_tail ? n_whole + tail_unit : at;
+        int split = in_tail ? (int)((at - n_whole) / tail) : 0, n_split = in_tail ? tail_split : 1;
+        int first_part = (int)tail_unit * tail_split, join_at = (int)tail_unit;
         // ---- which sequence, K/V head and rows
         int si = 0, kv_head = 0;
         long long t0 = -1;
         if (sorted) {
-          if (flat < n_units) {
-            const int slot = 31 - __clz(__ballot_sync(0xffffffffu, start[lane] <= flat && lane < p.a.n_seqs));
-            si = order[slot];
-            const unsigned int n = (unsigned int)((p.a.seqs[si].n_tokens + per_unit - 1) / per_unit);
-            const unsigned int local = (unsigned int)flat - start[slot];
-            kv_head = (int)(local / n);
-            t0 = (long long)(local % n) * per_unit;
+          const int slot = 31 - __clz(__ballot_sync(0xffffffffu, start[lane] <= flat && lane < p.a.n_seqs));
+          si = order[slot];
+          const int n = (notes[si].n_tok + per_unit - 1) / per_unit;
+          int local = (int)(flat - start[slot]);
+          if (n_part[slot] > 1) {                          // part by part: units that run together share their keys
+            n_split = n_part[slot];
+            split = local / n_unit[slot];
+            local -= split * n_unit[slot];
+            first_part = part0[slot] + local * n_split;
+            join_at = local;
+            for (int r = 0; r < slot; ++r) join_at += n_part[r] > 1 ? n_unit[r] : 0;
           }
+          kv_head = local / n;
+          t0 = (long long)(local - kv_head * n) * per_unit;
         } else {
           long long first;
           kv_head = (int)(flat / p.units);
@@ -697,18 +792,27 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
           if (t0 >= p.a.seqs[si].n_tokens) t0 = -1;
         }
         UnitDev un{};
-        if (t0 >= 0) {
+        un.t0 = (int)t0;
+        un.kv_head = kv_head;
+        if (sorted) {
+          const SeqNote& q = notes[si];
+          un.tok0 = q.tok0;
+          un.n_tok = q.n_tok;
+          un.span.n = q.n;
+          un.span.cap = q.cap;
+          un.span.begin = q.at;
+          un.span.table = kPaged ? p.d.c.table + q.at * p.d.c.width : nullptr;
+          un.span.mask = p.d.mask != nullptr ? p.d.mask + (kPaged ? q.at * p.d.mask_stride : (long long)q.at) : nullptr;
+        } else if (t0 >= 0) {
           const SeqDev& sq = p.a.seqs[si];
           un.span = find_span<kPaged>(p.d, sq.seq_id);
-          un.t0 = (int)t0;
           un.n_tok = sq.n_tokens;
           un.tok0 = sq.tok_start;
-          un.kv_head = kv_head;
         }
         const bool none = t0 < 0 || un.span.idle;
-        if (tail && n_split > 1 && split == 0 && lane == 0) p.join[in_tail] = JoinUnit{un.tok0, un.t0, none ? 0 : un.n_tok, kv_head, 0};
+        if (n_split > 1 && split == 0 && lane == 0) p.join[join_at] = JoinUnit{un.tok0, un.t0, none ? 0 : un.n_tok, kv_head, first_part, n_split, 0};
         if (none) continue;
-        un.part = n_split > 1 ? in_tail * n_split + split : -1;
+        un.part = n_split > 1 ? first_part + split : -1;
         un.n_tiles = un.n_tok - un.t0 > p.tok_per_tile ? 2 : 1;
         un.lim[0] = key_limit(un.span, un.n_tok, un.t0, p.a.causal);
         un.lim[1] = key_limit(un.span, un.n_tok, un.t0 + p.tok_per_tile, p.a.causal);
@@ -721,20 +825,23 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
           if (si != looked_at) {
             looked_at = si;
             live = 0;
-            for (int jt = 0; jt * 128 < un.span.cap && jt < 32; ++jt) {
-              bool on = false;
+            for (int jt = 0; jt * 128 < un.span.cap && jt < 32; jt += 4) {  // the loads of four tiles together
+              bool on[4] = {false, false, false, false};
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
+              for (int e = 0; e < 16; ++e) {
                 const int key = jt * 128 + e * 32 + lane;
-                on = on || (key < un.span.cap && __ldg(un.span.mask + key) != 0);
+                const bool counts = key < un.span.cap && __ldg(un.span.mask + key) != 0;
+                on[e >> 2] |= counts;
               }
-              live |= (__any_sync(0xffffffffu, on) ? 1u : 0u) << jt;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) live |= (__any_sync(0xffffffffu, on[e]) ? 1u : 0u) << (jt + e);
             }
           }
           const uint32_t mine = live & (un.n_keys > 0 ? (0xffffffffu >> (32 - un.n_keys)) << un.tile_begin : 0u);
           un.live = mine;
           un.n_keys = __popc(mine);
         }
+        un.withhold = p.fault_inject == 1u && at == 0;
         if (lane == 0) units[u & (kUnitRing - 1)] = un;
         break;
       }

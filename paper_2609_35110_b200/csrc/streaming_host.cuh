@@ -89,13 +89,13 @@ int take_context(const sol_attn3d_context* x, sol::KeysDev* d) {
 
 // ---- attention of few rows ------------------------------------------------------------------------------------------------
 // Splits of the keys: about 1,024 keys of the longest possible past per CTA, so that streams of different length even out; at least
-// what makes three waves of resident CTAs when there are few units, at most eight waves (a table may be far wider than its streams are
-// long, and a CTA without keys still costs its start); never below 256 keys.  Depends on the sizes of the call only (the lengths live
-// on the device).
+// a wave of resident CTAs when there are few units, at most eight waves (a table may be far wider than its streams are long, and a
+// CTA without keys still costs its start); never below 256 keys.  Depends on the sizes of the call only (the lengths live on the
+// device).
 constexpr long long kFewWave = 148 * sol::kFewResident, kFewMinKeys = 256, kFewMaxSplit = 256;
 int few_splits(long long items, long long capacity) {
   if (items < 1) return 1;
-  const long long want = std::min(std::max((capacity + 1023) / 1024, 3 * kFewWave / items), (8 * kFewWave + items - 1) / items);
+  const long long want = std::min(std::max((capacity + 1023) / 1024, kFewWave / items), (8 * kFewWave + items - 1) / items);
   return (int)std::max<long long>(1, std::min(std::min(want, kFewMaxSplit), capacity / kFewMinKeys));
 }
 long long few_units(sol_attn3d_plan_t p, int batch, int group) {
@@ -114,8 +114,7 @@ cudaError_t launch_few(const sol::FewArgs& f, cudaStream_t st, int* launches) {
   if ((e = launch_chained(sol::few_rows_kernel<D, kPaged>, items * (unsigned)f.n_split, sol::kFewThreads, sol::FewSmem<D>::kBytes, st, f)) != cudaSuccess) return e;
   ++*launches;
   if (f.partial != nullptr) {
-    const sol::JoinArgs j{f.a, f.d, f.n_split, sol::kFewRows, f.units, f.partial, nullptr};
-    if ((e = launch_chained(sol::join_rows_kernel<D, kPaged, false>, dim3(items, (sol::kFewRows * D / 8 + 255) / 256), 256, 0, st, j)) != cudaSuccess) return e;
+    if ((e = launch_chained(sol::join_few_kernel<D, kPaged>, items, 32 * sol::kJoinWarps, 0, st, f)) != cudaSuccess) return e;
     ++*launches;
   }
   return cudaSuccess;
@@ -152,7 +151,8 @@ struct ContextRoute {
   bool few;
   int group, tok_per_tile, n_split;
   long long units;              // per K/V head
-  long long n_whole, n_tail;    // units of all heads that take all of their keys; units whose keys are split
+  long long n_whole, n_tail;    // more than kSortedSeqs sequences: units of all heads that take all of their keys; units whose keys are split
+  long long max_parts, max_joins;   // what the workspace has room for
 };
 ContextRoute choose_route(sol_attn3d_plan_t p, int kv_heads, long long capacity, long long total_rows) {
   ContextRoute r{};
@@ -166,35 +166,45 @@ ContextRoute choose_route(sol_attn3d_plan_t p, int kv_heads, long long capacity,
   }
   r.tok_per_tile = 128 / r.group;
   const int per_unit = 2 * r.tok_per_tile;
-  // (sequences are sorted on the device up to kSortedSeqs; more are numbered with room for one empty unit each, see find_sequence)
-  for (const SeqDev& q : p->sched) r.units += (q.n_tokens + per_unit - 1) / per_unit;
-  if (p->n_seqs > sol::kSortedSeqs) r.units = p->total_tokens / per_unit + p->n_seqs;
-  // Units are dealt to 148 SMs.  What is left after the last whole wave, or all of them if there are few, is split by keys so that it
-  // ends as one wave of short units.  The cost of a unit is its key tiles (about 2 us each; the longest possible past is assumed) and
-  // 2 tiles' time for its start and end; a part's partial rows go through memory for 0.03, and joining is a launch: 1.5.
-  const long long flat = r.units * kv_heads, tiles = (capacity + 127) / 128, waves = flat / 148;
+  const long long tiles = (capacity + 127) / 128;
+  if (p->n_seqs <= sol::kSortedSeqs) {
+    // planned on the device: room for three waves of parts, or for all that units of four key tiles at least can make
+    for (const SeqDev& q : p->sched) r.units += (q.n_tokens + per_unit - 1) / per_unit;
+    r.n_split = 1;
+    r.n_whole = r.units * kv_heads;
+    const long long parts = std::min<long long>(32, tiles / 4);
+    if (parts >= 2) r.max_parts = std::min<long long>(3 * sol::kPlanSms, r.n_whole * parts);
+    r.max_joins = r.max_parts / 2;
+    return r;
+  }
+  // Many sequences: what is left after the last whole wave of units, or all of them if there are few, is split so that it ends as one
+  // wave of short units; the longest possible past is assumed.  Costs as in context_attn_kernel.
+  r.units = p->total_tokens / per_unit + p->n_seqs;
+  const long long flat = r.units * kv_heads, waves = flat / sol::kPlanSms;
   double best = 0.0;
-  for (long long back = 0; back <= 2 && back <= waves; ++back) {
-    const long long whole = (waves - back) * 148, tail = flat - whole;
-    for (int n = 1; n <= std::max<long long>(1, std::min<long long>(64, tiles / 2)); ++n) {
-      const double cost = (double)(waves - back) * (tiles + 2.0) + (double)((tail * n + 147) / 148) * ((tiles + n - 1) / n + 2.0) +
-                          (n > 1 ? 1.5 + 0.03 * (double)(tail * n) : 0.0);
-      if ((back == 0 && n == 1) || cost < 0.97 * best) {
-        best = cost;
-        r.n_split = n;
-        r.n_whole = n > 1 ? whole : flat;
-        r.n_tail = flat - r.n_whole;
-      }
+  for (int n = 1; n <= std::max<long long>(1, std::min<long long>(32, tiles / 4)); ++n) {
+    const long long whole = waves * sol::kPlanSms, tail = flat - whole;
+    const double cost = (double)waves * (tiles + 2.0) + (double)((tail * n + sol::kPlanSms - 1) / sol::kPlanSms) * ((tiles + n - 1) / n + 2.0) +
+                        (n > 1 ? 1.5 + 0.03 * (double)(tail * n) : 0.0);
+    if (n == 1 || cost < best) {
+      best = cost;
+      r.n_split = n;
+      r.n_whole = n > 1 ? whole : flat;
+      r.n_tail = flat - r.n_whole;
     }
+  }
+  if (r.n_tail == 0) r.n_split = 1;
+  if (r.n_split > 1) {
+    r.max_parts = r.n_tail * r.n_split;
+    r.max_joins = r.n_tail;
   }
   return r;
 }
 
-size_t join_list_bytes(const ContextRoute& r) { return align_up((size_t)r.n_tail * sizeof(sol::JoinUnit)); }
+size_t join_list_bytes(const ContextRoute& r) { return kAlign + align_up((size_t)r.max_joins * sizeof(sol::JoinUnit)); }
 
 size_t many_bytes(const ContextRoute& r, int head_dim) {
-  if (r.n_split == 1) return 0;
-  return join_list_bytes(r) + align_up((size_t)r.n_tail * r.n_split * 2 * r.tok_per_tile * r.group * (head_dim + 4) * sizeof(float));
+  return r.max_parts == 0 ? 0 : join_list_bytes(r) + align_up((size_t)r.max_parts * 2 * r.tok_per_tile * r.group * (head_dim + 4) * sizeof(float));
 }
 
 size_t context_bytes(sol_attn3d_plan_t p, int kv_heads, long long capacity, long long total_rows) {
@@ -221,24 +231,25 @@ int encode_boxes(sol_attn3d_plan_t p, CUtensorMap* tm, const void* base, int ran
 }
 
 template <int D, bool kPaged, bool kMask>
-cudaError_t launch_context_as(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const sol::ContextParams& c, int sms, cudaStream_t st, int* launches) {
+cudaError_t launch_context_as(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const sol::ContextParams& c, long long items, int sms, cudaStream_t st,
+                             int* launches) {
   cudaError_t e = cudaFuncSetAttribute(sol::context_attn_kernel<D, kPaged, kMask>, cudaFuncAttributeMaxDynamicSharedMemorySize, sol::ContextSmem<D>::kDynBytes);
   if (e != cudaSuccess) return e;
-  if ((e = launch_chained(sol::context_attn_kernel<D, kPaged, kMask>, (unsigned)std::min<long long>(c.total, sms), sol::kAttnThreads, sol::ContextSmem<D>::kDynBytes, st,
+  if ((e = launch_chained(sol::context_attn_kernel<D, kPaged, kMask>, (unsigned)std::min<long long>(items, sms), sol::kAttnThreads, sol::ContextSmem<D>::kDynBytes, st,
                           q, k, v, c)) != cudaSuccess) return e;
   ++*launches;
   if (c.partial != nullptr) {
-    const sol::JoinArgs j{c.a, c.d, c.n_split, 2 * c.tok_per_tile * c.a.group, c.units, c.partial, c.join};
-    if ((e = launch_chained(sol::join_rows_kernel<D, kPaged, true>, dim3((unsigned)c.n_tail, (unsigned)(j.rows_per_unit * D / 8 + 255) / 256), 256, 0, st, j)) != cudaSuccess)
-      return e;
+    const sol::JoinArgs j{c.a, 2 * c.tok_per_tile * c.a.group, c.partial, c.join, c.join_count};
+    if ((e = launch_chained(sol::join_units_kernel<D>, 4 * sol::kPlanSms, 32 * sol::kJoinWarps, 0, st, j)) != cudaSuccess) return e;
     ++*launches;
   }
   return cudaSuccess;
 }
 
 template <int D, bool kPaged>
-cudaError_t launch_context(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const sol::ContextParams& c, int sms, cudaStream_t st, int* launches) {
-  return c.d.mask != nullptr ? launch_context_as<D, kPaged, true>(q, k, v, c, sms, st, launches) : launch_context_as<D, kPaged, false>(q, k, v, c, sms, st, launches);
+cudaError_t launch_context(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const sol::ContextParams& c, long long items, int sms, cudaStream_t st, int* launches) {
+  return c.d.mask != nullptr ? launch_context_as<D, kPaged, true>(q, k, v, c, items, sms, st, launches)
+                             : launch_context_as<D, kPaged, false>(q, k, v, c, items, sms, st, launches);
 }
 
 int attend_many(sol_attn3d_plan_t p, const sol::QueriesDev& a, const sol::KeysDev& d, bool paged, const ContextRoute& r, void* workspace,
@@ -250,14 +261,16 @@ int attend_many(sol_attn3d_plan_t p, const sol::QueriesDev& a, const sol::KeysDe
   c.n_split = r.n_split;
   c.n_whole = r.n_whole;
   c.n_tail = r.n_tail;
-  c.total = r.n_whole + r.n_tail * r.n_split;
-  if (c.total >= (1ll << 31)) return SOL_ATTN3D_ERR_UNSUPPORTED_SHAPE;
+  const long long items = r.n_whole + r.n_tail * r.n_split + r.max_parts;   // at most (the grid need not be larger; the counter has to hold them)
+  if (items >= (1ll << 31)) return SOL_ATTN3D_ERR_UNSUPPORTED_SHAPE;
+  c.max_parts = (int)r.max_parts;
   c.tok_per_tile = r.tok_per_tile;
   c.inv_group = (65536u + r.group - 1) / r.group;
   c.lookahead = lookahead;
-  if (r.n_split > 1) {
+  if (r.max_parts > 0) {
     if (workspace == nullptr || workspace_bytes < many_bytes(r, p->head_dim) || (reinterpret_cast<uintptr_t>(workspace) % kAlign) != 0) return SOL_ATTN3D_ERR_NO_WORKSPACE;
-    c.join = static_cast<sol::JoinUnit*>(workspace);
+    c.join_count = static_cast<int*>(workspace);
+    c.join = reinterpret_cast<sol::JoinUnit*>(static_cast<unsigned char*>(workspace) + kAlign);
     c.partial = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + join_list_bytes(r));
   }
   c.counter = reinterpret_cast<unsigned int*>(p->ws + p->off_status + kUnitCounterOffset);
@@ -289,10 +302,10 @@ int attend_many(sol_attn3d_plan_t p, const sol::QueriesDev& a, const sol::KeysDe
     }
   }
   if (rc != SOL_ATTN3D_OK) return rc;
-  const cudaError_t e = p->head_dim == 128 ? (paged ? launch_context<128, true>(tm_q, tm_k, tm_v, c, p->sm_count, st, &p->launches)
-                                                    : launch_context<128, false>(tm_q, tm_k, tm_v, c, p->sm_count, st, &p->launches))
-                                           : (paged ? launch_context<64, true>(tm_q, tm_k, tm_v, c, p->sm_count, st, &p->launches)
-                                                    : launch_context<64, false>(tm_q, tm_k, tm_v, c, p->sm_count, st, &p->launches));
+  const cudaError_t e = p->head_dim == 128 ? (paged ? launch_context<128, true>(tm_q, tm_k, tm_v, c, items, p->sm_count, st, &p->launches)
+                                                    : launch_context<128, false>(tm_q, tm_k, tm_v, c, items, p->sm_count, st, &p->launches))
+                                           : (paged ? launch_context<64, true>(tm_q, tm_k, tm_v, c, items, p->sm_count, st, &p->launches)
+                                                    : launch_context<64, false>(tm_q, tm_k, tm_v, c, items, p->sm_count, st, &p->launches));
   return e == cudaSuccess ? SOL_ATTN3D_OK : fail_cuda(p, e);
 }
 
