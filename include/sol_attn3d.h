@@ -535,7 +535,7 @@ int sol_attn3d_linear_step(const void* q, const void* k, const void* v, void* ou
  *   lens      DEVICE, int32 [n_streams].  Values are clamped to [0, table_width * page_size].
  *   refs      DEVICE, int32 [n_pages]: how many streams hold a page; 0 = free.  NULL is fine for the calls that only read or
  *             write tokens (append and the attention); the others keep it.
- *   page_size a multiple of 16, at most 4096; n_pages * page_size and table_width * page_size below 2^31.
+ *   page_size a multiple of 16, at most 4096; n_pages * page_size and table_width * page_size at most 2^31 - 8192.
  * The struct is read during the call, the arrays when the kernels run.
  */
 typedef struct {
@@ -609,7 +609,8 @@ int sol_attn3d_cache_copy_pages(const sol_attn3d_paged_cache* cache, int n, cons
  * row i of sequence s, of n, becomes token lens - n + i of stream streams[s] (lens has been raised by sol_attn3d_cache_reserve);
  * rows whose token would be before the first one are not written.
  *   q, q_out       as in sol_attn3d_qknorm_rope (the plan's q strides; dense output), or both NULL.
- *   k, v           DEVICE, bf16 [total_tokens, kv_heads, head_dim], element strides {token, head} ({0,0} = dense).
+ *   k, v           DEVICE, bf16 [total_tokens, kv_heads, head_dim], element strides {token, head} ({0,0} = dense).  Head strides, these,
+ *                  the plan's of q and the cache's, below 2^31.
  *   streams        DEVICE, int32 [n_seqs], or NULL: sequence s is stream s.  A sequence whose stream is outside [0, n_streams) is
  *                  idle: nothing of it is read or written.  Of several sequences with one stream the first one's K and V count.
  *   pos0           DEVICE, int32 [n_seqs][3], offsets of (t, h, w) of the sequence's grid, or NULL (0).  Angles are found in fp64, so
@@ -675,7 +676,7 @@ typedef struct {
   const void* v;
   int64_t k_strides[2];
   int64_t v_strides[2];
-  int64_t total_rows;           /* below 2^31 */
+  int64_t total_rows;           /* at most 2^31 - 8192 */
   const int32_t* begins;
   const int32_t* lens;
   int64_t max_len;
@@ -768,7 +769,7 @@ int sol_attn3d_debug_build(void);
  * around it).  enable != 0 creates four CUDA events owned by the plan; every later forward records
  * them on its stream around its three steps.  sol_attn3d_last_forward_ms blocks on the last event
  * (cudaEventSynchronize) and writes ms[0..2] = {key-validity bits, rotary prologue, attention kernel}
- * of the most recent forward (0, or next to it, for a step that was skipped; sol_attn3d_forward_linear has the third only).  Returns INVALID_ARG if profiling is
+ * of the most recent forward (0, or next to it, for a step that was skipped; sol_attn3d_forward_linear, _paged and _cross have the third only).  Returns INVALID_ARG if profiling is
  * off or no forward ran.  enable == 0 destroys the events.
  */
 int sol_attn3d_set_profiling(sol_attn3d_plan_t plan, int enable);
@@ -779,7 +780,8 @@ int sol_attn3d_last_forward_ms(sol_attn3d_plan_t plan, float ms[3]);
  * sol_attn3d_rope_qk, sol_attn3d_qknorm_rope), counted as they were launched: the dense forward launches 2 (rotary
  * prologue, attention) plus 1 when the key-validity bits are rebuilt; the block-sparse forward adds 3 per sequence,
  * the rectangular one 1, and sol_attn3d_forward_host launches one such set per head group.  The differential forward
- * launches 2, plus 1 with a key mask and 1 with a query mask; the linear one 1, or 2 when sequences are cut.  Host-side counter, no
+ * launches 2, plus 1 with a key mask and 1 with a query mask; the linear one 1, or 2 when sequences are cut; those over a paged cache or
+ * a context 1, or 2 where keys may be split, sol_attn3d_cache_append 1.  Host-side counter, no
  * device access.  For launch accounting in benchmarks (Section 3.2 counts launches around "SDPA").
  */
 int sol_attn3d_last_launch_count(sol_attn3d_plan_t plan);

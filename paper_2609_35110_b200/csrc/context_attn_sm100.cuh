@@ -810,7 +810,7 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
           un.tok0 = sq.tok_start;
         }
         const bool none = t0 < 0 || un.span.idle;
-        if (n_split > 1 && split == 0 && lane == 0) p.join[join_at] = JoinUnit{un.tok0, un.t0, none ? 0 : un.n_tok, kv_head, first_part, n_split, 0};
+        if (n_split > 1 && split == 0 && lane == 0) p.join[join_at] = JoinUnit{un.tok0, none ? 0 : un.t0, none ? 0 : un.n_tok, kv_head, first_part, n_split, 0};
         if (none) continue;
         un.part = n_split > 1 ? first_part + split : -1;
         un.n_tiles = un.n_tok - un.t0 > p.tok_per_tile ? 2 : 1;

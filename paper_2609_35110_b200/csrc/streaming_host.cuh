@@ -23,6 +23,9 @@ cudaError_t launch_chained(void (*kernel)(Params...), dim3 grid, unsigned thread
   return e;
 }
 
+// Keys are counted in 32 bits, and the kernels look a tile or a page past them.
+constexpr long long kMaxKeys = (1ll << 31) - 8192;
+
 // Checks a cache and, for a layer, fills in what the kernels see of it.
 int take_cache(const sol_attn3d_paged_cache* c, int layer, sol::PagedDev* out) {
   if (c == nullptr || c->size != sizeof(sol_attn3d_paged_cache) || c->n_layers < 1 || c->page_size < 1 || c->kv_heads < 1 ||
@@ -30,7 +33,7 @@ int take_cache(const sol_attn3d_paged_cache* c, int layer, sol::PagedDev* out) {
     return SOL_ATTN3D_ERR_INVALID_ARG;
   if ((c->head_dim != 64 && c->head_dim != 128) || c->kv_heads > 65535 || c->page_size % 16 != 0 || c->page_size > 4096 ||
       c->n_pages >= (1ll << 31) || c->table_width >= (1ll << 31) || c->n_streams >= (1ll << 31) ||
-      c->n_pages * c->page_size >= (1ll << 31) || c->table_width * c->page_size >= (1ll << 31))
+      c->n_pages * c->page_size > kMaxKeys || c->table_width * c->page_size > kMaxKeys)
     return SOL_ATTN3D_ERR_UNSUPPORTED_SHAPE;
   if (c->k == nullptr || c->v == nullptr || c->table == nullptr || c->lens == nullptr || !aligned16(c->k) || !aligned16(c->v) ||
       !aligned4(c->table) || !aligned4(c->lens) || !aligned4(c->refs))
@@ -65,7 +68,7 @@ int take_cache(const sol_attn3d_paged_cache* c, int layer, sol::PagedDev* out) {
 int take_context(const sol_attn3d_context* x, sol::KeysDev* d) {
   if (x == nullptr || x->size != sizeof(sol_attn3d_context) || x->kv_heads < 1 || x->head_dim < 1 || x->total_rows < 0 || x->max_len < 0)
     return SOL_ATTN3D_ERR_INVALID_ARG;
-  if ((x->head_dim != 64 && x->head_dim != 128) || x->kv_heads > 65535 || x->total_rows >= (1ll << 31))
+  if ((x->head_dim != 64 && x->head_dim != 128) || x->kv_heads > 65535 || x->total_rows > kMaxKeys)
     return SOL_ATTN3D_ERR_UNSUPPORTED_SHAPE;
   if (x->begins == nullptr || x->lens == nullptr || !aligned4(x->begins) || !aligned4(x->lens) || !aligned16(x->k) || !aligned16(x->v) ||
       (x->total_rows > 0 && (x->k == nullptr || x->v == nullptr)))

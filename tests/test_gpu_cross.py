@@ -168,3 +168,30 @@ def test_strided_outputs():
     ref, mag = so.attend(q[:200], kv_t[begins[0]:begins[0] + 300, 0], kv_t[begins[0]:begins[0] + 300, 1], so.key_limits(200, 300, 0))
     close(out[:200].cpu(), ref, mag)
     assert bool((out[200:] == 0).all()) and bool((buf[:, 1::2] == 7.0).all()) and bool((buf[:, 4] == 7.0).all())
+
+
+@pytest.mark.parametrize("masked", [False, True])
+def test_many_sequences_with_split_keys(masked):
+    """More sequences than are planned on the device, contexts long enough to be split, empty units among the split ones."""
+    from paper_2609_35110_b200 import binding as B
+    sizes, lens = [(50 * i) % 299 + 1 for i in range(40)], [0 if i % 5 == 4 else 90 * i % 2000 + 1 for i in range(40)]
+    for heads, kv in ((1, 1), (6, 2)):
+        kv_t, begins = contexts(lens, kv, 64, seed=heads)
+        g = torch.Generator().manual_seed(2)
+        mask = (torch.rand(kv_t.shape[0], generator=g) < 0.7).to(torch.uint8) if masked else None
+        dev = kv_t.cuda()
+        ctx = B.sol_attn3d_context(dev[:, 0], dev[:, 1], ints(begins), ints(lens), 2000, key_mask=None if mask is None else mask.cuda())
+        q = torch.randn(sum(sizes), heads, 64, generator=g).bfloat16()
+        room = torch.full((sum(sizes) + 600, heads, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+        out = room[300:300 + sum(sizes)]                                # what lies before and behind stays
+        attn = B.Attn3d([(n, 0, 1, 1) for n in sizes], heads, 64, rope(64))
+        ws = torch.full((B.sol_attn3d_cross_workspace_bytes(attn.plan, ctx),), 255, dtype=torch.uint8, device="cuda")
+        assert ws.numel() > 0
+        B.sol_attn3d_forward_cross(attn.plan, q.cuda(), ctx, out, workspace=ws)
+        torch.cuda.synchronize()
+        assert attn.status() == 0 and bool((room[:300] == 7.0).all()) and bool((room[300 + sum(sizes):] == 7.0).all())
+        at = 0
+        for m, b, n in zip(sizes, begins, lens):
+            ref, mag = so.attend(q[at:at + m], kv_t[b:b + n, 0], kv_t[b:b + n, 1], so.key_limits(m, n, 0), None if mask is None else mask[b:b + n].bool())
+            close(out[at:at + m].cpu(), ref, mag)
+            at += m
