@@ -567,7 +567,7 @@ typedef struct {
  * Bookkeeping of streams.  All work is on the device, in stream order: no allocation, no synchronisation; may be captured.  The
  * result depends on the arrays alone: requests are served in their order, new pages are the free ones of the lowest index, and the
  * requests that need pages are served until the first one for which the free pages do not suffice.  A request that is not served
- * changes nothing and says why in status (which may be NULL).  n = 0 is a no-op; n is at most 4096.  Calls that may overlap on the
+ * changes nothing and says why in status (which may be NULL).  n = 0 is a no-op; n is at most 2048.  Calls that may overlap on the
  * GPU must not touch the same cache.
  *
  * reserve  lens[streams[i]] grows by amount[i] >= 0 tokens, with the pages that they need.  (Then sol_attn3d_cache_append, once per

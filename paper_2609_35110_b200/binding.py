@@ -9,6 +9,7 @@ a B200.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Optional, Sequence, Tuple
 
@@ -279,9 +280,13 @@ def _check(code: int, where: str) -> None:
 
 
 # ----------------------------------------------------------------- 1:1 wrappers
+class _Plan(ctypes.c_void_p):
+    """A plan's handle; `dims` (what sol_attn3d_plan_dims answers) is kept with it once asked for."""
+
+
 def sol_attn3d_plan(B: int, heads: int, head_dim: int, T: int, H: int, W: int, text_len: int,
                     rope_dims: Sequence[int]) -> ctypes.c_void_p:
-    h = ctypes.c_void_p()
+    h = _Plan()
     rd = (ctypes.c_int * 3)(*[int(x) for x in rope_dims])
     _check(_lib().sol_attn3d_plan(ctypes.byref(h), B, heads, head_dim, T, H, W, text_len, rd), "sol_attn3d_plan")
     return h
@@ -310,7 +315,7 @@ def sol_attn3d_plan_ex(seqs: Sequence[Tuple[int, int, int, int]], heads: int, he
                       ("out_strides", out_strides)):
         arr = getattr(d, name)
         arr[0], arr[1] = int(val[0]), int(val[1])
-    h = ctypes.c_void_p()
+    h = _Plan()
     _check(_lib().sol_attn3d_plan_ex(ctypes.byref(h), ctypes.byref(d)), "sol_attn3d_plan_ex")
     return h
 
@@ -782,6 +787,50 @@ def _check_decay(log_decay: torch.Tensor, heads: int) -> None:
         raise ValueError("log_decay must be a contiguous CUDA float32 tensor with one element per head")
 
 
+def _dims(plan) -> Tuple[int, int, int, int]:
+    """sol_attn3d_plan_dims, asked once per handle."""
+    dims = getattr(plan, "dims", None)
+    if dims is None:
+        dims = sol_attn3d_plan_dims(plan)
+        if isinstance(plan, _Plan):
+            plan.dims = dims
+    return dims
+
+
+_shared_strides = functools.lru_cache(maxsize=1024)(_I64x2)      # arrays that are only read
+
+
+def _shared_row_strides(t: torch.Tensor, head_dim: int):
+    """_row_strides without building an array for every call."""
+    if t.is_contiguous():
+        return _DENSE2
+    shape, st = t.shape, t.stride()
+    if shape[2] != head_dim or st[2] != 1:
+        raise ValueError("expected [tokens, heads, head_dim] with contiguous head_dim")
+    s0, s1 = st[0] if shape[0] > 1 else shape[1] * head_dim, st[1] if shape[1] > 1 else head_dim
+    if s0 == 0 or s1 == 0:
+        raise ValueError("expanded tensors (stride 0) are not supported")
+    return _shared_strides(s0, s1)
+
+
+def _one_device(tensors) -> int:
+    """The device that all of them live on."""
+    device = tensors[0].get_device()
+    if any(t.get_device() != device for t in tensors):
+        raise ValueError("all tensors must be on one device")
+    return device
+
+
+def _check_here(device: int, *tensors) -> None:
+    """_check_on_device for a holder of tensors (all on `device`) and some more."""
+    here = torch._C._cuda_getDevice()
+    if device != here:
+        raise ValueError(f"tensors on cuda:{device}, current device is cuda:{here}")
+    for t in tensors:
+        if t is not None and t.get_device() != here:
+            raise ValueError(f"tensor on {t.device}, current device is cuda:{here}")
+
+
 def _pool_strides(t: torch.Tensor, extents, n: int):
     """Element strides of all axes but the last; 0 (the dense value) where torch's is arbitrary (extent 0 or 1)."""
     st = t.stride()
@@ -810,6 +859,7 @@ class sol_attn3d_paged_cache:
         layers, pages, page, kv_heads, head_dim = k.shape
         self.k, self.v, self.table, self.lens, self.refs = k, v, table, lens, refs
         self.tensors = (k, v, table, lens) + (() if refs is None else (refs,))
+        self.device = _one_device(self.tensors)
         self.kv_heads, self.head_dim, self.n_streams = kv_heads, head_dim, table.shape[0]
         self.struct = _PagedCache(ctypes.sizeof(_PagedCache), layers, page, kv_heads, head_dim, k.data_ptr(), v.data_ptr(),
                                   _pool_strides(k, k.shape, 4), _pool_strides(v, v.shape, 4), pages, table.data_ptr(), lens.data_ptr(),
@@ -834,6 +884,7 @@ class sol_attn3d_context:
                                      key_mask.numel() != k.shape[0]):
             raise ValueError("key_mask must be a contiguous CUDA uint8 tensor with one element per row")
         self.tensors = (k, v, begins, lens) + (() if key_mask is None else (key_mask,))
+        self.device = _one_device(self.tensors)
         self.k, self.v, self.begins, self.lens, self.key_mask = k, v, begins, lens, key_mask
         self.kv_heads, self.head_dim, self.n = k.shape[1], k.shape[2], begins.numel()
         self.struct = _Context(ctypes.sizeof(_Context), k.shape[1], k.shape[2], k.data_ptr(), v.data_ptr(), _pool_strides(k, k.shape, 2),
@@ -853,9 +904,12 @@ def _check_requests(cache: sol_attn3d_paged_cache, status, *lists) -> int:
     n = lists[0].numel()
     if cache.refs is None:
         raise ValueError("this cache keeps no count of the streams that hold a page (refs)")
-    for t in lists + (status,):
-        _check_index(t, n, "streams, parents, amounts, status")
-    _check_on_device(*cache.tensors, *lists, status)
+    here = torch._C._cuda_getDevice()
+    if cache.device != here:
+        raise ValueError(f"the cache is on cuda:{cache.device}, current device is cuda:{here}")
+    for t in lists if status is None else (status,) + lists:
+        if t.dtype is not torch.int32 or t.get_device() != here or t.numel() != n or not t.is_contiguous():
+            raise ValueError(f"streams, parents, amounts, status must be contiguous int32 tensors of one size on cuda:{here}")
     return n
 
 
@@ -903,7 +957,7 @@ def sol_attn3d_cache_copy_pages(cache: sol_attn3d_paged_cache, src_pages: torch.
     n = src_pages.numel()
     _check_index(src_pages, n, "src_pages")
     _check_index(dst_pages, n, "dst_pages")
-    _check_on_device(*cache.tensors, src_pages, dst_pages)
+    _check_here(cache.device, src_pages, dst_pages)
     _check(_lib().sol_attn3d_cache_copy_pages(cache.ref, n, _ptr(src_pages), _ptr(dst_pages), _stream(stream)), "sol_attn3d_cache_copy_pages")
 
 
@@ -918,27 +972,35 @@ def sol_attn3d_cache_append(plan, q: Optional[torch.Tensor], k: torch.Tensor, v:
                             pos0: Optional[torch.Tensor] = None, q_gain: Optional[torch.Tensor] = None, k_gain: Optional[torch.Tensor] = None,
                             eps: float = 0.0, stream=None) -> None:
     """Norm and rotation of new tokens; K and V go to the last tokens of their streams, Q to q_out."""
-    n_seqs, heads, head_dim, tokens = sol_attn3d_plan_dims(plan)
-    both = [t for t in (q, q_out) if t is not None]
-    _check_bf16(k, v, *both)
-    _check_sizes(tokens, heads * head_dim, both, ())
+    n_seqs, heads, head_dim, tokens = _dims(plan)
+    here = torch._C._cuda_getDevice()
+    if cache.device != here:
+        raise ValueError(f"the cache is on cuda:{cache.device}, current device is cuda:{here}")
+    # (a tensor on the CPU has device -1)
+    for t in (k, v, q, q_out):
+        if t is not None and (t.dtype is not torch.bfloat16 or t.get_device() != here):
+            raise ValueError(f"q, k, v, q_out must be bf16 tensors on cuda:{here}")
+    for t in (q, q_out):
+        if t is not None and t.numel() < tokens * heads * head_dim:
+            raise ValueError(f"q, q_out: the plan has {tokens} tokens of {heads * head_dim} values")
     if q_out is not None and not q_out.is_contiguous():
         raise ValueError("q_out must be contiguous")
     want = (tokens, cache.kv_heads, cache.head_dim)
     if k.shape != want or v.shape != want:
         raise ValueError(f"k, v: {list(want)} for this plan and cache")
-    _check_index(streams, n_seqs, "streams")
-    if pos0 is not None and (not pos0.is_cuda or pos0.dtype != torch.int32 or not pos0.is_contiguous() or pos0.shape != (n_seqs, 3)):
-        raise ValueError("pos0 must be a contiguous CUDA int32 tensor [sequences, 3]")
+    for t, n, name in ((streams, n_seqs, "streams"), (pos0, 3 * n_seqs, "pos0")):
+        if t is not None and (t.dtype is not torch.int32 or t.get_device() != here or t.numel() != n or not t.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous int32 tensor of {n} elements on cuda:{here}")
     for g in (q_gain, k_gain):
-        if g is not None:
-            _check_gain(g)
-            if g.numel() != head_dim:
-                raise ValueError("gains have head_dim elements")
-    _check_on_device(*cache.tensors, k, v, *both, streams, pos0, q_gain, k_gain)
-    _check(_lib().sol_attn3d_cache_append(plan, _ptr(q), _ptr(k), _ptr(v), _row_strides(k, head_dim), _row_strides(v, head_dim), _ptr(q_out),
-                                          cache.ref, layer, _ptr(streams), _ptr(pos0), _ptr(q_gain), _ptr(k_gain), eps, _stream(stream)),
-           "sol_attn3d_cache_append")
+        if g is not None and (g.dtype is not torch.float32 or g.get_device() != here or g.numel() != head_dim or not g.is_contiguous()):
+            raise ValueError(f"gains must be contiguous float32 tensors of {head_dim} elements on cuda:{here}")
+    code = _lib().sol_attn3d_cache_append(
+        plan, None if q is None else q.data_ptr(), k.data_ptr(), v.data_ptr(), _shared_row_strides(k, head_dim), _shared_row_strides(v, head_dim),
+        None if q_out is None else q_out.data_ptr(), cache.ref, layer, None if streams is None else streams.data_ptr(),
+        None if pos0 is None else pos0.data_ptr(), None if q_gain is None else q_gain.data_ptr(),
+        None if k_gain is None else k_gain.data_ptr(), eps, _stream(stream))
+    if code != OK:
+        raise SolAttn3dError(code, "sol_attn3d_cache_append")
 
 
 def _check_key_mask(cache: sol_attn3d_paged_cache, key_mask: Optional[torch.Tensor]) -> int:
@@ -958,13 +1020,13 @@ def sol_attn3d_forward_paged(plan, q: torch.Tensor, cache: sol_attn3d_paged_cach
                              streams: Optional[torch.Tensor] = None, key_mask: Optional[torch.Tensor] = None, causal_block: int = 0,
                              workspace: Optional[torch.Tensor] = None, stream=None) -> None:
     """The plan's sequences are the last tokens of streams of the cache and attend to them; causal_block: see the header."""
-    n_seqs, heads, head_dim, tokens = sol_attn3d_plan_dims(plan)
+    n_seqs, heads, head_dim, tokens = _dims(plan)
     _check_bf16(q, out)
     _check_sizes(tokens, heads * head_dim, (q, out), ())
     _check_index(streams, n_seqs, "streams")
     width = _check_key_mask(cache, key_mask)
     nbytes = _check_workspace(workspace)
-    _check_on_device(*cache.tensors, q, out, streams, key_mask, workspace)
+    _check_here(cache.device, q, out, streams, key_mask, workspace)
     _check(_lib().sol_attn3d_forward_paged(plan, _ptr(q), cache.ref, layer, _ptr(out), _ptr(streams), _ptr(key_mask), width, causal_block,
                                            _ptr(workspace), nbytes, _stream(stream)), "sol_attn3d_forward_paged")
 
@@ -989,9 +1051,9 @@ def sol_attn3d_paged_step(q: torch.Tensor, cache: sol_attn3d_paged_cache, layer:
     _check_index(streams, batch, "streams")
     width = _check_key_mask(cache, key_mask)
     nbytes = _check_workspace(workspace)
-    _check_on_device(*cache.tensors, q, out, streams, key_mask, workspace)
-    _check(_lib().sol_attn3d_paged_step(_ptr(q), _DENSE2 if q.is_contiguous() else _row_strides(q, head_dim), cache.ref, layer, _ptr(streams),
-                                        _ptr(out), _DENSE2 if out.is_contiguous() else _row_strides(out, head_dim), batch, heads,
+    _check_here(cache.device, q, out, streams, key_mask, workspace)
+    _check(_lib().sol_attn3d_paged_step(_ptr(q), _shared_row_strides(q, head_dim), cache.ref, layer, _ptr(streams),
+                                        _ptr(out), _shared_row_strides(out, head_dim), batch, heads,
                                         _ptr(key_mask), width, _ptr(workspace), nbytes, _stream(stream)), "sol_attn3d_paged_step")
 
 
@@ -1002,13 +1064,13 @@ def sol_attn3d_cross_workspace_bytes(plan, context: sol_attn3d_context) -> int:
 def sol_attn3d_forward_cross(plan, q: torch.Tensor, context: sol_attn3d_context, out: torch.Tensor,
                              workspace: Optional[torch.Tensor] = None, stream=None) -> None:
     """Cross attention of the plan's sequences, each to its context."""
-    n_seqs, heads, head_dim, tokens = sol_attn3d_plan_dims(plan)
+    n_seqs, heads, head_dim, tokens = _dims(plan)
     _check_bf16(q, out)
     _check_sizes(tokens, heads * head_dim, (q, out), ())
     if context.n != n_seqs:
         raise ValueError(f"{n_seqs} sequences need as many contexts")
     nbytes = _check_workspace(workspace)
-    _check_on_device(*context.tensors, q, out, workspace)
+    _check_here(context.device, q, out, workspace)
     _check(_lib().sol_attn3d_forward_cross(plan, _ptr(q), context.ref, _ptr(out), _ptr(workspace), nbytes, _stream(stream)),
            "sol_attn3d_forward_cross")
 
@@ -1026,9 +1088,9 @@ def sol_attn3d_cross_step(q: torch.Tensor, context: sol_attn3d_context, out: tor
     if context.n != batch:
         raise ValueError("one context per row")
     nbytes = _check_workspace(workspace)
-    _check_on_device(*context.tensors, q, out, workspace)
-    _check(_lib().sol_attn3d_cross_step(_ptr(q), _DENSE2 if q.is_contiguous() else _row_strides(q, head_dim), context.ref, _ptr(out),
-                                        _DENSE2 if out.is_contiguous() else _row_strides(out, head_dim), batch, heads, _ptr(workspace), nbytes,
+    _check_here(context.device, q, out, workspace)
+    _check(_lib().sol_attn3d_cross_step(_ptr(q), _shared_row_strides(q, head_dim), context.ref, _ptr(out),
+                                        _shared_row_strides(out, head_dim), batch, heads, _ptr(workspace), nbytes,
                                         _stream(stream)), "sol_attn3d_cross_step")
 
 

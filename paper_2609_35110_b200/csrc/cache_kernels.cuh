@@ -256,7 +256,7 @@ __global__ void __launch_bounds__(256, 3) cache_append_kernel(const __grid_const
 // integer arithmetic whose result does not depend on the order in which threads run.
 // ---------------------------------------------------------------------------------------------
 enum : int { kCacheOk = 0, kCacheBadStream = 1, kCacheNoRoom = 2, kCacheNoPages = 3, kCacheNotEmpty = 4 };
-constexpr int kMaxRequests = 4096;
+constexpr int kMaxRequests = 2048;
 constexpr int kBookThreads = 512, kKeepThreads = 1024;
 
 struct BookArgs {

@@ -5,6 +5,21 @@ namespace {
 
 bool aligned4(const void* x) { return (reinterpret_cast<uintptr_t>(x) & 3u) == 0; }
 
+// Raises a kernel's limit of dynamic shared memory, once per device.
+template <auto kKernel>
+cudaError_t allow_shared_memory(int bytes) {
+  static std::atomic<unsigned long long> done{0};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const unsigned long long bit = dev < 64 ? 1ull << dev : 0ull;
+  if (done.load(std::memory_order_relaxed) & bit) return cudaSuccess;
+  e = cudaFuncSetAttribute(kKernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+  else (void)cudaGetLastError();
+  return e;
+}
+
 // Launches a kernel that begins with chained_wait(): it may be placed on the GPU while its predecessor in the stream still runs.
 template <typename... Params, typename... Args>
 cudaError_t launch_chained(void (*kernel)(Params...), dim3 grid, unsigned threads, size_t smem, cudaStream_t st, const Args&... args) {
@@ -112,7 +127,7 @@ size_t few_bytes(long long units, int kv_heads, int head_dim, long long capacity
 template <int D, bool kPaged>
 cudaError_t launch_few(const sol::FewArgs& f, cudaStream_t st, int* launches) {
   const unsigned items = (unsigned)(f.units * f.d.c.kv_heads);
-  cudaError_t e = cudaFuncSetAttribute(sol::few_rows_kernel<D, kPaged>, cudaFuncAttributeMaxDynamicSharedMemorySize, sol::FewSmem<D>::kBytes);
+  cudaError_t e = allow_shared_memory<&sol::few_rows_kernel<D, kPaged>>(sol::FewSmem<D>::kBytes);
   if (e != cudaSuccess) return e;
   if ((e = launch_chained(sol::few_rows_kernel<D, kPaged>, items * (unsigned)f.n_split, sol::kFewThreads, sol::FewSmem<D>::kBytes, st, f)) != cudaSuccess) return e;
   ++*launches;
@@ -236,7 +251,7 @@ int encode_boxes(sol_attn3d_plan_t p, CUtensorMap* tm, const void* base, int ran
 template <int D, bool kPaged, bool kMask>
 cudaError_t launch_context_as(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const sol::ContextParams& c, long long items, int sms, cudaStream_t st,
                              int* launches) {
-  cudaError_t e = cudaFuncSetAttribute(sol::context_attn_kernel<D, kPaged, kMask>, cudaFuncAttributeMaxDynamicSharedMemorySize, sol::ContextSmem<D>::kDynBytes);
+  cudaError_t e = allow_shared_memory<&sol::context_attn_kernel<D, kPaged, kMask>>(sol::ContextSmem<D>::kDynBytes);
   if (e != cudaSuccess) return e;
   if ((e = launch_chained(sol::context_attn_kernel<D, kPaged, kMask>, (unsigned)std::min<long long>(items, sms), sol::kAttnThreads, sol::ContextSmem<D>::kDynBytes, st,
                           q, k, v, c)) != cudaSuccess) return e;
@@ -431,10 +446,7 @@ constexpr size_t kBookSmem = sizeof(sol::BookSmem);
 
 template <typename K>
 int launch_book(K kernel, const sol::BookArgs& b, cudaStream_t st) {
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kBookSmem) != cudaSuccess) {
-    (void)cudaGetLastError();
-    return SOL_ATTN3D_ERR_CUDA;
-  }
+  static_assert(kBookSmem <= 48 * 1024, "what a launch may have without being asked for");
   return launch_chained(kernel, 1, sol::kBookThreads, kBookSmem, st, b) == cudaSuccess ? SOL_ATTN3D_OK : SOL_ATTN3D_ERR_CUDA;
 }
 

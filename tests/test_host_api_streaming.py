@@ -65,7 +65,7 @@ def test_cache_is_checked_by_every_call():
 def test_bookkeeping_refusals():
     lib = B._lib()
     need = lib.sol_attn3d_cache_workspace_bytes(cache(), 3)
-    assert need >= 3 * 640 * 8 and lib.sol_attn3d_cache_workspace_bytes(cache(), 0) == 0 and lib.sol_attn3d_cache_workspace_bytes(cache(), 4097) == 0
+    assert need >= 3 * 640 * 8 and lib.sol_attn3d_cache_workspace_bytes(cache(), 0) == 0 and lib.sol_attn3d_cache_workspace_bytes(cache(), 2049) == 0
     fork = lambda n=3, a=64, b=64, st=None, ws=256, size=need, c=None: lib.sol_attn3d_cache_fork(c or cache(), n, a, b, st, ws, size, None)
     thin = lambda n=3, a=64, keep=64, width=10, st=None, ws=256, size=need, c=None: lib.sol_attn3d_cache_compact(c or cache(), n, a, keep, width, st, ws, size, None)
     grow = lambda n=3, a=64, b=64, st=None, c=None: lib.sol_attn3d_cache_reserve(c or cache(), n, a, b, st, None)
@@ -73,7 +73,7 @@ def test_bookkeeping_refusals():
     for f in (fork, thin, grow, close):
         assert f(n=0) == B.OK                                           # nothing to do
         assert f(n=-1) == B.ERR_INVALID_ARG and f(a=None) == B.ERR_INVALID_ARG and f(a=65) == B.ERR_INVALID_ARG and f(st=66) == B.ERR_INVALID_ARG
-        assert f(n=4097) == B.ERR_UNSUPPORTED_SHAPE
+        assert f(n=2049) == B.ERR_UNSUPPORTED_SHAPE
         assert f(c=cache(refs=None)) == B.ERR_INVALID_ARG
     for f in (fork, grow):
         assert f(b=None) == B.ERR_INVALID_ARG and f(b=66) == B.ERR_INVALID_ARG
