@@ -45,7 +45,6 @@ struct ContextParams {
   // n_whole take all of their keys and the others' keys are split.
   long long units, n_whole, n_tail;
   int n_split;
-  int lookahead;                // units that a CTA draws before it has finished with the one in work: 2 or 4
   int tok_per_tile;             // 128 / group
   unsigned int inv_group;       // ceil(2^16 / group): x / group = x * inv_group >> 16 for x < 128
   int box_rows;                 // tokens of a K/V box: a power of two that divides the page size, at most 128
@@ -70,7 +69,7 @@ struct SeqNote {
   int n, cap;                   // as in Span; n < 0: idle
   int tok0, n_tok;              // first token in the packed tensors; new tokens
 };
-constexpr int kUnitRing = 4;
+constexpr int kUnitRing = 4, kNear = 6;
 
 template <int D>
 struct ContextSmem {
@@ -83,7 +82,7 @@ struct ContextSmem {
   static constexpr int kOffKV = 2 * kTile;
   static constexpr int kOffStage = kOffKV + kStages * kTile;   // 4 KB per softmax warp
   static constexpr int kOffBars = kOffStage + 8 * 4096;
-  static constexpr int kNumBars = 2 * kStages + 4 + 6 + 2 * kUnitRing + kVRing + 1;
+  static constexpr int kNumBars = 2 * kStages + 4 + 6 + 3 * kUnitRing + kVRing + 1;
   static constexpr int kOffTmemPtr = kOffBars + kNumBars * 8;
   static constexpr int kOffUnits = (kOffTmemPtr + 16 + 15) / 16 * 16;
   static constexpr int kOffOrder = kOffUnits + kUnitRing * (int)sizeof(UnitDev);   // sequence, first item, units, parts, first part: kSortedSeqs each
@@ -143,6 +142,7 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
   auto bar_u_empty = [&](uint32_t u) { return bars + 8u * (kB + 10 + kUnitRing + (u & (kUnitRing - 1))); };
   auto bar_v_clean = [&](uint32_t n) { return bars + 8u * (kB + 10 + 2 * kUnitRing + (n & (L::kVRing - 1))); };
   const uint32_t bar_drain = bars + 8u * (kB + 10 + 2 * kUnitRing + L::kVRing);
+  auto bar_near = [&](uint32_t u) { return bars + 8u * (kB + 11 + 2 * kUnitRing + L::kVRing + (u & (kUnitRing - 1))); };
   auto round_of = [](uint32_t u) { return (u / kUnitRing) & 1u; };
   volatile uint32_t* tmem_ptr_smem = reinterpret_cast<volatile uint32_t*>(smem + L::kOffTmemPtr);
   UnitDev* units = reinterpret_cast<UnitDev*>(smem + L::kOffUnits);
@@ -161,6 +161,7 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     }
     for (int u = 0; u < kUnitRing; ++u) {
       mbar_init(bar_u_full(u), 1);
+      mbar_init(bar_near(u), 1);                           // the loads of a unit are almost through
       mbar_init(bar_u_empty(u), 11);                       // eight softmax warps, loads, issuer, cleaner
     }
     for (int n = 0; n < L::kVRing; ++n) mbar_init(bar_v_clean(n), 1);
@@ -462,9 +463,14 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         int next_page = 0;
         TileWalk<kMask> walk(un);
         if (kPaged && ok) next_page = page_of(walk.jt);
+        bool near = false;
         while (walk.more() && ok) {
           const int jt = walk.jt;
           walk.next();
+          if (!near && walk.left <= kNear) {
+            near = true;
+            if (lane == 0) mbar_arrive(bar_near(u));
+          }
           const int page = next_page;
           if (kPaged && walk.more()) next_page = page_of(walk.jt);
 #pragma unroll
@@ -492,6 +498,8 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             ++it;
           }
         }
+      } else if (lane == 0) {
+        mbar_arrive(bar_near(u));
       }
       if (!ok) break;
       release_unit(u);
@@ -739,9 +747,13 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       }
     }
     if (p.join_count != nullptr && blockIdx.x == 0 && lane == 0) *p.join_count = joins;
-    bool drawn = false;
+    bool drawn = false, behind_long = false;
     for (uint32_t u = 0;; ++u) {
-      if (u >= (uint32_t)p.lookahead && !wait_long(bar_u_empty(u - p.lookahead), round_of(u - p.lookahead))) { ok = false; break; }
+      // Behind a long unit an item is drawn when the unit's last key tiles are being loaded, not sooner: it could wait there while other
+      // CTAs have nothing left (four streams of 7 to 100 key tiles: 349 us drawn a unit ahead, a quarter of it idle).  Behind a short
+      // one it is drawn at once: looking it up must not hold it back (packed cross attention: 162 and 149 us).
+      if (behind_long && !wait_long(bar_near(u - 1), round_of(u - 1))) { ok = false; break; }
+      if (u >= (uint32_t)kUnitRing && !wait_long(bar_u_empty(u), round_of(u) ^ 1u)) { ok = false; break; }
       int last = 0;
       for (;;) {
         // the first item of a CTA is its own number; the others come from the counter
@@ -843,6 +855,7 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         }
         un.withhold = p.fault_inject == 1u && at == 0;
         if (lane == 0) units[u & (kUnitRing - 1)] = un;
+        behind_long = un.n_keys > kNear;
         break;
       }
       if (lane == 0) {

@@ -271,7 +271,7 @@ cudaError_t launch_context(const CUtensorMap& q, const CUtensorMap& k, const CUt
 }
 
 int attend_many(sol_attn3d_plan_t p, const sol::QueriesDev& a, const sol::KeysDev& d, bool paged, const ContextRoute& r, void* workspace,
-                size_t workspace_bytes, int lookahead, cudaStream_t st) {
+                size_t workspace_bytes, cudaStream_t st) {
   sol::ContextParams c{};
   c.a = a;
   c.d = d;
@@ -284,7 +284,6 @@ int attend_many(sol_attn3d_plan_t p, const sol::QueriesDev& a, const sol::KeysDe
   c.max_parts = (int)r.max_parts;
   c.tok_per_tile = r.tok_per_tile;
   c.inv_group = (65536u + r.group - 1) / r.group;
-  c.lookahead = lookahead;
   if (r.max_parts > 0) {
     if (workspace == nullptr || workspace_bytes < many_bytes(r, p->head_dim) || (reinterpret_cast<uintptr_t>(workspace) % kAlign) != 0) return SOL_ATTN3D_ERR_NO_WORKSPACE;
     c.join_count = static_cast<int*>(workspace);
@@ -356,7 +355,7 @@ int forward_context(sol_attn3d_plan_t p, const void* q, void* out, const sol::Ke
       if ((e = cudaEventRecord(p->ev[i], st)) != cudaSuccess) return fail_cuda(p, e);
   }
   const int rc = r.few ? attend_few(a, d, paged, p->head_dim, r.units, capacity, workspace, workspace_bytes, st, &p->launches, &p->last_cuda)
-                       : attend_many(p, a, d, paged, r, workspace, workspace_bytes, capacity <= 2048 ? 4 : 2, st);   // short units: looking one up must not hold the next ones back
+                       : attend_many(p, a, d, paged, r, workspace, workspace_bytes, st);
   if (rc != SOL_ATTN3D_OK) return rc;
   if (p->prof) {
     if ((e = cudaEventRecord(p->ev[3], st)) != cudaSuccess) return fail_cuda(p, e);
