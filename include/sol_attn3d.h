@@ -616,7 +616,7 @@ int sol_attn3d_cache_copy_pages(const sol_attn3d_paged_cache* cache, int n, cons
  *   pos0           DEVICE, int32 [n_seqs][3], offsets of (t, h, w) of the sequence's grid, or NULL (0).  Angles are found in fp64, so
  *                  far positions keep their phase.  Prefix tokens are not rotated.
  *   q_gain, k_gain DEVICE, fp32 [head_dim], 16-byte aligned, or NULL: not normalised.  eps >= 0, finite.
- * q_out must not alias an input.  One kernel; deterministic; may be captured.  The plan's workspace must be bound.
+ * q_out must not alias an input, nor k and v the pages that are written.  One kernel; deterministic; may be captured.  The plan's workspace must be bound.
  * Errors: INVALID_ARG, NO_WORKSPACE, UNSUPPORTED_SHAPE, CUDA.
  */
 int sol_attn3d_cache_append(sol_attn3d_plan_t plan, const void* q, const void* k, const void* v, const int64_t k_strides[2],
@@ -637,7 +637,7 @@ int sol_attn3d_cache_append(sol_attn3d_plan_t plan, const void* q, const void* k
  *   streams      as in sol_attn3d_cache_append; rows of an idle sequence are left as they were.  Several may name one stream.
  *   workspace    DEVICE, 256-byte aligned, at least sol_attn3d_paged_workspace_bytes(plan, cache) bytes, which may be 0 (then NULL is
  *                fine): results of key ranges that different CTAs handle, written and read by every call.  Calls that may overlap
- *                on the GPU need one each.
+ *                on the GPU need one each, and a plan each (the plan's own workspace counts the units of work that have been taken).
  * Rows without a valid key are zeros.  K and V of tokens that are masked, or beyond the stream's length, may be anything
  * (infinities, NaN); those of tokens that some row sees must be finite where a mask or causal_block hides them from another.
  * Deterministic; may be captured; one or two kernels.  The plan's workspace must be bound; time-outs are reported by
@@ -708,7 +708,7 @@ int sol_attn3d_cross_step(const void* q, const int64_t q_strides[2], const sol_a
  * that loads the library holds those 32 MiB until the process ends, whether this function is used or not.
  *
  *   plan           any plan with sol_attn3d_workspace_bytes(plan) <= 32 MiB (33,554,432 bytes; the few bytes that
- *                  only sol_attn3d_forward_diff uses do not count); larger plans are refused with
+ *                  only the calls for other kinds of attention use do not count); larger plans are refused with
  *                  SOL_ATTN3D_ERR_SCRATCH_LIMIT before anything is enqueued.  No workspace needs to be bound.
  *   q, k, v, out, key_mask, stream   exactly as for sol_attn3d_forward.
  *   device_status  optional DEVICE pointer to one 4-byte word (4-byte aligned) that receives the status

@@ -281,7 +281,8 @@ def _check(code: int, where: str) -> None:
 
 # ----------------------------------------------------------------- 1:1 wrappers
 class _Plan(ctypes.c_void_p):
-    """A plan's handle; `dims` (what sol_attn3d_plan_dims answers) is kept with it once asked for."""
+    """A plan's handle; `dims` (what sol_attn3d_plan_dims answers) is kept with it once asked for, `device` (where its workspace is) once
+    one is bound."""
 
 
 def sol_attn3d_plan(B: int, heads: int, head_dim: int, T: int, H: int, W: int, text_len: int,
@@ -344,6 +345,8 @@ def sol_attn3d_workspace_bytes(plan) -> int:
 def sol_attn3d_set_workspace(plan, workspace: torch.Tensor) -> None:
     _check(_lib().sol_attn3d_set_workspace(plan, workspace.data_ptr(), workspace.numel() * workspace.element_size()),
            "sol_attn3d_set_workspace")
+    if isinstance(plan, _Plan):
+        plan.device = workspace.get_device()
 
 
 def _ptr(t: Optional[torch.Tensor]):
@@ -831,6 +834,11 @@ def _check_here(device: int, *tensors) -> None:
             raise ValueError(f"tensor on {t.device}, current device is cuda:{here}")
 
 
+def _check_plan(plan, here: int) -> None:
+    if getattr(plan, "device", here) != here:
+        raise ValueError(f"the plan's workspace is on cuda:{plan.device}, current device is cuda:{here}")
+
+
 def _pool_strides(t: torch.Tensor, extents, n: int):
     """Element strides of all axes but the last; 0 (the dense value) where torch's is arbitrary (extent 0 or 1)."""
     st = t.stride()
@@ -976,6 +984,7 @@ def sol_attn3d_cache_append(plan, q: Optional[torch.Tensor], k: torch.Tensor, v:
     here = torch._C._cuda_getDevice()
     if cache.device != here:
         raise ValueError(f"the cache is on cuda:{cache.device}, current device is cuda:{here}")
+    _check_plan(plan, here)
     # (a tensor on the CPU has device -1)
     for t in (k, v, q, q_out):
         if t is not None and (t.dtype is not torch.bfloat16 or t.get_device() != here):
@@ -1009,6 +1018,8 @@ def _check_key_mask(cache: sol_attn3d_paged_cache, key_mask: Optional[torch.Tens
     if not key_mask.is_cuda or key_mask.dtype != torch.uint8 or not key_mask.is_contiguous() or key_mask.dim() != 2 or \
             key_mask.shape[0] != cache.n_streams:
         raise ValueError("key_mask must be a contiguous CUDA uint8 tensor [streams, tokens]")
+    if key_mask.shape[1] == 0:               # (its address is null, which would mean "no mask")
+        raise ValueError("key_mask has no columns")
     return key_mask.shape[1]
 
 
@@ -1027,6 +1038,7 @@ def sol_attn3d_forward_paged(plan, q: torch.Tensor, cache: sol_attn3d_paged_cach
     width = _check_key_mask(cache, key_mask)
     nbytes = _check_workspace(workspace)
     _check_here(cache.device, q, out, streams, key_mask, workspace)
+    _check_plan(plan, cache.device)
     _check(_lib().sol_attn3d_forward_paged(plan, _ptr(q), cache.ref, layer, _ptr(out), _ptr(streams), _ptr(key_mask), width, causal_block,
                                            _ptr(workspace), nbytes, _stream(stream)), "sol_attn3d_forward_paged")
 
@@ -1071,6 +1083,7 @@ def sol_attn3d_forward_cross(plan, q: torch.Tensor, context: sol_attn3d_context,
         raise ValueError(f"{n_seqs} sequences need as many contexts")
     nbytes = _check_workspace(workspace)
     _check_here(context.device, q, out, workspace)
+    _check_plan(plan, context.device)
     _check(_lib().sol_attn3d_forward_cross(plan, _ptr(q), context.ref, _ptr(out), _ptr(workspace), nbytes, _stream(stream)),
            "sol_attn3d_forward_cross")
 

@@ -447,33 +447,40 @@ __global__ void __launch_bounds__(kFewThreads, kFewResident) few_rows_kernel(con
   }
 }
 
-// Joins the parts of split keys.  Rows of partial results: D values, maximum, sum, "has a valid key".  A warp per row: its lanes look at
-// the statistics of 32 parts at once; then a lane sums 8 dims over every second (D = 128) or fourth part, with weights that come by
+// Joins the parts of split keys.  Rows of partial results: D values, maximum, sum, "has a valid key".  A warp's lanes look at the
+// statistics of 32 parts at once; then a lane sums 8 dims over every second (D = 128) or fourth part, with weights that come by
 // shuffle, so that the loads of the values do not wait for one another.  All sums are in a fixed order.
-template <int D>
-__device__ __forceinline__ void join_row(const float* mine, long long step, int n_parts, float scale_log2, __nv_bfloat16* dst) {
-  constexpr int kChunks = D / 8, kTeams = 32 / kChunks;
-  const int lane = threadIdx.x & 31, d0 = lane % kChunks * 8, team = lane / kChunks;
+__device__ __forceinline__ float largest_part(const float* stats, long long step, int n_parts, bool* any) {
   float top = -CUDART_INF_F;
-  bool any = false;
-  for (int s = lane; s < n_parts; s += 32) {
-    const float4 t = __ldg(reinterpret_cast<const float4*>(mine + s * step + D));
+  bool some = false;
+  for (int s = threadIdx.x & 31; s < n_parts; s += 32) {
+    const float4 t = __ldg(reinterpret_cast<const float4*>(stats + s * step));
     top = fmaxf(top, t.x);
-    any = any || t.z != 0.f;
+    some = some || t.z != 0.f;
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-  any = __any_sync(0xffffffffu, any);
-  float sum = 0.f, acc[8] = {};
-  for (int s0 = 0; s0 < n_parts; s0 += 32) {
+  *any = __any_sync(0xffffffffu, some);
+  return top;
+}
+
+// Parts [begin, end) of a row, weighted against `top`; every lane ends with the sum of weights and the 8 dims at (lane % (D / 8)) * 8.
+template <int D>
+__device__ __forceinline__ void sum_parts(const float* mine, long long step, int begin, int end, float top, float scale_log2, float& sum, float (&acc)[8]) {
+  constexpr int kChunks = D / 8, kTeams = 32 / kChunks;
+  const int lane = threadIdx.x & 31, d0 = lane % kChunks * 8, team = lane / kChunks;
+  sum = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) acc[e] = 0.f;
+  for (int s0 = begin; s0 < end; s0 += 32) {
     float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (s0 + lane < n_parts) t = __ldg(reinterpret_cast<const float4*>(mine + (s0 + lane) * step + D));
+    if (s0 + lane < end) t = __ldg(reinterpret_cast<const float4*>(mine + (s0 + lane) * step + D));
     const float weight = t.z == 0.f ? 0.f : t.x == top ? 1.f : ex2_approx((t.x - top) * scale_log2);
     if (t.z != 0.f) sum = fmaf(t.y, weight, sum);
     const unsigned there = __ballot_sync(0xffffffffu, t.z != 0.f);         // (what a part without a valid key holds is not looked at)
 #pragma unroll 4
     for (int j = 0; j < 32; j += kTeams) {
-      if (s0 + j >= n_parts) break;
+      if (s0 + j >= end) break;
       const float f = __shfl_sync(0xffffffffu, weight, j + team);
       if ((there >> (j + team)) & 1u) {
         const float* v = mine + (s0 + j + team) * step + d0;
@@ -490,21 +497,30 @@ __device__ __forceinline__ void join_row(const float* mine, long long step, int 
 #pragma unroll
       for (int e = 0; e < 8; ++e) acc[e] += __shfl_xor_sync(0xffffffffu, acc[e], o);
   }
-  const float inv = 1.f / sum;
-  uint4 y = make_uint4(0, 0, 0, 0);                        // no valid key: zeros
-  if (any) y = make_uint4(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv),
-                          pack_bf16x2(acc[4] * inv, acc[5] * inv), pack_bf16x2(acc[6] * inv, acc[7] * inv));
-  if (team == 0) *reinterpret_cast<uint4*>(dst + d0) = y;
 }
 
-constexpr int kJoinWarps = 8;
+// 8 dims of a joined row; zeros where there is no valid key.
+__device__ __forceinline__ void store_joined(__nv_bfloat16* dst, const float (&acc)[8], float sum, bool any) {
+  const float inv = 1.f / sum;
+  uint4 y = make_uint4(0, 0, 0, 0);
+  if (any) y = make_uint4(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv),
+                          pack_bf16x2(acc[4] * inv, acc[5] * inv), pack_bf16x2(acc[6] * inv, acc[7] * inv));
+  *reinterpret_cast<uint4*>(dst) = y;
+}
 
-// After few_rows_kernel: a CTA per unit and K/V head.
-template <int D, bool kPaged>
-__global__ void __launch_bounds__(32 * kJoinWarps) join_few_kernel(const __grid_constant__ FewArgs p) {
+constexpr int kJoinWarps = 8, kJoinFewWarps = 4;
+
+// After few_rows_kernel.  Grid: units x K/V heads, rows of a unit.  With many parts a CTA takes a row, a quarter of the parts per warp:
+// a long past has some hundred, and few rows (one stream of 111,856 keys, 15 rows x 8 K/V heads, attention and join: 167 us with
+// all rows of a unit in one CTA, 112 us so).  With few parts a warp takes a row (kWarps = 1).  960 units of 12 rows,
+// 4 parts: 500 us with a CTA per row, 484 with a warp; 192 of 5 rows, 13 parts: 111 and 115; so the line is drawn at 8.
+template <int D, bool kPaged, int kWarps>
+__global__ void __launch_bounds__(32 * kJoinFewWarps) join_few_kernel(const __grid_constant__ FewArgs p) {
+  __shared__ float part_acc[kWarps][D], part_sum[kWarps];
   chained_wait();
   chained_next();
-  const int kv_head = (int)(blockIdx.x / p.units);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int kv_head = (int)(blockIdx.x / p.units), row = blockIdx.y * (kJoinFewWarps / kWarps) + (kWarps == 1 ? warp : 0);
   const long long unit = blockIdx.x % p.units;
   int entry, n_tok, row0;
   long long tok0;
@@ -526,13 +542,33 @@ __global__ void __launch_bounds__(32 * kJoinWarps) join_few_kernel(const __grid_
     const long long stream = p.d.streams != nullptr ? p.d.streams[entry] : entry;
     if (stream < 0 || stream >= p.d.c.n_streams) return;
   }
-  const int n_rows = min(kFewRows, n_tok * p.a.group - row0);
-  const float* part = p.partial + (long long)blockIdx.x * p.n_split * kFewRows * (D + 4);
-  for (int row = threadIdx.x >> 5; row < n_rows; row += kJoinWarps) {
-    const int r = row0 + row;
-    join_row<D>(part + row * (D + 4), (long long)kFewRows * (D + 4), p.n_split, p.a.scale_log2,
-                p.a.out + (tok0 + r / p.a.group) * p.a.o_tok + ((long long)kv_head * p.a.group + r % p.a.group) * p.a.o_head);
+  if (row >= n_tok * p.a.group - row0) return;
+  const int d0 = lane % (D / 8) * 8;
+  const long long step = (long long)kFewRows * (D + 4);
+  const float* mine = p.partial + ((long long)blockIdx.x * p.n_split * kFewRows + row) * (D + 4);
+  bool any;
+  const float top = largest_part(mine + D, step, p.n_split, &any);
+  const int each = (p.n_split + kWarps - 1) / kWarps, begin = kWarps == 1 ? 0 : min(warp * each, p.n_split);
+  float sum, acc[8];
+  sum_parts<D>(mine, step, begin, min(begin + each, p.n_split), top, p.a.scale_log2, sum, acc);
+  if (kWarps > 1) {
+    if (lane < D / 8) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) part_acc[warp][d0 + e] = acc[e];
+      if (lane == 0) part_sum[warp] = sum;
+    }
+    __syncthreads();                                       // (the rows of a CTA are one: all its warps are here)
+    if (warp > 0) return;
+#pragma unroll
+    for (int w = 1; w < kWarps; ++w) {
+      sum += part_sum[w];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] += part_acc[w][d0 + e];
+    }
   }
+  if (lane >= D / 8) return;
+  const int r = row0 + row;
+  store_joined(p.a.out + (tok0 + r / p.a.group) * p.a.o_tok + ((long long)kv_head * p.a.group + r % p.a.group) * p.a.o_head + d0, acc, sum, any);
 }
 
 // After context_attn_kernel: the units whose keys it split are listed on the device.  A warp per row of one.
@@ -561,8 +597,13 @@ __global__ void __launch_bounds__(32 * kJoinWarps) join_units_kernel(const __gri
     const int row = (int)(x % p.rows_per_unit), tok = u.t0 + row / p.a.group;
     if (tok >= u.n_tok) continue;
     const long long step = (long long)p.rows_per_unit * (D + 4);
-    join_row<D>(p.partial + u.first_part * step + row * (D + 4), step, u.n_parts, p.a.scale_log2,
-                p.a.out + (u.tok0 + tok) * p.a.o_tok + ((long long)u.kv_head * p.a.group + row % p.a.group) * p.a.o_head);
+    const float* mine = p.partial + u.first_part * step + row * (D + 4);
+    bool any;
+    const float top = largest_part(mine + D, step, u.n_parts, &any);
+    float sum, acc[8];
+    sum_parts<D>(mine, step, 0, u.n_parts, top, p.a.scale_log2, sum, acc);
+    const int lane = threadIdx.x & 31, d0 = lane * 8;
+    if (lane < D / 8) store_joined(p.a.out + (u.tok0 + tok) * p.a.o_tok + ((long long)u.kv_head * p.a.group + row % p.a.group) * p.a.o_head + d0, acc, sum, any);
   }
 }
 

@@ -125,22 +125,26 @@ size_t few_bytes(long long units, int kv_heads, int head_dim, long long capacity
 }
 
 template <int D, bool kPaged>
-cudaError_t launch_few(const sol::FewArgs& f, cudaStream_t st, int* launches) {
+cudaError_t launch_few(const sol::FewArgs& f, int rows, cudaStream_t st, int* launches) {
   const unsigned items = (unsigned)(f.units * f.d.c.kv_heads);
   cudaError_t e = allow_shared_memory<&sol::few_rows_kernel<D, kPaged>>(sol::FewSmem<D>::kBytes);
   if (e != cudaSuccess) return e;
   if ((e = launch_chained(sol::few_rows_kernel<D, kPaged>, items * (unsigned)f.n_split, sol::kFewThreads, sol::FewSmem<D>::kBytes, st, f)) != cudaSuccess) return e;
   ++*launches;
   if (f.partial != nullptr) {
-    if ((e = launch_chained(sol::join_few_kernel<D, kPaged>, items, 32 * sol::kJoinWarps, 0, st, f)) != cudaSuccess) return e;
+    const bool shared = f.n_split > 8;                     // a row's parts over the CTA's warps, or a warp per row: see join_few_kernel
+    e = shared ? launch_chained(sol::join_few_kernel<D, kPaged, sol::kJoinFewWarps>, dim3(items, (unsigned)rows), 32 * sol::kJoinFewWarps, 0, st, f)
+               : launch_chained(sol::join_few_kernel<D, kPaged, 1>, dim3(items, (unsigned)(rows + sol::kJoinFewWarps - 1) / sol::kJoinFewWarps),
+                                32 * sol::kJoinFewWarps, 0, st, f);
+    if (e != cudaSuccess) return e;
     ++*launches;
   }
   return cudaSuccess;
 }
 
-// Attention of `units` units of few rows; plan or batch as in few_units.
-int attend_few(sol::QueriesDev a, const sol::KeysDev& d, bool paged, int head_dim, long long units, long long capacity, void* workspace,
-               size_t workspace_bytes, cudaStream_t st, int* launches, int* cuda_error) {
+// Attention of `units` units of few rows; plan or batch as in few_units, no sequence of more than `longest` tokens.
+int attend_few(sol::QueriesDev a, const sol::KeysDev& d, bool paged, int head_dim, long long units, long long longest, long long capacity,
+               void* workspace, size_t workspace_bytes, cudaStream_t st, int* launches, int* cuda_error) {
   sol::FewArgs f{};
   f.a = a;
   f.d = d;
@@ -153,8 +157,9 @@ int attend_few(sol::QueriesDev a, const sol::KeysDev& d, bool paged, int head_di
       return SOL_ATTN3D_ERR_NO_WORKSPACE;
     f.partial = static_cast<float*>(workspace);
   }
-  const cudaError_t e = head_dim == 128 ? (paged ? launch_few<128, true>(f, st, launches) : launch_few<128, false>(f, st, launches))
-                                        : (paged ? launch_few<64, true>(f, st, launches) : launch_few<64, false>(f, st, launches));
+  const int rows = (int)std::min<long long>(sol::kFewRows, longest * a.group);
+  const cudaError_t e = head_dim == 128 ? (paged ? launch_few<128, true>(f, rows, st, launches) : launch_few<128, false>(f, rows, st, launches))
+                                        : (paged ? launch_few<64, true>(f, rows, st, launches) : launch_few<64, false>(f, rows, st, launches));
   if (e == cudaSuccess) return SOL_ATTN3D_OK;
   *cuda_error = (int)e;
   return SOL_ATTN3D_ERR_CUDA;
@@ -164,7 +169,9 @@ int attend_few(sol::QueriesDev a, const sol::KeysDev& d, bool paged, int head_di
 constexpr size_t kUnitCounterOffset = 128;   // next unit of context_attn_kernel inside the 256-byte status block of a workspace
 
 // How a plan's rows are served for `kv_heads` K/V heads and pasts of up to `capacity` keys.  Few rows per K/V head (one unit of
-// few_rows_kernel in every sequence) go to that kernel; more to the tensor-core kernel, whose tile is 128 rows high.
+// few_rows_kernel in every sequence) go to that kernel, more to the tensor-core kernel, whose tile is 128 rows high.  Both kernels, 40 / 8
+// heads x 128: 24 streams of 200 to 11,700 keys, 15 rows each 120 and 165 us, 20 rows 175 and 166; one stream of 111,856 keys, 5 rows 98
+// and 106, 15 rows 111 and 106, 20 rows 177 and 107; 40 / 40 heads, 24 streams, 12 rows 482 and 600, 20 rows 810 and 573.
 struct ContextRoute {
   bool few;
   int group, tok_per_tile, n_split;
@@ -354,7 +361,7 @@ int forward_context(sol_attn3d_plan_t p, const void* q, void* out, const sol::Ke
     for (int i = 0; i < 3; ++i)
       if ((e = cudaEventRecord(p->ev[i], st)) != cudaSuccess) return fail_cuda(p, e);
   }
-  const int rc = r.few ? attend_few(a, d, paged, p->head_dim, r.units, capacity, workspace, workspace_bytes, st, &p->launches, &p->last_cuda)
+  const int rc = r.few ? attend_few(a, d, paged, p->head_dim, r.units, p->sched.front().n_tokens, capacity, workspace, workspace_bytes, st, &p->launches, &p->last_cuda)
                        : attend_many(p, a, d, paged, r, workspace, workspace_bytes, st);
   if (rc != SOL_ATTN3D_OK) return rc;
   if (p->prof) {
@@ -384,7 +391,7 @@ int step_context(const void* q, const int64_t q_strides[2], const sol::KeysDev& 
   a.group = heads / d.c.kv_heads;
   a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)head_dim));
   int launches = 0, cuda_error = 0;
-  return attend_few(a, d, paged, head_dim, few_units(nullptr, batch, a.group), capacity, workspace, workspace_bytes,
+  return attend_few(a, d, paged, head_dim, few_units(nullptr, batch, a.group), 1, capacity, workspace, workspace_bytes,
                     static_cast<cudaStream_t>(stream), &launches, &cuda_error);
 }
 

@@ -321,3 +321,56 @@ def test_many_streams_with_split_keys():
 def test_more_heads_per_key_head_than_a_tile_has_rows(heads, kv):
     c = Cache([500, 90], 32, kv, 64, seed=1)
     check_chunk([(20, 0, 1, 1), (1, 0, 1, 1)], None, c, heads, 1)
+
+
+@pytest.mark.parametrize("heads,kv,d", [(15, 1, 128), (5, 1, 64), (40, 2, 128)])
+@pytest.mark.parametrize("longest", [900, 12000])
+def test_step_joins_few_and_many_parts(heads, kv, d, longest):
+    """Few parts are joined by a warp per row, many by four: idle and empty streams, one without a valid key, units of 16 and of 4 rows."""
+    from paper_2609_35110_b200 import binding as B
+    lens = [longest, 0, longest // 3, 700, 1]
+    c = Cache(lens, 64, kv, d, seed=heads)
+    g = torch.Generator().manual_seed(8)
+    mask = (torch.rand(5, longest, generator=g) < 0.7).to(torch.uint8)
+    mask[3] = 0
+    mask[4] = 1
+    streams = [2, 1, 9, 0, 3, 4]
+    q = torch.randn(len(streams), heads, d, generator=g).bfloat16()
+    out = torch.full((len(streams), heads, d), 7.0, dtype=torch.bfloat16, device="cuda")
+    nbytes = B.sol_attn3d_paged_step_workspace_bytes(c.cache, len(streams), heads)
+    units = len(streams) * -(-heads // kv // 16) * kv
+    assert (nbytes > units * 8 * 16 * (d + 4) * 4 + 256) == (longest > 900)          # more than 8 parts, or not
+    B.sol_attn3d_paged_step(q.cuda(), c.cache, c.layer, out, streams=torch.tensor(streams, dtype=torch.int32, device="cuda"), key_mask=mask.cuda(),
+                            workspace=torch.full((nbytes,), 255, dtype=torch.uint8, device="cuda"))
+    out = out.cpu()
+    for b, s in enumerate(streams):
+        if s >= len(lens):
+            assert bool((out[b] == 7.0).all())
+            continue
+        ref, mag = so.attend(q[b:b + 1], c.k[s], c.v[s], so.key_limits(1, lens[s], 0), mask[s, :lens[s]].bool())
+        close(out[b:b + 1], ref, mag)
+
+
+def test_the_binding_refuses_masks_without_columns_and_plans_from_elsewhere():
+    from paper_2609_35110_b200 import binding as B
+    c = Cache([40], 16, 2, 64, seed=0)
+    q = torch.zeros(3, 2, 64, dtype=torch.bfloat16, device="cuda")
+    out = torch.full_like(q, 7.0)
+    nothing = torch.zeros(1, 0, dtype=torch.uint8, device="cuda")
+    attn = B.Attn3d([(3, 0, 1, 1)], 2, 64, rope(64))
+    with pytest.raises(ValueError):
+        B.sol_attn3d_forward_paged(attn.plan, q, c.cache, 0, out, key_mask=nothing)
+    with pytest.raises(ValueError):
+        B.sol_attn3d_paged_step(q[:1], c.cache, 0, out[:1], key_mask=nothing)
+    one = torch.tensor([0], dtype=torch.int32, device="cuda")
+    x = torch.zeros(40, 2, 64, dtype=torch.bfloat16, device="cuda")
+    context = B.sol_attn3d_context(x, x, one, one, 1)
+    kv = torch.zeros(3, 2, 64, dtype=torch.bfloat16, device="cuda")
+    assert attn.plan.device == torch.cuda.current_device()
+    attn.plan.device += 1                                               # as if its workspace had been bound there
+    for call in (lambda: B.sol_attn3d_forward_paged(attn.plan, q, c.cache, 0, out), lambda: B.sol_attn3d_forward_cross(attn.plan, q, context, out),
+                 lambda: B.sol_attn3d_cache_append(attn.plan, None, kv, kv, None, c.cache, 0)):
+        with pytest.raises(ValueError):
+            call()
+    torch.cuda.synchronize()
+    assert bool((out == 7.0).all())
