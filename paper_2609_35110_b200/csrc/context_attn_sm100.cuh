@@ -4,18 +4,24 @@
 //
 // A tile is 128 (token, head) rows of one K/V head: 128 / group tokens x the group's heads, head fastest, which one TMA box brings
 // side by side; so grouped heads share every K and V tile.  A unit is two such tiles, one K/V head and a range of key tiles (all of
-// them, or a part when there are few units; the parts are joined by join_rows_kernel).
+// them, or a part when there are few units; the parts are joined by join_units_kernel).
 //
 // CTAs are persistent, one per SM, and take units from a counter, so that short contexts do not pay for a CTA's start (tensor
 // memory, barriers, the first loads) and its last stores per unit, and streams of different length even out.  A warp looks the
 // next unit up while the present one is computed: its Q, K and V are on their way, and its first scores are computed, while the
 // softmax warps still write the last one's rows.
 //   warps 0-3, 4-7  softmax and epilogue of tile 0, tile 1 (thread = row)
-//   warp 8          loads: Q by one box per tile half; K and V pages by one box per page part, a lane each
+//   warp 8          loads: Q by one box per tile half; K and V pages by one box per page part and half, a lane each
 //   warp 9          tcgen05.mma issuer
 //   warp 10         takes units
 //   warp 11         values of keys that do not count become zeros in shared memory (0 * NaN would not be 0)
 // Tensor memory: S0 | S1 | O0 | O1 as in attn_fwd_sm100.cuh.
+//
+// What bounds it is the chain scores -> softmax -> P -> product of two tiles in turn: 3,650 cycles per 128 keys, as in the dense kernel;
+// the tensor pipe works 40 to 55 % of that, the exponentials as much.  4,680 rows x 40 heads x 128 over 25,216 keys: 2.0 ms (1.2
+// PFLOP/s) in a short run, 2.3 in a long one (1 kW); 60 tokens x 40 / 8 heads over 111,856 keys: 213 to 235 us; 25,216 rows x 40 heads over 512
+// states: 280 to 330 us, of which 5,800 cycles per unit and four key tiles are its start and end.  No gain: packed pairs of fp32
+// operations, a polynomial for an eighth to a third of the exponentials (2 to 5 % slower), one MMA issuer per tile (a quarter slower).
 #pragma once
 #include "attn_fwd_sm100.cuh"
 #include "context_attn.cuh"
