@@ -124,10 +124,12 @@ __device__ __forceinline__ uint32_t below(int limit, int first) {
   return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u;
 }
 
-template <int D, bool kPaged, bool kMask>
+// kBoxes: rows are written by TMA boxes; for contexts, where 32 is a multiple of the heads per K/V head.  (Short contexts have many
+// epilogues; in the masked paged kernel the registers for it cost more than it gave: four streams by frames 324 and 336 us.)
+template <int D, bool kPaged, bool kMask, bool kBoxes>
 __global__ void __launch_bounds__(kAttnThreads, 1)
 context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
-                    const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ ContextParams p) {
+                    const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_o, const __grid_constant__ ContextParams p) {
   using L = ContextSmem<D>;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw_addr = smem_u32(smem_raw);
@@ -176,6 +178,7 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     prefetch_tensormap(&tm_q);
     prefetch_tensormap(&tm_k);
     prefetch_tensormap(&tm_v);
+    if (kBoxes) prefetch_tensormap(&tm_o);
   }
   if (threadIdx.x == 0) tmem_ptr_smem[1] = *reinterpret_cast<volatile unsigned int*>(p.status);
   if (warp == 9) {
@@ -379,20 +382,25 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         }
         if (mine) *reinterpret_cast<float4*>(dst + D) = make_float4(m_ref, l, seen ? 1.f : 0.f, 0.f);
       } else {
-        // Rows are staged 64 columns at a time (16-byte chunks XOR-swizzled by row) and written with eight lanes per row, four rows
-        // at a time; a lane's eight places are found first, so that its stores follow one another.
+        // Rows are staged 64 columns at a time (16-byte chunks XOR-swizzled by row) and written by one box (kBoxes) where a warp's rows
+        // are whole tokens of the sequence, otherwise with eight lanes per row, four rows at a time; a lane's eight places are found first, so
+        // that its stores follow one another.  (25,216 rows x 40 heads over 512 states: 284 us with lanes' stores, 272 with boxes.)
         const float inv = 1.0f / l;
         uint8_t* stage = smem + L::kOffStage + warp * 4096;
         int own = lane;
         asm volatile("" : "+r"(own));                      // keeps what follows from it out of the registers of the main loop
         const int first_tok = un.t0 + t * p.tok_per_tile, left = un.n_tok - first_tok, ch = own & 7;
         __nv_bfloat16* base = p.a.out + (un.tok0 + first_tok) * p.a.o_tok + (long long)(un.kv_head * group) * p.a.o_head + ch * 8;
+        const int warp_tok = (int)(wq * 32 * p.inv_group >> 16);           // where a warp's rows are whole tokens: its first
+        const bool boxed = kBoxes && warp_tok + (int)(32 * p.inv_group >> 16) <= left;
         __nv_bfloat16* place[8];
+        if (!boxed) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int tile_row = wq * 32 + 4 * e + (own >> 3);
-          const int in_tile = (int)(tile_row * p.inv_group >> 16);         // token of the tile
-          place[e] = tile_row < tile_rows && in_tile < left ? base + in_tile * p.a.o_tok + (tile_row - in_tile * group) * p.a.o_head : nullptr;
+          for (int e = 0; e < 8; ++e) {
+            const int tile_row = wq * 32 + 4 * e + (own >> 3);
+            const int in_tile = (int)(tile_row * p.inv_group >> 16);       // token of the tile
+            place[e] = tile_row < tile_rows && in_tile < left ? base + in_tile * p.a.o_tok + (tile_row - in_tile * group) * p.a.o_head : nullptr;
+          }
         }
         const uint64_t pol_once = l2_policy_evict_first();
 #pragma unroll 1
@@ -401,6 +409,7 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
           tmem_ld32(tO + hf * 64, *reinterpret_cast<uint32_t(*)[32]>(&o[0]));
           tmem_ld32(tO + hf * 64 + 32, *reinterpret_cast<uint32_t(*)[32]>(&o[32]));
           tmem_wait_ld_dep64(o);
+          if (kBoxes && lane == 0) bulk_wait_read();      // the last box has left the staging rows
           __syncwarp();
 #pragma unroll
           for (int v = 0; v < 8; ++v) {
@@ -412,6 +421,15 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
               w.w = pack_bf16x2(__uint_as_float(o[8 * v + 6]) * inv, __uint_as_float(o[8 * v + 7]) * inv);
             }
             *reinterpret_cast<uint4*>(stage + own * 128 + ((v ^ ch) << 4)) = w;
+          }
+          if (boxed) {
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+              tma_store_3d_hint(&tm_o, sbase + L::kOffStage + warp * 4096, hf * 64, un.kv_head * group, (int)un.tok0 + first_tok + warp_tok, pol_once);
+              bulk_commit();
+            }
+            continue;
           }
           __syncwarp();
           uint4 w[8];
@@ -427,6 +445,7 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       }
       release_unit(u);
     }
+    if (kBoxes && lane == 0) bulk_wait();
     if (!ok && lane == 0) atomicCAS(p.status, 0u, kStatusTimeoutSoftmax);
   } else {
     setmaxnreg_dec<SOL_REGS_OTHER>();

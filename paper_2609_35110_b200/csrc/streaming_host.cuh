@@ -255,13 +255,13 @@ int encode_boxes(sol_attn3d_plan_t p, CUtensorMap* tm, const void* base, int ran
   return SOL_ATTN3D_ERR_CUDA;
 }
 
-template <int D, bool kPaged, bool kMask>
-cudaError_t launch_context_as(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const sol::ContextParams& c, long long items, int sms, cudaStream_t st,
-                             int* launches) {
-  cudaError_t e = allow_shared_memory<&sol::context_attn_kernel<D, kPaged, kMask>>(sol::ContextSmem<D>::kDynBytes);
+template <int D, bool kPaged, bool kMask, bool kBoxes>
+cudaError_t launch_context_as(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const CUtensorMap& o, const sol::ContextParams& c, long long items,
+                             int sms, cudaStream_t st, int* launches) {
+  cudaError_t e = allow_shared_memory<&sol::context_attn_kernel<D, kPaged, kMask, kBoxes>>(sol::ContextSmem<D>::kDynBytes);
   if (e != cudaSuccess) return e;
-  if ((e = launch_chained(sol::context_attn_kernel<D, kPaged, kMask>, (unsigned)std::min<long long>(items, sms), sol::kAttnThreads, sol::ContextSmem<D>::kDynBytes, st,
-                          q, k, v, c)) != cudaSuccess) return e;
+  if ((e = launch_chained(sol::context_attn_kernel<D, kPaged, kMask, kBoxes>, (unsigned)std::min<long long>(items, sms), sol::kAttnThreads, sol::ContextSmem<D>::kDynBytes, st,
+                          q, k, v, o, c)) != cudaSuccess) return e;
   ++*launches;
   if (c.partial != nullptr) {
     const sol::JoinArgs j{c.a, 2 * c.tok_per_tile * c.a.group, c.partial, c.join, c.join_count};
@@ -272,9 +272,14 @@ cudaError_t launch_context_as(const CUtensorMap& q, const CUtensorMap& k, const 
 }
 
 template <int D, bool kPaged>
-cudaError_t launch_context(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const sol::ContextParams& c, long long items, int sms, cudaStream_t st, int* launches) {
-  return c.d.mask != nullptr ? launch_context_as<D, kPaged, true>(q, k, v, c, items, sms, st, launches)
-                             : launch_context_as<D, kPaged, false>(q, k, v, c, items, sms, st, launches);
+cudaError_t launch_context(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const CUtensorMap& o, const sol::ContextParams& c, long long items, int sms,
+                           cudaStream_t st, int* launches) {
+  if constexpr (!kPaged)
+    if (32 % c.a.group == 0)                               // a warp's 32 rows are whole tokens: a box of o
+      return c.d.mask != nullptr ? launch_context_as<D, false, true, true>(q, k, v, o, c, items, sms, st, launches)
+                                 : launch_context_as<D, false, false, true>(q, k, v, o, c, items, sms, st, launches);
+  return c.d.mask != nullptr ? launch_context_as<D, kPaged, true, false>(q, k, v, o, c, items, sms, st, launches)
+                             : launch_context_as<D, kPaged, false, false>(q, k, v, o, c, items, sms, st, launches);
 }
 
 int attend_many(sol_attn3d_plan_t p, const sol::QueriesDev& a, const sol::KeysDev& d, bool paged, const ContextRoute& r, void* workspace,
@@ -304,10 +309,16 @@ int attend_many(sol_attn3d_plan_t p, const sol::QueriesDev& a, const sol::KeysDe
   c.fault_inject = p->fault_inject;
   c.v_lbo = p->v_lbo;
   c.v_sbo = p->v_sbo;
-  CUtensorMap tm_q, tm_k, tm_v;
+  CUtensorMap tm_q, tm_k, tm_v, tm_o;
   const long long q_dims[3] = {p->head_dim, p->heads, p->total_tokens}, q_strides[2] = {a.q_head, a.q_tok};
   const int q_box[3] = {64, r.group, r.tok_per_tile};
   int rc = encode_boxes(p, &tm_q, a.q, 3, q_dims, q_strides, q_box);
+  tm_o = tm_q;                                             // (not looked at, unless rows are written by boxes)
+  if (rc == SOL_ATTN3D_OK && !paged && 32 % r.group == 0) {
+    const long long o_strides[2] = {a.o_head, a.o_tok};
+    const int o_box[3] = {64, r.group, 32 / r.group};
+    rc = encode_boxes(p, &tm_o, a.out, 3, q_dims, o_strides, o_box);
+  }
   for (int kv = 0; kv < 2 && rc == SOL_ATTN3D_OK; ++kv) {
     CUtensorMap* tm = kv ? &tm_v : &tm_k;
     const void* base = kv ? d.c.v : d.c.k;
@@ -326,10 +337,10 @@ int attend_many(sol_attn3d_plan_t p, const sol::QueriesDev& a, const sol::KeysDe
     }
   }
   if (rc != SOL_ATTN3D_OK) return rc;
-  const cudaError_t e = p->head_dim == 128 ? (paged ? launch_context<128, true>(tm_q, tm_k, tm_v, c, items, p->sm_count, st, &p->launches)
-                                                    : launch_context<128, false>(tm_q, tm_k, tm_v, c, items, p->sm_count, st, &p->launches))
-                                           : (paged ? launch_context<64, true>(tm_q, tm_k, tm_v, c, items, p->sm_count, st, &p->launches)
-                                                    : launch_context<64, false>(tm_q, tm_k, tm_v, c, items, p->sm_count, st, &p->launches));
+  const cudaError_t e = p->head_dim == 128 ? (paged ? launch_context<128, true>(tm_q, tm_k, tm_v, tm_o, c, items, p->sm_count, st, &p->launches)
+                                                    : launch_context<128, false>(tm_q, tm_k, tm_v, tm_o, c, items, p->sm_count, st, &p->launches))
+                                           : (paged ? launch_context<64, true>(tm_q, tm_k, tm_v, tm_o, c, items, p->sm_count, st, &p->launches)
+                                                    : launch_context<64, false>(tm_q, tm_k, tm_v, tm_o, c, items, p->sm_count, st, &p->launches));
   return e == cudaSuccess ? SOL_ATTN3D_OK : fail_cuda(p, e);
 }
 

@@ -195,3 +195,35 @@ def test_many_sequences_with_split_keys(masked):
             ref, mag = so.attend(q[at:at + m], kv_t[b:b + n, 0], kv_t[b:b + n, 1], so.key_limits(m, n, 0), None if mask is None else mask[b:b + n].bool())
             close(out[at:at + m].cpu(), ref, mag)
             at += m
+
+
+@pytest.mark.parametrize("heads,kv", [(2, 2), (4, 2), (8, 1), (32, 1), (12, 2)])
+@pytest.mark.parametrize("d,masked", [(64, True), (128, False), (128, True)])
+@pytest.mark.parametrize("head_major", [False, True])
+def test_whole_and_cut_tiles_at_output_strides(heads, kv, d, masked, head_major):
+    """Warps whose rows are whole tokens of their sequence, and warps that a sequence's end cuts; what lies between rows stays."""
+    from paper_2609_35110_b200 import binding as B
+    sizes, lens = [300, 31, 1, 97, 64], [300, 0, 140, 1, 513]
+    total = sum(sizes)
+    kv_t, begins = contexts(lens, kv, d, seed=heads)
+    g = torch.Generator().manual_seed(4)
+    mask = (torch.rand(kv_t.shape[0], generator=g) < 0.7).to(torch.uint8) if masked else None
+    dev = kv_t.cuda()
+    ctx = B.sol_attn3d_context(dev[:, 0], dev[:, 1], ints(begins), ints(lens), 513, key_mask=None if mask is None else mask.cuda())
+    q = torch.randn(total, heads, d, generator=g).bfloat16()
+    shape = (heads + 1, total + 5, d + 8) if head_major else (total + 5, heads + 1, d + 8)
+    buf = torch.full(shape, 7.0, dtype=torch.bfloat16, device="cuda")
+    out = (buf.transpose(0, 1) if head_major else buf)[2:2 + total, 1:, :d]
+    st = out.stride()
+    attn = B.Attn3d([(n, 0, 1, 1) for n in sizes], heads, d, rope(d), out_strides=st[:2])
+    ws = torch.empty(B.sol_attn3d_cross_workspace_bytes(attn.plan, ctx), dtype=torch.uint8, device="cuda")
+    B.sol_attn3d_forward_cross(attn.plan, q.cuda(), ctx, out, workspace=ws)
+    torch.cuda.synchronize()
+    assert attn.status() == 0
+    at, got = 0, out.cpu()
+    for m, b, n in zip(sizes, begins, lens):
+        ref, mag = so.attend(q[at:at + m], kv_t[b:b + n, 0], kv_t[b:b + n, 1], so.key_limits(m, n, 0), None if mask is None else mask[b:b + n].bool())
+        close(got[at:at + m], ref, mag)
+        at += m
+    out.fill_(7.0)
+    assert bool((buf == 7.0).all())
