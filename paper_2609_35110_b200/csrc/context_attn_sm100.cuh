@@ -19,8 +19,8 @@
 //
 // What bounds it is the chain scores -> softmax -> P -> product of two tiles in turn: 3,650 cycles per 128 keys, as in the dense kernel;
 // the tensor pipe works 40 to 55 % of that, the exponentials as much.  4,680 rows x 40 heads x 128 over 25,216 keys: 2.0 ms (1.2
-// PFLOP/s) in a short run, 2.3 in a long one (1 kW); 60 tokens x 40 / 8 heads over 111,856 keys: 213 to 235 us; 25,216 rows x 40 heads over 512
-// states: 280 to 330 us, of which 5,800 cycles per unit and four key tiles are its start and end.  No gain: packed pairs of fp32
+// PFLOP/s) in a short run, 2.3 in a long one (1 kW); 60 tokens x 40 / 8 heads over 111,856 keys: 209 to 230 us; 25,216 rows x 40 heads over 512
+// states: 271 to 314 us, of which some 5,000 cycles per unit and four key tiles are its start and end.  No gain: packed pairs of fp32
 // operations, a polynomial for an eighth to a third of the exponentials (2 to 5 % slower), one MMA issuer per tile (a quarter slower).
 #pragma once
 #include "attn_fwd_sm100.cuh"
