@@ -591,12 +591,14 @@ struct JoinArgs {
   const float* partial;
   const JoinUnit* list;
   const int* count;
+  const unsigned int* status;   // not zero: a wait ran out, now or earlier, and list and count may never have been written
 };
 
 template <int D>
 __global__ void __launch_bounds__(32 * kJoinWarps) join_units_kernel(const __grid_constant__ JoinArgs p) {
   chained_wait();
   chained_next();
+  if (*p.status != 0) return;
   const long long all = (long long)*p.count * p.rows_per_unit;
   for (long long x = (long long)blockIdx.x * kJoinWarps + (threadIdx.x >> 5); x < all; x += (long long)gridDim.x * kJoinWarps) {
     const JoinUnit u = p.list[x / p.rows_per_unit];

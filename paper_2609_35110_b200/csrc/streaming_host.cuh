@@ -264,7 +264,7 @@ cudaError_t launch_context_as(const CUtensorMap& q, const CUtensorMap& k, const 
                           q, k, v, o, c)) != cudaSuccess) return e;
   ++*launches;
   if (c.partial != nullptr) {
-    const sol::JoinArgs j{c.a, 2 * c.tok_per_tile * c.a.group, c.partial, c.join, c.join_count};
+    const sol::JoinArgs j{c.a, 2 * c.tok_per_tile * c.a.group, c.partial, c.join, c.join_count, c.status};
     if ((e = launch_chained(sol::join_units_kernel<D>, 4 * sol::kPlanSms, 32 * sol::kJoinWarps, 0, st, j)) != cudaSuccess) return e;
     ++*launches;
   }
