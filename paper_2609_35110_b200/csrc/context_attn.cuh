@@ -598,8 +598,9 @@ template <int D>
 __global__ void __launch_bounds__(32 * kJoinWarps) join_units_kernel(const __grid_constant__ JoinArgs p) {
   chained_wait();
   chained_next();
-  if (*p.status != 0) return;
-  const long long all = (long long)*p.count * p.rows_per_unit;
+  const int count = *p.count;
+  if (count <= 0 || *p.status != 0) return;
+  const long long all = (long long)count * p.rows_per_unit;
   for (long long x = (long long)blockIdx.x * kJoinWarps + (threadIdx.x >> 5); x < all; x += (long long)gridDim.x * kJoinWarps) {
     const JoinUnit u = p.list[x / p.rows_per_unit];
     const int row = (int)(x % p.rows_per_unit), tok = u.t0 + row / p.a.group;
