@@ -71,7 +71,7 @@ __global__ void __launch_bounds__(256, 3) cache_append_kernel(const __grid_const
   constexpr int kBatch = 4, kChunks = D / 8;
   __shared__ __align__(16) float2 angle[kTokens][D / 2];
   __shared__ __nv_bfloat16* place[3][kTokens];             // where a token's first Q, K and V head go; nullptr: nowhere
-  __shared__ int found[kTokens], rotates[kTokens];
+  __shared__ int found[kTokens], rotates[kTokens], home[kTokens];          // home: the token's stream, or -1: of an idle sequence
   const int rows_per_pass = blockDim.x / kChunks;
   const int chunk = threadIdx.x % kChunks, sub = threadIdx.x / kChunks;
   const unsigned lanes = __activemask();
@@ -91,8 +91,31 @@ __global__ void __launch_bounds__(256, 3) cache_append_kernel(const __grid_const
 
   for (long long tok0 = (long long)blockIdx.x * kTokens; tok0 < a.total_tokens; tok0 += (long long)gridDim.x * kTokens) {
     const int n_tok = (int)min((long long)kTokens, a.total_tokens - tok0);
+    // ---- the tokens' sequences and streams; an idle sequence's rows are not read
+    const int my_tok = threadIdx.x % kTokens;
+    if (my_tok < n_tok)
+      for (int s = threadIdx.x / kTokens; s < a.n_seqs; s += blockDim.x / kTokens) {
+        const SeqDev& sq = a.seqs[s];
+        if (tok0 + my_tok >= sq.tok_start && tok0 + my_tok < sq.tok_start + sq.n_tokens) {
+          const long long stream = a.streams != nullptr ? a.streams[sq.seq_id] : sq.seq_id;
+          found[my_tok] = s;
+          home[my_tok] = stream >= 0 && stream < a.c.n_streams ? (int)stream : -1;
+        }
+      }
+    __syncthreads();
+    unsigned pick = 0;                                     // a byte per token: itself, or where it is not there or idle the first that is not
+    int live = -1;
+#pragma unroll
+    for (int g = kTokens - 1; g >= 0; --g)
+      if (g < n_tok && home[g] >= 0) live = g;
+    if (live < 0) {
+      __syncthreads();                                     // (homes have been read)
+      continue;
+    }
+#pragma unroll
+    for (int g = 0; g < kTokens; ++g) pick |= (unsigned)(g < n_tok && home[g] >= 0 ? g : live) << (8 * g);
     uint4 ahead[kBatch];
-    auto load = [&](int it) {                              // (past the end: the last head or token again, not stored)
+    auto load = [&](int it) {                              // (past the last head: that one again, not stored)
       int which, n, h0;
       step_of(it, which, n, h0);
       const long long x_tok = a.x_tok[which];
@@ -101,15 +124,11 @@ __global__ void __launch_bounds__(256, 3) cache_append_kernel(const __grid_const
 #pragma unroll
       for (int b = 0; b < kBatch; ++b) {
         const int h = min(h0 + b / kTokens * rows_per_pass, n - 1);
-        ahead[b] = __ldg(reinterpret_cast<const uint4*>(src + min(b % kTokens, n_tok - 1) * x_tok + (long long)h * x_head));
+        ahead[b] = __ldg(reinterpret_cast<const uint4*>(src + (int)((pick >> (8 * (b % kTokens))) & 255u) * x_tok + (long long)h * x_head));
       }
     };
     load(0);
-    // ---- the tokens' sequences, places and angles
-    for (int g = 0; g < n_tok; ++g)
-      for (int s = threadIdx.x; s < a.n_seqs; s += blockDim.x)
-        if (tok0 + g >= a.seqs[s].tok_start && tok0 + g < a.seqs[s].tok_start + a.seqs[s].n_tokens) found[g] = s;
-    __syncthreads();
+    // ---- their angles and places
     for (int j = threadIdx.x; j < n_tok * (D / 2); j += blockDim.x) {
       const int g = j / (D / 2), pair = j % (D / 2);
       const SeqDev& sq = a.seqs[found[g]];
@@ -135,7 +154,7 @@ __global__ void __launch_bounds__(256, 3) cache_append_kernel(const __grid_const
       const int lane = threadIdx.x & 31;
       for (int g = 0; g < n_tok; ++g) {
         const SeqDev& sq = a.seqs[found[g]];
-        const long long stream = a.streams != nullptr ? a.streams[sq.seq_id] : sq.seq_id;
+        const long long stream = home[g];
         // Of several sequences with one stream the first counts: they would write the same rows.
         bool again = false;
         if (a.streams != nullptr)
@@ -143,7 +162,7 @@ __global__ void __launch_bounds__(256, 3) cache_append_kernel(const __grid_const
         again = __any_sync(0xffffffffu, again);
         if (lane == 0) {
           place[0][g] = place[1][g] = place[2][g] = nullptr;
-          if (stream >= 0 && stream < a.c.n_streams) {     // (otherwise an idle sequence)
+          if (stream >= 0) {                               // (otherwise an idle sequence)
             place[0][g] = a.q_out + (tok0 + g) * a.g.heads * (long long)D;
             const long long at = stream_tokens(a.c, stream) - sq.n_tokens + (tok0 + g - sq.tok_start);
             if (at >= 0 && !again) {
