@@ -76,6 +76,7 @@ __global__ void __launch_bounds__(256, 3) cache_append_kernel(const __grid_const
   const int chunk = threadIdx.x % kChunks, sub = threadIdx.x / kChunks;
   const unsigned lanes = __activemask();
   const int d1 = a.g.rope[0], d2 = d1 + a.g.rope[1], d3 = d2 + a.g.rope[2];
+  const int turned = max(0, min(4, (d3 >> 1) - 4 * chunk));  // pairs of this thread's chunk that rotate; the rest pass as they are, infinities too
   // Step: a tensor and a batch of its heads.
   constexpr int kHeads = kBatch / kTokens;
   const int head_step = kHeads * rows_per_pass;
@@ -250,16 +251,20 @@ __global__ void __launch_bounds__(256, 3) cache_append_kernel(const __grid_const
 #pragma unroll
             for (int e = 0; e < 8; ++e) f[e] *= rinv[b] * gains[e];
           }
-          if (rotates[b % kTokens] != 0) {
+          if (rotates[b % kTokens] != 0 && turned > 0) {
             const float4* cs = reinterpret_cast<const float4*>(&angle[b % kTokens][chunk * 4]);
 #pragma unroll
             for (int u = 0; u < 2; ++u) {                  // two pairs: cos, sin, cos, sin
               const float4 t = cs[u];
               const float e0 = f[4 * u], o0 = f[4 * u + 1], e1 = f[4 * u + 2], o1 = f[4 * u + 3];
-              f[4 * u] = fmaf(e0, t.x, -(o0 * t.y));
-              f[4 * u + 1] = fmaf(e0, t.y, o0 * t.x);
-              f[4 * u + 2] = fmaf(e1, t.z, -(o1 * t.w));
-              f[4 * u + 3] = fmaf(e1, t.w, o1 * t.z);
+              if (2 * u < turned) {
+                f[4 * u] = fmaf(e0, t.x, -(o0 * t.y));
+                f[4 * u + 1] = fmaf(e0, t.y, o0 * t.x);
+              }
+              if (2 * u + 1 < turned) {
+                f[4 * u + 2] = fmaf(e1, t.z, -(o1 * t.w));
+                f[4 * u + 3] = fmaf(e1, t.w, o1 * t.z);
+              }
             }
           }
           y = make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
