@@ -282,7 +282,7 @@ def _check(code: int, where: str) -> None:
 # ----------------------------------------------------------------- 1:1 wrappers
 class _Plan(ctypes.c_void_p):
     """A plan's handle; `dims` (what sol_attn3d_plan_dims answers) is kept with it once asked for, `device` (where its workspace is) once
-    one is bound."""
+    one is bound, `strides` (element strides of q and of out) from the start."""
 
 
 def sol_attn3d_plan(B: int, heads: int, head_dim: int, T: int, H: int, W: int, text_len: int,
@@ -290,6 +290,7 @@ def sol_attn3d_plan(B: int, heads: int, head_dim: int, T: int, H: int, W: int, t
     h = _Plan()
     rd = (ctypes.c_int * 3)(*[int(x) for x in rope_dims])
     _check(_lib().sol_attn3d_plan(ctypes.byref(h), B, heads, head_dim, T, H, W, text_len, rd), "sol_attn3d_plan")
+    h.strides = dict.fromkeys(("q", "out"), (heads * head_dim, head_dim, 1))
     return h
 
 
@@ -318,6 +319,7 @@ def sol_attn3d_plan_ex(seqs: Sequence[Tuple[int, int, int, int]], heads: int, he
         arr[0], arr[1] = int(val[0]), int(val[1])
     h = _Plan()
     _check(_lib().sol_attn3d_plan_ex(ctypes.byref(h), ctypes.byref(d)), "sol_attn3d_plan_ex")
+    h.strides = {name: (int(val[0]) or heads * head_dim, int(val[1]) or head_dim, 1) for name, val in (("q", q_strides), ("out", out_strides))}
     return h
 
 
@@ -834,6 +836,26 @@ def _check_here(device: int, *tensors) -> None:
             raise ValueError(f"tensor on {t.device}, current device is cuda:{here}")
 
 
+_NO_STRIDES = dict.fromkeys(("q", "out"))
+
+
+def _check_strides(plan, name: str, t: torch.Tensor, heads: int, head_dim: int) -> None:
+    """The kernels take q and out by the plan's strides.  A tensor of the shape [tokens, heads, head_dim], or [tokens, heads * head_dim], has to
+    have them; any other is memory that the plan's strides lead through."""
+    want, st = getattr(plan, "strides", None), t.stride()
+    if want is None or st == want[name]:
+        return
+    (tok, head, _), shape = want[name], t.shape
+    if len(shape) == 3 and shape[1] == heads and shape[2] == head_dim:
+        same = st[2] == 1 and (heads == 1 or st[1] == head)
+    elif len(shape) == 2 and shape[1] == heads * head_dim:
+        same = st[1] == 1 and (heads == 1 or head == head_dim)
+    else:
+        return
+    if not same or (shape[0] > 1 and st[0] != tok):
+        raise ValueError(f"{name}: strides {st}, but the plan was made for {want[name]}")
+
+
 def _check_plan(plan, here: int) -> None:
     if getattr(plan, "device", here) != here:
         raise ValueError(f"the plan's workspace is on cuda:{plan.device}, current device is cuda:{here}")
@@ -980,11 +1002,12 @@ def sol_attn3d_cache_append(plan, q: Optional[torch.Tensor], k: torch.Tensor, v:
                             pos0: Optional[torch.Tensor] = None, q_gain: Optional[torch.Tensor] = None, k_gain: Optional[torch.Tensor] = None,
                             eps: float = 0.0, stream=None) -> None:
     """Norm and rotation of new tokens; K and V go to the last tokens of their streams, Q to q_out."""
-    n_seqs, heads, head_dim, tokens = _dims(plan)
+    n_seqs, heads, head_dim, tokens = getattr(plan, "dims", None) or _dims(plan)
     here = torch._C._cuda_getDevice()
     if cache.device != here:
         raise ValueError(f"the cache is on cuda:{cache.device}, current device is cuda:{here}")
-    _check_plan(plan, here)
+    if getattr(plan, "device", here) != here:
+        _check_plan(plan, here)
     # (a tensor on the CPU has device -1)
     for t in (k, v, q, q_out):
         if t is not None and (t.dtype is not torch.bfloat16 or t.get_device() != here):
@@ -992,6 +1015,8 @@ def sol_attn3d_cache_append(plan, q: Optional[torch.Tensor], k: torch.Tensor, v:
     for t in (q, q_out):
         if t is not None and t.numel() < tokens * heads * head_dim:
             raise ValueError(f"q, q_out: the plan has {tokens} tokens of {heads * head_dim} values")
+    if q is not None and q.stride() != getattr(plan, "strides", _NO_STRIDES)["q"]:
+        _check_strides(plan, "q", q, heads, head_dim)
     if q_out is not None and not q_out.is_contiguous():
         raise ValueError("q_out must be contiguous")
     want = (tokens, cache.kv_heads, cache.head_dim)
@@ -1003,8 +1028,10 @@ def sol_attn3d_cache_append(plan, q: Optional[torch.Tensor], k: torch.Tensor, v:
     for g in (q_gain, k_gain):
         if g is not None and (g.dtype is not torch.float32 or g.get_device() != here or g.numel() != head_dim or not g.is_contiguous()):
             raise ValueError(f"gains must be contiguous float32 tensors of {head_dim} elements on cuda:{here}")
+    ks = _shared_row_strides(k, head_dim)    # (K and V are mostly slices of one tensor)
+    vs = ks if ks is not _DENSE2 and v.stride() == k.stride() else _shared_row_strides(v, head_dim)
     code = _lib().sol_attn3d_cache_append(
-        plan, None if q is None else q.data_ptr(), k.data_ptr(), v.data_ptr(), _shared_row_strides(k, head_dim), _shared_row_strides(v, head_dim),
+        plan, None if q is None else q.data_ptr(), k.data_ptr(), v.data_ptr(), ks, vs,
         None if q_out is None else q_out.data_ptr(), cache.ref, layer, None if streams is None else streams.data_ptr(),
         None if pos0 is None else pos0.data_ptr(), None if q_gain is None else q_gain.data_ptr(),
         None if k_gain is None else k_gain.data_ptr(), eps, _stream(stream))
@@ -1034,6 +1061,8 @@ def sol_attn3d_forward_paged(plan, q: torch.Tensor, cache: sol_attn3d_paged_cach
     n_seqs, heads, head_dim, tokens = _dims(plan)
     _check_bf16(q, out)
     _check_sizes(tokens, heads * head_dim, (q, out), ())
+    _check_strides(plan, "q", q, heads, head_dim)
+    _check_strides(plan, "out", out, heads, head_dim)
     _check_index(streams, n_seqs, "streams")
     width = _check_key_mask(cache, key_mask)
     nbytes = _check_workspace(workspace)
@@ -1079,6 +1108,8 @@ def sol_attn3d_forward_cross(plan, q: torch.Tensor, context: sol_attn3d_context,
     n_seqs, heads, head_dim, tokens = _dims(plan)
     _check_bf16(q, out)
     _check_sizes(tokens, heads * head_dim, (q, out), ())
+    _check_strides(plan, "q", q, heads, head_dim)
+    _check_strides(plan, "out", out, heads, head_dim)
     if context.n != n_seqs:
         raise ValueError(f"{n_seqs} sequences need as many contexts")
     nbytes = _check_workspace(workspace)
