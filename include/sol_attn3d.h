@@ -796,7 +796,10 @@ int sol_attn3d_last_launch_count(sol_attn3d_plan_t plan);
  */
 int sol_attn3d_softmax_rescale_count(sol_attn3d_plan_t plan, unsigned long long* count);
 
-/* cudaError_t of the last failing CUDA call made on behalf of this plan (0 if none). */
+/*
+ * cudaError_t of the last failing CUDA call made on behalf of this plan (0 if none).  NULL: of the last one made by a call that
+ * takes no plan, on the calling thread.
+ */
 int sol_attn3d_last_cuda_error(sol_attn3d_plan_t plan);
 
 /* Static string for an error code. */

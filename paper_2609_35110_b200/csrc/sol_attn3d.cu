@@ -103,6 +103,15 @@ int fail_cuda(sol_attn3d_plan_t p, cudaError_t e) {
   return SOL_ATTN3D_ERR_CUDA;
 }
 
+// The same for a call that has no plan to keep the code in: sol_attn3d_last_cuda_error(NULL) has it, per thread.
+thread_local int planless_cuda = 0;
+int planless_status(cudaError_t e) {
+  if (e == cudaSuccess) return SOL_ATTN3D_OK;
+  planless_cuda = (int)e;
+  (void)cudaGetLastError();
+  return SOL_ATTN3D_ERR_CUDA;
+}
+
 // Streams and events of sol_attn3d_forward_host (host-side objects only).
 void release_host_pipe(sol_attn3d_plan_t p) {
   if (p->s_h2d != nullptr) (void)cudaStreamDestroy(p->s_h2d);
@@ -721,7 +730,7 @@ int sol_attn3d_exchange_pack_qkv(const void* q, const void* k, const void* v, co
   const long long want = (items + 255) / 256;
   const unsigned blocks = (unsigned)std::max<long long>(1, std::min<long long>(want, 148ll * 16));
   sol::exchange_pack_qkv_kernel<<<blocks, 256, 0, static_cast<cudaStream_t>(stream)>>>(a);
-  return cudaGetLastError() == cudaSuccess ? SOL_ATTN3D_OK : SOL_ATTN3D_ERR_CUDA;
+  return planless_status(cudaGetLastError());
 }
 
 int sol_attn3d_exchange_merge_heads(const void* recv, void* out, int64_t n_local, int heads, int record_bytes,
@@ -746,7 +755,7 @@ int sol_attn3d_exchange_merge_heads(const void* recv, void* out, int64_t n_local
   sol::exchange_merge_heads_kernel<<<blocks, 256, 0, static_cast<cudaStream_t>(stream)>>>(
       static_cast<const uint8_t*>(recv), static_cast<uint8_t*>(out), n_local, heads / n_ranks, n_ranks, chunks, ots,
       (int)(ors / 16));
-  return cudaGetLastError() == cudaSuccess ? SOL_ATTN3D_OK : SOL_ATTN3D_ERR_CUDA;
+  return planless_status(cudaGetLastError());
 }
 
 size_t sol_attn3d_exchange_record_bytes(int kind, int head_dim) {
@@ -801,7 +810,7 @@ int launch_quantize(const void* const src[3], const int64_t* const strides[3], i
   const long long n_items = n_rows * n_ranks * group_heads * (long long)(NW * head_dim / 32);   // one thread per group of 32 values
   const unsigned blocks = (unsigned)std::max<long long>(1, std::min<long long>((n_items + 255) / 256, 148ll * 16));
   sol::quantize_records_kernel<NW><<<blocks, 256, 0, st>>>(a);
-  return cudaGetLastError() == cudaSuccess ? SOL_ATTN3D_OK : SOL_ATTN3D_ERR_CUDA;
+  return planless_status(cudaGetLastError());
 }
 }  // namespace
 }  // extern "C++"
@@ -841,7 +850,7 @@ int launch_dequantize(const void* records, void* out, int64_t n_rows, int heads,
   sol::dequantize_records_kernel<NW><<<blocks, 256, 0, st>>>(static_cast<const uint8_t*>(records),
                                                               static_cast<__nv_bfloat16*>(out), n_rows, heads, head_dim,
                                                               (int)rec_bytes);
-  return cudaGetLastError() == cudaSuccess ? SOL_ATTN3D_OK : SOL_ATTN3D_ERR_CUDA;
+  return planless_status(cudaGetLastError());
 }
 }  // namespace
 }  // extern "C++"
@@ -1362,12 +1371,10 @@ int sol_attn3d_diff_step(const void* q, const int64_t q_strides[2], const sol_at
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const unsigned items = (unsigned)batch * (unsigned)a.pairs;
   sol::diff_step_kernel<<<items * (unsigned)a.n_split, sol::kStepThreads, 0, st>>>(a);
-  if (cudaGetLastError() != cudaSuccess) return SOL_ATTN3D_ERR_CUDA;
-  if (a.n_split > 1) {
-    sol::diff_step_join_kernel<<<items, 256, 0, st>>>(a);
-    if (cudaGetLastError() != cudaSuccess) return SOL_ATTN3D_ERR_CUDA;
-  }
-  return SOL_ATTN3D_OK;
+  const int launched = planless_status(cudaGetLastError());
+  if (launched != SOL_ATTN3D_OK || a.n_split == 1) return launched;
+  sol::diff_step_join_kernel<<<items, 256, 0, st>>>(a);
+  return planless_status(cudaGetLastError());
 }
 
 int sol_attn3d_linear_step(const void* q, const void* k, const void* v, void* out, const int64_t q_strides[2],
@@ -1413,7 +1420,7 @@ int sol_attn3d_linear_step(const void* q, const void* k, const void* v, void* ou
   a.n_slots = n_slots;
   if (head_dim == 128) sol::linear_step_kernel<128><<<(unsigned)ctas, 128, 0, static_cast<cudaStream_t>(stream)>>>(a);
   else                 sol::linear_step_kernel<64><<<(unsigned)ctas, 128, 0, static_cast<cudaStream_t>(stream)>>>(a);
-  return cudaGetLastError() == cudaSuccess ? SOL_ATTN3D_OK : SOL_ATTN3D_ERR_CUDA;
+  return planless_status(cudaGetLastError());
 }
 
 extern "C++" {
@@ -1773,7 +1780,7 @@ int sol_attn3d_softmax_rescale_count(sol_attn3d_plan_t p, unsigned long long* co
   return SOL_ATTN3D_OK;
 }
 
-int sol_attn3d_last_cuda_error(sol_attn3d_plan_t p) { return p ? p->last_cuda : 0; }
+int sol_attn3d_last_cuda_error(sol_attn3d_plan_t p) { return p ? p->last_cuda : planless_cuda; }
 
 const char* sol_attn3d_strerror(int code) {
   switch (code) {

@@ -144,7 +144,7 @@ cudaError_t launch_few(const sol::FewArgs& f, int rows, cudaStream_t st, int* la
 
 // Attention of `units` units of few rows; plan or batch as in few_units, no sequence of more than `longest` tokens.
 int attend_few(sol::QueriesDev a, const sol::KeysDev& d, bool paged, int head_dim, long long units, long long longest, long long capacity,
-               void* workspace, size_t workspace_bytes, cudaStream_t st, int* launches, int* cuda_error) {
+               void* workspace, size_t workspace_bytes, cudaStream_t st, int* launches, cudaError_t* cuda_error) {
   sol::FewArgs f{};
   f.a = a;
   f.d = d;
@@ -158,11 +158,9 @@ int attend_few(sol::QueriesDev a, const sol::KeysDev& d, bool paged, int head_di
     f.partial = static_cast<float*>(workspace);
   }
   const int rows = (int)std::min<long long>(sol::kFewRows, longest * a.group);
-  const cudaError_t e = head_dim == 128 ? (paged ? launch_few<128, true>(f, rows, st, launches) : launch_few<128, false>(f, rows, st, launches))
-                                        : (paged ? launch_few<64, true>(f, rows, st, launches) : launch_few<64, false>(f, rows, st, launches));
-  if (e == cudaSuccess) return SOL_ATTN3D_OK;
-  *cuda_error = (int)e;
-  return SOL_ATTN3D_ERR_CUDA;
+  *cuda_error = head_dim == 128 ? (paged ? launch_few<128, true>(f, rows, st, launches) : launch_few<128, false>(f, rows, st, launches))
+                                : (paged ? launch_few<64, true>(f, rows, st, launches) : launch_few<64, false>(f, rows, st, launches));
+  return *cuda_error == cudaSuccess ? SOL_ATTN3D_OK : SOL_ATTN3D_ERR_CUDA;
 }
 
 // ---- attention over a plan's sequences ---------------------------------------------------------------------------------------
@@ -372,8 +370,10 @@ int forward_context(sol_attn3d_plan_t p, const void* q, void* out, const sol::Ke
     for (int i = 0; i < 3; ++i)
       if ((e = cudaEventRecord(p->ev[i], st)) != cudaSuccess) return fail_cuda(p, e);
   }
-  const int rc = r.few ? attend_few(a, d, paged, p->head_dim, r.units, p->sched.front().n_tokens, capacity, workspace, workspace_bytes, st, &p->launches, &p->last_cuda)
+  e = cudaSuccess;
+  const int rc = r.few ? attend_few(a, d, paged, p->head_dim, r.units, p->sched.front().n_tokens, capacity, workspace, workspace_bytes, st, &p->launches, &e)
                        : attend_many(p, a, d, paged, r, workspace, workspace_bytes, st);
+  if (e != cudaSuccess) return fail_cuda(p, e);
   if (rc != SOL_ATTN3D_OK) return rc;
   if (p->prof) {
     if ((e = cudaEventRecord(p->ev[3], st)) != cudaSuccess) return fail_cuda(p, e);
@@ -401,9 +401,11 @@ int step_context(const void* q, const int64_t q_strides[2], const sol::KeysDev& 
   a.n_seqs = batch;
   a.group = heads / d.c.kv_heads;
   a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)head_dim));
-  int launches = 0, cuda_error = 0;
-  return attend_few(a, d, paged, head_dim, few_units(nullptr, batch, a.group), 1, capacity, workspace, workspace_bytes,
-                    static_cast<cudaStream_t>(stream), &launches, &cuda_error);
+  int launches = 0;                                        // (a plan counts them)
+  cudaError_t e = cudaSuccess;
+  const int rc = attend_few(a, d, paged, head_dim, few_units(nullptr, batch, a.group), 1, capacity, workspace, workspace_bytes,
+                            static_cast<cudaStream_t>(stream), &launches, &e);
+  return e != cudaSuccess ? planless_status(e) : rc;
 }
 
 size_t step_bytes(int batch, int heads, int kv_heads, int head_dim, long long capacity) {
@@ -464,7 +466,7 @@ constexpr size_t kBookSmem = sizeof(sol::BookSmem);
 template <typename K>
 int launch_book(K kernel, const sol::BookArgs& b, cudaStream_t st) {
   static_assert(kBookSmem <= 48 * 1024, "what a launch may have without being asked for");
-  return launch_chained(kernel, 1, sol::kBookThreads, kBookSmem, st, b) == cudaSuccess ? SOL_ATTN3D_OK : SOL_ATTN3D_ERR_CUDA;
+  return planless_status(launch_chained(kernel, 1, sol::kBookThreads, kBookSmem, st, b));
 }
 
 template <bool kPages>
@@ -486,7 +488,7 @@ int launch_move(const sol_attn3d_paged_cache* c, sol::MoveArgs m, cudaStream_t s
   m.head_dim = c->head_dim;
   m.n_pages = c->n_pages;
   // the number of rows is on the device: eight resident blocks per SM walk over them
-  return launch_chained(sol::cache_move_kernel<kPages>, 148 * 8, 256, 0, st, m) == cudaSuccess ? SOL_ATTN3D_OK : SOL_ATTN3D_ERR_CUDA;
+  return planless_status(launch_chained(sol::cache_move_kernel<kPages>, 148 * 8, 256, 0, st, m));
 }
 
 }  // namespace
@@ -536,7 +538,7 @@ int sol_attn3d_cache_compact(const sol_attn3d_paged_cache* cache, int n, const i
   b.keep = keep;
   b.keep_stride = keep_width;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (launch_chained(sol::cache_keep_kernel, (unsigned)n, sol::kKeepThreads, 0, st, b) != cudaSuccess) return SOL_ATTN3D_ERR_CUDA;
+  if ((rc = planless_status(launch_chained(sol::cache_keep_kernel, (unsigned)n, sol::kKeepThreads, 0, st, b))) != SOL_ATTN3D_OK) return rc;
   if ((rc = launch_book(sol::cache_compact_kernel, b, st)) != SOL_ATTN3D_OK) return rc;
   sol::MoveArgs m{};
   m.n = n;
