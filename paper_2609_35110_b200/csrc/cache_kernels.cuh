@@ -26,6 +26,8 @@ struct PagedDev {
 
 // Kernels of this family may be launched while their predecessor in the stream still runs (programmatic dependent launch): each waits
 // for it here before it touches memory, and lets its own successor be launched at once, which saves some 3 us between short kernels.
+// Such a kernel lives while its predecessor still writes, so what callers or predecessors write is read by plain loads: __ldg is for memory that
+// nobody writes as long as the kernel lives (here: the plan's tables), and the compiler may move it across the wait.
 __device__ __forceinline__ void chained_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void chained_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
@@ -125,7 +127,7 @@ __global__ void __launch_bounds__(256, 3) cache_append_kernel(const __grid_const
 #pragma unroll
       for (int b = 0; b < kBatch; ++b) {
         const int h = min(h0 + b / kTokens * rows_per_pass, n - 1);
-        ahead[b] = __ldg(reinterpret_cast<const uint4*>(src + (int)((pick >> (8 * (b % kTokens))) & 255u) * x_tok + (long long)h * x_head));
+        ahead[b] = *reinterpret_cast<const uint4*>(src + (int)((pick >> (8 * (b % kTokens))) & 255u) * x_tok + (long long)h * x_head);
       }
     };
     load(0);
@@ -193,8 +195,8 @@ __global__ void __launch_bounds__(256, 3) cache_append_kernel(const __grid_const
       float rinv[kBatch], gains[8];
       const bool norm = which < 2 && a.gain[which & 1] != nullptr;
       if (norm) {
-          *reinterpret_cast<float4*>(&gains[0]) = __ldg(reinterpret_cast<const float4*>(a.gain[which & 1] + chunk * 8));
-          *reinterpret_cast<float4*>(&gains[4]) = __ldg(reinterpret_cast<const float4*>(a.gain[which & 1] + chunk * 8) + 1);
+          *reinterpret_cast<float4*>(&gains[0]) = *reinterpret_cast<const float4*>(a.gain[which & 1] + chunk * 8);
+          *reinterpret_cast<float4*>(&gains[4]) = *(reinterpret_cast<const float4*>(a.gain[which & 1] + chunk * 8) + 1);
           // Sums of squares of the rows, by shuffles over a row's chunks; where they leave fp32's range, once more on scaled values.
           auto squares = [&](float scale, float (&ss)[kBatch]) {
 #pragma unroll

@@ -185,7 +185,7 @@ __global__ void __launch_bounds__(kFewThreads, kFewResident) few_rows_kernel(con
     for (int k = 0; k < D / 16; ++k)
 #pragma unroll
       for (int half = 0; half < 2; ++half)
-        q[k][2 * half + r] = there ? __ldg(reinterpret_cast<const unsigned int*>(src + 16 * k + 8 * half)) : 0u;
+        q[k][2 * half + r] = there ? *reinterpret_cast<const unsigned int*>(src + 16 * k + 8 * half) : 0u;
   }
   const int last_tok = (row0 + n_rows - 1) / p.a.group;
   const int most = key_limit(sp, n_tok, last_tok, p.a.causal);            // limits grow with the token
@@ -214,14 +214,14 @@ __global__ void __launch_bounds__(kFewThreads, kFewResident) few_rows_kernel(con
   auto look_up = [&](int b) {
     if (b >= b_end) return;
     if (kPaged) {
-      page_ahead = __ldg(sp.table + col);
+      page_ahead = sp.table[col];
       row_ahead = in_page;
       col += page_cols;
       in_page += page_rows;
       if (in_page >= page) { in_page -= page; ++col; }
     }
     const int key = b * 16 + (lane & 15);
-    on_ahead = key < most && (sp.mask == nullptr || __ldg(sp.mask + key) != 0);
+    on_ahead = key < most && (sp.mask == nullptr || sp.mask[key] != 0);
   };
   // K of block b into a stage, then V of the same block: two steps, because K's place is free as soon as the scores are computed
   uint32_t v_valid = 0;
@@ -263,8 +263,8 @@ __global__ void __launch_bounds__(kFewThreads, kFewResident) few_rows_kernel(con
   };
   auto fetch_v = [&](int b, int stage) {
     if (b < b_end) {
-      copy_rows(ring + stage * 2 * L::kBlock + L::kBlock + row_first * L::kPitch + chunk * 16, v_next, v_step, v_valid, p.d.c.v);
       look_up(b + kFewWarps);
+      copy_rows(ring + stage * 2 * L::kBlock + L::kBlock + row_first * L::kPitch + chunk * 16, v_next, v_step, v_valid, p.d.c.v);
     }
     cp_async_commit();
   };
@@ -460,7 +460,7 @@ __device__ __forceinline__ float largest_part(const float* stats, long long step
   float top = -CUDART_INF_F;
   bool some = false;
   for (int s = threadIdx.x & 31; s < n_parts; s += 32) {
-    const float4 t = __ldg(reinterpret_cast<const float4*>(stats + s * step));
+    const float4 t = *reinterpret_cast<const float4*>(stats + s * step);
     top = fmaxf(top, t.x);
     some = some || t.z != 0.f;
   }
@@ -480,7 +480,7 @@ __device__ __forceinline__ void sum_parts(const float* mine, long long step, int
   for (int e = 0; e < 8; ++e) acc[e] = 0.f;
   for (int s0 = begin; s0 < end; s0 += 32) {
     float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (s0 + lane < end) t = __ldg(reinterpret_cast<const float4*>(mine + (s0 + lane) * step + D));
+    if (s0 + lane < end) t = *reinterpret_cast<const float4*>(mine + (s0 + lane) * step + D);
     const float weight = t.z == 0.f ? 0.f : t.x == top ? 1.f : ex2_approx((t.x - top) * scale_log2);
     if (t.z != 0.f) sum = fmaf(t.y, weight, sum);
     const unsigned there = __ballot_sync(0xffffffffu, t.z != 0.f);         // (what a part without a valid key holds is not looked at)
@@ -490,7 +490,7 @@ __device__ __forceinline__ void sum_parts(const float* mine, long long step, int
       const float f = __shfl_sync(0xffffffffu, weight, j + team);
       if ((there >> (j + team)) & 1u) {
         const float* v = mine + (s0 + j + team) * step + d0;
-        const float4 a = __ldg(reinterpret_cast<const float4*>(v)), b = __ldg(reinterpret_cast<const float4*>(v + 4));
+        const float4 a = *reinterpret_cast<const float4*>(v), b = *reinterpret_cast<const float4*>(v + 4);
         acc[0] = fmaf(a.x, f, acc[0]); acc[1] = fmaf(a.y, f, acc[1]); acc[2] = fmaf(a.z, f, acc[2]); acc[3] = fmaf(a.w, f, acc[3]);
         acc[4] = fmaf(b.x, f, acc[4]); acc[5] = fmaf(b.y, f, acc[5]); acc[6] = fmaf(b.z, f, acc[6]); acc[7] = fmaf(b.w, f, acc[7]);
       }

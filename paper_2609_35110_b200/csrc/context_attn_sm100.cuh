@@ -256,7 +256,7 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int key = jt * 128 + e * 32 + lane;
-          if (key < cap && __ldg(mask + key) != 0) w |= 1u << e;
+          if (key < cap && mask[key] != 0) w |= 1u << e;
         }
         return w;
       };
@@ -482,7 +482,7 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         auto page_of = [&](int jt) {
           const int key = jt * 128 + lane * p.box_rows;
           if (lane * p.box_rows >= 128 || key >= n) return (int)p.d.c.n_pages;
-          const int page = __ldg(table + key / p.d.c.page);
+          const int page = table[key / p.d.c.page];
           return page >= 0 && page < p.d.c.n_pages ? page : (int)p.d.c.n_pages;
         };
         int next_page = 0;
@@ -867,7 +867,7 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
 #pragma unroll
               for (int e = 0; e < 16; ++e) {
                 const int key = jt * 128 + e * 32 + lane;
-                const bool counts = key < un.span.cap && __ldg(un.span.mask + key) != 0;
+                const bool counts = key < un.span.cap && un.span.mask[key] != 0;
                 on[e >> 2] |= counts;
               }
 #pragma unroll
@@ -911,7 +911,7 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int key = jt * 128 + e * 32 + lane;
-            if (key >= cap || (kMask && __ldg(mask + key) == 0)) drop |= 1u << e;
+            if (key >= cap || (kMask && mask[key] == 0)) drop |= 1u << e;
           }
         }
         if (!mbar_wait_warp(bar_kv_full(stage), (v_it / L::kStages) & 1, limit)) { ok = false; break; }
