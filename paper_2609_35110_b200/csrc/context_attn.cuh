@@ -131,6 +131,21 @@ struct FewArgs {
   float* partial;               // [kv_head][unit][split][16][D + 4], or nullptr: one split
 };
 
+// Which rows unit `unit` of a K/V head holds: entry of the batch, new tokens of it, first (token, head) row, its first token.
+struct FewUnit {
+  int entry, n_tok, row0;
+  long long tok0;
+};
+__device__ __forceinline__ FewUnit find_few_rows(const QueriesDev& a, long long unit) {
+  if (a.seqs != nullptr) {
+    long long first;
+    const SeqDev& sq = a.seqs[find_sequence(a, unit, kFewRows, &first)];
+    return {sq.seq_id, sq.n_tokens, (int)(unit - first) * kFewRows, sq.tok_start};
+  }
+  const int per = (a.group + kFewRows - 1) / kFewRows, entry = (int)(unit / per);
+  return {entry, 1, (int)(unit % per) * kFewRows, entry};
+}
+
 __device__ __forceinline__ void mma_bf16_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
@@ -150,22 +165,7 @@ __global__ void __launch_bounds__(kFewThreads, kFewResident) few_rows_kernel(con
   const long long rest = blockIdx.x / p.n_split;
   const int kv_head = (int)(rest % p.d.c.kv_heads);
   const long long unit = rest / p.d.c.kv_heads;
-  int entry, n_tok, row0;                               // of the batch; new tokens; first (token, head) row
-  long long tok0;
-  if (p.a.seqs != nullptr) {
-    long long first;
-    const SeqDev& sq = p.a.seqs[find_sequence(p.a, unit, kFewRows, &first)];
-    entry = sq.seq_id;
-    n_tok = sq.n_tokens;
-    tok0 = sq.tok_start;
-    row0 = (int)(unit - first) * kFewRows;
-  } else {
-    const int per = (p.a.group + kFewRows - 1) / kFewRows;
-    entry = (int)(unit / per);
-    n_tok = 1;
-    tok0 = entry;
-    row0 = (int)(unit % per) * kFewRows;
-  }
+  const auto [entry, n_tok, row0, tok0] = find_few_rows(p.a, unit);
   const int n_rows = min(kFewRows, n_tok * p.a.group - row0);
   if (n_rows <= 0) return;
   const Span sp = find_span<kPaged>(p.d, entry);
@@ -528,22 +528,7 @@ __global__ void __launch_bounds__(32 * kJoinFewWarps) join_few_kernel(const __gr
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int kv_head = (int)(blockIdx.x / p.units), row = blockIdx.y * (kJoinFewWarps / kWarps) + (kWarps == 1 ? warp : 0);
   const long long unit = blockIdx.x % p.units;
-  int entry, n_tok, row0;
-  long long tok0;
-  if (p.a.seqs != nullptr) {
-    long long first;
-    const SeqDev& sq = p.a.seqs[find_sequence(p.a, unit, kFewRows, &first)];
-    entry = sq.seq_id;
-    n_tok = sq.n_tokens;
-    tok0 = sq.tok_start;
-    row0 = (int)(unit - first) * kFewRows;
-  } else {
-    const int per = (p.a.group + kFewRows - 1) / kFewRows;
-    entry = (int)(unit / per);
-    n_tok = 1;
-    tok0 = entry;
-    row0 = (int)(unit % per) * kFewRows;
-  }
+  const auto [entry, n_tok, row0, tok0] = find_few_rows(p.a, unit);
   if (kPaged) {
     const long long stream = p.d.streams != nullptr ? p.d.streams[entry] : entry;
     if (stream < 0 || stream >= p.d.c.n_streams) return;

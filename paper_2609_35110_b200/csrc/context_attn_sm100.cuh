@@ -409,7 +409,7 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
           tmem_ld32(tO + hf * 64, *reinterpret_cast<uint32_t(*)[32]>(&o[0]));
           tmem_ld32(tO + hf * 64 + 32, *reinterpret_cast<uint32_t(*)[32]>(&o[32]));
           tmem_wait_ld_dep64(o);
-          if (kBoxes && lane == 0) bulk_wait_read();      // the last box has left the staging rows
+          if (kBoxes && lane == 0) bulk_wait_read_all();      // the last box has left the staging rows
           __syncwarp();
 #pragma unroll
           for (int v = 0; v < 8; ++v) {
@@ -427,7 +427,7 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             __syncwarp();
             if (lane == 0) {
               tma_store_3d_hint(&tm_o, sbase + L::kOffStage + warp * 4096, hf * 64, un.kv_head * group, (int)un.tok0 + first_tok + warp_tok, pol_once);
-              bulk_commit();
+              bulk_commit_group();
             }
             continue;
           }
@@ -445,7 +445,7 @@ context_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       }
       release_unit(u);
     }
-    if (kBoxes && lane == 0) bulk_wait();
+    if (kBoxes && lane == 0) bulk_wait_all();
     if (!ok && lane == 0) atomicCAS(p.status, 0u, kStatusTimeoutSoftmax);
   } else {
     setmaxnreg_dec<SOL_REGS_OTHER>();
