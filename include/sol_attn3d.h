@@ -633,7 +633,8 @@ int sol_attn3d_cache_append(sol_attn3d_plan_t plan, const void* q, const void* k
  *   q, out       DEVICE, bf16 [total_tokens, heads, head_dim], the plan's q and out strides, 16-byte aligned; q is rotated.
  *                heads must be a multiple of the cache's kv_heads; head h reads K/V head h / (heads / kv_heads).
  *   key_mask     DEVICE, uint8 [n_streams][mask_width] by token, rows mask_width apart, nonzero = attend; or NULL.  Tokens at or beyond
- *                mask_width do not count.
+ *                mask_width do not count.  Blocks of 128 tokens without one that counts are left out where rows see at most 4,096 tokens;
+ *                in longer streams a mask saves no time (sol_attn3d_cache_compact, with a window's keep list, does).
  *   streams      as in sol_attn3d_cache_append; rows of an idle sequence are left as they were.  Several may name one stream.
  *   workspace    DEVICE, 256-byte aligned, at least sol_attn3d_paged_workspace_bytes(plan, cache) bytes, which may be 0 (then NULL is
  *                fine): results of key ranges that different CTAs handle, written and read by every call.  Calls that may overlap
@@ -641,7 +642,11 @@ int sol_attn3d_cache_append(sol_attn3d_plan_t plan, const void* q, const void* k
  * Rows without a valid key are zeros.  K and V of tokens that are masked, or beyond the stream's length, may be anything
  * (infinities, NaN); those of tokens that some row sees must be finite where a mask or causal_block hides them from another.
  * Deterministic; may be captured; one or two kernels.  The plan's workspace must be bound; time-outs are reported by
- * sol_attn3d_status.
+ * sol_attn3d_status (out is undefined then).
+ * Sequences whose rows of one K/V head (tokens x heads / kv_heads) are at most 16, and any with more than 128 heads per K/V head, are
+ * served 16 such rows at a time by a kernel that reads K and V once for them; the others by tensor-core tiles of 128 rows.  There P is
+ * rounded to bf16 for its product with V, as in sol_attn3d_forward; the first kernel holds it in two bf16 parts.  So the
+ * forms for chunks and for single tokens agree to rounding (relative error 0.0024 and 0.0017), not to the bit.
  * Errors: INVALID_ARG, NO_WORKSPACE, UNSUPPORTED_SHAPE, CUDA.
  */
 size_t sol_attn3d_paged_workspace_bytes(sol_attn3d_plan_t plan, const sol_attn3d_paged_cache* cache);
@@ -651,7 +656,8 @@ int sol_attn3d_forward_paged(sol_attn3d_plan_t plan, const void* q, const sol_at
 
 /*
  * The same for one token per row without a plan: row b of q [batch, heads, head_dim] (element strides {row, head}, {0,0} = dense)
- * is the last token of stream streams[b] (NULL: stream b) and sees all of the stream.  No device-side wait.
+ * is the last token of stream streams[b] (NULL: stream b) and sees all of the stream.  No device-side wait.  Keys are split over CTAs by
+ * the size of the table, not by the lengths: one long stream among very many short ones is read by few of them.
  */
 size_t sol_attn3d_paged_step_workspace_bytes(const sol_attn3d_paged_cache* cache, int batch, int heads);
 int sol_attn3d_paged_step(const void* q, const int64_t q_strides[2], const sol_attn3d_paged_cache* cache, int layer,
@@ -684,8 +690,8 @@ typedef struct {
 } sol_attn3d_context;
 
 /*
- * q, out, workspace, masked values, rows without a key: as for sol_attn3d_forward_paged; q is taken as it is.  The step form takes one
- * row per context, batch of them (begins and lens [batch]).
+ * q, out, workspace, masked values (and key blocks without one that counts), rows without a key, the kernels' arithmetic: as for
+ * sol_attn3d_forward_paged; q is taken as it is.  The step form takes one row per context, batch of them (begins and lens [batch]).
  */
 size_t sol_attn3d_cross_workspace_bytes(sol_attn3d_plan_t plan, const sol_attn3d_context* context);
 int sol_attn3d_forward_cross(sol_attn3d_plan_t plan, const void* q, const sol_attn3d_context* context, void* out,

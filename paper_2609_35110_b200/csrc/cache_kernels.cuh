@@ -40,16 +40,17 @@ __device__ __forceinline__ long long stream_tokens(const PagedDev& c, long long 
 // ---------------------------------------------------------------------------------------------
 // New tokens of a plan's sequences into one layer of a cache: K and (optionally) Q are RMS-normalised per head, rotated by
 // the token's (t, h, w), offset per sequence, and rounded once; V is copied.  Row i of a chunk of n tokens becomes token
-// N - n + i of a stream of N.  Every value is read and written once, 45 us of HBM for 4,680 tokens x 40 heads x 128; it takes 67 us
-// (0.288 GB, 4.3 TB/s): issuing instructions (60 % of the slots) and the barriers around a group's angles bound it.  16 tokens x 40 / 8
-// heads: 6 us on the GPU.
+// N - n + i of a stream of N.  Every value is read and written once, 45 us of HBM for 4,680 tokens x 40 heads x 128; it takes 66 us
+// (0.288 GB, 4.4 TB/s): the barriers around a group's angles, the largest stall, and issuing instructions (63 % of the slots) bound it.
+// 16 tokens x 40 / 8 heads: 6 us on the GPU.
 //
-// A block takes up to four neighbouring tokens at a time.  Its threads first find the angles of the tokens' pairs, one each, and the
-// tokens' places in the cache: the angles from the plan's tables, or, where positions are offset, from position times frequency in
-// fp64, brought to (-pi, pi] there (the tables end with the grid, and fp32 loses far positions).  Then a thread owns 16-byte chunks (8
-// dims) of rows, four rows at a time: the same head of the four tokens (kTokens = 4), or four heads of one (kTokens = 1: few tokens);
-// all Q heads, then all K heads, then V.  A row's address is a base per token and an offset per head (found row by row they made 183
-// instructions per 8 values of a lane: 98 us; every thread finding its own angles: 106 us; one token at a time: 93 us).
+// A block takes up to four neighbouring tokens at a time.  It finds their sequences and streams, and sends for the first rows of those that
+// are not idle.  Then its threads find the angles of the tokens' pairs, one each, and the tokens' places in the cache: the angles from the
+// plan's tables, or, where positions are offset, from position times frequency in fp64, brought to (-pi, pi] there (the tables end
+// with the grid, and fp32 loses far positions).  Then a thread owns 16-byte chunks (8 dims) of rows, four rows at a time: the same head of
+// the four tokens (kTokens = 4), or four heads of one (kTokens = 1: few tokens); all Q heads, then all K heads, then V.  A row's address
+// is a base per token and an offset per head (found row by row they made 183 instructions per 8 values of a lane: 98 us; every thread
+// finding its own angles: 106 us; one token at a time: 93 us).
 // ---------------------------------------------------------------------------------------------
 struct AppendArgs {
   const __nv_bfloat16* x[3];    // q, k, v of the new tokens (q may be nullptr)
@@ -639,7 +640,7 @@ __global__ void __launch_bounds__(kBookThreads) cache_compact_kernel(const BookA
 
 // ---------------------------------------------------------------------------------------------
 // Copies rows from page to page, in all layers, K and V.  Bound by HBM: 98 us for 0.624 GB read and written (4 streams, up to
-// 3,120 rows each, 8 layers x 8 heads x 128), 6.4 TB/s.  A warp takes one row of one layer: its K and V (kv_heads * head_dim values
+// 3,120 rows each, 8 layers x 8 heads x 128), 6.4 TB/s; 400 whole pages of 64 tokens, 1.68 GB: 264 us, as much.  A warp takes one row of one layer: its K and V (kv_heads * head_dim values
 // each) in 16-byte chunks, eight loads in flight.
 // ---------------------------------------------------------------------------------------------
 struct MoveArgs {

@@ -89,8 +89,10 @@ __device__ __forceinline__ int find_sequence(const QueriesDev& a, long long unit
 
 // ---------------------------------------------------------------------------------------------
 // Few query rows per K/V head (one token per stream, its heads that share the K/V head; a small chunk).  Bound by reading K and V
-// once, and close behind by instructions (576 per warp and 16 keys): 24 streams of 77 to 12,736 tokens, 40 / 8 heads x 128,
-// masked, 0.567 GB: 109 us (5.2 TB/s; the loads alone 105), and 5 for the join; 24 rows x 40 heads x 128 against 77 to 491 states, 0.140 GB: 31 us.
+// once, of which latency leaves a fifth: 24 streams of 77 to 12,736 tokens, 40 / 8 heads x 128, masked, 0.567 GB: 108 us with the join in
+// ten calls after a pause, 114 to 120 in a run (4.9 TB/s; 88 at the copy bandwidth); 12 warps per SM with two blocks of 16 keys in flight
+// use 40 % of the issue slots (530 instructions per block), and wait for K and V as long as for their own instructions.  24 rows x 40 heads x 128 against 77 to 491 states,
+// 0.140 GB: 31 us.
 // A unit is up to 16 rows, the height of an mma.sync tile (m16n8k16); a CTA of four warps takes a unit and a range of
 // keys, a warp 16 keys at a time.  The tensor core is there for the grouped heads: on the FMA pipes 16 rows would cost 16 x
 // 256 operations per key and bind long before HBM does; a tcgen05 tile has 128 rows, of which 16 or fewer would be filled, and
@@ -205,8 +207,9 @@ __global__ void __launch_bounds__(kFewThreads, kFewResident) few_rows_kernel(con
   const __nv_bfloat16* kh = p.d.c.k + kv_head * p.d.c.ks[2] + chunk * 8;
   const __nv_bfloat16* vh = p.d.c.v + kv_head * p.d.c.vs[2] + chunk * 8;
   const long long k_step = kRowStep * p.d.c.ks[1], v_step = kRowStep * p.d.c.vs[1];
-  // What a block needs before its loads can start is fetched a turn earlier: its page, and the mask's word on its keys.  Its place among
-  // the pages moves with it (four blocks a turn), without a division.
+  // What a block needs before its loads can start is fetched a turn earlier, ahead of V of the turn's block (behind it: 24 streams 122 us
+  // instead of 116): its page, and the mask's word on its keys.  Its place among the pages moves with it (four blocks a turn), without a
+  // division.
   const int page = kPaged ? p.d.c.page : 1, page_cols = 16 * kFewWarps / page, page_rows = 16 * kFewWarps % page;
   int col = kPaged ? b_first * 16 / page : 0, in_page = kPaged ? b_first * 16 % page : 0;
   int page_ahead = 0, row_ahead = 0;

@@ -17,11 +17,16 @@
 //   warp 11         values of keys that do not count become zeros in shared memory (0 * NaN would not be 0)
 // Tensor memory: S0 | S1 | O0 | O1 as in attn_fwd_sm100.cuh.
 //
-// What bounds it is the chain scores -> softmax -> P -> product of two tiles in turn: 3,650 cycles per 128 keys, as in the dense kernel;
-// the tensor pipe works 40 to 55 % of that, the exponentials as much.  4,680 rows x 40 heads x 128 over 25,216 keys: 2.0 ms (1.2
-// PFLOP/s) in a short run, 2.3 in a long one (1 kW); 60 tokens x 40 / 8 heads over 111,856 keys: 209 to 230 us; 25,216 rows x 40 heads over 512
-// states: 271 to 314 us, of which some 5,000 cycles per unit and four key tiles are its start and end.  No gain: packed pairs of fp32
-// operations, a polynomial for an eighth to a third of the exponentials (2 to 5 % slower), one MMA issuer per tile (a quarter slower).
+// Rounding: S, the running sums and O are fp32; P is rounded to bf16, the type of V, for its product (half a step of every term: 0.0023
+// relative error against 0.0017 of the output's own rounding).  A second bf16 part of P, as in few_rows_kernel, would be another
+// product per key tile and twice P's way through tensor memory, on the chain that bounds the kernel.
+//
+// What bounds it is that chain, scores -> softmax -> P -> product of two tiles in turn: 3,650 cycles per 128 keys, as in the dense kernel;
+// the tensor pipe works 40 to 55 % of that, the exponentials as much.  In ten calls after a pause, and in a run of seconds (clocks under
+// the 1 kW cap): 4,680 rows x 40 heads x 128 over 25,216 keys 1.94 ms (1.25 PFLOP/s) and 2.25 to 2.33; 60 tokens x 40 / 8 heads over
+// 111,856 keys 208 us and 231 to 238 (the second tile's place is empty in half of the units); 25,216 rows x 40 heads over 512 states 269
+// and 311 to 322, of which some 5,000 cycles per unit and four key tiles are its start and end, of both tiles at the same time.  No gain: packed pairs of
+// fp32 operations, a polynomial for an eighth to a third of the exponentials (2 to 5 % slower), one MMA issuer per tile (a quarter slower).
 #pragma once
 #include "attn_fwd_sm100.cuh"
 #include "context_attn.cuh"
